@@ -45,7 +45,10 @@ typedef enum {
   JD_ERR_ALLOC = 4,       /* device or host allocation failed */
   JD_ERR_CUDA = 5,        /* a CUDA runtime or driver call failed */
   JD_ERR_TIMEOUT = 6,     /* device status: a bounded wait inside a kernel ran out */
-  JD_ERR_BAD_TOKEN = 7    /* device status: a draft token was outside [0, V) and was clamped */
+  JD_ERR_BAD_TOKEN = 7,   /* device status: a draft token was outside [0, V) and was clamped */
+  JD_ERR_PAGES = 8,       /* device status: a cache has too few free pages, or a sequence too many; nothing was reserved */
+  JD_ERR_BAD_INDEX = 9    /* device status: a slot, page, node or length of a cache call was out of range, named twice or
+                             not held; that entry was skipped */
 } jd_status_t;
 
 /* Storage type of the head. F32 / BF16: W, H and w_judge all have that type. FP8_E4M3: W holds
@@ -282,6 +285,210 @@ jd_status_t jd_check_workspace_guards(jd_handle_t h, int32_t* damaged);
  * stream or thread, race with each other, so order them. Asynchronous on `cuda_stream`. */
 jd_status_t jd_verify_static(int32_t d, int32_t V, const void* W, const void* w_judge, float b_judge,
                              const jd_verify_args_t* args, uint32_t* device_status, void* cuda_stream);
+
+/* =========================================================================================
+ * Around the verification call: rotary positions, a paged key / value cache and the attention
+ * of a drafted block over it. One decoding step of a target layer stack is
+ *
+ *   jd_cache_reserve   pages for the block's T nodes            (once a step)
+ *   jd_cache_append    rotate q and k, write k and v            (every layer)
+ *   jd_cache_attend    attention over context + visible nodes   (every layer)
+ *   jd_verify          accept_len, next_token                   (once a step)
+ *   jd_cache_commit    keep the accepted nodes' rows, drop the others, advance the lengths
+ *
+ * Lengths, page tables and accept_len stay on the device throughout: no call of a step waits for
+ * the host, and a whole step can be captured in a CUDA graph. A block is what Sec. 3.1 forwards in
+ * parallel: node 0 is the last context token, nodes 1..T-1 are draft tokens, in a chain or in a
+ * tree (a node's number is larger than its parent's).
+ * ========================================================================================= */
+
+/* Which elements of a head turn together. HALF: i with i + rot_dim / 2; INTERLEAVED: 2 i with 2 i + 1. */
+typedef enum { JD_ROPE_HALF = 0, JD_ROPE_INTERLEAVED = 1 } jd_rope_layout_t;
+
+/* How the frequencies base^(-2 i / rot_dim) are changed for contexts longer than the model was trained on.
+ * LINEAR: divided by `factor`.
+ * BANDS:  by wavelength: those shorter than original_len / high are kept, those longer than
+ *         original_len / low divided by `factor`, and linearly blended in between (in turns per
+ *         original_len).
+ * YARN:   the same blend along the index i, between the indices whose frequencies make `high` and
+ *         `low` turns in original_len (rounded down and up), and the outputs are multiplied by
+ *         0.1 ln(factor) + 1. */
+typedef enum { JD_ROPE_SCALE_NONE = 0, JD_ROPE_SCALE_LINEAR = 1, JD_ROPE_SCALE_BANDS = 2, JD_ROPE_SCALE_YARN = 3 } jd_rope_scaling_t;
+
+/* HOST helper: writes the rot_dim / 2 frequencies (HOST array) and the amplitude (HOST, may be NULL).
+ * rot_dim even, 2..256; base > 1; factor >= 1, original_len >= 1 and 0 < low < high where the scaling uses them. */
+jd_status_t jd_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, double original_len,
+                                double low, double high, float* inv_freq, float* amplitude);
+
+typedef struct {
+  const float* inv_freq;   /* [rot_dim / 2] radians per position, 4-byte aligned */
+  int32_t rot_dim;         /* elements of a head that turn, even, 2..min(head_dim, 256); the rest pass through */
+  int32_t layout;          /* jd_rope_layout_t */
+  float amplitude;         /* factor on the turned elements, 1 without scaling; finite */
+} jd_rope_t;
+
+typedef struct {
+  int64_t tokens;          /* >= 0; 0 launches nothing */
+  int32_t heads, head_dim; /* >= 1; head_dim 1..256 */
+  int32_t dtype;           /* JD_DTYPE_F32 or JD_DTYPE_BF16 */
+  int32_t inverse;         /* 1: turn by the negative angle. The map is linear and this is its transpose:
+                              with the output's gradient as x it returns the input's gradient. */
+  const void* x;           /* [tokens][heads][head_dim], x_stride elements between tokens (0: dense) */
+  void* out;               /* same shape, out_stride elements between tokens (0: dense). out == x with the same
+                              stride turns in place; any other overlap is undefined */
+  int64_t x_stride, out_stride;
+  const int32_t* positions;  /* [tokens], any int32 */
+  jd_rope_t rope;
+} jd_rope_args_t;
+
+/* Rotary positions: (a, b) -> amplitude (a cos t - b sin t, b cos t + a sin t) with t = position x inv_freq,
+ * for every token and head. The angle is formed and reduced in float64, so that far positions lose nothing;
+ * the products are float32, rounded once. Asynchronous on the stream; uses the current device. */
+jd_status_t jd_rope(const jd_rope_args_t* args, void* cuda_stream);
+
+/* ---------------------------------------------------------------- paged cache */
+
+typedef struct {
+  int32_t num_layers;   /* >= 1 */
+  int32_t num_pages;    /* pages of a layer's pool, >= 1 */
+  int32_t page_size;    /* tokens of a page: a power of two, 8..1024 */
+  int32_t q_heads;      /* a multiple of kv_heads */
+  int32_t kv_heads;
+  int32_t head_dim;     /* a multiple of 8, 8..256 */
+  int32_t max_seqs;     /* slots for sequences */
+  int32_t max_pages;    /* page-table entries of a slot; max_pages * page_size <= 2^24 */
+  int32_t max_nodes;    /* largest block, 1..128 */
+  int32_t dtype;        /* JD_DTYPE_F32 or JD_DTYPE_BF16: K, V, q and outputs */
+  int32_t device;       /* CUDA device ordinal that every buffer lives on */
+} jd_cache_config_t;
+
+/* DEVICE buffers, all owned by the caller and borrowed until jd_cache_destroy. A new cache starts from
+ * page_table = -1, seq_len = held = refs = 0, every free_bits bit of a page = 1 and the bits behind the last page = 0,
+ * and a workspace of zeroes. The calls below keep them; between calls a caller may read them, in stream order. */
+typedef struct {
+  void* k_pages;        /* [num_layers][num_pages][kv_heads][page_size][head_dim], 16-byte aligned */
+  void* v_pages;        /* same */
+  int32_t* page_table;  /* [max_seqs][max_pages] page numbers, -1 where none */
+  int32_t* seq_len;     /* [max_seqs] committed tokens */
+  int32_t* held;        /* [max_seqs] leading page-table entries in use */
+  int32_t* refs;        /* [num_pages] sequences that hold the page, 0 = free */
+  uint32_t* free_bits;  /* [ceil(num_pages / 32)] bit p % 32 of word p / 32: page p is free */
+  void* workspace;      /* zero-filled, 256-byte aligned, jd_cache_workspace_bytes() */
+  size_t workspace_bytes;
+} jd_cache_buffers_t;
+
+typedef struct jd_cache_s* jd_cache_t;
+
+/* Bytes of workspace a cache of this configuration needs, 0 for an invalid one. */
+size_t jd_cache_workspace_bytes(const jd_cache_config_t* cfg);
+
+/* Creates a handle: host memory and tensor maps only, no device allocation and nothing enqueued. Calls on one
+ * handle share its workspace and must be ordered on the device (one stream, or explicit dependencies); graphs
+ * captured from one handle must not run at the same time. Streams that attend at the same time take two handles
+ * on the same buffers, each with a workspace of its own; calls that change the cache are always ordered. */
+jd_status_t jd_cache_create(jd_cache_t* out, const jd_cache_config_t* cfg, const jd_cache_buffers_t* buffers);
+jd_status_t jd_cache_destroy(jd_cache_t c);   /* frees host memory only; NULL is accepted */
+
+/* Slots: every call below takes B sequences, 1..min(max_seqs, 1024), and `slots` [B] (device) with the slot of
+ * each, or NULL for slots 0..B-1. Entry -1 marks a padding sequence: skipped, its outputs are left as they were.
+ * Other slots outside [0, max_seqs) are skipped and reported. jd_cache_attend may name a slot several times; in the
+ * calls that change the cache the first naming counts, later ones are skipped and reported. */
+
+/* Makes room for n more tokens (1..) of every sequence: pages for [seq_len, seq_len + n), the lowest free ones, in the
+ * sequences' order; and where the page that holds token seq_len has rows in use and other owners, a copy of those
+ * rows in a page of the sequence's own (all layers). A sequence named later in the call counts as owner until its turn,
+ * so that the last one keeps the page. All or nothing: if pages are short, or a table is, nothing changes and
+ * JD_ERR_PAGES is reported. Reserve before append, and fork only between commit and append. */
+jd_status_t jd_cache_reserve(jd_cache_t c, int32_t B, const int32_t* slots, int32_t n, void* cuda_stream);
+
+/* The block of drafted tokens of a step. */
+typedef struct {
+  int32_t nodes;              /* T, 1..max_nodes */
+  int32_t per_seq;            /* 0: one mask and depth for all sequences, 1: one for each */
+  const uint32_t* mask;       /* [T][W] or [B][T][W], W = ceil(T / 32): bit j % 32 of word j / 32 of row i: node i sees
+                                 node j (its own bit included). NULL: a chain, node i sees 0..i. Bits >= T are ignored */
+  const int32_t* depth;       /* [T] or [B][T] tokens between the context's end and the node: position = seq_len + depth.
+                                 NULL: depth = node number */
+  const int32_t* num_nodes;   /* [B] nodes of each sequence, 0..T (clamped), or NULL: T. Rows behind them are neither
+                                 read nor written, in no output */
+} jd_tree_t;
+
+typedef struct {
+  int32_t B, layer;
+  const int32_t* slots;
+  jd_tree_t tree;
+  const void* k;              /* [B][T][kv_heads][head_dim], k_stride elements between tokens (0: dense) */
+  const void* v;              /* same, v_stride */
+  const void* q;              /* [B][T][q_heads][head_dim], q_stride; NULL: no queries */
+  void* q_out;                /* same shape, q_out_stride; may be q itself with the same stride */
+  int64_t k_stride, v_stride, q_stride, q_out_stride;
+  const jd_rope_t* rope;      /* HOST struct; NULL: keys and queries as they are */
+} jd_append_args_t;
+
+/* Writes keys (turned to their positions) and values of a block behind the sequences' tokens, node j at token
+ * seq_len + j, and the turned queries to q_out. seq_len stays. Rows whose page is missing or has other owners are
+ * skipped and reported (jd_cache_reserve has to come first). Pointers 16-byte aligned, strides multiples of 16 bytes. */
+jd_status_t jd_cache_append(jd_cache_t c, const jd_append_args_t* args, void* cuda_stream);
+
+/* Kernel family of jd_cache_attend. TENSOR: tcgen05 kernel, bf16 with head_dim 64 or 128. SIMT: any cache. */
+typedef enum { JD_ATTEND_AUTO = 0, JD_ATTEND_SIMT = 1, JD_ATTEND_TENSOR = 2 } jd_attend_variant_t;
+
+typedef struct {
+  int32_t B, layer;
+  const int32_t* slots;
+  jd_tree_t tree;             /* depth is not read */
+  const void* q;              /* [B][T][q_heads][head_dim], q_stride elements between tokens (0: dense); head h reads
+                                 kv head h / (q_heads / kv_heads) */
+  void* out;                  /* same shape and type, out_stride; not q */
+  int64_t q_stride, out_stride;
+  float* lse;                 /* [B][T][q_heads] log sum exp of the scaled scores, or NULL */
+  float scale;                /* on q . k, finite */
+  int32_t variant;            /* jd_attend_variant_t */
+} jd_attend_args_t;
+
+/* Attention of a block's nodes over the sequence's seq_len cached tokens and the nodes they may see:
+ * out = softmax(scale q k^T) v, statistics and sums in float32; the bf16 kernel rounds the softmax weights to
+ * bf16 in front of their product with v. A row that sees nothing gets out = 0 and lse = -inf. Whatever stands
+ * in rows that a node may not see (infinities and NaN too) stays without effect on it. Pointers 16-byte aligned,
+ * strides multiples of 16 bytes. */
+jd_status_t jd_cache_attend(jd_cache_t c, const jd_attend_args_t* args, void* cuda_stream);
+
+typedef struct {
+  int32_t B;
+  const int32_t* slots;
+  const int32_t* accept_len;  /* [B][num_paths] accepted draft tokens, as jd_verify writes them */
+  int32_t num_paths;          /* >= 1 candidate paths of every sequence; the one with the largest accept_len is kept, the
+                                 first of equals. (With several, verify by JD_RULE_TOPK: under the sampling rule the pick
+                                 would bias the tokens.) */
+  int32_t path_len;           /* entries of a path, 0..max_nodes - 1 */
+  const int32_t* paths;       /* [B][num_paths][path_len] nodes of the draft tokens along the path, rising; NULL:
+                                 nodes 1, 2, .. (path_len then bounds accept_len; use T - 1) */
+  int32_t* chosen;            /* [B] the kept path, or NULL */
+} jd_commit_args_t;
+
+/* Ends a step: node 0 and the first accept_len nodes of the kept path become the sequence's next tokens. Their rows
+ * are moved together in all layers, seq_len grows by accept_len + 1 and the pages behind are released. accept_len is
+ * clamped to 0..path_len; where a path does not rise, or reaches max_nodes or a row that the sequence does not hold, it is
+ * cut there and reported. */
+jd_status_t jd_cache_commit(jd_cache_t c, const jd_commit_args_t* args, void* cuda_stream);
+
+/* dst[i] becomes a copy of src[i] (device arrays [n], n <= 1024) that shares its pages; jd_cache_reserve gives each its
+ * own where they part. dst must be empty, named once and no source of the same call, else it is skipped and reported;
+ * entries with src or dst -1 are padding. */
+jd_status_t jd_cache_fork(jd_cache_t c, int32_t n, const int32_t* src, const int32_t* dst, void* cuda_stream);
+
+/* Cuts the sequences to length[b] tokens (device [B]; NULL: 0, which frees them) and releases the pages behind, uncommitted
+ * ones too. A length outside 0..seq_len is skipped and reported. */
+jd_status_t jd_cache_truncate(jd_cache_t c, int32_t B, const int32_t* slots, const int32_t* length, void* cuda_stream);
+
+/* Moves the pages in use to the lowest numbers, in all layers, so that the first `used` pages hold everything and the rest
+ * of the pool can go: the highest pages in use fill the lowest free ones, the k-th of those moved into the k-th of those
+ * free, both counted from below. Page numbers change; sequences do not. used: device pointer to one int32, or NULL. */
+jd_status_t jd_cache_compact(jd_cache_t c, int32_t* used, void* cuda_stream);
+
+/* Synchronises the stream of the cache's last call and returns and clears the device status: *out = JD_OK, JD_ERR_PAGES,
+ * JD_ERR_BAD_INDEX or JD_ERR_TIMEOUT, the first since the last query. Not during a capture. */
+jd_status_t jd_cache_last_status(jd_cache_t c, int* out);
 
 #ifdef __cplusplus
 }

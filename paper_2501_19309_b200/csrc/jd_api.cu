@@ -233,6 +233,8 @@ const char* jd_status_string(jd_status_t s) {
     case JD_ERR_CUDA: return "CUDA call failed";
     case JD_ERR_TIMEOUT: return "a bounded device-side wait ran out";
     case JD_ERR_BAD_TOKEN: return "a draft token was outside the vocabulary and was clamped";
+    case JD_ERR_PAGES: return "too few free pages, or page-table entries, for a reserve";
+    case JD_ERR_BAD_INDEX: return "a slot, page, node or length of a cache call was out of range, repeated or not held";
   }
   return "unknown status";
 }

@@ -1,0 +1,337 @@
+// Attention of a drafted block over the paged cache on CUDA cores: any type and head width, float32 throughout; and the
+// kernel that joins the partial results of split sequences, which the tensor-core variant shares.
+//
+// A CTA takes 16 query rows of a (sequence, kv head) - a row is a node and one of the query heads that share the kv
+// head - and walks its run of tiles of 64 cached tokens (jd_cache.h says how runs are cut). Per tile: K and V to shared
+// memory, 16 x 64 scores by 256 threads (four rows of one token each), running maximum and sum by a warp for two rows,
+// and the weighted sum of V with every warp taking an eighth of the tokens for all 16 rows and up to 256 columns in
+// registers, so that one shared-memory read of V serves 16 rows. The warps' sums meet once per segment. For float32 the
+// product with the shared-memory operands bounds it (about twice the HBM time of a tile at two CTAs per SM).
+#include <algorithm>
+#include <cmath>
+
+#include "jd_cache.h"
+#include "jd_sm100_ptx.cuh"
+
+namespace jd {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTile = 1 << kSimtTileShift;
+constexpr int kRows = kSimtRows;
+constexpr int kScorePad = 20;     // floats between tokens of the score buffer: 16 rows + padding, 16-byte aligned
+
+template <typename T> __device__ __forceinline__ void load4(const T* p, float* v);
+template <> __device__ __forceinline__ void load4<float>(const float* p, float* v) {
+  const float4 a = *reinterpret_cast<const float4*>(p);
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+}
+template <> __device__ __forceinline__ void load4<__nv_bfloat16>(const __nv_bfloat16* p, float* v) {
+  const uint2 a = *reinterpret_cast<const uint2*>(p);
+  v[0] = __uint_as_float(a.x << 16); v[1] = __uint_as_float(a.x & 0xFFFF0000u);
+  v[2] = __uint_as_float(a.y << 16); v[3] = __uint_as_float(a.y & 0xFFFF0000u);
+}
+__device__ __forceinline__ void store4(float* p, const float* v) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, const float* v) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]), b = __floats2bfloat162_rn(v[2], v[3]);
+  *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+
+__host__ __device__ constexpr int pitch_of(int head_dim) { return head_dim + 4; }   // floats; keeps 16-byte accesses off one bank group
+
+size_t simt_smem(int head_dim) {
+  return sizeof(float) * ((size_t)2 * kTile * pitch_of(head_dim) + kRows * head_dim + kTile * kScorePad);
+}
+
+// kCols: groups of 128 columns that a lane's accumulators cover (head_dim <= 128 kCols)
+template <typename T, int kCols>
+__global__ void __launch_bounds__(kThreads) attend_simt_kernel(AttendParams p) {
+  extern __shared__ __align__(16) float smem[];
+  __shared__ int prefix[kMaxCacheBatch + 1], warp_sums[kThreads / 32], pages[kTile / 8];
+  __shared__ float s_m[kRows], s_l[kRows], s_fac[kRows];
+  __shared__ uint32_t s_mask[kRows][kMaxNodes / 32];
+  const int D = p.c.head_dim, pitch = pitch_of(D);
+  float* sK = smem;
+  float* sV = sK + kTile * pitch;
+  float* sQ = sV + kTile * pitch;
+  float* sS = sQ + kRows * D;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int g = blockIdx.x / p.row_blocks, rb = blockIdx.x - g * p.row_blocks;
+  const int r0 = rb * kRows, nrows = min(kRows, p.rows - r0);
+  tile_prefix(p, prefix, warp_sums);
+  pdl_trigger();
+  const int64_t units = (int64_t)prefix[p.B] * p.c.kv_heads;
+  if (units == 0) return;
+  const int64_t run0 = run_start(units, p.groups, g), run1 = run_start(units, p.groups, g + 1);
+  const T* kbase = reinterpret_cast<const T*>(p.c.k);
+  const T* vbase = reinterpret_cast<const T*>(p.c.v);
+
+  for (int64_t u = run0; u < run1;) {
+    const int b = seq_of_unit(prefix, p.B, p.c.kv_heads, u);
+    const int tiles = prefix[b + 1] - prefix[b];
+    const int64_t in_seq = u - (int64_t)prefix[b] * p.c.kv_heads;
+    const int head = (int)(in_seq / tiles), tile0 = (int)(in_seq - (int64_t)head * tiles);
+    const int ntiles = (int)min((int64_t)(tiles - tile0), run1 - u);
+    const SeqExtent ex = seq_extent(p, b);
+
+    __syncthreads();   // the previous segment's buffers are free
+    for (int i = tid; i < kRows * (D / 4); i += kThreads) {
+      const int r = i / (D / 4), d = (i - r * (D / 4)) * 4;
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
+      const int t = (r0 + r) / p.group, gq = (r0 + r) - t * p.group;
+      if (r < nrows && t < ex.nodes)
+        load4<T>(reinterpret_cast<const T*>(p.q + ((int64_t)b * p.T + t) * p.q_stride) + (int64_t)(head * p.group + gq) * D + d, v);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sQ[r * D + d + k] = v[k];
+    }
+    if (tid < kRows) { s_m[tid] = -INFINITY; s_l[tid] = 0.f; }
+    for (int i = tid; i < kRows * p.W; i += kThreads) {
+      const int r = i / p.W, w = i - r * p.W, t = (r0 + r) / p.group;
+      s_mask[r][w] = r < nrows && t < ex.nodes ? node_word(p, b, t, w, ex.nodes) : 0u;
+    }
+    float acc[kRows][4 * kCols];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+#pragma unroll
+      for (int k = 0; k < 4 * kCols; ++k) acc[r][k] = 0.f;
+
+    for (int tile = tile0; tile < tile0 + ntiles; ++tile) {
+      const int kv0 = tile * kTile, nkv = max(0, min(kTile, ex.kv_end - kv0));
+      __syncthreads();   // the previous tile's buffers are free
+      if (tid < kTile >> min(p.c.page_shift, kSimtTileShift)) {
+        const int at = (kv0 >> p.c.page_shift) + tid;
+        int page = (at << p.c.page_shift) < ex.kv_end ? __ldg(p.c.table + (int64_t)ex.slot * p.c.max_pages + at) : 0;
+        if (page < 0 || page >= p.c.pages) { set_status(p.c.status, JD_ERR_BAD_INDEX); page = 0; }
+        pages[tid] = page;
+      }
+      __syncthreads();
+      const int vec = D / 4;
+      for (int i = tid; i < kTile * vec; i += kThreads) {
+        const int r = i / vec, d = (i - r * vec) * 4;
+        float kx[4] = {0.f, 0.f, 0.f, 0.f}, vx[4] = {0.f, 0.f, 0.f, 0.f};
+        if (r < nkv) {   // rows behind the sequence may hold anything: they become zeroes here
+          const int kv = kv0 + r;
+          const int page = pages[(kv >> p.c.page_shift) - (kv0 >> p.c.page_shift)];
+          const int64_t off = page_row(p.c, p.layer, page, head, kv & (p.c.page_size - 1)) * D + d;
+          load4<T>(kbase + off, kx);
+          load4<T>(vbase + off, vx);
+        }
+        store4(sK + r * pitch + d, kx);
+        store4(sV + r * pitch + d, vx);
+      }
+      __syncthreads();
+      {   // scores: token tid % 64, rows 4 (tid / 64) ..
+        const int kv = tid & (kTile - 1), rg = (tid >> kSimtTileShift) * 4;
+        float s[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int d = 0; d < D; d += 4) {
+          const float4 x = *reinterpret_cast<const float4*>(sK + kv * pitch + d);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float4 y = *reinterpret_cast<const float4*>(sQ + (rg + r) * D + d);
+            s[r] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s[r]))));
+          }
+        }
+        const int node = kv0 + kv - ex.ctx;   // < 0: context
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const bool see = kv < nkv && (node < 0 || ((s_mask[rg + r][node >> 5] >> (node & 31)) & 1u));
+          s[r] = see ? s[r] * p.scale_log2 : -INFINITY;
+        }
+        store4(sS + kv * kScorePad + rg, s);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < kRows / 8; ++k) {   // statistics: a warp for two rows
+        const int r = warp * (kRows / 8) + k;
+        float* a = sS + lane * kScorePad + r;
+        float* c = sS + (lane + 32) * kScorePad + r;
+        const float x = *a, y = *c;
+        float m = fmaxf(x, y);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        const float before = s_m[r], now = fmaxf(before, m);
+        const float base = now == -INFINITY ? 0.f : now;   // nothing seen yet: every weight is exp2(-inf) = 0
+        const float px = exp2f(x - base), py = exp2f(y - base);
+        float l = px + py;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        *a = px;
+        *c = py;
+        __syncwarp();
+        if (lane == 0) {
+          const float fac = exp2f(before - base);
+          s_fac[r] = fac;
+          s_l[r] = s_l[r] * fac + l;
+          s_m[r] = now;
+        }
+      }
+      __syncthreads();
+      {   // weighted sum of V: this warp's tokens, all rows, columns 4 lane + 128 j. A row that must not see a token
+          // has weight 0 for it, but 0 x inf is not 0: where a token's values are not finite, such rows skip it.
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+          const float f = s_fac[r];
+#pragma unroll
+          for (int k = 0; k < 4 * kCols; ++k) acc[r][k] *= f;
+        }
+        for (int i = 0; i < kTile / 8; ++i) {
+          const int kv = warp * (kTile / 8) + i;
+          if (kv >= nkv) break;
+          float w[kRows];
+#pragma unroll
+          for (int r = 0; r < kRows; r += 4) {
+            const float4 x = *reinterpret_cast<const float4*>(sS + kv * kScorePad + r);
+            w[r] = x.x; w[r + 1] = x.y; w[r + 2] = x.z; w[r + 3] = x.w;
+          }
+          const int node = kv0 + kv - ex.ctx;
+#pragma unroll
+          for (int j = 0; j < kCols; ++j) {
+            const int d = lane * 4 + 128 * j;
+            if (d >= D) continue;
+            const float4 x = *reinterpret_cast<const float4*>(sV + kv * pitch + d);
+            const bool plain = node < 0 || (isfinite(x.x) && isfinite(x.y) && isfinite(x.z) && isfinite(x.w));
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+              if (plain || ((s_mask[r][node >> 5] >> (node & 31)) & 1u)) {
+                acc[r][4 * j] = fmaf(w[r], x.x, acc[r][4 * j]);
+                acc[r][4 * j + 1] = fmaf(w[r], x.y, acc[r][4 * j + 1]);
+                acc[r][4 * j + 2] = fmaf(w[r], x.z, acc[r][4 * j + 2]);
+                acc[r][4 * j + 3] = fmaf(w[r], x.w, acc[r][4 * j + 3]);
+              }
+            }
+          }
+        }
+      }
+    }
+
+    // the warps' sums, one after the other, in the K buffer
+    for (int w = 0; w < kThreads / 32; ++w) {
+      __syncthreads();
+      if (warp == w) {
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+#pragma unroll
+          for (int j = 0; j < kCols; ++j) {
+            const int d = lane * 4 + 128 * j;
+            if (d >= D) continue;
+            float4* o = reinterpret_cast<float4*>(sK + r * pitch + d);
+            float4 x = w == 0 ? make_float4(0.f, 0.f, 0.f, 0.f) : *o;
+            x.x += acc[r][4 * j]; x.y += acc[r][4 * j + 1]; x.z += acc[r][4 * j + 2]; x.w += acc[r][4 * j + 3];
+            *o = x;
+          }
+      }
+    }
+    __syncthreads();
+    const bool whole = ntiles == tiles;
+    for (int i = tid; i < nrows * (D / 4); i += kThreads) {
+      const int r = i / (D / 4), d = (i - r * (D / 4)) * 4;
+      float4 x = *reinterpret_cast<const float4*>(sK + r * pitch + d);
+      if (whole) {
+        const int t = (r0 + r) / p.group, gq = (r0 + r) - t * p.group;
+        if (t >= ex.nodes) continue;
+        const float l = s_l[r], inv = l == 0.f ? 0.f : 1.f / l;
+        const float o[4] = {x.x * inv, x.y * inv, x.z * inv, x.w * inv};
+        const int h = head * p.group + gq;
+        store4(reinterpret_cast<T*>(p.out + ((int64_t)b * p.T + t) * p.out_stride) + (int64_t)h * D + d, o);
+        if (d == 0 && p.lse) p.lse[((int64_t)b * p.T + t) * p.q_heads + h] = l == 0.f ? -INFINITY : (s_m[r] + log2f(l)) * 0.69314718055994531f;
+      } else {
+        float* part = p.part + (((int64_t)blockIdx.x * 2 + (tile0 == 0 ? 1 : 0)) * p.part_rows + r) * (D + kPartPad);
+        *reinterpret_cast<float4*>(part + d) = x;
+        if (d == 0) { part[D] = s_m[r]; part[D + 1] = s_l[r]; }
+      }
+    }
+    u += ntiles;
+  }
+}
+
+// Joins the partial results: a warp per query row of a segment that was split; rows of whole segments are written already.
+// out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i over the parts in order.
+template <typename T>
+__global__ void __launch_bounds__(256) attend_join_kernel(AttendParams p) {
+  __shared__ int prefix[kMaxCacheBatch + 1], warp_sums[8];
+  pdl_wait();
+  tile_prefix(p, prefix, warp_sums);
+  const int64_t units = (int64_t)prefix[p.B] * p.c.kv_heads;
+  if (units == 0) return;
+  const int lane = threadIdx.x & 31;
+  const int D = p.c.head_dim, pitch = D + kPartPad;
+  const int64_t all = (int64_t)p.B * p.c.kv_heads * p.rows;
+  for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < all; i += (int64_t)gridDim.x * 8) {
+    const int row = (int)(i % p.rows);
+    const int64_t seg = i / p.rows;
+    const int head = (int)(seg % p.c.kv_heads), b = (int)(seg / p.c.kv_heads);
+    const int tiles = prefix[b + 1] - prefix[b];
+    if (tiles == 0) continue;
+    const int64_t u0 = (int64_t)prefix[b] * p.c.kv_heads + (int64_t)head * tiles;
+    const int g0 = run_of(units, p.groups, u0), g1 = run_of(units, p.groups, u0 + tiles - 1);
+    if (g0 == g1) continue;
+    const int t = row / p.group, nodes = p.num_nodes ? min(max(__ldg(p.num_nodes + b), 0), p.T) : p.T;
+    if (t >= nodes) continue;
+    const int rb = row / p.rows_per_block, r = row - rb * p.rows_per_block;
+    auto part_of = [&](int g) {
+      return p.part + (((int64_t)(g * p.row_blocks + rb) * 2 + (g == g0 ? 1 : 0)) * p.part_rows + r) * pitch;
+    };
+    float m = -INFINITY;
+    for (int g = g0 + lane; g <= g1; g += 32) m = fmaxf(m, __ldcg(part_of(g) + D));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const float base = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    const int h = head * p.group + row - t * p.group;
+    T* out = reinterpret_cast<T*>(p.out + ((int64_t)b * p.T + t) * p.out_stride) + (int64_t)h * D;
+    for (int d0 = 0; d0 < D; d0 += 128) {
+      const int d = d0 + lane * 4;
+      float o[4] = {0.f, 0.f, 0.f, 0.f};
+      l = 0.f;
+#pragma unroll 4
+      for (int g = g0; g <= g1; ++g) {
+        const float* part = part_of(g);
+        const float2 ml = __ldcg(reinterpret_cast<const float2*>(part + D));
+        const float f = exp2f(ml.x - base);
+        l += f * ml.y;
+        if (d < D && ml.x != -INFINITY) {   // a part that saw nothing has no say, whatever it holds
+          const float4 x = __ldcg(reinterpret_cast<const float4*>(part + d));
+          o[0] = fmaf(f, x.x, o[0]); o[1] = fmaf(f, x.y, o[1]); o[2] = fmaf(f, x.z, o[2]); o[3] = fmaf(f, x.w, o[3]);
+        }
+      }
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] *= inv;
+      if (d < D) store4(out + d, o);
+    }
+    if (p.lse && lane == 0)
+      p.lse[((int64_t)b * p.T + t) * p.q_heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+  }
+}
+
+template <typename T>
+cudaError_t launch_simt(const AttendParams& p, cudaStream_t st) {
+  auto kernel = p.c.head_dim <= 128 ? attend_simt_kernel<T, 1> : attend_simt_kernel<T, 2>;
+  kernel<<<(unsigned)(p.groups * p.row_blocks), kThreads, simt_smem(p.c.head_dim), st>>>(p);
+  return cudaGetLastError();
+}
+
+template <typename K>
+bool raise_limit(K kernel, size_t bytes) {
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
+}
+
+}  // namespace
+
+cudaError_t run_attend_simt(const AttendParams& p, int dtype, cudaStream_t st) {
+  return dtype == JD_DTYPE_F32 ? launch_simt<float>(p, st) : launch_simt<__nv_bfloat16>(p, st);
+}
+
+cudaError_t run_attend_join(const AttendParams& p, int dtype, cudaStream_t st) {
+  const int64_t rows = (int64_t)p.B * p.c.kv_heads * p.rows;
+  const unsigned blocks = (unsigned)std::min<int64_t>((rows + 7) / 8, 8 * kMaxCtas);
+  return dtype == JD_DTYPE_F32 ? launch_chained(attend_join_kernel<float>, dim3(blocks), dim3(256), 0, st, p)
+                               : launch_chained(attend_join_kernel<__nv_bfloat16>, dim3(blocks), dim3(256), 0, st, p);
+}
+
+bool simt_attend_configure() {
+  return raise_limit(attend_simt_kernel<float, 1>, simt_smem(128)) && raise_limit(attend_simt_kernel<float, 2>, simt_smem(256)) &&
+         raise_limit(attend_simt_kernel<__nv_bfloat16, 1>, simt_smem(128)) && raise_limit(attend_simt_kernel<__nv_bfloat16, 2>, simt_smem(256));
+}
+
+}  // namespace jd

@@ -20,12 +20,16 @@ _lib = None
 
 JD_OK, JD_ERR_INVALID_ARG, JD_ERR_UNSUPPORTED, JD_ERR_ARCH = 0, 1, 2, 3
 JD_ERR_ALLOC, JD_ERR_CUDA, JD_ERR_TIMEOUT, JD_ERR_BAD_TOKEN = 4, 5, 6, 7
+JD_ERR_PAGES, JD_ERR_BAD_INDEX = 8, 9
 JD_DTYPE_F32, JD_DTYPE_BF16, JD_DTYPE_FP8_E4M3 = 0, 1, 2
 JD_MODE_STANDARD, JD_MODE_JUDGE, JD_MODE_JUDGE_OR_STANDARD = 0, 1, 2
 JD_RESAMPLE_RESIDUAL, JD_RESAMPLE_TARGET_P = 0, 1
 JD_VARIANT_AUTO, JD_VARIANT_SIMT, JD_VARIANT_FUSED, JD_VARIANT_BATCHED = 0, 1, 2, 3
 JD_RULE_SAMPLING, JD_RULE_TOPK = 0, 1
 JD_NORM_NONE, JD_NORM_RMS = 0, 1
+JD_ROPE_HALF, JD_ROPE_INTERLEAVED = 0, 1
+JD_ROPE_SCALE_NONE, JD_ROPE_SCALE_LINEAR, JD_ROPE_SCALE_BANDS, JD_ROPE_SCALE_YARN = 0, 1, 2, 3
+JD_ATTEND_AUTO, JD_ATTEND_SIMT, JD_ATTEND_TENSOR = 0, 1, 2
 
 MODES = {"standard": JD_MODE_STANDARD, "judge": JD_MODE_JUDGE, "judge_or_standard": JD_MODE_JUDGE_OR_STANDARD}
 RESAMPLE = {"residual": JD_RESAMPLE_RESIDUAL, "target_p": JD_RESAMPLE_TARGET_P}
@@ -36,7 +40,9 @@ EXPORTS = ["jd_version", "jd_status_string", "jd_workspace_bytes", "jd_create", 
            "jd_verify", "jd_verify_host", "jd_last_device_status", "jd_last_launch_info", "jd_philox_uniforms",
            "jd_verify_static", "jd_set_head_fp8", "jd_selftest_timeout", "jd_stream_read_probe",
            "jd_quantize_rows_e4m3", "jd_check_workspace_guards", "jd_selftest_stale_timeout",
-           "jd_debug_phase_stamps"]
+           "jd_debug_phase_stamps", "jd_rope_frequencies", "jd_rope", "jd_cache_workspace_bytes", "jd_cache_create",
+           "jd_cache_destroy", "jd_cache_reserve", "jd_cache_append", "jd_cache_attend", "jd_cache_commit",
+           "jd_cache_fork", "jd_cache_truncate", "jd_cache_compact", "jd_cache_last_status"]
 
 
 class jd_config_t(C.Structure):
@@ -51,6 +57,49 @@ class jd_verify_args_t(C.Structure):
                 ("accept_len", C.c_void_p), ("next_token", C.c_void_p), ("judge_scores", C.c_void_p),
                 ("p_draft", C.c_void_p), ("q_draft", C.c_void_p), ("masks", C.c_void_p),
                 ("row_max", C.c_void_p), ("row_lse", C.c_void_p), ("logits_debug", C.c_void_p)]
+
+
+class jd_rope_t(C.Structure):
+    _fields_ = [("inv_freq", C.c_void_p), ("rot_dim", C.c_int32), ("layout", C.c_int32), ("amplitude", C.c_float)]
+
+
+class jd_rope_args_t(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+                ("inverse", C.c_int32), ("x", C.c_void_p), ("out", C.c_void_p), ("x_stride", C.c_int64),
+                ("out_stride", C.c_int64), ("positions", C.c_void_p), ("rope", jd_rope_t)]
+
+
+class jd_cache_config_t(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("num_layers", "num_pages", "page_size", "q_heads", "kv_heads", "head_dim",
+                                         "max_seqs", "max_pages", "max_nodes", "dtype", "device")]
+
+
+class jd_cache_buffers_t(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k_pages", "v_pages", "page_table", "seq_len", "held", "refs", "free_bits",
+                                          "workspace")] + [("workspace_bytes", C.c_size_t)]
+
+
+class jd_tree_t(C.Structure):
+    _fields_ = [("nodes", C.c_int32), ("per_seq", C.c_int32), ("mask", C.c_void_p), ("depth", C.c_void_p),
+                ("num_nodes", C.c_void_p)]
+
+
+class jd_append_args_t(C.Structure):
+    _fields_ = [("B", C.c_int32), ("layer", C.c_int32), ("slots", C.c_void_p), ("tree", jd_tree_t), ("k", C.c_void_p),
+                ("v", C.c_void_p), ("q", C.c_void_p), ("q_out", C.c_void_p), ("k_stride", C.c_int64),
+                ("v_stride", C.c_int64), ("q_stride", C.c_int64), ("q_out_stride", C.c_int64),
+                ("rope", C.POINTER(jd_rope_t))]
+
+
+class jd_attend_args_t(C.Structure):
+    _fields_ = [("B", C.c_int32), ("layer", C.c_int32), ("slots", C.c_void_p), ("tree", jd_tree_t), ("q", C.c_void_p),
+                ("out", C.c_void_p), ("q_stride", C.c_int64), ("out_stride", C.c_int64), ("lse", C.c_void_p),
+                ("scale", C.c_float), ("variant", C.c_int32)]
+
+
+class jd_commit_args_t(C.Structure):
+    _fields_ = [("B", C.c_int32), ("slots", C.c_void_p), ("accept_len", C.c_void_p), ("num_paths", C.c_int32),
+                ("path_len", C.c_int32), ("paths", C.c_void_p), ("chosen", C.c_void_p)]
 
 
 class JdError(RuntimeError):
@@ -95,8 +144,23 @@ def load():
     lib.jd_check_workspace_guards.argtypes = [C.c_void_p, C.POINTER(C.c_int32)]
     lib.jd_selftest_stale_timeout.argtypes = [C.c_void_p, C.c_void_p]
     lib.jd_debug_phase_stamps.argtypes = [C.c_void_p, C.c_int32]
+    lib.jd_rope_frequencies.argtypes = [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_double, C.c_double, C.c_double,
+                                        C.c_void_p, C.c_void_p]
+    lib.jd_rope.argtypes = [C.POINTER(jd_rope_args_t), C.c_void_p]
+    lib.jd_cache_workspace_bytes.restype = C.c_size_t
+    lib.jd_cache_workspace_bytes.argtypes = [C.POINTER(jd_cache_config_t)]
+    lib.jd_cache_create.argtypes = [C.POINTER(C.c_void_p), C.POINTER(jd_cache_config_t), C.POINTER(jd_cache_buffers_t)]
+    lib.jd_cache_destroy.argtypes = [C.c_void_p]
+    lib.jd_cache_reserve.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p]
+    lib.jd_cache_append.argtypes = [C.c_void_p, C.POINTER(jd_append_args_t), C.c_void_p]
+    lib.jd_cache_attend.argtypes = [C.c_void_p, C.POINTER(jd_attend_args_t), C.c_void_p]
+    lib.jd_cache_commit.argtypes = [C.c_void_p, C.POINTER(jd_commit_args_t), C.c_void_p]
+    lib.jd_cache_fork.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.jd_cache_truncate.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.jd_cache_compact.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.jd_cache_last_status.argtypes = [C.c_void_p, C.POINTER(C.c_int)]
     for name in EXPORTS:
-        if name not in ("jd_version", "jd_status_string", "jd_workspace_bytes"):
+        if name not in ("jd_version", "jd_status_string", "jd_workspace_bytes", "jd_cache_workspace_bytes"):
             getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib
@@ -332,3 +396,11 @@ class Verifier:
 
     def damaged_guards(self) -> int:
         return jd_check_workspace_guards(self.h)
+
+
+# ------------------------------------------------------------------ around the verification call (cache.py)
+def __getattr__(name: str):
+    if name in ("PagedCache", "Rotary", "Tree", "rope_frequencies", "mask_words"):     # torch is imported on first use only
+        from . import cache
+        return getattr(cache, name)
+    raise AttributeError("module %r has no attribute %r" % (__name__, name))

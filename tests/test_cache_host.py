@@ -1,0 +1,227 @@
+"""What of the cache's interface needs no device: struct layouts, refusals, frequencies, trees, and the CPU model itself."""
+import ctypes as C
+import math
+import os
+import re
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache_oracle as O
+from paper_2501_19309_b200 import jd
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.mark.parametrize("name", ["jd_rope_t", "jd_rope_args_t", "jd_cache_config_t", "jd_cache_buffers_t", "jd_tree_t",
+                                  "jd_append_args_t", "jd_attend_args_t", "jd_commit_args_t"])
+def test_struct_layouts_follow_the_header(name):
+    src = open(os.path.join(ROOT, "include", "jd.h")).read()
+    src = re.sub(r"/\*.*?\*/", "", src, flags=re.S)
+    body = re.search(r"typedef struct \{([^{}]*)\} %s;" % name, src).group(1)
+    fields = []
+    for decl in body.split(";"):
+        for part in decl.split(","):
+            m = re.search(r"([A-Za-z_0-9]+)\s*$", part.strip())
+            if m:
+                fields.append(m.group(1))
+    assert fields == [f[0] for f in getattr(jd, name)._fields_]
+
+
+def test_struct_sizes_match_a_c_compiler(tmp_path):
+    import shutil
+    import subprocess
+    if shutil.which("gcc") is None:
+        pytest.skip("gcc is not installed")
+    names = ["jd_rope_t", "jd_rope_args_t", "jd_cache_config_t", "jd_cache_buffers_t", "jd_tree_t", "jd_append_args_t",
+             "jd_attend_args_t", "jd_commit_args_t"]
+    src = '#include <stdio.h>\n#include "jd.h"\nint main(void) {\n%s  return 0;\n}\n' % "".join(
+        '  printf("%%d\\n", (int)sizeof(%s));\n' % n for n in names)
+    (tmp_path / "s.c").write_text(src)
+    subprocess.run(["gcc", "-std=c99", "-I", os.path.join(ROOT, "include"), str(tmp_path / "s.c"), "-o", str(tmp_path / "s")], check=True)
+    got = subprocess.run([str(tmp_path / "s")], capture_output=True, text=True, check=True).stdout.split()
+    assert [int(x) for x in got] == [C.sizeof(getattr(jd, n)) for n in names]
+
+
+def config(**kw):
+    base = dict(num_layers=2, num_pages=100, page_size=16, q_heads=8, kv_heads=2, head_dim=128, max_seqs=4, max_pages=32,
+                max_nodes=26, dtype=jd.JD_DTYPE_BF16, device=0)
+    base.update(kw)
+    return jd.jd_cache_config_t(*[base[f[0]] for f in jd.jd_cache_config_t._fields_])
+
+
+BAD = [dict(num_layers=0), dict(num_pages=0), dict(page_size=4), dict(page_size=24), dict(page_size=2048), dict(q_heads=7), dict(q_heads=0),
+       dict(kv_heads=0), dict(kv_heads=-2), dict(head_dim=12), dict(head_dim=0), dict(head_dim=264), dict(max_seqs=0), dict(max_pages=0),
+       dict(max_pages=1 << 21), dict(max_nodes=0), dict(max_nodes=129), dict(dtype=jd.JD_DTYPE_FP8_E4M3), dict(dtype=5),
+       dict(num_pages=1 << 24, num_layers=64)]
+
+
+def test_workspace_and_configurations():
+    need = jd.load().jd_cache_workspace_bytes
+    small, large = need(C.byref(config(max_nodes=1))), need(C.byref(config()))
+    assert 0 < small < large < 1 << 30
+    for kw in BAD:
+        assert need(C.byref(config(**kw))) == 0, kw
+    assert need(None) == 0
+
+
+def test_refusals_without_a_device():
+    lib = jd.load()
+    h = C.c_void_p()
+    buf = jd.jd_cache_buffers_t()
+    cfg = config()
+    assert lib.jd_cache_create(C.byref(h), C.byref(cfg), C.byref(buf)) == jd.JD_ERR_INVALID_ARG        # null buffers
+    need = lib.jd_cache_workspace_bytes(C.byref(cfg))
+    for name, at in (("k_pages", 8), ("page_table", 2), ("workspace", 128), ("workspace_bytes", need - 1)):
+        buf = jd.jd_cache_buffers_t(*([1 << 20] * 8), need)
+        setattr(buf, name, at if name == "workspace_bytes" else (1 << 20) + at)
+        assert lib.jd_cache_create(C.byref(h), C.byref(cfg), C.byref(buf)) == jd.JD_ERR_INVALID_ARG, name
+    bad = config(page_size=24)
+    buf = jd.jd_cache_buffers_t(*([1 << 20] * 8), need)
+    assert lib.jd_cache_create(C.byref(h), C.byref(bad), C.byref(buf)) == jd.JD_ERR_INVALID_ARG
+    assert not h.value
+    assert lib.jd_cache_destroy(None) == jd.JD_OK
+    one = C.c_int(0)
+    for f, args in (("reserve", (1, None, 1, None)), ("append", (C.byref(jd.jd_append_args_t()), None)), ("attend", (C.byref(jd.jd_attend_args_t()), None)),
+                    ("commit", (C.byref(jd.jd_commit_args_t()), None)), ("fork", (1, None, None, None)), ("truncate", (1, None, None, None)),
+                    ("compact", (None, None)), ("last_status", (C.byref(one),))):
+        assert getattr(lib, "jd_cache_" + f)(None, *args) == jd.JD_ERR_INVALID_ARG, f
+
+
+def rope_args(**kw):
+    r = dict(inv_freq=4096, rot_dim=64, layout=0, amplitude=1.0)
+    a = dict(tokens=2, heads=2, head_dim=64, dtype=jd.JD_DTYPE_BF16, inverse=0, x=1 << 20, out=1 << 21, x_stride=0, out_stride=0, positions=4096)
+    for k, v in kw.items():
+        (r if k in r else a)[k] = v
+    return jd.jd_rope_args_t(*[a[f[0]] if f[0] != "rope" else jd.jd_rope_t(*[r[g[0]] for g in jd.jd_rope_t._fields_])
+                               for f in jd.jd_rope_args_t._fields_])
+
+
+@pytest.mark.parametrize("kw", [dict(tokens=-1), dict(heads=0), dict(head_dim=0), dict(head_dim=257), dict(dtype=2), dict(x=0), dict(out=0),
+                                dict(positions=0), dict(positions=4098), dict(x=(1 << 20) + 1), dict(inv_freq=0), dict(inv_freq=4097),
+                                dict(rot_dim=0), dict(rot_dim=63), dict(rot_dim=66), dict(layout=2), dict(layout=-1), dict(x_stride=127),
+                                dict(out_stride=-128), dict(amplitude=math.nan), dict(amplitude=math.inf), dict(out=1 << 20, x_stride=256)])
+def test_rope_refusals(kw):
+    """None of these reaches the device."""
+    assert jd.load().jd_rope(C.byref(rope_args(**kw)), None) == jd.JD_ERR_INVALID_ARG
+
+
+def test_rope_nothing_to_do():
+    assert jd.load().jd_rope(None, None) == jd.JD_ERR_INVALID_ARG
+    assert jd.load().jd_rope(C.byref(rope_args(tokens=0, x=0, out=0, positions=0)), None) == jd.JD_OK
+
+
+@pytest.mark.parametrize("rot,base", [(2, 10000.0), (64, 10000.0), (128, 500000.0), (256, 1e6)])
+def test_frequencies(rot, base):
+    f0 = base ** (-np.arange(0, rot, 2) / rot)
+    half_ulp = 2.0 ** -24 * (1 + 1e-9)
+
+    def near(got, want):
+        return (np.abs(got.numpy().astype(np.float64) - want) <= half_ulp * want * 2).all()
+
+    got, amp = jd.rope_frequencies(rot, base)
+    assert near(got, f0) and amp == 1.0
+    got, amp = jd.rope_frequencies(rot, base, "linear", 4.0)
+    assert near(got, f0 / 4) and amp == 1.0
+    factor, old, low, high = 8.0, 8192.0, 1.0, 4.0
+    want = []
+    for f in f0:                                         # by wavelength, in three cases
+        wave = 2 * math.pi / f
+        if wave < old / high:
+            want.append(f)
+        elif wave > old / low:
+            want.append(f / factor)
+        else:
+            s = (old / wave - low) / (high - low)
+            want.append((1 - s) * f / factor + s * f)
+    got, amp = jd.rope_frequencies(rot, base, "bands", factor, old, low, high)
+    assert near(got, np.array(want)) and amp == 1.0
+    got, amp = jd.rope_frequencies(rot, base, "yarn", factor, old, 1.0, 32.0)
+    dim = [rot * math.log(old / (t * 2 * math.pi)) / (2 * math.log(base)) for t in (32.0, 1.0)]
+    lo, hi = max(math.floor(dim[0]), 0), min(math.ceil(dim[1]), rot // 2 - 1)
+    if hi <= lo:
+        hi = lo + 0.001
+    ramp = np.clip((np.arange(rot // 2) - lo) / (hi - lo), 0, 1)
+    assert near(got, f0 / factor * ramp + f0 * (1 - ramp)) and abs(amp - (0.1 * math.log(factor) + 1)) < 1e-6
+
+
+@pytest.mark.parametrize("kw", [dict(rot_dim=0), dict(rot_dim=3), dict(rot_dim=258), dict(base=1.0), dict(base=math.inf), dict(base=math.nan),
+                                dict(scaling="linear", factor=0.5), dict(scaling="bands", factor=2.0, low=4.0, high=4.0),
+                                dict(scaling="yarn", factor=2.0, original_len=0.0), dict(scaling="yarn", factor=2.0, low=0.0),
+                                dict(scaling="linear", factor=math.inf)])
+def test_frequency_refusals(kw):
+    with pytest.raises(jd.JdError):
+        jd.rope_frequencies(kw.pop("rot_dim", 64), **kw)
+
+
+def test_trees():
+    rng = np.random.default_rng(0)
+    for T in (1, 2, 31, 32, 33, 100):
+        parents = [-1] + [int(rng.integers(0, i)) for i in range(1, T)]
+        see, depth = O.visible(parents)
+        t = jd.Tree.from_parents(parents, "cpu")
+        words = t.mask.numpy().view(np.uint32)
+        got = np.array([[(words[i, j // 32] >> (j % 32)) & 1 for j in range(T)] for i in range(T)], dtype=bool)
+        assert np.array_equal(got, see) and np.array_equal(t.depth.numpy(), depth) and t.batch == 0
+        assert jd.Tree.from_parents([parents, parents], "cpu").batch == 2
+    for bad in ([0], [-1, 1], [-1, 0, 3], [-1, -1]):
+        with pytest.raises(ValueError):
+            jd.Tree.from_parents(bad, "cpu")
+    with pytest.raises(ValueError):
+        jd.Tree(33, mask=torch.zeros(33, 1, dtype=torch.int32))
+    with pytest.raises(ValueError):
+        jd.Tree(3, mask=torch.zeros(2, 3, 1, dtype=torch.int32), depth=torch.zeros(3, dtype=torch.int32))
+
+
+def model(seqs=4, pages=12, page=8, per_seq=4, D=4):
+    rng = np.random.default_rng(1)
+    return O.Cache(rng.standard_normal((1, pages, 1, page, D)), rng.standard_normal((1, pages, 1, page, D)), np.full((seqs, per_seq), -1),
+                   np.zeros(seqs), np.zeros(seqs), np.zeros(pages), 8)
+
+
+def test_model_copies_a_shared_page_before_it_is_written():
+    m = model()
+    m.reserve(5, [0])
+    k = np.arange(20.0).reshape(1, 5, 1, 4)
+    m.append(0, k, -k, [0])
+    m.commit([4], None, [0], 4)
+    m.fork([0], [1])
+    assert m.refs[0] == 2 and m.len[1] == 5
+    m.reserve(1, [1])
+    assert m.refs[0] == 1 and m.table[1, 0] == 1 and np.array_equal(m.sequence(0, 0, 1)[0], m.sequence(0, 0, 0)[0])
+    m.append(0, k[:, :1] + 100, k[:, :1], [1])
+    assert np.array_equal(m.sequence(0, 0, 0)[0], k[0, :, 0]) and m.status == O.OK
+    m.truncate(None, [0])
+    assert m.refs.tolist()[:2] == [0, 1] and m.compact() == 1 and m.table[1, 0] == 0
+
+
+def test_model_commits_a_path():
+    m = model()
+    m.reserve(8, [2])
+    k = np.arange(32.0).reshape(1, 8, 1, 4)
+    m.append(0, k, k, [2])
+    chosen = m.commit([[1, 3]], np.array([[[1, 2, 3], [2, 4, 7]]]), [2])
+    assert chosen == {0: 1} and m.len[2] == 4
+    assert np.array_equal(m.sequence(0, 0, 2)[0], k[0, [0, 2, 4, 7], 0])
+
+
+def test_model_attention_is_a_softmax():
+    rng = np.random.default_rng(2)
+    q, k, v = rng.standard_normal((2, 4)), rng.standard_normal((5, 4)), rng.standard_normal((5, 3))
+    see = np.array([[1, 1, 0, 1, 0], [0, 0, 0, 0, 0]], dtype=bool)
+    out, lse = O.attend(q, k, v, see, 0.5)
+    e = np.exp(0.5 * k[[0, 1, 3]] @ q[0])
+    assert np.allclose(out[0], e @ v[[0, 1, 3]] / e.sum()) and np.isclose(lse[0], np.log(e.sum()))
+    assert (out[1] == 0).all() and np.isneginf(lse[1])
+
+
+def test_model_rotation():
+    x = np.array([[[1.0, 2.0, 3.0, 4.0, 9.0]]])
+    f = np.array([0.5, 0.25], dtype=np.float32)
+    y = O.rope(x, [2], f, "half")
+    assert np.allclose(y[0, 0], [math.cos(1) - 3 * math.sin(1), 2 * math.cos(.5) - 4 * math.sin(.5), 3 * math.cos(1) + math.sin(1),
+                                 4 * math.cos(.5) + 2 * math.sin(.5), 9.0])
+    y = O.rope(x, [2], f, "interleaved", 2.0)
+    assert np.allclose(y[0, 0, :2], [2 * (math.cos(1) - 2 * math.sin(1)), 2 * (2 * math.cos(1) + math.sin(1))])
+    assert np.allclose(O.rope(O.rope(x, [7], f, "half"), [7], f, "half", inverse=True), x)

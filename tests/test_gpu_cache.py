@@ -1,0 +1,639 @@
+"""Rotary positions, the paged cache and the attention of a drafted block against the CPU model in float64."""
+import numpy as np
+import pytest
+import torch
+
+import cache_testlib as L
+from oracle import cache_oracle as O
+from paper_2501_19309_b200 import jd
+
+pytestmark = pytest.mark.gpu
+
+
+def rand(shape, seed, dtype="bf16", scale=1.0):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    return (torch.randn(shape, generator=gen, device="cuda") * scale).to(L.DT[dtype])
+
+
+# ------------------------------------------------------------------------------------------- rotary positions
+ROPE = [  # tokens, heads, head_dim, rot_dim, layout, dtype
+    (1, 1, 64, 64, "half", "bf16"), (26, 40, 128, 128, "half", "bf16"), (7, 3, 128, 64, "half", "f32"),
+    (300, 5, 80, 48, "interleaved", "bf16"), (33, 2, 256, 256, "interleaved", "f32"), (5, 4, 20, 6, "half", "bf16"),
+    (9, 1, 7, 2, "interleaved", "f32"), (1025, 9, 96, 96, "half", "f32"), (4, 80, 128, 32, "interleaved", "bf16")]
+
+
+def rope_bound(x, freq, pos, amplitude, dtype):
+    """A turned element is two products of |x| <= X and a cosine that is off by 2^-22 (half turns rounded to float32: pi 2^-25;
+    sincospi 2 ulp), summed in float32, and rounded once."""
+    X = np.abs(x).max() * amplitude
+    return 2 * X * 2.0 ** -21 + X * np.sqrt(2) * (2.0 ** -8 if dtype == "bf16" else 2.0 ** -23)
+
+
+@pytest.mark.parametrize("inverse", [False, True])
+@pytest.mark.parametrize("n,heads,D,rot,layout,dtype", ROPE)
+def test_rotate(n, heads, D, rot, layout, dtype, inverse):
+    x = rand((n, heads, D), 1, dtype)
+    pos = torch.randint(-3, 1 << 20, (n,), generator=torch.Generator().manual_seed(2)).to(torch.int32)
+    if n > 2:
+        pos[0], pos[1] = 2 ** 31 - 1, -2 ** 31
+    freq, amp = jd.rope_frequencies(rot, 10000.0, "yarn", 4.0, 2048.0, 1.0, 32.0)
+    r = jd.Rotary(freq.cuda(), layout, amp)
+    want = O.rope(L.f64(x), pos.numpy(), freq.numpy(), layout, amp, inverse)
+    got = r.rotate(x, pos.cuda(), inverse=inverse)
+    assert np.abs(L.f64(got) - want).max() <= rope_bound(L.f64(x), freq, pos, amp, dtype)
+    assert torch.equal(got[..., rot:], x[..., rot:])                    # what does not turn keeps its bits
+    inplace = x.clone()
+    assert r.rotate(inplace, pos.cuda(), out=inplace, inverse=inverse) is inplace
+    assert torch.equal(inplace, got)
+
+
+def test_rotate_strided_rows_leave_the_rest_alone():
+    n, heads, D = 19, 4, 64
+    for offset in (0, 1):            # the second one is not on 16 bytes: single elements
+        buf = torch.full((n, 900), 7.0, dtype=torch.bfloat16, device="cuda")
+        x = buf[:, offset:offset + heads * D].view(n, heads, D) if offset == 0 else buf.as_strided((n, heads, D), (900, D, 1), 1)
+        x.copy_(rand((n, heads, D), 3))
+        pos = L.ints(np.arange(n) * 1000)
+        freq, _ = jd.rope_frequencies(64)
+        r = jd.Rotary(freq.cuda())
+        want = r.rotate(x.clone(memory_format=torch.contiguous_format), pos)
+        got = r.rotate(x, pos, out=x)
+        assert torch.equal(got, want)
+        rest = torch.ones_like(buf, dtype=torch.bool)
+        rest[:, offset:offset + heads * D] = False
+        assert bool((buf[rest] == 7.0).all())
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_rotation_gradient(layout):
+    """inverse=True is the transpose: against the formula's products and against differences (the map is linear, so a difference
+    over a step of 1 is exact up to rounding)."""
+    n, heads, D, rot = 3, 2, 16, 12
+    freq, amp = jd.rope_frequencies(rot, 10000.0, "yarn", 8.0, 64.0)
+    r = jd.Rotary(freq.cuda(), layout, amp)
+    pos = L.ints([5, 100, 77777])
+    x, gy = rand((n, heads, D), 4, "f32"), rand((n, heads, D), 5, "f32")
+    gx = r.rotate(gy, pos, inverse=True)
+    want = O.rope(L.f64(gy), pos.cpu().numpy(), freq.numpy(), layout, amp, inverse=True)
+    assert np.abs(L.f64(gx) - want).max() <= rope_bound(L.f64(gy), freq, pos, amp, "f32")
+    y0 = L.f64(r.rotate(x, pos))
+    num = np.zeros((n, heads, D))
+    for d in range(D):
+        e = x.clone()
+        e[..., d] += 1.0
+        num[..., d] = ((L.f64(r.rotate(e, pos)) - y0) * L.f64(gy)).sum(-1)
+    # each of the D products holds two rounded values of at most 5 x amplitude
+    assert np.abs(num - L.f64(gx)).max() <= D * 2 * 2.0 ** -20 * 6 * np.abs(L.f64(gy)).max() * amp
+
+
+def test_rotate_no_tokens():
+    freq, _ = jd.rope_frequencies(8)
+    x = torch.empty(0, 3, 8, device="cuda")
+    assert jd.Rotary(freq.cuda()).rotate(x, torch.empty(0, dtype=torch.int32, device="cuda")).shape == (0, 3, 8)
+
+
+# ------------------------------------------------------------------------------------------- append
+@pytest.mark.parametrize("dtype,D,rot,layout", [("bf16", 128, 128, "half"), ("bf16", 64, 32, "interleaved"), ("f32", 40, 24, "half"),
+                                                ("f32", 72, 72, "interleaved"), ("bf16", 64, 0, "half")])
+@pytest.mark.parametrize("packed", [False, True])
+def test_append(dtype, D, rot, layout, packed):
+    rng = np.random.default_rng(3)
+    lens, T, Hq, H = [0, 5, 31, 200, 16], 6, 4, 2
+    c = L.filled_cache(lens, T, D=D, q_heads=Hq, kv_heads=H, layers=3, dtype=dtype, max_nodes=8)
+    m = L.model_of(c)
+    B = 4
+    slots, nodes = L.ints([3, 0, -1, 1]), L.ints([6, 2, 6, 0])
+    parents = [L.random_tree(T, rng) for _ in range(B)]
+    tree = L.device_tree(parents, num_nodes=nodes)
+    if packed:                       # q, k and v as slices of one projection
+        qkv = rand((B, T, Hq + 2 * H, D), 6, dtype)
+        q, k, v = qkv[:, :, :Hq], qkv[:, :, Hq:Hq + H], qkv[:, :, Hq + H:]
+    else:
+        q, k, v = rand((B, T, Hq, D), 6, dtype), rand((B, T, H, D), 7, dtype), rand((B, T, H, D), 8, dtype)
+    freq = jd.rope_frequencies(rot, 10000.0)[0] if rot else None
+    rotary = jd.Rotary(freq.cuda(), layout) if rot else None
+    q_out = torch.full((B, T, Hq, D), 9.0, dtype=L.DT[dtype], device="cuda")
+    k_before, v_before = c.k.clone(), c.v.clone()
+    c.append(1, k, v, tree, rotary=rotary, q=q, q_out=q_out, slots=slots)
+    assert c.status() == jd.JD_OK
+    L.same_books(c, m)
+    touched = torch.zeros_like(c.k, dtype=torch.bool)
+    for b, slot in enumerate([3, 0, None, 1]):
+        see, depth = O.visible(parents[b])
+        n = int(nodes[b])
+        if slot is None or n == 0:
+            assert bool((q_out[b] == 9.0).all())
+            continue
+        pos = lens[slot] + depth
+        if rot:
+            wk, wq = (O.rope(L.f64(x[b]), pos, freq.numpy(), layout) for x in (k, q))
+        else:
+            wk, wq = L.f64(k[b]), L.f64(q[b])
+        bound = rope_bound(L.f64(qkv if packed else q), freq, pos, 1.0, dtype) if rot else 0.0
+        bound = max(bound, rope_bound(L.f64(k), freq, pos, 1.0, dtype)) if rot else 0.0
+        assert np.abs(L.f64(q_out[b, :n]) - wq[:n]).max() <= bound
+        assert bool((q_out[b, n:] == 9.0).all())
+        for t in range(n):
+            p, r = m.row(slot, lens[slot] + t)
+            assert np.abs(L.f64(c.k[1, p, :, r]) - wk[t]).max() <= bound
+            assert torch.equal(c.v[1, p, :, r], v[b, t])
+            touched[1, p, :, r] = True
+    assert torch.equal(c.k[~touched], k_before[~touched]) and torch.equal(c.v[~touched], v_before[~touched])
+
+
+def test_append_reports_rows_without_a_page_of_their_own():
+    c = L.filled_cache([14, 20], 0, layers=2, max_nodes=8)
+    T = 4
+    k, v = rand((2, T, 2, 64), 1), rand((2, T, 2, 64), 2)
+    c.append(0, k, v)                                  # pages for 16 and 32 tokens: nodes 2, 3 of the first have none
+    assert c.status() == jd.JD_ERR_BAD_INDEX
+    assert torch.equal(c.v[0, int(c.page_table[0, 0]), :, 14:16].transpose(0, 1), v[0, :2])
+    page = int(c.page_table[1, 1])
+    assert torch.equal(c.v[0, page, :, 4:8].transpose(0, 1), v[1])
+    c.refs[page] += 1                                  # another owner
+    before = c.v.clone()
+    c.append(0, k[1:], rand((1, T, 2, 64), 3), slots=L.ints([1]))
+    assert c.status() == jd.JD_ERR_BAD_INDEX and torch.equal(c.v, before)
+    c.append(0, k, v, slots=L.ints([1, 1]))            # the same slot twice
+    assert c.status() == jd.JD_ERR_BAD_INDEX
+    c.append(0, k, v, slots=L.ints([7, -5]))
+    assert c.status() == jd.JD_ERR_BAD_INDEX
+    assert c.status() == jd.JD_OK                      # a query clears it
+
+
+# ------------------------------------------------------------------------------------------- attention
+ATTEND = [  # lens, T, page, q_heads, kv_heads, D, dtype, variant, tree
+    ([0], 1, 16, 1, 1, 64, "bf16", "simt", "chain"),
+    ([1, 0, 63, 64, 65, 127, 128, 129], 5, 16, 4, 2, 64, "bf16", "simt", "tree"),
+    ([300, 2], 9, 32, 6, 2, 80, "f32", "simt", "star"),
+    ([37], 128, 8, 5, 1, 200, "f32", "simt", "tree"),
+    ([1000], 3, 128, 8, 8, 8, "f32", "simt", "chain"),
+    ([500, 1], 33, 64, 16, 1, 128, "bf16", "simt", "tree")]
+
+
+def run_attend(c, m, T, parents, dtype, variant, seed, slots=None, num_nodes=None, scale=None, layer=0, B=None):
+    B = len(c.seq_len) if B is None else B
+    q = rand((B, T, c.q_heads, c.head_dim), seed, dtype)
+    see = np.stack([O.visible(p)[0] for p in parents]) if isinstance(parents[0], list) else O.visible(parents)[0]
+    tree = L.device_tree(parents, num_nodes=num_nodes)
+    out = dict(out=torch.full(q.shape, 5.0, dtype=q.dtype, device="cuda"), lse=torch.full(q.shape[:3], 5.0, device="cuda"))
+    c.attend(layer, q, tree, scale=scale, out=out, slots=slots, variant=variant)
+    assert c.status() == jd.JD_OK
+    scale = c.head_dim ** -0.5 if scale is None else scale
+    host = dict(slots=None if slots is None else slots.cpu().numpy(), num_nodes=None if num_nodes is None else num_nodes.cpu().numpy())
+    want, lse = m.attend(layer, L.f64(q), see, scale, **host)
+    tol, ltol = L.attend_tolerance(m, layer, L.f64(q), see, scale, np.nan_to_num(want), dtype, **host)
+    return out, want, lse, tol, ltol
+
+
+def check_attend(out, want, lse, tol, ltol):
+    got, glse = L.f64(out["out"]), L.f64(out["lse"])
+    rows = ~np.isnan(lse)
+    assert (got[~rows] == 5.0).all() and (glse[~rows] == 5.0).all()       # rows that no node has are left as they were
+    err = np.abs(got - want)[rows]
+    assert (err <= tol[rows]).all(), (err.max(), (err - tol[rows]).max(), np.argwhere((err > tol[rows])).tolist()[:5])
+    dead = np.isneginf(lse) & rows
+    assert (got[dead] == 0).all() and np.isneginf(glse[dead]).all()
+    live = rows & ~dead
+    assert (np.abs(glse[live] - lse[live]) <= ltol[live] + 2.0 ** -22 * np.abs(lse[live])).all()
+
+
+@pytest.mark.parametrize("lens,T,page,q_heads,kv_heads,D,dtype,variant,style", ATTEND)
+def test_attend(lens, T, page, q_heads, kv_heads, D, dtype, variant, style):
+    rng = np.random.default_rng(T)
+    c = L.filled_cache(lens, T, page=page, q_heads=q_heads, kv_heads=kv_heads, D=D, dtype=dtype, max_nodes=T, seed=T)
+    parents = [L.random_tree(T, rng, style) for _ in lens]
+    r = run_attend(c, L.model_of(c), T, parents, dtype, variant, 11)
+    check_attend(*r)
+    again = run_attend(c, L.model_of(c), T, parents, dtype, variant, 11)
+    assert torch.equal(r[0]["out"], again[0]["out"]) and torch.equal(r[0]["lse"], again[0]["lse"])
+
+
+VARIANTS = [("simt", "bf16", 64), ("simt", "f32", 72)]
+
+
+@pytest.mark.parametrize("variant,dtype,D", VARIANTS)
+def test_attend_slots_padding_layers_and_masks_that_leave_nothing(variant, dtype, D):
+    """Padding entries, the same slot twice, padded blocks, another layer; a mask with empty rows on an empty sequence."""
+    lens, T = [0, 70, 500, 3], 7
+    c = L.filled_cache(lens, T, D=D, dtype=dtype, layers=3, max_nodes=T, seed=4)
+    m = L.model_of(c)
+    slots, nodes = L.ints([2, -1, 0, 1, 2, 3]), L.ints([7, 7, 5, 0, 3, -4])
+    q = rand((6, T, 4, D), 9, dtype)
+    see = np.tril(np.ones((T, T), dtype=bool))
+    see[2] = False
+    see[0, 0] = False
+    tree = jd.Tree(T, mask=jd.mask_words(torch.from_numpy(see)).cuda(), num_nodes=nodes)
+    out = dict(out=torch.full(q.shape, 5.0, dtype=q.dtype, device="cuda"), lse=torch.full(q.shape[:3], 5.0, device="cuda"))
+    c.attend(2, q, tree, scale=0.3, out=out, slots=slots, variant=variant)
+    assert c.status() == jd.JD_OK
+    host = dict(slots=slots.cpu().numpy(), num_nodes=nodes.cpu().numpy())
+    want, lse = m.attend(2, L.f64(q), see, 0.3, **host)
+    assert np.isneginf(lse[2, 0]).all() and np.isneginf(lse[2, 2]).all()       # the empty sequence's rows that see nothing
+    check_attend(out, want, lse, *L.attend_tolerance(m, 2, L.f64(q), see, 0.3, np.nan_to_num(want), dtype, **host))
+
+
+@pytest.mark.parametrize("variant,dtype,D", VARIANTS)
+def test_attend_ignores_what_stands_in_hidden_rows(variant, dtype, D):
+    """Rows behind the block, other pages and hidden nodes hold infinities and NaN; a node that is not finite spoils the rows
+    that see it and no other."""
+    lens, T = [130, 0, 257], 12
+    c = L.filled_cache(lens, T, D=D, dtype=dtype, max_nodes=T, seed=5)
+    m = L.model_of(c)
+    parents = L.random_tree(T, np.random.default_rng(8), "star")
+    clean = run_attend(c, m, T, parents, dtype, variant, 12)
+    check_attend(*clean)
+    junk = torch.tensor([float("nan"), float("inf"), float("-inf")], device="cuda").to(L.DT[dtype])
+    used = torch.zeros(c.k.shape[1], c.k.shape[3], dtype=torch.bool, device="cuda")
+    for s, n in enumerate(lens):
+        for t in range(n + T):
+            p, r = m.row(s, t)
+            used[p, r] = True
+    hidden = ~used[None, :, None, :, None].expand(c.k.shape)
+    c.k[hidden] = junk[torch.arange(int(hidden.sum()), device="cuda") % 3]
+    c.v[hidden] = junk[torch.arange(int(hidden.sum()), device="cuda") % 3]
+    got = run_attend(c, m, T, parents, dtype, variant, 12)
+    assert torch.equal(got[0]["out"], clean[0]["out"]) and torch.equal(got[0]["lse"], clean[0]["lse"])
+    # node 3 of every sequence: only node 3's own rows see it
+    for s, n in enumerate(lens):
+        p, r = m.row(s, n + 3)
+        c.k[0, p, :, r] = float("nan")
+        c.v[0, p, 0, r, 5] = float("inf")
+        c.v[0, p, 1, r, 6] = float("nan")
+    got = run_attend(c, m, T, parents, dtype, variant, 12)[0]
+    keep = [t for t in range(T) if t != 3]
+    assert torch.equal(got["out"][:, keep], clean[0]["out"][:, keep]) and torch.equal(got["lse"][:, keep], clean[0]["lse"][:, keep])
+    assert bool(torch.isnan(got["out"][:, 3]).all())
+    # values alone: the element is spoilt, its row's other elements are not
+    for s, n in enumerate(lens):
+        p, r = m.row(s, n + 3)
+        c.k[0, p, :, r] = 0.25
+    got = run_attend(c, m, T, parents, dtype, variant, 12)[0]["out"].float()
+    assert torch.equal(got[:, keep], clean[0]["out"].float()[:, keep])
+    assert bool(torch.isinf(got[:, 3, :2, 5]).all()) and bool(torch.isnan(got[:, 3, 2:, 6]).all())
+    assert bool(torch.isfinite(got[:, 3, :2, 6]).all()) and bool(torch.isfinite(got[:, 3, 2:, 5]).all())
+
+
+@pytest.mark.parametrize("variant,dtype,D", VARIANTS)
+def test_attend_extreme_scores(variant, dtype, D):
+    """Maxima that jump from tile to tile, scores of hundreds, and keys of the type's lowest value."""
+    lens, T = [900], 4
+    c = L.filled_cache(lens, T, D=D, dtype=dtype, max_nodes=T, seed=6)
+    gen = torch.Generator().manual_seed(1)
+    order = L.f64(c.page_table[0, :-4]).astype(int)
+    for i, p in enumerate(order):                       # growing keys, then a jump, then small ones
+        c.k[0, p] *= (0.1 + 0.2 * i) if i < 40 else (20.0 if i == 41 else 0.01)
+    c.k[0, order[3], :, 2] = torch.finfo(L.DT[dtype]).min / 1e30
+    r = run_attend(c, L.model_of(c), T, L.random_tree(T, np.random.default_rng(2)), dtype, variant, 13)
+    # scores of hundreds: the bound's A is large, so compare where it says something
+    got, want, tol = L.f64(r[0]["out"]), r[1], r[3]
+    assert np.isfinite(got).all() and (np.abs(got - want) <= tol).all()
+
+
+@pytest.mark.parametrize("variant,dtype,D", VARIANTS)
+def test_attend_strided_queries_and_outputs(variant, dtype, D):
+    c = L.filled_cache([40, 9], 5, D=D, dtype=dtype, max_nodes=5)
+    qkv = rand((2, 5, 8, D), 3, dtype)
+    q = qkv[:, :, :4]
+    buf = torch.zeros(2, 5, 6, D, dtype=q.dtype, device="cuda")
+    a = c.attend(0, q, variant=variant)
+    b = c.attend(0, q.contiguous(), out=dict(out=buf[:, :, 1:5]), variant=variant)
+    assert torch.equal(a["out"], b["out"]) and bool((buf[:, :, 0] == 0).all()) and bool((buf[:, :, 5] == 0).all())
+
+
+@pytest.mark.parametrize("variant", ["simt"])
+def test_attend_beyond_four_gigabytes(variant):
+    """The sequence's pages lie at both ends of a pool of more than 2^32 bytes and 2^31 elements."""
+    page, H, D, layers = 64, 8, 128, 2
+    pages = (1 << 31) // (layers * H * page * D) + 40
+    c = L.empty_cache(layers, pages, page, 8, H, D, 1, 8, 4)
+    assert c.k.numel() > 1 << 31
+    rows = [pages - 1, 0, pages - 2, pages // 2, 1]
+    c.page_table[0, :5] = L.ints(rows)
+    c.refs[rows] = 1
+    c.seq_len[0], c.held[0] = 300, 5
+    small = L.filled_cache([300], 4, page=page, q_heads=8, kv_heads=H, D=D, max_nodes=4, seed=9)
+    for i, p in enumerate(rows):
+        c.k[1, p], c.v[1, p] = small.k[0, int(small.page_table[0, i])], small.v[0, int(small.page_table[0, i])]
+    q = rand((1, 4, 8, D), 5)
+    a, b = c.attend(1, q, variant=variant), small.attend(0, q, variant=variant)
+    assert c.status() == jd.JD_OK
+    assert torch.equal(a["out"], b["out"]) and torch.equal(a["lse"], b["lse"])
+    k, v = rand((1, 4, H, D), 6), rand((1, 4, H, D), 7)
+    c.append(1, k, v)
+    at = [(rows[t // page], t % page) for t in range(300, 304)]
+    assert all(torch.equal(c.k[1, p, :, r], k[0, i]) and torch.equal(c.v[1, p, :, r], v[0, i]) for i, (p, r) in enumerate(at))
+    c.close()
+
+
+# ------------------------------------------------------------------------------------------- pages
+@pytest.mark.parametrize("seed,dtype,page,layers,H,D", [(0, "bf16", 8, 2, 1, 8), (1, "f32", 8, 1, 2, 16), (2, "bf16", 16, 3, 2, 64),
+                                                        (3, "bf16", 32, 1, 3, 40), (4, "f32", 64, 2, 1, 8)])
+def test_random_programs_against_the_model(seed, dtype, page, layers, H, D):
+    """Reserve, append, commit, fork, truncate and compact in random order, bad entries among them: tables, owners and the
+    sequences' rows stay those of the model, bit for bit."""
+    rng = np.random.default_rng(seed)
+    seqs, per_seq, T = 12, 6, 9
+    c = L.empty_cache(layers, 40, page, H, H, D, seqs, per_seq, T, dtype, fill=seed)
+    m = L.model_of(c)
+
+    def pick(n, bad=0.1):
+        s = rng.permutation(seqs)[:n].tolist()
+        return [int(rng.choice([-1, seqs, -3, s[0]])) if rng.random() < bad else x for x in s]
+
+    for step in range(60):
+        m.status = O.OK
+        n = int(rng.integers(1, 6))
+        op = rng.choice(["step", "step", "step", "fork", "truncate", "free", "reserve", "compact"])
+        if op == "step":
+            slots = pick(n)
+            t = int(rng.integers(1, T + 1))
+            c.reserve(t, L.ints(slots)); m.reserve(t, slots)
+            for layer in range(layers):
+                k, v = rand((n, t, H, D), 1000 + step, dtype), rand((n, t, H, D), 2000 + step, dtype)
+                c.append(layer, k, v, slots=L.ints(slots)); m.append(layer, L.f64(k), L.f64(v), slots)
+            if t == 1 or rng.random() < 0.3:
+                acc = rng.integers(-1, t + 1, n)
+                c.commit(L.ints(acc), slots=L.ints(slots), path_len=t - 1); m.commit(acc, None, slots, t - 1)
+            else:
+                paths = np.sort(rng.permuted(np.tile(np.arange(1, t), (n, 3, 1)), axis=2)[:, :, :int(rng.integers(1, t))], axis=2)
+                if rng.random() < 0.15:
+                    paths[0, 0, -1] = rng.integers(-2, T + 2)
+                acc = rng.integers(0, paths.shape[2] + 1, (n, 3))
+                chosen = c.commit(L.ints(acc), L.ints(paths), slots=L.ints(slots)).cpu().numpy()
+                for i, want in m.commit(acc, paths, slots).items():
+                    assert chosen[i] == want
+        elif op == "reserve":
+            slots, t = pick(n), int(rng.integers(1, 3 * page))
+            c.reserve(t, L.ints(slots)); m.reserve(t, slots)
+        elif op == "fork":
+            src = rng.integers(0, seqs, n).tolist()
+            empty = [s for s in range(seqs) if m.held[s] == 0 and m.len[s] == 0]
+            dst = [int(rng.choice(empty)) if empty and rng.random() < 0.8 else int(rng.integers(-2, seqs + 1)) for _ in range(n)]
+            c.fork(L.ints(src), L.ints(dst)); m.fork(src, dst)
+        elif op == "truncate":
+            slots = pick(n)
+            to = [int(rng.integers(-1, m.len[s] + 2)) if 0 <= s < seqs else 0 for s in slots]
+            c.truncate(L.ints(to), L.ints(slots)); m.truncate(to, slots)
+        elif op == "free":
+            slots = pick(n)
+            c.free(L.ints(slots)); m.truncate(None, slots, n)
+        else:
+            assert int(c.compact()) == m.compact()
+        status = c.status()
+        assert (status == jd.JD_OK) == (m.status == O.OK), (step, op, status, m.status)
+        L.same_books(c, m)
+        for s in range(seqs):
+            for layer in range(layers):
+                for h in range(H):
+                    want = m.sequence(layer, h, s)
+                    pages = torch.as_tensor(m.table[s, :m.held[s]], device="cuda")
+                    for x, w in zip((c.k, c.v), want):
+                        got = L.f64(x[layer, pages, h].reshape(-1, D)[:len(w)])
+                        assert np.array_equal(got, w), (step, op, s)
+
+
+def test_reserve_is_all_or_nothing_and_takes_the_lowest_pages():
+    c = L.empty_cache(1, 70, 8, 1, 1, 8, 3, 64, 4)
+    c.reserve(33 * 8, L.ints([0]))                      # pages 0..32: past a word of the bitmap
+    assert c.status() == jd.JD_OK and c.page_table[0, :33].cpu().tolist() == list(range(33))
+    before = [x.clone() for x in (c.page_table, c.held, c.refs, c.free_bits)]
+    c.reserve(20 * 8, L.ints([1, 2]))                   # 40 pages of 37
+    assert c.status() == jd.JD_ERR_PAGES
+    c.reserve(65 * 8, L.ints([1]))                      # more than a table has
+    assert c.status() == jd.JD_ERR_PAGES
+    c.reserve((1 << 31) - 1, L.ints([1]))
+    assert c.status() == jd.JD_ERR_PAGES
+    assert all(torch.equal(x, y) for x, y in zip(before, (c.page_table, c.held, c.refs, c.free_bits)))
+    c.reserve(37 * 8, L.ints([1]))                      # the last 37
+    assert c.status() == jd.JD_OK and bool((c.free_bits == 0).all())
+    c.free(L.ints([0]))
+    c.reserve(1, L.ints([2]))
+    assert c.status() == jd.JD_OK and int(c.page_table[2, 0]) == 0 and int(c.held[0]) == 0
+
+
+def test_large_pool_and_many_sequences():
+    """A pool of more words than the reserving block has threads, and a call of 1024 sequences."""
+    c = L.empty_cache(1, 50000, 8, 1, 1, 8, 1024, 64, 4)
+    c.reserve(8 * 48)                                   # 49152 pages
+    assert c.status() == jd.JD_OK
+    assert torch.equal(c.page_table[:, :48].flatten().cpu(), torch.arange(49152, dtype=torch.int32))
+    c.reserve(8 * 49)
+    assert c.status() == jd.JD_ERR_PAGES
+    odd = torch.arange(1, 1024, 2, dtype=torch.int32, device="cuda")
+    c.free(odd)
+    assert c.status() == jd.JD_OK and int((c.refs == 0).sum()) == 50000 - 49152 + 512 * 48
+    assert int(c.compact()) == 512 * 48
+    assert bool((c.refs[:512 * 48] == 1).all()) and bool((c.refs[512 * 48:] == 0).all())
+
+
+def test_forks_share_until_they_write():
+    c = L.empty_cache(2, 16, 8, 1, 1, 8, 4, 4, 4, fill=3)
+    c.reserve(4, L.ints([0]))
+    for layer in range(2):
+        c.append(layer, rand((1, 4, 1, 8), layer), rand((1, 4, 1, 8), 9), slots=L.ints([0]))
+    c.commit(L.ints([2]), slots=L.ints([0]))            # 3 tokens in one page
+    c.fork(L.ints([0, 0]), L.ints([1, 3]))
+    assert c.status() == jd.JD_OK and int(c.refs[0]) == 3 and c.seq_len.cpu().tolist() == [3, 3, 0, 3]
+    c.append(0, rand((1, 1, 1, 8), 1), rand((1, 1, 1, 8), 2), slots=L.ints([1]))      # not reserved: shared
+    assert c.status() == jd.JD_ERR_BAD_INDEX
+    c.reserve(2, L.ints([1, 0, 3]))                     # the last of the three keeps the page
+    assert c.status() == jd.JD_OK
+    assert [int(c.page_table[s, 0]) for s in (0, 1, 3)] == [2, 1, 0] and c.refs[:3].cpu().tolist() == [1, 1, 1]
+    for s in (0, 1):
+        p = int(c.page_table[s, 0])
+        assert torch.equal(c.k[:, p, :, :3], c.k[:, 0, :, :3]) and torch.equal(c.v[:, p, :, :3], c.v[:, 0, :, :3])
+
+
+# ------------------------------------------------------------------------------------------- refusals
+def refused(f, status=jd.JD_ERR_INVALID_ARG):
+    with pytest.raises(jd.JdError) as e:
+        f()
+    assert e.value.status == status
+
+
+def test_refusals():
+    c = L.filled_cache([20, 30], 4, max_nodes=4)
+    q, k = rand((2, 4, 4, 64), 1), rand((2, 4, 2, 64), 2)
+    for layer in (-1, 1):
+        refused(lambda: c.attend(layer, q))
+        refused(lambda: c.append(layer, k, k))
+    refused(lambda: c.attend(0, rand((2, 5, 4, 64), 1)))                  # more nodes than max_nodes
+    refused(lambda: c.attend(0, rand((3, 4, 4, 64), 1)))                  # more sequences than slots
+    refused(lambda: c.attend(0, q, out=dict(out=q)))
+    refused(lambda: c.attend(0, q, scale=float("nan")))
+    refused(lambda: c.attend(0, q, variant=3))
+    refused(lambda: c.reserve(0))
+    refused(lambda: c.commit(L.ints([1, 1]), path_len=4))
+    refused(lambda: c.commit(L.ints([1, 1]), path_len=-1))
+    f32 = L.filled_cache([20], 4, dtype="f32", max_nodes=4)
+    refused(lambda: f32.attend(0, rand((1, 4, 4, 64), 1, "f32"), variant="tensor"), jd.JD_ERR_UNSUPPORTED)
+    odd = L.filled_cache([20], 4, D=72, max_nodes=4)
+    refused(lambda: odd.attend(0, rand((1, 4, 4, 72), 1), variant="tensor"), jd.JD_ERR_UNSUPPORTED)
+    freq, _ = jd.rope_frequencies(128)
+    refused(lambda: c.append(0, k, k, rotary=jd.Rotary(freq.cuda())))     # wider than a head
+    # alignment and strides that 16-byte accesses cannot take
+    buf = torch.zeros(4096, dtype=torch.bfloat16, device="cuda")
+    refused(lambda: c.attend(0, buf[1:1 + 2 * 4 * 256].view(2, 4, 4, 64)))
+    wide = torch.zeros(2, 4, 260, dtype=torch.bfloat16, device="cuda")
+    refused(lambda: c.attend(0, wide[..., :256].unflatten(2, (4, 64))))
+    with pytest.raises(ValueError):
+        c.attend(0, rand((2, 4, 4, 128), 1))
+    with pytest.raises(ValueError):
+        c.attend(0, q.float())
+    with pytest.raises(ValueError):
+        c.reserve(1, slots=torch.zeros(2, dtype=torch.int64, device="cuda"))
+    with pytest.raises(ValueError):
+        c.attend(0, q, jd.Tree(3))
+    with pytest.raises(ValueError):
+        c.attend(0, q.transpose(1, 2).contiguous().transpose(1, 2))
+    for kw in (dict(page=24), dict(page=4), dict(D=12), dict(D=264), dict(max_nodes=129), dict(q_heads=3)):
+        with pytest.raises(jd.JdError):
+            L.filled_cache([4], 1, **kw)
+    assert c.status() == jd.JD_OK
+
+
+# ------------------------------------------------------------------------------------------- together
+def decode_step(c, layers, T, tree, slots, tokens, rotary, dtype, seed):
+    """One step's cache work for a made-up target: every layer's k, v, q are drawn; returns the last layer's outputs."""
+    B = slots.shape[0]
+    c.reserve(T, slots)
+    for layer in range(layers):
+        k, v, q = (rand((B, T, h, c.head_dim), seed + 10 * layer + i, dtype) for i, h in enumerate((c.kv_heads, c.kv_heads, c.q_heads)))
+        q = c.append(layer, k, v, tree, rotary=rotary, q=q, slots=slots)
+        out = c.attend(layer, q, tree, slots=slots)
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_steps_with_verification(dtype):
+    """Reserve, append, attend, verify, commit as a decoding loop makes them: the accept lengths go from jd_verify to the
+    cache on the device, and after every step the cache holds what a cache that got only the kept tokens holds."""
+    import jd_testlib as JT
+    from paper_2501_19309_b200 import inputs as I
+    B, M, layers, Hq, H, D = 3, 5, 2, 4, 2, 64
+    d = Hq * D
+    wl = I.CONFIGS[1].scaled("steps", B=B, M=M, d=d, V=3000)
+    c = L.empty_cache(layers, 64, 8, Hq, H, D, B, 20, M + 1, dtype)
+    ref = L.model_of(c)
+    freq, _ = jd.rope_frequencies(D, 10000.0)
+    rotary = jd.Rotary(freq.cuda())
+    tree = jd.Tree(M + 1)
+    slots = L.ints([2, 0, 1])
+    total = np.zeros(B, dtype=int)
+    for step in range(4):
+        out = decode_step(c, layers, M + 1, tree, slots, None, rotary, dtype, 100 * step)
+        inp = I.make_inputs(wl, step)
+        dev = JT.upload(inp)
+        ver = JT.make_verifier(inp, dev)
+        Hs = out["out"].reshape(B, M + 1, d).to(torch.bfloat16).contiguous()
+        res = ver.verify(Hs, dev["x"], dev["dl"], inp.tau, step, "judge_or_standard")
+        before = c.seq_len.clone()
+        c.commit(res["accept_len"], slots=slots, path_len=M)
+        assert c.status() == jd.JD_OK and ver.device_status() == jd.JD_OK
+        a = res["accept_len"].cpu().numpy()
+        assert np.array_equal((c.seq_len - before)[slots.long()].cpu().numpy(), a + 1)
+        # the kept tokens alone, through the model
+        ref.reserve(M + 1, slots.cpu().numpy())
+        for layer in range(layers):
+            k, v = (L.f64(rand((B, M + 1, H, D), 100 * step + 10 * layer + i, dtype)) for i in range(2))
+            ref.append(layer, k, v, slots.cpu().numpy())
+        ref.commit(a, None, slots.cpu().numpy(), M)
+        L.same_books(c, ref)
+        for s in range(B):
+            for layer in range(layers):
+                for h in range(H):
+                    k, v = ref.sequence(layer, h, s)
+                    pages = torch.as_tensor(ref.table[s, :ref.held[s]], device="cuda")
+                    assert np.array_equal(L.f64(c.v[layer, pages, h].reshape(-1, D)[:len(v)]), v)
+        total += a + 1
+        ver.close()
+    assert total.sum() > B
+
+
+def test_tree_step_equals_the_chain_that_was_kept():
+    """A tree is attended and its longest accepted path committed; the same tokens as a chain give the same rows, and the next
+    block's attention is bit for bit the same."""
+    Hq, H, D, page = 4, 2, 64, 16
+    parents = [-1, 0, 0, 1, 1, 2, 3, 5]
+    tree = L.device_tree(parents)
+    paths = [[[1, 3, 6], [2, 5, 7]]]                       # two root-to-leaf paths
+    acc = [[1, 3]]
+    freq, _ = jd.rope_frequencies(D, 10000.0)
+    rotary = jd.Rotary(freq.cuda())
+    a = L.filled_cache([37], 0, page=page, max_nodes=8, seed=3, spare=6)
+    b = L.filled_cache([37], 0, page=page, max_nodes=8, seed=3, spare=6)
+    T = len(parents)
+    k, v, q = rand((1, T, H, D), 1), rand((1, T, H, D), 2), rand((1, T, Hq, D), 3)
+    a.reserve(T)
+    qa = a.append(0, k, v, tree, rotary=rotary, q=q)
+    oa = a.attend(0, qa, tree)
+    chosen = a.commit(L.ints(acc), L.ints(paths))
+    assert a.status() == jd.JD_OK and chosen.cpu().tolist() == [1]
+    keep = [0, 2, 5, 7]
+    b.reserve(4)
+    qb = b.append(0, k[:, keep].contiguous(), v[:, keep].contiguous(), rotary=rotary, q=q[:, keep].contiguous())
+    ob = b.attend(0, qb)
+    b.commit(L.ints([3]), path_len=3)
+    assert torch.equal(qa[:, keep], qb)
+    # same rows, other tile columns: the softmax weights' sums run in another order
+    assert (oa["out"][:, keep].float() - ob["out"].float()).abs().max() <= 2.0 ** -7 * ob["out"].float().abs().max()
+    assert torch.equal(a.seq_len, b.seq_len) and torch.equal(a.held, b.held)
+    nxt = rand((1, 3, Hq, D), 7)
+    for c in (a, b):
+        c.reserve(3)
+        c.append(0, rand((1, 3, H, D), 8), rand((1, 3, H, D), 9))
+    oa, ob = a.attend(0, nxt), b.attend(0, nxt)
+    assert torch.equal(oa["out"], ob["out"]) and torch.equal(oa["lse"], ob["lse"])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_captured_step_replays(dtype):
+    """A whole step in a CUDA graph, replayed while lengths grow: the lengths are read on the device."""
+    B, T, layers, Hq, H, D = 2, 3, 2, 4, 2, 64
+    freq, _ = jd.rope_frequencies(D, 10000.0)
+    rotary = jd.Rotary(freq.cuda())
+    eager = L.filled_cache([30, 2], 0, page=8, layers=layers, max_nodes=T, dtype=dtype, spare=40, seed=1)
+    graph = L.filled_cache([30, 2], 0, page=8, layers=layers, max_nodes=T, dtype=dtype, spare=40, seed=1)
+    k, v, q = rand((B, T, H, D), 1, dtype), rand((B, T, H, D), 2, dtype), rand((B, T, Hq, D), 3, dtype)
+    acc = L.ints([2, 1])
+
+    def step(c, q_out, out, chosen):
+        c.reserve(T)
+        for layer in range(layers):
+            c.append(layer, k, v, rotary=rotary, q=q, q_out=q_out)
+            c.attend(layer, q_out, out=out)
+        c.commit(acc, chosen=chosen, path_len=T - 1)
+
+    bufs = [(torch.empty_like(q), dict(out=torch.empty_like(q), lse=torch.empty(B, T, Hq, device="cuda")),
+             torch.empty(B, dtype=torch.int32, device="cuda")) for _ in range(2)]
+    g = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(g, stream=side):
+        step(graph, *bufs[1])
+    for _ in range(5):
+        step(eager, *bufs[0])
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(bufs[0][1]["out"], bufs[1][1]["out"]) and torch.equal(bufs[0][1]["lse"], bufs[1][1]["lse"])
+        for name in ("page_table", "seq_len", "held", "refs", "free_bits", "k", "v"):
+            assert torch.equal(getattr(eager, name), getattr(graph, name)), name
+    assert eager.seq_len.cpu().tolist() == [45, 12]
+
+
+def test_two_handles_attend_on_two_streams():
+    """Handles on the same buffers, each with its own workspace, at the same time."""
+    a = L.filled_cache([5000, 700], 9, q_heads=8, kv_heads=1, D=128, max_nodes=9, seed=2)
+    b = jd.PagedCache(a.k, a.v, a.page_table, a.seq_len, a.held, a.refs, a.free_bits, q_heads=8, max_nodes=9)
+    qa, qb = rand((2, 9, 8, 128), 1), rand((2, 9, 8, 128), 2)
+    want = a.attend(0, qa), a.attend(0, qb)
+    torch.cuda.synchronize()
+    sa, sb = torch.cuda.Stream(), torch.cuda.Stream()
+    outs = []
+    for _ in range(20):
+        outs.append((a.attend(0, qa, stream=sa), b.attend(0, qb, stream=sb)))
+    torch.cuda.synchronize()
+    for x, y in outs:
+        assert torch.equal(x["out"], want[0]["out"]) and torch.equal(y["out"], want[1]["out"])
