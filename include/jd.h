@@ -442,7 +442,7 @@ typedef struct {
   void* out;                  /* same shape and type, out_stride; not q */
   int64_t q_stride, out_stride;
   float* lse;                 /* [B][T][q_heads] log sum exp of the scaled scores, or NULL */
-  float scale;                /* on q . k, finite */
+  float scale;                /* on q . k, positive and finite */
   int32_t variant;            /* jd_attend_variant_t */
 } jd_attend_args_t;
 

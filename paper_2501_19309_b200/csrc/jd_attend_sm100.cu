@@ -1,9 +1,569 @@
-// Attention of a drafted block on the tensor cores: not written yet, jd_cache_attend takes the CUDA-core kernel.
+// Attention of a drafted block over the paged cache on the tensor cores (bf16, head width 64 or 128).
+//
+// Rows of a (sequence, kv head) are its nodes times the query heads that share the kv head; a CTA takes up to 128 or 256
+// of them through its run of tiles of 128 cached tokens (jd_cache.h says how runs are cut). Per tile and 128 rows:
+//
+//   S = Q K^T            tcgen05.mma, Q and K tiles in shared memory, S (128 x 128 fp32) in tensor memory
+//   P = 2^(S c - m)      a thread per row reads its row of S, keeps the running maximum m and sum l in registers and
+//                        writes P as bf16 over S
+//   O = O + P V          tcgen05.mma with P from tensor memory, V as it lies in its pages (tokens x columns: the
+//                        transposed operand form), O (128 x head width fp32) in tensor memory
+//
+// Two softmax warpgroups keep the tensor pipe busy: with up to 128 rows they take alternate tiles, each with its own O, m
+// and l (two independent chains that meet when the segment ends); with more rows each takes 128 rows of every tile, and
+// K and V are fetched once for both. O is rescaled only when a row's maximum has grown by more than 2^8 since it was last
+// (the weights stay below 2^8 until then, far inside bf16's range), which after the first tiles is rare.
+// A producer warp follows the page table and fetches pages by TMA, a box per page and 64 columns, through a ring of K and V
+// tiles; a fourth role issues the MMAs. Where few rows are attended the call streams K and V once and is bound by HBM:
+// at 26 GB/s and SM a tile of 64 KB takes as long as the tensor pipe needs for two and a half.
+#include <algorithm>
+
 #include "jd_cache.h"
+#include "jd_sm100_ptx.cuh"
 
 namespace jd {
+namespace {
 
-cudaError_t run_attend_tensor(const AttendParams&, const CUtensorMap&, const CUtensorMap&, cudaStream_t) { return cudaErrorNotSupported; }
-bool attend_configure() { return simt_attend_configure(); }
+constexpr int kTile = 1 << kTensorTileShift;   // cached tokens of a tile
+constexpr int kThreads = 320;                  // warps 0-3, 4-7: softmax; 8: TMA; 9: MMA
+constexpr float kLazy = 8.f;                   // log2 of how far a maximum may grow before O is rescaled
+
+template <int D, bool kPair> struct Shape {
+  static constexpr int kChunks = D / 64;                       // 128-byte column groups
+  static constexpr int kChunkBytes = kTile * 128;
+  static constexpr int kTileBytes = kChunks * kChunkBytes;     // one K, V or Q tile
+  static constexpr int kStages = D == 128 ? (kPair ? 4 : 5) : 8;
+  static constexpr int kQTiles = kPair ? 2 : 1;
+};
+
+struct Shared {
+  uint64_t full[8], empty[8];
+  uint64_t s_full[2], p_ready[2], o_done[2], q_ready;
+  uint32_t tmem_base;
+  int abort_flag;
+  int odd_values;                        // the segment's nodes hold values that are not finite
+  int warp_sums[kThreads / 32];
+  uint32_t node_mask[kMaxNodes][kMaxNodes / 32];
+  float ml[2][kTile][2];                 // m and l of the two chains
+  int prefix[kMaxCacheBatch + 1];
+};
+
+template <int D, bool kPair>
+constexpr size_t attend_smem() {
+  using S = Shape<D, kPair>;
+  return 1024 + (sizeof(Shared) + 1023) / 1024 * 1024 + (size_t)(S::kStages + S::kQTiles) * S::kTileBytes;
+}
+
+// Bounded wait that gives up as soon as another role has.
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  for (unsigned it = 0; it < kSpinLimit; ++it) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if (*abort_flag) return false;
+    if (it > 128) __nanosleep(64);
+  }
+  *abort_flag = 1;
+  return false;
+}
+
+__device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+__device__ __forceinline__ uint64_t policy_evict_normal() {
+  uint64_t p;
+  asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
+  return p;
+}
+
+// V tile as the MMA's B operand [tokens x columns], columns contiguous: 128-byte swizzle, 64-column groups kChunkBytes apart,
+// groups of 8 tokens 1024 bytes apart.
+__device__ __forceinline__ uint64_t make_v_desc(uint32_t saddr, uint32_t chunk_bytes) {
+  uint64_t d = 0;
+  d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)(chunk_bytes >> 4) << 16;
+  d |= (uint64_t)(1024u >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+constexpr uint32_t kTransposeB = 1u << 16;
+
+// A from tensor memory: lane = row, two bf16 per column
+__device__ __forceinline__ void umma_bf16_ta(uint32_t tmem_d, uint32_t tmem_a, uint64_t db, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(tmem_d), "r"(tmem_a), "l"(db), "r"(idesc), "r"(acc) : "memory");
+}
+
+__device__ __forceinline__ void ld32_issue(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// keeps what reads the registers behind the wait in front of it (the statement itself is empty)
+__device__ __forceinline__ void pin32(uint32_t* r) {
+#pragma unroll
+  for (int i = 0; i < 32; i += 8)
+    asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7])
+                 :: "memory");
+}
+__device__ __forceinline__ void st16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void st32(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+        "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
+        "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// One stretch of a run inside a segment.
+struct Piece {
+  int b, head, tile0, tiles, all;   // all: tiles of the whole segment
+  SeqExtent ex;
+};
+__device__ __forceinline__ Piece piece_at(const AttendParams& p, const int* prefix, int64_t u, int64_t run1) {
+  Piece x;
+  x.b = seq_of_unit(prefix, p.B, p.c.kv_heads, u);
+  x.all = prefix[x.b + 1] - prefix[x.b];
+  const int64_t in_seq = u - (int64_t)prefix[x.b] * p.c.kv_heads;
+  x.head = (int)(in_seq / x.all);
+  x.tile0 = (int)(in_seq - (int64_t)x.head * x.all);
+  x.tiles = (int)min((int64_t)(x.all - x.tile0), run1 - u);
+  x.ex = seq_extent(p, x.b);
+  return x;
+}
+
+template <int D, bool kPair>
+__global__ void __launch_bounds__(kThreads, 1)
+attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const AttendParams p) {
+  using Sh = Shape<D, kPair>;
+  constexpr int kStages = Sh::kStages, kChunks = Sh::kChunks, kChunkBytes = Sh::kChunkBytes, kTileBytes = Sh::kTileBytes;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  Shared& sh = *reinterpret_cast<Shared*>(smem);
+  uint8_t* q_smem = smem + (sizeof(Shared) + 1023) / 1024 * 1024;
+  uint8_t* ring = q_smem + Sh::kQTiles * kTileBytes;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  volatile int* abort_flag = &sh.abort_flag;
+  const int g = blockIdx.x / p.row_blocks, rb = blockIdx.x - g * p.row_blocks;
+
+  pdl_trigger();
+  tile_prefix(p, sh.prefix, sh.warp_sums);
+  const int64_t units = (int64_t)sh.prefix[p.B] * p.c.kv_heads;
+  const int64_t run0 = run_start(units, p.groups, g), run1 = run_start(units, p.groups, g + 1);
+  if (run0 == run1) return;
+
+  if (tid == 0) {
+    for (int s = 0; s < kStages; ++s) { mbar_init(smem_u32(&sh.full[s]), 1); mbar_init(smem_u32(&sh.empty[s]), 1); }
+    for (int w = 0; w < 2; ++w) {
+      mbar_init(smem_u32(&sh.s_full[w]), 1);
+      mbar_init(smem_u32(&sh.p_ready[w]), 4);
+      mbar_init(smem_u32(&sh.o_done[w]), 1);
+    }
+    mbar_init(smem_u32(&sh.q_ready), 8);
+    sh.abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 9) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem_base)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sh.tmem_base;
+  const uint32_t ring_addr = smem_u32(ring), q_addr = smem_u32(q_smem);
+
+  if (warp == 8) {
+    // ------------------------------------------------------------------ producer: item 2 j = K of tile j, 2 j + 1 = its V
+    const uint64_t policy = p.row_blocks == 1 ? policy_evict_first() : policy_evict_normal();
+    const int shift = p.c.page_shift, box_shift = min(shift, kTensorTileShift), boxes_per_tile = kTile >> box_shift;
+    const int no_row = (int)page_row(p.c, p.c.layers, 0, 0, 0);   // one behind the last: reads as zero
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int64_t u = run0; u < run1 && ok;) {
+      const Piece x = piece_at(p, sh.prefix, u, run1);
+      const int32_t* table = p.c.table + (int64_t)x.ex.slot * p.c.max_pages;
+      auto row_of = [&](int tile) {      // this lane's box of the tile
+        const int at = tile * kTile + (lane << box_shift);
+        if (lane >= boxes_per_tile || at >= x.ex.kv_end) return -1;
+        const int page = __ldg(table + (at >> shift));
+        if (page < 0 || page >= p.c.pages) { set_status(p.c.status, JD_ERR_BAD_INDEX); return no_row; }
+        return (int)page_row(p.c, p.layer, page, x.head, at & (p.c.page_size - 1));
+      };
+      int row = row_of(x.tile0);
+      for (int t = 0; t < x.tiles && ok; ++t) {
+        const int next = t + 1 < x.tiles ? row_of(x.tile0 + t + 1) : -1;
+        const int boxes = __popc(__ballot_sync(0xffffffffu, row >= 0));
+        for (int kv = 0; kv < 2; ++kv) {
+          const uint32_t bar = smem_u32(&sh.full[stage]);
+          if (lane == 0) {
+            ok = wait(smem_u32(&sh.empty[stage]), phase ^ 1u, abort_flag);
+            if (ok) mbar_expect_tx(bar, (uint32_t)(boxes * kChunks) << (box_shift + 7));
+          }
+          ok = __shfl_sync(0xffffffffu, ok, 0);
+          if (!ok) break;
+          if (row >= 0) {
+            const uint32_t dst = ring_addr + stage * kTileBytes + ((uint32_t)lane << (box_shift + 7));
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c)
+              tma_load_2d(dst + c * kChunkBytes, kv ? &tm_v : &tm_k, bar, c * 64, row, policy);
+          }
+          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        }
+        row = next;
+      }
+      u += x.tiles;
+    }
+    if (!ok && lane == 0) set_status(p.c.status, JD_ERR_TIMEOUT);
+  } else if (warp == 9) {
+    // ------------------------------------------------------------------ MMA issue, one thread
+    if (lane == 0) {
+      const uint32_t idesc_s = make_idesc(kTile), idesc_o = make_idesc(D) | kTransposeB;
+      int item = 0;                                  // ring items, counted over the whole run
+      uint32_t p_phase[2] = {0, 0}, q_phase = 0;
+      bool ok = true;
+      auto full_of = [&](int i) {
+        ok = ok && wait(smem_u32(&sh.full[i % kStages]), (uint32_t)(i / kStages) & 1u, abort_flag);
+        tc_fence_after();
+      };
+      auto issue_s = [&](int w, int i) {             // S_w = Q K^T, K in item i
+        if (!ok) return;
+        const uint32_t a = q_addr + (kPair ? w * kTileBytes : 0), b = ring_addr + (i % kStages) * kTileBytes;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const uint32_t off = (k >> 2) * kChunkBytes + (k & 3) * 32;
+          umma_bf16(tmem + w * 128, make_smem_desc(a + off), make_smem_desc(b + off), idesc_s, k > 0);
+        }
+        umma_commit(smem_u32(&sh.s_full[w]));
+      };
+      auto issue_o = [&](int w, int i, bool first) { // O_w (+)= P_w V, V in item i
+        ok = ok && wait(smem_u32(&sh.p_ready[w]), p_phase[w], abort_flag);
+        p_phase[w] ^= 1u;
+        tc_fence_after();
+        if (!ok) return;
+        const uint32_t b = ring_addr + (i % kStages) * kTileBytes;
+#pragma unroll
+        for (int k = 0; k < kTile / 16; ++k)
+          umma_bf16_ta(tmem + 256 + w * 128, tmem + w * 128 + k * 8, make_v_desc(b + k * 2048, kChunkBytes), idesc_o, !first || k > 0);
+        umma_commit(smem_u32(&sh.o_done[w]));
+      };
+      auto release = [&](int i) { if (ok) umma_commit(smem_u32(&sh.empty[i % kStages])); };
+      for (int64_t u = run0; u < run1 && ok;) {
+        const Piece x = piece_at(p, sh.prefix, u, run1);
+        const int n = x.tiles;
+        ok = wait(smem_u32(&sh.q_ready), q_phase, abort_flag);
+        q_phase ^= 1u;
+        tc_fence_after();
+        if (kPair) {
+          full_of(item);
+          issue_s(0, item);
+          issue_s(1, item);
+          release(item);
+          for (int t = 0; t < n && ok; ++t) {
+            const int v = item + 2 * t + 1, k = v + 1;
+            full_of(v);
+            issue_o(0, v, t == 0);
+            if (t + 1 < n) { full_of(k); issue_s(0, k); }
+            issue_o(1, v, t == 0);
+            release(v);
+            if (t + 1 < n) { issue_s(1, k); release(k); }
+          }
+        } else {
+          for (int t = 0; t < min(n, 2); ++t) { full_of(item + 2 * t); issue_s(t, item + 2 * t); release(item + 2 * t); }
+          for (int t = 0; t < n && ok; ++t) {
+            const int v = item + 2 * t + 1, w = t & 1;
+            full_of(v);
+            issue_o(w, v, t < 2);
+            release(v);
+            if (t + 2 < n) { full_of(v + 3); issue_s(w, v + 3); release(v + 3); }
+          }
+        }
+        item += 2 * n;
+        u += n;
+      }
+      if (!ok) set_status(p.c.status, JD_ERR_TIMEOUT);
+    }
+  } else {
+    // ------------------------------------------------------------------ softmax: thread = row
+    const int w = warp >> 2, r = tid & 127;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t t_s = tmem + lanes + w * 128, t_o = tmem + lanes + 256 + w * 128;
+    const int r0 = rb * p.rows_per_block;
+    const int my_row = r0 + r + (kPair ? w * 128 : 0);
+    const int warp_row = my_row - lane;
+    const bool warp_live = warp_row < p.rows;
+    const int t_node = my_row / p.group, gq = my_row - t_node * p.group;
+    const float c2 = p.scale_log2;
+    uint32_t s_phase = 0, o_phase = 0;
+    int tile_count = 0;                              // tiles of the run in front of this piece
+    for (int64_t u = run0; u < run1;) {
+      const Piece x = piece_at(p, sh.prefix, u, run1);
+      const SeqExtent& ex = x.ex;
+      softmax_sync();                                // everybody is through with the last piece's Q, masks and sums
+      for (int i = tid; i < p.T * p.W; i += 256) {
+        const int t = i / p.W, k = i - t * p.W;
+        sh.node_mask[t][k] = t < ex.nodes ? node_word(p, x.b, t, k, ex.nodes) : 0u;
+      }
+      if (tid == 0) sh.odd_values = 0;
+      constexpr int kVecs = D / 8;
+      for (int i = kPair ? r : tid; i < 128 * kVecs; i += kPair ? 128 : 256) {
+        const int row = i / kVecs, c = i - row * kVecs;
+        const int q_row = r0 + (kPair ? w * 128 : 0) + row, t = q_row / p.group, h = q_row - t * p.group;
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (q_row < p.rows && t < ex.nodes)
+          v = __ldg(reinterpret_cast<const uint4*>(p.q + ((int64_t)x.b * p.T + t) * p.q_stride + (int64_t)(x.head * p.group + h) * (D * 2)) + c);
+        *reinterpret_cast<uint4*>(q_smem + (kPair ? w * kTileBytes : 0) + (c >> 3) * kChunkBytes + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = v;
+      }
+      fence_async_proxy();
+      tc_fence_before();
+      softmax_sync();
+      if (lane == 0) mbar_arrive(smem_u32(&sh.q_ready));
+
+      float m = -INFINITY, l = 0.f;
+      int done = 0;                                  // tiles of this piece that this warpgroup has taken
+      for (int t = kPair ? 0 : w; t < x.tiles; t += kPair ? 1 : 2, ++done) {
+        const int kv0 = (x.tile0 + t) * kTile;
+        const bool tail = kv0 + kTile > ex.ctx;      // holds nodes, or ends behind the sequence
+        // V rows that are no tokens may hold anything: 0 x NaN would reach every row. They become zeroes; and so do values of nodes
+        // that are not finite, which the rows that see them get back at the end.
+        if (tail && (!kPair || w == 0)) {
+          const int item = 2 * (tile_count + t) + 1;
+          wait(smem_u32(&sh.full[item % kStages]), (uint32_t)(item / kStages) & 1u, abort_flag);
+          uint8_t* v = ring + (item % kStages) * kTileBytes;
+          const int first = max(0, ex.ctx - kv0), valid = min(kTile, max(0, ex.kv_end - kv0));
+          for (int i = first * kVecs + r; i < kTile * kVecs; i += 128) {
+            const int row = i / kVecs, c = i - row * kVecs;
+            uint4* at = reinterpret_cast<uint4*>(v + (c >> 3) * kChunkBytes + row * 128 + (((c & 7) ^ (row & 7)) << 4));
+            if (row >= valid) { *at = make_uint4(0u, 0u, 0u, 0u); continue; }
+            uint4 y = *at;
+            uint32_t* e = &y.x;
+            bool odd = false;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              if ((e[k] & 0x7F80u) == 0x7F80u) { e[k] &= 0xFFFF0000u; odd = true; }
+              if ((e[k] & 0x7F800000u) == 0x7F800000u) { e[k] &= 0xFFFFu; odd = true; }
+            }
+            if (odd) { *at = y; sh.odd_values = 1; }
+          }
+          fence_async_proxy();
+        }
+        wait(smem_u32(&sh.s_full[w]), s_phase, abort_flag);
+        s_phase ^= 1u;
+        if (warp_live) {
+          tc_fence_after();
+          uint32_t s[128];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) ld32_issue(t_s + k * 32, s + 32 * k);
+          ld_wait();
+#pragma unroll
+          for (int k = 0; k < 4; ++k) pin32(s + 32 * k);
+          if (tail) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const int off = kv0 + 32 * k - ex.ctx, word = off >> 5, valid = ex.kv_end - (kv0 + 32 * k);
+              auto bits_of = [&](int i) { return i < 0 ? 0xFFFFFFFFu : (i < p.W && t_node < p.T ? sh.node_mask[t_node][i] : 0u); };
+              uint32_t see = __funnelshift_r(bits_of(word), bits_of(word + 1), off & 31);
+              if (valid < 32) see &= valid <= 0 ? 0u : (1u << valid) - 1u;
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (!((see >> i) & 1u)) s[32 * k + i] = 0xFF800000u;   // -inf
+            }
+          }
+          float mx[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) mx[k] = __uint_as_float(s[k]);
+#pragma unroll
+          for (int i = 4; i < 128; i += 4)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], __uint_as_float(s[i + k]));
+          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+          // a row that has seen nothing yet has O = 0 and l = 0: its maximum may jump without a rescale
+          const bool grow = top > m && (m == -INFINITY || (top - m) * c2 > kLazy);
+          const float m_new = grow ? top : m;
+          const bool rescale = grow && m != -INFINITY;
+          if (__any_sync(0xffffffffu, rescale) && done > 0) {
+            const float f = rescale ? fast_exp2((m - m_new) * c2) : 1.f;
+            wait(smem_u32(&sh.o_done[w]), o_phase ^ 1u, abort_flag);   // the last product has been added
+            tc_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < D; c += 32) {
+              uint32_t o[32];
+              ld32_issue(t_o + c, o);
+              ld_wait();
+              pin32(o);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+              st32(t_o + c, o);
+            }
+            l *= f;
+          }
+          m = m_new;
+          const float base = m == -INFINITY ? 0.f : m * c2;
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            uint32_t pk[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float a = fast_exp2(fmaf(__uint_as_float(s[32 * k + 2 * i]), c2, -base));
+              const float b = fast_exp2(fmaf(__uint_as_float(s[32 * k + 2 * i + 1]), c2, -base));
+              sum[i & 1] += a;
+              sum[2 + (i & 1)] += b;
+              pk[i] = pack_bf16(a, b);
+            }
+            st16(t_s + k * 16, pk);
+          }
+          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          st_wait();
+          tc_fence_before();
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sh.p_ready[w]));
+        o_phase ^= 1u;
+      }
+      // ---------------------------------------------------------------- the piece's end
+      if (done > 0) wait(smem_u32(&sh.o_done[w]), o_phase ^ 1u, abort_flag);
+      tc_fence_after();
+      const bool whole = x.tiles == x.all;
+      const bool live = my_row < p.rows && t_node < ex.nodes;
+      float f0 = 1.f, f1 = 0.f;                      // factors on O_0 and O_1 (one chain: on its own O)
+      if (!kPair) {
+        sh.ml[w][r][0] = m;
+        sh.ml[w][r][1] = l;
+        softmax_sync();
+        const float m0 = sh.ml[0][r][0], m1 = sh.ml[1][r][0];
+        m = fmaxf(m0, m1);
+        const float base = m == -INFINITY ? 0.f : m;
+        f0 = m0 == -INFINITY ? 0.f : fast_exp2((m0 - base) * c2);
+        f1 = m1 == -INFINITY ? 0.f : fast_exp2((m1 - base) * c2);
+        l = f0 * sh.ml[0][r][1] + f1 * sh.ml[1][r][1];
+      }
+      const bool two = !kPair && x.tiles > 1;
+      if (warp_live) {
+        const float inv = !whole ? 1.f : (l == 0.f ? 0.f : 1.f / l);
+        const int64_t out_row = ((int64_t)x.b * p.T + t_node);
+        const int h = x.head * p.group + gq;
+        float* part = p.part + (((int64_t)blockIdx.x * 2 + (x.tile0 == 0 ? 1 : 0)) * p.part_rows + (my_row - r0)) * (D + kPartPad);
+        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out + out_row * p.out_stride) + (int64_t)h * D;
+        const bool odd = *reinterpret_cast<volatile int*>(&sh.odd_values) != 0;
+        // alternate tiles: the two warpgroups write half of the columns each
+        const int c_begin = kPair ? 0 : w * (D / 2), c_end = kPair ? D : c_begin + D / 2;
+#pragma unroll 1
+        for (int c = c_begin; c < c_end; c += 32) {
+          uint32_t a[32], b[32];
+          ld32_issue((kPair ? t_o : tmem + lanes + 256) + c, a);
+          if (two) ld32_issue(tmem + lanes + 384 + c, b);
+          ld_wait();
+          pin32(a);
+          if (two) pin32(b);
+          float o[32];
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            o[i] = kPair ? __uint_as_float(a[i]) : (f0 == 0.f ? 0.f : __uint_as_float(a[i]) * f0);
+            if (two && f1 != 0.f) o[i] = fmaf(__uint_as_float(b[i]), f1, o[i]);
+          }
+          if (odd && live) {
+            for (int j = 0; j < ex.nodes; ++j) {
+              const int kv = ex.ctx + j;
+              if (kv < x.tile0 * kTile || kv >= (x.tile0 + x.tiles) * kTile || kv >= ex.kv_end || !((sh.node_mask[t_node][j >> 5] >> (j & 31)) & 1u)) continue;
+              const int page = p.c.table[(int64_t)ex.slot * p.c.max_pages + (kv >> p.c.page_shift)];
+              if (page < 0 || page >= p.c.pages) continue;
+              const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(p.c.v) + page_row(p.c, p.layer, page, x.head, kv & (p.c.page_size - 1)) * D + c;
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                const float y = __bfloat162float(v[i]);
+                if (!isfinite(y)) o[i] += y;
+              }
+            }
+          }
+          if (!live) continue;
+          if (whole) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) {
+              uint4 v;
+              v.x = pack_bf16(o[i] * inv, o[i + 1] * inv); v.y = pack_bf16(o[i + 2] * inv, o[i + 3] * inv);
+              v.z = pack_bf16(o[i + 4] * inv, o[i + 5] * inv); v.w = pack_bf16(o[i + 6] * inv, o[i + 7] * inv);
+              *reinterpret_cast<uint4*>(out + c + i) = v;
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(part + c + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+          }
+        }
+        if (live && c_begin == 0) {
+          const float m2 = m * c2;
+          if (whole) {
+            if (p.lse) p.lse[out_row * p.q_heads + h] = l == 0.f ? -INFINITY : (m2 + log2f(l)) * 0.69314718055994531f;
+          } else {
+            *reinterpret_cast<float2*>(part + D) = make_float2(m == -INFINITY ? -INFINITY : m2, l);
+          }
+        }
+      }
+      tc_fence_before();
+      tile_count += x.tiles;
+      u += x.tiles;
+    }
+  }
+
+  __syncthreads();
+  if (sh.abort_flag) {   // copies that are under way land before the block goes
+    for (int i = 0; i < 64; ++i) __nanosleep(2000);
+    __syncthreads();
+  }
+  if (warp == 9) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+  }
+}
+
+template <int D, bool kPair>
+cudaError_t launch(const AttendParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st) {
+  attend_sm100_kernel<D, kPair><<<(unsigned)(p.groups * p.row_blocks), kThreads, attend_smem<D, kPair>(), st>>>(tm_k, tm_v, p);
+  return cudaGetLastError();
+}
+template <int D, bool kPair>
+bool configure() {
+  static_assert(attend_smem<D, kPair>() <= 227 * 1024, "shared memory of an SM");
+  return cudaFuncSetAttribute(attend_sm100_kernel<D, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)attend_smem<D, kPair>()) == cudaSuccess;
+}
+
+}  // namespace
+
+cudaError_t run_attend_tensor(const AttendParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st) {
+  const bool pair = p.rows_per_block > 128;
+  if (p.c.head_dim == 64) return pair ? launch<64, true>(p, tm_k, tm_v, st) : launch<64, false>(p, tm_k, tm_v, st);
+  return pair ? launch<128, true>(p, tm_k, tm_v, st) : launch<128, false>(p, tm_k, tm_v, st);
+}
+
+bool attend_configure() {
+  return simt_attend_configure() && configure<64, false>() && configure<64, true>() && configure<128, false>() && configure<128, true>();
+}
 
 }  // namespace jd

@@ -531,7 +531,7 @@ jd_status_t jd_cache_create(jd_cache_t* out, const jd_cache_config_t* cfg, const
   if (cfg->dtype == JD_DTYPE_BF16 && (cfg->head_dim == 64 || cfg->head_dim == 128)) {
     const uint64_t rows = (uint64_t)cfg->num_layers * cfg->num_pages * cfg->kv_heads * cfg->page_size;
     const uint32_t box = (uint32_t)std::min(cfg->page_size, 1 << kTensorTileShift);
-    c->tm_ok = false && encode_rows(&c->tm_k, b->k_pages, rows, (uint64_t)cfg->head_dim, box) &&
+    c->tm_ok = encode_rows(&c->tm_k, b->k_pages, rows, (uint64_t)cfg->head_dim, box) &&
                encode_rows(&c->tm_v, b->v_pages, rows, (uint64_t)cfg->head_dim, box);
   }
   *out = c;
@@ -585,7 +585,7 @@ jd_status_t jd_cache_attend(jd_cache_t c, const jd_attend_args_t* a, void* cuda_
   if (a->layer < 0 || a->layer >= g.num_layers || !a->q || !a->out || a->q == a->out || !on16(a->q) || !on16(a->out) || !on4(a->lse))
     return JD_ERR_INVALID_ARG;
   const int64_t qd = (int64_t)g.q_heads * g.head_dim;
-  if (!stride_ok(a->q_stride, qd, e) || !stride_ok(a->out_stride, qd, e) || !std::isfinite(a->scale)) return JD_ERR_INVALID_ARG;
+  if (!stride_ok(a->q_stride, qd, e) || !stride_ok(a->out_stride, qd, e) || !(a->scale > 0.f && std::isfinite(a->scale))) return JD_ERR_INVALID_ARG;
   if (a->variant < JD_ATTEND_AUTO || a->variant > JD_ATTEND_TENSOR) return JD_ERR_INVALID_ARG;
   if (a->variant == JD_ATTEND_TENSOR && !c->tm_ok) return JD_ERR_UNSUPPORTED;
   const bool tensor = a->variant != JD_ATTEND_SIMT && c->tm_ok;

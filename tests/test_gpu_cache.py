@@ -169,7 +169,17 @@ ATTEND = [  # lens, T, page, q_heads, kv_heads, D, dtype, variant, tree
     ([300, 2], 9, 32, 6, 2, 80, "f32", "simt", "star"),
     ([37], 128, 8, 5, 1, 200, "f32", "simt", "tree"),
     ([1000], 3, 128, 8, 8, 8, "f32", "simt", "chain"),
-    ([500, 1], 33, 64, 16, 1, 128, "bf16", "simt", "tree")]
+    ([500, 1], 33, 64, 16, 1, 128, "bf16", "simt", "tree"),
+    ([0], 1, 16, 1, 1, 64, "bf16", "tensor", "chain"),
+    ([0, 1, 2], 1, 8, 8, 1, 128, "bf16", "tensor", "chain"),
+    ([1, 0, 63, 64, 65, 127, 128, 129], 5, 16, 4, 2, 64, "bf16", "tensor", "tree"),
+    ([255, 256, 257, 120, 383], 9, 32, 8, 2, 128, "bf16", "tensor", "tree"),
+    ([700, 33], 26, 64, 8, 1, 128, "bf16", "tensor", "star"),             # 208 rows: two row tiles
+    ([500, 127], 26, 128, 32, 2, 128, "bf16", "tensor", "tree"),          # 416 rows: two blocks
+    ([100, 4000, 3], 128, 16, 4, 1, 64, "bf16", "tensor", "tree"),        # 512 rows
+    ([2000, 5], 127, 256, 3, 1, 128, "bf16", "tensor", "chain"),
+    ([5000], 1, 1024, 5, 5, 64, "bf16", "tensor", "chain"),
+    ([20000], 2, 16, 16, 1, 128, "bf16", "tensor", "tree")]               # one segment over all SMs
 
 
 def run_attend(c, m, T, parents, dtype, variant, seed, slots=None, num_nodes=None, scale=None, layer=0, B=None):
@@ -210,7 +220,7 @@ def test_attend(lens, T, page, q_heads, kv_heads, D, dtype, variant, style):
     assert torch.equal(r[0]["out"], again[0]["out"]) and torch.equal(r[0]["lse"], again[0]["lse"])
 
 
-VARIANTS = [("simt", "bf16", 64), ("simt", "f32", 72)]
+VARIANTS = [("simt", "bf16", 64), ("simt", "f32", 72), ("tensor", "bf16", 64), ("tensor", "bf16", 128)]
 
 
 @pytest.mark.parametrize("variant,dtype,D", VARIANTS)
@@ -302,7 +312,7 @@ def test_attend_strided_queries_and_outputs(variant, dtype, D):
     assert torch.equal(a["out"], b["out"]) and bool((buf[:, :, 0] == 0).all()) and bool((buf[:, :, 5] == 0).all())
 
 
-@pytest.mark.parametrize("variant", ["simt"])
+@pytest.mark.parametrize("variant", ["simt", "tensor"])
 def test_attend_beyond_four_gigabytes(variant):
     """The sequence's pages lie at both ends of a pool of more than 2^32 bytes and 2^31 elements."""
     page, H, D, layers = 64, 8, 128, 2
@@ -462,7 +472,8 @@ def test_refusals():
     refused(lambda: c.attend(0, rand((2, 5, 4, 64), 1)))                  # more nodes than max_nodes
     refused(lambda: c.attend(0, rand((3, 4, 4, 64), 1)))                  # more sequences than slots
     refused(lambda: c.attend(0, q, out=dict(out=q)))
-    refused(lambda: c.attend(0, q, scale=float("nan")))
+    for scale in (float("nan"), float("inf"), 0.0, -0.1):
+        refused(lambda: c.attend(0, q, scale=scale))
     refused(lambda: c.attend(0, q, variant=3))
     refused(lambda: c.reserve(0))
     refused(lambda: c.commit(L.ints([1, 1]), path_len=4))
