@@ -58,8 +58,8 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(AttendParams p) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int g = blockIdx.x / p.row_blocks, rb = blockIdx.x - g * p.row_blocks;
   const int r0 = rb * kRows, nrows = min(kRows, p.rows - r0);
-  tile_prefix(p, prefix, warp_sums);
   pdl_trigger();
+  unit_prefix(p, prefix, warp_sums);
   const int64_t units = (int64_t)prefix[p.B] * p.c.kv_heads;
   if (units == 0) return;
   const int64_t run0 = run_start(units, p.groups, g), run1 = run_start(units, p.groups, g + 1);
@@ -67,11 +67,10 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(AttendParams p) {
   const T* vbase = reinterpret_cast<const T*>(p.c.v);
 
   for (int64_t u = run0; u < run1;) {
-    const int b = seq_of_unit(prefix, p.B, p.c.kv_heads, u);
-    const int tiles = prefix[b + 1] - prefix[b];
-    const int64_t in_seq = u - (int64_t)prefix[b] * p.c.kv_heads;
-    const int head = (int)(in_seq / tiles), tile0 = (int)(in_seq - (int64_t)head * tiles);
-    const int ntiles = (int)min((int64_t)(tiles - tile0), run1 - u);
+    const Piece x = piece_at(p, prefix, u, run1);
+    u = x.next;
+    if (x.tiles == 0) continue;
+    const int b = x.b, head = x.head, tiles = x.all, tile0 = x.tile0, ntiles = x.tiles;
     const SeqExtent ex = seq_extent(p, b);
 
     __syncthreads();   // the previous segment's buffers are free
@@ -240,30 +239,34 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(AttendParams p) {
         if (d == 0) { part[D] = s_m[r]; part[D + 1] = s_l[r]; }
       }
     }
-    u += ntiles;
   }
 }
 
-// Joins the partial results: a warp per query row of a segment that was split; rows of whole segments are written already.
+// Joins the partial results of split segments; rows of whole segments are written already.
 // out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i over the parts in order.
+// A block takes one query row at a time, 128 columns by the lanes of a warp, and its warps take the parts in turn, eight loads in
+// flight each: a row of one long sequence has a part from every SM, and what the join costs is their latency. The warps'
+// sums meet in shared memory. Everything up to the first part is read before the attention kernel has ended.
+constexpr int kJoinWarps = 4;
 template <typename T>
-__global__ void __launch_bounds__(256) attend_join_kernel(AttendParams p) {
-  __shared__ int prefix[kMaxCacheBatch + 1], warp_sums[8];
-  pdl_wait();
-  tile_prefix(p, prefix, warp_sums);
+__global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendParams p) {
+  __shared__ int prefix[kMaxCacheBatch + 1], warp_sums[kJoinWarps];
+  __shared__ float4 s_o[kJoinWarps][2][32];
+  __shared__ float2 s_ml[kJoinWarps];
+  unit_prefix(p, prefix, warp_sums);
   const int64_t units = (int64_t)prefix[p.B] * p.c.kv_heads;
-  if (units == 0) return;
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int D = p.c.head_dim, pitch = D + kPartPad;
   const int64_t all = (int64_t)p.B * p.c.kv_heads * p.rows;
-  for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < all; i += (int64_t)gridDim.x * 8) {
-    const int row = (int)(i % p.rows);
+  bool waited = false;
+  for (int64_t i = blockIdx.x; i < all; i += gridDim.x) {
     const int64_t seg = i / p.rows;
-    const int head = (int)(seg % p.c.kv_heads), b = (int)(seg / p.c.kv_heads);
-    const int tiles = prefix[b + 1] - prefix[b];
-    if (tiles == 0) continue;
-    const int64_t u0 = (int64_t)prefix[b] * p.c.kv_heads + (int64_t)head * tiles;
-    const int g0 = run_of(units, p.groups, u0), g1 = run_of(units, p.groups, u0 + tiles - 1);
+    const int row = (int)(i - seg * p.rows);
+    const int b = (int)(seg / p.c.kv_heads), head = (int)(seg - (int64_t)b * p.c.kv_heads);
+    const int n = prefix[b + 1] - prefix[b];
+    if (n == 0) continue;
+    const int64_t u0 = (int64_t)prefix[b] * p.c.kv_heads + (int64_t)head * n;
+    const int g0 = run_of(units, p.groups, u0 + p.seg_cost), g1 = run_of(units, p.groups, u0 + n - 1);
     if (g0 == g1) continue;
     const int t = row / p.group, nodes = p.num_nodes ? min(max(__ldg(p.num_nodes + b), 0), p.T) : p.T;
     if (t >= nodes) continue;
@@ -271,37 +274,78 @@ __global__ void __launch_bounds__(256) attend_join_kernel(AttendParams p) {
     auto part_of = [&](int g) {
       return p.part + (((int64_t)(g * p.row_blocks + rb) * 2 + (g == g0 ? 1 : 0)) * p.part_rows + r) * pitch;
     };
-    float m = -INFINITY;
-    for (int g = g0 + lane; g <= g1; g += 32) m = fmaxf(m, __ldcg(part_of(g) + D));
+    if (!waited) { pdl_wait(); waited = true; }
+    const int d = lane * 4;
+    // this warp's parts: a running maximum, sum and numerators (columns 4 lane and 128 + 4 lane)
+    float m = -INFINITY, l = 0.f, o[2][4] = {};
+    constexpr int kBatch = 8;
+    for (int first = g0 + warp; first <= g1; first += kJoinWarps * kBatch) {
+      float2 ml[kBatch];
+      float4 x[kBatch][2];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    const float base = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
-    const int h = head * p.group + row - t * p.group;
-    T* out = reinterpret_cast<T*>(p.out + ((int64_t)b * p.T + t) * p.out_stride) + (int64_t)h * D;
-    for (int d0 = 0; d0 < D; d0 += 128) {
-      const int d = d0 + lane * 4;
-      float o[4] = {0.f, 0.f, 0.f, 0.f};
-      l = 0.f;
-#pragma unroll 4
-      for (int g = g0; g <= g1; ++g) {
-        const float* part = part_of(g);
-        const float2 ml = __ldcg(reinterpret_cast<const float2*>(part + D));
-        const float f = exp2f(ml.x - base);
-        l += f * ml.y;
-        if (d < D && ml.x != -INFINITY) {   // a part that saw nothing has no say, whatever it holds
-          const float4 x = __ldcg(reinterpret_cast<const float4*>(part + d));
-          o[0] = fmaf(f, x.x, o[0]); o[1] = fmaf(f, x.y, o[1]); o[2] = fmaf(f, x.z, o[2]); o[3] = fmaf(f, x.w, o[3]);
+      for (int k = 0; k < kBatch; ++k) {
+        const int gg = first + k * kJoinWarps;
+        ml[k] = make_float2(-INFINITY, 0.f);
+        x[k][0] = x[k][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (gg <= g1) {
+          const float* part = part_of(gg);
+          ml[k] = __ldcg(reinterpret_cast<const float2*>(part + D));
+          if (d < D) x[k][0] = __ldcg(reinterpret_cast<const float4*>(part + d));
+          if (d + 128 < D) x[k][1] = __ldcg(reinterpret_cast<const float4*>(part + d + 128));
         }
       }
-      const float inv = l == 0.f ? 0.f : 1.f / l;
+      float top = m;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) o[k] *= inv;
-      if (d < D) store4(out + d, o);
+      for (int k = 0; k < kBatch; ++k) top = fmaxf(top, ml[k].x);
+      const float base = top == -INFINITY ? 0.f : top, f0 = exp2f(m - base);
+      l *= f0;
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[j][e] *= f0;
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const float f = exp2f(ml[k].x - base);
+        l += f * ml[k].y;
+        if (ml[k].x == -INFINITY) continue;   // a part that saw nothing has no say, whatever it holds
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          o[j][0] = fmaf(f, x[k][j].x, o[j][0]); o[j][1] = fmaf(f, x[k][j].y, o[j][1]);
+          o[j][2] = fmaf(f, x[k][j].z, o[j][2]); o[j][3] = fmaf(f, x[k][j].w, o[j][3]);
+        }
+      }
+      m = top;
     }
-    if (p.lse && lane == 0)
-      p.lse[((int64_t)b * p.T + t) * p.q_heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+    __syncthreads();   // the last row's sums have been read
+    s_o[warp][0][lane] = make_float4(o[0][0], o[0][1], o[0][2], o[0][3]);
+    s_o[warp][1][lane] = make_float4(o[1][0], o[1][1], o[1][2], o[1][3]);
+    if (lane == 0) s_ml[warp] = make_float2(m, l);
+    __syncthreads();
+    if (warp < 2) {    // columns 128 warp ..
+      float top = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, s_ml[w].x);
+      const float base = top == -INFINITY ? 0.f : top;
+      float sum = 0.f, y[4] = {};
+#pragma unroll
+      for (int w = 0; w < kJoinWarps; ++w) {
+        const float f = exp2f(s_ml[w].x - base);
+        const float4 x = s_o[w][warp][lane];
+        sum += f * s_ml[w].y;
+        if (s_ml[w].x == -INFINITY) continue;
+        y[0] = fmaf(f, x.x, y[0]); y[1] = fmaf(f, x.y, y[1]); y[2] = fmaf(f, x.z, y[2]); y[3] = fmaf(f, x.w, y[3]);
+      }
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] *= inv;
+      const int h = head * p.group + row - t * p.group;
+      if (d + 128 * warp < D)
+        store4(reinterpret_cast<T*>(p.out + ((int64_t)b * p.T + t) * p.out_stride) + (int64_t)h * D + d + 128 * warp, y);
+      if (p.lse && warp == 0 && lane == 0)
+        p.lse[((int64_t)b * p.T + t) * p.q_heads + h] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
+    }
   }
+  if (!waited) pdl_wait();   // the next kernel on the stream counts on the attention having ended when this one has
 }
 
 template <typename T>
@@ -324,9 +368,9 @@ cudaError_t run_attend_simt(const AttendParams& p, int dtype, cudaStream_t st) {
 
 cudaError_t run_attend_join(const AttendParams& p, int dtype, cudaStream_t st) {
   const int64_t rows = (int64_t)p.B * p.c.kv_heads * p.rows;
-  const unsigned blocks = (unsigned)std::min<int64_t>((rows + 7) / 8, 8 * kMaxCtas);
-  return dtype == JD_DTYPE_F32 ? launch_chained(attend_join_kernel<float>, dim3(blocks), dim3(256), 0, st, p)
-                               : launch_chained(attend_join_kernel<__nv_bfloat16>, dim3(blocks), dim3(256), 0, st, p);
+  const unsigned blocks = (unsigned)std::min<int64_t>(rows, 8 * kMaxCtas);
+  return dtype == JD_DTYPE_F32 ? launch_chained(attend_join_kernel<float>, dim3(blocks), dim3(32 * kJoinWarps), 0, st, p)
+                               : launch_chained(attend_join_kernel<__nv_bfloat16>, dim3(blocks), dim3(32 * kJoinWarps), 0, st, p);
 }
 
 bool simt_attend_configure() {

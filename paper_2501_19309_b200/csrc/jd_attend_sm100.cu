@@ -25,7 +25,8 @@ namespace jd {
 namespace {
 
 constexpr int kTile = 1 << kTensorTileShift;   // cached tokens of a tile
-constexpr int kThreads = 320;                  // warps 0-3, 4-7: softmax; 8: TMA; 9: MMA
+constexpr int kThreads = 384;                  // warps 0-3, 4-7: softmax; 8: TMA; 9: MMA; 10, 11: idle
+constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;   // 2 x 128 x 216 + 128 x 72 = 384 x 168, what the block is launched with
 constexpr float kLazy = 8.f;                   // log2 of how far a maximum may grow before O is rescaled
 
 template <int D, bool kPair> struct Shape {
@@ -38,7 +39,7 @@ template <int D, bool kPair> struct Shape {
 
 struct Shared {
   uint64_t full[8], empty[8];
-  uint64_t s_full[2], p_ready[2], o_done[2], q_ready;
+  uint64_t s_full[2], p_ready[2][2], o_done[2], q_ready;   // p_ready: first and second 64 columns of P
   uint32_t tmem_base;
   int abort_flag;
   int odd_values;                        // the segment's nodes hold values that are not finite
@@ -46,6 +47,7 @@ struct Shared {
   uint32_t node_mask[kMaxNodes][kMaxNodes / 32];
   float ml[2][kTile][2];                 // m and l of the two chains
   int prefix[kMaxCacheBatch + 1];
+  SeqExtent extents[kMaxCacheBatch];
 };
 
 template <int D, bool kPair>
@@ -141,21 +143,38 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return r;
 }
 
-// One stretch of a run inside a segment.
-struct Piece {
-  int b, head, tile0, tiles, all;   // all: tiles of the whole segment
-  SeqExtent ex;
-};
-__device__ __forceinline__ Piece piece_at(const AttendParams& p, const int* prefix, int64_t u, int64_t run1) {
-  Piece x;
-  x.b = seq_of_unit(prefix, p.B, p.c.kv_heads, u);
-  x.all = prefix[x.b + 1] - prefix[x.b];
-  const int64_t in_seq = u - (int64_t)prefix[x.b] * p.c.kv_heads;
-  x.head = (int)(in_seq / x.all);
-  x.tile0 = (int)(in_seq - (int64_t)x.head * x.all);
-  x.tiles = (int)min((int64_t)(x.all - x.tile0), run1 - u);
-  x.ex = seq_extent(p, x.b);
-  return x;
+// one lane of the converged warp
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xFFFFFFFF;\n\tselp.b32 %0, 1, 0, q;\n\t}" : "=r"(p));
+  return p != 0;
+}
+__device__ __forceinline__ int64_t uniform64(int64_t x) {
+  const uint32_t lo = __shfl_sync(0xffffffffu, (uint32_t)x, 0), hi = __shfl_sync(0xffffffffu, (uint32_t)((uint64_t)x >> 32), 0);
+  return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+
+// two float32 at once: one issue slot for two lanes' worth of the FMA pipe
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
 }
 
 template <int D, bool kPair>
@@ -168,21 +187,17 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   Shared& sh = *reinterpret_cast<Shared*>(smem);
   uint8_t* q_smem = smem + (sizeof(Shared) + 1023) / 1024 * 1024;
   uint8_t* ring = q_smem + Sh::kQTiles * kTileBytes;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   volatile int* abort_flag = &sh.abort_flag;
   const int g = blockIdx.x / p.row_blocks, rb = blockIdx.x - g * p.row_blocks;
 
   pdl_trigger();
-  tile_prefix(p, sh.prefix, sh.warp_sums);
-  const int64_t units = (int64_t)sh.prefix[p.B] * p.c.kv_heads;
-  const int64_t run0 = run_start(units, p.groups, g), run1 = run_start(units, p.groups, g + 1);
-  if (run0 == run1) return;
-
   if (tid == 0) {
-    for (int s = 0; s < kStages; ++s) { mbar_init(smem_u32(&sh.full[s]), 1); mbar_init(smem_u32(&sh.empty[s]), 1); }
+    for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&sh.full[i]), 1); mbar_init(smem_u32(&sh.empty[i]), 1); }
     for (int w = 0; w < 2; ++w) {
       mbar_init(smem_u32(&sh.s_full[w]), 1);
-      mbar_init(smem_u32(&sh.p_ready[w]), 4);
+      mbar_init(smem_u32(&sh.p_ready[w][0]), 4);
+      mbar_init(smem_u32(&sh.p_ready[w][1]), 4);
       mbar_init(smem_u32(&sh.o_done[w]), 1);
     }
     mbar_init(smem_u32(&sh.q_ready), 8);
@@ -194,11 +209,15 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
-  __syncthreads();
+  unit_prefix(p, sh.prefix, sh.warp_sums, sh.extents);   // ends with a barrier
   tc_fence_after();
-  const uint32_t tmem = sh.tmem_base;
+  const int64_t units = (int64_t)sh.prefix[p.B] * p.c.kv_heads;
+  const int64_t run0 = run_start(units, p.groups, g), run1 = run_start(units, p.groups, g + 1);
+  const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem_base, 0);
   const uint32_t ring_addr = smem_u32(ring), q_addr = smem_u32(q_smem);
 
+  if (warp >= 8) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
   if (warp == 8) {
     // ------------------------------------------------------------------ producer: item 2 j = K of tile j, 2 j + 1 = its V
     const uint64_t policy = p.row_blocks == 1 ? policy_evict_first() : policy_evict_normal();
@@ -209,10 +228,13 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     bool ok = true;
     for (int64_t u = run0; u < run1 && ok;) {
       const Piece x = piece_at(p, sh.prefix, u, run1);
-      const int32_t* table = p.c.table + (int64_t)x.ex.slot * p.c.max_pages;
+      u = x.next;
+      if (x.tiles == 0) continue;
+      const SeqExtent ex = sh.extents[x.b];
+      const int32_t* table = p.c.table + (int64_t)ex.slot * p.c.max_pages;
       auto row_of = [&](int tile) {      // this lane's box of the tile
         const int at = tile * kTile + (lane << box_shift);
-        if (lane >= boxes_per_tile || at >= x.ex.kv_end) return -1;
+        if (lane >= boxes_per_tile || at >= ex.kv_end) return -1;
         const int page = __ldg(table + (at >> shift));
         if (page < 0 || page >= p.c.pages) { set_status(p.c.status, JD_ERR_BAD_INDEX); return no_row; }
         return (int)page_row(p.c, p.layer, page, x.head, at & (p.c.page_size - 1));
@@ -239,78 +261,103 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         }
         row = next;
       }
-      u += x.tiles;
     }
     if (!ok && lane == 0) set_status(p.c.status, JD_ERR_TIMEOUT);
   } else if (warp == 9) {
-    // ------------------------------------------------------------------ MMA issue, one thread
-    if (lane == 0) {
-      const uint32_t idesc_s = make_idesc(kTile), idesc_o = make_idesc(D) | kTransposeB;
-      int item = 0;                                  // ring items, counted over the whole run
-      uint32_t p_phase[2] = {0, 0}, q_phase = 0;
-      bool ok = true;
-      auto full_of = [&](int i) {
-        ok = ok && wait(smem_u32(&sh.full[i % kStages]), (uint32_t)(i / kStages) & 1u, abort_flag);
-        tc_fence_after();
-      };
-      auto issue_s = [&](int w, int i) {             // S_w = Q K^T, K in item i
-        if (!ok) return;
-        const uint32_t a = q_addr + (kPair ? w * kTileBytes : 0), b = ring_addr + (i % kStages) * kTileBytes;
+    // ------------------------------------------------------------------ MMA issue
+    // The whole warp walks the schedule and one elected lane issues: descriptors and addresses then live in uniform registers,
+    // which is what the instruction takes. (With the walk inside an `if (lane == 0)` every one of a tile's 16 MMAs per
+    // 128 rows moved its operands there first, and the issue took longer than the products.)
+    const uint32_t idesc_s = make_idesc(kTile), idesc_o = make_idesc(D) | kTransposeB;
+    int stage_k = 0, stage_v = 1;                    // ring slots of the next K and V tile, two apart from one tile to the next
+    uint32_t phase_k = 0, phase_v = 0, p_phase[2] = {0, 0}, q_phase = 0;
+    bool ok = true;                                  // after a wait that ran out nothing waits any more; what is issued reads stale tiles
+    auto advance = [](int& stage, uint32_t& phase) { stage += 2; if (stage >= kStages) { stage -= kStages; phase ^= 1u; } };
+    auto await = [&](uint64_t* bar, uint32_t phase) {
+      ok = wait(smem_u32(bar), phase, abort_flag) && ok;
+      __syncwarp();
+      tc_fence_after();
+    };
+    auto commit = [&](uint64_t* bar) { if (elect_one()) umma_commit(smem_u32(bar)); __syncwarp(); };
+    auto issue_s = [&](int w) {                      // S_w = Q K^T
+      const uint64_t a = make_smem_desc(q_addr + (kPair ? w * kTileBytes : 0)), b = make_smem_desc(ring_addr + stage_k * kTileBytes);
+      if (elect_one()) {
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
-          const uint32_t off = (k >> 2) * kChunkBytes + (k & 3) * 32;
-          umma_bf16(tmem + w * 128, make_smem_desc(a + off), make_smem_desc(b + off), idesc_s, k > 0);
+          const uint32_t off = ((k >> 2) * kChunkBytes + (k & 3) * 32) >> 4;
+          if (k == 0) umma_bf16(tmem + w * 128, a + off, b + off, idesc_s, 0u);
+          else umma_bf16(tmem + w * 128, a + off, b + off, idesc_s, 1u);
         }
         umma_commit(smem_u32(&sh.s_full[w]));
-      };
-      auto issue_o = [&](int w, int i, bool first) { // O_w (+)= P_w V, V in item i
-        ok = ok && wait(smem_u32(&sh.p_ready[w]), p_phase[w], abort_flag);
-        p_phase[w] ^= 1u;
-        tc_fence_after();
-        if (!ok) return;
-        const uint32_t b = ring_addr + (i % kStages) * kTileBytes;
+      }
+      __syncwarp();
+    };
+    auto issue_o = [&](int w, uint32_t acc) {        // O_w (+)= P_w V as the halves of P arrive
+      const uint64_t b = make_v_desc(ring_addr + stage_v * kTileBytes, kChunkBytes);
 #pragma unroll
-        for (int k = 0; k < kTile / 16; ++k)
-          umma_bf16_ta(tmem + 256 + w * 128, tmem + w * 128 + k * 8, make_v_desc(b + k * 2048, kChunkBytes), idesc_o, !first || k > 0);
-        umma_commit(smem_u32(&sh.o_done[w]));
-      };
-      auto release = [&](int i) { if (ok) umma_commit(smem_u32(&sh.empty[i % kStages])); };
-      for (int64_t u = run0; u < run1 && ok;) {
-        const Piece x = piece_at(p, sh.prefix, u, run1);
-        const int n = x.tiles;
-        ok = wait(smem_u32(&sh.q_ready), q_phase, abort_flag);
-        q_phase ^= 1u;
-        tc_fence_after();
-        if (kPair) {
-          full_of(item);
-          issue_s(0, item);
-          issue_s(1, item);
-          release(item);
-          for (int t = 0; t < n && ok; ++t) {
-            const int v = item + 2 * t + 1, k = v + 1;
-            full_of(v);
-            issue_o(0, v, t == 0);
-            if (t + 1 < n) { full_of(k); issue_s(0, k); }
-            issue_o(1, v, t == 0);
-            release(v);
-            if (t + 1 < n) { issue_s(1, k); release(k); }
-          }
-        } else {
-          for (int t = 0; t < min(n, 2); ++t) { full_of(item + 2 * t); issue_s(t, item + 2 * t); release(item + 2 * t); }
-          for (int t = 0; t < n && ok; ++t) {
-            const int v = item + 2 * t + 1, w = t & 1;
-            full_of(v);
-            issue_o(w, v, t < 2);
-            release(v);
-            if (t + 2 < n) { full_of(v + 3); issue_s(w, v + 3); release(v + 3); }
+      for (int half = 0; half < 2; ++half) {
+        await(&sh.p_ready[w][half], p_phase[w]);
+        if (elect_one()) {
+#pragma unroll
+          for (int k = half * (kTile / 32); k < (half + 1) * (kTile / 32); ++k)
+            umma_bf16_ta(tmem + 256 + w * 128, tmem + w * 128 + k * 8, b + (k * 2048 >> 4), idesc_o, k == 0 ? acc : 1u);
+          if (half == 1) umma_commit(smem_u32(&sh.o_done[w]));
+        }
+        __syncwarp();
+      }
+      p_phase[w] ^= 1u;
+    };
+    for (int64_t u = uniform64(run0); u < uniform64(run1);) {
+      const Piece x = piece_at(p, sh.prefix, u, run1);
+      const int n = __shfl_sync(0xffffffffu, x.tiles, 0);
+      u = uniform64(x.next);
+      if (n == 0) continue;
+      await(&sh.q_ready, q_phase);
+      q_phase ^= 1u;
+      if constexpr (kPair) {
+        await(&sh.full[stage_k], phase_k);
+        issue_s(0);
+        issue_s(1);
+        commit(&sh.empty[stage_k]);
+        advance(stage_k, phase_k);
+        for (int t = 0; t < n; ++t) {
+          await(&sh.full[stage_v], phase_v);
+          issue_o(0, t > 0);
+          if (t + 1 < n) { await(&sh.full[stage_k], phase_k); issue_s(0); }
+          issue_o(1, t > 0);
+          commit(&sh.empty[stage_v]);
+          advance(stage_v, phase_v);
+          if (t + 1 < n) { issue_s(1); commit(&sh.empty[stage_k]); advance(stage_k, phase_k); }
+        }
+      } else {
+        auto next_s = [&](int w) {
+          await(&sh.full[stage_k], phase_k);
+          issue_s(w);
+          commit(&sh.empty[stage_k]);
+          advance(stage_k, phase_k);
+        };
+        next_s(0);
+        if (n > 1) next_s(1);
+        for (int t = 0; t < n; t += 2) {
+          await(&sh.full[stage_v], phase_v);
+          issue_o(0, t > 0);
+          commit(&sh.empty[stage_v]);
+          advance(stage_v, phase_v);
+          if (t + 2 < n) next_s(0);
+          if (t + 1 < n) {
+            await(&sh.full[stage_v], phase_v);
+            issue_o(1, t > 0);
+            commit(&sh.empty[stage_v]);
+            advance(stage_v, phase_v);
+            if (t + 3 < n) next_s(1);
           }
         }
-        item += 2 * n;
-        u += n;
       }
-      if (!ok) set_status(p.c.status, JD_ERR_TIMEOUT);
     }
+    if (!ok && lane == 0) set_status(p.c.status, JD_ERR_TIMEOUT);
+  }
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
     // ------------------------------------------------------------------ softmax: thread = row
     const int w = warp >> 2, r = tid & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
@@ -325,21 +372,38 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     int tile_count = 0;                              // tiles of the run in front of this piece
     for (int64_t u = run0; u < run1;) {
       const Piece x = piece_at(p, sh.prefix, u, run1);
-      const SeqExtent& ex = x.ex;
+      u = x.next;
+      if (x.tiles == 0) continue;
+      const SeqExtent ex = sh.extents[x.b];
+      // Q rows, eight 16-byte loads in flight; a thread keeps its place within a row
+      constexpr int kVecs = D / 8, kQThreads = kPair ? 128 : 256, kQRows = kQThreads / kVecs;
+      const int q_first = kPair ? r : tid, q_c = q_first % kVecs, q_r = q_first / kVecs;
+      const char* q_seq = p.q + (int64_t)x.b * p.T * p.q_stride + (int64_t)x.head * p.group * (D * 2) + q_c * 16;
+      auto load_q = [&](int i) {
+        const int q_row = r0 + (kPair ? w * 128 : 0) + q_r + i * kQRows, t = q_row / p.group, h = q_row - t * p.group;
+        return q_row < p.rows && t < ex.nodes ? __ldg(reinterpret_cast<const uint4*>(q_seq + t * p.q_stride + h * (D * 2))) : make_uint4(0u, 0u, 0u, 0u);
+      };
+      uint4 q_regs[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) if (i * kQRows < 128) q_regs[i] = load_q(i);
       softmax_sync();                                // everybody is through with the last piece's Q, masks and sums
       for (int i = tid; i < p.T * p.W; i += 256) {
         const int t = i / p.W, k = i - t * p.W;
         sh.node_mask[t][k] = t < ex.nodes ? node_word(p, x.b, t, k, ex.nodes) : 0u;
       }
       if (tid == 0) sh.odd_values = 0;
-      constexpr int kVecs = D / 8;
-      for (int i = kPair ? r : tid; i < 128 * kVecs; i += kPair ? 128 : 256) {
-        const int row = i / kVecs, c = i - row * kVecs;
-        const int q_row = r0 + (kPair ? w * 128 : 0) + row, t = q_row / p.group, h = q_row - t * p.group;
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (q_row < p.rows && t < ex.nodes)
-          v = __ldg(reinterpret_cast<const uint4*>(p.q + ((int64_t)x.b * p.T + t) * p.q_stride + (int64_t)(x.head * p.group + h) * (D * 2)) + c);
-        *reinterpret_cast<uint4*>(q_smem + (kPair ? w * kTileBytes : 0) + (c >> 3) * kChunkBytes + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = v;
+      uint8_t* q_dst = q_smem + (kPair ? w * kTileBytes : 0) + (q_c >> 3) * kChunkBytes;
+#pragma unroll
+      for (int i0 = 0; i0 < 128 / kQRows; i0 += 8) {
+        if (i0 > 0)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) q_regs[i] = load_q(i0 + i);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if ((i0 + i) * kQRows < 128) {
+            const int row = q_r + (i0 + i) * kQRows;
+            *reinterpret_cast<uint4*>(q_dst + row * 128 + (((q_c & 7) ^ (row & 7)) << 4)) = q_regs[i];
+          }
       }
       fence_async_proxy();
       tc_fence_before();
@@ -400,10 +464,12 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
 #pragma unroll
           for (int k = 0; k < 4; ++k) mx[k] = __uint_as_float(s[k]);
 #pragma unroll
-          for (int i = 4; i < 128; i += 4)
+          for (int i = 4; i < 124; i += 8)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], __uint_as_float(s[i + k]));
-          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+            for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], __uint_as_float(s[i + k]), __uint_as_float(s[i + 4 + k]));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], __uint_as_float(s[124 + k]));
+          const float top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
           // a row that has seen nothing yet has O = 0 and l = 0: its maximum may jump without a rescale
           const bool grow = top > m && (m == -INFINITY || (top - m) * c2 > kLazy);
           const float m_new = grow ? top : m;
@@ -426,26 +492,39 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           }
           m = m_new;
           const float base = m == -INFINITY ? 0.f : m * c2;
-          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+          const uint64_t c2_2 = pack2(c2, c2), base_2 = pack2(-base, -base);
+          uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             uint32_t pk[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              const float a = fast_exp2(fmaf(__uint_as_float(s[32 * k + 2 * i]), c2, -base));
-              const float b = fast_exp2(fmaf(__uint_as_float(s[32 * k + 2 * i + 1]), c2, -base));
-              sum[i & 1] += a;
-              sum[2 + (i & 1)] += b;
+              float a, b;
+              unpack2(fma2(pack2(__uint_as_float(s[32 * k + 2 * i]), __uint_as_float(s[32 * k + 2 * i + 1])), c2_2, base_2), a, b);
+              a = fast_exp2(a);
+              b = fast_exp2(b);
+              sum[i & 1] = add2(sum[i & 1], pack2(a, b));
               pk[i] = pack_bf16(a, b);
             }
             st16(t_s + k * 16, pk);
+            if (k == 1) {          // the first half may go
+              st_wait();
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(smem_u32(&sh.p_ready[w][0]));
+            }
           }
-          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          float l0, l1;
+          unpack2(add2(sum[0], sum[1]), l0, l1);
+          l += l0 + l1;
           st_wait();
           tc_fence_before();
+        } else {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&sh.p_ready[w][0]));
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&sh.p_ready[w]));
+        if (lane == 0) mbar_arrive(smem_u32(&sh.p_ready[w][1]));
         o_phase ^= 1u;
       }
       // ---------------------------------------------------------------- the piece's end
@@ -528,7 +607,6 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       }
       tc_fence_before();
       tile_count += x.tiles;
-      u += x.tiles;
     }
   }
 

@@ -607,9 +607,11 @@ jd_status_t jd_cache_attend(jd_cache_t c, const jd_attend_args_t* a, void* cuda_
   p.part = c->part;
   if (tensor) {
     p.tile_shift = kTensorTileShift;
+    p.seg_cost = kTensorSegCost;
     p.rows_per_block = p.rows > 128 ? 256 : 128;
   } else {
     p.tile_shift = kSimtTileShift;
+    p.seg_cost = kSimtSegCost;
     p.rows_per_block = kSimtRows;
   }
   p.part_rows = std::min(p.rows, p.rows_per_block);

@@ -70,11 +70,12 @@ __device__ __forceinline__ void slot_state(const CacheView& c, int slot, int& le
 // ---------------------------------------------------------------------------------------
 // Attention: the call's rows and their division.
 //
-// A (sequence, kv head) pair is a segment of ceil(kv_end / tile) tiles of the cache, at least one. All tiles of all
-// segments, sequence-major, are cut into `groups` runs of equal length, one for each group of `row_blocks` CTAs; the
-// CTAs of a group take the same tiles for different blocks of query rows, so that all but one find them in L2.
-// A run that covers only a part of a segment leaves a partial result (numerator, running maximum, sum); the last
-// part of a segment's first tiles goes to slot 1 of its group and a continuation to slot 0, so two slots are enough.
+// A (sequence, kv head) pair is a segment of ceil(kv_end / tile) tiles of the cache, at least one. Work is counted in units: a
+// segment has seg_cost units for what it costs to begin and end it, and one for each tile. All units of all segments,
+// sequence-major, are cut into `groups` runs of equal length, one for each group of `row_blocks` CTAs; the CTAs of a group
+// take the same tiles for different blocks of query rows, so that all but one find them in L2.
+// A run that covers only a part of a segment's tiles leaves a partial result (numerator, running maximum, sum): in slot 1
+// of its group if the part begins the segment, else in slot 0, so two slots are enough.
 // The cut depends on nothing but the lengths and the SM count: results repeat bit for bit.
 // ---------------------------------------------------------------------------------------
 struct AttendParams {
@@ -86,6 +87,7 @@ struct AttendParams {
   int groups;
   int part_rows;                   // rows of a partial result: min(rows, rows_per_block)
   int tile_shift;
+  int seg_cost;
   const int32_t* slots;
   const uint32_t* mask;
   int64_t mask_stride;             // words between sequences, 0: shared
@@ -114,18 +116,24 @@ __device__ __forceinline__ SeqExtent seq_extent(const AttendParams& p, int b) {
   e.kv_end = min(e.ctx + e.nodes, held << p.c.page_shift);
   return e;
 }
-__device__ __forceinline__ int extent_tiles(const AttendParams& p, const SeqExtent& e) {
+__device__ __forceinline__ int extent_units(const AttendParams& p, const SeqExtent& e) {
   if (e.slot < 0 || e.nodes == 0) return 0;
-  return max(1, (e.kv_end + (1 << p.tile_shift) - 1) >> p.tile_shift);
+  return p.seg_cost + max(1, (e.kv_end + (1 << p.tile_shift) - 1) >> p.tile_shift);
 }
 
-// prefix[b] = tiles of one kv head in the sequences before b, prefix[B] = all; by the whole block.
-__device__ __forceinline__ void tile_prefix(const AttendParams& p, int* prefix, int* warp_sums) {
+// prefix[b] = units of one kv head in the sequences before b, prefix[B] = all; extents (optional): what seq_extent says of each
+// sequence. By the whole block.
+__device__ __forceinline__ void unit_prefix(const AttendParams& p, int* prefix, int* warp_sums, SeqExtent* extents = nullptr) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nthreads = blockDim.x, nwarps = nthreads >> 5;
   int carry = 0;
   for (int b0 = 0; b0 < p.B; b0 += nthreads) {
     const int b = b0 + tid;
-    const int n = b < p.B ? extent_tiles(p, seq_extent(p, b)) : 0;
+    int n = 0;
+    if (b < p.B) {
+      const SeqExtent e = seq_extent(p, b);
+      if (extents) extents[b] = e;
+      n = extent_units(p, e);
+    }
     int x = n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -147,17 +155,40 @@ __device__ __forceinline__ void tile_prefix(const AttendParams& p, int* prefix, 
   __syncthreads();
 }
 
-__device__ __forceinline__ int64_t run_start(int64_t units, int groups, int g) { return units * g / groups; }
-// the group whose run holds unit u
-__device__ __forceinline__ int run_of(int64_t units, int groups, int64_t u) { return (int)(((u + 1) * groups - 1) / units); }
-// the sequence that unit u belongs to: the last b with prefix[b] * kv_heads <= u among those with tiles
-__device__ __forceinline__ int seq_of_unit(const int* prefix, int B, int kv_heads, int64_t u) {
-  int lo = 0, hi = B - 1;
+// First unit of run g, and the run that holds unit u; 32-bit divisions where they are enough (64-bit ones take ten times as long).
+__device__ __forceinline__ int64_t run_start(int64_t units, int groups, int g) {
+  const int64_t n = units * g;
+  return units < (1 << 22) ? (int64_t)((uint32_t)n / (uint32_t)groups) : n / groups;
+}
+__device__ __forceinline__ int run_of(int64_t units, int groups, int64_t u) {
+  const int64_t n = (u + 1) * groups - 1;
+  return units < (1 << 22) ? (int)((uint32_t)n / (uint32_t)units) : (int)(n / units);
+}
+
+// One stretch of a run inside a segment. tiles may be 0: the run holds only units that stand for the segment's fixed cost.
+struct Piece {
+  int b, head, tile0, tiles, all;   // all: tiles of the whole segment
+  int64_t next;                     // first unit behind it
+};
+__device__ __forceinline__ Piece piece_at(const AttendParams& p, const int* prefix, int64_t u, int64_t run1) {
+  Piece x;
+  int lo = 0, hi = p.B - 1;         // the last sequence with units whose first is at or before u
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
-    if ((int64_t)prefix[mid] * kv_heads <= u) lo = mid; else hi = mid - 1;
+    if ((int64_t)prefix[mid] * p.c.kv_heads <= u) lo = mid; else hi = mid - 1;
   }
-  return lo;
+  x.b = lo;
+  const int n = prefix[lo + 1] - prefix[lo];
+  const int64_t first = (int64_t)prefix[lo] * p.c.kv_heads;
+  const int in_seq = (int)(u - first);
+  x.head = (int)((uint32_t)in_seq / (uint32_t)n);
+  const int at = in_seq - x.head * n;
+  const int64_t seg_end = first + (int64_t)(x.head + 1) * n;
+  x.next = min(seg_end, run1);
+  x.all = n - p.seg_cost;
+  x.tile0 = max(0, at - p.seg_cost);
+  x.tiles = max(0, at + (int)(x.next - u) - p.seg_cost) - x.tile0;
+  return x;
 }
 
 // Mask word of node t for nodes 32 w .. 32 w + 31, nodes behind the sequence's last one hidden.
@@ -195,8 +226,8 @@ cudaError_t run_attend_tensor(const AttendParams& p, const CUtensorMap& tm_k, co
 cudaError_t run_attend_join(const AttendParams& p, int dtype, cudaStream_t st);
 bool simt_attend_configure();
 bool attend_configure();   // dynamic shared-memory limits on the current device, once per device
-constexpr int kSimtRows = 16, kSimtTileShift = 6;
-constexpr int kTensorTileShift = 7;
+constexpr int kSimtRows = 16, kSimtTileShift = 6, kSimtSegCost = 1;
+constexpr int kTensorTileShift = 7, kTensorSegCost = 2;
 
 bool rope_valid(const jd_rope_t& r, int head_dim);
 cudaError_t run_append(const CacheView& c, const jd_append_args_t& a, int q_heads, int dtype, cudaStream_t st);
