@@ -25,7 +25,7 @@ namespace jd {
 namespace {
 
 constexpr int kTile = 1 << kTensorTileShift;   // cached tokens of a tile
-constexpr int kThreads = 384;                  // warps 0-3, 4-7: softmax; 8: TMA; 9: MMA; 10, 11: idle
+constexpr int kThreads = 384;                  // warps 0-3, 4-7: softmax; 8, 10: TMA; 9: MMA; 11: idle
 constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;   // 2 x 128 x 216 + 128 x 72 = 384 x 168, what the block is launched with
 constexpr float kLazy = 8.f;                   // log2 of how far a maximum may grow before O is rescaled
 
@@ -218,12 +218,16 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
 
   if (warp >= 8) {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-  if (warp == 8) {
-    // ------------------------------------------------------------------ producer: item 2 j = K of tile j, 2 j + 1 = its V
+  if (warp == 8 || warp == 10) {
+    // ------------------------------------------------------------------ producers: warp 8 fetches K tiles, warp 10 V tiles
+    // Ring items are K and V of the run's tiles in turn. A box costs the issuing warp about 100 cycles, whatever its size, which with
+    // small pages is most of a tile's time: hence a warp each. Page numbers are fetched two tiles ahead.
+    const bool is_v = warp == 10;
+    const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
     const uint64_t policy = p.row_blocks == 1 ? policy_evict_first() : policy_evict_normal();
     const int shift = p.c.page_shift, box_shift = min(shift, kTensorTileShift), boxes_per_tile = kTile >> box_shift;
     const int no_row = (int)page_row(p.c, p.c.layers, 0, 0, 0);   // one behind the last: reads as zero
-    int stage = 0;
+    int stage = is_v ? 1 : 0;
     uint32_t phase = 0;
     bool ok = true;
     for (int64_t u = run0; u < run1 && ok;) {
@@ -232,34 +236,38 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       if (x.tiles == 0) continue;
       const SeqExtent ex = sh.extents[x.b];
       const int32_t* table = p.c.table + (int64_t)ex.slot * p.c.max_pages;
-      auto row_of = [&](int tile) {      // this lane's box of the tile
-        const int at = tile * kTile + (lane << box_shift);
-        if (lane >= boxes_per_tile || at >= ex.kv_end) return -1;
-        const int page = __ldg(table + (at >> shift));
-        if (page < 0 || page >= p.c.pages) { set_status(p.c.status, JD_ERR_BAD_INDEX); return no_row; }
-        return (int)page_row(p.c, p.layer, page, x.head, at & (p.c.page_size - 1));
+      auto token_of = [&](int t) { return (x.tile0 + t) * kTile + (lane << box_shift); };   // this lane's box of tile t
+      auto fetch = [&](int t) {
+        const int at = token_of(t);
+        return t < x.tiles && lane < boxes_per_tile && at < ex.kv_end ? __ldg(table + (at >> shift)) : 0;
       };
-      int row = row_of(x.tile0);
-      for (int t = 0; t < x.tiles && ok; ++t) {
-        const int next = t + 1 < x.tiles ? row_of(x.tile0 + t + 1) : -1;
-        const int boxes = __popc(__ballot_sync(0xffffffffu, row >= 0));
-        for (int kv = 0; kv < 2; ++kv) {
-          const uint32_t bar = smem_u32(&sh.full[stage]);
-          if (lane == 0) {
-            ok = wait(smem_u32(&sh.empty[stage]), phase ^ 1u, abort_flag);
-            if (ok) mbar_expect_tx(bar, (uint32_t)(boxes * kChunks) << (box_shift + 7));
-          }
-          ok = __shfl_sync(0xffffffffu, ok, 0);
-          if (!ok) break;
-          if (row >= 0) {
-            const uint32_t dst = ring_addr + stage * kTileBytes + ((uint32_t)lane << (box_shift + 7));
-#pragma unroll
-            for (int c = 0; c < kChunks; ++c)
-              tma_load_2d(dst + c * kChunkBytes, kv ? &tm_v : &tm_k, bar, c * 64, row, policy);
-          }
-          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+      int page0 = fetch(0), page1 = fetch(1);
+      for (int t = 0; t < x.tiles; ++t) {
+        const int page = page0;
+        page0 = page1;
+        page1 = fetch(t + 2);
+        const int at = token_of(t);
+        const bool mine = lane < boxes_per_tile && at < ex.kv_end;
+        int row = no_row;
+        if (mine) {
+          if (page >= 0 && page < p.c.pages) row = (int)page_row(p.c, p.layer, page, x.head, at & (p.c.page_size - 1));
+          else set_status(p.c.status, JD_ERR_BAD_INDEX);
         }
-        row = next;
+        const int boxes = __popc(__ballot_sync(0xffffffffu, mine));
+        const uint32_t bar = smem_u32(&sh.full[stage]);
+        if (lane == 0) {
+          ok = wait(smem_u32(&sh.empty[stage]), phase ^ 1u, abort_flag);
+          if (ok) mbar_expect_tx(bar, (uint32_t)(boxes * kChunks) << (box_shift + 7));
+        }
+        ok = __shfl_sync(0xffffffffu, ok, 0);
+        if (!ok) break;
+        if (mine) {
+          const uint32_t dst = ring_addr + stage * kTileBytes + ((uint32_t)lane << (box_shift + 7));
+#pragma unroll
+          for (int c = 0; c < kChunks; ++c) tma_load_2d(dst + c * kChunkBytes, tm, bar, c * 64, row, policy);
+        }
+        stage += 2;
+        if (stage >= kStages) { stage -= kStages; phase ^= 1u; }
       }
     }
     if (!ok && lane == 0) set_status(p.c.status, JD_ERR_TIMEOUT);
