@@ -25,7 +25,7 @@ namespace jd {
 namespace {
 
 constexpr int kTile = 1 << kTensorTileShift;   // cached tokens of a tile
-constexpr int kThreads = 384;                  // warps 0-3, 4-7: softmax; 8, 10: TMA; 9: MMA; 11: idle
+constexpr int kThreads = 384;                  // warps 0-3, 4-7: softmax; 8, 10: TMA; 9, 11: MMA
 constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;   // 2 x 128 x 216 + 128 x 72 = 384 x 168, what the block is launched with
 constexpr float kLazy = 8.f;                   // log2 of how far a maximum may grow before O is rescaled
 
@@ -33,13 +33,15 @@ template <int D, bool kPair> struct Shape {
   static constexpr int kChunks = D / 64;                       // 128-byte column groups
   static constexpr int kChunkBytes = kTile * 128;
   static constexpr int kTileBytes = kChunks * kChunkBytes;     // one K, V or Q tile
-  static constexpr int kStages = D == 128 ? (kPair ? 4 : 5) : 8;
+  // A multiple of 4, so that K and V keep to slots of their own and, with alternate tiles, so do the two chains: a slot's barrier is then
+  // only ever waited on by those that used up its previous content, and two phases cannot be taken for one another.
+  static constexpr int kStages = D == 128 ? 4 : 8;
   static constexpr int kQTiles = kPair ? 2 : 1;
 };
 
 struct Shared {
   uint64_t full[8], empty[8];
-  uint64_t s_full[2], p_ready[2][2], o_done[2], q_ready;   // p_ready: first and second 64 columns of P
+  uint64_t s_full[2], p_ready[2][2], o_done[2], q_ready[2];   // p_ready: first and second 64 columns of P
   uint32_t tmem_base;
   int abort_flag;
   int odd_values;                        // the segment's nodes hold values that are not finite
@@ -199,8 +201,8 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       mbar_init(smem_u32(&sh.p_ready[w][0]), 4);
       mbar_init(smem_u32(&sh.p_ready[w][1]), 4);
       mbar_init(smem_u32(&sh.o_done[w]), 1);
+      mbar_init(smem_u32(&sh.q_ready[w]), 8);
     }
-    mbar_init(smem_u32(&sh.q_ready), 8);
     sh.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -271,37 +273,40 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       }
     }
     if (!ok && lane == 0) set_status(p.c.status, JD_ERR_TIMEOUT);
-  } else if (warp == 9) {
+  } else if (!kPair || warp == 9) {
     // ------------------------------------------------------------------ MMA issue
+    // Alternate tiles: warp 9 for chain 0, warp 11 for chain 1, since S -> softmax -> P V -> S is what a chain waits for and each
+    // wait and issue costs its warp some 150 cycles. Every tile for both chains: warp 9 alone, because its order (all of chain 0's
+    // products, then chain 1's) is what keeps one chain's softmax beside the other's products; two warps' products
+    // interleave, the chains fall into step, and the long-context call takes a third longer (342 against 258 us).
     // The whole warp walks the schedule and one elected lane issues: descriptors and addresses then live in uniform registers,
-    // which is what the instruction takes. (With the walk inside an `if (lane == 0)` every one of a tile's 16 MMAs per
-    // 128 rows moved its operands there first, and the issue took longer than the products.)
+    // which is what the instruction takes. (Inside an `if (lane == 0)` every MMA moved its operands there first, and the
+    // issue took longer than the products.)
     const uint32_t idesc_s = make_idesc(kTile), idesc_o = make_idesc(D) | kTransposeB;
-    int stage_k = 0, stage_v = 1;                    // ring slots of the next K and V tile, two apart from one tile to the next
-    uint32_t phase_k = 0, phase_v = 0, p_phase[2] = {0, 0}, q_phase = 0;
+    uint32_t p_phase[2] = {0, 0}, q_phase[2] = {0, 0};
     bool ok = true;                                  // after a wait that ran out nothing waits any more; what is issued reads stale tiles
-    auto advance = [](int& stage, uint32_t& phase) { stage += 2; if (stage >= kStages) { stage -= kStages; phase ^= 1u; } };
     auto await = [&](uint64_t* bar, uint32_t phase) {
       ok = wait(smem_u32(bar), phase, abort_flag) && ok;
       __syncwarp();
       tc_fence_after();
     };
-    auto commit = [&](uint64_t* bar) { if (elect_one()) umma_commit(smem_u32(bar)); __syncwarp(); };
-    auto issue_s = [&](int w) {                      // S_w = Q K^T
-      const uint64_t a = make_smem_desc(q_addr + (kPair ? w * kTileBytes : 0)), b = make_smem_desc(ring_addr + stage_k * kTileBytes);
+    auto slot = [](int item) { return item % kStages; };
+    auto await_item = [&](int item) { await(&sh.full[slot(item)], (uint32_t)(item / kStages) & 1u); };
+    auto issue_s = [&](int w, int item, bool release) {   // S = Q K^T; the last chain that reads K lets it go
+      const uint64_t a = make_smem_desc(q_addr + (kPair ? w * kTileBytes : 0)), b = make_smem_desc(ring_addr + slot(item) * kTileBytes);
       if (elect_one()) {
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
           const uint32_t off = ((k >> 2) * kChunkBytes + (k & 3) * 32) >> 4;
-          if (k == 0) umma_bf16(tmem + w * 128, a + off, b + off, idesc_s, 0u);
-          else umma_bf16(tmem + w * 128, a + off, b + off, idesc_s, 1u);
+          umma_bf16(tmem + w * 128, a + off, b + off, idesc_s, k == 0 ? 0u : 1u);
         }
         umma_commit(smem_u32(&sh.s_full[w]));
+        if (release) umma_commit(smem_u32(&sh.empty[slot(item)]));
       }
       __syncwarp();
     };
-    auto issue_o = [&](int w, uint32_t acc) {        // O_w (+)= P_w V as the halves of P arrive
-      const uint64_t b = make_v_desc(ring_addr + stage_v * kTileBytes, kChunkBytes);
+    auto issue_o = [&](int w, int item, uint32_t acc, bool release) {   // O (+)= P V as the halves of P arrive
+      const uint64_t b = make_v_desc(ring_addr + slot(item) * kTileBytes, kChunkBytes);
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         await(&sh.p_ready[w][half], p_phase[w]);
@@ -309,58 +314,55 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
 #pragma unroll
           for (int k = half * (kTile / 32); k < (half + 1) * (kTile / 32); ++k)
             umma_bf16_ta(tmem + 256 + w * 128, tmem + w * 128 + k * 8, b + (k * 2048 >> 4), idesc_o, k == 0 ? acc : 1u);
-          if (half == 1) umma_commit(smem_u32(&sh.o_done[w]));
+          if (half == 1) {
+            umma_commit(smem_u32(&sh.o_done[w]));
+            if (release) umma_commit(smem_u32(&sh.empty[slot(item)]));
+          }
         }
         __syncwarp();
       }
       p_phase[w] ^= 1u;
     };
+    int base = 0;                                    // ring items of the pieces in front
     for (int64_t u = uniform64(run0); u < uniform64(run1);) {
       const Piece x = piece_at(p, sh.prefix, u, run1);
       const int n = __shfl_sync(0xffffffffu, x.tiles, 0);
       u = uniform64(x.next);
       if (n == 0) continue;
-      await(&sh.q_ready, q_phase);
-      q_phase ^= 1u;
       if constexpr (kPair) {
-        await(&sh.full[stage_k], phase_k);
-        issue_s(0);
-        issue_s(1);
-        commit(&sh.empty[stage_k]);
-        advance(stage_k, phase_k);
+        await(&sh.q_ready[0], q_phase[0]);
+        await(&sh.q_ready[1], q_phase[0]);
+        q_phase[0] ^= 1u;
+        await_item(base);
+        issue_s(0, base, false);
+        issue_s(1, base, true);
         for (int t = 0; t < n; ++t) {
-          await(&sh.full[stage_v], phase_v);
-          issue_o(0, t > 0);
-          if (t + 1 < n) { await(&sh.full[stage_k], phase_k); issue_s(0); }
-          issue_o(1, t > 0);
-          commit(&sh.empty[stage_v]);
-          advance(stage_v, phase_v);
-          if (t + 1 < n) { issue_s(1); commit(&sh.empty[stage_k]); advance(stage_k, phase_k); }
+          const int v = base + 2 * t + 1;
+          const bool more = t + 1 < n;
+          await_item(v);
+          issue_o(0, v, t > 0, false);
+          if (more) { await_item(v + 1); issue_s(0, v + 1, false); }
+          issue_o(1, v, t > 0, true);
+          if (more) issue_s(1, v + 1, true);
         }
       } else {
-        auto next_s = [&](int w) {
-          await(&sh.full[stage_k], phase_k);
-          issue_s(w);
-          commit(&sh.empty[stage_k]);
-          advance(stage_k, phase_k);
-        };
-        next_s(0);
-        if (n > 1) next_s(1);
-        for (int t = 0; t < n; t += 2) {
-          await(&sh.full[stage_v], phase_v);
-          issue_o(0, t > 0);
-          commit(&sh.empty[stage_v]);
-          advance(stage_v, phase_v);
-          if (t + 2 < n) next_s(0);
-          if (t + 1 < n) {
-            await(&sh.full[stage_v], phase_v);
-            issue_o(1, t > 0);
-            commit(&sh.empty[stage_v]);
-            advance(stage_v, phase_v);
-            if (t + 3 < n) next_s(1);
-          }
+        const int w = warp == 11 ? 1 : 0;            // tiles w, w + 2, .. are this chain's
+        if (w < n) {
+          await(&sh.q_ready[w], q_phase[w]);
+          q_phase[w] ^= 1u;
+          await_item(base + 2 * w);
+          issue_s(w, base + 2 * w, true);
+        }
+        for (int t = w; t < n; t += 2) {
+          const int v = base + 2 * t + 1;
+          const bool more = t + 2 < n;
+          await_item(v);                             // ahead of P, so that nothing stands between P's arrival and the products
+          if (more) await_item(v + 3);
+          issue_o(w, v, t > w, true);
+          if (more) issue_s(w, v + 3, true);
         }
       }
+      base += 2 * n;
     }
     if (!ok && lane == 0) set_status(p.c.status, JD_ERR_TIMEOUT);
   }
@@ -416,7 +418,10 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       fence_async_proxy();
       tc_fence_before();
       softmax_sync();
-      if (lane == 0) mbar_arrive(smem_u32(&sh.q_ready));
+      if (lane == 0) {                               // to the chains that have tiles in this piece: no other waits for it
+        mbar_arrive(smem_u32(&sh.q_ready[0]));
+        if (kPair || x.tiles > 1) mbar_arrive(smem_u32(&sh.q_ready[1]));
+      }
 
       float m = -INFINITY, l = 0.f;
       int done = 0;                                  // tiles of this piece that this warpgroup has taken
@@ -424,7 +429,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         const int kv0 = (x.tile0 + t) * kTile;
         const bool tail = kv0 + kTile > ex.ctx;      // holds nodes, or ends behind the sequence
         // V rows that are no tokens may hold anything: 0 x NaN would reach every row. They become zeroes; and so do values of nodes
-        // that are not finite, which the rows that see them get back at the end.
+        // that are not finite, which the rows that see them get back at the end. (Chain 1's products of a tile are issued behind chain 0's.)
         if (tail && (!kPair || w == 0)) {
           const int item = 2 * (tile_count + t) + 1;
           wait(smem_u32(&sh.full[item % kStages]), (uint32_t)(item / kStages) & 1u, abort_flag);

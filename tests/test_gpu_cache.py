@@ -179,6 +179,7 @@ ATTEND = [  # lens, T, page, q_heads, kv_heads, D, dtype, variant, tree
     ([100, 4000, 3], 128, 16, 4, 1, 64, "bf16", "tensor", "tree"),        # 512 rows
     ([2000, 5], 127, 256, 3, 1, 128, "bf16", "tensor", "chain"),
     ([5000], 1, 1024, 5, 5, 64, "bf16", "tensor", "chain"),
+    ([9000, 17, 12000], 4, 8, 4, 1, 128, "bf16", "tensor", "tree"),
     ([20000], 2, 16, 16, 1, 128, "bf16", "tensor", "tree")]               # one segment over all SMs
 
 
