@@ -17,6 +17,7 @@
 // tiles; a fourth role issues the MMAs. Where few rows are attended the call streams K and V once and is bound by HBM:
 // at 26 GB/s and SM a tile of 64 KB takes as long as the tensor pipe needs for two and a half.
 #include <algorithm>
+#include <type_traits>
 
 #include "jd_cache.h"
 #include "jd_sm100_ptx.cuh"
@@ -29,7 +30,15 @@ constexpr int kThreads = 384;                  // warps 0-3, 4-7: softmax; 8, 10
 constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;   // 2 x 128 x 216 + 128 x 72 = 384 x 168, what the block is launched with
 constexpr float kLazy = 8.f;                   // log2 of how far a maximum may grow before O is rescaled
 
-template <int D, bool kPair> struct Shape {
+// How a CTA's rows lie in the 128 rows of an MMA. kPairMode: up to 256 rows, two MMAs, every tile for both chains. Else up to 128 / kMode rows,
+// kMode times over: the copies weigh a kMode-th of a tile's columns each and have zeroes for the rest of P, so that few rows
+// keep all four SM partitions' exponential units busy instead of one; their O, m and l are parts that meet at the end.
+constexpr int kPairMode = 0;
+template <int D, int kMode> struct Shape {
+  static constexpr bool kPair = kMode == kPairMode;
+  static constexpr int kCopies = kPair ? 1 : kMode;
+  static constexpr int kCopyRows = 128 / kCopies;              // rows of a copy
+  static constexpr int kCols = kTile / kCopies;                // columns of S that a thread weighs
   static constexpr int kChunks = D / 64;                       // 128-byte column groups
   static constexpr int kChunkBytes = kTile * 128;
   static constexpr int kTileBytes = kChunks * kChunkBytes;     // one K, V or Q tile
@@ -48,13 +57,14 @@ struct Shared {
   int warp_sums[kThreads / 32];
   uint32_t node_mask[kMaxNodes][kMaxNodes / 32];
   float ml[2][kTile][2];                 // m and l of the two chains
+  float inv[2][kTile / 2];               // 1 / l of a row, for the threads that put its copies together
   int prefix[kMaxCacheBatch + 1];
   SeqExtent extents[kMaxCacheBatch];
 };
 
-template <int D, bool kPair>
+template <int D, int kMode>
 constexpr size_t attend_smem() {
-  using S = Shape<D, kPair>;
+  using S = Shape<D, kMode>;
   return 1024 + (sizeof(Shared) + 1023) / 1024 * 1024 + (size_t)(S::kStages + S::kQTiles) * S::kTileBytes;
 }
 
@@ -113,6 +123,12 @@ __device__ __forceinline__ void ld32_issue(uint32_t taddr, uint32_t* r) {
       : "memory");
 }
 __device__ __forceinline__ void ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void pin16(uint32_t* r) {
+#pragma unroll
+  for (int i = 0; i < 16; i += 8)
+    asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7])
+                 :: "memory");
+}
 // keeps what reads the registers behind the wait in front of it (the statement itself is empty)
 __device__ __forceinline__ void pin32(uint32_t* r) {
 #pragma unroll
@@ -179,10 +195,12 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
-template <int D, bool kPair>
+template <int D, int kMode>
 __global__ void __launch_bounds__(kThreads, 1)
 attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const AttendParams p) {
-  using Sh = Shape<D, kPair>;
+  using Sh = Shape<D, kMode>;
+  constexpr bool kPair = Sh::kPair;
+  constexpr int kCopies = Sh::kCopies, kCopyRows = Sh::kCopyRows, kCols = Sh::kCols;
   constexpr int kStages = Sh::kStages, kChunks = Sh::kChunks, kChunkBytes = Sh::kChunkBytes, kTileBytes = Sh::kTileBytes;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -373,9 +391,9 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t t_s = tmem + lanes + w * 128, t_o = tmem + lanes + 256 + w * 128;
     const int r0 = rb * p.rows_per_block;
-    const int my_row = r0 + r + (kPair ? w * 128 : 0);
-    const int warp_row = my_row - lane;
-    const bool warp_live = warp_row < p.rows;
+    const int copy = r / kCopyRows, col0 = copy * kCols;            // the copy that this warp belongs to, and its columns
+    const int my_row = r0 + r % kCopyRows + (kPair ? w * 128 : 0);
+    const bool warp_live = my_row - lane < p.rows;
     const int t_node = my_row / p.group, gq = my_row - t_node * p.group;
     const float c2 = p.scale_log2;
     uint32_t s_phase = 0, o_phase = 0;
@@ -390,7 +408,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       const int q_first = kPair ? r : tid, q_c = q_first % kVecs, q_r = q_first / kVecs;
       const char* q_seq = p.q + (int64_t)x.b * p.T * p.q_stride + (int64_t)x.head * p.group * (D * 2) + q_c * 16;
       auto load_q = [&](int i) {
-        const int q_row = r0 + (kPair ? w * 128 : 0) + q_r + i * kQRows, t = q_row / p.group, h = q_row - t * p.group;
+        const int q_row = r0 + (kPair ? w * 128 : 0) + (q_r + i * kQRows) % kCopyRows, t = q_row / p.group, h = q_row - t * p.group;
         return q_row < p.rows && t < ex.nodes ? __ldg(reinterpret_cast<const uint4*>(q_seq + t * p.q_stride + h * (D * 2))) : make_uint4(0u, 0u, 0u, 0u);
       };
       uint4 q_regs[8];
@@ -455,33 +473,38 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         s_phase ^= 1u;
         if (warp_live) {
           tc_fence_after();
-          uint32_t s[128];
+          uint32_t s[kCols];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) ld32_issue(t_s + k * 32, s + 32 * k);
+          for (int k = 0; k < kCols; k += 32) ld32_issue(t_s + col0 + k, s + k);
           ld_wait();
 #pragma unroll
-          for (int k = 0; k < 4; ++k) pin32(s + 32 * k);
+          for (int k = 0; k < kCols; k += 32) pin32(s + k);
+          if constexpr (kCopies > 1) {               // the other copies' columns of P
+            const uint32_t zero[16] = {};
+#pragma unroll
+            for (int k = 0; k < (kTile - kCols) / 2; k += 16) st16(t_s + ((col0 / 2 + kCols / 2 + k) & (kTile / 2 - 1)), zero);
+          }
           if (tail) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const int off = kv0 + 32 * k - ex.ctx, word = off >> 5, valid = ex.kv_end - (kv0 + 32 * k);
+            for (int k = 0; k < kCols; k += 32) {
+              const int at = kv0 + col0 + k, off = at - ex.ctx, word = off >> 5, valid = ex.kv_end - at;
               auto bits_of = [&](int i) { return i < 0 ? 0xFFFFFFFFu : (i < p.W && t_node < p.T ? sh.node_mask[t_node][i] : 0u); };
               uint32_t see = __funnelshift_r(bits_of(word), bits_of(word + 1), off & 31);
               if (valid < 32) see &= valid <= 0 ? 0u : (1u << valid) - 1u;
 #pragma unroll
               for (int i = 0; i < 32; ++i)
-                if (!((see >> i) & 1u)) s[32 * k + i] = 0xFF800000u;   // -inf
+                if (!((see >> i) & 1u)) s[k + i] = 0xFF800000u;   // -inf
             }
           }
           float mx[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) mx[k] = __uint_as_float(s[k]);
 #pragma unroll
-          for (int i = 4; i < 124; i += 8)
+          for (int i = 4; i < kCols - 4; i += 8)
 #pragma unroll
             for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], __uint_as_float(s[i + k]), __uint_as_float(s[i + 4 + k]));
 #pragma unroll
-          for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], __uint_as_float(s[124 + k]));
+          for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], __uint_as_float(s[kCols - 4 + k]));
           const float top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
           // a row that has seen nothing yet has O = 0 and l = 0: its maximum may jump without a rescale
           const bool grow = top > m && (m == -INFINITY || (top - m) * c2 > kLazy);
@@ -508,7 +531,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           const uint64_t c2_2 = pack2(c2, c2), base_2 = pack2(-base, -base);
           uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
+          for (int k = 0; k < kCols / 32; ++k) {
             uint32_t pk[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -519,8 +542,8 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
               sum[i & 1] = add2(sum[i & 1], pack2(a, b));
               pk[i] = pack_bf16(a, b);
             }
-            st16(t_s + k * 16, pk);
-            if (k == 1) {          // the first half may go
+            st16(t_s + col0 / 2 + k * 16, pk);
+            if (kCopies == 1 && k == 1) {   // the first half may go
               st_wait();
               tc_fence_before();
               __syncwarp();
@@ -532,12 +555,12 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           l += l0 + l1;
           st_wait();
           tc_fence_before();
-        } else {
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&sh.p_ready[w][0]));
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&sh.p_ready[w][1]));
+        if (lane == 0) {
+          if (kCopies > 1 || !warp_live) mbar_arrive(smem_u32(&sh.p_ready[w][0]));
+          mbar_arrive(smem_u32(&sh.p_ready[w][1]));
+        }
         o_phase ^= 1u;
       }
       // ---------------------------------------------------------------- the piece's end
@@ -545,77 +568,118 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       tc_fence_after();
       const bool whole = x.tiles == x.all;
       const bool live = my_row < p.rows && t_node < ex.nodes;
-      float f0 = 1.f, f1 = 0.f;                      // factors on O_0 and O_1 (one chain: on its own O)
-      if (!kPair) {
+      float f0 = 1.f, f1 = 0.f;                      // factors on this lane's O_0 and O_1 (pair mode: on its own O)
+      if constexpr (!kPair) {
         sh.ml[w][r][0] = m;
         sh.ml[w][r][1] = l;
         softmax_sync();
+        tc_fence_after();
         const float m0 = sh.ml[0][r][0], m1 = sh.ml[1][r][0];
-        m = fmaxf(m0, m1);
+        m = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 2 * kCopies; ++i) m = fmaxf(m, sh.ml[i & 1][(i >> 1) * kCopyRows + r % kCopyRows][0]);
         const float base = m == -INFINITY ? 0.f : m;
         f0 = m0 == -INFINITY ? 0.f : fast_exp2((m0 - base) * c2);
         f1 = m1 == -INFINITY ? 0.f : fast_exp2((m1 - base) * c2);
-        l = f0 * sh.ml[0][r][1] + f1 * sh.ml[1][r][1];
+        l = 0.f;
+#pragma unroll
+        for (int i = 0; i < 2 * kCopies; ++i) {
+          const float* ml = sh.ml[i & 1][(i >> 1) * kCopyRows + r % kCopyRows];
+          l += (ml[0] == -INFINITY ? 0.f : fast_exp2((ml[0] - base) * c2)) * ml[1];
+        }
+        if (kCopies > 1 && copy == 0) sh.inv[w][r] = l == 0.f ? 0.f : 1.f / l;   // each warpgroup its own
       }
       const bool two = !kPair && x.tiles > 1;
-      if (warp_live) {
-        const float inv = !whole ? 1.f : (l == 0.f ? 0.f : 1.f / l);
-        const int64_t out_row = ((int64_t)x.b * p.T + t_node);
-        const int h = x.head * p.group + gq;
-        float* part = p.part + (((int64_t)blockIdx.x * 2 + (x.tile0 == 0 ? 1 : 0)) * p.part_rows + (my_row - r0)) * (D + kPartPad);
-        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out + out_row * p.out_stride) + (int64_t)h * D;
-        const bool odd = *reinterpret_cast<volatile int*>(&sh.odd_values) != 0;
-        // alternate tiles: the two warpgroups write half of the columns each
-        const int c_begin = kPair ? 0 : w * (D / 2), c_end = kPair ? D : c_begin + D / 2;
-#pragma unroll 1
-        for (int c = c_begin; c < c_end; c += 32) {
-          uint32_t a[32], b[32];
-          ld32_issue((kPair ? t_o : tmem + lanes + 256) + c, a);
-          if (two) ld32_issue(tmem + lanes + 384 + c, b);
-          ld_wait();
-          pin32(a);
-          if (two) pin32(b);
-          float o[32];
+      const float inv = !whole ? 1.f : (l == 0.f ? 0.f : 1.f / l);
+      const bool odd = *reinterpret_cast<volatile int*>(&sh.odd_values) != 0;
+      float* part0 = p.part + (((int64_t)blockIdx.x * 2 + (x.tile0 == 0 ? 1 : 0)) * p.part_rows - r0) * (D + kPartPad);
+      // kN elements of a query row from column c: back to a part, or out
+      auto write = [&](auto count, int row, int c, float* o, float factor) {
+        constexpr int kN = decltype(count)::value;
+        const int t = row / p.group, h = x.head * p.group + row - t * p.group;
+        if (row >= p.rows || t >= ex.nodes) return;
+        if (odd) {                                   // values of this piece's nodes that are not finite, to the rows that see them
+          for (int j = 0; j < ex.nodes; ++j) {
+            const int kv = ex.ctx + j;
+            if (kv < x.tile0 * kTile || kv >= (x.tile0 + x.tiles) * kTile || kv >= ex.kv_end || !((sh.node_mask[t][j >> 5] >> (j & 31)) & 1u)) continue;
+            const int page = p.c.table[(int64_t)ex.slot * p.c.max_pages + (kv >> p.c.page_shift)];
+            if (page < 0 || page >= p.c.pages) continue;
+            const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(p.c.v) + page_row(p.c, p.layer, page, x.head, kv & (p.c.page_size - 1)) * D + c;
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            o[i] = kPair ? __uint_as_float(a[i]) : (f0 == 0.f ? 0.f : __uint_as_float(a[i]) * f0);
-            if (two && f1 != 0.f) o[i] = fmaf(__uint_as_float(b[i]), f1, o[i]);
-          }
-          if (odd && live) {
-            for (int j = 0; j < ex.nodes; ++j) {
-              const int kv = ex.ctx + j;
-              if (kv < x.tile0 * kTile || kv >= (x.tile0 + x.tiles) * kTile || kv >= ex.kv_end || !((sh.node_mask[t_node][j >> 5] >> (j & 31)) & 1u)) continue;
-              const int page = p.c.table[(int64_t)ex.slot * p.c.max_pages + (kv >> p.c.page_shift)];
-              if (page < 0 || page >= p.c.pages) continue;
-              const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(p.c.v) + page_row(p.c, p.layer, page, x.head, kv & (p.c.page_size - 1)) * D + c;
-#pragma unroll
-              for (int i = 0; i < 32; ++i) {
-                const float y = __bfloat162float(v[i]);
-                if (!isfinite(y)) o[i] += y;
-              }
+            for (int i = 0; i < kN; ++i) {
+              const float y = __bfloat162float(v[i]);
+              if (!isfinite(y)) o[i] += y;
             }
-          }
-          if (!live) continue;
-          if (whole) {
-#pragma unroll
-            for (int i = 0; i < 32; i += 8) {
-              uint4 v;
-              v.x = pack_bf16(o[i] * inv, o[i + 1] * inv); v.y = pack_bf16(o[i + 2] * inv, o[i + 3] * inv);
-              v.z = pack_bf16(o[i + 4] * inv, o[i + 5] * inv); v.w = pack_bf16(o[i + 6] * inv, o[i + 7] * inv);
-              *reinterpret_cast<uint4*>(out + c + i) = v;
-            }
-          } else {
-#pragma unroll
-            for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(part + c + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
           }
         }
-        if (live && c_begin == 0) {
-          const float m2 = m * c2;
-          if (whole) {
-            if (p.lse) p.lse[out_row * p.q_heads + h] = l == 0.f ? -INFINITY : (m2 + log2f(l)) * 0.69314718055994531f;
-          } else {
-            *reinterpret_cast<float2*>(part + D) = make_float2(m == -INFINITY ? -INFINITY : m2, l);
+        if (whole) {
+          uint2* out = reinterpret_cast<uint2*>(p.out + ((int64_t)x.b * p.T + t) * p.out_stride + ((int64_t)h * D + c) * 2);
+#pragma unroll
+          for (int i = 0; i < kN; i += 4) out[i / 4] = make_uint2(pack_bf16(o[i] * factor, o[i + 1] * factor), pack_bf16(o[i + 2] * factor, o[i + 3] * factor));
+        } else {
+          float4* part = reinterpret_cast<float4*>(part0 + (int64_t)row * (D + kPartPad) + c);
+#pragma unroll
+          for (int i = 0; i < kN; i += 4) part[i / 4] = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+        }
+      };
+      // this lane's sum of the two chains, 16 columns
+      auto read_o = [&](int c, float* o) {
+        uint32_t a[16], b[16];
+        tmem_ld16_issue((kPair ? t_o : tmem + lanes + 256) + c, a);
+        if (two) tmem_ld16_issue(tmem + lanes + 384 + c, b);
+        ld_wait();
+        pin16(a);
+        if (two) pin16(b);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          o[i] = kPair ? __uint_as_float(a[i]) : (f0 == 0.f ? 0.f : __uint_as_float(a[i]) * f0);
+          if (two && f1 != 0.f) o[i] = fmaf(__uint_as_float(b[i]), f1, o[i]);
+        }
+      };
+      if constexpr (kCopies == 1) {
+        if (warp_live) {
+          // alternate tiles: the two warpgroups write half of the columns each
+          const int c_begin = kPair ? 0 : w * (D / 2), c_end = kPair ? D : c_begin + D / 2;
+#pragma unroll 1
+          for (int c = c_begin; c < c_end; c += 16) {
+            float o[16];
+            read_o(c, o);
+            write(std::integral_constant<int, 16>(), my_row, c, o, inv);
           }
+        }
+      } else {
+        // The copies' sums meet in shared memory, over Q, which is not needed any more: 16 columns at a time, alternately by warpgroup.
+        float* stage = reinterpret_cast<float*>(q_smem) + w * 128 * 16;
+#pragma unroll 1
+        for (int c = 16 * w; c < D; c += 32) {
+          float o[16];
+          if (warp_live) {
+            read_o(c, o);
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4*>(stage + r * 16 + ((i + 4 * r) & 15)) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+          }
+          asm volatile("bar.sync %0, 128;" ::"r"(2 + w) : "memory");
+          for (int i = r; i < kCopyRows * 4; i += 128) {
+            const int row = i >> 2, q = (i & 3) * 4;
+            if (r0 + row >= p.rows) continue;
+            float y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < kCopies; ++k) {
+              const int at = k * kCopyRows + row;
+              const float4 v = *reinterpret_cast<const float4*>(stage + at * 16 + ((q + 4 * at) & 15));
+              y[0] += v.x; y[1] += v.y; y[2] += v.z; y[3] += v.w;
+            }
+            write(std::integral_constant<int, 4>(), r0 + row, c + q, y, whole ? sh.inv[w][row] : 1.f);
+          }
+          asm volatile("bar.sync %0, 128;" ::"r"(2 + w) : "memory");
+        }
+      }
+      if (live && copy == 0 && (kPair || w == 0)) {
+        const float m2 = m * c2;
+        if (whole) {
+          if (p.lse) p.lse[((int64_t)x.b * p.T + t_node) * p.q_heads + x.head * p.group + gq] = l == 0.f ? -INFINITY : (m2 + log2f(l)) * 0.69314718055994531f;
+        } else {
+          *reinterpret_cast<float2*>(part0 + (int64_t)my_row * (D + kPartPad) + D) = make_float2(m == -INFINITY ? -INFINITY : m2, l);
         }
       }
       tc_fence_before();
@@ -634,27 +698,31 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   }
 }
 
-template <int D, bool kPair>
+template <int D, int kMode>
 cudaError_t launch(const AttendParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st) {
-  attend_sm100_kernel<D, kPair><<<(unsigned)(p.groups * p.row_blocks), kThreads, attend_smem<D, kPair>(), st>>>(tm_k, tm_v, p);
+  attend_sm100_kernel<D, kMode><<<(unsigned)(p.groups * p.row_blocks), kThreads, attend_smem<D, kMode>(), st>>>(tm_k, tm_v, p);
   return cudaGetLastError();
 }
-template <int D, bool kPair>
-bool configure() {
-  static_assert(attend_smem<D, kPair>() <= 227 * 1024, "shared memory of an SM");
-  return cudaFuncSetAttribute(attend_sm100_kernel<D, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)attend_smem<D, kPair>()) == cudaSuccess;
+template <int D>
+cudaError_t launch_mode(const AttendParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st) {
+  if (p.rows_per_block > 128) return launch<D, kPairMode>(p, tm_k, tm_v, st);
+  if (p.rows > 64) return launch<D, 1>(p, tm_k, tm_v, st);
+  return p.rows > 32 ? launch<D, 2>(p, tm_k, tm_v, st) : launch<D, 4>(p, tm_k, tm_v, st);
 }
+template <int D, int kMode>
+bool configure() {
+  static_assert(attend_smem<D, kMode>() <= 227 * 1024, "shared memory of an SM");
+  return cudaFuncSetAttribute(attend_sm100_kernel<D, kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)attend_smem<D, kMode>()) == cudaSuccess;
+}
+template <int D>
+bool configure_modes() { return configure<D, kPairMode>() && configure<D, 1>() && configure<D, 2>() && configure<D, 4>(); }
 
 }  // namespace
 
 cudaError_t run_attend_tensor(const AttendParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st) {
-  const bool pair = p.rows_per_block > 128;
-  if (p.c.head_dim == 64) return pair ? launch<64, true>(p, tm_k, tm_v, st) : launch<64, false>(p, tm_k, tm_v, st);
-  return pair ? launch<128, true>(p, tm_k, tm_v, st) : launch<128, false>(p, tm_k, tm_v, st);
+  return p.c.head_dim == 64 ? launch_mode<64>(p, tm_k, tm_v, st) : launch_mode<128>(p, tm_k, tm_v, st);
 }
 
-bool attend_configure() {
-  return simt_attend_configure() && configure<64, false>() && configure<64, true>() && configure<128, false>() && configure<128, true>();
-}
+bool attend_configure() { return simt_attend_configure() && configure_modes<64>() && configure_modes<128>(); }
 
 }  // namespace jd
