@@ -59,6 +59,7 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(AttendParams p) {
   const int g = blockIdx.x / p.row_blocks, rb = blockIdx.x - g * p.row_blocks;
   const int r0 = rb * kRows, nrows = min(kRows, p.rows - r0);
   pdl_trigger();
+  if (rb == 0 && tid == 0) split_none(p, g);
   unit_prefix(p, prefix, warp_sums);
   const int64_t units = (int64_t)prefix[p.B] * p.c.kv_heads;
   if (units == 0) return;
@@ -222,6 +223,7 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(AttendParams p) {
     }
     __syncthreads();
     const bool whole = ntiles == tiles;
+    if (!whole && tile0 == 0 && rb == 0 && tid == 0) split_set(p, g, units, x);
     for (int i = tid; i < nrows * (D / 4); i += kThreads) {
       const int r = i / (D / 4), d = (i - r * (D / 4)) * 4;
       float4 x = *reinterpret_cast<const float4*>(sK + r * pitch + d);
@@ -244,82 +246,101 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(AttendParams p) {
 
 // Joins the partial results of split segments; rows of whole segments are written already.
 // out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i over the parts in order.
-// A block takes one query row at a time, 128 columns by the lanes of a warp, and its warps take the parts in turn, eight loads in
-// flight each: a row of one long sequence has a part from every SM, and what the join costs is their latency. The warps'
-// sums meet in shared memory. Everything up to the first part is read before the attention kernel has ended.
-constexpr int kJoinWarps = 4;
+// Block (k, g) takes a few rows of the segment that group g left unfinished, if it left one: with up to kJoinFewRows rows in all one row,
+// whose parts its warps take in turn (what the join costs is their latency, and a row of one long sequence has a part from
+// every SM); with more four rows, and a warp for each unless the parts are many.
+constexpr int kJoinWarps = 4, kJoinBatch = 8, kJoinFewRows = 32, kJoinFewParts = 32;
+__host__ __device__ constexpr int join_rows(int rows) { return rows <= kJoinFewRows ? 1 : kJoinWarps; }
+
+struct RowSum {
+  float m, l, o[2][4];   // columns 4 lane .. and 128 + 4 lane ..
+};
+
+// parts first, first + step, .. last of a row; at(g) is where part g stands
+template <typename At>
+__device__ __forceinline__ RowSum sum_parts(int first, int last, int step, int D, int lane, At at) {
+  RowSum s = {-INFINITY, 0.f, {}};
+  const int d = lane * 4;
+  for (int g0 = first; g0 <= last; g0 += step * kJoinBatch) {
+    float2 ml[kJoinBatch];
+    float4 x[kJoinBatch][2];
+#pragma unroll
+    for (int k = 0; k < kJoinBatch; ++k) {
+      const int g = g0 + k * step;
+      ml[k] = make_float2(-INFINITY, 0.f);
+      x[k][0] = x[k][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (g <= last) {
+        const float* part = at(g);
+        ml[k] = __ldcg(reinterpret_cast<const float2*>(part + D));
+        if (d < D) x[k][0] = __ldcg(reinterpret_cast<const float4*>(part + d));
+        if (d + 128 < D) x[k][1] = __ldcg(reinterpret_cast<const float4*>(part + d + 128));
+      }
+    }
+    float top = s.m;
+#pragma unroll
+    for (int k = 0; k < kJoinBatch; ++k) top = fmaxf(top, ml[k].x);
+    const float base = top == -INFINITY ? 0.f : top, f0 = exp2f(s.m - base);
+    s.l *= f0;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s.o[j][e] *= f0;
+#pragma unroll
+    for (int k = 0; k < kJoinBatch; ++k) {
+      const float f = exp2f(ml[k].x - base);
+      s.l += f * ml[k].y;
+      if (ml[k].x == -INFINITY) continue;   // a part that saw nothing has no say, whatever it holds
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        s.o[j][0] = fmaf(f, x[k][j].x, s.o[j][0]); s.o[j][1] = fmaf(f, x[k][j].y, s.o[j][1]);
+        s.o[j][2] = fmaf(f, x[k][j].z, s.o[j][2]); s.o[j][3] = fmaf(f, x[k][j].w, s.o[j][3]);
+      }
+    }
+    s.m = top;
+  }
+  return s;
+}
+
 template <typename T>
 __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendParams p) {
-  __shared__ int prefix[kMaxCacheBatch + 1], warp_sums[kJoinWarps];
   __shared__ float4 s_o[kJoinWarps][2][32];
   __shared__ float2 s_ml[kJoinWarps];
-  unit_prefix(p, prefix, warp_sums);
-  const int64_t units = (int64_t)prefix[p.B] * p.c.kv_heads;
+  pdl_wait();
+  const int g0 = blockIdx.y;
+  const int4 split = __ldcg(p.split + g0);
+  const int b = split.x, head = split.y, g1 = split.z;
+  if (b < 0) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int D = p.c.head_dim, pitch = D + kPartPad;
-  const int64_t all = (int64_t)p.B * p.c.kv_heads * p.rows;
-  bool waited = false;
-  for (int64_t i = blockIdx.x; i < all; i += gridDim.x) {
-    const int64_t seg = i / p.rows;
-    const int row = (int)(i - seg * p.rows);
-    const int b = (int)(seg / p.c.kv_heads), head = (int)(seg - (int64_t)b * p.c.kv_heads);
-    const int n = prefix[b + 1] - prefix[b];
-    if (n == 0) continue;
-    const int64_t u0 = (int64_t)prefix[b] * p.c.kv_heads + (int64_t)head * n;
-    const int g0 = run_of(units, p.groups, u0 + p.seg_cost), g1 = run_of(units, p.groups, u0 + n - 1);
-    if (g0 == g1) continue;
-    const int t = row / p.group, nodes = p.num_nodes ? min(max(__ldg(p.num_nodes + b), 0), p.T) : p.T;
-    if (t >= nodes) continue;
+  const int nodes = p.num_nodes ? min(max(__ldg(p.num_nodes + b), 0), p.T) : p.T;
+  const int rows = min(p.rows, nodes * p.group);
+  auto write = [&](int row, int d, const float* o, float m, float l) {   // columns d .. d + 3
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+    const int t = row / p.group, h = head * p.group + row - t * p.group;
+    if (d < D) store4(reinterpret_cast<T*>(p.out + ((int64_t)b * p.T + t) * p.out_stride) + (int64_t)h * D + d, y);
+    if (d == 0 && p.lse) p.lse[((int64_t)b * p.T + t) * p.q_heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+  };
+  auto place = [&](int row) {
     const int rb = row / p.rows_per_block, r = row - rb * p.rows_per_block;
-    auto part_of = [&](int g) {
-      return p.part + (((int64_t)(g * p.row_blocks + rb) * 2 + (g == g0 ? 1 : 0)) * p.part_rows + r) * pitch;
-    };
-    if (!waited) { pdl_wait(); waited = true; }
-    const int d = lane * 4;
-    // this warp's parts: a running maximum, sum and numerators (columns 4 lane and 128 + 4 lane)
-    float m = -INFINITY, l = 0.f, o[2][4] = {};
-    constexpr int kBatch = 8;
-    for (int first = g0 + warp; first <= g1; first += kJoinWarps * kBatch) {
-      float2 ml[kBatch];
-      float4 x[kBatch][2];
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k) {
-        const int gg = first + k * kJoinWarps;
-        ml[k] = make_float2(-INFINITY, 0.f);
-        x[k][0] = x[k][1] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (gg <= g1) {
-          const float* part = part_of(gg);
-          ml[k] = __ldcg(reinterpret_cast<const float2*>(part + D));
-          if (d < D) x[k][0] = __ldcg(reinterpret_cast<const float4*>(part + d));
-          if (d + 128 < D) x[k][1] = __ldcg(reinterpret_cast<const float4*>(part + d + 128));
-        }
-      }
-      float top = m;
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k) top = fmaxf(top, ml[k].x);
-      const float base = top == -INFINITY ? 0.f : top, f0 = exp2f(m - base);
-      l *= f0;
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[j][e] *= f0;
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k) {
-        const float f = exp2f(ml[k].x - base);
-        l += f * ml[k].y;
-        if (ml[k].x == -INFINITY) continue;   // a part that saw nothing has no say, whatever it holds
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          o[j][0] = fmaf(f, x[k][j].x, o[j][0]); o[j][1] = fmaf(f, x[k][j].y, o[j][1]);
-          o[j][2] = fmaf(f, x[k][j].z, o[j][2]); o[j][3] = fmaf(f, x[k][j].w, o[j][3]);
-        }
-      }
-      m = top;
-    }
+    const float* base = p.part + ((int64_t)rb * 2 * p.part_rows + r) * pitch;
+    return [=](int g) { return base + ((int64_t)g * p.row_blocks * 2 + (g == g0 ? 1 : 0)) * p.part_rows * pitch; };
+  };
+  const int block_rows = join_rows(p.rows), first_row = blockIdx.x * block_rows;
+  if (block_rows > 1 && g1 - g0 < kJoinFewParts) {
+    const int row = first_row + warp;
+    if (row >= rows) return;
+    const RowSum s = sum_parts(g0, g1, 1, D, lane, place(row));
+    write(row, lane * 4, s.o[0], s.m, s.l);
+    if (D > 128) write(row, 128 + lane * 4, s.o[1], s.m, s.l);
+    return;
+  }
+  for (int row = first_row; row < min(rows, first_row + block_rows); ++row) {
+    const RowSum s = sum_parts(g0 + warp, g1, kJoinWarps, D, lane, place(row));
     __syncthreads();   // the last row's sums have been read
-    s_o[warp][0][lane] = make_float4(o[0][0], o[0][1], o[0][2], o[0][3]);
-    s_o[warp][1][lane] = make_float4(o[1][0], o[1][1], o[1][2], o[1][3]);
-    if (lane == 0) s_ml[warp] = make_float2(m, l);
+    s_o[warp][0][lane] = make_float4(s.o[0][0], s.o[0][1], s.o[0][2], s.o[0][3]);
+    s_o[warp][1][lane] = make_float4(s.o[1][0], s.o[1][1], s.o[1][2], s.o[1][3]);
+    if (lane == 0) s_ml[warp] = make_float2(s.m, s.l);
     __syncthreads();
     if (warp < 2) {    // columns 128 warp ..
       float top = -INFINITY;
@@ -335,17 +356,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendPara
         if (s_ml[w].x == -INFINITY) continue;
         y[0] = fmaf(f, x.x, y[0]); y[1] = fmaf(f, x.y, y[1]); y[2] = fmaf(f, x.z, y[2]); y[3] = fmaf(f, x.w, y[3]);
       }
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] *= inv;
-      const int h = head * p.group + row - t * p.group;
-      if (d + 128 * warp < D)
-        store4(reinterpret_cast<T*>(p.out + ((int64_t)b * p.T + t) * p.out_stride) + (int64_t)h * D + d + 128 * warp, y);
-      if (p.lse && warp == 0 && lane == 0)
-        p.lse[((int64_t)b * p.T + t) * p.q_heads + h] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
+      write(row, 128 * warp + lane * 4, y, top, sum);
     }
   }
-  if (!waited) pdl_wait();   // the next kernel on the stream counts on the attention having ended when this one has
 }
 
 template <typename T>
@@ -367,10 +380,10 @@ cudaError_t run_attend_simt(const AttendParams& p, int dtype, cudaStream_t st) {
 }
 
 cudaError_t run_attend_join(const AttendParams& p, int dtype, cudaStream_t st) {
-  const int64_t rows = (int64_t)p.B * p.c.kv_heads * p.rows;
-  const unsigned blocks = (unsigned)std::min<int64_t>(rows, 8 * kMaxCtas);
-  return dtype == JD_DTYPE_F32 ? launch_chained(attend_join_kernel<float>, dim3(blocks), dim3(32 * kJoinWarps), 0, st, p)
-                               : launch_chained(attend_join_kernel<__nv_bfloat16>, dim3(blocks), dim3(32 * kJoinWarps), 0, st, p);
+  const int n = join_rows(p.rows);
+  const dim3 grid((unsigned)((p.rows + n - 1) / n), (unsigned)p.groups);
+  return dtype == JD_DTYPE_F32 ? launch_chained(attend_join_kernel<float>, grid, dim3(32 * kJoinWarps), 0, st, p)
+                               : launch_chained(attend_join_kernel<__nv_bfloat16>, grid, dim3(32 * kJoinWarps), 0, st, p);
 }
 
 bool simt_attend_configure() {

@@ -213,6 +213,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
 
   pdl_trigger();
   if (tid == 0) {
+    if (rb == 0) split_none(p, g);
     for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&sh.full[i]), 1); mbar_init(smem_u32(&sh.empty[i]), 1); }
     for (int w = 0; w < 2; ++w) {
       mbar_init(smem_u32(&sh.s_full[w]), 1);
@@ -398,40 +399,58 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     const float c2 = p.scale_log2;
     uint32_t s_phase = 0, o_phase = 0;
     int tile_count = 0;                              // tiles of the run in front of this piece
-    for (int64_t u = run0; u < run1;) {
-      const Piece x = piece_at(p, sh.prefix, u, run1);
-      u = x.next;
-      if (x.tiles == 0) continue;
-      const SeqExtent ex = sh.extents[x.b];
-      // Q rows, eight 16-byte loads in flight; a thread keeps its place within a row
-      constexpr int kVecs = D / 8, kQThreads = kPair ? 128 : 256, kQRows = kQThreads / kVecs;
-      const int q_first = kPair ? r : tid, q_c = q_first % kVecs, q_r = q_first / kVecs;
-      const char* q_seq = p.q + (int64_t)x.b * p.T * p.q_stride + (int64_t)x.head * p.group * (D * 2) + q_c * 16;
-      auto load_q = [&](int i) {
-        const int q_row = r0 + (kPair ? w * 128 : 0) + (q_r + i * kQRows) % kCopyRows, t = q_row / p.group, h = q_row - t * p.group;
-        return q_row < p.rows && t < ex.nodes ? __ldg(reinterpret_cast<const uint4*>(q_seq + t * p.q_stride + h * (D * 2))) : make_uint4(0u, 0u, 0u, 0u);
-      };
-      uint4 q_regs[8];
+    // A piece's Q rows and mask words, fetched while the piece before it ends: a thread keeps its place within a row of Q
+    constexpr int kVecs = D / 8, kQThreads = kPair ? 128 : 256, kQRows = kQThreads / kVecs, kQLoads = 128 / kQRows;
+    constexpr int kMaskLoads = kMaxNodes * (kMaxNodes / 32) / 256;
+    const int q_first = kPair ? r : tid, q_c = q_first % kVecs, q_r = q_first / kVecs;
+    uint4 q_regs[kQLoads];
+    uint32_t mask_regs[kMaskLoads];
+    int64_t u = run0;
+    auto next_piece = [&]() {                        // tiles == 0: none left
+      Piece y;
+      y.tiles = 0;
+      while (u < run1) {
+        y = piece_at(p, sh.prefix, u, run1);
+        u = y.next;
+        if (y.tiles > 0) break;
+      }
+      return y;
+    };
+    auto fetch = [&](const Piece& y) {
+      if (y.tiles == 0) return;
+      const int nodes = sh.extents[y.b].nodes;
+      const char* q_seq = p.q + (int64_t)y.b * p.T * p.q_stride + (int64_t)y.head * p.group * (D * 2) + q_c * 16;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) if (i * kQRows < 128) q_regs[i] = load_q(i);
+      for (int i = 0; i < kQLoads; ++i) {
+        const int q_row = r0 + (kPair ? w * 128 : 0) + (q_r + i * kQRows) % kCopyRows, t = q_row / p.group, h = q_row - t * p.group;
+        q_regs[i] = q_row < p.rows && t < nodes ? __ldg(reinterpret_cast<const uint4*>(q_seq + t * p.q_stride + h * (D * 2)))
+                                                : make_uint4(0u, 0u, 0u, 0u);
+      }
+#pragma unroll
+      for (int i = 0; i < kMaskLoads; ++i) {
+        const int at = tid + i * 256, t = at / p.W, k = at - t * p.W;
+        mask_regs[i] = t < nodes ? node_word(p, y.b, t, k, nodes) : 0u;
+      }
+    };
+    // ahead of time where the registers are there for it: 256 rows of 128 columns are 64 registers a thread
+    constexpr bool kFetchAhead = kQLoads <= 8;
+    Piece x = next_piece();
+    if (kFetchAhead) fetch(x);
+    while (x.tiles > 0) {
+      const SeqExtent ex = sh.extents[x.b];
+      if (!kFetchAhead) fetch(x);
       softmax_sync();                                // everybody is through with the last piece's Q, masks and sums
-      for (int i = tid; i < p.T * p.W; i += 256) {
-        const int t = i / p.W, k = i - t * p.W;
-        sh.node_mask[t][k] = t < ex.nodes ? node_word(p, x.b, t, k, ex.nodes) : 0u;
+#pragma unroll
+      for (int i = 0; i < kMaskLoads; ++i) {
+        const int at = tid + i * 256, t = at / p.W;
+        if (t < p.T) sh.node_mask[t][at - t * p.W] = mask_regs[i];
       }
       if (tid == 0) sh.odd_values = 0;
       uint8_t* q_dst = q_smem + (kPair ? w * kTileBytes : 0) + (q_c >> 3) * kChunkBytes;
 #pragma unroll
-      for (int i0 = 0; i0 < 128 / kQRows; i0 += 8) {
-        if (i0 > 0)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) q_regs[i] = load_q(i0 + i);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if ((i0 + i) * kQRows < 128) {
-            const int row = q_r + (i0 + i) * kQRows;
-            *reinterpret_cast<uint4*>(q_dst + row * 128 + (((q_c & 7) ^ (row & 7)) << 4)) = q_regs[i];
-          }
+      for (int i = 0; i < kQLoads; ++i) {
+        const int row = q_r + i * kQRows;
+        *reinterpret_cast<uint4*>(q_dst + row * 128 + (((q_c & 7) ^ (row & 7)) << 4)) = q_regs[i];
       }
       fence_async_proxy();
       tc_fence_before();
@@ -564,9 +583,12 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         o_phase ^= 1u;
       }
       // ---------------------------------------------------------------- the piece's end
+      const Piece next = next_piece();
+      if (kFetchAhead) fetch(next);
       if (done > 0) wait(smem_u32(&sh.o_done[w]), o_phase ^ 1u, abort_flag);
       tc_fence_after();
       const bool whole = x.tiles == x.all;
+      if (!whole && x.tile0 == 0 && rb == 0 && tid == 0) split_set(p, g, units, x);
       const bool live = my_row < p.rows && t_node < ex.nodes;
       float f0 = 1.f, f1 = 0.f;                      // factors on this lane's O_0 and O_1 (pair mode: on its own O)
       if constexpr (!kPair) {
@@ -684,6 +706,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       }
       tc_fence_before();
       tile_count += x.tiles;
+      x = next;
     }
   }
 

@@ -416,13 +416,14 @@ size_t carve_cache(const jd_cache_config_t& g, char* base, jd_cache_s* c) {
   int* ms = (int*)take((size_t)g.num_pages * 4);
   int* md = (int*)take((size_t)g.num_pages * 4);
   int* mc = (int*)take(256);
+  int4* sp = (int4*)take((size_t)2 * kMaxCtas * sizeof(int4));
   // two partial results for each CTA of an attention call: up to 256 rows each on the tensor cores (one CTA per SM),
   // kSimtRows on CUDA cores (two per SM)
   const size_t rows = std::max<size_t>(std::min(rows_of(g), 256), 2 * kSimtRows);
   float* part = (float*)take((size_t)kMaxCtas * 2 * rows * (g.head_dim + kPartPad) * 4);
   if (c) {
     c->status = status; c->commit_cnt = cnt; c->copy_src = cs; c->copy_dst = cd; c->copy_rows = cr;
-    c->page_list = pl; c->move_src = ms; c->move_dst = md; c->move_cnt = mc; c->part = part;
+    c->page_list = pl; c->move_src = ms; c->move_dst = md; c->move_cnt = mc; c->split = sp; c->part = part;
   }
   return off;
 }
@@ -605,9 +606,10 @@ jd_status_t jd_cache_attend(jd_cache_t c, const jd_attend_args_t* a, void* cuda_
   p.lse = a->lse;
   p.scale_log2 = a->scale * 1.4426950408889634f;
   p.part = c->part;
+  p.split = c->split;
   if (tensor) {
     p.tile_shift = kTensorTileShift;
-    p.seg_cost = kTensorSegCost;
+    p.seg_cost = tensor_seg_cost(g.head_dim);
     p.rows_per_block = p.rows > 128 ? 256 : 128;
   } else {
     p.tile_shift = kSimtTileShift;

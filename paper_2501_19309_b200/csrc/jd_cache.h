@@ -24,6 +24,7 @@ struct jd_cache_s {
   int* move_src;              // [num_pages] compaction: pages to move, and where to
   int* move_dst;
   int* move_cnt;              // [1]
+  int4* split;                // [2 kMaxCtas] the segment that a group of an attention call begins and others go on with
   float* part;                // partial attention results of split sequences
 };
 
@@ -97,6 +98,7 @@ struct AttendParams {
   int64_t q_stride, out_stride;    // bytes between tokens
   float* lse;
   float scale_log2;                // scale x log2(e)
+  int4* split;                     // [groups] sequence, kv head and last group of the segment that the group leaves unfinished; x < 0: none
   float* part;                     // [groups * row_blocks][2][part_rows][head_dim + kPartPad]
 };
 
@@ -201,6 +203,13 @@ __device__ __forceinline__ uint32_t node_word(const AttendParams& p, int b, int 
   return left >= 32 ? m : m & ((1u << left) - 1u);
 }
 
+// What the join goes by: group g begins this segment and run `last` ends it. By one thread of the group's first CTA: none() as the kernel
+// starts, set() where a piece begins a segment that it does not end.
+__device__ __forceinline__ void split_none(const AttendParams& p, int g) { p.split[g] = make_int4(-1, 0, 0, 0); }
+__device__ __forceinline__ void split_set(const AttendParams& p, int g, int64_t units, const Piece& x) {
+  p.split[g] = make_int4(x.b, x.head, run_of(units, p.groups, x.next + (x.all - x.tiles) - 1), 0);
+}
+
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
@@ -227,7 +236,10 @@ cudaError_t run_attend_join(const AttendParams& p, int dtype, cudaStream_t st);
 bool simt_attend_configure();
 bool attend_configure();   // dynamic shared-memory limits on the current device, once per device
 constexpr int kSimtRows = 16, kSimtTileShift = 6, kSimtSegCost = 1;
-constexpr int kTensorTileShift = 7, kTensorSegCost = 2;
+constexpr int kTensorTileShift = 7;
+// what beginning and ending a segment costs, in tiles: some 8,000 cycles, against 1,400 (64 columns) or 2,800 (128) for a tile at
+// HBM rate. A batch of 16 chains up to 6,000 tokens long: 63 us at 2, 48 at 6, 51 at 12 (64 columns).
+constexpr int tensor_seg_cost(int head_dim) { return head_dim == 64 ? 6 : 4; }
 
 bool rope_valid(const jd_rope_t& r, int head_dim);
 cudaError_t run_append(const CacheView& c, const jd_append_args_t& a, int q_heads, int dtype, cudaStream_t st);
