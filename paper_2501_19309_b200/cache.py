@@ -40,16 +40,21 @@ def _require(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
-def _stream(stream, device) -> int:
-    return (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
+# These calls are made for every layer of every token: what follows avoids what costs microseconds in Python (stream objects,
+# device comparisons, messages that are formatted before they are needed).
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
-def _ints(x, name: str, device, shape=None) -> Optional[int]:
+def _stream(stream, index: int) -> int:
+    return stream.cuda_stream if stream is not None else _raw_stream(index)
+
+
+def _ints(x, name: str, index: int, shape=None) -> Optional[int]:
     """Pointer of an int32 device tensor, or None."""
     if x is None:
         return None
-    _require(x.dtype == torch.int32 and x.is_contiguous() and x.device == device, "%s: a contiguous int32 tensor on the cache's device" % name)
-    _require(shape is None or tuple(x.shape) == shape, "%s: shape %s expected" % (name, shape))
+    if x.dtype is not torch.int32 or x.get_device() != index or not x.is_contiguous() or (shape is not None and x.shape != shape):
+        raise ValueError("%s: a contiguous int32 tensor%s on the cache's device" % (name, "" if shape is None else " of shape %s" % (shape,)))
     return x.data_ptr()
 
 
@@ -74,31 +79,46 @@ class Rotary:
         self.rot_dim = 2 * inv_freq.numel()
         self.c = jd.jd_rope_t(inv_freq.data_ptr(), self.rot_dim, LAYOUTS[layout], self.amplitude)
         self.ref = C.pointer(self.c)
+        self.index = inv_freq.get_device()
+        self._lib = jd.load()
 
     def rotate(self, x: torch.Tensor, positions: torch.Tensor, out: Optional[torch.Tensor] = None, inverse: bool = False,
                stream=None) -> torch.Tensor:
         """Turns x [tokens, heads, head_dim] (tokens may be strided) to its positions [tokens] (int32). ``inverse`` turns back: with
         the gradient of the output as x, the result is the gradient of the input. ``out`` may be x."""
-        _require(x.dim() == 3 and x.is_cuda and x.dtype in _DTYPES, "x: [tokens, heads, head_dim], float32 or bfloat16, on the device")
+        if x.dim() != 3 or x.dtype not in _DTYPES or not x.is_cuda:
+            raise ValueError("x: [tokens, heads, head_dim], float32 or bfloat16, on the device")
         n, heads, dim = x.shape
+        index = x.get_device()
         if out is None:
             out = torch.empty(n, heads, dim, dtype=x.dtype, device=x.device)
-        _require(out.shape == x.shape and out.dtype == x.dtype and out.device == x.device, "out: like x")
-        for t, name in ((x, "x"), (out, "out")):
-            _require((dim == 1 or t.stride(2) == 1) and (heads == 1 or t.stride(1) == dim), "%s: heads of a token contiguous" % name)
-        _ints(positions, "positions", x.device, (n,))
-        _require(self.inv_freq.device == x.device, "inv_freq and x on one device")
+        elif out.shape != x.shape or out.dtype is not x.dtype or out.get_device() != index:
+            raise ValueError("out: like x")
+        x_step, out_step = self._step(x, "x", n, heads, dim), self._step(out, "out", n, heads, dim)
+        at = _ints(positions, "positions", index, (n,))
+        if self.index != index:
+            raise ValueError("inv_freq and x on one device")
         if n == 0:
             return out
-        a = jd.jd_rope_args_t(n, heads, dim, _DTYPES[x.dtype], 1 if inverse else 0, x.data_ptr(), out.data_ptr(),
-                              x.stride(0) if n > 1 else 0, out.stride(0) if n > 1 else 0, positions.data_ptr(), self.c)
-        if torch.cuda.current_device() == x.device.index:
-            st = jd.load().jd_rope(C.byref(a), _stream(stream, x.device))
+        a = jd.jd_rope_args_t(n, heads, dim, _DTYPES[x.dtype], 1 if inverse else 0, x.data_ptr(), out.data_ptr(), x_step, out_step, at, self.c)
+        if torch._C._cuda_getDevice() == index:
+            st = self._lib.jd_rope(a, _stream(stream, index))
         else:
-            with torch.cuda.device(x.device):
-                st = jd.load().jd_rope(C.byref(a), _stream(stream, x.device))
-        _check(st, "jd_rope")
+            with torch.cuda.device(index):
+                st = self._lib.jd_rope(a, _stream(stream, index))
+        if st != jd.JD_OK:
+            raise jd.JdError(st, "jd_rope")
         return out
+
+    @staticmethod
+    def _step(t: torch.Tensor, name: str, n: int, heads: int, dim: int) -> int:
+        """Elements between tokens, 0: dense."""
+        if t.is_contiguous():
+            return 0
+        step, by_head, by_element = t.stride()
+        if (dim > 1 and by_element != 1) or (heads > 1 and by_head != dim):
+            raise ValueError("%s: heads of a token contiguous" % name)
+        return step if n > 1 else 0
 
 
 class Tree:
@@ -121,9 +141,10 @@ class Tree:
             _require(num_nodes.dtype == torch.int32 and num_nodes.is_contiguous() and num_nodes.dim() == 1, "num_nodes: a contiguous int32 vector")
         _require(len(batched) <= 1, "mask and depth: both per sequence, of one batch size, or neither")
         self.batch = batched.pop() if batched else 0            # 0: shared
-        self.device = next((x.device for x in (mask, depth, num_nodes) if x is not None), None)
+        self.index = next((x.get_device() for x in (mask, depth, num_nodes) if x is not None), None)
         for x in (mask, depth, num_nodes):
-            _require(x is None or x.device == self.device, "mask, depth and num_nodes on one device")
+            _require(x is None or x.get_device() == self.index, "mask, depth and num_nodes on one device")
+        self.sequences = None if num_nodes is None else num_nodes.shape[0]
         ptr = [None if x is None else x.data_ptr() for x in (mask, depth, num_nodes)]
         self.c = jd.jd_tree_t(self.nodes, 1 if self.batch else 0, *ptr)
 
@@ -169,7 +190,8 @@ class PagedCache:
         self.h = None
         _require(k.dim() == 5 and k.is_cuda and k.is_contiguous() and k.dtype in _DTYPES, "k: contiguous [layers, pages, kv_heads, page_size, head_dim]")
         _require(v.shape == k.shape and v.dtype == k.dtype and v.device == k.device and v.is_contiguous(), "v: like k")
-        self.device = dev = k.device
+        self.device, self.index, self.dtype = k.device, k.get_device(), k.dtype
+        dev = self.index
         layers, pages, kv_heads, page_size, dim = k.shape
         _require(page_table.dim() == 2, "page_table: [seqs, pages of a sequence]")
         seqs, per_seq = page_table.shape
@@ -179,12 +201,12 @@ class PagedCache:
         self.k, self.v, self.page_table, self.seq_len, self.held, self.refs, self.free_bits = k, v, page_table, seq_len, held, refs, free_bits
         self.q_heads, self.kv_heads, self.head_dim, self.max_nodes, self.max_seqs = int(q_heads), kv_heads, dim, int(max_nodes), seqs
         self.cfg = jd.jd_cache_config_t(layers, pages, page_size, self.q_heads, kv_heads, dim, seqs, per_seq, self.max_nodes,
-                                        _DTYPES[k.dtype], dev.index)
+                                        _DTYPES[k.dtype], dev)
         self._lib = lib = jd.load()
         need = lib.jd_cache_workspace_bytes(C.byref(self.cfg))
         if need == 0:
             raise jd.JdError(jd.JD_ERR_INVALID_ARG, "jd_cache_workspace_bytes")
-        self.workspace = torch.zeros(need, dtype=torch.uint8, device=dev)
+        self.workspace = torch.zeros(need, dtype=torch.uint8, device=self.device)
         buf = jd.jd_cache_buffers_t(k.data_ptr(), v.data_ptr(), *ptrs, self.workspace.data_ptr(), need)
         h = C.c_void_p()
         _check(lib.jd_cache_create(C.byref(h), C.byref(self.cfg), C.byref(buf)), "jd_cache_create")
@@ -192,6 +214,7 @@ class PagedCache:
         self._attend = jd.jd_attend_args_t()
         self._append = jd.jd_append_args_t()
         self._commit = jd.jd_commit_args_t()
+        self._scale = 1.0 / math.sqrt(dim)
 
     @classmethod
     def allocate(cls, num_layers: int, num_pages: int, page_size: int, q_heads: int, kv_heads: int, head_dim: int, max_seqs: int,
@@ -222,61 +245,71 @@ class PagedCache:
     def _batch(self, slots, B: Optional[int] = None) -> int:
         if slots is None:
             return self.max_seqs if B is None else B
-        _require(slots.dim() == 1 and (B is None or slots.shape[0] == B), "slots: one for each sequence")
+        if slots.dim() != 1 or (B is not None and slots.shape[0] != B):
+            raise ValueError("slots: one for each sequence")
         return slots.shape[0]
 
-    def _tokens(self, x: torch.Tensor, name: str, heads: int):
-        """(pointer, stride between tokens) of [B, T, heads, head_dim] whose tokens lie evenly, heads contiguous."""
-        B, T, H, D = x.shape
-        _require(H == heads and D == self.head_dim and x.dtype == self.k.dtype and x.device == self.device,
-                 "%s: [B, T, %d, %d] of the cache's type and device" % (name, heads, self.head_dim))
+    def _tokens(self, x: torch.Tensor, name: str, shape) -> int:
+        """Elements between tokens (0: dense) of [B, T, heads, head_dim] whose tokens lie evenly, heads contiguous."""
+        if x.shape != shape or x.dtype is not self.dtype or x.get_device() != self.index:
+            raise ValueError("%s: %s of the cache's type, on its device" % (name, list(shape)))
         if x.is_contiguous():
-            return x.data_ptr(), 0
+            return 0
+        B, T, H, D = shape
         sb, st, sh, sd = x.stride()
         step = st if T > 1 else sb
-        _require((D == 1 or sd == 1) and (H == 1 or sh == D) and (B == 1 or T == 1 or sb == T * st),
-                 "%s: heads of a token contiguous, tokens evenly spaced" % name)
-        return x.data_ptr(), step if B * T > 1 else 0
+        if (D > 1 and sd != 1) or (H > 1 and sh != D) or (B > 1 and T > 1 and sb != T * st):
+            raise ValueError("%s: heads of a token contiguous, tokens evenly spaced" % name)
+        return step if B * T > 1 else 0
 
     def _tree(self, tree: Optional[Tree], B: int, T: int):
         if tree is None:
             return jd.jd_tree_t(T, 0, None, None, None)
-        _require(tree.nodes == T and tree.batch in (0, B) and (tree.num_nodes is None or tree.num_nodes.shape[0] == B),
-                 "tree: of %d nodes, shared or for %d sequences" % (T, B))
-        _require(tree.device is None or tree.device == self.device, "tree: on the cache's device")
+        if tree.nodes != T or (tree.batch != 0 and tree.batch != B) or (tree.sequences is not None and tree.sequences != B):
+            raise ValueError("tree: of %d nodes, shared or for %d sequences" % (T, B))
+        if tree.index is not None and tree.index != self.index:
+            raise ValueError("tree: on the cache's device")
         return tree.c
 
     def reserve(self, n: int, slots: Optional[torch.Tensor] = None, stream=None) -> None:
         """Pages for n more tokens of every sequence (``jd_cache_reserve``)."""
         B = self._batch(slots)
-        _check(self._lib.jd_cache_reserve(self.h, B, _ints(slots, "slots", self.device), n, _stream(stream, self.device)), "jd_cache_reserve")
+        st = self._lib.jd_cache_reserve(self.h, B, _ints(slots, "slots", self.index), n, _stream(stream, self.index))
+        if st != jd.JD_OK:
+            raise jd.JdError(st, "jd_cache_reserve")
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, tree: Optional[Tree] = None, rotary: Optional[Rotary] = None,
                q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None, stream=None):
         """Writes a block's keys and values [B, T, kv_heads, head_dim] behind the sequences' tokens, turned to their positions,
         and returns the turned queries (q_out; a new tensor if None), or None without q."""
-        _require(k.dim() == 4 and v.shape == k.shape, "k, v: [B, T, kv_heads, head_dim]")
-        B, T = k.shape[:2]
-        self._batch(slots, B)
+        if k.dim() != 4:
+            raise ValueError("k, v: [B, T, kv_heads, head_dim]")
+        B, T, _, D = k.shape
+        if slots is not None:
+            self._batch(slots, B)
         a = self._append
-        a.B, a.layer, a.slots, a.tree = B, layer, _ints(slots, "slots", self.device), self._tree(tree, B, T)
-        a.k, a.k_stride = self._tokens(k, "k", self.kv_heads)
-        a.v, a.v_stride = self._tokens(v, "v", self.kv_heads)
+        a.B, a.layer, a.slots, a.tree = B, layer, _ints(slots, "slots", self.index), self._tree(tree, B, T)
+        kv = (B, T, self.kv_heads, self.head_dim)
+        a.k, a.k_stride = k.data_ptr(), self._tokens(k, "k", kv)
+        a.v, a.v_stride = v.data_ptr(), self._tokens(v, "v", kv)
         if q is not None:
             if q_out is None:
                 q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            _require(q.dim() == 4 and q.shape[:2] == (B, T) and q_out.shape == q.shape, "q, q_out: [B, T, q_heads, head_dim]")
-            a.q, a.q_stride = self._tokens(q, "q", self.q_heads)
-            a.q_out, a.q_out_stride = self._tokens(q_out, "q_out", self.q_heads)
+            qs = (B, T, self.q_heads, self.head_dim)
+            a.q, a.q_stride = q.data_ptr(), self._tokens(q, "q", qs)
+            a.q_out, a.q_out_stride = q_out.data_ptr(), self._tokens(q_out, "q_out", qs)
         else:
             a.q = a.q_out = None
             q_out = None
-        if rotary is not None:
-            _require(rotary.inv_freq.device == self.device, "rotary: on the cache's device")
-            a.rope = rotary.ref
-        else:
+        if rotary is None:
             a.rope = None
-        _check(self._lib.jd_cache_append(self.h, a, _stream(stream, self.device)), "jd_cache_append")
+        elif rotary.index != self.index:
+            raise ValueError("rotary: on the cache's device")
+        else:
+            a.rope = rotary.ref
+        st = self._lib.jd_cache_append(self.h, a, _stream(stream, self.index))
+        if st != jd.JD_OK:
+            raise jd.JdError(st, "jd_cache_append")
         return q_out
 
     def attend(self, layer: int, q: torch.Tensor, tree: Optional[Tree] = None, scale: Optional[float] = None, out: Optional[dict] = None,
@@ -284,27 +317,31 @@ class PagedCache:
         """Attention of q [B, T, q_heads, head_dim] over the sequences' tokens and the block's visible nodes; scale: on q . k,
         default head_dim ** -0.5. Returns (and takes) a dict with "out" like q and "lse" [B, T, q_heads] (may be absent in a
         dict that is given)."""
-        _require(q.dim() == 4, "q: [B, T, q_heads, head_dim]")
+        if q.dim() != 4:
+            raise ValueError("q: [B, T, q_heads, head_dim]")
         B, T, H, D = q.shape
-        self._batch(slots, B)
+        if slots is not None:
+            self._batch(slots, B)
         if out is None:
             out = dict(out=torch.empty(B, T, H, D, dtype=q.dtype, device=q.device),
                        lse=torch.empty(B, T, H, dtype=torch.float32, device=q.device))
         o, lse = out["out"], out.get("lse")
-        _require(o.shape == q.shape, "out: like q")
         a = self._attend
-        a.B, a.layer, a.slots, a.tree = B, layer, _ints(slots, "slots", self.device), self._tree(tree, B, T)
-        a.q, a.q_stride = self._tokens(q, "q", self.q_heads)
-        a.out, a.out_stride = self._tokens(o, "out", self.q_heads)
-        if lse is not None:
-            _require(lse.dtype == torch.float32 and lse.is_contiguous() and lse.device == self.device and lse.shape == q.shape[:3],
-                     "lse: contiguous float32 [B, T, q_heads]")
-            a.lse = lse.data_ptr()
-        else:
+        a.B, a.layer, a.slots, a.tree = B, layer, _ints(slots, "slots", self.index), self._tree(tree, B, T)
+        shape = (B, T, self.q_heads, self.head_dim)
+        a.q, a.q_stride = q.data_ptr(), self._tokens(q, "q", shape)
+        a.out, a.out_stride = o.data_ptr(), self._tokens(o, "out", shape)
+        if lse is None:
             a.lse = None
-        a.scale = 1.0 / math.sqrt(self.head_dim) if scale is None else scale
+        elif lse.dtype is not torch.float32 or lse.get_device() != self.index or not lse.is_contiguous() or lse.shape != shape[:3]:
+            raise ValueError("lse: contiguous float32 [B, T, q_heads]")
+        else:
+            a.lse = lse.data_ptr()
+        a.scale = self._scale if scale is None else scale
         a.variant = ATTEND_VARIANTS[variant] if isinstance(variant, str) else int(variant)
-        _check(self._lib.jd_cache_attend(self.h, a, _stream(stream, self.device)), "jd_cache_attend")
+        st = self._lib.jd_cache_attend(self.h, a, _stream(stream, self.index))
+        if st != jd.JD_OK:
+            raise jd.JdError(st, "jd_cache_attend")
         return out
 
     def commit(self, accept_len: torch.Tensor, paths: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None,
@@ -312,45 +349,58 @@ class PagedCache:
         """Keeps node 0 and the accepted nodes. accept_len [B] or [B, num_paths] (int32, as ``Verifier.verify`` returns it); paths
         [B, num_paths, path_len] nodes of the draft tokens along every path, None: a chain (path_len then bounds
         accept_len, default max_nodes - 1). Returns the number of the kept path of every sequence, [B]."""
-        _require(accept_len.dim() in (1, 2), "accept_len: [B] or [B, num_paths]")
+        if accept_len.dim() not in (1, 2):
+            raise ValueError("accept_len: [B] or [B, num_paths]")
         B = accept_len.shape[0]
         n = accept_len.shape[1] if accept_len.dim() == 2 else 1
-        self._batch(slots, B)
+        if slots is not None:
+            self._batch(slots, B)
         a = self._commit
         if paths is not None:
-            _require(paths.dim() == 3 and paths.shape[:2] == (B, n), "paths: [B, num_paths, path_len]")
+            if paths.dim() != 3 or paths.shape[0] != B or paths.shape[1] != n:
+                raise ValueError("paths: [B, num_paths, path_len]")
             path_len = paths.shape[2]
         elif path_len is None:
             path_len = self.max_nodes - 1
         if chosen is None:
             chosen = torch.empty(B, dtype=torch.int32, device=self.device)
-        a.B, a.slots, a.accept_len = B, _ints(slots, "slots", self.device), _ints(accept_len, "accept_len", self.device)
-        a.num_paths, a.path_len, a.paths = n, path_len, _ints(paths, "paths", self.device)
-        a.chosen = _ints(chosen, "chosen", self.device, (B,))
-        _check(self._lib.jd_cache_commit(self.h, a, _stream(stream, self.device)), "jd_cache_commit")
+        a.B, a.slots, a.accept_len = B, _ints(slots, "slots", self.index), _ints(accept_len, "accept_len", self.index)
+        a.num_paths, a.path_len, a.paths = n, path_len, _ints(paths, "paths", self.index)
+        a.chosen = _ints(chosen, "chosen", self.index, (B,))
+        st = self._lib.jd_cache_commit(self.h, a, _stream(stream, self.index))
+        if st != jd.JD_OK:
+            raise jd.JdError(st, "jd_cache_commit")
         return chosen
 
     def fork(self, src: torch.Tensor, dst: torch.Tensor, stream=None) -> None:
         """The empty slots dst[i] become copies of src[i] that share its pages until they part (``jd_cache_fork``)."""
-        _require(src.dim() == 1 and src.shape == dst.shape, "src, dst: [n]")
-        _check(self._lib.jd_cache_fork(self.h, src.shape[0], _ints(src, "src", self.device), _ints(dst, "dst", self.device),
-                                       _stream(stream, self.device)), "jd_cache_fork")
+        if src.dim() != 1 or src.shape != dst.shape:
+            raise ValueError("src, dst: [n]")
+        st = self._lib.jd_cache_fork(self.h, src.shape[0], _ints(src, "src", self.index), _ints(dst, "dst", self.index), _stream(stream, self.index))
+        if st != jd.JD_OK:
+            raise jd.JdError(st, "jd_cache_fork")
 
     def truncate(self, length: Optional[torch.Tensor], slots: Optional[torch.Tensor] = None, stream=None) -> None:
         """Cuts the sequences to length [B] tokens (None: 0); pages behind are released."""
         B = self._batch(slots, None if length is None else length.shape[0])
-        _check(self._lib.jd_cache_truncate(self.h, B, _ints(slots, "slots", self.device), _ints(length, "length", self.device, (B,)),
-                                           _stream(stream, self.device)), "jd_cache_truncate")
+        st = self._lib.jd_cache_truncate(self.h, B, _ints(slots, "slots", self.index), _ints(length, "length", self.index, (B,)),
+                                         _stream(stream, self.index))
+        if st != jd.JD_OK:
+            raise jd.JdError(st, "jd_cache_truncate")
 
     def free(self, slots: torch.Tensor, stream=None) -> None:
         """Empties slots."""
+        if slots is None:
+            raise ValueError("slots: which to empty")
         self.truncate(None, slots, stream)
 
     def compact(self, used: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """Moves the pages in use to the front of the pool; returns their number, [1] (``jd_cache_compact``)."""
         if used is None:
             used = torch.empty(1, dtype=torch.int32, device=self.device)
-        _check(self._lib.jd_cache_compact(self.h, _ints(used, "used", self.device, (1,)), _stream(stream, self.device)), "jd_cache_compact")
+        st = self._lib.jd_cache_compact(self.h, _ints(used, "used", self.index, (1,)), _stream(stream, self.index))
+        if st != jd.JD_OK:
+            raise jd.JdError(st, "jd_cache_compact")
         return used
 
     def status(self) -> int:
