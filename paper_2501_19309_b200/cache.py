@@ -17,6 +17,7 @@ from __future__ import annotations
 
 import ctypes as C
 import math
+import struct
 from typing import Optional
 
 import torch
@@ -42,17 +43,23 @@ def _require(ok: bool, what: str) -> None:
 
 # These calls are made for every layer of every token: what follows avoids what costs microseconds in Python (stream objects,
 # device comparisons, messages that are formatted before they are needed).
+# Argument structs are packed in one go, in the C compiler's layout, instead of field by field.
 _raw_stream = torch._C._cuda_getCurrentRawStream
+_TREE = "iiPPP"
+_ROPE_ARGS = struct.Struct("@qiiiiPPqqPPiif")
+_APPEND_ARGS = struct.Struct("@iiP" + _TREE + "PPPPqqqqP")
+_ATTEND_ARGS = struct.Struct("@iiP" + _TREE + "PPqqPfi")
+_COMMIT_ARGS = struct.Struct("@iPPiiPP")
 
 
 def _stream(stream, index: int) -> int:
     return stream.cuda_stream if stream is not None else _raw_stream(index)
 
 
-def _ints(x, name: str, index: int, shape=None) -> Optional[int]:
-    """Pointer of an int32 device tensor, or None."""
+def _ints(x, name: str, index: int, shape=None) -> int:
+    """Pointer of an int32 device tensor, 0 for None."""
     if x is None:
-        return None
+        return 0
     if x.dtype is not torch.int32 or x.get_device() != index or not x.is_contiguous() or (shape is not None and x.shape != shape):
         raise ValueError("%s: a contiguous int32 tensor%s on the cache's device" % (name, "" if shape is None else " of shape %s" % (shape,)))
     return x.data_ptr()
@@ -77,8 +84,9 @@ class Rotary:
                  "inv_freq: a contiguous float32 vector")
         self.inv_freq, self.layout, self.amplitude = inv_freq, layout, float(amplitude)
         self.rot_dim = 2 * inv_freq.numel()
-        self.c = jd.jd_rope_t(inv_freq.data_ptr(), self.rot_dim, LAYOUTS[layout], self.amplitude)
-        self.ref = C.pointer(self.c)
+        self._layout = LAYOUTS[layout]
+        self.c = jd.jd_rope_t(inv_freq.data_ptr(), self.rot_dim, self._layout, self.amplitude)
+        self.ref = C.addressof(self.c)
         self.index = inv_freq.get_device()
         self._lib = jd.load()
 
@@ -100,7 +108,9 @@ class Rotary:
             raise ValueError("inv_freq and x on one device")
         if n == 0:
             return out
-        a = jd.jd_rope_args_t(n, heads, dim, _DTYPES[x.dtype], 1 if inverse else 0, x.data_ptr(), out.data_ptr(), x_step, out_step, at, self.c)
+        a = jd.jd_rope_args_t()
+        _ROPE_ARGS.pack_into(a, 0, n, heads, dim, _DTYPES[x.dtype], 1 if inverse else 0, x.data_ptr(), out.data_ptr(), x_step, out_step, at,
+                             self.inv_freq.data_ptr(), self.rot_dim, self._layout, self.amplitude)
         if torch._C._cuda_getDevice() == index:
             st = self._lib.jd_rope(a, _stream(stream, index))
         else:
@@ -145,8 +155,7 @@ class Tree:
         for x in (mask, depth, num_nodes):
             _require(x is None or x.get_device() == self.index, "mask, depth and num_nodes on one device")
         self.sequences = None if num_nodes is None else num_nodes.shape[0]
-        ptr = [None if x is None else x.data_ptr() for x in (mask, depth, num_nodes)]
-        self.c = jd.jd_tree_t(self.nodes, 1 if self.batch else 0, *ptr)
+        self.c = (self.nodes, 1 if self.batch else 0, *(0 if x is None else x.data_ptr() for x in (mask, depth, num_nodes)))
 
     @classmethod
     def from_parents(cls, parents, device, num_nodes: Optional[torch.Tensor] = None) -> "Tree":
@@ -211,9 +220,6 @@ class PagedCache:
         h = C.c_void_p()
         _check(lib.jd_cache_create(C.byref(h), C.byref(self.cfg), C.byref(buf)), "jd_cache_create")
         self.h = h
-        self._attend = jd.jd_attend_args_t()
-        self._append = jd.jd_append_args_t()
-        self._commit = jd.jd_commit_args_t()
         self._scale = 1.0 / math.sqrt(dim)
 
     @classmethod
@@ -264,7 +270,7 @@ class PagedCache:
 
     def _tree(self, tree: Optional[Tree], B: int, T: int):
         if tree is None:
-            return jd.jd_tree_t(T, 0, None, None, None)
+            return (T, 0, 0, 0, 0)
         if tree.nodes != T or (tree.batch != 0 and tree.batch != B) or (tree.sequences is not None and tree.sequences != B):
             raise ValueError("tree: of %d nodes, shared or for %d sequences" % (T, B))
         if tree.index is not None and tree.index != self.index:
@@ -287,26 +293,25 @@ class PagedCache:
         B, T, _, D = k.shape
         if slots is not None:
             self._batch(slots, B)
-        a = self._append
-        a.B, a.layer, a.slots, a.tree = B, layer, _ints(slots, "slots", self.index), self._tree(tree, B, T)
+        at = _ints(slots, "slots", self.index)
+        t0, t1, t2, t3, t4 = self._tree(tree, B, T)
         kv = (B, T, self.kv_heads, self.head_dim)
-        a.k, a.k_stride = k.data_ptr(), self._tokens(k, "k", kv)
-        a.v, a.v_stride = v.data_ptr(), self._tokens(v, "v", kv)
+        k_step, v_step = self._tokens(k, "k", kv), self._tokens(v, "v", kv)
+        q_ptr = o_ptr = q_step = o_step = rope = 0
         if q is not None:
             if q_out is None:
                 q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
             qs = (B, T, self.q_heads, self.head_dim)
-            a.q, a.q_stride = q.data_ptr(), self._tokens(q, "q", qs)
-            a.q_out, a.q_out_stride = q_out.data_ptr(), self._tokens(q_out, "q_out", qs)
+            q_ptr, q_step = q.data_ptr(), self._tokens(q, "q", qs)
+            o_ptr, o_step = q_out.data_ptr(), self._tokens(q_out, "q_out", qs)
         else:
-            a.q = a.q_out = None
             q_out = None
-        if rotary is None:
-            a.rope = None
-        elif rotary.index != self.index:
-            raise ValueError("rotary: on the cache's device")
-        else:
-            a.rope = rotary.ref
+        if rotary is not None:
+            if rotary.index != self.index:
+                raise ValueError("rotary: on the cache's device")
+            rope = rotary.ref
+        a = jd.jd_append_args_t()
+        _APPEND_ARGS.pack_into(a, 0, B, layer, at, t0, t1, t2, t3, t4, k.data_ptr(), v.data_ptr(), q_ptr, o_ptr, k_step, v_step, q_step, o_step, rope)
         st = self._lib.jd_cache_append(self.h, a, _stream(stream, self.index))
         if st != jd.JD_OK:
             raise jd.JdError(st, "jd_cache_append")
@@ -326,19 +331,17 @@ class PagedCache:
             out = dict(out=torch.empty(B, T, H, D, dtype=q.dtype, device=q.device),
                        lse=torch.empty(B, T, H, dtype=torch.float32, device=q.device))
         o, lse = out["out"], out.get("lse")
-        a = self._attend
-        a.B, a.layer, a.slots, a.tree = B, layer, _ints(slots, "slots", self.index), self._tree(tree, B, T)
+        at = _ints(slots, "slots", self.index)
+        t0, t1, t2, t3, t4 = self._tree(tree, B, T)
         shape = (B, T, self.q_heads, self.head_dim)
-        a.q, a.q_stride = q.data_ptr(), self._tokens(q, "q", shape)
-        a.out, a.out_stride = o.data_ptr(), self._tokens(o, "out", shape)
-        if lse is None:
-            a.lse = None
-        elif lse.dtype is not torch.float32 or lse.get_device() != self.index or not lse.is_contiguous() or lse.shape != shape[:3]:
-            raise ValueError("lse: contiguous float32 [B, T, q_heads]")
-        else:
-            a.lse = lse.data_ptr()
-        a.scale = self._scale if scale is None else scale
-        a.variant = ATTEND_VARIANTS[variant] if isinstance(variant, str) else int(variant)
+        q_step, o_step, l_ptr = self._tokens(q, "q", shape), self._tokens(o, "out", shape), 0
+        if lse is not None:
+            if lse.dtype is not torch.float32 or lse.get_device() != self.index or not lse.is_contiguous() or lse.shape != shape[:3]:
+                raise ValueError("lse: contiguous float32 [B, T, q_heads]")
+            l_ptr = lse.data_ptr()
+        a = jd.jd_attend_args_t()
+        _ATTEND_ARGS.pack_into(a, 0, B, layer, at, t0, t1, t2, t3, t4, q.data_ptr(), o.data_ptr(), q_step, o_step, l_ptr,
+                               self._scale if scale is None else scale, ATTEND_VARIANTS[variant] if isinstance(variant, str) else int(variant))
         st = self._lib.jd_cache_attend(self.h, a, _stream(stream, self.index))
         if st != jd.JD_OK:
             raise jd.JdError(st, "jd_cache_attend")
@@ -355,7 +358,6 @@ class PagedCache:
         n = accept_len.shape[1] if accept_len.dim() == 2 else 1
         if slots is not None:
             self._batch(slots, B)
-        a = self._commit
         if paths is not None:
             if paths.dim() != 3 or paths.shape[0] != B or paths.shape[1] != n:
                 raise ValueError("paths: [B, num_paths, path_len]")
@@ -364,9 +366,9 @@ class PagedCache:
             path_len = self.max_nodes - 1
         if chosen is None:
             chosen = torch.empty(B, dtype=torch.int32, device=self.device)
-        a.B, a.slots, a.accept_len = B, _ints(slots, "slots", self.index), _ints(accept_len, "accept_len", self.index)
-        a.num_paths, a.path_len, a.paths = n, path_len, _ints(paths, "paths", self.index)
-        a.chosen = _ints(chosen, "chosen", self.index, (B,))
+        a = jd.jd_commit_args_t()
+        _COMMIT_ARGS.pack_into(a, 0, B, _ints(slots, "slots", self.index), _ints(accept_len, "accept_len", self.index), n, path_len,
+                               _ints(paths, "paths", self.index), _ints(chosen, "chosen", self.index, (B,)))
         st = self._lib.jd_cache_commit(self.h, a, _stream(stream, self.index))
         if st != jd.JD_OK:
             raise jd.JdError(st, "jd_cache_commit")

@@ -44,6 +44,31 @@ def test_struct_sizes_match_a_c_compiler(tmp_path):
     assert [int(x) for x in got] == [C.sizeof(getattr(jd, n)) for n in names]
 
 
+def test_packed_arguments_have_the_struct_layout():
+    from paper_2501_19309_b200 import cache
+    for packer, name in ((cache._ROPE_ARGS, "jd_rope_args_t"), (cache._APPEND_ARGS, "jd_append_args_t"), (cache._ATTEND_ARGS, "jd_attend_args_t"),
+                         (cache._COMMIT_ARGS, "jd_commit_args_t")):
+        t = getattr(jd, name)
+        flat = []
+
+        def leaves(s, base):
+            for f, ft in s._fields_:
+                off = base + getattr(s, f).offset
+                if isinstance(ft, type) and issubclass(ft, C.Structure):
+                    leaves(ft, off)
+                else:
+                    flat.append((off, C.sizeof(ft)))
+
+        leaves(t, 0)
+        a = t()
+        packer.pack_into(a, 0, *range(1, len(flat) + 1))
+        raw = bytes(a)
+        for i, (off, size) in enumerate(flat):
+            got = int.from_bytes(raw[off:off + size], "little")
+            assert got == i + 1 or np.frombuffer(raw[off:off + size], dtype=np.float32)[0] == i + 1, (name, i)
+        assert packer.size <= C.sizeof(t)
+
+
 def config(**kw):
     base = dict(num_layers=2, num_pages=100, page_size=16, q_heads=8, kv_heads=2, head_dim=128, max_seqs=4, max_pages=32,
                 max_nodes=26, dtype=jd.JD_DTYPE_BF16, device=0)
