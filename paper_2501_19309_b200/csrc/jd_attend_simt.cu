@@ -58,6 +58,7 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(AttendParams p) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int g = blockIdx.x / p.row_blocks, rb = blockIdx.x - g * p.row_blocks;
   const int r0 = rb * kRows, nrows = min(kRows, p.rows - r0);
+  pdl_wait();
   pdl_trigger();
   if (rb == 0 && tid == 0) split_none(p, g);
   unit_prefix(p, prefix, warp_sums);
@@ -364,8 +365,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendPara
 template <typename T>
 cudaError_t launch_simt(const AttendParams& p, cudaStream_t st) {
   auto kernel = p.c.head_dim <= 128 ? attend_simt_kernel<T, 1> : attend_simt_kernel<T, 2>;
-  kernel<<<(unsigned)(p.groups * p.row_blocks), kThreads, simt_smem(p.c.head_dim), st>>>(p);
-  return cudaGetLastError();
+  return launch_chained(kernel, dim3((unsigned)(p.groups * p.row_blocks)), dim3(kThreads), simt_smem(p.c.head_dim), st, p);
 }
 
 template <typename K>

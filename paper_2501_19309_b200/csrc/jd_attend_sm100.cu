@@ -211,9 +211,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   volatile int* abort_flag = &sh.abort_flag;
   const int g = blockIdx.x / p.row_blocks, rb = blockIdx.x - g * p.row_blocks;
 
-  pdl_trigger();
   if (tid == 0) {
-    if (rb == 0) split_none(p, g);
     for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&sh.full[i]), 1); mbar_init(smem_u32(&sh.empty[i]), 1); }
     for (int w = 0; w < 2; ++w) {
       mbar_init(smem_u32(&sh.s_full[w]), 1);
@@ -230,6 +228,9 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
+  pdl_wait();      // so far nothing was touched that another kernel knows of
+  pdl_trigger();
+  if (rb == 0 && tid == 0) split_none(p, g);
   unit_prefix(p, sh.prefix, sh.warp_sums, sh.extents);   // ends with a barrier
   tc_fence_after();
   const int64_t units = (int64_t)sh.prefix[p.B] * p.c.kv_heads;
@@ -723,8 +724,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
 
 template <int D, int kMode>
 cudaError_t launch(const AttendParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st) {
-  attend_sm100_kernel<D, kMode><<<(unsigned)(p.groups * p.row_blocks), kThreads, attend_smem<D, kMode>(), st>>>(tm_k, tm_v, p);
-  return cudaGetLastError();
+  return launch_chained(attend_sm100_kernel<D, kMode>, dim3((unsigned)(p.groups * p.row_blocks)), dim3(kThreads), attend_smem<D, kMode>(), st, tm_k, tm_v, p);
 }
 template <int D>
 cudaError_t launch_mode(const AttendParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st) {

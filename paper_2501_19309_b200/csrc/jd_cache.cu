@@ -1,7 +1,7 @@
 // The paged cache: handle, argument checks, and the kernels that keep its pages.
 //
 // The tables are small and every call is a handful of dependent loads, so these kernels are bound by latency: one
-// launch each (two where pages are copied), no host round trip, no lists that grow. The pool's state is a count of
+// launch each (a compaction: three), no host round trip, no lists that grow. The pool's state is a count of
 // owners per page and a bitmap of the free ones. Releasing a page is one atomic on its count and, for the last owner,
 // one on its bit: the result does not depend on the order. Handing out pages is one block's scan of the bitmap, lowest
 // pages first, so that the same calls always give the same page numbers.
@@ -59,6 +59,8 @@ __device__ __forceinline__ void cut_slot(const CacheView& c, int slot, int held,
 
 __global__ void __launch_bounds__(256) truncate_kernel(CacheView c, const int32_t* slots, const int32_t* length) {
   __shared__ int flag;
+  pdl_wait();
+  pdl_trigger();
   const int b = blockIdx.x, slot = slot_of(c, slots, b);
   if (slot < 0) return;
   if (named_before(slots, b, slot, &flag)) { if (threadIdx.x == 0) set_status(c.status, JD_ERR_BAD_INDEX); return; }
@@ -72,6 +74,8 @@ __global__ void __launch_bounds__(256) truncate_kernel(CacheView c, const int32_
 
 __global__ void __launch_bounds__(256) fork_kernel(CacheView c, int n, const int32_t* src, const int32_t* dst) {
   __shared__ int flag;
+  pdl_wait();
+  pdl_trigger();
   const int i = blockIdx.x;
   const int s = __ldg(src + i), d = __ldg(dst + i);
   if (s == -1 || d == -1) return;
@@ -124,13 +128,34 @@ __device__ __forceinline__ int block_exclusive(int v, int* warp_sums, int* all) 
   return x - v + (warp > 0 ? warp_sums[warp - 1] : 0);
 }
 
-// Hands out pages: one block, thread b for sequence b, then all threads over the bitmap's words and over the
-// table entries. page_list[k] = the k-th page handed out.
-__global__ void __launch_bounds__(kBookThreads) reserve_kernel(CacheView c, int B, const int32_t* slots, int n, int* page_list,
-                                                               int* copy_src, int* copy_dst, int* copy_rows) {
+// Copies n rows of page `from` to page `to` in one plane (layer, K or V, head); by kCopyThreads threads of which this is number t.
+constexpr int kCopyThreads = 256;
+__device__ __forceinline__ void copy_rows_of_page(const CacheView& c, int from, int to, int n, int plane, int t) {
+  const int units = n * (c.row_bytes / 16), head = plane % c.kv_heads, lk = plane / c.kv_heads;
+  char* base = (lk & 1) ? c.v : c.k;
+  const uint4* s = reinterpret_cast<const uint4*>(base + page_row(c, lk >> 1, from, head, 0) * c.row_bytes);
+  uint4* d = reinterpret_cast<uint4*>(base + page_row(c, lk >> 1, to, head, 0) * c.row_bytes);
+  for (int u0 = t; u0 < units; u0 += 4 * kCopyThreads) {   // four loads in flight
+    uint4 x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (u0 + k * kCopyThreads < units) x[k] = s[u0 + k * kCopyThreads];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (u0 + k * kCopyThreads < units) d[u0 + k * kCopyThreads] = x[k];
+  }
+}
+
+// Hands out pages and copies those that are about to be written and have other owners, in one launch without a block waiting for
+// another: every block works out the whole plan from the state as it stands (thread b for sequence b, then all threads over
+// the bitmap's words), copies its share of the rows, and counts itself done; the last one done writes the new state, which
+// nobody reads any more. page_list[k] = the k-th page handed out; all blocks write the same.
+__global__ void __launch_bounds__(kBookThreads) reserve_kernel(CacheView c, int B, const int32_t* slots, int n, int* page_list, int* blocks_done) {
   __shared__ int s_slot[kMaxCacheBatch], s_last[kMaxCacheBatch], s_off[kMaxCacheBatch], s_first[kMaxCacheBatch], warp_sums[32];
-  __shared__ bool s_copy[kMaxCacheBatch];
-  __shared__ int fail;
+  __shared__ int s_rows[kMaxCacheBatch];   // rows to copy, 0: none
+  __shared__ int fail, last_one;
+  pdl_wait();
+  pdl_trigger();
   const int b = threadIdx.x;
   if (b == 0) fail = 0;
   s_slot[b] = b < B ? slot_of(c, slots, b) : -1;
@@ -170,33 +195,45 @@ __global__ void __launch_bounds__(kBookThreads) reserve_kernel(CacheView c, int 
   int mine = 0;
   for (int w = w0; w < w1; ++w) mine += __popc(c.free_bits[w]);
   const int first = block_exclusive(mine, warp_sums, &available);
-  if (fail || total > available) {   // nothing changes
-    if (b == 0) set_status(c.status, JD_ERR_PAGES);
-    if (b < B) copy_rows[b] = 0;
-    return;
-  }
-  int rank = first;
-  for (int w = w0; w < w1 && rank < total; ++w) {
-    uint32_t bits = c.free_bits[w], taken = 0;
-    while (bits && rank < total) {
-      const int i = __ffs(bits) - 1;
-      bits &= bits - 1;
-      taken |= 1u << i;
-      c.refs[32 * w + i] = 1;
-      page_list[rank++] = 32 * w + i;
-    }
-    if (taken) c.free_bits[w] &= ~taken;
+  const bool ok = !fail && total <= available;   // else nothing changes
+  if (!ok && b == 0) set_status(c.status, JD_ERR_PAGES);
+  if (ok) {
+    int rank = first;
+    for (int w = w0; w < w1 && rank < total; ++w)
+      for (uint32_t bits = c.free_bits[w]; bits && rank < total; bits &= bits - 1) page_list[rank++] = 32 * w + __ffs(bits) - 1;
   }
   s_off[b] = off;
   s_first[b] = held - (copy ? 1 : 0);
-  s_copy[b] = copy;
+  s_rows[b] = ok && copy ? rows : 0;
   __syncthreads();
-  if (b < B) copy_rows[b] = copy ? rows : 0;
-  if (copy) {
-    const int to = page_list[off];
-    copy_src[b] = s_last[b];
-    copy_dst[b] = to;
-    c.table[(int64_t)slot * c.max_pages + last] = to;
+  if (ok) {
+    const int planes = c.layers * 2 * c.kv_heads;
+    constexpr int kGroups = kBookThreads / kCopyThreads;
+    for (int j = 0; j < B; ++j)
+      if (s_rows[j] > 0)
+        for (int plane = blockIdx.x * kGroups + b / kCopyThreads; plane < planes; plane += gridDim.x * kGroups)
+          copy_rows_of_page(c, s_last[j], page_list[s_off[j]], s_rows[j], plane, b % kCopyThreads);
+  }
+  __syncthreads();
+  if (b == 0) {
+    __threadfence();
+    last_one = atomicAdd(blocks_done, 1) == (int)gridDim.x - 1;
+    if (last_one) *blocks_done = 0;
+  }
+  __syncthreads();
+  if (!last_one || !ok) return;
+  int rank = first;
+  for (int w = w0; w < w1 && rank < total; ++w) {
+    uint32_t bits = c.free_bits[w], taken = 0;
+    for (; bits && rank < total; bits &= bits - 1, ++rank) {
+      const int i = __ffs(bits) - 1;
+      taken |= 1u << i;
+      c.refs[32 * w + i] = 1;
+    }
+    if (taken) c.free_bits[w] &= ~taken;
+  }
+  if (s_rows[b] > 0) {
+    c.table[(int64_t)slot * c.max_pages + last] = page_list[off];
     atomicSub(c.refs + s_last[b], 1);
   }
   if (slot >= 0 && want > held) c.held[slot] = want;
@@ -207,34 +244,16 @@ __global__ void __launch_bounds__(kBookThreads) reserve_kernel(CacheView c, int 
       const int mid = (lo + hi + 1) >> 1;
       if (s_off[mid] <= k) lo = mid; else hi = mid - 1;
     }
-    const int i = s_first[lo] + (k - s_off[lo]);
-    if (k > s_off[lo] || !s_copy[lo]) c.table[(int64_t)s_slot[lo] * c.max_pages + i] = page_list[k];
+    if (k > s_off[lo] || s_rows[lo] == 0) c.table[(int64_t)s_slot[lo] * c.max_pages + s_first[lo] + (k - s_off[lo])] = page_list[k];
   }
 }
 
-// Copies rows of pages in all layers, K and V: blockIdx.y = entry, blockIdx.x strides over (layer, K or V, head).
-__global__ void __launch_bounds__(256) copy_pages_kernel(CacheView c, const int* src, const int* dst, const int* rows,
-                                                         const int* count) {
+// Moves pages of a compaction: blockIdx.y strides over the moves, blockIdx.x over (layer, K or V, head).
+__global__ void __launch_bounds__(kCopyThreads) move_pages_kernel(CacheView c, const int* src, const int* dst, const int* count) {
   pdl_wait();
-  const int planes = c.layers * 2 * c.kv_heads;
-  for (int i = blockIdx.y; i < (count ? *count : (int)gridDim.y); i += gridDim.y) {
-    const int n = rows ? rows[i] : c.page_size;
-    if (n == 0) continue;
-    const int64_t units = (int64_t)n * c.row_bytes / 16;
-    const int from = src[i], to = dst[i];
-    for (int p = blockIdx.x; p < planes; p += gridDim.x) {
-      const int head = p % c.kv_heads, lk = p / c.kv_heads;
-      char* base = (lk & 1) ? c.v : c.k;
-      const uint4* s = reinterpret_cast<const uint4*>(base + page_row(c, lk >> 1, from, head, 0) * c.row_bytes);
-      uint4* d = reinterpret_cast<uint4*>(base + page_row(c, lk >> 1, to, head, 0) * c.row_bytes);
-      int64_t u = threadIdx.x;
-      for (; u + 768 < units; u += 1024) {   // four loads in flight
-        const uint4 a0 = s[u], a1 = s[u + 256], a2 = s[u + 512], a3 = s[u + 768];
-        d[u] = a0; d[u + 256] = a1; d[u + 512] = a2; d[u + 768] = a3;
-      }
-      for (; u < units; u += 256) d[u] = s[u];
-    }
-  }
+  pdl_trigger();
+  for (int i = blockIdx.y; i < *count; i += gridDim.y) 
+    for (int plane = blockIdx.x; plane < c.layers * 2 * c.kv_heads; plane += gridDim.x) copy_rows_of_page(c, src[i], dst[i], c.page_size, plane, threadIdx.x);
 }
 
 // Commit: blocks (x, b) move 16-byte columns of sequence b's kept rows, every thread its own column through all rows in
@@ -248,6 +267,8 @@ __global__ void __launch_bounds__(kMoveThreads) commit_kernel(CacheView c, const
   __shared__ int64_t s_from[kMaxNodes], s_to[kMaxNodes];
   __shared__ int s_node[kMaxNodes];
   __shared__ int flag, s_cut, s_moves, s_last;
+  pdl_wait();
+  pdl_trigger();
   const int b = blockIdx.y, slot = slot_of(c, slots, b);
   if (slot < 0) return;
   if (named_before(slots, b, slot, &flag)) { if (threadIdx.x == 0) set_status(c.status, JD_ERR_BAD_INDEX); return; }
@@ -323,6 +344,8 @@ __global__ void __launch_bounds__(kMoveThreads) commit_kernel(CacheView c, const
 __global__ void __launch_bounds__(kBookThreads) compact_plan_kernel(CacheView c, int* map, int* move_src, int* move_dst, int* move_cnt,
                                                                     int32_t* used_out) {
   __shared__ int warp_sums[32];
+  pdl_wait();
+  pdl_trigger();
   const int t = threadIdx.x, words = (c.pages + 31) >> 5, per = (words + kBookThreads - 1) / kBookThreads;
   const int w0 = min(t * per, words), w1 = min(w0 + per, words);
   auto used_bits = [&](int w) {
@@ -371,6 +394,8 @@ __global__ void __launch_bounds__(kBookThreads) compact_plan_kernel(CacheView c,
 
 // Step 2: the tables' page numbers. Runs behind the plan and beside or behind the copies.
 __global__ void __launch_bounds__(256) remap_kernel(CacheView c, const int* map) {
+  pdl_wait();
+  pdl_trigger();
   const int slot = blockIdx.x;
   int len, held;
   slot_state(c, slot, len, held);
@@ -409,9 +434,7 @@ size_t carve_cache(const jd_cache_config_t& g, char* base, jd_cache_s* c) {
   };
   unsigned* status = (unsigned*)take(256);
   int* cnt = (int*)take(kMaxCacheBatch * 4);
-  int* cs = (int*)take(kMaxCacheBatch * 4);
-  int* cd = (int*)take(kMaxCacheBatch * 4);
-  int* cr = (int*)take(kMaxCacheBatch * 4);
+  int* rc = (int*)take(256);
   int* pl = (int*)take((size_t)g.num_pages * 4);
   int* ms = (int*)take((size_t)g.num_pages * 4);
   int* md = (int*)take((size_t)g.num_pages * 4);
@@ -422,7 +445,7 @@ size_t carve_cache(const jd_cache_config_t& g, char* base, jd_cache_s* c) {
   const size_t rows = std::max<size_t>(std::min(rows_of(g), 256), 2 * kSimtRows);
   float* part = (float*)take((size_t)kMaxCtas * 2 * rows * (g.head_dim + kPartPad) * 4);
   if (c) {
-    c->status = status; c->commit_cnt = cnt; c->copy_src = cs; c->copy_dst = cd; c->copy_rows = cr;
+    c->status = status; c->commit_cnt = cnt; c->reserve_cnt = rc;
     c->page_list = pl; c->move_src = ms; c->move_dst = md; c->move_cnt = mc; c->split = sp; c->part = part;
   }
   return off;
@@ -550,16 +573,11 @@ jd_status_t jd_cache_reserve(jd_cache_t c, int32_t B, const int32_t* slots, int3
   if (!dev.ok()) return JD_ERR_CUDA;
   cudaStream_t st = (cudaStream_t)cuda_stream;
   const CacheView v = view_of(c);
-  reserve_kernel<<<1, kBookThreads, 0, st>>>(v, B, slots, n, c->page_list, c->copy_src, c->copy_dst, c->copy_rows);
-  cudaError_t err = cudaGetLastError();
-  if (err == cudaSuccess) {
-    // Most reserves copy nothing: the grid is kept to about two blocks per SM, each striding over the planes.
-    const int planes = v.layers * 2 * v.kv_heads;
-    const int per = std::max(1, std::min(planes, (4 * c->num_sms + B - 1) / B));
-    err = launch_chained(copy_pages_kernel, dim3((unsigned)per, (unsigned)B), dim3(256), 0, st, v, (const int*)c->copy_src,
-                         (const int*)c->copy_dst, (const int*)c->copy_rows, (const int*)nullptr);
-  }
-  return finish(c, err, st);
+  // One block is enough unless pages are copied, which the host does not know: a group of
+  // 256 threads for each plane, up to what is resident at once.
+  const int blocks = (v.layers * 2 * v.kv_heads + kBookThreads / kCopyThreads - 1) / (kBookThreads / kCopyThreads);
+  return finish(c, launch_chained(reserve_kernel, dim3((unsigned)std::min(blocks, 2 * c->num_sms)), dim3(kBookThreads), 0, st, v, B, slots, n,
+                                  c->page_list, c->reserve_cnt), st);
 }
 
 jd_status_t jd_cache_append(jd_cache_t c, const jd_append_args_t* a, void* cuda_stream) {
@@ -637,25 +655,24 @@ jd_status_t jd_cache_commit(jd_cache_t c, const jd_commit_args_t* a, void* cuda_
   const CacheView v = view_of(c);
   const int64_t columns = (int64_t)v.layers * 2 * v.kv_heads * (v.row_bytes / 16);
   const int blocks = a->paths && a->path_len > 0 ? (int)std::min<int64_t>((columns + kMoveThreads - 1) / kMoveThreads, 65535) : 1;
-  commit_kernel<<<dim3((unsigned)blocks, (unsigned)a->B), kMoveThreads, 0, st>>>(v, a->slots, a->accept_len, a->num_paths, a->path_len, a->paths,
-                                                                                 c->cfg.max_nodes, a->chosen, c->commit_cnt);
-  return finish(c, cudaGetLastError(), st);
+  return finish(c, launch_chained(commit_kernel, dim3((unsigned)blocks, (unsigned)a->B), dim3(kMoveThreads), 0, st, v, a->slots, a->accept_len,
+                                  a->num_paths, a->path_len, a->paths, c->cfg.max_nodes, a->chosen, c->commit_cnt), st);
 }
 
 jd_status_t jd_cache_fork(jd_cache_t c, int32_t n, const int32_t* src, const int32_t* dst, void* cuda_stream) {
   if (!c || n < 1 || n > kMaxCacheBatch || !src || !dst || !on4(src) || !on4(dst)) return JD_ERR_INVALID_ARG;
   OnDevice dev(c->cfg.device);
   if (!dev.ok()) return JD_ERR_CUDA;
-  fork_kernel<<<(unsigned)n, 256, 0, (cudaStream_t)cuda_stream>>>(view_of(c), n, src, dst);
-  return finish(c, cudaGetLastError(), (cudaStream_t)cuda_stream);
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  return finish(c, launch_chained(fork_kernel, dim3((unsigned)n), dim3(256), 0, st, view_of(c), n, src, dst), st);
 }
 
 jd_status_t jd_cache_truncate(jd_cache_t c, int32_t B, const int32_t* slots, const int32_t* length, void* cuda_stream) {
   if (!c || !batch_ok(c, B, slots) || !on4(length)) return JD_ERR_INVALID_ARG;
   OnDevice dev(c->cfg.device);
   if (!dev.ok()) return JD_ERR_CUDA;
-  truncate_kernel<<<(unsigned)B, 256, 0, (cudaStream_t)cuda_stream>>>(view_of(c), slots, length);
-  return finish(c, cudaGetLastError(), (cudaStream_t)cuda_stream);
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  return finish(c, launch_chained(truncate_kernel, dim3((unsigned)B), dim3(256), 0, st, view_of(c), slots, length), st);
 }
 
 jd_status_t jd_cache_compact(jd_cache_t c, int32_t* used, void* cuda_stream) {
@@ -664,12 +681,11 @@ jd_status_t jd_cache_compact(jd_cache_t c, int32_t* used, void* cuda_stream) {
   if (!dev.ok()) return JD_ERR_CUDA;
   cudaStream_t st = (cudaStream_t)cuda_stream;
   const CacheView v = view_of(c);
-  compact_plan_kernel<<<1, kBookThreads, 0, st>>>(v, c->page_list, c->move_src, c->move_dst, c->move_cnt, used);
-  remap_kernel<<<(unsigned)v.max_seqs, 256, 0, st>>>(v, c->page_list);
-  cudaError_t err = cudaGetLastError();
+  cudaError_t err = launch_chained(compact_plan_kernel, dim3(1), dim3(kBookThreads), 0, st, v, c->page_list, c->move_src, c->move_dst, c->move_cnt, used);
+  if (err == cudaSuccess) err = launch_chained(remap_kernel, dim3((unsigned)v.max_seqs), dim3(256), 0, st, v, (const int*)c->page_list);
   if (err == cudaSuccess)
-    err = launch_chained(copy_pages_kernel, dim3((unsigned)std::min(v.layers * 2 * v.kv_heads, 16), (unsigned)std::min(v.pages, 64)), dim3(256), 0, st, v,
-                         (const int*)c->move_src, (const int*)c->move_dst, (const int*)nullptr, (const int*)c->move_cnt);
+    err = launch_chained(move_pages_kernel, dim3((unsigned)std::min(v.layers * 2 * v.kv_heads, 16), (unsigned)std::min(v.pages, 64)), dim3(256), 0, st, v,
+                         (const int*)c->move_src, (const int*)c->move_dst, (const int*)c->move_cnt);
   return finish(c, err, st);
 }
 

@@ -17,9 +17,7 @@ struct jd_cache_s {
   // regions of the workspace
   unsigned* status;
   int* commit_cnt;            // [1024] blocks of the sequence that have finished moving (self-resetting)
-  int* copy_src;              // [1024] page copies decided by jd_cache_reserve: from, to, rows (0: none)
-  int* copy_dst;
-  int* copy_rows;
+  int* reserve_cnt;           // [1] blocks of a reserve that are done (self-resetting)
   int* page_list;             // [num_pages] pages handed out by a reserve; page map of a compaction
   int* move_src;              // [num_pages] compaction: pages to move, and where to
   int* move_dst;
@@ -213,8 +211,8 @@ __device__ __forceinline__ void split_set(const AttendParams& p, int g, int64_t 
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
-// Launches a kernel that may start before the one in front of it has ended; it calls pdl_wait() before it reads
-// anything that one writes.
+// Launches a kernel that may start before the one in front of it on the stream has ended; it calls pdl_wait() before it reads or
+// writes anything that another kernel touches. (In front of a kernel that triggers nothing itself this saves the launch's latency alone.)
 template <typename... Params, typename... Args>
 inline cudaError_t launch_chained(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
   cudaLaunchConfig_t cfg = {};

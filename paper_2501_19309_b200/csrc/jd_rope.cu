@@ -125,6 +125,8 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const T* x, T* out, 
                                                             const int32_t* __restrict__ positions, const float* __restrict__ inv_freq,
                                                             int half, int layout, float amplitude, int inverse, int per_block) {
   __shared__ float2 cs[kTokensPerBlock][kMaxHalf];
+  pdl_wait();
+  pdl_trigger();
   const int64_t t0 = (int64_t)blockIdx.x * per_block;
   const int n = (int)min((int64_t)per_block, tokens - t0);
   for (int i = threadIdx.x; i < n * half; i += kRopeThreads) {
@@ -162,6 +164,8 @@ template <typename T, bool kVec>
 __global__ void __launch_bounds__(kRopeThreads) append_kernel(AppendParams p) {
   __shared__ float2 cs[kMaxHalf];
   __shared__ int dup;
+  pdl_wait();
+  pdl_trigger();
   const int b = blockIdx.x / p.T, t = blockIdx.x - b * p.T;
   const CacheView& c = p.c;
   const int slot = slot_of(c, p.slots, b);
@@ -233,10 +237,9 @@ cudaError_t launch_rope(const jd_rope_args_t& a, int64_t xs, int64_t os, cudaStr
   const int per_block = std::max(1, std::min(kTokensPerBlock, kRopeThreads * kRopeUnitsPerThread / std::max(1, units)));
   const int64_t blocks = (a.tokens + per_block - 1) / per_block;
   if (blocks > 0x7FFFFFFF) return cudaErrorInvalidValue;
-  auto kernel = vec ? rope_kernel<T, true> : rope_kernel<T, false>;
-  kernel<<<(unsigned)blocks, kRopeThreads, 0, st>>>((const T*)a.x, (T*)a.out, a.tokens, a.heads, a.head_dim, xs, os, a.positions,
-                                                    a.rope.inv_freq, half, a.rope.layout, a.rope.amplitude, a.inverse, per_block);
-  return cudaGetLastError();
+  return launch_chained(vec ? rope_kernel<T, true> : rope_kernel<T, false>, dim3((unsigned)blocks), dim3(kRopeThreads), 0, st, (const T*)a.x,
+                        (T*)a.out, a.tokens, a.heads, a.head_dim, xs, os, a.positions, a.rope.inv_freq, half, a.rope.layout, a.rope.amplitude,
+                        a.inverse, per_block);
 }
 
 }  // namespace
@@ -266,14 +269,9 @@ cudaError_t run_append(const CacheView& c, const jd_append_args_t& a, int q_head
   // few nodes: one piece per thread, spread over the SMs; many: a block per node
   const int parts = nodes >= 512 ? 1 : std::max(1, std::min(8, (units + kRopeThreads - 1) / kRopeThreads));
   const dim3 grid((unsigned)nodes, (unsigned)parts);
-  if (dtype == JD_DTYPE_F32) {
-    if (vec) append_kernel<float, true><<<grid, kRopeThreads, 0, st>>>(p);
-    else append_kernel<float, false><<<grid, kRopeThreads, 0, st>>>(p);
-  } else {
-    if (vec) append_kernel<__nv_bfloat16, true><<<grid, kRopeThreads, 0, st>>>(p);
-    else append_kernel<__nv_bfloat16, false><<<grid, kRopeThreads, 0, st>>>(p);
-  }
-  return cudaGetLastError();
+  auto kernel = dtype == JD_DTYPE_F32 ? (vec ? append_kernel<float, true> : append_kernel<float, false>)
+                                      : (vec ? append_kernel<__nv_bfloat16, true> : append_kernel<__nv_bfloat16, false>);
+  return launch_chained(kernel, grid, dim3(kRopeThreads), 0, st, p);
 }
 
 bool rope_valid(const jd_rope_t& r, int head_dim) { return rope_ok(r, head_dim); }
