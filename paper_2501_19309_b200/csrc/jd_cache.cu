@@ -163,8 +163,10 @@ __global__ void __launch_bounds__(kBookThreads) reserve_kernel(CacheView c, int 
   __syncthreads();
   int slot = s_slot[b], len = 0, held = 0, want = 0, last = 0, rows = 0;
   if (slot >= 0 && slots) {
-    for (int j = 0; j < b; ++j)
-      if (s_slot[j] == slot) { set_status(c.status, JD_ERR_BAD_INDEX); slot = -1; break; }
+    bool named = false;
+#pragma unroll 8
+    for (int j = 0; j < b; ++j) named |= s_slot[j] == slot;
+    if (named) { set_status(c.status, JD_ERR_BAD_INDEX); slot = -1; }
   }
   if (slot >= 0) {
     slot_state(c, slot, len, held);
@@ -184,6 +186,7 @@ __global__ void __launch_bounds__(kBookThreads) reserve_kernel(CacheView c, int 
   if (slot >= 0 && s_last[b] >= 0) {
     int owners = c.refs[s_last[b]];
     if (owners > 1)
+#pragma unroll 8
       for (int j = 0; j < b; ++j) owners -= s_last[j] == s_last[b];
     copy = owners > 1;
   }
@@ -205,8 +208,7 @@ __global__ void __launch_bounds__(kBookThreads) reserve_kernel(CacheView c, int 
   s_off[b] = off;
   s_first[b] = held - (copy ? 1 : 0);
   s_rows[b] = ok && copy ? rows : 0;
-  __syncthreads();
-  if (ok) {
+  if (__syncthreads_or(s_rows[b] > 0)) {
     const int planes = c.layers * 2 * c.kv_heads;
     constexpr int kGroups = kBookThreads / kCopyThreads;
     for (int j = 0; j < B; ++j)
