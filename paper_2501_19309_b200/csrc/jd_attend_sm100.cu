@@ -466,8 +466,12 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       for (int t = kPair ? 0 : w; t < x.tiles; t += kPair ? 1 : 2, ++done) {
         const int kv0 = (x.tile0 + t) * kTile;
         const bool tail = kv0 + kTile > ex.ctx;      // holds nodes, or ends behind the sequence
+        wait(smem_u32(&sh.s_full[w]), s_phase, abort_flag);
+        s_phase ^= 1u;
         // V rows that are no tokens may hold anything: 0 x NaN would reach every row. They become zeroes; and so do values of nodes
         // that are not finite, which the rows that see them get back at the end. (Chain 1's products of a tile are issued behind chain 0's.)
+        // Behind the wait for S, because only then has the slot's last content been used up: waiting for V any earlier could take
+        // that content's phase for this one's, and zeroes would go into a tile that is still to be multiplied.
         if (tail && (!kPair || w == 0)) {
           const int item = 2 * (tile_count + t) + 1;
           wait(smem_u32(&sh.full[item % kStages]), (uint32_t)(item / kStages) & 1u, abort_flag);
@@ -489,8 +493,6 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           }
           fence_async_proxy();
         }
-        wait(smem_u32(&sh.s_full[w]), s_phase, abort_flag);
-        s_phase ^= 1u;
         if (warp_live) {
           tc_fence_after();
           uint32_t s[kCols];

@@ -221,6 +221,25 @@ def test_attend(lens, T, page, q_heads, kv_heads, D, dtype, variant, style):
     assert torch.equal(r[0]["out"], again[0]["out"]) and torch.equal(r[0]["lse"], again[0]["lse"])
 
 
+@pytest.mark.parametrize("T,q_heads,kv_heads,D,ctx", [(17, 10, 2, 128, 5338), (17, 6, 2, 128, 5338), (16, 32, 8, 64, 3333), (1, 8, 8, 128, 7000),
+                                                      (26, 16, 2, 128, 3000), (3, 8, 8, 64, 2049)])
+def test_attend_many_pieces_repeat_bit_for_bit(T, q_heads, kv_heads, D, ctx):
+    """Sequences cut into pieces of odd numbers of tiles whose last tile ends behind the sequence: the same bits every time."""
+    rng = np.random.default_rng(T)
+    c = L.filled_cache([ctx] * 16, T, page=32, q_heads=q_heads, kv_heads=kv_heads, D=D, max_nodes=T, seed=1)
+    q = rand((16, T, q_heads, D), 3)
+    tree = L.device_tree([L.random_tree(T, rng) for _ in range(16)])
+    first = c.attend(0, q, tree)
+    simt = c.attend(0, q, tree, variant="simt")
+    runs = [c.attend(0, q, tree) for _ in range(30)]
+    torch.cuda.synchronize()
+    for r in runs:
+        assert torch.equal(r["out"], first["out"]) and torch.equal(r["lse"], first["lse"])
+    # both kernels' outputs are weighted means of values of size 1: a weight that is off by 2^-8 moves them by no more than
+    # 2^-8 of the sum of weight x |value|, which is below 1 here, and each rounds its output once
+    assert (first["out"].float() - simt["out"].float()).abs().max() <= 2.0 ** -8 * (1 + 2 * simt["out"].float().abs().max())
+
+
 VARIANTS = [("simt", "bf16", 64), ("simt", "f32", 72), ("tensor", "bf16", 64), ("tensor", "bf16", 128)]
 
 
