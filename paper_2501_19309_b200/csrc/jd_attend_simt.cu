@@ -5,7 +5,7 @@
 // head - and walks its run of tiles of 64 cached tokens (jd_cache.h says how runs are cut). Per tile: K and V to shared
 // memory, 16 x 64 scores by 256 threads (four rows of one token each), running maximum and sum by a warp for two rows,
 // and the weighted sum of V with every warp taking an eighth of the tokens for all 16 rows and up to 256 columns in
-// registers, so that one shared-memory read of V serves 16 rows. The warps' sums meet once per segment. For float32 the
+// registers, so that one shared-memory read of V serves 16 rows. The warps' sums meet once per piece of a segment. For float32 the
 // product with the shared-memory operands bounds it (about twice the HBM time of a tile at two CTAs per SM).
 #include <algorithm>
 #include <cmath>
@@ -18,8 +18,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kTile = 1 << kSimtTileShift;
-constexpr int kRows = kSimtRows;
-constexpr int kScorePad = 20;     // floats between tokens of the score buffer: 16 rows + padding, 16-byte aligned
 
 template <typename T> __device__ __forceinline__ void load4(const T* p, float* v);
 template <> __device__ __forceinline__ void load4<float>(const float* p, float* v) {
@@ -37,15 +35,24 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, const float* v) {
   *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
 }
 
+// 16 bytes from global to shared memory without a register in between; zeroes if !there (src is then not read, but has to be an address)
+__device__ __forceinline__ void copy16_or_zero(float* dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+
 __host__ __device__ constexpr int pitch_of(int head_dim) { return head_dim + 4; }   // floats; keeps 16-byte accesses off one bank group
 
-size_t simt_smem(int head_dim) {
-  return sizeof(float) * ((size_t)2 * kTile * pitch_of(head_dim) + kRows * head_dim + kTile * kScorePad);
+// floats between tokens of the score buffer: the rows and padding, 16-byte aligned
+__host__ __device__ constexpr int score_pad(int rows) { return rows == 4 ? 12 : rows + 4; }
+size_t simt_smem(int head_dim, int rows) {
+  return sizeof(float) * ((size_t)2 * kTile * pitch_of(head_dim) + rows * head_dim + kTile * score_pad(rows));
 }
 
 // kCols: groups of 128 columns that a lane's accumulators cover (head_dim <= 128 kCols)
-template <typename T, int kCols>
-__global__ void __launch_bounds__(kThreads) attend_simt_kernel(AttendParams p) {
+// kRows: query rows of the block, 4 or 16
+template <typename T, int kCols, int kRows>
+__global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_simt_kernel(AttendParams p) {
+  constexpr int kScorePad = score_pad(kRows);
   extern __shared__ __align__(16) float smem[];
   __shared__ int prefix[kMaxCacheBatch + 1], warp_sums[kThreads / 32], pages[kTile / 8];
   __shared__ float s_m[kRows], s_l[kRows], s_fac[kRows];
@@ -107,43 +114,66 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(AttendParams p) {
       }
       __syncthreads();
       const int vec = D / 4;
-      for (int i = tid; i < kTile * vec; i += kThreads) {
-        const int r = i / vec, d = (i - r * vec) * 4;
-        float kx[4] = {0.f, 0.f, 0.f, 0.f}, vx[4] = {0.f, 0.f, 0.f, 0.f};
-        if (r < nkv) {   // rows behind the sequence may hold anything: they become zeroes here
-          const int kv = kv0 + r;
+      if constexpr (sizeof(T) == 4) {              // straight to shared memory; rows behind the sequence may hold anything: zeroes
+        for (int i = tid; i < kTile * vec; i += kThreads) {
+          const int r = i / vec, d = (i - r * vec) * 4;
+          const int kv = kv0 + min(r, max(nkv - 1, 0));
           const int page = pages[(kv >> p.c.page_shift) - (kv0 >> p.c.page_shift)];
           const int64_t off = page_row(p.c, p.layer, page, head, kv & (p.c.page_size - 1)) * D + d;
-          load4<T>(kbase + off, kx);
-          load4<T>(vbase + off, vx);
+          copy16_or_zero(sK + r * pitch + d, kbase + off, r < nkv);
+          copy16_or_zero(sV + r * pitch + d, vbase + off, r < nkv);
         }
-        store4(sK + r * pitch + d, kx);
-        store4(sV + r * pitch + d, vx);
+        asm volatile("cp.async.wait_all;" ::: "memory");
+      } else {
+        constexpr int kAhead = 4;                  // pieces of K and of V whose loads are under way at once
+        for (int i0 = tid; i0 < kTile * vec; i0 += kAhead * kThreads) {
+          float kx[kAhead][4], vx[kAhead][4];
+#pragma unroll
+          for (int j = 0; j < kAhead; ++j) {
+            const int i = i0 + j * kThreads, r = i / vec, d = (i - r * vec) * 4;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) kx[j][e] = vx[j][e] = 0.f;
+            if (r < nkv) {
+              const int kv = kv0 + r;
+              const int page = pages[(kv >> p.c.page_shift) - (kv0 >> p.c.page_shift)];
+              const int64_t off = page_row(p.c, p.layer, page, head, kv & (p.c.page_size - 1)) * D + d;
+              load4<T>(kbase + off, kx[j]);
+              load4<T>(vbase + off, vx[j]);
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < kAhead; ++j) {
+            const int i = i0 + j * kThreads, r = i / vec, d = (i - r * vec) * 4;
+            if (i < kTile * vec) {
+              store4(sK + r * pitch + d, kx[j]);
+              store4(sV + r * pitch + d, vx[j]);
+            }
+          }
+        }
       }
       __syncthreads();
-      {   // scores: token tid % 64, rows 4 (tid / 64) ..
-        const int kv = tid & (kTile - 1), rg = (tid >> kSimtTileShift) * 4;
-        float s[4] = {0.f, 0.f, 0.f, 0.f};
+      {   // scores: token tid % 64, kRows / 4 rows from (tid / 64) on
+        constexpr int kMine = kRows / 4;
+        const int kv = tid & (kTile - 1), rg = (tid >> kSimtTileShift) * kMine;
+        float s[kMine] = {};
+#pragma unroll 4
         for (int d = 0; d < D; d += 4) {
           const float4 x = *reinterpret_cast<const float4*>(sK + kv * pitch + d);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
+          for (int r = 0; r < kMine; ++r) {
             const float4 y = *reinterpret_cast<const float4*>(sQ + (rg + r) * D + d);
             s[r] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s[r]))));
           }
         }
         const int node = kv0 + kv - ex.ctx;   // < 0: context
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
+        for (int r = 0; r < kMine; ++r) {
           const bool see = kv < nkv && (node < 0 || ((s_mask[rg + r][node >> 5] >> (node & 31)) & 1u));
-          s[r] = see ? s[r] * p.scale_log2 : -INFINITY;
+          sS[kv * kScorePad + rg + r] = see ? s[r] * p.scale_log2 : -INFINITY;
         }
-        store4(sS + kv * kScorePad + rg, s);
       }
       __syncthreads();
-#pragma unroll
-      for (int k = 0; k < kRows / 8; ++k) {   // statistics: a warp for two rows
-        const int r = warp * (kRows / 8) + k;
+      for (int r = warp; r < kRows; r += kThreads / 32) {   // statistics: a row per warp and turn
         float* a = sS + lane * kScorePad + r;
         float* c = sS + (lane + 32) * kScorePad + r;
         const float x = *a, y = *c;
@@ -205,29 +235,26 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(AttendParams p) {
       }
     }
 
-    // the warps' sums, one after the other, in the K buffer
-    for (int w = 0; w < kThreads / 32; ++w) {
-      __syncthreads();
-      if (warp == w) {
+    // the warps' sums meet over the K and V buffers, which hold 8 x kRows x D floats: each its own place, then all added
+    __syncthreads();
 #pragma unroll
-        for (int r = 0; r < kRows; ++r)
+    for (int r = 0; r < kRows; ++r)
 #pragma unroll
-          for (int j = 0; j < kCols; ++j) {
-            const int d = lane * 4 + 128 * j;
-            if (d >= D) continue;
-            float4* o = reinterpret_cast<float4*>(sK + r * pitch + d);
-            float4 x = w == 0 ? make_float4(0.f, 0.f, 0.f, 0.f) : *o;
-            x.x += acc[r][4 * j]; x.y += acc[r][4 * j + 1]; x.z += acc[r][4 * j + 2]; x.w += acc[r][4 * j + 3];
-            *o = x;
-          }
+      for (int j = 0; j < kCols; ++j) {
+        const int d = lane * 4 + 128 * j;
+        if (d < D) store4(sK + (warp * kRows + r) * D + d, &acc[r][4 * j]);
       }
-    }
     __syncthreads();
     const bool whole = ntiles == tiles;
     if (!whole && tile0 == 0 && rb == 0 && tid == 0) split_set(p, g, units, x);
     for (int i = tid; i < nrows * (D / 4); i += kThreads) {
       const int r = i / (D / 4), d = (i - r * (D / 4)) * 4;
-      float4 x = *reinterpret_cast<const float4*>(sK + r * pitch + d);
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kThreads / 32; ++w) {
+        const float4 y = *reinterpret_cast<const float4*>(sK + (w * kRows + r) * D + d);
+        x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+      }
       if (whole) {
         const int t = (r0 + r) / p.group, gq = (r0 + r) - t * p.group;
         if (t >= ex.nodes) continue;
@@ -247,34 +274,38 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(AttendParams p) {
 
 // Joins the partial results of split segments; rows of whole segments are written already.
 // out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i over the parts in order.
-// Block (k, g) takes a few rows of the segment that group g left unfinished, if it left one: with up to kJoinFewRows rows in all one row,
-// whose parts its warps take in turn (what the join costs is their latency, and a row of one long sequence has a part from
-// every SM); with more four rows, and a warp for each unless the parts are many.
+// Block (k, j) takes a few rows of the segments that groups j, j + gridDim.y, .. left unfinished: with up to kJoinFewRows rows in all one
+// row, whose parts its warps take in turn (what the join costs is their latency, and a row of one long sequence has a part
+// from every SM); with more four rows, and a warp for each unless the parts are many. gridDim.y is the number of segments where
+// that is smaller than the number of groups: blocks that find nothing to do cost the join more than its loads (16 us against 6 for
+// 4 trees x 208 rows with a block for every group).
 constexpr int kJoinWarps = 4, kJoinBatch = 8, kJoinFewRows = 32, kJoinFewParts = 32;
 __host__ __device__ constexpr int join_rows(int rows) { return rows <= kJoinFewRows ? 1 : kJoinWarps; }
 
-struct RowSum {
-  float m, l, o[2][4];   // columns 4 lane .. and 128 + 4 lane ..
+template <int kCols> struct RowSum {   // kCols: groups of 128 columns
+  float m, l, o[kCols][4];             // columns 4 lane .. of each group
 };
 
 // parts first, first + step, .. last of a row; at(g) is where part g stands
-template <typename At>
-__device__ __forceinline__ RowSum sum_parts(int first, int last, int step, int D, int lane, At at) {
-  RowSum s = {-INFINITY, 0.f, {}};
+template <int kCols, typename At>
+__device__ __forceinline__ RowSum<kCols> sum_parts(int first, int last, int step, int D, int lane, At at) {
+  RowSum<kCols> s = {-INFINITY, 0.f, {}};
   const int d = lane * 4;
   for (int g0 = first; g0 <= last; g0 += step * kJoinBatch) {
     float2 ml[kJoinBatch];
-    float4 x[kJoinBatch][2];
+    float4 x[kJoinBatch][kCols];
 #pragma unroll
     for (int k = 0; k < kJoinBatch; ++k) {
       const int g = g0 + k * step;
       ml[k] = make_float2(-INFINITY, 0.f);
-      x[k][0] = x[k][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) x[k][j] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (g <= last) {
         const float* part = at(g);
         ml[k] = __ldcg(reinterpret_cast<const float2*>(part + D));
-        if (d < D) x[k][0] = __ldcg(reinterpret_cast<const float4*>(part + d));
-        if (d + 128 < D) x[k][1] = __ldcg(reinterpret_cast<const float4*>(part + d + 128));
+#pragma unroll
+        for (int j = 0; j < kCols; ++j)
+          if (d + 128 * j < D) x[k][j] = __ldcg(reinterpret_cast<const float4*>(part + d + 128 * j));
       }
     }
     float top = s.m;
@@ -283,7 +314,7 @@ __device__ __forceinline__ RowSum sum_parts(int first, int last, int step, int D
     const float base = top == -INFINITY ? 0.f : top, f0 = exp2f(s.m - base);
     s.l *= f0;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < kCols; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) s.o[j][e] *= f0;
 #pragma unroll
@@ -292,7 +323,7 @@ __device__ __forceinline__ RowSum sum_parts(int first, int last, int step, int D
       s.l += f * ml[k].y;
       if (ml[k].x == -INFINITY) continue;   // a part that saw nothing has no say, whatever it holds
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
+      for (int j = 0; j < kCols; ++j) {
         s.o[j][0] = fmaf(f, x[k][j].x, s.o[j][0]); s.o[j][1] = fmaf(f, x[k][j].y, s.o[j][1]);
         s.o[j][2] = fmaf(f, x[k][j].z, s.o[j][2]); s.o[j][3] = fmaf(f, x[k][j].w, s.o[j][3]);
       }
@@ -302,70 +333,77 @@ __device__ __forceinline__ RowSum sum_parts(int first, int last, int step, int D
   return s;
 }
 
-template <typename T>
+template <typename T, int kCols>
 __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendParams p) {
-  __shared__ float4 s_o[kJoinWarps][2][32];
+  __shared__ float4 s_o[kJoinWarps][kCols][32];
   __shared__ float2 s_ml[kJoinWarps];
   pdl_wait();
-  const int g0 = blockIdx.y;
-  const int4 split = __ldcg(p.split + g0);
-  const int b = split.x, head = split.y, g1 = split.z;
-  if (b < 0) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int D = p.c.head_dim, pitch = D + kPartPad;
-  const int nodes = p.num_nodes ? min(max(__ldg(p.num_nodes + b), 0), p.T) : p.T;
-  const int rows = min(p.rows, nodes * p.group);
-  auto write = [&](int row, int d, const float* o, float m, float l) {   // columns d .. d + 3
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    const float y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-    const int t = row / p.group, h = head * p.group + row - t * p.group;
-    if (d < D) store4(reinterpret_cast<T*>(p.out + ((int64_t)b * p.T + t) * p.out_stride) + (int64_t)h * D + d, y);
-    if (d == 0 && p.lse) p.lse[((int64_t)b * p.T + t) * p.q_heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
-  };
-  auto place = [&](int row) {
-    const int rb = row / p.rows_per_block, r = row - rb * p.rows_per_block;
-    const float* base = p.part + ((int64_t)rb * 2 * p.part_rows + r) * pitch;
-    return [=](int g) { return base + ((int64_t)g * p.row_blocks * 2 + (g == g0 ? 1 : 0)) * p.part_rows * pitch; };
-  };
   const int block_rows = join_rows(p.rows), first_row = blockIdx.x * block_rows;
-  if (block_rows > 1 && g1 - g0 < kJoinFewParts) {
-    const int row = first_row + warp;
-    if (row >= rows) return;
-    const RowSum s = sum_parts(g0, g1, 1, D, lane, place(row));
-    write(row, lane * 4, s.o[0], s.m, s.l);
-    if (D > 128) write(row, 128 + lane * 4, s.o[1], s.m, s.l);
-    return;
-  }
-  for (int row = first_row; row < min(rows, first_row + block_rows); ++row) {
-    const RowSum s = sum_parts(g0 + warp, g1, kJoinWarps, D, lane, place(row));
-    __syncthreads();   // the last row's sums have been read
-    s_o[warp][0][lane] = make_float4(s.o[0][0], s.o[0][1], s.o[0][2], s.o[0][3]);
-    s_o[warp][1][lane] = make_float4(s.o[1][0], s.o[1][1], s.o[1][2], s.o[1][3]);
-    if (lane == 0) s_ml[warp] = make_float2(s.m, s.l);
-    __syncthreads();
-    if (warp < 2) {    // columns 128 warp ..
-      float top = -INFINITY;
+  // this block's groups, a lane each, then those among them that left a segment
+  for (int base_g = blockIdx.y; base_g < p.groups; base_g += 32 * gridDim.y) {
+   const int my_g = base_g + lane * gridDim.y;
+   const int4 mine = my_g < p.groups ? __ldcg(p.split + my_g) : make_int4(-1, 0, 0, 0);
+   for (unsigned left = __ballot_sync(0xffffffffu, mine.x >= 0); left; left &= left - 1) {
+    const int from = __ffs(left) - 1, g0 = base_g + from * gridDim.y;
+    const int b = __shfl_sync(0xffffffffu, mine.x, from), head = __shfl_sync(0xffffffffu, mine.y, from), g1 = __shfl_sync(0xffffffffu, mine.z, from);
+    const int nodes = p.num_nodes ? min(max(__ldg(p.num_nodes + b), 0), p.T) : p.T;
+    const int rows = min(p.rows, nodes * p.group);
+    auto write = [&](int row, int d, const float* o, float m, float l) {   // columns d .. d + 3
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const float y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+      const int t = row / p.group, h = head * p.group + row - t * p.group;
+      if (d < D) store4(reinterpret_cast<T*>(p.out + ((int64_t)b * p.T + t) * p.out_stride) + (int64_t)h * D + d, y);
+      if (d == 0 && p.lse) p.lse[((int64_t)b * p.T + t) * p.q_heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+    };
+    auto place = [&](int row) {
+      const int rb = row / p.rows_per_block, r = row - rb * p.rows_per_block;
+      const float* base = p.part + ((int64_t)rb * 2 * p.part_rows + r) * pitch;
+      return [=](int g) { return base + ((int64_t)g * p.row_blocks * 2 + (g == g0 ? 1 : 0)) * p.part_rows * pitch; };
+    };
+    if (block_rows > 1 && g1 - g0 < kJoinFewParts) {
+      const int row = first_row + warp;
+      if (row >= rows) continue;
+      const RowSum<kCols> s = sum_parts<kCols>(g0, g1, 1, D, lane, place(row));
 #pragma unroll
-      for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, s_ml[w].x);
-      const float base = top == -INFINITY ? 0.f : top;
-      float sum = 0.f, y[4] = {};
-#pragma unroll
-      for (int w = 0; w < kJoinWarps; ++w) {
-        const float f = exp2f(s_ml[w].x - base);
-        const float4 x = s_o[w][warp][lane];
-        sum += f * s_ml[w].y;
-        if (s_ml[w].x == -INFINITY) continue;
-        y[0] = fmaf(f, x.x, y[0]); y[1] = fmaf(f, x.y, y[1]); y[2] = fmaf(f, x.z, y[2]); y[3] = fmaf(f, x.w, y[3]);
-      }
-      write(row, 128 * warp + lane * 4, y, top, sum);
+      for (int j = 0; j < kCols; ++j) write(row, 128 * j + lane * 4, s.o[j], s.m, s.l);
+      continue;
     }
+    for (int row = first_row; row < min(rows, first_row + block_rows); ++row) {
+      const RowSum<kCols> s = sum_parts<kCols>(g0 + warp, g1, kJoinWarps, D, lane, place(row));
+      __syncthreads();   // the last row's sums have been read
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) s_o[warp][j][lane] = make_float4(s.o[j][0], s.o[j][1], s.o[j][2], s.o[j][3]);
+      if (lane == 0) s_ml[warp] = make_float2(s.m, s.l);
+      __syncthreads();
+      if (warp < kCols) {   // columns 128 warp ..
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, s_ml[w].x);
+        const float base = top == -INFINITY ? 0.f : top;
+        float sum = 0.f, y[4] = {};
+#pragma unroll
+        for (int w = 0; w < kJoinWarps; ++w) {
+          const float f = exp2f(s_ml[w].x - base);
+          const float4 x = s_o[w][warp][lane];
+          sum += f * s_ml[w].y;
+          if (s_ml[w].x == -INFINITY) continue;
+          y[0] = fmaf(f, x.x, y[0]); y[1] = fmaf(f, x.y, y[1]); y[2] = fmaf(f, x.z, y[2]); y[3] = fmaf(f, x.w, y[3]);
+        }
+        write(row, 128 * warp + lane * 4, y, top, sum);
+      }
+    }
+   }
   }
 }
 
 template <typename T>
 cudaError_t launch_simt(const AttendParams& p, cudaStream_t st) {
-  auto kernel = p.c.head_dim <= 128 ? attend_simt_kernel<T, 1> : attend_simt_kernel<T, 2>;
-  return launch_chained(kernel, dim3((unsigned)(p.groups * p.row_blocks)), dim3(kThreads), simt_smem(p.c.head_dim), st, p);
+  const bool few = p.rows_per_block == 4;
+  auto kernel = p.c.head_dim <= 128 ? (few ? attend_simt_kernel<T, 1, 4> : attend_simt_kernel<T, 1, 16>)
+                                    : (few ? attend_simt_kernel<T, 2, 4> : attend_simt_kernel<T, 2, 16>);
+  return launch_chained(kernel, dim3((unsigned)(p.groups * p.row_blocks)), dim3(kThreads), simt_smem(p.c.head_dim, p.rows_per_block), st, p);
 }
 
 template <typename K>
@@ -381,14 +419,17 @@ cudaError_t run_attend_simt(const AttendParams& p, int dtype, cudaStream_t st) {
 
 cudaError_t run_attend_join(const AttendParams& p, int dtype, cudaStream_t st) {
   const int n = join_rows(p.rows);
-  const dim3 grid((unsigned)((p.rows + n - 1) / n), (unsigned)p.groups);
-  return dtype == JD_DTYPE_F32 ? launch_chained(attend_join_kernel<float>, grid, dim3(32 * kJoinWarps), 0, st, p)
-                               : launch_chained(attend_join_kernel<__nv_bfloat16>, grid, dim3(32 * kJoinWarps), 0, st, p);
+  const dim3 grid((unsigned)((p.rows + n - 1) / n), (unsigned)std::min<int64_t>(p.groups, (int64_t)p.B * p.c.kv_heads));
+  auto kernel = dtype == JD_DTYPE_F32 ? (p.c.head_dim <= 128 ? attend_join_kernel<float, 1> : attend_join_kernel<float, 2>)
+                                      : (p.c.head_dim <= 128 ? attend_join_kernel<__nv_bfloat16, 1> : attend_join_kernel<__nv_bfloat16, 2>);
+  return launch_chained(kernel, grid, dim3(32 * kJoinWarps), 0, st, p);
 }
 
-bool simt_attend_configure() {
-  return raise_limit(attend_simt_kernel<float, 1>, simt_smem(128)) && raise_limit(attend_simt_kernel<float, 2>, simt_smem(256)) &&
-         raise_limit(attend_simt_kernel<__nv_bfloat16, 1>, simt_smem(128)) && raise_limit(attend_simt_kernel<__nv_bfloat16, 2>, simt_smem(256));
+template <typename T>
+bool raise_limits() {
+  return raise_limit(attend_simt_kernel<T, 1, 4>, simt_smem(128, 4)) && raise_limit(attend_simt_kernel<T, 1, 16>, simt_smem(128, 16)) &&
+         raise_limit(attend_simt_kernel<T, 2, 4>, simt_smem(256, 4)) && raise_limit(attend_simt_kernel<T, 2, 16>, simt_smem(256, 16));
 }
+bool simt_attend_configure() { return raise_limits<float>() && raise_limits<__nv_bfloat16>(); }
 
 }  // namespace jd

@@ -634,7 +634,7 @@ jd_status_t jd_cache_attend(jd_cache_t c, const jd_attend_args_t* a, void* cuda_
   } else {
     p.tile_shift = kSimtTileShift;
     p.seg_cost = kSimtSegCost;
-    p.rows_per_block = kSimtRows;
+    p.rows_per_block = p.rows <= 4 ? 4 : kSimtRows;   // one token's few rows leave the others' registers and products out
   }
   p.part_rows = std::min(p.rows, p.rows_per_block);
   p.row_blocks = (p.rows + p.rows_per_block - 1) / p.rows_per_block;
