@@ -9,6 +9,7 @@
 // product with the shared-memory operands bounds it (about twice the HBM time of a tile at two CTAs per SM).
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "jd_cache.h"
 #include "jd_sm100_ptx.cuh"
@@ -114,9 +115,11 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
       }
       __syncthreads();
       const int vec = D / 4;
+      // i / vec for i < 64 x 64: (2^20 / vec rounded up) x i is off by less than 4096 x 63 < 2^20
+      const uint32_t per_vec = ((1u << 20) + vec - 1) / vec;
       if constexpr (sizeof(T) == 4) {              // straight to shared memory; rows behind the sequence may hold anything: zeroes
         for (int i = tid; i < kTile * vec; i += kThreads) {
-          const int r = i / vec, d = (i - r * vec) * 4;
+          const int r = (int)((i * per_vec) >> 20), d = (i - r * vec) * 4;
           const int kv = kv0 + min(r, max(nkv - 1, 0));
           const int page = pages[(kv >> p.c.page_shift) - (kv0 >> p.c.page_shift)];
           const int64_t off = page_row(p.c, p.layer, page, head, kv & (p.c.page_size - 1)) * D + d;
@@ -205,9 +208,7 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
 #pragma unroll
           for (int k = 0; k < 4 * kCols; ++k) acc[r][k] *= f;
         }
-        for (int i = 0; i < kTile / 8; ++i) {
-          const int kv = warp * (kTile / 8) + i;
-          if (kv >= nkv) break;
+        auto add_token = [&](int kv, auto check) {
           float w[kRows];
 #pragma unroll
           for (int r = 0; r < kRows; r += 4) {
@@ -220,7 +221,7 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
             const int d = lane * 4 + 128 * j;
             if (d >= D) continue;
             const float4 x = *reinterpret_cast<const float4*>(sV + kv * pitch + d);
-            const bool plain = node < 0 || (isfinite(x.x) && isfinite(x.y) && isfinite(x.z) && isfinite(x.w));
+            const bool plain = !decltype(check)::value || node < 0 || (isfinite(x.x) && isfinite(x.y) && isfinite(x.z) && isfinite(x.w));
 #pragma unroll
             for (int r = 0; r < kRows; ++r) {
               if (plain || ((s_mask[r][node >> 5] >> (node & 31)) & 1u)) {
@@ -231,6 +232,13 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
               }
             }
           }
+        };
+        const int first = warp * (kTile / 8);
+        if (kv0 + kTile <= ex.ctx) {               // context alone: every row sees every token
+#pragma unroll 2
+          for (int i = 0; i < kTile / 8; ++i) add_token(first + i, std::false_type());
+        } else {
+          for (int i = 0; i < min(kTile / 8, nkv - first); ++i) add_token(first + i, std::true_type());
         }
       }
     }
