@@ -401,7 +401,8 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     uint32_t s_phase = 0, o_phase = 0;
     int tile_count = 0;                              // tiles of the run in front of this piece
     // A piece's Q rows and mask words, fetched while the piece before it ends: a thread keeps its place within a row of Q
-    constexpr int kVecs = D / 8, kQThreads = kPair ? 128 : 256, kQRows = kQThreads / kVecs, kQLoads = 128 / kQRows;
+    constexpr int kVecs = D / 8, kQThreads = kPair ? 128 : 256, kQRows = kQThreads / kVecs, kQLoads = kCopyRows / kQRows;
+    static_assert(kCopyRows % kQRows == 0, "whole steps");
     constexpr int kMaskLoads = kMaxNodes * (kMaxNodes / 32) / 256;
     const int q_first = kPair ? r : tid, q_c = q_first % kVecs, q_r = q_first / kVecs;
     uint4 q_regs[kQLoads];
@@ -423,7 +424,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       const char* q_seq = p.q + (int64_t)y.b * p.T * p.q_stride + (int64_t)y.head * p.group * (D * 2) + q_c * 16;
 #pragma unroll
       for (int i = 0; i < kQLoads; ++i) {
-        const int q_row = r0 + (kPair ? w * 128 : 0) + (q_r + i * kQRows) % kCopyRows, t = q_row / p.group, h = q_row - t * p.group;
+        const int q_row = r0 + (kPair ? w * 128 : 0) + q_r + i * kQRows, t = q_row / p.group, h = q_row - t * p.group;
         q_regs[i] = q_row < p.rows && t < nodes ? __ldg(reinterpret_cast<const uint4*>(q_seq + t * p.q_stride + h * (D * 2)))
                                                 : make_uint4(0u, 0u, 0u, 0u);
       }
@@ -450,8 +451,10 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       uint8_t* q_dst = q_smem + (kPair ? w * kTileBytes : 0) + (q_c >> 3) * kChunkBytes;
 #pragma unroll
       for (int i = 0; i < kQLoads; ++i) {
-        const int row = q_r + i * kQRows;
-        *reinterpret_cast<uint4*>(q_dst + row * 128 + (((q_c & 7) ^ (row & 7)) << 4)) = q_regs[i];
+        const int row = q_r + i * kQRows;            // and the same row of every copy: kCopyRows keeps row % 8
+#pragma unroll
+        for (int k = 0; k < kCopies; ++k)
+          *reinterpret_cast<uint4*>(q_dst + (row + k * kCopyRows) * 128 + (((q_c & 7) ^ (row & 7)) << 4)) = q_regs[i];
       }
       fence_async_proxy();
       tc_fence_before();
@@ -673,28 +676,34 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           }
         }
       } else {
-        // The copies' sums meet in shared memory, over Q, which is not needed any more: 16 columns at a time, alternately by warpgroup.
-        float* stage = reinterpret_cast<float*>(q_smem) + w * 128 * 16;
+        // The copies' sums meet in shared memory, over Q, which is not needed any more: a quarter of the columns at a time, alternately
+        // by warpgroup. A row's 16-byte places are turned by its number, so that neighbouring rows do not meet in a bank.
+        constexpr int kStageCols = D / 4, kPlaces = kStageCols / 4;
+        static_assert(2 * 128 * kStageCols * 4 <= kTileBytes, "the stages fit over Q");
+        float* stage = reinterpret_cast<float*>(q_smem) + w * 128 * kStageCols;
+        auto place = [&](int at, int k) { return reinterpret_cast<float4*>(stage + at * kStageCols) + ((k + at) & (kPlaces - 1)); };
 #pragma unroll 1
-        for (int c = 16 * w; c < D; c += 32) {
-          float o[16];
+        for (int c = kStageCols * w; c < D; c += 2 * kStageCols) {
           if (warp_live) {
-            read_o(c, o);
+#pragma unroll 1
+            for (int k = 0; k < kStageCols; k += 16) {
+              float o[16];
+              read_o(c + k, o);
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4*>(stage + r * 16 + ((i + 4 * r) & 15)) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+              for (int i = 0; i < 16; i += 4) *place(r, (k + i) / 4) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+            }
           }
           asm volatile("bar.sync %0, 128;" ::"r"(2 + w) : "memory");
-          for (int i = r; i < kCopyRows * 4; i += 128) {
-            const int row = i >> 2, q = (i & 3) * 4;
+          for (int i = r; i < kCopyRows * kPlaces; i += 128) {
+            const int row = i / kPlaces, q = i % kPlaces;
             if (r0 + row >= p.rows) continue;
             float y[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < kCopies; ++k) {
-              const int at = k * kCopyRows + row;
-              const float4 v = *reinterpret_cast<const float4*>(stage + at * 16 + ((q + 4 * at) & 15));
+              const float4 v = *place(k * kCopyRows + row, q);
               y[0] += v.x; y[1] += v.y; y[2] += v.z; y[3] += v.w;
             }
-            write(std::integral_constant<int, 4>(), r0 + row, c + q, y, whole ? sh.inv[w][row] : 1.f);
+            write(std::integral_constant<int, 4>(), r0 + row, c + q * 4, y, whole ? sh.inv[w][row] : 1.f);
           }
           asm volatile("bar.sync %0, 128;" ::"r"(2 + w) : "memory");
         }
