@@ -46,6 +46,8 @@ template <int D, int kMode> struct Shape {
   // only ever waited on by those that used up its previous content, and two phases cannot be taken for one another.
   static constexpr int kStages = D == 128 ? 4 : 8;
   static constexpr int kQTiles = kPair ? 2 : 1;
+  static constexpr int kStageCols = D / 4;                     // columns of O that the copies' sums go through shared memory by
+  static constexpr int kStageBytes = kCopies > 1 ? 2 * 128 * kStageCols * 4 : 0;
 };
 
 struct Shared {
@@ -53,11 +55,13 @@ struct Shared {
   uint64_t s_full[2], p_ready[2][2], o_done[2], q_ready[2];   // p_ready: first and second 64 columns of P
   uint32_t tmem_base;
   int abort_flag;
-  int odd_values;                        // the segment's nodes hold values that are not finite
   int warp_sums[kThreads / 32];
-  uint32_t node_mask[kMaxNodes][kMaxNodes / 32];
-  float ml[2][kTile][2];                 // m and l of the two chains
-  float inv[2][kTile / 2];               // 1 / l of a row, for the threads that put its copies together
+  struct PerPiece {                      // of a piece, and of the next one, which begins while this one is written out
+    uint32_t node_mask[kMaxNodes][kMaxNodes / 32];
+    float ml[2][kTile][2];               // m and l of the two chains
+    float inv[2][kTile / 2];             // 1 / l of a row, for the threads that put its copies together
+    int odd_values;                      // nodes hold values that are not finite
+  } piece[2];
   int prefix[kMaxCacheBatch + 1];
   SeqExtent extents[kMaxCacheBatch];
 };
@@ -65,7 +69,7 @@ struct Shared {
 template <int D, int kMode>
 constexpr size_t attend_smem() {
   using S = Shape<D, kMode>;
-  return 1024 + (sizeof(Shared) + 1023) / 1024 * 1024 + (size_t)(S::kStages + S::kQTiles) * S::kTileBytes;
+  return 1024 + (sizeof(Shared) + 1023) / 1024 * 1024 + (size_t)(S::kStages + S::kQTiles) * S::kTileBytes + S::kStageBytes;
 }
 
 // Bounded wait that gives up as soon as another role has.
@@ -207,6 +211,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   Shared& sh = *reinterpret_cast<Shared*>(smem);
   uint8_t* q_smem = smem + (sizeof(Shared) + 1023) / 1024 * 1024;
   uint8_t* ring = q_smem + Sh::kQTiles * kTileBytes;
+  uint8_t* stage_smem = ring + kStages * kTileBytes;
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   volatile int* abort_flag = &sh.abort_flag;
   const int g = blockIdx.x / p.row_blocks, rb = blockIdx.x - g * p.row_blocks;
@@ -436,18 +441,15 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     };
     // ahead of time where the registers are there for it: 256 rows of 128 columns are 64 registers a thread
     constexpr bool kFetchAhead = kQLoads <= 8;
-    Piece x = next_piece();
-    if (kFetchAhead) fetch(x);
-    while (x.tiles > 0) {
-      const SeqExtent ex = sh.extents[x.b];
-      if (!kFetchAhead) fetch(x);
-      softmax_sync();                                // everybody is through with the last piece's Q, masks and sums
+    int parity = 0;
+    // the fetched piece's masks and Q to shared memory, and the word to the chains that have tiles in it: no other waits for it
+    auto hand_over = [&](const Piece& y, Shared::PerPiece& to) {
 #pragma unroll
       for (int i = 0; i < kMaskLoads; ++i) {
         const int at = tid + i * 256, t = at / p.W;
-        if (t < p.T) sh.node_mask[t][at - t * p.W] = mask_regs[i];
+        if (t < p.T) to.node_mask[t][at - t * p.W] = mask_regs[i];
       }
-      if (tid == 0) sh.odd_values = 0;
+      if (tid == 0) to.odd_values = 0;
       uint8_t* q_dst = q_smem + (kPair ? w * kTileBytes : 0) + (q_c >> 3) * kChunkBytes;
 #pragma unroll
       for (int i = 0; i < kQLoads; ++i) {
@@ -458,12 +460,20 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       }
       fence_async_proxy();
       tc_fence_before();
-      softmax_sync();
-      if (lane == 0) {                               // to the chains that have tiles in this piece: no other waits for it
+      __syncwarp();
+      if (lane == 0) {
         mbar_arrive(smem_u32(&sh.q_ready[0]));
-        if (kPair || x.tiles > 1) mbar_arrive(smem_u32(&sh.q_ready[1]));
+        if (kPair || y.tiles > 1) mbar_arrive(smem_u32(&sh.q_ready[1]));
       }
-
+    };
+    Piece x = next_piece();
+    if (x.tiles > 0) {
+      fetch(x);
+      hand_over(x, sh.piece[0]);
+    }
+    while (x.tiles > 0) {
+      const SeqExtent ex = sh.extents[x.b];
+      Shared::PerPiece& mine = sh.piece[parity];
       float m = -INFINITY, l = 0.f;
       int done = 0;                                  // tiles of this piece that this warpgroup has taken
       for (int t = kPair ? 0 : w; t < x.tiles; t += kPair ? 1 : 2, ++done) {
@@ -492,7 +502,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
               if ((e[k] & 0x7F80u) == 0x7F80u) { e[k] &= 0xFFFF0000u; odd = true; }
               if ((e[k] & 0x7F800000u) == 0x7F800000u) { e[k] &= 0xFFFFu; odd = true; }
             }
-            if (odd) { *at = y; sh.odd_values = 1; }
+            if (odd) { *at = y; mine.odd_values = 1; }
           }
           fence_async_proxy();
         }
@@ -513,7 +523,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
 #pragma unroll
             for (int k = 0; k < kCols; k += 32) {
               const int at = kv0 + col0 + k, off = at - ex.ctx, word = off >> 5, valid = ex.kv_end - at;
-              auto bits_of = [&](int i) { return i < 0 ? 0xFFFFFFFFu : (i < p.W && t_node < p.T ? sh.node_mask[t_node][i] : 0u); };
+              auto bits_of = [&](int i) { return i < 0 ? 0xFFFFFFFFu : (i < p.W && t_node < p.T ? mine.node_mask[t_node][i] : 0u); };
               uint32_t see = __funnelshift_r(bits_of(word), bits_of(word + 1), off & 31);
               if (valid < 32) see &= valid <= 0 ? 0u : (1u << valid) - 1u;
 #pragma unroll
@@ -598,28 +608,37 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       const bool live = my_row < p.rows && t_node < ex.nodes;
       float f0 = 1.f, f1 = 0.f;                      // factors on this lane's O_0 and O_1 (pair mode: on its own O)
       if constexpr (!kPair) {
-        sh.ml[w][r][0] = m;
-        sh.ml[w][r][1] = l;
+        mine.ml[w][r][0] = m;
+        mine.ml[w][r][1] = l;
+      }
+      // Every product of this piece has ended: the next one's Q takes its place, and its S runs while this one is written out. Its
+      // P V waits for the softmax of these same warps, so O stays until they have read it. (With every tile for both chains a
+      // warpgroup's Q and O are its own, and neither waits for the other; with alternate tiles both read both.)
+      if constexpr (!kPair) {
+        tc_fence_before();
         softmax_sync();
         tc_fence_after();
-        const float m0 = sh.ml[0][r][0], m1 = sh.ml[1][r][0];
+      }
+      if (kFetchAhead && next.tiles > 0) hand_over(next, sh.piece[parity ^ 1]);
+      if constexpr (!kPair) {
+        const float m0 = mine.ml[0][r][0], m1 = mine.ml[1][r][0];
         m = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 2 * kCopies; ++i) m = fmaxf(m, sh.ml[i & 1][(i >> 1) * kCopyRows + r % kCopyRows][0]);
+        for (int i = 0; i < 2 * kCopies; ++i) m = fmaxf(m, mine.ml[i & 1][(i >> 1) * kCopyRows + r % kCopyRows][0]);
         const float base = m == -INFINITY ? 0.f : m;
         f0 = m0 == -INFINITY ? 0.f : fast_exp2((m0 - base) * c2);
         f1 = m1 == -INFINITY ? 0.f : fast_exp2((m1 - base) * c2);
         l = 0.f;
 #pragma unroll
         for (int i = 0; i < 2 * kCopies; ++i) {
-          const float* ml = sh.ml[i & 1][(i >> 1) * kCopyRows + r % kCopyRows];
+          const float* ml = mine.ml[i & 1][(i >> 1) * kCopyRows + r % kCopyRows];
           l += (ml[0] == -INFINITY ? 0.f : fast_exp2((ml[0] - base) * c2)) * ml[1];
         }
-        if (kCopies > 1 && copy == 0) sh.inv[w][r] = l == 0.f ? 0.f : 1.f / l;   // each warpgroup its own
+        if (kCopies > 1 && copy == 0) mine.inv[w][r] = l == 0.f ? 0.f : 1.f / l;   // each warpgroup its own
       }
       const bool two = !kPair && x.tiles > 1;
       const float inv = !whole ? 1.f : (l == 0.f ? 0.f : 1.f / l);
-      const bool odd = *reinterpret_cast<volatile int*>(&sh.odd_values) != 0;
+      const bool odd = *reinterpret_cast<volatile int*>(&mine.odd_values) != 0;
       float* part0 = p.part + (((int64_t)blockIdx.x * 2 + (x.tile0 == 0 ? 1 : 0)) * p.part_rows - r0) * (D + kPartPad);
       // kN elements of a query row from column c: back to a part, or out
       auto write = [&](auto count, int row, int c, float* o, float factor) {
@@ -629,7 +648,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         if (odd) {                                   // values of this piece's nodes that are not finite, to the rows that see them
           for (int j = 0; j < ex.nodes; ++j) {
             const int kv = ex.ctx + j;
-            if (kv < x.tile0 * kTile || kv >= (x.tile0 + x.tiles) * kTile || kv >= ex.kv_end || !((sh.node_mask[t][j >> 5] >> (j & 31)) & 1u)) continue;
+            if (kv < x.tile0 * kTile || kv >= (x.tile0 + x.tiles) * kTile || kv >= ex.kv_end || !((mine.node_mask[t][j >> 5] >> (j & 31)) & 1u)) continue;
             const int page = p.c.table[(int64_t)ex.slot * p.c.max_pages + (kv >> p.c.page_shift)];
             if (page < 0 || page >= p.c.pages) continue;
             const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(p.c.v) + page_row(p.c, p.layer, page, x.head, kv & (p.c.page_size - 1)) * D + c;
@@ -676,11 +695,10 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           }
         }
       } else {
-        // The copies' sums meet in shared memory, over Q, which is not needed any more: a quarter of the columns at a time, alternately
+        // The copies' sums meet in shared memory: a quarter of the columns at a time, alternately
         // by warpgroup. A row's 16-byte places are turned by its number, so that neighbouring rows do not meet in a bank.
-        constexpr int kStageCols = D / 4, kPlaces = kStageCols / 4;
-        static_assert(2 * 128 * kStageCols * 4 <= kTileBytes, "the stages fit over Q");
-        float* stage = reinterpret_cast<float*>(q_smem) + w * 128 * kStageCols;
+        constexpr int kStageCols = Sh::kStageCols, kPlaces = kStageCols / 4;
+        float* stage = reinterpret_cast<float*>(stage_smem) + w * 128 * kStageCols;
         auto place = [&](int at, int k) { return reinterpret_cast<float4*>(stage + at * kStageCols) + ((k + at) & (kPlaces - 1)); };
 #pragma unroll 1
         for (int c = kStageCols * w; c < D; c += 2 * kStageCols) {
@@ -703,7 +721,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
               const float4 v = *place(k * kCopyRows + row, q);
               y[0] += v.x; y[1] += v.y; y[2] += v.z; y[3] += v.w;
             }
-            write(std::integral_constant<int, 4>(), r0 + row, c + q * 4, y, whole ? sh.inv[w][row] : 1.f);
+            write(std::integral_constant<int, 4>(), r0 + row, c + q * 4, y, whole ? mine.inv[w][row] : 1.f);
           }
           asm volatile("bar.sync %0, 128;" ::"r"(2 + w) : "memory");
         }
@@ -717,8 +735,14 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         }
       }
       tc_fence_before();
+      if constexpr (!kPair) softmax_sync();          // both warpgroups have read both chains' O, which the next piece's first products overwrite
+      if (!kFetchAhead && next.tiles > 0) {
+        fetch(next);
+        hand_over(next, sh.piece[parity ^ 1]);
+      }
       tile_count += x.tiles;
       x = next;
+      parity ^= 1;
     }
   }
 
