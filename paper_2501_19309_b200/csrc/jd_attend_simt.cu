@@ -1,12 +1,14 @@
 // Attention of a drafted block over the paged cache on CUDA cores: any type and head width, float32 throughout; and the
 // kernel that joins the partial results of split sequences, which the tensor-core variant shares.
 //
-// A CTA takes 16 query rows of a (sequence, kv head) - a row is a node and one of the query heads that share the kv
-// head - and walks its run of tiles of 64 cached tokens (jd_cache.h says how runs are cut). Per tile: K and V to shared
-// memory, 16 x 64 scores by 256 threads (four rows of one token each), running maximum and sum by a warp for two rows,
-// and the weighted sum of V with every warp taking an eighth of the tokens for all 16 rows and up to 256 columns in
-// registers, so that one shared-memory read of V serves 16 rows. The warps' sums meet once per piece of a segment. For float32 the
-// product with the shared-memory operands bounds it (about twice the HBM time of a tile at two CTAs per SM).
+// A CTA takes 16 query rows (4 where there are no more) of a (sequence, kv head) - a row is a node and one of the query
+// heads that share the kv head - and walks its run of tiles of 64 cached tokens (jd_cache.h says how runs are cut). Per tile: K and
+// V to shared memory, the scores by 256 threads (a token each and a quarter of the rows), running maximum and sum by a warp
+// for a row, and the weighted sum of V with every warp taking an eighth of the tokens for all rows and up to 256 columns in
+// registers, so that one shared-memory read of V serves all rows. The warps' sums meet once per piece of a segment.
+// Two CTAs on an SM, so that one's loads run beside the other's products. float32, B200: 16 sequences of 8,000 tokens, 8 heads of
+// 128, one token each: 296 us, 3.5 TB/s; blocks of 26 nodes, 2 x 8 heads over 2,000 tokens: 17 TFLOP/s, bound by issuing
+// shared-memory reads and products (a tile is some 5,000 issue slots of each SM partition).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -351,58 +353,58 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendPara
   const int block_rows = join_rows(p.rows), first_row = blockIdx.x * block_rows;
   // this block's groups, a lane each, then those among them that left a segment
   for (int base_g = blockIdx.y; base_g < p.groups; base_g += 32 * gridDim.y) {
-   const int my_g = base_g + lane * gridDim.y;
-   const int4 mine = my_g < p.groups ? __ldcg(p.split + my_g) : make_int4(-1, 0, 0, 0);
-   for (unsigned left = __ballot_sync(0xffffffffu, mine.x >= 0); left; left &= left - 1) {
-    const int from = __ffs(left) - 1, g0 = base_g + from * gridDim.y;
-    const int b = __shfl_sync(0xffffffffu, mine.x, from), head = __shfl_sync(0xffffffffu, mine.y, from), g1 = __shfl_sync(0xffffffffu, mine.z, from);
-    const int nodes = p.num_nodes ? min(max(__ldg(p.num_nodes + b), 0), p.T) : p.T;
-    const int rows = min(p.rows, nodes * p.group);
-    auto write = [&](int row, int d, const float* o, float m, float l) {   // columns d .. d + 3
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      const float y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-      const int t = row / p.group, h = head * p.group + row - t * p.group;
-      if (d < D) store4(reinterpret_cast<T*>(p.out + ((int64_t)b * p.T + t) * p.out_stride) + (int64_t)h * D + d, y);
-      if (d == 0 && p.lse) p.lse[((int64_t)b * p.T + t) * p.q_heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
-    };
-    auto place = [&](int row) {
-      const int rb = row / p.rows_per_block, r = row - rb * p.rows_per_block;
-      const float* base = p.part + ((int64_t)rb * 2 * p.part_rows + r) * pitch;
-      return [=](int g) { return base + ((int64_t)g * p.row_blocks * 2 + (g == g0 ? 1 : 0)) * p.part_rows * pitch; };
-    };
-    if (block_rows > 1 && g1 - g0 < kJoinFewParts) {
-      const int row = first_row + warp;
-      if (row >= rows) continue;
-      const RowSum<kCols> s = sum_parts<kCols>(g0, g1, 1, D, lane, place(row));
+    const int my_g = base_g + lane * gridDim.y;
+    const int4 mine = my_g < p.groups ? __ldcg(p.split + my_g) : make_int4(-1, 0, 0, 0);
+    for (unsigned left = __ballot_sync(0xffffffffu, mine.x >= 0); left; left &= left - 1) {
+      const int from = __ffs(left) - 1, g0 = base_g + from * gridDim.y;
+      const int b = __shfl_sync(0xffffffffu, mine.x, from), head = __shfl_sync(0xffffffffu, mine.y, from), g1 = __shfl_sync(0xffffffffu, mine.z, from);
+      const int nodes = p.num_nodes ? min(max(__ldg(p.num_nodes + b), 0), p.T) : p.T;
+      const int rows = min(p.rows, nodes * p.group);
+      auto write = [&](int row, int d, const float* o, float m, float l) {   // columns d .. d + 3
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const float y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+        const int t = row / p.group, h = head * p.group + row - t * p.group;
+        if (d < D) store4(reinterpret_cast<T*>(p.out + ((int64_t)b * p.T + t) * p.out_stride) + (int64_t)h * D + d, y);
+        if (d == 0 && p.lse) p.lse[((int64_t)b * p.T + t) * p.q_heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+      };
+      auto place = [&](int row) {
+        const int rb = row / p.rows_per_block, r = row - rb * p.rows_per_block;
+        const float* base = p.part + ((int64_t)rb * 2 * p.part_rows + r) * pitch;
+        return [=](int g) { return base + ((int64_t)g * p.row_blocks * 2 + (g == g0 ? 1 : 0)) * p.part_rows * pitch; };
+      };
+      if (block_rows > 1 && g1 - g0 < kJoinFewParts) {
+        const int row = first_row + warp;
+        if (row >= rows) continue;
+        const RowSum<kCols> s = sum_parts<kCols>(g0, g1, 1, D, lane, place(row));
 #pragma unroll
-      for (int j = 0; j < kCols; ++j) write(row, 128 * j + lane * 4, s.o[j], s.m, s.l);
-      continue;
-    }
-    for (int row = first_row; row < min(rows, first_row + block_rows); ++row) {
-      const RowSum<kCols> s = sum_parts<kCols>(g0 + warp, g1, kJoinWarps, D, lane, place(row));
-      __syncthreads();   // the last row's sums have been read
+        for (int j = 0; j < kCols; ++j) write(row, 128 * j + lane * 4, s.o[j], s.m, s.l);
+        continue;
+      }
+      for (int row = first_row; row < min(rows, first_row + block_rows); ++row) {
+        const RowSum<kCols> s = sum_parts<kCols>(g0 + warp, g1, kJoinWarps, D, lane, place(row));
+        __syncthreads();   // the last row's sums have been read
 #pragma unroll
-      for (int j = 0; j < kCols; ++j) s_o[warp][j][lane] = make_float4(s.o[j][0], s.o[j][1], s.o[j][2], s.o[j][3]);
-      if (lane == 0) s_ml[warp] = make_float2(s.m, s.l);
-      __syncthreads();
-      if (warp < kCols) {   // columns 128 warp ..
-        float top = -INFINITY;
+        for (int j = 0; j < kCols; ++j) s_o[warp][j][lane] = make_float4(s.o[j][0], s.o[j][1], s.o[j][2], s.o[j][3]);
+        if (lane == 0) s_ml[warp] = make_float2(s.m, s.l);
+        __syncthreads();
+        if (warp < kCols) {   // columns 128 warp ..
+          float top = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, s_ml[w].x);
-        const float base = top == -INFINITY ? 0.f : top;
-        float sum = 0.f, y[4] = {};
+          for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, s_ml[w].x);
+          const float base = top == -INFINITY ? 0.f : top;
+          float sum = 0.f, y[4] = {};
 #pragma unroll
-        for (int w = 0; w < kJoinWarps; ++w) {
-          const float f = exp2f(s_ml[w].x - base);
-          const float4 x = s_o[w][warp][lane];
-          sum += f * s_ml[w].y;
-          if (s_ml[w].x == -INFINITY) continue;
-          y[0] = fmaf(f, x.x, y[0]); y[1] = fmaf(f, x.y, y[1]); y[2] = fmaf(f, x.z, y[2]); y[3] = fmaf(f, x.w, y[3]);
+          for (int w = 0; w < kJoinWarps; ++w) {
+            const float f = exp2f(s_ml[w].x - base);
+            const float4 x = s_o[w][warp][lane];
+            sum += f * s_ml[w].y;
+            if (s_ml[w].x == -INFINITY) continue;
+            y[0] = fmaf(f, x.x, y[0]); y[1] = fmaf(f, x.y, y[1]); y[2] = fmaf(f, x.z, y[2]); y[3] = fmaf(f, x.w, y[3]);
+          }
+          write(row, 128 * warp + lane * 4, y, top, sum);
         }
-        write(row, 128 * warp + lane * 4, y, top, sum);
       }
     }
-   }
   }
 }
 

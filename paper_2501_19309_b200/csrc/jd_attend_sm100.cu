@@ -9,13 +9,27 @@
 //   O = O + P V          tcgen05.mma with P from tensor memory, V as it lies in its pages (tokens x columns: the
 //                        transposed operand form), O (128 x head width fp32) in tensor memory
 //
-// Two softmax warpgroups keep the tensor pipe busy: with up to 128 rows they take alternate tiles, each with its own O, m
-// and l (two independent chains that meet when the segment ends); with more rows each takes 128 rows of every tile, and
-// K and V are fetched once for both. O is rescaled only when a row's maximum has grown by more than 2^8 since it was last
-// (the weights stay below 2^8 until then, far inside bf16's range), which after the first tiles is rare.
-// A producer warp follows the page table and fetches pages by TMA, a box per page and 64 columns, through a ring of K and V
-// tiles; a fourth role issues the MMAs. Where few rows are attended the call streams K and V once and is bound by HBM:
-// at 26 GB/s and SM a tile of 64 KB takes as long as the tensor pipe needs for two and a half.
+// P is rounded to bf16, by 2^-8 of each weight at most, because the product takes no wider type at this rate; l is the sum of the
+// weights before they are rounded, so that the logarithm of the sum keeps float32. O is rescaled only when a row's
+// maximum has grown by more than 2^8 since it was last (the weights stay below 2^8 until then), which after the first
+// tiles is rare.
+//
+// Two chains S -> softmax -> P V keep the pipe busy while each waits for itself, a warpgroup for each one's softmax. With up to 128
+// rows they take alternate tiles, each with its own O, m and l that meet when the segment ends; with more rows each takes 128
+// rows of every tile, and K and V are fetched once for both. Two warps follow the page table and fetch K and V tiles by
+// TMA, a box per page and 64 columns, through a ring; one or two more issue the MMAs.
+//
+// What bounds it (B200, 148 SMs):
+//   up to 128 rows   HBM: 16 sequences of 40,000 tokens, 8 kv heads of 128, one token each: 395 us, 6.6 TB/s; heads of 64: 206 us, 6.4 TB/s
+//   129 rows and up  the chains' own latency: a pair of row tiles takes about 3,450 cycles a tile, of which its products are 2,200 (S: 75
+//                    cycles a step of 16 columns, as Q comes from shared memory again every time; P V: 64), its exponentials
+//                    2,050 on each SM partition and the rest the hand-overs between them; 416 rows over 131,046 tokens: 257 us,
+//                    870 TFLOP/s, at clocks that the power limit holds near 1.5 GHz
+//   short contexts   about 8,000 cycles to begin and end a segment
+// Tried and slower: a second pair of softmax warpgroups, half the columns each (275 against 260 us on that case); a quarter of the
+// exponentials as polynomials on the FMA pipe (274); S in halves of 64 tokens with a buffer each, so that the next is ready when
+// one is done (282: a product of 64 columns costs what one of 128 does); weighing against the maximum so far while the
+// tile's own is found (265).
 #include <algorithm>
 #include <type_traits>
 
@@ -244,153 +258,153 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   const uint32_t ring_addr = smem_u32(ring), q_addr = smem_u32(q_smem);
 
   if (warp >= 8) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-  if (warp == 8 || warp == 10) {
-    // ------------------------------------------------------------------ producers: warp 8 fetches K tiles, warp 10 V tiles
-    // Ring items are K and V of the run's tiles in turn. A box costs the issuing warp about 100 cycles, whatever its size, which with
-    // small pages is most of a tile's time: hence a warp each. Page numbers are fetched two tiles ahead.
-    const bool is_v = warp == 10;
-    const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
-    const uint64_t policy = p.row_blocks == 1 ? policy_evict_first() : policy_evict_normal();
-    const int shift = p.c.page_shift, box_shift = min(shift, kTensorTileShift), boxes_per_tile = kTile >> box_shift;
-    const int no_row = (int)page_row(p.c, p.c.layers, 0, 0, 0);   // one behind the last: reads as zero
-    int stage = is_v ? 1 : 0;
-    uint32_t phase = 0;
-    bool ok = true;
-    for (int64_t u = run0; u < run1 && ok;) {
-      const Piece x = piece_at(p, sh.prefix, u, run1);
-      u = x.next;
-      if (x.tiles == 0) continue;
-      const SeqExtent ex = sh.extents[x.b];
-      const int32_t* table = p.c.table + (int64_t)ex.slot * p.c.max_pages;
-      auto token_of = [&](int t) { return (x.tile0 + t) * kTile + (lane << box_shift); };   // this lane's box of tile t
-      auto fetch = [&](int t) {
-        const int at = token_of(t);
-        return t < x.tiles && lane < boxes_per_tile && at < ex.kv_end ? __ldg(table + (at >> shift)) : 0;
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (warp == 8 || warp == 10) {
+      // ------------------------------------------------------------------ producers: warp 8 fetches K tiles, warp 10 V tiles
+      // Ring items are K and V of the run's tiles in turn. A box costs the issuing warp about 100 cycles, whatever its size, which with
+      // small pages is most of a tile's time: hence a warp each. Page numbers are fetched two tiles ahead.
+      const bool is_v = warp == 10;
+      const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
+      const uint64_t policy = p.row_blocks == 1 ? policy_evict_first() : policy_evict_normal();
+      const int shift = p.c.page_shift, box_shift = min(shift, kTensorTileShift), boxes_per_tile = kTile >> box_shift;
+      const int no_row = (int)page_row(p.c, p.c.layers, 0, 0, 0);   // one behind the last: reads as zero
+      int stage = is_v ? 1 : 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int64_t u = run0; u < run1 && ok;) {
+        const Piece x = piece_at(p, sh.prefix, u, run1);
+        u = x.next;
+        if (x.tiles == 0) continue;
+        const SeqExtent ex = sh.extents[x.b];
+        const int32_t* table = p.c.table + (int64_t)ex.slot * p.c.max_pages;
+        auto token_of = [&](int t) { return (x.tile0 + t) * kTile + (lane << box_shift); };   // this lane's box of tile t
+        auto fetch = [&](int t) {
+          const int at = token_of(t);
+          return t < x.tiles && lane < boxes_per_tile && at < ex.kv_end ? __ldg(table + (at >> shift)) : 0;
+        };
+        int page0 = fetch(0), page1 = fetch(1);
+        for (int t = 0; t < x.tiles; ++t) {
+          const int page = page0;
+          page0 = page1;
+          page1 = fetch(t + 2);
+          const int at = token_of(t);
+          const bool mine = lane < boxes_per_tile && at < ex.kv_end;
+          int row = no_row;
+          if (mine) {
+            if (page >= 0 && page < p.c.pages) row = (int)page_row(p.c, p.layer, page, x.head, at & (p.c.page_size - 1));
+            else set_status(p.c.status, JD_ERR_BAD_INDEX);
+          }
+          const int boxes = __popc(__ballot_sync(0xffffffffu, mine));
+          const uint32_t bar = smem_u32(&sh.full[stage]);
+          if (lane == 0) {
+            ok = wait(smem_u32(&sh.empty[stage]), phase ^ 1u, abort_flag);
+            if (ok) mbar_expect_tx(bar, (uint32_t)(boxes * kChunks) << (box_shift + 7));
+          }
+          ok = __shfl_sync(0xffffffffu, ok, 0);
+          if (!ok) break;
+          if (mine) {
+            const uint32_t dst = ring_addr + stage * kTileBytes + ((uint32_t)lane << (box_shift + 7));
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c) tma_load_2d(dst + c * kChunkBytes, tm, bar, c * 64, row, policy);
+          }
+          stage += 2;
+          if (stage >= kStages) { stage -= kStages; phase ^= 1u; }
+        }
+      }
+      if (!ok && lane == 0) set_status(p.c.status, JD_ERR_TIMEOUT);
+    } else if (!kPair || warp == 9) {
+      // ------------------------------------------------------------------ MMA issue
+      // Alternate tiles: warp 9 for chain 0, warp 11 for chain 1, since S -> softmax -> P V -> S is what a chain waits for and each
+      // wait and issue costs its warp some 150 cycles. Every tile for both chains: warp 9 alone, because its order (all of chain 0's
+      // products, then chain 1's) is what keeps one chain's softmax beside the other's products; two warps' products
+      // interleave, the chains fall into step, and the long-context call takes a third longer (342 against 258 us).
+      // The whole warp walks the schedule and one elected lane issues: descriptors and addresses then live in uniform registers,
+      // which is what the instruction takes. (Inside an `if (lane == 0)` every MMA moved its operands there first, and the
+      // issue took longer than the products.)
+      const uint32_t idesc_s = make_idesc(kTile), idesc_o = make_idesc(D) | kTransposeB;
+      uint32_t p_phase[2] = {0, 0}, q_phase[2] = {0, 0};
+      bool ok = true;                                  // after a wait that ran out nothing waits any more; what is issued reads stale tiles
+      auto await = [&](uint64_t* bar, uint32_t phase) {
+        ok = wait(smem_u32(bar), phase, abort_flag) && ok;
+        __syncwarp();
+        tc_fence_after();
       };
-      int page0 = fetch(0), page1 = fetch(1);
-      for (int t = 0; t < x.tiles; ++t) {
-        const int page = page0;
-        page0 = page1;
-        page1 = fetch(t + 2);
-        const int at = token_of(t);
-        const bool mine = lane < boxes_per_tile && at < ex.kv_end;
-        int row = no_row;
-        if (mine) {
-          if (page >= 0 && page < p.c.pages) row = (int)page_row(p.c, p.layer, page, x.head, at & (p.c.page_size - 1));
-          else set_status(p.c.status, JD_ERR_BAD_INDEX);
-        }
-        const int boxes = __popc(__ballot_sync(0xffffffffu, mine));
-        const uint32_t bar = smem_u32(&sh.full[stage]);
-        if (lane == 0) {
-          ok = wait(smem_u32(&sh.empty[stage]), phase ^ 1u, abort_flag);
-          if (ok) mbar_expect_tx(bar, (uint32_t)(boxes * kChunks) << (box_shift + 7));
-        }
-        ok = __shfl_sync(0xffffffffu, ok, 0);
-        if (!ok) break;
-        if (mine) {
-          const uint32_t dst = ring_addr + stage * kTileBytes + ((uint32_t)lane << (box_shift + 7));
-#pragma unroll
-          for (int c = 0; c < kChunks; ++c) tma_load_2d(dst + c * kChunkBytes, tm, bar, c * 64, row, policy);
-        }
-        stage += 2;
-        if (stage >= kStages) { stage -= kStages; phase ^= 1u; }
-      }
-    }
-    if (!ok && lane == 0) set_status(p.c.status, JD_ERR_TIMEOUT);
-  } else if (!kPair || warp == 9) {
-    // ------------------------------------------------------------------ MMA issue
-    // Alternate tiles: warp 9 for chain 0, warp 11 for chain 1, since S -> softmax -> P V -> S is what a chain waits for and each
-    // wait and issue costs its warp some 150 cycles. Every tile for both chains: warp 9 alone, because its order (all of chain 0's
-    // products, then chain 1's) is what keeps one chain's softmax beside the other's products; two warps' products
-    // interleave, the chains fall into step, and the long-context call takes a third longer (342 against 258 us).
-    // The whole warp walks the schedule and one elected lane issues: descriptors and addresses then live in uniform registers,
-    // which is what the instruction takes. (Inside an `if (lane == 0)` every MMA moved its operands there first, and the
-    // issue took longer than the products.)
-    const uint32_t idesc_s = make_idesc(kTile), idesc_o = make_idesc(D) | kTransposeB;
-    uint32_t p_phase[2] = {0, 0}, q_phase[2] = {0, 0};
-    bool ok = true;                                  // after a wait that ran out nothing waits any more; what is issued reads stale tiles
-    auto await = [&](uint64_t* bar, uint32_t phase) {
-      ok = wait(smem_u32(bar), phase, abort_flag) && ok;
-      __syncwarp();
-      tc_fence_after();
-    };
-    auto slot = [](int item) { return item % kStages; };
-    auto await_item = [&](int item) { await(&sh.full[slot(item)], (uint32_t)(item / kStages) & 1u); };
-    auto issue_s = [&](int w, int item, bool release) {   // S = Q K^T; the last chain that reads K lets it go
-      const uint64_t a = make_smem_desc(q_addr + (kPair ? w * kTileBytes : 0)), b = make_smem_desc(ring_addr + slot(item) * kTileBytes);
-      if (elect_one()) {
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          const uint32_t off = ((k >> 2) * kChunkBytes + (k & 3) * 32) >> 4;
-          umma_bf16(tmem + w * 128, a + off, b + off, idesc_s, k == 0 ? 0u : 1u);
-        }
-        umma_commit(smem_u32(&sh.s_full[w]));
-        if (release) umma_commit(smem_u32(&sh.empty[slot(item)]));
-      }
-      __syncwarp();
-    };
-    auto issue_o = [&](int w, int item, uint32_t acc, bool release) {   // O (+)= P V as the halves of P arrive
-      const uint64_t b = make_v_desc(ring_addr + slot(item) * kTileBytes, kChunkBytes);
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        await(&sh.p_ready[w][half], p_phase[w]);
+      auto slot = [](int item) { return item % kStages; };
+      auto await_item = [&](int item) { await(&sh.full[slot(item)], (uint32_t)(item / kStages) & 1u); };
+      auto issue_s = [&](int w, int item, bool release) {   // S = Q K^T; the last chain that reads K lets it go
+        const uint64_t a = make_smem_desc(q_addr + (kPair ? w * kTileBytes : 0)), b = make_smem_desc(ring_addr + slot(item) * kTileBytes);
         if (elect_one()) {
 #pragma unroll
-          for (int k = half * (kTile / 32); k < (half + 1) * (kTile / 32); ++k)
-            umma_bf16_ta(tmem + 256 + w * 128, tmem + w * 128 + k * 8, b + (k * 2048 >> 4), idesc_o, k == 0 ? acc : 1u);
-          if (half == 1) {
-            umma_commit(smem_u32(&sh.o_done[w]));
-            if (release) umma_commit(smem_u32(&sh.empty[slot(item)]));
+          for (int k = 0; k < D / 16; ++k) {
+            const uint32_t off = ((k >> 2) * kChunkBytes + (k & 3) * 32) >> 4;
+            umma_bf16(tmem + w * 128, a + off, b + off, idesc_s, k == 0 ? 0u : 1u);
           }
+          umma_commit(smem_u32(&sh.s_full[w]));
+          if (release) umma_commit(smem_u32(&sh.empty[slot(item)]));
         }
         __syncwarp();
+      };
+      auto issue_o = [&](int w, int item, uint32_t acc, bool release) {   // O (+)= P V as the halves of P arrive
+        const uint64_t b = make_v_desc(ring_addr + slot(item) * kTileBytes, kChunkBytes);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          await(&sh.p_ready[w][half], p_phase[w]);
+          if (elect_one()) {
+#pragma unroll
+            for (int k = half * (kTile / 32); k < (half + 1) * (kTile / 32); ++k)
+              umma_bf16_ta(tmem + 256 + w * 128, tmem + w * 128 + k * 8, b + (k * 2048 >> 4), idesc_o, k == 0 ? acc : 1u);
+            if (half == 1) {
+              umma_commit(smem_u32(&sh.o_done[w]));
+              if (release) umma_commit(smem_u32(&sh.empty[slot(item)]));
+            }
+          }
+          __syncwarp();
+        }
+        p_phase[w] ^= 1u;
+      };
+      int base = 0;                                    // ring items of the pieces in front
+      for (int64_t u = uniform64(run0); u < uniform64(run1);) {
+        const Piece x = piece_at(p, sh.prefix, u, run1);
+        const int n = __shfl_sync(0xffffffffu, x.tiles, 0);
+        u = uniform64(x.next);
+        if (n == 0) continue;
+        if constexpr (kPair) {
+          await(&sh.q_ready[0], q_phase[0]);
+          await(&sh.q_ready[1], q_phase[0]);
+          q_phase[0] ^= 1u;
+          await_item(base);
+          issue_s(0, base, false);
+          issue_s(1, base, true);
+          for (int t = 0; t < n; ++t) {
+            const int v = base + 2 * t + 1;
+            const bool more = t + 1 < n;
+            await_item(v);
+            issue_o(0, v, t > 0, false);
+            if (more) { await_item(v + 1); issue_s(0, v + 1, false); }
+            issue_o(1, v, t > 0, true);
+            if (more) issue_s(1, v + 1, true);
+          }
+        } else {
+          const int w = warp == 11 ? 1 : 0;            // tiles w, w + 2, .. are this chain's
+          if (w < n) {
+            await(&sh.q_ready[w], q_phase[w]);
+            q_phase[w] ^= 1u;
+            await_item(base + 2 * w);
+            issue_s(w, base + 2 * w, true);
+          }
+          for (int t = w; t < n; t += 2) {
+            const int v = base + 2 * t + 1;
+            const bool more = t + 2 < n;
+            await_item(v);                             // ahead of P, so that nothing stands between P's arrival and the products
+            if (more) await_item(v + 3);
+            issue_o(w, v, t > w, true);
+            if (more) issue_s(w, v + 3, true);
+          }
+        }
+        base += 2 * n;
       }
-      p_phase[w] ^= 1u;
-    };
-    int base = 0;                                    // ring items of the pieces in front
-    for (int64_t u = uniform64(run0); u < uniform64(run1);) {
-      const Piece x = piece_at(p, sh.prefix, u, run1);
-      const int n = __shfl_sync(0xffffffffu, x.tiles, 0);
-      u = uniform64(x.next);
-      if (n == 0) continue;
-      if constexpr (kPair) {
-        await(&sh.q_ready[0], q_phase[0]);
-        await(&sh.q_ready[1], q_phase[0]);
-        q_phase[0] ^= 1u;
-        await_item(base);
-        issue_s(0, base, false);
-        issue_s(1, base, true);
-        for (int t = 0; t < n; ++t) {
-          const int v = base + 2 * t + 1;
-          const bool more = t + 1 < n;
-          await_item(v);
-          issue_o(0, v, t > 0, false);
-          if (more) { await_item(v + 1); issue_s(0, v + 1, false); }
-          issue_o(1, v, t > 0, true);
-          if (more) issue_s(1, v + 1, true);
-        }
-      } else {
-        const int w = warp == 11 ? 1 : 0;            // tiles w, w + 2, .. are this chain's
-        if (w < n) {
-          await(&sh.q_ready[w], q_phase[w]);
-          q_phase[w] ^= 1u;
-          await_item(base + 2 * w);
-          issue_s(w, base + 2 * w, true);
-        }
-        for (int t = w; t < n; t += 2) {
-          const int v = base + 2 * t + 1;
-          const bool more = t + 2 < n;
-          await_item(v);                             // ahead of P, so that nothing stands between P's arrival and the products
-          if (more) await_item(v + 3);
-          issue_o(w, v, t > w, true);
-          if (more) issue_s(w, v + 3, true);
-        }
-      }
-      base += 2 * n;
+      if (!ok && lane == 0) set_status(p.c.status, JD_ERR_TIMEOUT);
     }
-    if (!ok && lane == 0) set_status(p.c.status, JD_ERR_TIMEOUT);
-  }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
     // ------------------------------------------------------------------ softmax: thread = row
