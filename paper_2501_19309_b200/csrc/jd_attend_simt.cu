@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
       __syncthreads();   // the previous tile's buffers are free
       if (tid < kTile >> min(p.c.page_shift, kSimtTileShift)) {
         const int at = (kv0 >> p.c.page_shift) + tid;
-        int page = (at << p.c.page_shift) < ex.kv_end ? __ldg(p.c.table + (int64_t)ex.slot * p.c.max_pages + at) : 0;
+        int page = (at << p.c.page_shift) < ex.kv_end ? __ldcg(p.c.table + (int64_t)ex.slot * p.c.max_pages + at) : 0;
         if (page < 0 || page >= p.c.pages) { set_status(p.c.status, JD_ERR_BAD_INDEX); page = 0; }
         pages[tid] = page;
       }
@@ -358,7 +358,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendPara
     for (unsigned left = __ballot_sync(0xffffffffu, mine.x >= 0); left; left &= left - 1) {
       const int from = __ffs(left) - 1, g0 = base_g + from * gridDim.y;
       const int b = __shfl_sync(0xffffffffu, mine.x, from), head = __shfl_sync(0xffffffffu, mine.y, from), g1 = __shfl_sync(0xffffffffu, mine.z, from);
-      const int nodes = p.num_nodes ? min(max(__ldg(p.num_nodes + b), 0), p.T) : p.T;
+      const int nodes = p.num_nodes ? min(max(__ldcg(p.num_nodes + b), 0), p.T) : p.T;
       const int rows = min(p.rows, nodes * p.group);
       auto write = [&](int row, int d, const float* o, float m, float l) {   // columns d .. d + 3
         const float inv = l == 0.f ? 0.f : 1.f / l;

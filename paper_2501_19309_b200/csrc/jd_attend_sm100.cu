@@ -280,7 +280,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         auto token_of = [&](int t) { return (x.tile0 + t) * kTile + (lane << box_shift); };   // this lane's box of tile t
         auto fetch = [&](int t) {
           const int at = token_of(t);
-          return t < x.tiles && lane < boxes_per_tile && at < ex.kv_end ? __ldg(table + (at >> shift)) : 0;
+          return t < x.tiles && lane < boxes_per_tile && at < ex.kv_end ? __ldcg(table + (at >> shift)) : 0;
         };
         int page0 = fetch(0), page1 = fetch(1);
         for (int t = 0; t < x.tiles; ++t) {
@@ -444,7 +444,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
 #pragma unroll
       for (int i = 0; i < kQLoads; ++i) {
         const int q_row = r0 + (kPair ? w * 128 : 0) + q_r + i * kQRows, t = q_row / p.group, h = q_row - t * p.group;
-        q_regs[i] = q_row < p.rows && t < nodes ? __ldg(reinterpret_cast<const uint4*>(q_seq + t * p.q_stride + h * (D * 2)))
+        q_regs[i] = q_row < p.rows && t < nodes ? __ldcg(reinterpret_cast<const uint4*>(q_seq + t * p.q_stride + h * (D * 2)))
                                                 : make_uint4(0u, 0u, 0u, 0u);
       }
 #pragma unroll

@@ -31,7 +31,7 @@ __device__ __forceinline__ bool named_before(const int32_t* slots, int b, int sl
   __syncthreads();
   if (slots)
     for (int i = threadIdx.x; i < b; i += blockDim.x)
-      if (__ldg(slots + i) == slot) *flag = 1;
+      if (__ldcg(slots + i) == slot) *flag = 1;
   __syncthreads();
   return *flag != 0;
 }
@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(256) truncate_kernel(CacheView c, const int32_
   if (named_before(slots, b, slot, &flag)) { if (threadIdx.x == 0) set_status(c.status, JD_ERR_BAD_INDEX); return; }
   int len, held;
   slot_state(c, slot, len, held);
-  const int to = length ? __ldg(length + b) : 0;
+  const int to = length ? __ldcg(length + b) : 0;
   if (to < 0 || to > len) { if (threadIdx.x == 0) set_status(c.status, JD_ERR_BAD_INDEX); return; }
   __syncthreads();   // everybody has read the slot's state
   cut_slot(c, slot, held, pages_for(c, to), to);
@@ -77,13 +77,13 @@ __global__ void __launch_bounds__(256) fork_kernel(CacheView c, int n, const int
   pdl_wait();
   pdl_trigger();
   const int i = blockIdx.x;
-  const int s = __ldg(src + i), d = __ldg(dst + i);
+  const int s = __ldcg(src + i), d = __ldcg(dst + i);
   if (s == -1 || d == -1) return;
   if (threadIdx.x == 0) flag = s < 0 || s >= c.max_seqs || d < 0 || d >= c.max_seqs;
   __syncthreads();
   if (!flag)
     for (int j = threadIdx.x; j < n; j += blockDim.x)
-      if (__ldg(src + j) == d || (j < i && __ldg(dst + j) == d && __ldg(src + j) != -1)) flag = 1;
+      if (__ldcg(src + j) == d || (j < i && __ldcg(dst + j) == d && __ldcg(src + j) != -1)) flag = 1;
   __syncthreads();
   if (!flag && threadIdx.x == 0 && (c.held[d] != 0 || c.seq_len[d] != 0)) flag = 1;
   __syncthreads();
@@ -276,9 +276,9 @@ __global__ void __launch_bounds__(kMoveThreads) commit_kernel(CacheView c, const
   if (named_before(slots, b, slot, &flag)) { if (threadIdx.x == 0) set_status(c.status, JD_ERR_BAD_INDEX); return; }
   int len, held;
   slot_state(c, slot, len, held);
-  int pick = 0, a = __ldg(accept_len + (int64_t)b * num_paths);
+  int pick = 0, a = __ldcg(accept_len + (int64_t)b * num_paths);
   for (int i = 1; i < num_paths; ++i) {
-    const int x = __ldg(accept_len + (int64_t)b * num_paths + i);
+    const int x = __ldcg(accept_len + (int64_t)b * num_paths + i);
     if (x > a) { a = x; pick = i; }
   }
   a = min(max(a, 0), path_len);
@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(kMoveThreads) commit_kernel(CacheView c, const
   const int32_t* table = c.table + (int64_t)slot * c.max_pages;
   const int limit = held << c.page_shift;          // tokens that the sequence holds
   if (threadIdx.x == 0) { s_cut = a; s_moves = 0; }
-  if (threadIdx.x < a) s_node[threadIdx.x] = paths ? __ldg(paths + ((int64_t)b * num_paths + pick) * path_len + threadIdx.x) : (int)threadIdx.x + 1;
+  if (threadIdx.x < a) s_node[threadIdx.x] = paths ? __ldcg(paths + ((int64_t)b * num_paths + pick) * path_len + threadIdx.x) : (int)threadIdx.x + 1;
   __syncthreads();
   if (threadIdx.x < a) {
     const int i = threadIdx.x, node = s_node[i], before = i ? s_node[i - 1] : 0;

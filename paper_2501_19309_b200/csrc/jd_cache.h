@@ -54,7 +54,7 @@ __device__ __forceinline__ int64_t page_row(const CacheView& c, int layer, int p
 // Slot of entry b: -1 for padding and for entries out of range (reported).
 __device__ __forceinline__ int slot_of(const CacheView& c, const int32_t* slots, int b) {
   if (!slots) return b;
-  const int s = __ldg(slots + b);
+  const int s = __ldcg(slots + b);
   if (s >= 0 && s < c.max_seqs) return s;
   if (s != -1) set_status(c.status, JD_ERR_BAD_INDEX);
   return -1;
@@ -112,7 +112,7 @@ __device__ __forceinline__ SeqExtent seq_extent(const AttendParams& p, int b) {
   if (e.slot < 0) return e;
   int held;
   slot_state(p.c, e.slot, e.ctx, held);
-  e.nodes = p.num_nodes ? min(max(__ldg(p.num_nodes + b), 0), p.T) : p.T;
+  e.nodes = p.num_nodes ? min(max(__ldcg(p.num_nodes + b), 0), p.T) : p.T;
   e.kv_end = min(e.ctx + e.nodes, held << p.c.page_shift);
   return e;
 }
@@ -196,7 +196,7 @@ __device__ __forceinline__ uint32_t node_word(const AttendParams& p, int b, int 
   const int left = nodes - 32 * w;
   if (left <= 0) return 0u;
   uint32_t m;
-  if (p.mask) m = __ldg(p.mask + (int64_t)b * p.mask_stride + (int64_t)t * p.W + w);
+  if (p.mask) m = __ldcg(p.mask + (int64_t)b * p.mask_stride + (int64_t)t * p.W + w);
   else { const int own = t + 1 - 32 * w; m = own >= 32 ? 0xFFFFFFFFu : (own <= 0 ? 0u : (1u << own) - 1u); }
   return left >= 32 ? m : m & ((1u << left) - 1u);
 }
@@ -211,6 +211,9 @@ __device__ __forceinline__ void split_set(const AttendParams& p, int g, int64_t 
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
+// A kernel that starts early runs while the one in front of it still writes, so nothing it reads is read-only for its whole life: the
+// kernels here use no non-coherent loads (__ldg, const __restrict__), and take what other kernels write from L2 (__ldcg) or by plain
+// loads behind pdl_wait().
 // Launches a kernel that may start before the one in front of it on the stream has ended; it calls pdl_wait() before it reads or
 // writes anything that another kernel touches. (In front of a kernel that triggers nothing itself this saves the launch's latency alone.)
 template <typename... Params, typename... Args>

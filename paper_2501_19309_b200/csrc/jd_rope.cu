@@ -124,7 +124,7 @@ __host__ __device__ __forceinline__ int units_of_head(int head_dim, int half, in
 template <typename T, bool kVec>
 __global__ void __launch_bounds__(kRopeThreads, sizeof(T) == 2 ? 8 : 1) rope_kernel(const T* x, T* out, int64_t tokens, int heads,
                                                             int head_dim, int64_t x_stride, int64_t out_stride,
-                                                            const int32_t* __restrict__ positions, const float* __restrict__ inv_freq,
+                                                            const int32_t* positions, const float* inv_freq,
                                                             int half, int layout, float amplitude, int inverse, int per_block) {
   __shared__ float2 cs[kTokensPerBlock][kMaxHalf];
   pdl_wait();
@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(kRopeThreads, sizeof(T) == 2 ? 8 : 1) rope_ker
   const int n = (int)min((int64_t)per_block, tokens - t0);
   for (int i = threadIdx.x; i < n * half; i += kRopeThreads) {
     const int t = i / half, f = i - t * half;
-    cs[t][f] = turn_of(__ldg(positions + t0 + t), __ldg(inv_freq + f), amplitude, inverse != 0);
+    cs[t][f] = turn_of(__ldcg(positions + t0 + t), __ldcg(inv_freq + f), amplitude, inverse != 0);
   }
   __syncthreads();
   const int units = units_of_head(head_dim, half, layout, kVec), per_token = units * heads;
@@ -172,22 +172,22 @@ __global__ void __launch_bounds__(kRopeThreads) append_kernel(AppendParams p) {
   const CacheView& c = p.c;
   const int slot = slot_of(c, p.slots, b);
   if (slot < 0) return;
-  if (p.num_nodes && t >= __ldg(p.num_nodes + b)) return;
+  if (p.num_nodes && t >= __ldcg(p.num_nodes + b)) return;
   if (threadIdx.x == 0) dup = 0;
   __syncthreads();
   if (p.slots)
     for (int i = threadIdx.x; i < b; i += kRopeThreads)
-      if (__ldg(p.slots + i) == slot) dup = 1;
+      if (__ldcg(p.slots + i) == slot) dup = 1;
   int len, held;
   slot_state(c, slot, len, held);
   const int at = len + t;
-  const int pos = len + (p.depth ? __ldg(p.depth + (int64_t)b * p.depth_stride + t) : t);
-  for (int f = threadIdx.x; f < p.half; f += kRopeThreads) cs[f] = turn_of(pos, __ldg(p.inv_freq + f), p.amplitude, false);
+  const int pos = len + (p.depth ? __ldcg(p.depth + (int64_t)b * p.depth_stride + t) : t);
+  for (int f = threadIdx.x; f < p.half; f += kRopeThreads) cs[f] = turn_of(pos, __ldcg(p.inv_freq + f), p.amplitude, false);
   // the row's page: held, in range, and this sequence's alone
   int page = -1;
   if ((at >> c.page_shift) < held) {
-    page = __ldg(c.table + (int64_t)slot * c.max_pages + (at >> c.page_shift));
-    if (page < 0 || page >= c.pages || __ldg(c.refs + page) > 1) page = -1;
+    page = __ldcg(c.table + (int64_t)slot * c.max_pages + (at >> c.page_shift));
+    if (page < 0 || page >= c.pages || __ldcg(c.refs + page) > 1) page = -1;
   }
   __syncthreads();
   if (dup) {   // an earlier entry names this slot: it counts

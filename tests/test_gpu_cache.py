@@ -240,6 +240,17 @@ def test_attend_many_pieces_repeat_bit_for_bit(T, q_heads, kv_heads, D, ctx):
     assert (first["out"].float() - simt["out"].float()).abs().max() <= 2.0 ** -8 * (1 + 2 * simt["out"].float().abs().max())
 
 
+@pytest.mark.parametrize("T,group", [(32, 1), (33, 1), (16, 4), (65, 1), (128, 1), (43, 3), (16, 16), (86, 3), (128, 4), (1, 128)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attend_where_the_kernel_changes_its_form(T, group, D):
+    """Rows (nodes x query heads of a kv head) on both sides of 32, 64, 128 and 256."""
+    rng = np.random.default_rng(T + group)
+    lens = [700, 130, 0]
+    c = L.filled_cache(lens, T, page=16, q_heads=2 * group, kv_heads=2, D=D, max_nodes=T, seed=T)
+    parents = [L.random_tree(T, rng) for _ in lens]
+    check_attend(*run_attend(c, L.model_of(c), T, parents, "bf16", "tensor", 21))
+
+
 VARIANTS = [("simt", "bf16", 64), ("simt", "f32", 72), ("tensor", "bf16", 64), ("tensor", "bf16", 128)]
 
 
@@ -652,6 +663,46 @@ def test_a_captured_step_replays(dtype):
         for name in ("page_table", "seq_len", "held", "refs", "free_bits", "k", "v"):
             assert torch.equal(getattr(eager, name), getattr(graph, name)), name
     assert eager.seq_len.cpu().tolist() == [45, 12]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_calls_in_a_row_equal_calls_that_are_waited_for(dtype):
+    """Kernels start behind one another's launch: many steps without a wait leave what the same steps leave with one after every call."""
+    B, T, layers, Hq, H, D = 5, 7, 3, 8, 2, 64
+    freq, _ = jd.rope_frequencies(D, 10000.0)
+    rotary = jd.Rotary(freq.cuda(), "interleaved")
+    rng = np.random.default_rng(4)
+    parents = L.random_tree(T, rng)
+    tree = L.device_tree(parents)
+    paths = np.sort(np.stack([rng.permuted(np.arange(1, T))[:4] for _ in range(B * 3)]).reshape(B, 3, 4), axis=2)
+    results = []
+    for wait in (True, False):
+        sync = torch.cuda.synchronize if wait else (lambda: None)
+        c = L.filled_cache([60, 5, 130, 0, 33], 0, page=8, layers=layers, q_heads=Hq, kv_heads=H, D=D, max_nodes=T, dtype=dtype, spare=200,
+                           extra_seqs=2, seed=7)
+        kept = []
+        torch.cuda.synchronize()
+        for step in range(12):
+            k, v, q = (rand((B, T, h, D), 10 * step + i, dtype) for i, h in enumerate((H, H, Hq)))
+            acc = torch.randint(0, 5, (B, 3), generator=torch.Generator().manual_seed(step)).to(torch.int32).cuda()
+            slots = L.ints([0, 1, 2, 3, 4])
+            c.reserve(T, slots); sync()
+            for layer in range(layers):
+                qq = c.append(layer, k, v, tree, rotary=rotary, q=q, slots=slots); sync()
+                o = c.attend(layer, qq, tree, slots=slots); sync()
+                kept += [qq, o["out"], o["lse"]]
+            kept.append(c.commit(acc, L.ints(paths), slots=slots)); sync()
+            if step == 5:
+                c.fork(L.ints([2, 0]), L.ints([5, 6])); sync()
+                c.truncate(L.ints([3]), L.ints([1])); sync()
+            if step == 8:
+                c.free(L.ints([5])); sync()
+                kept.append(c.compact()); sync()
+        # the first sequence outgrows its table of 12 pages on the way: from there on reserves are refused, which has to repeat as well
+        assert c.status() == jd.JD_ERR_PAGES
+        results.append(kept + [c.k, c.v, c.page_table, c.seq_len, c.held, c.refs, c.free_bits])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
 
 
 def test_two_handles_attend_on_two_streams():
