@@ -424,6 +424,8 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     static_assert(kCopyRows % kQRows == 0, "whole steps");
     constexpr int kMaskLoads = kMaxNodes * (kMaxNodes / 32) / 256;
     const int q_first = kPair ? r : tid, q_c = q_first % kVecs, q_r = q_first / kVecs;
+    const int q_row0 = r0 + (kPair ? w * 128 : 0) + q_r, q_t = q_row0 / p.group, q_h = q_row0 - q_t * p.group;
+    const int step_t = kQRows / p.group, step_h = kQRows - step_t * p.group;
     uint4 q_regs[kQLoads];
     uint32_t mask_regs[kMaskLoads];
     int64_t u = run0;
@@ -441,11 +443,16 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       if (y.tiles == 0) return;
       const int nodes = sh.extents[y.b].nodes;
       const char* q_seq = p.q + (int64_t)y.b * p.T * p.q_stride + (int64_t)y.head * p.group * (D * 2) + q_c * 16;
+      // every load is made, rows that are not there from the first one's place: no branch stands between a load and the next
+      int t = q_t, h = q_h;
 #pragma unroll
       for (int i = 0; i < kQLoads; ++i) {
-        const int q_row = r0 + (kPair ? w * 128 : 0) + q_r + i * kQRows, t = q_row / p.group, h = q_row - t * p.group;
-        q_regs[i] = q_row < p.rows && t < nodes ? __ldcg(reinterpret_cast<const uint4*>(q_seq + t * p.q_stride + h * (D * 2)))
-                                                : make_uint4(0u, 0u, 0u, 0u);
+        const bool there = t < min(nodes, p.T);
+        const uint4 v = __ldcg(reinterpret_cast<const uint4*>(q_seq + (there ? t * p.q_stride + h * (D * 2) : 0)));
+        q_regs[i] = make_uint4(there ? v.x : 0u, there ? v.y : 0u, there ? v.z : 0u, there ? v.w : 0u);
+        t += step_t;
+        h += step_h;
+        if (h >= p.group) { h -= p.group; ++t; }
       }
 #pragma unroll
       for (int i = 0; i < kMaskLoads; ++i) {
