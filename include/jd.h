@@ -468,8 +468,9 @@ typedef struct {
 
 /* Ends a step: node 0 and the first accept_len nodes of the kept path become the sequence's next tokens. Their rows
  * are moved together in all layers, seq_len grows by accept_len + 1 and the pages behind are released. accept_len is
- * clamped to 0..path_len; where a path does not rise, or reaches max_nodes or a row that the sequence does not hold, it is
- * cut there and reported. */
+ * clamped to 0..path_len; where a path does not rise, or reaches max_nodes or a row that the sequence does not hold or not
+ * alone, it is cut there and reported; where that is node 0's row, seq_len stays. A sequence that had no nodes in the step
+ * (num_nodes 0) is left out by slot -1. */
 jd_status_t jd_cache_commit(jd_cache_t c, const jd_commit_args_t* args, void* cuda_stream);
 
 /* dst[i] becomes a copy of src[i] (device arrays [n], n <= 1024) that shares its pages; jd_cache_reserve gives each its

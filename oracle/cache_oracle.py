@@ -129,6 +129,10 @@ class Cache:
                 p, r = self.row(s, at)
                 self.k[layer, p, :, r], self.v[layer, p, :, r] = k[i, t], v[i, t]
 
+    def owned(self, s, token):
+        at = token // self.page
+        return at < self.held[s] and self.refs[self.table[s, at]] <= 1
+
     def commit(self, accept, paths=None, slots=None, path_len=None):
         accept = np.asarray(accept).reshape(len(accept), -1)
         chosen = {}
@@ -137,18 +141,20 @@ class Cache:
             chosen[i] = pick
             length = paths.shape[2] if paths is not None else path_len
             a = min(max(int(accept[i, pick]), 0), length)
-            limit, base, before, kept = self.held[s] * self.page, int(self.len[s]), 0, 0
+            base, before, kept = int(self.len[s]), 0, 0
+            if not self.owned(s, base):
+                a, kept = 0, -1
             for j in range(a):
                 node = int(paths[i, pick, j]) if paths is not None else j + 1
-                if node <= before or node >= self.max_nodes or base + node >= limit:
+                if node <= before or node >= self.max_nodes or not self.owned(s, base + node) or not self.owned(s, base + 1 + j):
                     break
                 (fp, fr), (tp, tr) = self.row(s, base + node), self.row(s, base + 1 + j)
                 for x in (self.k, self.v):
                     x[:, tp, :, tr] = x[:, fp, :, fr]
                 before, kept = node, kept + 1
-            if kept < a or base + 1 > limit:
+            if kept < a:
                 self.report(BAD_INDEX)
-            self.len[s] = min(base + kept + 1, limit)
+            self.len[s] = base + kept + 1
             self.release(s, self.pages_for(self.len[s]))
         return chosen
 

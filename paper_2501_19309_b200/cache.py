@@ -11,7 +11,9 @@ One decoding step of a stack of target layers::
     cache.commit(out["accept_len"])                              # keep the accepted nodes, drop the rest
 
 Argument marshalling only; every step runs inside the library's kernels.  All calls are enqueued on ``stream`` (default:
-torch's current stream of the cache's device) and none waits for the device, except :meth:`PagedCache.status`.
+torch's current stream of the cache's device) and none waits for the device, except :meth:`PagedCache.status`.  Outputs that a
+call makes itself are allocated on the current stream: with another ``stream``, pass them in.  Nothing here records a graph for
+autograd: inputs that require gradients are refused while gradients are enabled.
 """
 from __future__ import annotations
 
@@ -123,11 +125,15 @@ class Rotary:
     @staticmethod
     def _step(t: torch.Tensor, name: str, n: int, heads: int, dim: int) -> int:
         """Elements between tokens, 0: dense."""
+        if t.requires_grad and torch.is_grad_enabled():
+            raise ValueError("%s: no autograd here; detach it, the gradient is rotate(grad, positions, inverse=True)" % name)
         if t.is_contiguous():
             return 0
         step, by_head, by_element = t.stride()
         if (dim > 1 and by_element != 1) or (heads > 1 and by_head != dim):
             raise ValueError("%s: heads of a token contiguous" % name)
+        if n > 1 and step < heads * dim:      # a broadcast among them: its step of 0 would stand for dense
+            raise ValueError("%s: tokens must not overlap" % name)
         return step if n > 1 else 0
 
 
@@ -146,6 +152,7 @@ class Tree:
                 continue
             _require(x.dtype == torch.int32 and x.is_contiguous(), "%s: a contiguous int32 tensor" % name)
             _require(tuple(x.shape[-len(tail):]) == tail and x.dim() <= len(tail) + 1, "%s: shape %s, or with B in front" % (name, tail))
+            _require(x.numel() > 0, "%s: at least one sequence" % name)
             batched.add(int(x.shape[0]) if x.dim() > len(tail) else 0)
         if num_nodes is not None:
             _require(num_nodes.dtype == torch.int32 and num_nodes.is_contiguous() and num_nodes.dim() == 1, "num_nodes: a contiguous int32 vector")
@@ -221,6 +228,7 @@ class PagedCache:
         _check(lib.jd_cache_create(C.byref(h), C.byref(self.cfg), C.byref(buf)), "jd_cache_create")
         self.h = h
         self._scale = 1.0 / math.sqrt(dim)
+        torch.cuda.current_stream(dev).synchronize()     # the zeroes are there, whatever stream the first call is on
 
     @classmethod
     def allocate(cls, num_layers: int, num_pages: int, page_size: int, q_heads: int, kv_heads: int, head_dim: int, max_seqs: int,
@@ -259,6 +267,8 @@ class PagedCache:
         """Elements between tokens (0: dense) of [B, T, heads, head_dim] whose tokens lie evenly, heads contiguous."""
         if x.shape != shape or x.dtype is not self.dtype or x.get_device() != self.index:
             raise ValueError("%s: %s of the cache's type, on its device" % (name, list(shape)))
+        if x.requires_grad and torch.is_grad_enabled():
+            raise ValueError("%s: no autograd here; detach it" % name)
         if x.is_contiguous():
             return 0
         B, T, H, D = shape
@@ -266,6 +276,8 @@ class PagedCache:
         step = st if T > 1 else sb
         if (D > 1 and sd != 1) or (H > 1 and sh != D) or (B > 1 and T > 1 and sb != T * st):
             raise ValueError("%s: heads of a token contiguous, tokens evenly spaced" % name)
+        if B * T > 1 and step < H * D:        # a broadcast among them: its step of 0 would stand for dense
+            raise ValueError("%s: tokens must not overlap" % name)
         return step if B * T > 1 else 0
 
     def _tree(self, tree: Optional[Tree], B: int, T: int):
@@ -351,7 +363,8 @@ class PagedCache:
                chosen: Optional[torch.Tensor] = None, path_len: Optional[int] = None, stream=None) -> torch.Tensor:
         """Keeps node 0 and the accepted nodes. accept_len [B] or [B, num_paths] (int32, as ``Verifier.verify`` returns it); paths
         [B, num_paths, path_len] nodes of the draft tokens along every path, None: a chain (path_len then bounds
-        accept_len, default max_nodes - 1). Returns the number of the kept path of every sequence, [B]."""
+        accept_len, default max_nodes - 1). Returns the number of the kept path of every sequence, [B]
+        (entries of padding sequences stay as they were)."""
         if accept_len.dim() not in (1, 2):
             raise ValueError("accept_len: [B] or [B, num_paths]")
         B = accept_len.shape[0]
@@ -406,7 +419,7 @@ class PagedCache:
         return used
 
     def status(self) -> int:
-        """Waits for the cache's last call; the first device-side problem since the last query, or JD_OK."""
+        """Waits for the stream of the cache's last call (a replayed graph's stream is the caller's to wait for); the first device-side problem since the last query, or JD_OK."""
         out = C.c_int(0)
         _check(self._lib.jd_cache_last_status(self.h, C.byref(out)), "jd_cache_last_status")
         return out.value

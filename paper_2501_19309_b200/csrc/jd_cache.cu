@@ -36,6 +36,12 @@ __device__ __forceinline__ bool named_before(const int32_t* slots, int b, int sl
   return *flag != 0;
 }
 
+// Free pages of word w of the bitmap; bits behind the last page count for nothing, whatever they are.
+__device__ __forceinline__ uint32_t free_word(const CacheView& c, int w) {
+  const int left = c.pages - 32 * w;
+  return c.free_bits[w] & (left >= 32 ? 0xFFFFFFFFu : (1u << left) - 1u);
+}
+
 // One owner less for a page; its last one frees it.
 __device__ __forceinline__ void release_page(const CacheView& c, int page) {
   if (page < 0 || page >= c.pages) { set_status(c.status, JD_ERR_BAD_INDEX); return; }
@@ -196,14 +202,14 @@ __global__ void __launch_bounds__(kBookThreads) reserve_kernel(CacheView c, int 
   const int words = (c.pages + 31) >> 5, per = (words + kBookThreads - 1) / kBookThreads;
   const int w0 = min(b * per, words), w1 = min(w0 + per, words);
   int mine = 0;
-  for (int w = w0; w < w1; ++w) mine += __popc(c.free_bits[w]);
+  for (int w = w0; w < w1; ++w) mine += __popc(free_word(c, w));
   const int first = block_exclusive(mine, warp_sums, &available);
   const bool ok = !fail && total <= available;   // else nothing changes
   if (!ok && b == 0) set_status(c.status, JD_ERR_PAGES);
   if (ok) {
     int rank = first;
     for (int w = w0; w < w1 && rank < total; ++w)
-      for (uint32_t bits = c.free_bits[w]; bits && rank < total; bits &= bits - 1) page_list[rank++] = 32 * w + __ffs(bits) - 1;
+      for (uint32_t bits = free_word(c, w); bits && rank < total; bits &= bits - 1) page_list[rank++] = 32 * w + __ffs(bits) - 1;
   }
   s_off[b] = off;
   s_first[b] = held - (copy ? 1 : 0);
@@ -226,7 +232,7 @@ __global__ void __launch_bounds__(kBookThreads) reserve_kernel(CacheView c, int 
   if (!last_one || !ok) return;
   int rank = first;
   for (int w = w0; w < w1 && rank < total; ++w) {
-    uint32_t bits = c.free_bits[w], taken = 0;
+    uint32_t bits = free_word(c, w), taken = 0;
     for (; bits && rank < total; bits &= bits - 1, ++rank) {
       const int i = __ffs(bits) - 1;
       taken |= 1u << i;
@@ -254,8 +260,9 @@ __global__ void __launch_bounds__(kBookThreads) reserve_kernel(CacheView c, int 
 __global__ void __launch_bounds__(kCopyThreads) move_pages_kernel(CacheView c, const int* src, const int* dst, const int* count) {
   pdl_wait();
   pdl_trigger();
-  for (int i = blockIdx.y; i < *count; i += gridDim.y) 
-    for (int plane = blockIdx.x; plane < c.layers * 2 * c.kv_heads; plane += gridDim.x) copy_rows_of_page(c, src[i], dst[i], c.page_size, plane, threadIdx.x);
+  for (int i = blockIdx.y; i < *count; i += gridDim.y)
+    for (int plane = blockIdx.x; plane < c.layers * 2 * c.kv_heads; plane += gridDim.x)
+      copy_rows_of_page(c, src[i], dst[i], c.page_size, plane, threadIdx.x);
 }
 
 // Commit: blocks (x, b) move 16-byte columns of sequence b's kept rows, every thread its own column through all rows in
@@ -285,7 +292,17 @@ __global__ void __launch_bounds__(kMoveThreads) commit_kernel(CacheView c, const
   // check the path and find its rows
   const int32_t* table = c.table + (int64_t)slot * c.max_pages;
   const int limit = held << c.page_shift;          // tokens that the sequence holds
-  if (threadIdx.x == 0) { s_cut = a; s_moves = 0; }
+  // Rows of a page that has other owners are not the sequence's to take or to write (a reserve that found no pages leaves it
+  // at that). Owners of such a page hold tokens in it, so no block of this call releases it: every block sees the same count.
+  if (threadIdx.x == 0) {
+    s_moves = 0;
+    bool own = len < limit;
+    if (own) {
+      const int page = table[len >> c.page_shift];
+      own = page >= 0 && page < c.pages && c.refs[page] <= 1;
+    }
+    s_cut = own ? a : -1;
+  }
   if (threadIdx.x < a) s_node[threadIdx.x] = paths ? __ldcg(paths + ((int64_t)b * num_paths + pick) * path_len + threadIdx.x) : (int)threadIdx.x + 1;
   __syncthreads();
   if (threadIdx.x < a) {
@@ -294,6 +311,7 @@ __global__ void __launch_bounds__(kMoveThreads) commit_kernel(CacheView c, const
     if (ok) {
       const int fp = table[(len + node) >> c.page_shift], tp = table[(len + 1 + i) >> c.page_shift];
       ok = fp >= 0 && fp < c.pages && tp >= 0 && tp < c.pages;
+      if (ok) ok = (c.refs[fp] <= 1) & (c.refs[tp] <= 1);
       const int mask = c.page_size - 1;
       s_from[i] = (((int64_t)fp * c.kv_heads) << c.page_shift) + ((len + node) & mask);
       s_to[i] = (((int64_t)tp * c.kv_heads) << c.page_shift) + ((len + 1 + i) & mask);
@@ -303,7 +321,7 @@ __global__ void __launch_bounds__(kMoveThreads) commit_kernel(CacheView c, const
   }
   __syncthreads();
   const int kept = s_cut;
-  if (threadIdx.x == 0 && blockIdx.x == 0 && (kept < a || len + 1 > limit)) set_status(c.status, JD_ERR_BAD_INDEX);
+  if (threadIdx.x == 0 && blockIdx.x == 0 && kept < a) set_status(c.status, JD_ERR_BAD_INDEX);
   if (s_moves && kept > 0) {
     int skip = 0;
     while (skip < kept && s_node[skip] == skip + 1) ++skip;
@@ -337,7 +355,7 @@ __global__ void __launch_bounds__(kMoveThreads) commit_kernel(CacheView c, const
     if (gridDim.x > 1) commit_cnt[b] = 0;
     if (chosen) chosen[b] = pick;
   }
-  const int new_len = min(len + kept + 1, limit);
+  const int new_len = len + kept + 1;
   cut_slot(c, slot, held, pages_for(c, new_len), new_len);
 }
 

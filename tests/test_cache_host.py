@@ -250,3 +250,56 @@ def test_model_rotation():
     y = O.rope(x, [2], f, "interleaved", 2.0)
     assert np.allclose(y[0, 0, :2], [2 * (math.cos(1) - 2 * math.sin(1)), 2 * (2 * math.cos(1) + math.sin(1))])
     assert np.allclose(O.rope(O.rope(x, [7], f, "half"), [7], f, "half", inverse=True), x)
+
+
+def test_strides_that_steps_cannot_say_are_refused():
+    """A step of 0 stands for dense tokens: broadcast and overlapping tokens must not come out as that."""
+    from paper_2501_19309_b200.cache import PagedCache, Rotary
+    one = torch.zeros(1, 4, 64)
+    with pytest.raises(ValueError):
+        Rotary._step(one.expand(5, 4, 64), "x", 5, 4, 64)
+    with pytest.raises(ValueError):
+        Rotary._step(torch.zeros(5 * 256).as_strided((3, 4, 64), (128, 64, 1)), "x", 3, 4, 64)
+    assert Rotary._step(one.expand(1, 4, 64), "x", 1, 4, 64) == 0
+    assert Rotary._step(torch.zeros(5, 6, 64)[:, :4], "x", 5, 4, 64) == 384
+    c = object.__new__(PagedCache)
+    c.h, c.dtype, c.index = None, torch.float32, -1
+    for B, T in ((1, 5), (5, 1), (2, 5)):
+        with pytest.raises(ValueError):
+            c._tokens(one.unsqueeze(0).expand(B, T, 4, 64), "q", (B, T, 4, 64))
+    with pytest.raises(ValueError):
+        c._tokens(torch.zeros(2048).as_strided((1, 3, 4, 64), (256, 128, 64, 1)), "q", (1, 3, 4, 64))
+    assert c._tokens(torch.zeros(2, 5, 6, 64)[:, :, :4], "q", (2, 5, 4, 64)) == 384
+    assert c._tokens(torch.zeros(2, 5, 4, 64)[:, :1], "q", (2, 1, 4, 64)) == 5 * 256
+
+
+def test_inputs_that_require_gradients_are_refused():
+    from paper_2501_19309_b200.cache import PagedCache, Rotary
+    c = object.__new__(PagedCache)
+    c.h, c.dtype, c.index = None, torch.float32, -1
+    x = torch.zeros(2, 3, 4, 64, requires_grad=True)
+    with pytest.raises(ValueError):
+        c._tokens(x, "q", (2, 3, 4, 64))
+    with pytest.raises(ValueError):
+        Rotary._step(x[0], "x", 3, 4, 64)
+    with torch.no_grad():
+        assert c._tokens(x, "q", (2, 3, 4, 64)) == 0 and Rotary._step(x[0], "x", 3, 4, 64) == 0
+
+
+def test_a_tree_for_no_sequence_is_refused():
+    with pytest.raises(ValueError):
+        jd.Tree(3, mask=torch.zeros(0, 3, 1, dtype=torch.int32))
+    with pytest.raises(ValueError):
+        jd.Tree(3, depth=torch.zeros(0, 3, dtype=torch.int32))
+
+
+def test_model_leaves_rows_of_shared_pages_alone():
+    """Without pages to part on, a commit takes and moves nothing in a page that another sequence still reads."""
+    m = O.Cache(np.zeros((1, 1, 1, 8, 2)), np.zeros((1, 1, 1, 8, 2)), np.full((2, 1), -1), np.zeros(2, int), np.zeros(2, int), np.zeros(1, int), 4)
+    m.reserve(4, [0])
+    m.append(0, np.arange(4.).reshape(1, 4, 1, 1).repeat(2, 3), np.zeros((1, 4, 1, 2)), [0])
+    m.commit([3], None, [0], 3)
+    m.fork([0], [1])
+    m.truncate([1], [0])
+    m.commit([[1]], np.array([[[2]]]), [0])           # would move row 3 over row 2 of sequence 1
+    assert m.status == O.BAD_INDEX and m.len.tolist() == [1, 4] and m.k[0, 0, 0, :4, 0].tolist() == [0, 1, 2, 3]

@@ -487,6 +487,52 @@ def test_forks_share_until_they_write():
         assert torch.equal(c.k[:, p, :, :3], c.k[:, 0, :, :3]) and torch.equal(c.v[:, p, :, :3], c.v[:, 0, :, :3])
 
 
+@pytest.mark.parametrize("tree", [False, True])
+def test_commit_leaves_rows_of_shared_pages_alone(tree):
+    """A reserve that finds no pages leaves a page shared; the rest of the step then takes and moves nothing in it."""
+    c = L.empty_cache(2, 1, 8, 1, 1, 8, 2, 4, 4)
+    c.reserve(4, L.ints([0]))
+    for layer in range(2):
+        c.append(layer, rand((1, 4, 1, 8), layer), rand((1, 4, 1, 8), 9), slots=L.ints([0]))
+    c.commit(L.ints([3]), slots=L.ints([0]), path_len=3)
+    c.fork(L.ints([0]), L.ints([1]))
+    c.truncate(L.ints([1]), L.ints([0]))
+    assert c.status() == jd.JD_OK
+    k, v = c.k.clone(), c.v.clone()
+    c.reserve(4, L.ints([0]))
+    assert c.status() == jd.JD_ERR_PAGES
+    for layer in range(2):
+        c.append(layer, rand((1, 4, 1, 8), 5), rand((1, 4, 1, 8), 6), slots=L.ints([0]))
+    c.commit(L.ints([[1]]), L.ints([[[2]]]) if tree else None, slots=L.ints([0]), path_len=3)
+    assert c.status() == jd.JD_ERR_BAD_INDEX
+    assert torch.equal(c.k, k) and torch.equal(c.v, v) and c.seq_len.cpu().tolist() == [1, 4] and c.refs.cpu().tolist() == [2]
+    c.free(L.ints([1]))                                 # now the page is the first one's alone
+    c.reserve(3, L.ints([0]))
+    c.commit(L.ints([[1]]), L.ints([[[2]]]), slots=L.ints([0]))
+    assert c.status() == jd.JD_OK and int(c.seq_len[0]) == 3 and torch.equal(c.k[:, 0, :, 2], k[:, 0, :, 3])
+
+
+def test_bits_behind_the_last_page_are_not_handed_out():
+    c = L.empty_cache(1, 5, 8, 1, 1, 8, 2, 16, 4)
+    c.free_bits.fill_(-1)
+    c.reserve(6 * 8, L.ints([0]))
+    assert c.status() == jd.JD_ERR_PAGES and int(c.held[0]) == 0
+    c.reserve(5 * 8, L.ints([0]))
+    assert c.status() == jd.JD_OK and c.page_table[0, :5].cpu().tolist() == [0, 1, 2, 3, 4] and c.refs.cpu().tolist() == [1] * 5
+
+
+def test_broadcast_inputs_and_gradients_are_refused():
+    c = L.filled_cache([20, 30], 4, max_nodes=4)
+    q = rand((1, 1, 4, 64), 1).expand(2, 4, 4, 64)
+    with pytest.raises(ValueError):
+        c.attend(0, q)
+    with pytest.raises(ValueError):
+        c.append(0, q[:, :, :2], q[:, :, :2])
+    with pytest.raises(ValueError):
+        c.attend(0, rand((2, 4, 4, 64), 1).requires_grad_())
+    assert c.status() == jd.JD_OK
+
+
 # ------------------------------------------------------------------------------------------- refusals
 def refused(f, status=jd.JD_ERR_INVALID_ARG):
     with pytest.raises(jd.JdError) as e:
