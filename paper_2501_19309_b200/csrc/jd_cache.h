@@ -156,11 +156,15 @@ __device__ __forceinline__ void unit_prefix(const AttendParams& p, int* prefix, 
 }
 
 // First unit of run g, and the run that holds unit u; 32-bit divisions where they are enough (64-bit ones take ten times as long).
+// With fewer units than groups the first `units` groups take one each: a run between two others is never empty, so that every group
+// between a segment's first and its last has left a part.
 __device__ __forceinline__ int64_t run_start(int64_t units, int groups, int g) {
+  if (units <= groups) return min((int64_t)g, units);
   const int64_t n = units * g;
   return units < (1 << 22) ? (int64_t)((uint32_t)n / (uint32_t)groups) : n / groups;
 }
 __device__ __forceinline__ int run_of(int64_t units, int groups, int64_t u) {
+  if (units <= groups) return (int)u;
   const int64_t n = (u + 1) * groups - 1;
   return units < (1 << 22) ? (int)((uint32_t)n / (uint32_t)units) : (int)(n / units);
 }

@@ -240,6 +240,18 @@ def test_attend_many_pieces_repeat_bit_for_bit(T, q_heads, kv_heads, D, ctx):
     assert (first["out"].float() - simt["out"].float()).abs().max() <= 2.0 ** -8 * (1 + 2 * simt["out"].float().abs().max())
 
 
+@pytest.mark.parametrize("variant,dtype,D", [("simt", "f32", 72), ("tensor", "bf16", 64), ("tensor", "bf16", 128)])
+@pytest.mark.parametrize("T,q_heads", [(1, 8), (5, 8), (26, 16), (26, 48)])
+def test_attend_short_calls_behind_a_long_one(variant, dtype, D, T, q_heads):
+    """A call that gives work to a part of the SMs reads nothing that an earlier, larger one left in the workspace."""
+    c = L.filled_cache([7000], T, page=16, q_heads=q_heads, kv_heads=4, D=D, dtype=dtype, max_nodes=T, seed=3)
+    parents = L.random_tree(T, np.random.default_rng(T), "tree")
+    for n in (7000, 2500, 1300, 701, 300, 120, 3):
+        c.truncate(L.ints([n]))
+        c.reserve(T)
+        check_attend(*run_attend(c, L.model_of(c), T, parents, dtype, variant, n))
+
+
 @pytest.mark.parametrize("T,group", [(32, 1), (33, 1), (16, 4), (65, 1), (128, 1), (43, 3), (16, 16), (86, 3), (128, 4), (1, 128)])
 @pytest.mark.parametrize("D", [64, 128])
 def test_attend_where_the_kernel_changes_its_form(T, group, D):
