@@ -348,6 +348,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendPara
   __shared__ float4 s_o[kJoinWarps][kCols][32];
   __shared__ float2 s_ml[kJoinWarps];
   pdl_wait();
+  pdl_trigger();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int D = p.c.head_dim, pitch = D + kPartPad;
   const int block_rows = join_rows(p.rows), first_row = blockIdx.x * block_rows;
