@@ -252,6 +252,27 @@ def test_attend_short_calls_behind_a_long_one(variant, dtype, D, T, q_heads):
         check_attend(*run_attend(c, L.model_of(c), T, parents, dtype, variant, n))
 
 
+@pytest.mark.parametrize("seed,kv_heads,group,D", [(0, 2, 4, 64), (1, 1, 8, 128), (2, 8, 1, 128), (3, 3, 10, 64)])
+def test_attend_random_calls_on_one_cache(seed, kv_heads, group, D):
+    """Calls of every size in turn, both kernels, on one workspace: none sees what another left."""
+    rng = np.random.default_rng(seed)
+    lens = [0, 1, 127, 400, 2000, 5000]
+    c = L.filled_cache(lens, 40, page=16, q_heads=kv_heads * group, kv_heads=kv_heads, D=D, max_nodes=64, seed=seed)
+    for call in range(24):
+        if call % 3 == 2:                              # shorter, and longer again as far as the rows go
+            b = int(rng.integers(0, 6))
+            if int(c.seq_len[b]) > 0:
+                c.seq_len[b] = int(rng.integers(0, lens[b] + 1))
+        T = int(rng.choice([1, 2, 5, 9, 17, 33, 64]))
+        slots = rng.choice([-1, 0, 1, 2, 3, 4, 5], int(rng.integers(1, 8)), replace=True).tolist()
+        while len(slots) > 6:
+            slots.pop()
+        nodes = L.ints(rng.integers(0, T + 1, len(slots))) if rng.random() < 0.4 else None
+        parents = [L.random_tree(T, rng, "tree") for _ in slots]
+        variant = "simt" if rng.random() < 0.3 else "tensor"
+        check_attend(*run_attend(c, L.model_of(c), T, parents, "bf16", variant, call, slots=L.ints(slots), num_nodes=nodes, B=len(slots)))
+
+
 @pytest.mark.parametrize("T,group", [(32, 1), (33, 1), (16, 4), (65, 1), (128, 1), (43, 3), (16, 16), (86, 3), (128, 4), (1, 128)])
 @pytest.mark.parametrize("D", [64, 128])
 def test_attend_where_the_kernel_changes_its_form(T, group, D):
