@@ -284,6 +284,7 @@ __global__ void __launch_bounds__(kMoveThreads) commit_kernel(CacheView c, const
   int len, held;
   slot_state(c, slot, len, held);
   int pick = 0, a = __ldcg(accept_len + (int64_t)b * num_paths);
+#pragma unroll 4
   for (int i = 1; i < num_paths; ++i) {
     const int x = __ldcg(accept_len + (int64_t)b * num_paths + i);
     if (x > a) { a = x; pick = i; }
@@ -294,15 +295,7 @@ __global__ void __launch_bounds__(kMoveThreads) commit_kernel(CacheView c, const
   const int limit = held << c.page_shift;          // tokens that the sequence holds
   // Rows of a page that has other owners are not the sequence's to take or to write (a reserve that found no pages leaves it
   // at that). Owners of such a page hold tokens in it, so no block of this call releases it: every block sees the same count.
-  if (threadIdx.x == 0) {
-    s_moves = 0;
-    bool own = len < limit;
-    if (own) {
-      const int page = table[len >> c.page_shift];
-      own = page >= 0 && page < c.pages && c.refs[page] <= 1;
-    }
-    s_cut = own ? a : -1;
-  }
+  if (threadIdx.x == 0) { s_cut = a; s_moves = 0; }
   if (threadIdx.x < a) s_node[threadIdx.x] = paths ? __ldcg(paths + ((int64_t)b * num_paths + pick) * path_len + threadIdx.x) : (int)threadIdx.x + 1;
   __syncthreads();
   if (threadIdx.x < a) {
@@ -319,6 +312,14 @@ __global__ void __launch_bounds__(kMoveThreads) commit_kernel(CacheView c, const
     }
     if (!ok) atomicMin(&s_cut, i);
   }
+  if (threadIdx.x == kMaxNodes) {                  // node 0, by a thread that has no node to check
+    bool ok = len < limit;
+    if (ok) {
+      const int page = table[len >> c.page_shift];
+      ok = page >= 0 && page < c.pages && c.refs[page] <= 1;
+    }
+    if (!ok) atomicMin(&s_cut, -1);
+  }
   __syncthreads();
   const int kept = s_cut;
   if (threadIdx.x == 0 && blockIdx.x == 0 && kept < a) set_status(c.status, JD_ERR_BAD_INDEX);
@@ -326,11 +327,10 @@ __global__ void __launch_bounds__(kMoveThreads) commit_kernel(CacheView c, const
     int skip = 0;
     while (skip < kept && s_node[skip] == skip + 1) ++skip;
     const int chunks = c.row_bytes / 16;
-    const int64_t columns = (int64_t)c.layers * 2 * c.kv_heads * chunks;
-    for (int64_t u = (int64_t)blockIdx.x * kMoveThreads + threadIdx.x; u < columns; u += (int64_t)gridDim.x * kMoveThreads) {
-      const int chunk = (int)(u % chunks);
-      const int64_t plane = u / chunks;
-      const int head = (int)(plane % c.kv_heads), lk = (int)(plane / c.kv_heads);
+    const uint32_t columns = (uint32_t)c.layers * 2 * c.kv_heads * chunks;   // at most 4096 x 2 x 1024 x 64
+    for (uint32_t u = blockIdx.x * kMoveThreads + threadIdx.x; u < columns; u += gridDim.x * kMoveThreads) {
+      const uint32_t plane = u / chunks;
+      const int chunk = (int)(u - plane * chunks), lk = (int)(plane / c.kv_heads), head = (int)plane - lk * c.kv_heads;
       char* base = ((lk & 1) ? c.v : c.k) + page_row(c, lk >> 1, 0, head, 0) * c.row_bytes + chunk * 16;
       for (int i0 = skip; i0 < kept; i0 += kMoveBatch) {
         uint4 x[kMoveBatch];
@@ -674,7 +674,14 @@ jd_status_t jd_cache_commit(jd_cache_t c, const jd_commit_args_t* a, void* cuda_
   cudaStream_t st = (cudaStream_t)cuda_stream;
   const CacheView v = view_of(c);
   const int64_t columns = (int64_t)v.layers * 2 * v.kv_heads * (v.row_bytes / 16);
-  const int blocks = a->paths && a->path_len > 0 ? (int)std::min<int64_t>((columns + kMoveThreads - 1) / kMoveThreads, 65535) : 1;
+  int blocks = a->paths && a->path_len > 0 ? (int)std::min<int64_t>((columns + kMoveThreads - 1) / kMoveThreads, 65535) : 1;
+  // Finding a sequence's rows takes a block longer than a turn of moving them: three blocks on an SM in all, in even turns. 64 trees of 26
+  // nodes in 32 layers of 8 heads of 128, with the truncation and the reserve in front of it: 45 us, a block for each turn 51.
+  const int most = std::max(1, 3 * c->num_sms / a->B);
+  if (blocks > most) {
+    const int turns = (blocks + most - 1) / most;
+    blocks = (blocks + turns - 1) / turns;
+  }
   return finish(c, launch_chained(commit_kernel, dim3((unsigned)blocks, (unsigned)a->B), dim3(kMoveThreads), 0, st, v, a->slots, a->accept_len,
                                   a->num_paths, a->path_len, a->paths, c->cfg.max_nodes, a->chosen, c->commit_cnt), st);
 }
