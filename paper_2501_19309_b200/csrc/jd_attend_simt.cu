@@ -3,12 +3,13 @@
 //
 // A CTA takes 16 query rows (4 where there are no more) of a (sequence, kv head) - a row is a node and one of the query
 // heads that share the kv head - and walks its run of tiles of 64 cached tokens (jd_cache.h says how runs are cut). Per tile: K and
-// V to shared memory, the scores by 256 threads (a token each and a quarter of the rows), running maximum and sum by a warp
-// for a row, and the weighted sum of V with every warp taking an eighth of the tokens for all rows and up to 256 columns in
+// V to shared memory, the scores by 256 threads (two tokens, four rows and half of the columns each), running maximum and sum
+// by a warp for a row, and the weighted sum of V with every warp taking an eighth of the tokens for all rows and up to 256 columns in
 // registers, so that one shared-memory read of V serves all rows. The warps' sums meet once per piece of a segment.
 // Two CTAs on an SM, so that one's loads run beside the other's products. float32, B200: 16 sequences of 8,000 tokens, 8 heads of
-// 128, one token each: 296 us, 3.5 TB/s; blocks of 26 nodes, 2 x 8 heads over 2,000 tokens: 17 TFLOP/s, bound by issuing
-// shared-memory reads and products (a tile is some 5,000 issue slots of each SM partition).
+// 128, one token each: 260 us, 4.0 TB/s; 8 blocks of 26 nodes, 16 heads on 4 of 128 over 2,000 tokens: 200 us, 17 TFLOP/s, of which
+// 58 % of the issue slots, 50 % of the shared-memory accesses and 36 % of the FMA pipe: what stays is the wait between a tile's
+// four phases with 16 warps on an SM.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -48,7 +49,7 @@ __host__ __device__ constexpr int pitch_of(int head_dim) { return head_dim + 4; 
 // floats between tokens of the score buffer: the rows and padding, 16-byte aligned
 __host__ __device__ constexpr int score_pad(int rows) { return rows == 4 ? 12 : rows + 4; }
 size_t simt_smem(int head_dim, int rows) {
-  return sizeof(float) * ((size_t)2 * kTile * pitch_of(head_dim) + rows * head_dim + kTile * score_pad(rows));
+  return sizeof(float) * ((size_t)2 * kTile * pitch_of(head_dim) + rows * pitch_of(head_dim) + (rows == 4 ? 1 : 2) * kTile * score_pad(rows));
 }
 
 // kCols: groups of 128 columns that a lane's accumulators cover (head_dim <= 128 kCols)
@@ -57,14 +58,16 @@ template <typename T, int kCols, int kRows>
 __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_simt_kernel(AttendParams p) {
   constexpr int kScorePad = score_pad(kRows);
   extern __shared__ __align__(16) float smem[];
-  __shared__ int prefix[kMaxCacheBatch + 1], warp_sums[kThreads / 32], pages[kTile / 8];
+  __shared__ int prefix[kMaxCacheBatch + 1], warp_sums[kThreads / 32];
+  __shared__ int64_t s_row[kTile];   // elements in front of a token's row of K and V
   __shared__ float s_m[kRows], s_l[kRows], s_fac[kRows];
   __shared__ uint32_t s_mask[kRows][kMaxNodes / 32];
   const int D = p.c.head_dim, pitch = pitch_of(D);
   float* sK = smem;
   float* sV = sK + kTile * pitch;
   float* sQ = sV + kTile * pitch;
-  float* sS = sQ + kRows * D;
+  float* sS = sQ + kRows * pitch;
+  float* sS1 = sS + kTile * kScorePad;   // 16 rows: the other half of the columns' share
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int g = blockIdx.x / p.row_blocks, rb = blockIdx.x - g * p.row_blocks;
   const int r0 = rb * kRows, nrows = min(kRows, p.rows - r0);
@@ -78,6 +81,7 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
   const T* kbase = reinterpret_cast<const T*>(p.c.k);
   const T* vbase = reinterpret_cast<const T*>(p.c.v);
 
+  const int step = kCols == 1 && D <= 64 ? 2 : 1, col_lane = step == 2 ? lane & 15 : lane, my_token = step == 2 ? lane >> 4 : 0;
   for (int64_t u = run0; u < run1;) {
     const Piece x = piece_at(p, prefix, u, run1);
     u = x.next;
@@ -93,7 +97,7 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
       if (r < nrows && t < ex.nodes)
         load4<T>(reinterpret_cast<const T*>(p.q + ((int64_t)b * p.T + t) * p.q_stride) + (int64_t)(head * p.group + gq) * D + d, v);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) sQ[r * D + d + k] = v[k];
+      for (int k = 0; k < 4; ++k) sQ[r * pitch + d + k] = v[k];
     }
     if (tid < kRows) { s_m[tid] = -INFINITY; s_l[tid] = 0.f; }
     for (int i = tid; i < kRows * p.W; i += kThreads) {
@@ -106,14 +110,20 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
 #pragma unroll
       for (int k = 0; k < 4 * kCols; ++k) acc[r][k] = 0.f;
 
+    // page of this thread's token of a tile (rows behind the sequence: the last one's), fetched a tile ahead
+    auto token_of = [&](int tile) { return tile * kTile + min(tid, max(min(kTile, ex.kv_end - tile * kTile) - 1, 0)); };
+    auto page_of = [&](int tile) {
+      const int kv = token_of(tile);
+      return tid < kTile && kv < ex.kv_end ? __ldcg(p.c.table + (int64_t)ex.slot * p.c.max_pages + (kv >> p.c.page_shift)) : 0;
+    };
+    int page = page_of(tile0);
     for (int tile = tile0; tile < tile0 + ntiles; ++tile) {
       const int kv0 = tile * kTile, nkv = max(0, min(kTile, ex.kv_end - kv0));
       __syncthreads();   // the previous tile's buffers are free
-      if (tid < kTile >> min(p.c.page_shift, kSimtTileShift)) {
-        const int at = (kv0 >> p.c.page_shift) + tid;
-        int page = (at << p.c.page_shift) < ex.kv_end ? __ldcg(p.c.table + (int64_t)ex.slot * p.c.max_pages + at) : 0;
+      if (tid < kTile) {
         if (page < 0 || page >= p.c.pages) { set_status(p.c.status, JD_ERR_BAD_INDEX); page = 0; }
-        pages[tid] = page;
+        s_row[tid] = page_row(p.c, p.layer, page, head, token_of(tile) & (p.c.page_size - 1)) * D;
+        if (tile + 1 < tile0 + ntiles) page = page_of(tile + 1);
       }
       __syncthreads();
       const int vec = D / 4;
@@ -122,9 +132,7 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
       if constexpr (sizeof(T) == 4) {              // straight to shared memory; rows behind the sequence may hold anything: zeroes
         for (int i = tid; i < kTile * vec; i += kThreads) {
           const int r = (int)((i * per_vec) >> 20), d = (i - r * vec) * 4;
-          const int kv = kv0 + min(r, max(nkv - 1, 0));
-          const int page = pages[(kv >> p.c.page_shift) - (kv0 >> p.c.page_shift)];
-          const int64_t off = page_row(p.c, p.layer, page, head, kv & (p.c.page_size - 1)) * D + d;
+          const int64_t off = s_row[r] + d;
           copy16_or_zero(sK + r * pitch + d, kbase + off, r < nkv);
           copy16_or_zero(sV + r * pitch + d, vbase + off, r < nkv);
         }
@@ -139,9 +147,7 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
 #pragma unroll
             for (int e = 0; e < 4; ++e) kx[j][e] = vx[j][e] = 0.f;
             if (r < nkv) {
-              const int kv = kv0 + r;
-              const int page = pages[(kv >> p.c.page_shift) - (kv0 >> p.c.page_shift)];
-              const int64_t off = page_row(p.c, p.layer, page, head, kv & (p.c.page_size - 1)) * D + d;
+              const int64_t off = s_row[r] + d;
               load4<T>(kbase + off, kx[j]);
               load4<T>(vbase + off, vx[j]);
             }
@@ -157,31 +163,53 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
         }
       }
       __syncthreads();
-      {   // scores: token tid % 64, kRows / 4 rows from (tid / 64) on
-        constexpr int kMine = kRows / 4;
-        const int kv = tid & (kTile - 1), rg = (tid >> kSimtTileShift) * kMine;
-        float s[kMine] = {};
+      auto score = [&](float s, int kv, int r) {   // scaled; -inf where row r must not see token kv of the tile
+        const int node = kv0 + kv - ex.ctx;        // < 0: context
+        return kv < nkv && (node < 0 || ((s_mask[r][node >> 5] >> (node & 31)) & 1u)) ? s * p.scale_log2 : -INFINITY;
+      };
+      if constexpr (kRows == 4) {   // scores: token tid % 64, row tid / 64
+        const int kv = tid & (kTile - 1), r = tid >> kSimtTileShift;
+        float s = 0.f;
 #pragma unroll 4
         for (int d = 0; d < D; d += 4) {
           const float4 x = *reinterpret_cast<const float4*>(sK + kv * pitch + d);
+          const float4 y = *reinterpret_cast<const float4*>(sQ + r * pitch + d);
+          s = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s))));
+        }
+        sS[kv * kScorePad + r] = score(s, kv, r);
+      } else {
+        // A warp takes 16 tokens, all rows and half of the columns; a lane two tokens and four rows: eight lanes read eight tokens and
+        // four read four rows in one shared-memory access each, six of them for 32 products. (A token and four rows a lane read
+        // 16 bytes of Q at a time for a whole warp, and the accesses took twice as long as the products.)
+        const int t0 = (warp & 3) * 16 + (lane & 7), rl = lane >> 3, half = D / 2, d0 = (warp >> 2) * half;
+        float s[2][4] = {};
+#pragma unroll 2
+        for (int d = d0; d < d0 + half; d += 4) {
+          float4 x[2];
 #pragma unroll
-          for (int r = 0; r < kMine; ++r) {
-            const float4 y = *reinterpret_cast<const float4*>(sQ + (rg + r) * D + d);
-            s[r] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s[r]))));
+          for (int j = 0; j < 2; ++j) x[j] = *reinterpret_cast<const float4*>(sK + (t0 + 8 * j) * pitch + d);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float4 y = *reinterpret_cast<const float4*>(sQ + (4 * r + rl) * pitch + d);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) s[j][r] = fmaf(x[j].x, y.x, fmaf(x[j].y, y.y, fmaf(x[j].z, y.z, fmaf(x[j].w, y.w, s[j][r]))));
           }
         }
-        const int node = kv0 + kv - ex.ctx;   // < 0: context
+        float* to = warp >> 2 ? sS1 : sS;
 #pragma unroll
-        for (int r = 0; r < kMine; ++r) {
-          const bool see = kv < nkv && (node < 0 || ((s_mask[rg + r][node >> 5] >> (node & 31)) & 1u));
-          sS[kv * kScorePad + rg + r] = see ? s[r] * p.scale_log2 : -INFINITY;
-        }
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) to[(t0 + 8 * j) * kScorePad + 4 * r + rl] = s[j][r];
       }
       __syncthreads();
       for (int r = warp; r < kRows; r += kThreads / 32) {   // statistics: a row per warp and turn
         float* a = sS + lane * kScorePad + r;
         float* c = sS + (lane + 32) * kScorePad + r;
-        const float x = *a, y = *c;
+        float x = *a, y = *c;
+        if constexpr (kRows != 4) {
+          x = score(x + sS1[lane * kScorePad + r], lane, r);
+          y = score(y + sS1[(lane + 32) * kScorePad + r], lane + 32, r);
+        }
         float m = fmaxf(x, y);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -202,7 +230,8 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
         }
       }
       __syncthreads();
-      {   // weighted sum of V: this warp's tokens, all rows, columns 4 lane + 128 j. A row that must not see a token
+      {   // weighted sum of V: this warp's tokens, all rows, columns 4 lane + 128 j (up to 64 columns: half a warp takes every other
+          // token). A row that must not see a token
           // has weight 0 for it, but 0 x inf is not 0: where a token's values are not finite, such rows skip it.
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
@@ -220,7 +249,7 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
           const int node = kv0 + kv - ex.ctx;
 #pragma unroll
           for (int j = 0; j < kCols; ++j) {
-            const int d = lane * 4 + 128 * j;
+            const int d = col_lane * 4 + 128 * j;
             if (d >= D) continue;
             const float4 x = *reinterpret_cast<const float4*>(sV + kv * pitch + d);
             const bool plain = !decltype(check)::value || node < 0 || (isfinite(x.x) && isfinite(x.y) && isfinite(x.z) && isfinite(x.w));
@@ -235,24 +264,30 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
             }
           }
         };
-        const int first = warp * (kTile / 8);
+        const int first = warp * (kTile / 8);      // tokens behind the sequence have weight 0 and value 0
         if (kv0 + kTile <= ex.ctx) {               // context alone: every row sees every token
 #pragma unroll 2
-          for (int i = 0; i < kTile / 8; ++i) add_token(first + i, std::false_type());
+          for (int i = 0; i < kTile / 8; i += step) add_token(first + i + my_token, std::false_type());
         } else {
-          for (int i = 0; i < min(kTile / 8, nkv - first); ++i) add_token(first + i, std::true_type());
+          for (int i = 0; i < min(kTile / 8, nkv - first); i += step) add_token(first + i + my_token, std::true_type());
         }
       }
     }
 
     // the warps' sums meet over the K and V buffers, which hold 8 x kRows x D floats: each its own place, then all added
     __syncthreads();
+    if (step == 2) {
+#pragma unroll
+      for (int r = 0; r < kRows; ++r)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[r][k] += __shfl_xor_sync(0xffffffffu, acc[r][k], 16);
+    }
 #pragma unroll
     for (int r = 0; r < kRows; ++r)
 #pragma unroll
       for (int j = 0; j < kCols; ++j) {
-        const int d = lane * 4 + 128 * j;
-        if (d < D) store4(sK + (warp * kRows + r) * D + d, &acc[r][4 * j]);
+        const int d = col_lane * 4 + 128 * j;
+        if (d < D && my_token == 0) store4(sK + (warp * kRows + r) * D + d, &acc[r][4 * j]);
       }
     __syncthreads();
     const bool whole = ntiles == tiles;
