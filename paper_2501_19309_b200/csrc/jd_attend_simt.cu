@@ -8,8 +8,8 @@
 // registers, so that one shared-memory read of V serves all rows. The warps' sums meet once per piece of a segment.
 // Two CTAs on an SM, so that one's loads run beside the other's products. float32, B200: 16 sequences of 8,000 tokens, 8 heads of
 // 128, one token each: 260 us, 4.0 TB/s; 8 blocks of 26 nodes, 16 heads on 4 of 128 over 2,000 tokens: 200 us, 17 TFLOP/s, of which
-// 58 % of the issue slots, 50 % of the shared-memory accesses and 36 % of the FMA pipe: what stays is the wait between a tile's
-// four phases with 16 warps on an SM.
+// 58 % of the issue slots, 50 % of the shared-memory accesses and 36 % of the FMA pipe: what stays is shared memory's latency (the
+// largest stall) and the barriers between a tile's four phases, with 16 warps on an SM.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
