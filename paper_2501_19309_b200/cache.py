@@ -8,7 +8,7 @@ One decoding step of a stack of target layers::
         q = cache.append(layer, k, v, tree, rotary=rotary, q=q)  # turn q and k, write k and v
         o = cache.attend(layer, q, tree)["out"]                  # context + the nodes each node may see
     out = verifier.verify(H, draft_tokens, draft_logits, ...)    # accept_len stays on the device
-    cache.commit(out["accept_len"])                              # keep the accepted nodes, drop the rest
+    cache.commit(out["accept_len"])                              # keep the accepted nodes, drop the rest (of a tree: with paths)
 
 Argument marshalling only; every step runs inside the library's kernels.  All calls are enqueued on ``stream`` (default:
 torch's current stream of the cache's device) and none waits for the device, except :meth:`PagedCache.status`.  Outputs that a

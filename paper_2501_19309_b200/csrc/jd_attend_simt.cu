@@ -319,12 +319,13 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
 
 // Joins the partial results of split segments; rows of whole segments are written already.
 // out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i over the parts in order.
-// Block (k, j) takes a few rows of the segments that groups j, j + gridDim.y, .. left unfinished: with up to kJoinFewRows rows in all one
+// Block (k, j) takes a few rows of the j-th segment that a group left unfinished: with up to kJoinFewRows rows in all one
 // row, whose parts its warps take in turn (what the join costs is their latency, and a row of one long sequence has a part
-// from every SM); with more four rows, and a warp for each unless the parts are many. gridDim.y is the number of segments where
-// that is smaller than the number of groups: blocks that find nothing to do cost the join more than its loads (16 us against 6 for
-// 4 trees x 208 rows with a block for every group).
-constexpr int kJoinWarps = 4, kJoinBatch = 8, kJoinFewRows = 32, kJoinFewParts = 32;
+// from every SM); with more four rows, and a warp for each unless the parts are many. With fewer segments than half the groups there is
+// a block for each segment and looks for it: blocks that find nothing to do cost the join more than its loads (16 us against 6 for
+// 4 trees x 208 rows with a block for every group). With more there is a block for each group and knows its place (16 trees x 208
+// rows: the whole call 73 us, 81 with blocks that look).
+constexpr int kJoinWarps = 4, kJoinBatch = 8, kJoinFewRows = 32, kJoinFewParts = 32, kJoinAhead = 5;
 __host__ __device__ constexpr int join_rows(int rows) { return rows <= kJoinFewRows ? 1 : kJoinWarps; }
 
 template <int kCols> struct RowSum {   // kCols: groups of 128 columns
@@ -387,59 +388,77 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendPara
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int D = p.c.head_dim, pitch = D + kPartPad;
   const int block_rows = join_rows(p.rows), first_row = blockIdx.x * block_rows;
-  // this block's groups, a lane each, then those among them that left a segment
-  for (int base_g = blockIdx.y; base_g < p.groups; base_g += 32 * gridDim.y) {
-    const int my_g = base_g + lane * gridDim.y;
-    const int4 mine = my_g < p.groups ? __ldcg(p.split + my_g) : make_int4(-1, 0, 0, 0);
-    for (unsigned left = __ballot_sync(0xffffffffu, mine.x >= 0); left; left &= left - 1) {
-      const int from = __ffs(left) - 1, g0 = base_g + from * gridDim.y;
-      const int b = __shfl_sync(0xffffffffu, mine.x, from), head = __shfl_sync(0xffffffffu, mine.y, from), g1 = __shfl_sync(0xffffffffu, mine.z, from);
-      const int nodes = p.num_nodes ? min(max(__ldcg(p.num_nodes + b), 0), p.T) : p.T;
-      const int rows = min(p.rows, nodes * p.group);
-      auto write = [&](int row, int d, const float* o, float m, float l) {   // columns d .. d + 3
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        const float y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-        const int t = row / p.group, h = head * p.group + row - t * p.group;
-        if (d < D) store4(reinterpret_cast<T*>(p.out + ((int64_t)b * p.T + t) * p.out_stride) + (int64_t)h * D + d, y);
-        if (d == 0 && p.lse) p.lse[((int64_t)b * p.T + t) * p.q_heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
-      };
-      auto place = [&](int row) {
-        const int rb = row / p.rows_per_block, r = row - rb * p.rows_per_block;
-        const float* base = p.part + ((int64_t)rb * 2 * p.part_rows + r) * pitch;
-        return [=](int g) { return base + ((int64_t)g * p.row_blocks * 2 + (g == g0 ? 1 : 0)) * p.part_rows * pitch; };
-      };
-      if (block_rows > 1 && g1 - g0 < kJoinFewParts) {
-        const int row = first_row + warp;
-        if (row >= rows) continue;
-        const RowSum<kCols> s = sum_parts<kCols>(g0, g1, 1, D, lane, place(row));
+  // this block's segment: the one that group blockIdx.y left unfinished, or number blockIdx.y of all those (there are no more than blocks)
+  int b = -1, head = 0, g0 = 0, g1 = 0;
+  if ((int)gridDim.y == p.groups) {
+    const int4 x = __ldcg(p.split + blockIdx.y);
+    b = x.x; head = x.y; g0 = blockIdx.y; g1 = x.z;
+  } else for (int base_g = 0, seen = 0; base_g < p.groups && b < 0; base_g += 32 * kJoinAhead) {
+    int4 mine[kJoinAhead];
 #pragma unroll
-        for (int j = 0; j < kCols; ++j) write(row, 128 * j + lane * 4, s.o[j], s.m, s.l);
-        continue;
+    for (int k = 0; k < kJoinAhead; ++k) {
+      const int g = base_g + 32 * k + lane;
+      mine[k] = g < p.groups ? __ldcg(p.split + g) : make_int4(-1, 0, 0, 0);
+    }
+#pragma unroll
+    for (int k = 0; k < kJoinAhead; ++k) {
+      const unsigned left = __ballot_sync(0xffffffffu, mine[k].x >= 0);
+      const unsigned hit = __ballot_sync(0xffffffffu, mine[k].x >= 0 && seen + __popc(left & ((1u << lane) - 1u)) == (int)blockIdx.y);
+      seen += __popc(left);
+      if (hit) {
+        const int from = __ffs(hit) - 1;
+        b = __shfl_sync(0xffffffffu, mine[k].x, from);
+        head = __shfl_sync(0xffffffffu, mine[k].y, from);
+        g0 = base_g + 32 * k + from;
+        g1 = __shfl_sync(0xffffffffu, mine[k].z, from);
       }
-      for (int row = first_row; row < min(rows, first_row + block_rows); ++row) {
-        const RowSum<kCols> s = sum_parts<kCols>(g0 + warp, g1, kJoinWarps, D, lane, place(row));
-        __syncthreads();   // the last row's sums have been read
+    }
+  }
+  if (b < 0) return;
+  const int nodes = p.num_nodes ? min(max(__ldcg(p.num_nodes + b), 0), p.T) : p.T;
+  const int rows = min(p.rows, nodes * p.group);
+  auto write = [&](int row, int d, const float* o, float m, float l) {   // columns d .. d + 3
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+    const int t = row / p.group, h = head * p.group + row - t * p.group;
+    if (d < D) store4(reinterpret_cast<T*>(p.out + ((int64_t)b * p.T + t) * p.out_stride) + (int64_t)h * D + d, y);
+    if (d == 0 && p.lse) p.lse[((int64_t)b * p.T + t) * p.q_heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+  };
+  auto place = [&](int row) {
+    const int rb = row / p.rows_per_block, r = row - rb * p.rows_per_block;
+    const float* base = p.part + ((int64_t)rb * 2 * p.part_rows + r) * pitch;
+    return [=](int g) { return base + ((int64_t)g * p.row_blocks * 2 + (g == g0 ? 1 : 0)) * p.part_rows * pitch; };
+  };
+  if (block_rows > 1 && g1 - g0 < kJoinFewParts) {
+    const int row = first_row + warp;
+    if (row >= rows) return;
+    const RowSum<kCols> s = sum_parts<kCols>(g0, g1, 1, D, lane, place(row));
 #pragma unroll
-        for (int j = 0; j < kCols; ++j) s_o[warp][j][lane] = make_float4(s.o[j][0], s.o[j][1], s.o[j][2], s.o[j][3]);
-        if (lane == 0) s_ml[warp] = make_float2(s.m, s.l);
-        __syncthreads();
-        if (warp < kCols) {   // columns 128 warp ..
-          float top = -INFINITY;
+    for (int j = 0; j < kCols; ++j) write(row, 128 * j + lane * 4, s.o[j], s.m, s.l);
+    return;
+  }
+  for (int row = first_row; row < min(rows, first_row + block_rows); ++row) {
+    const RowSum<kCols> s = sum_parts<kCols>(g0 + warp, g1, kJoinWarps, D, lane, place(row));
+    __syncthreads();   // the last row's sums have been read
 #pragma unroll
-          for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, s_ml[w].x);
-          const float base = top == -INFINITY ? 0.f : top;
-          float sum = 0.f, y[4] = {};
+    for (int j = 0; j < kCols; ++j) s_o[warp][j][lane] = make_float4(s.o[j][0], s.o[j][1], s.o[j][2], s.o[j][3]);
+    if (lane == 0) s_ml[warp] = make_float2(s.m, s.l);
+    __syncthreads();
+    if (warp < kCols) {   // columns 128 warp ..
+      float top = -INFINITY;
 #pragma unroll
-          for (int w = 0; w < kJoinWarps; ++w) {
-            const float f = exp2f(s_ml[w].x - base);
-            const float4 x = s_o[w][warp][lane];
-            sum += f * s_ml[w].y;
-            if (s_ml[w].x == -INFINITY) continue;
-            y[0] = fmaf(f, x.x, y[0]); y[1] = fmaf(f, x.y, y[1]); y[2] = fmaf(f, x.z, y[2]); y[3] = fmaf(f, x.w, y[3]);
-          }
-          write(row, 128 * warp + lane * 4, y, top, sum);
-        }
+      for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, s_ml[w].x);
+      const float base = top == -INFINITY ? 0.f : top;
+      float sum = 0.f, y[4] = {};
+#pragma unroll
+      for (int w = 0; w < kJoinWarps; ++w) {
+        const float f = exp2f(s_ml[w].x - base);
+        const float4 x = s_o[w][warp][lane];
+        sum += f * s_ml[w].y;
+        if (s_ml[w].x == -INFINITY) continue;
+        y[0] = fmaf(f, x.x, y[0]); y[1] = fmaf(f, x.y, y[1]); y[2] = fmaf(f, x.z, y[2]); y[3] = fmaf(f, x.w, y[3]);
       }
+      write(row, 128 * warp + lane * 4, y, top, sum);
     }
   }
 }
@@ -465,7 +484,8 @@ cudaError_t run_attend_simt(const AttendParams& p, int dtype, cudaStream_t st) {
 
 cudaError_t run_attend_join(const AttendParams& p, int dtype, cudaStream_t st) {
   const int n = join_rows(p.rows);
-  const dim3 grid((unsigned)((p.rows + n - 1) / n), (unsigned)std::min<int64_t>(p.groups, (int64_t)p.B * p.c.kv_heads));
+  const int64_t segments = (int64_t)p.B * p.c.kv_heads;
+  const dim3 grid((unsigned)((p.rows + n - 1) / n), (unsigned)(2 * segments < p.groups ? segments : p.groups));
   auto kernel = dtype == JD_DTYPE_F32 ? (p.c.head_dim <= 128 ? attend_join_kernel<float, 1> : attend_join_kernel<float, 2>)
                                       : (p.c.head_dim <= 128 ? attend_join_kernel<__nv_bfloat16, 1> : attend_join_kernel<__nv_bfloat16, 2>);
   return launch_chained(kernel, grid, dim3(32 * kJoinWarps), 0, st, p);

@@ -647,7 +647,7 @@ jd_status_t jd_cache_attend(jd_cache_t c, const jd_attend_args_t* a, void* cuda_
   p.split = c->split;
   if (tensor) {
     p.tile_shift = kTensorTileShift;
-    p.seg_cost = tensor_seg_cost(g.head_dim);
+    p.seg_cost = tensor_seg_cost(g.head_dim, p.rows);
     p.rows_per_block = p.rows > 128 ? 256 : 128;
   } else {
     p.tile_shift = kSimtTileShift;

@@ -243,8 +243,10 @@ bool attend_configure();   // dynamic shared-memory limits on the current device
 constexpr int kSimtRows = 16, kSimtTileShift = 6, kSimtSegCost = 1;
 constexpr int kTensorTileShift = 7;
 // what beginning and ending a segment costs, in tiles: some 8,000 cycles, against 1,400 (64 columns) or 2,800 (128) for a tile at
-// HBM rate. A batch of 16 chains up to 6,000 tokens long: 63 us at 2, 48 at 6, 51 at 12 (64 columns).
-constexpr int tensor_seg_cost(int head_dim) { return head_dim == 64 ? 6 : 4; }
+// HBM rate. A batch of 16 chains up to 6,000 tokens long: 40 us at 3, 36 at 6, 38 at 10 (64 columns). More than 128 rows: a pair of row
+// tiles takes longer a tile, and its parts are large, so that cutting a segment less often pays too (16 trees of 208 rows on 200 to
+// 4,000 tokens: 101 us at 1, 70 at 4, 66 at 5, 68 at 6).
+constexpr int tensor_seg_cost(int head_dim, int rows) { return head_dim == 64 ? 6 : (rows > 128 ? 5 : 4); }
 
 bool rope_valid(const jd_rope_t& r, int head_dim);
 cudaError_t run_append(const CacheView& c, const jd_append_args_t& a, int q_heads, int dtype, cudaStream_t st);
