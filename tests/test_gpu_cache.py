@@ -798,3 +798,43 @@ def test_two_handles_attend_on_two_streams():
     torch.cuda.synchronize()
     for x, y in outs:
         assert torch.equal(x["out"], want[0]["out"]) and torch.equal(y["out"], want[1]["out"])
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("f32", 64)])
+def test_a_captured_step_with_a_side_stream(dtype, D):
+    """Calls that start early, between branches that part and meet: the same as one after another."""
+    c = L.filled_cache([300, 2000], 8, D=D, dtype=dtype, max_nodes=8, seed=4)
+    q, k, v = (rand((2, 8, h, D), i, dtype) for i, h in enumerate((4, 2, 2)))
+    main, side = torch.cuda.Stream(), torch.cuda.Stream()
+    first, second = ({"out": torch.zeros_like(q)} for _ in range(2))
+    turned, other = torch.zeros_like(q), torch.zeros_like(q)
+
+    def step(branch):
+        torch.add(q, 0, out=turned)
+        c.append(0, k, v)
+        c.attend(0, turned, out=first)
+        if branch:
+            side.wait_stream(main)
+        with torch.cuda.stream(side if branch else main):
+            torch.mul(first["out"], 2, out=other)
+            torch.neg(turned, out=turned)
+        c.append(0, v, k)
+        if branch:
+            main.wait_stream(side)
+        torch.add(other, turned, out=other)
+        c.attend(0, other, out=second)
+
+    torch.cuda.synchronize()
+    with torch.cuda.stream(main):
+        step(False)
+        torch.cuda.synchronize()
+        want = [first["out"].clone(), second["out"].clone()]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=main):
+            step(True)
+        for _ in range(3):
+            first["out"].zero_(), second["out"].zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(first["out"], want[0]) and torch.equal(second["out"], want[1])
+    assert c.status() == jd.JD_OK
