@@ -20,11 +20,11 @@
 // TMA, a box per page and 64 columns, through a ring; one or two more issue the MMAs.
 //
 // What bounds it (B200, 148 SMs):
-//   up to 128 rows   HBM: 16 sequences of 40,000 tokens, 8 kv heads of 128, one token each: 395 us, 6.6 TB/s; heads of 64: 206 us, 6.4 TB/s
+//   up to 128 rows   HBM: 16 sequences of 40,000 tokens, 8 kv heads of 128, one token each: 386 us, 6.8 TB/s; heads of 64: 204 us, 6.4 TB/s
 //   129 rows and up  the chains' own latency: a pair of row tiles takes about 3,450 cycles a tile, of which its products are 2,200 (S: 75
 //                    cycles a step of 16 columns, as Q comes from shared memory again every time; P V: 64), its exponentials
-//                    2,050 on each SM partition and the rest the hand-overs between them; 416 rows over 131,046 tokens: 257 us,
-//                    870 TFLOP/s, at clocks that the power limit holds near 1.5 GHz
+//                    2,050 on each SM partition and the rest the hand-overs between them; 416 rows over 131,046 tokens: 252 us,
+//                    885 TFLOP/s, at clocks that the power limit holds near 1.5 GHz
 //   short contexts   about 8,000 cycles to begin and end a segment
 // Tried and slower: a second pair of softmax warpgroups, half the columns each (275 against 260 us on that case); a quarter of the
 // exponentials as polynomials on the FMA pipe (274); S in halves of 64 tokens with a buffer each, so that the next is ready when
