@@ -18,7 +18,7 @@ LIB = os.path.join(PKG, "libjd_b200.so")
 LIB_STAMPS = os.path.join(PKG, "libjd_b200_stamps.so")
 SOURCES = ["jd_api.cu", "jd_simt.cu", "jd_fused_sm100.cu", "jd_batched_sm100.cu", "jd_static.cu",
            "jd_rope.cu", "jd_cache.cu", "jd_attend_simt.cu", "jd_attend_sm100.cu"]
-HEADERS = ["jd_common.cuh", "jd_kernels.h", "jd_sm100_ptx.cuh", "jd_cache.h"]
+HEADERS = ["jd_common.cuh", "jd_kernels.h", "jd_sm100_ptx.cuh", "jd_cache.h", "jd_path.h"]
 
 
 def _nvcc() -> str:

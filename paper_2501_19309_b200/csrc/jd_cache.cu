@@ -14,6 +14,7 @@
 #include <new>
 
 #include "jd_cache.h"
+#include "jd_path.h"
 
 using namespace jd;
 
@@ -300,9 +301,10 @@ __global__ void __launch_bounds__(kMoveThreads) commit_kernel(CacheView c, const
   __syncthreads();
   if (threadIdx.x < a) {
     const int i = threadIdx.x, node = s_node[i], before = i ? s_node[i - 1] : 0;
-    bool ok = node > before && node < max_nodes && len + node < limit;
+    int from, to;
+    bool ok = path_entries(len, limit, i, node, before, max_nodes, c.page_shift, &from, &to);
     if (ok) {
-      const int fp = table[(len + node) >> c.page_shift], tp = table[(len + 1 + i) >> c.page_shift];
+      const int fp = table[from], tp = table[to];
       ok = fp >= 0 && fp < c.pages && tp >= 0 && tp < c.pages;
       if (ok) ok = (c.refs[fp] <= 1) & (c.refs[tp] <= 1);
       const int mask = c.page_size - 1;

@@ -303,3 +303,49 @@ def test_model_leaves_rows_of_shared_pages_alone():
     m.truncate([1], [0])
     m.commit([[1]], np.array([[[2]]]), [0])           # would move row 3 over row 2 of sequence 1
     assert m.status == O.BAD_INDEX and m.len.tolist() == [1, 4] and m.k[0, 0, 0, :4, 0].tolist() == [0, 1, 2, 3]
+
+
+PATH_HARNESS = r"""
+#include <stdio.h>
+#include <stdlib.h>
+#include "jd_path.h"
+int main(int argc, char** argv) {
+  const int len = atoi(argv[1]), limit = atoi(argv[2]), max_nodes = atoi(argv[3]), shift = atoi(argv[4]);
+  for (int i = 0, before = 0; i + 5 < argc; ++i) {
+    const int node = atoi(argv[5 + i]);
+    int from = 0, to = 0;
+    const bool ok = jd::path_entries(len, limit, i, node, before, max_nodes, shift, &from, &to);
+    printf("%d %d %d\n", (int)ok, from, to);
+    before = node;
+  }
+}
+"""
+
+
+def test_no_node_of_a_path_leads_out_of_the_page_table(tmp_path):
+    """A commit judges all nodes of a path at once, those behind a cut too: whatever stands there, a node that passes goes from and
+    to entries of pages that the sequence holds, and up to the first that does not pass the answers are the definition's."""
+    import shutil
+    import subprocess
+    if shutil.which("g++") is None:
+        pytest.skip("g++ is not installed")
+    (tmp_path / "p.cpp").write_text(PATH_HARNESS)
+    csrc = os.path.join(ROOT, "paper_2501_19309_b200", "csrc")
+    subprocess.run(["g++", "-std=c++17", "-I", csrc, str(tmp_path / "p.cpp"), "-o", str(tmp_path / "p")], check=True)
+    rng = np.random.default_rng(0)
+    far = 2 ** 31
+    cases = [(0, 1, [-5, -3]), (0, 1, [-far, -far + 1]), (29, 4, [7, 1, 2]), (28, 4, [9, 1, 2, 3]), (5, 2, [1, 2, 3, 0, 1]), (0, 0, [1, 2]), (8, 1, [1, 2]),
+             (0, 3, [far - 1, -far, -1, 0, 1, 2])]
+    for _ in range(60):
+        held = int(rng.integers(0, 4))
+        cases.append((int(rng.integers(0, 8 * held + 1)), held, rng.integers(-4, 12, int(rng.integers(1, 9))).tolist()))
+    for length, held, path in cases:
+        text = subprocess.run([str(tmp_path / "p"), str(length), str(8 * held), "10", "3", *map(str, path)], capture_output=True, text=True,
+                              check=True).stdout
+        before, cut = 0, False
+        for i, (node, line) in enumerate(zip(path, text.splitlines())):
+            ok, at, to = map(int, line.split())
+            assert not ok or (0 <= at < held and 0 <= to < held), (length, held, path, i)
+            if not cut:
+                assert ok == (before < node < 10 and length + node < 8 * held), (length, held, path, i)
+            cut, before = cut or not ok, node

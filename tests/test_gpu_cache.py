@@ -838,3 +838,28 @@ def test_a_captured_step_with_a_side_stream(dtype, D):
             torch.cuda.synchronize()
             assert torch.equal(first["out"], want[0]) and torch.equal(second["out"], want[1])
     assert c.status() == jd.JD_OK
+
+
+@pytest.mark.parametrize("layers,H,D", [(1, 1, 8), (3, 2, 64)])
+def test_commit_of_paths_with_several_bad_nodes(layers, H, D):
+    """Nodes behind a cut count for nothing, whatever they say: negative ones in a row, a row that falls and rises again, tables used to
+    their last entry."""
+    per_seq, page, T = 2, 8, 8
+    paths = [[-5, -3, -1], [7, 1, 2], [1, 3, 2], [-1, 0, 2], [2, 1, 3], [9, 10, 11], [2, 2, 3], [1, 2, 4]]
+    for room in (1, 3, 8):
+        for order in (paths, paths[::-1]):
+            B = len(order)
+            c = L.empty_cache(layers, B * per_seq + 2, page, H, H, D, B, per_seq, T, fill=room)
+            c.reserve(per_seq * page)
+            c.commit(L.ints([6] * B), path_len=6)                              # 7 tokens
+            c.reserve(per_seq * page - 7)
+            if page * per_seq - room > 7:
+                c.commit(L.ints([min(page * per_seq - room - 8, 7)] * B), path_len=7)
+                c.reserve(room)
+            assert c.status() == jd.JD_OK and bool((c.held == per_seq).all())
+            m = L.model_of(c)
+            chosen = c.commit(L.ints([[3]] * B), L.ints([[p] for p in order]))
+            m.commit([[3]] * B, np.array([[p] for p in order]), list(range(B)))
+            assert c.status() == jd.JD_ERR_BAD_INDEX and m.status == O.BAD_INDEX and bool((chosen == 0).all())
+            L.same_books(c, m)
+            assert np.array_equal(L.f64(c.k), m.k) and np.array_equal(L.f64(c.v), m.v)
