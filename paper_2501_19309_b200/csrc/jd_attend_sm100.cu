@@ -62,20 +62,25 @@ template <int D, int kMode> struct Shape {
   static constexpr int kQTiles = kPair ? 2 : 1;
   static constexpr int kStageCols = D / 4;                     // columns of O that the copies' sums go through shared memory by
   static constexpr int kStageBytes = kCopies > 1 ? 2 * 128 * kStageCols * 4 : 0;
+  // Q of the next piece is fetched while this one ends, where the registers are there for it: 256 rows of 128 columns are 64 a thread.
+  static constexpr bool kFetchAhead = !kPair || D == 64;
+  // What is kept of a piece (Shared::PerPiece): this one's and the next's. With every tile for both chains and Q fetched ahead a warpgroup
+  // can be through with a short piece while the other still writes the one before it out, and hands over the one behind: three.
+  static constexpr int kPieces = kPair && kFetchAhead ? 3 : 2;
 };
 
-struct Shared {
+template <int kPieces> struct Shared {
   uint64_t full[8], empty[8];
   uint64_t s_full[2], p_ready[2][2], o_done[2], q_ready[2];   // p_ready: first and second 64 columns of P
   uint32_t tmem_base;
   int abort_flag;
   int warp_sums[kThreads / 32];
-  struct PerPiece {                      // of a piece, and of the next one, which begins while this one is written out
+  struct PerPiece {                      // of a piece, and of the next ones, which begin while this one is written out
     uint32_t node_mask[kMaxNodes][kMaxNodes / 32];
     float ml[2][kTile][2];               // m and l of the two chains
     float inv[2][kTile / 2];             // 1 / l of a row, for the threads that put its copies together
     int odd_values;                      // nodes hold values that are not finite
-  } piece[2];
+  } piece[kPieces];
   int prefix[kMaxCacheBatch + 1];
   SeqExtent extents[kMaxCacheBatch];
 };
@@ -83,7 +88,7 @@ struct Shared {
 template <int D, int kMode>
 constexpr size_t attend_smem() {
   using S = Shape<D, kMode>;
-  return 1024 + (sizeof(Shared) + 1023) / 1024 * 1024 + (size_t)(S::kStages + S::kQTiles) * S::kTileBytes + S::kStageBytes;
+  return 1024 + (sizeof(Shared<S::kPieces>) + 1023) / 1024 * 1024 + (size_t)(S::kStages + S::kQTiles) * S::kTileBytes + S::kStageBytes;
 }
 
 // Bounded wait that gives up as soon as another role has.
@@ -222,8 +227,9 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   constexpr int kStages = Sh::kStages, kChunks = Sh::kChunks, kChunkBytes = Sh::kChunkBytes, kTileBytes = Sh::kTileBytes;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  Shared& sh = *reinterpret_cast<Shared*>(smem);
-  uint8_t* q_smem = smem + (sizeof(Shared) + 1023) / 1024 * 1024;
+  using Shm = Shared<Sh::kPieces>;
+  Shm& sh = *reinterpret_cast<Shm*>(smem);
+  uint8_t* q_smem = smem + (sizeof(Shm) + 1023) / 1024 * 1024;
   uint8_t* ring = q_smem + Sh::kQTiles * kTileBytes;
   uint8_t* stage_smem = ring + kStages * kTileBytes;
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
@@ -460,11 +466,12 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         mask_regs[i] = t < nodes ? node_word(p, y.b, t, k, nodes) : 0u;
       }
     };
-    // ahead of time where the registers are there for it: 256 rows of 128 columns are 64 registers a thread
-    constexpr bool kFetchAhead = kQLoads <= 8;
-    int parity = 0;
+    constexpr bool kFetchAhead = Sh::kFetchAhead;
+    static_assert(!kFetchAhead || kQLoads <= 8, "registers");
+    int now = 0;                                     // this piece's place in sh.piece, and the next one's
+    auto behind = [&]() { return now + 1 == Sh::kPieces ? 0 : now + 1; };
     // the fetched piece's masks and Q to shared memory, and the word to the chains that have tiles in it: no other waits for it
-    auto hand_over = [&](const Piece& y, Shared::PerPiece& to) {
+    auto hand_over = [&](const Piece& y, typename Shm::PerPiece& to) {
 #pragma unroll
       for (int i = 0; i < kMaskLoads; ++i) {
         const int at = tid + i * 256, t = at / p.W;
@@ -494,7 +501,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     }
     while (x.tiles > 0) {
       const SeqExtent ex = sh.extents[x.b];
-      Shared::PerPiece& mine = sh.piece[parity];
+      typename Shm::PerPiece& mine = sh.piece[now];
       float m = -INFINITY, l = 0.f;
       int done = 0;                                  // tiles of this piece that this warpgroup has taken
       for (int t = kPair ? 0 : w; t < x.tiles; t += kPair ? 1 : 2, ++done) {
@@ -640,7 +647,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         softmax_sync();
         tc_fence_after();
       }
-      if (kFetchAhead && next.tiles > 0) hand_over(next, sh.piece[parity ^ 1]);
+      if (kFetchAhead && next.tiles > 0) hand_over(next, sh.piece[behind()]);
       if constexpr (!kPair) {
         const float m0 = mine.ml[0][r][0], m1 = mine.ml[1][r][0];
         m = -INFINITY;
@@ -759,11 +766,11 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       if constexpr (!kPair) softmax_sync();          // both warpgroups have read both chains' O, which the next piece's first products overwrite
       if (!kFetchAhead && next.tiles > 0) {
         fetch(next);
-        hand_over(next, sh.piece[parity ^ 1]);
+        hand_over(next, sh.piece[behind()]);
       }
       tile_count += x.tiles;
       x = next;
-      parity ^= 1;
+      now = behind();
     }
   }
 

@@ -863,3 +863,32 @@ def test_commit_of_paths_with_several_bad_nodes(layers, H, D):
             assert c.status() == jd.JD_ERR_BAD_INDEX and m.status == O.BAD_INDEX and bool((chosen == 0).all())
             L.same_books(c, m)
             assert np.array_equal(L.f64(c.k), m.k) and np.array_equal(L.f64(c.v), m.v)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("T,group", [(26, 8), (26, 16), (12, 8), (12, 4), (6, 4)])
+def test_values_that_are_not_finite_in_pieces_that_follow_one_another(D, T, group):
+    """A CTA's pieces are of sequences with trees and node counts of their own, most of them a tile long; in every third sequence
+    a node's value is infinite. Each row gets the infinities of the nodes that it sees, and no others."""
+    B = 600
+    rng = np.random.default_rng(T)
+    lens = [int(x) for x in rng.integers(0, 100, B)]
+    c = L.filled_cache(lens, T, page=16, q_heads=group, kv_heads=1, D=D, max_nodes=T, seed=1)
+    parents = [L.random_tree(T, rng, ("chain", "star", "star")[b % 3]) for b in range(B)]
+    count = [(T, 1, T)[b % 3] for b in range(B)]
+    tree = L.device_tree(parents, num_nodes=L.ints(count))
+    q = rand((B, T, group, D), 2)
+    clean = c.attend(0, q, tree)["out"].float()
+    at = torch.tensor(lens)[::3] + 3                          # node 3 of sequences 0, 3, ..
+    page, row = c.page_table[::3].cpu()[torch.arange(len(at)), at // 16].long().cuda(), (at % 16).cuda()
+    c.v[0, page, 0, row, 5] = float("inf")
+    c.v[0, page, 0, row, D - 1] = float("-inf")
+    alive = (torch.arange(T)[None, :] < torch.tensor(count)[:, None]).cuda()
+    want = clean.clone()
+    want[::3, 3:, :, 5] = float("inf")                       # of a chain, every node from 3 on sees node 3
+    want[::3, 3:, :, D - 1] = float("-inf")
+    for _ in range(20):
+        got = c.attend(0, q, tree)["out"].float()
+        same = (got == want)[alive]
+        assert bool(same.all()), int((~same).sum())
+    assert c.status() == jd.JD_OK
