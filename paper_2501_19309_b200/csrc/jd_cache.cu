@@ -109,23 +109,23 @@ __global__ void __launch_bounds__(256) fork_kernel(CacheView c, int n, const int
   if (threadIdx.x == 0) { c.seq_len[d] = len; c.held[d] = keep; }
 }
 
-// Exclusive prefix sum of one int per thread over a block of kBookThreads; total in *all.
-__device__ __forceinline__ int block_exclusive(int v, int* warp_sums, int* all) {
+// Exclusive prefix sum of one number per thread over a block of kBookThreads; total in *all.
+__device__ __forceinline__ uint32_t block_exclusive(uint32_t v, uint32_t* warp_sums, uint32_t* all) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int x = v;
+  uint32_t x = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
     if (lane >= o) x += y;
   }
   __syncthreads();
   if (lane == 31) warp_sums[warp] = x;
   __syncthreads();
   if (warp == 0) {
-    int w = warp_sums[lane];
+    uint32_t w = warp_sums[lane];
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, w, o);
+      const uint32_t y = __shfl_up_sync(0xffffffffu, w, o);
       if (lane >= o) w += y;
     }
     warp_sums[lane] = w;
@@ -158,8 +158,9 @@ __device__ __forceinline__ void copy_rows_of_page(const CacheView& c, int from, 
 // the bitmap's words), copies its share of the rows, and counts itself done; the last one done writes the new state, which
 // nobody reads any more. page_list[k] = the k-th page handed out; all blocks write the same.
 __global__ void __launch_bounds__(kBookThreads) reserve_kernel(CacheView c, int B, const int32_t* slots, int n, int* page_list, int* blocks_done) {
-  __shared__ int s_slot[kMaxCacheBatch], s_last[kMaxCacheBatch], s_off[kMaxCacheBatch], s_first[kMaxCacheBatch], warp_sums[32];
+  __shared__ int s_slot[kMaxCacheBatch], s_last[kMaxCacheBatch], s_off[kMaxCacheBatch], s_first[kMaxCacheBatch];
   __shared__ int s_rows[kMaxCacheBatch];   // rows to copy, 0: none
+  __shared__ uint32_t warp_sums[32];
   __shared__ int fail, last_one;
   pdl_wait();
   pdl_trigger();
@@ -198,14 +199,15 @@ __global__ void __launch_bounds__(kBookThreads) reserve_kernel(CacheView c, int 
     copy = owners > 1;
   }
   const int need = slot >= 0 ? (want - held) + (copy ? 1 : 0) : 0;
-  int total, available;
-  const int off = block_exclusive(need, warp_sums, &total);
+  uint32_t all_pages, available;   // 1024 sequences may ask for 2^21 + 1 pages each, which 32 bits hold and 31 do not
+  const int off = block_exclusive(need, warp_sums, &all_pages);
   const int words = (c.pages + 31) >> 5, per = (words + kBookThreads - 1) / kBookThreads;
   const int w0 = min(b * per, words), w1 = min(w0 + per, words);
   int mine = 0;
   for (int w = w0; w < w1; ++w) mine += __popc(free_word(c, w));
   const int first = block_exclusive(mine, warp_sums, &available);
-  const bool ok = !fail && total <= available;   // else nothing changes
+  const bool ok = !fail && all_pages <= available;   // else nothing changes
+  const int total = ok ? (int)all_pages : 0;
   if (!ok && b == 0) set_status(c.status, JD_ERR_PAGES);
   if (ok) {
     int rank = first;
@@ -365,7 +367,7 @@ __global__ void __launch_bounds__(kMoveThreads) commit_kernel(CacheView c, const
 // The owner counts and the bitmap follow; map[p] = new number of page p.
 __global__ void __launch_bounds__(kBookThreads) compact_plan_kernel(CacheView c, int* map, int* move_src, int* move_dst, int* move_cnt,
                                                                     int32_t* used_out) {
-  __shared__ int warp_sums[32];
+  __shared__ uint32_t warp_sums[32];
   pdl_wait();
   pdl_trigger();
   const int t = threadIdx.x, words = (c.pages + 31) >> 5, per = (words + kBookThreads - 1) / kBookThreads;
@@ -374,10 +376,11 @@ __global__ void __launch_bounds__(kBookThreads) compact_plan_kernel(CacheView c,
     const int left = c.pages - 32 * w;
     return ~c.free_bits[w] & (left >= 32 ? 0xFFFFFFFFu : (1u << left) - 1u);
   };
-  int mine = 0, used;
+  uint32_t mine = 0, all_used, all_holes, all_movers;
   for (int w = w0; w < w1; ++w) mine += __popc(used_bits(w));
-  block_exclusive(mine, warp_sums, &used);
-  int holes = 0, movers = 0, all_holes, all_movers;
+  block_exclusive(mine, warp_sums, &all_used);
+  const int used = (int)all_used;
+  int holes = 0, movers = 0;
   for (int w = w0; w < w1; ++w) {
     const uint32_t u = used_bits(w);
     const int below = min(max(used - 32 * w, 0), 32);          // pages of this word with numbers < used
@@ -397,7 +400,7 @@ __global__ void __launch_bounds__(kBookThreads) compact_plan_kernel(CacheView c,
     }
   }
   __syncthreads();
-  for (int k = t; k < all_movers; k += kBookThreads) {
+  for (int k = t; k < (int)all_movers; k += kBookThreads) {
     const int s = move_src[k], d = move_dst[k];
     map[s] = d;
     c.refs[d] = c.refs[s];

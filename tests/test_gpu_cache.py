@@ -892,3 +892,13 @@ def test_values_that_are_not_finite_in_pieces_that_follow_one_another(D, T, grou
         same = (got == want)[alive]
         assert bool(same.all()), int((~same).sum())
     assert c.status() == jd.JD_OK
+
+
+def test_a_reserve_of_two_to_the_31_pages_is_refused():
+    """1024 sequences that ask for 2^21 pages each: the sum does not fit 31 bits."""
+    c = jd.PagedCache.allocate(1, 16, 8, 1, 1, 8, 1024, 1 << 21, 4)
+    c.reserve(1 << 24)
+    assert c.status() == jd.JD_ERR_PAGES and bool((c.held == 0).all()) and bool((c.refs == 0).all())
+    c.reserve(8, L.ints([1000, 3]))
+    assert c.status() == jd.JD_OK and c.page_table[[1000, 3], 0].cpu().tolist() == [0, 1]
+    c.close()
