@@ -159,7 +159,7 @@ class Cache:
         return chosen
 
     def fork(self, src, dst):
-        used, srcs = set(), {int(s) for s in src}
+        used, srcs = set(), {int(s) for s, d in zip(src, dst) if int(d) != -1}
         for s, d in zip(map(int, src), map(int, dst)):
             if s == -1 or d == -1:
                 continue

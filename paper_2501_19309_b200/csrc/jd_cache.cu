@@ -89,8 +89,10 @@ __global__ void __launch_bounds__(256) fork_kernel(CacheView c, int n, const int
   if (threadIdx.x == 0) flag = s < 0 || s >= c.max_seqs || d < 0 || d >= c.max_seqs;
   __syncthreads();
   if (!flag)
-    for (int j = threadIdx.x; j < n; j += blockDim.x)
-      if (__ldcg(src + j) == d || (j < i && __ldcg(dst + j) == d && __ldcg(src + j) != -1)) flag = 1;
+    for (int j = threadIdx.x; j < n; j += blockDim.x) {
+      const int sj = __ldcg(src + j), dj = __ldcg(dst + j);
+      if (sj != -1 && dj != -1 && (sj == d || (j < i && dj == d))) flag = 1;   // padding entries name nothing
+    }
   __syncthreads();
   if (!flag && threadIdx.x == 0 && (c.held[d] != 0 || c.seq_len[d] != 0)) flag = 1;
   __syncthreads();

@@ -349,3 +349,11 @@ def test_no_node_of_a_path_leads_out_of_the_page_table(tmp_path):
             if not cut:
                 assert ok == (before < node < 10 and length + node < 8 * held), (length, held, path, i)
             cut, before = cut or not ok, node
+
+
+def test_model_takes_no_names_from_padding_entries_of_a_fork():
+    m = model(seqs=6)
+    m.reserve(3, [0])
+    m.commit([2], None, [0], 3)
+    m.fork([4, 0, -1, 0, 0, -1], [-1, 4, 2, 2, 5, 3])
+    assert m.status == O.OK and m.len.tolist() == [3, 0, 3, 0, 3, 3] and m.refs[0] == 4

@@ -902,3 +902,16 @@ def test_a_reserve_of_two_to_the_31_pages_is_refused():
     c.reserve(8, L.ints([1000, 3]))
     assert c.status() == jd.JD_OK and c.page_table[[1000, 3], 0].cpu().tolist() == [0, 1]
     c.close()
+
+
+def test_padding_entries_of_a_fork_name_nothing():
+    """An entry with -1 on either side is no source and no target for the others."""
+    c = L.empty_cache(1, 8, 8, 1, 1, 8, 6, 4, 4)
+    c.reserve(4, L.ints([0]))
+    c.commit(L.ints([2]), slots=L.ints([0]), path_len=3)
+    m = L.model_of(c)
+    src, dst = [4, 0, -1, 0, 0, -1], [-1, 4, 2, 2, 5, 3]
+    c.fork(L.ints(src), L.ints(dst)), m.fork(src, dst)
+    assert c.status() == jd.JD_OK and m.status == O.OK
+    assert c.seq_len.cpu().tolist() == [3, 0, 3, 0, 3, 3] and int(c.refs[0]) == 4
+    L.same_books(c, m)
