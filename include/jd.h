@@ -311,8 +311,8 @@ typedef enum { JD_ROPE_HALF = 0, JD_ROPE_INTERLEAVED = 1 } jd_rope_layout_t;
  *         original_len / low divided by `factor`, and linearly blended in between (in turns per
  *         original_len).
  * YARN:   the same blend along the index i, between the indices whose frequencies make `high` and
- *         `low` turns in original_len (rounded down and up), and the outputs are multiplied by
- *         0.1 ln(factor) + 1. */
+ *         `low` turns in original_len (rounded down and up, kept to 0..rot_dim - 1: the upper one
+ *         may lie behind the last index), and the outputs are multiplied by 0.1 ln(factor) + 1. */
 typedef enum { JD_ROPE_SCALE_NONE = 0, JD_ROPE_SCALE_LINEAR = 1, JD_ROPE_SCALE_BANDS = 2, JD_ROPE_SCALE_YARN = 3 } jd_rope_scaling_t;
 
 /* HOST helper: writes the rot_dim / 2 frequencies (HOST array) and the amplitude (HOST, may be NULL).

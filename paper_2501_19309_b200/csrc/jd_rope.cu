@@ -299,7 +299,7 @@ jd_status_t jd_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, d
   double first = 0.0, last = 0.0;
   if (scaling == JD_ROPE_SCALE_YARN) {
     first = std::fmax(std::floor(index_of(high)), 0.0);
-    last = std::fmin(std::ceil(index_of(low)), half - 1.0);
+    last = std::fmin(std::ceil(index_of(low)), rot_dim - 1.0);   // may lie behind the last index, half - 1: the blend then ends part of the way
     if (last <= first) last = first + 0.001;
   }
   for (int i = 0; i < half; ++i) {

@@ -357,3 +357,18 @@ def test_model_takes_no_names_from_padding_entries_of_a_fork():
     m.commit([2], None, [0], 3)
     m.fork([4, 0, -1, 0, 0, -1], [-1, 4, 2, 2, 5, 3])
     assert m.status == O.OK and m.len.tolist() == [3, 0, 3, 0, 3, 3] and m.refs[0] == 4
+
+
+@pytest.mark.parametrize("rot,base,old,factor,low,high", [(128, 1e4, 65536.0, 4.0, 1.0, 32.0), (128, 1e4, 131072.0, 4.0, 1.0, 32.0), (64, 1e4, 1e6, 8.0, 1.0, 32.0),
+                                                          (32, 100.0, 4096.0, 16.0, 2.0, 8.0), (8, 10.0, 1e9, 2.0, 1.0, 4.0), (128, 5e5, 8192.0, 8.0, 1.0, 32.0)])
+def test_yarn_blend_runs_past_the_last_frequency(rot, base, old, factor, low, high):
+    """From the definition: index x makes old x base^(-2 x / rot) / 2 pi turns; kept up to where that is `high` (rounded down), divided from
+    where it is `low` (rounded up, rot - 1 at most), also where that lies behind the last of the rot / 2 indices."""
+    f0 = base ** (-np.arange(0, rot, 2) / rot)
+    turns = lambda x: old * base ** (-2 * x / rot) / (2 * math.pi)   # noqa: E731
+    first = max([x for x in range(0, 40 * rot) if turns(x) >= high], default=0)
+    last = min(min(x for x in range(0, 40 * rot) if turns(x) <= low), rot - 1)
+    divided = np.clip((np.arange(rot // 2) - first) / (last - first if last > first else 0.001), 0, 1)
+    got, amp = jd.rope_frequencies(rot, base, "yarn", factor, old, low, high)
+    want = f0 * (1 - divided) + f0 / factor * divided
+    assert (np.abs(got.numpy().astype(np.float64) - want) <= 2.0 ** -23 * (1 + 1e-9) * want).all() and abs(amp - (0.1 * math.log(factor) + 1)) < 1e-6
