@@ -44,6 +44,11 @@ constexpr int kThreads = 384;                  // warps 0-3, 4-7: softmax; 8, 10
 constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;   // 2 x 128 x 216 + 128 x 72 = 384 x 168, what the block is launched with
 constexpr float kLazy = 8.f;                   // log2 of how far a maximum may grow before O is rescaled
 
+// 2^(s c - base) with base = m c rounded is off by 2^(2^-24 base) in all weights of a row alike, which the sum divides out again as long as
+// float32 holds it. From this base on neighbouring float32 scores are 16 and more apart, so that a weight is 1 or next to nothing, any
+// factor not below c tells which, and with the next power of two base is exact.
+constexpr float kFar = 0x1p28f;
+
 // How a CTA's rows lie in the 128 rows of an MMA. kPairMode: up to 256 rows, two MMAs, every tile for both chains. Else up to 128 / kMode rows,
 // kMode times over: the copies weigh a kMode-th of a tile's columns each and have zeroes for the rest of P, so that few rows
 // keep all four SM partitions' exponential units busy instead of one; their O, m and l are parts that meet at the end.
@@ -423,6 +428,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     const bool warp_live = my_row - lane < p.rows;
     const int t_node = my_row / p.group, gq = my_row - t_node * p.group;
     const float c2 = p.scale_log2;
+    const float c2_far = __uint_as_float((__float_as_uint(c2) + 0x7FFFFFu) & 0xFF800000u);
     uint32_t s_phase = 0, o_phase = 0;
     int tile_count = 0;                              // tiles of the run in front of this piece
     // A piece's Q rows and mask words, fetched while the piece before it ends: a thread keeps its place within a row of Q
@@ -590,8 +596,15 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             l *= f;
           }
           m = m_new;
-          const float base = m == -INFINITY ? 0.f : m * c2;
-          const uint64_t c2_2 = pack2(c2, c2), base_2 = pack2(-base, -base);
+          float base = m == -INFINITY ? 0.f : m * c2;
+          uint64_t c2_2 = pack2(c2, c2);
+          const bool far = fabsf(base) >= kFar;
+          if (__any_sync(0xffffffffu, far)) {
+            const float c2_row = far ? c2_far : c2;
+            base = m == -INFINITY ? 0.f : m * c2_row;
+            c2_2 = pack2(c2_row, c2_row);
+          }
+          const uint64_t base_2 = pack2(-base, -base);
           uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
           for (int k = 0; k < kCols / 32; ++k) {

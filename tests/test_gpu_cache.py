@@ -915,3 +915,38 @@ def test_padding_entries_of_a_fork_name_nothing():
     assert c.status() == jd.JD_OK and m.status == O.OK
     assert c.seq_len.cpu().tolist() == [3, 0, 3, 0, 3, 3] and int(c.refs[0]) == 4
     L.same_books(c, m)
+
+
+FORMS = [(12, 2), (20, 2), (25, 4), (26, 8), (52, 8)]     # nodes x query heads of a kv head: 24, 40, 100, 208, 416 rows
+
+
+@pytest.mark.parametrize("variant,dtype,D", VARIANTS)
+@pytest.mark.parametrize("T,group", [(1, 1)] + FORMS)
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_scores_of_many_billions(variant, dtype, D, T, group, sign):
+    """One key so far above the others (or all but one so far below) that its weight is 1: the output is its value, the logarithm of the
+    sum its score, whose size alone must not spoil either."""
+    lens = [300, 5, 1000]
+    c = L.filled_cache(lens, T, q_heads=2 * group, D=D, dtype=dtype, max_nodes=T, seed=5)
+    q = torch.full((3, T, 2 * group, D), 1.171875 * 2.0 ** 15, device="cuda").to(L.DT[dtype])        # whole multiples of a power of two
+    best = [77, 0, 640]
+    if sign > 0:
+        c.k.fill_(1.0)
+    else:
+        c.k.fill_(-1.328125 * 2.0 ** 20)
+    want = torch.empty_like(q)
+    for s, token in enumerate(best):
+        page, row = int(c.page_table[s, token // 16]), token % 16
+        c.k[0, page, :, row] = 1.328125 * 2.0 ** 20 if sign > 0 else -1.0
+        for h in range(2):
+            want[s, :, h * group:(h + 1) * group] = c.v[0, page, h, row]
+    scale = D ** -0.5
+    top = D * scale * 1.171875 * 2.0 ** 15 * (1.328125 * 2.0 ** 20 if sign > 0 else -1.0)
+    got = c.attend(0, q, variant=variant)
+    # D sums, the scale and log2 e, there and back: each off by 2^-24 of the score, which is far from any other
+    assert bool(((got["lse"].double() - top).abs() <= (D + 6) * 2.0 ** -24 * abs(top)).all())
+    if variant == "simt":
+        assert torch.equal(got["out"], want)
+    else:      # the weight, 2^(s c2 - base) with base rounded, is near 1; it is rounded to bf16 for the product and not for the sum: 2^-8, and 2^-8 for the output
+        assert bool(((got["out"].double() - want.double()).abs() <= (2.0 ** -7 + 2.0 ** -15) * want.double().abs()).all())
+    assert c.status() == jd.JD_OK
