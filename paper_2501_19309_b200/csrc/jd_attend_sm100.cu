@@ -681,24 +681,42 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       const float inv = !whole ? 1.f : (l == 0.f ? 0.f : 1.f / l);
       const bool odd = *reinterpret_cast<volatile int*>(&mine.odd_values) != 0;
       float* part0 = p.part + (((int64_t)blockIdx.x * 2 + (x.tile0 == 0 ? 1 : 0)) * p.part_rows - r0) * (D + kPartPad);
-      // kN elements of a query row from column c: back to a part, or out
-      auto write = [&](auto count, int row, int c, float* o, float factor) {
+      // kN elements of a query row from column c: back to a part, or out. With copies, an element that is no number while the row's
+      // sum is one has met an infinity of V: one copy's weight makes it that infinity, the others' zeroes make it NaN.
+      auto write = [&](auto count, int row, int c, float* o, float factor, bool sum_ok) {
         constexpr int kN = decltype(count)::value;
         const int t = row / p.group, h = x.head * p.group + row - t * p.group;
         if (row >= p.rows || t >= ex.nodes) return;
-        if (odd) {                                   // values of this piece's nodes that are not finite, to the rows that see them
-          for (int j = 0; j < ex.nodes; ++j) {
-            const int kv = ex.ctx + j;
-            if (kv < x.tile0 * kTile || kv >= (x.tile0 + x.tiles) * kTile || kv >= ex.kv_end || !((mine.node_mask[t][j >> 5] >> (j & 31)) & 1u)) continue;
+        bool lost = false;
+        if constexpr (kCopies > 1) {
+#pragma unroll
+          for (int i = 0; i < kN; ++i) lost |= isnan(o[i]);
+          lost &= sum_ok;
+        }
+        if (odd || lost) {
+          // The values that are not finite, of this piece's nodes (taken out of V) or of all its tokens, to the rows that see them. What is finite does
+          // not count beside them.
+          float sum[kN] = {};
+          const int end = min((x.tile0 + x.tiles) * kTile, ex.kv_end);
+          for (int kv = max(x.tile0 * kTile, lost ? 0 : ex.ctx); kv < end; ++kv) {
+            const int j = kv - ex.ctx;
+            if (j >= 0 && !((mine.node_mask[t][j >> 5] >> (j & 31)) & 1u)) continue;
             const int page = p.c.table[(int64_t)ex.slot * p.c.max_pages + (kv >> p.c.page_shift)];
             if (page < 0 || page >= p.c.pages) continue;
             const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(p.c.v) + page_row(p.c, p.layer, page, x.head, kv & (p.c.page_size - 1)) * D + c;
 #pragma unroll
             for (int i = 0; i < kN; ++i) {
               const float y = __bfloat162float(v[i]);
-              if (!isfinite(y)) o[i] += y;
+              if (!isfinite(y)) sum[i] += y;
             }
+            bool settled = !odd;                     // nothing changes a NaN
+#pragma unroll
+            for (int i = 0; i < kN; ++i) settled &= isnan(sum[i]) || !isnan(o[i]);
+            if (settled) break;
           }
+#pragma unroll
+          for (int i = 0; i < kN; ++i)
+            if (sum[i] != 0.f) o[i] = lost && isnan(o[i]) ? sum[i] : o[i] + sum[i];
         }
         if (whole) {
           uint2* out = reinterpret_cast<uint2*>(p.out + ((int64_t)x.b * p.T + t) * p.out_stride + ((int64_t)h * D + c) * 2);
@@ -732,7 +750,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           for (int c = c_begin; c < c_end; c += 16) {
             float o[16];
             read_o(c, o);
-            write(std::integral_constant<int, 16>(), my_row, c, o, inv);
+            write(std::integral_constant<int, 16>(), my_row, c, o, inv, true);
           }
         }
       } else {
@@ -762,7 +780,8 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
               const float4 v = *place(k * kCopyRows + row, q);
               y[0] += v.x; y[1] += v.y; y[2] += v.z; y[3] += v.w;
             }
-            write(std::integral_constant<int, 4>(), r0 + row, c + q * 4, y, whole ? mine.inv[w][row] : 1.f);
+            const float by = mine.inv[w][row];
+            write(std::integral_constant<int, 4>(), r0 + row, c + q * 4, y, whole ? by : 1.f, !isnan(by));
           }
           asm volatile("bar.sync %0, 128;" ::"r"(2 + w) : "memory");
         }

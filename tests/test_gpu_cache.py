@@ -950,3 +950,32 @@ def test_scores_of_many_billions(variant, dtype, D, T, group, sign):
     else:      # the weight, 2^(s c2 - base) with base rounded, is near 1; it is rounded to bf16 for the product and not for the sum: 2^-8, and 2^-8 for the output
         assert bool(((got["out"].double() - want.double()).abs() <= (2.0 ** -7 + 2.0 ** -15) * want.double().abs()).all())
     assert c.status() == jd.JD_OK
+
+
+@pytest.mark.parametrize("variant,dtype,D", VARIANTS)
+@pytest.mark.parametrize("T,group", [(1, 1)] + FORMS)
+def test_infinite_values_of_context_tokens(variant, dtype, D, T, group):
+    """A value of a token that every row sees: an infinity stays that infinity, two of opposite signs and a NaN give NaN, and other
+    elements keep their bits - also where the sequence is cut, where an infinity is a node's as well, and in more than one tile."""
+    lens = [300, 1, 1000, 140]
+    c = L.filled_cache(lens, T, q_heads=2 * group, D=D, dtype=dtype, max_nodes=T, seed=5)
+    q = rand((4, T, 2 * group, D), 12, dtype)
+    clean = c.attend(0, q, variant=variant)
+    want = clean["out"].clone()
+
+    def put(s, token, head, d, x):
+        c.v[0, int(c.page_table[s, token // 16]), head, token % 16, d] = x
+
+    inf, nan = float("inf"), float("nan")
+    for s, token, head, d, x, y in [(0, 0, 0, 0, inf, inf), (0, 299, 1, 1, -inf, -inf), (2, 77, 0, D - 1, inf, inf), (2, 900, 0, D - 1, inf, inf),
+                                    (2, 5, 1, 7, inf, nan), (2, 6, 1, 7, -inf, nan), (3, 139, 0, 9, nan, nan), (3, 10, 0, 9, inf, nan), (1, 0, 1, 3, -inf, -inf),
+                                    (0, 300, 0, 0, inf, inf), (3, 50, 1, 2, inf, inf), (3, 51, 1, 2, inf, inf)]:
+        put(s, token, head, d, x)
+        want[s, :, head * group:(head + 1) * group, d] = y
+    got = c.attend(0, q, variant=variant)
+    assert bool(((got["out"] == want) | (got["out"].isnan() & want.isnan())).all()) and torch.equal(got["lse"], clean["lse"])
+    # scores that are no numbers stay so whatever the values are
+    c.k[0, int(c.page_table[3, 0]), 0, 3, 0] = nan
+    got = c.attend(0, q, variant=variant)
+    assert bool(got["out"][3, :, :group].isnan().all()) and bool(got["lse"][3, :, :group].isnan().all())
+    assert c.status() == jd.JD_OK
