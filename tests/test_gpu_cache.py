@@ -979,3 +979,168 @@ def test_infinite_values_of_context_tokens(variant, dtype, D, T, group):
     got = c.attend(0, q, variant=variant)
     assert bool(got["out"][3, :, :group].isnan().all()) and bool(got["lse"][3, :, :group].isnan().all())
     assert c.status() == jd.JD_OK
+
+
+@pytest.mark.parametrize("variant,dtype,D", VARIANTS)
+@pytest.mark.parametrize("T,group", FORMS)
+@pytest.mark.parametrize("B", [3, 90])
+def test_hidden_and_spoilt_rows_in_every_form(variant, dtype, D, T, group, B):
+    """What stands in hidden rows has no effect, and a node that is not finite spoils those that see it alone, for every number of rows
+    and with several pieces on a CTA."""
+    lens = [(130, 0, 257, 61)[b % 4] + b % 7 for b in range(B)]
+    c = L.filled_cache(lens, T, q_heads=2 * group, D=D, dtype=dtype, max_nodes=T, seed=5)
+    rng = np.random.default_rng(8)
+    parents = [L.random_tree(T, rng, ("star", "chain")[b % 2]) for b in range(B)]
+    see = torch.from_numpy(np.stack([O.visible(p)[0] for p in parents])).cuda()
+    tree = L.device_tree(parents)
+    q = rand((B, T, 2 * group, D), 12, dtype)
+    clean = c.attend(0, q, tree, variant=variant)
+    table = c.page_table.cpu()
+    used = torch.zeros(c.k.shape[1], c.k.shape[3], dtype=torch.bool)
+    at = []
+    for s, n in enumerate(lens):
+        t = torch.arange(n + T)
+        used[table[s, t // 16].long(), t % 16] = True
+        at.append((int(table[s, (n + 3) // 16]), (n + 3) % 16))
+    hidden = (~used).cuda()[None, :, None, :, None].expand(c.k.shape)
+    junk = torch.tensor([float("nan"), float("inf"), float("-inf")], device="cuda").to(L.DT[dtype])[torch.arange(int(hidden.sum()), device="cuda") % 3]
+    c.k[hidden], c.v[hidden] = junk, junk
+    got = c.attend(0, q, tree, variant=variant)
+    assert torch.equal(got["out"], clean["out"]) and torch.equal(got["lse"], clean["lse"])
+    sees = see[:, :, 3][:, :, None].expand(B, T, 2 * group)
+    page, row = (torch.tensor(x, device="cuda") for x in zip(*at))
+    c.v[0, page, 0, row, 5], c.v[0, page, 1, row, 6] = float("inf"), float("nan")
+    got = c.attend(0, q, tree, variant=variant)
+    want = clean["out"].clone()
+    want[:, :, :group, 5][sees[:, :, :group]] = float("inf")
+    want[:, :, group:, 6][sees[:, :, group:]] = float("nan")
+    assert bool(((got["out"] == want) | (got["out"].isnan() & want.isnan())).all()) and torch.equal(got["lse"], clean["lse"])
+    c.k[0, page, :, row] = float("nan")
+    got = c.attend(0, q, tree, variant=variant)
+    assert torch.equal(got["out"][~sees], clean["out"][~sees]) and torch.equal(got["lse"][~sees], clean["lse"][~sees])
+    assert bool(got["out"][sees].isnan().all()) and bool(got["lse"][sees].isnan().all())
+    assert c.status() == jd.JD_OK
+
+
+def attend64(c, q, see, scale):
+    """Softmax attention of blocks q [B, T, heads, D] in float64 on the device, over all pages of every sequence at once, and the bound that
+    attend_tolerance of the library's tests derives, with each row's own |q|: (out, lse, bound of out, bound of lse)."""
+    B, T, Hq, D = q.shape
+    H = c.kv_heads
+    outs = []
+    for b in range(B):
+        n = int(c.seq_len[b])
+        at = torch.arange(n + T, device="cuda")
+        page, row = c.page_table[b].long()[at // c.k.shape[3]], at % c.k.shape[3]
+        k, v = (x[0, page, :, row].double().transpose(0, 1) for x in (c.k, c.v))                       # [H, n + T, D]
+        qb = q[b].double().view(T, H, Hq // H, D).permute(1, 2, 0, 3)                                  # [H, G, T, D]
+        s = scale * (qb @ k[:, None].transpose(2, 3))
+        s[..., n:].masked_fill_(~see[b], float("-inf"))
+        lse = s.logsumexp(-1)
+        p = (s - lse[..., None]).exp()
+        A = scale * qb.norm(dim=-1) * k.norm(dim=-1).max()
+        w = 2 * (D + 4) * 2.0 ** -24 * A + 2.0 ** -20 + (n + T) * 2.0 ** -24
+        out = p @ v[:, None]
+        extra, step = (2.0 ** -8, 2.0 ** -8) if q.dtype == torch.bfloat16 else (0.0, 2.0 ** -24)
+        tol = (p @ v.abs()[:, None]) * (w + extra)[..., None] + out.abs() * step + 1e-30
+        back = lambda x: x.movedim(2, 0).flatten(1, 2)                                                 # noqa: E731
+        outs.append((back(out), back(lse), back(tol), back(w + 2.0 ** -22 * lse.abs())))
+    return [torch.stack(x) for x in zip(*outs)]
+
+
+@pytest.mark.parametrize("variant,dtype,D", VARIANTS)
+@pytest.mark.parametrize("T,group", FORMS)
+@pytest.mark.parametrize("falling", [False, True])
+def test_scores_that_grow_from_tile_to_tile(variant, dtype, D, T, group, falling):
+    """Every tile's scores lie some 6 above the last one's (or below, or jump), so that sums and numerators found so far are weighed again and again
+    by factors that count, in rows that differ in how fast: out and lse within the bound."""
+    lens = [1500, 700, 1024, 90] * 10                         # 80 segments: pieces of many tiles
+    B = len(lens)
+    c = L.filled_cache(lens, T, q_heads=2 * group, D=D, dtype=dtype, max_nodes=T, seed=5)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(3)
+    u = torch.randn(D, generator=gen, device="cuda")
+    u /= u.norm()
+    q = torch.randn(B, T, 2 * group, D, generator=gen, device="cuda")
+    q += u * (torch.randint(0, 4, (B, T, 2 * group, 1), generator=gen, device="cuda") - 1) * D ** 0.5   # rows along u, against it and across
+    q = q.to(L.DT[dtype])
+    for b, n in enumerate(lens):
+        at = torch.arange(n + T, device="cuda")
+        page, row = c.page_table[b].long()[at // 16], at % 16
+        height = at.float() * (0.05 if b % 3 else 0.02)
+        if falling:
+            height = height.flip(0)
+        if b % 4 == 2:
+            height = (at // 128 % 3).float() * 15
+        c.k[0, page, :, row] = (torch.randn(n + T, 2, D, generator=gen, device="cuda") + height[:, None, None] * u).to(L.DT[dtype])
+    rng = np.random.default_rng(2)
+    parents = [L.random_tree(T, rng) for _ in lens]
+    see = torch.from_numpy(np.stack([O.visible(p)[0] for p in parents])).cuda()
+    out, lse, tol, ltol = attend64(c, q, see, D ** -0.5)
+    got = c.attend(0, q, L.device_tree(parents), variant=variant)
+    assert c.status() == jd.JD_OK
+    assert float(lse.max()) > 20 and float((tol / out.abs().clamp_min(0.1)).median()) < 0.05           # the bound says something
+    err = (got["out"].double() - out).abs()
+    assert bool((err <= tol).all()), float((err - tol).max())
+    assert bool(((got["lse"].double() - lse).abs() <= ltol).all())
+
+
+@pytest.mark.parametrize("D", [8, 40, 72, 80, 96, 112, 136, 192, 256])
+@pytest.mark.parametrize("T,q_heads,kv_heads", [(1, 2, 2), (2, 4, 2), (6, 6, 2), (11, 8, 1)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attend_head_widths(D, T, q_heads, kv_heads, dtype):
+    """Widths on both sides of 128 and types, four rows and sixteen, whole segments and split ones; the tensor-core kernel is
+    refused where it has no form."""
+    lens = [0, 65, 3, 900]
+    c = L.filled_cache(lens, T, q_heads=q_heads, kv_heads=kv_heads, D=D, dtype=dtype, max_nodes=T, seed=D)
+    rng = np.random.default_rng(D)
+    parents = [L.random_tree(T, rng) for _ in lens]
+    check_attend(*run_attend(c, L.model_of(c), T, parents, dtype, "auto", D))
+    with pytest.raises(jd.JdError) as e:
+        c.attend(0, rand((4, T, q_heads, D), 1, dtype), variant="tensor")
+    assert e.value.status == jd.JD_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("variant,dtype,D", VARIANTS + [("simt", "bf16", 192)])
+@pytest.mark.parametrize("B", [257, 385, 1024])
+def test_attend_many_sequences(variant, dtype, D, B):
+    """More sequences than a block has threads, padding and empty ones among them."""
+    T, seqs = 2, 60
+    rng = np.random.default_rng(B)
+    lens = [int(x) for x in rng.integers(0, 150, seqs)]
+    c = L.filled_cache(lens, T, q_heads=2, kv_heads=1, D=D, dtype=dtype, max_nodes=T, seed=2)
+    slots = rng.integers(-1, seqs, B)
+    nodes = rng.integers(0, T + 1, B)
+    check_attend(*run_attend(c, L.model_of(c), T, [-1, 0], dtype, variant, 3, slots=L.ints(slots), num_nodes=L.ints(nodes), B=B))
+
+
+@pytest.mark.parametrize("variant,dtype,D", VARIANTS)
+def test_a_prompt_in_blocks(variant, dtype, D):
+    """Prompts of different lengths go in as chains of up to 128 tokens that are kept whole; every row attends to what stands in
+    front of it, as one pass over the prompts has it."""
+    T, Hq, H, lens = 128, 4, 2, [300, 128, 1, 257]
+    B, n = len(lens), max(lens)
+    c = L.empty_cache(1, 80, 16, Hq, H, D, B, 24, T, dtype)
+    k, v, q = (rand((B, n, h, D), i, dtype) for i, h in enumerate((H, H, Hq)))
+    out = torch.zeros(B, n, Hq, D, dtype=q.dtype, device="cuda")
+    for at in range(0, n, T):
+        m = min(T, n - at)
+        left = [min(max(x - at, 0), m) for x in lens]
+        slots = L.ints([b if left[b] else -1 for b in range(B)])
+        c.reserve(m, slots)
+        tree = jd.Tree(m, num_nodes=L.ints(left))
+        part = [x[:, at:at + m].contiguous() for x in (k, v, q)]
+        c.append(0, part[0], part[1], tree, slots=slots)
+        out[:, at:at + m] = c.attend(0, part[2], tree, slots=slots, variant=variant)["out"]
+        c.commit(L.ints([max(x - 1, 0) for x in left]), slots=slots, path_len=m - 1)
+    assert c.status() == jd.JD_OK and c.seq_len.cpu().tolist() == lens
+    for b, x in enumerate(lens):
+        kk, vv = (t[b, :x].double().transpose(0, 1).repeat_interleave(Hq // H, 0) for t in (k, v))
+        s = D ** -0.5 * (q[b, :x].double().transpose(0, 1) @ kk.transpose(1, 2))
+        s.masked_fill_(torch.ones(x, x, dtype=torch.bool, device="cuda").triu(1), float("-inf"))
+        p = s.softmax(-1)
+        want, spread = p @ vv, p @ vv.abs()
+        A = D ** -0.5 * q[b, :x].double().norm(dim=-1).max() * kk.norm(dim=-1).max()
+        w = 2 * (D + 4) * 2.0 ** -24 * A + 2.0 ** -20 + x * 2.0 ** -24
+        extra, step = (2.0 ** -8, 2.0 ** -8) if dtype == "bf16" else (0.0, 2.0 ** -24)
+        assert bool(((out[b, :x].double().transpose(0, 1) - want).abs() <= spread * (w + extra) + want.abs() * step + 1e-30).all())
