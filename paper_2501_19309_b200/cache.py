@@ -13,7 +13,7 @@ One decoding step of a stack of target layers::
 Argument marshalling only; every step runs inside the library's kernels.  All calls are enqueued on ``stream`` (default:
 torch's current stream of the cache's device) and none waits for the device, except :meth:`PagedCache.status`.  Outputs that a
 call makes itself are allocated on the current stream: with another ``stream``, pass them in.  Nothing here records a graph for
-autograd: inputs that require gradients are refused while gradients are enabled.
+autograd: inputs that require gradients are refused while gradients are enabled, and so are inputs with a forward-mode tangent.
 """
 from __future__ import annotations
 
@@ -23,6 +23,7 @@ import struct
 from typing import Optional
 
 import torch
+import torch.autograd.forward_ad as _fw
 
 from . import jd
 
@@ -53,6 +54,10 @@ _ROPE_ARGS = struct.Struct("@qiiiiPPqqPPiif")
 _APPEND_ARGS = struct.Struct("@iiP" + _TREE + "PPPPqqqqP")
 _ATTEND_ARGS = struct.Struct("@iiP" + _TREE + "PPqqPfi")
 _COMMIT_ARGS = struct.Struct("@iPPiiPP")
+
+
+def _has_tangent(x: torch.Tensor) -> bool:
+    return _fw.unpack_dual(x).tangent is not None
 
 
 def _stream(stream, index: int) -> int:
@@ -126,7 +131,7 @@ class Rotary:
     @staticmethod
     def _step(t: torch.Tensor, name: str, n: int, heads: int, dim: int) -> int:
         """Elements between tokens, 0: dense."""
-        if t.requires_grad and torch.is_grad_enabled():
+        if t.requires_grad and torch.is_grad_enabled() or _fw._current_level >= 0 and _has_tangent(t):
             raise ValueError("%s: no autograd here; detach it, the gradient is rotate(grad, positions, inverse=True)" % name)
         if t.is_contiguous():
             return 0
@@ -268,7 +273,7 @@ class PagedCache:
         """Elements between tokens (0: dense) of [B, T, heads, head_dim] whose tokens lie evenly, heads contiguous."""
         if x.shape != shape or x.dtype is not self.dtype or x.get_device() != self.index:
             raise ValueError("%s: %s of the cache's type, on its device" % (name, list(shape)))
-        if x.requires_grad and torch.is_grad_enabled():
+        if x.requires_grad and torch.is_grad_enabled() or _fw._current_level >= 0 and _has_tangent(x):
             raise ValueError("%s: no autograd here; detach it" % name)
         if x.is_contiguous():
             return 0

@@ -372,3 +372,20 @@ def test_yarn_blend_runs_past_the_last_frequency(rot, base, old, factor, low, hi
     got, amp = jd.rope_frequencies(rot, base, "yarn", factor, old, low, high)
     want = f0 * (1 - divided) + f0 / factor * divided
     assert (np.abs(got.numpy().astype(np.float64) - want) <= 2.0 ** -23 * (1 + 1e-9) * want).all() and abs(amp - (0.1 * math.log(factor) + 1)) < 1e-6
+
+
+def test_tensors_with_a_tangent_are_refused():
+    """Forward-mode derivatives would be lost as silently as a graph."""
+    import torch.autograd.forward_ad as fw
+    from paper_2501_19309_b200.cache import PagedCache, Rotary
+    c = object.__new__(PagedCache)
+    c.h, c.dtype, c.index = None, torch.float32, -1
+    x = torch.zeros(2, 3, 4, 64)
+    with fw.dual_level():
+        dual = fw.make_dual(x, torch.ones_like(x))
+        with pytest.raises(ValueError):
+            c._tokens(dual, "q", (2, 3, 4, 64))
+        with pytest.raises(ValueError):
+            Rotary._step(fw.make_dual(x[0], torch.ones_like(x[0])), "x", 3, 4, 64)
+        assert c._tokens(x, "q", (2, 3, 4, 64)) == 0 and Rotary._step(x[0], "x", 3, 4, 64) == 0
+    assert c._tokens(x, "q", (2, 3, 4, 64)) == 0
