@@ -297,6 +297,8 @@ class PagedCache:
 
     def reserve(self, n: int, slots: Optional[torch.Tensor] = None, stream=None) -> None:
         """Pages for n more tokens of every sequence (``jd_cache_reserve``)."""
+        if not -1 << 31 <= n < 1 << 31:           # ctypes would drop the upper bits
+            raise ValueError("n: a number of tokens")
         B = self._batch(slots)
         st = self._lib.jd_cache_reserve(self.h, B, _ints(slots, "slots", self.index), n, _stream(stream, self.index))
         if st != jd.JD_OK:

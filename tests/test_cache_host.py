@@ -389,3 +389,12 @@ def test_tensors_with_a_tangent_are_refused():
             Rotary._step(fw.make_dual(x[0], torch.ones_like(x[0])), "x", 3, 4, 64)
         assert c._tokens(x, "q", (2, 3, 4, 64)) == 0 and Rotary._step(x[0], "x", 3, 4, 64) == 0
     assert c._tokens(x, "q", (2, 3, 4, 64)) == 0
+
+
+def test_a_reserve_that_32_bits_do_not_hold_is_refused():
+    from paper_2501_19309_b200.cache import PagedCache
+    c = object.__new__(PagedCache)
+    c.h, c.max_seqs, c.index, c._lib = None, 1, -1, None
+    for n in ((1 << 32) + 1, 1 << 31, -(1 << 32) + 5):
+        with pytest.raises(ValueError):
+            c.reserve(n)
