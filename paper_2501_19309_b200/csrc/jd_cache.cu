@@ -450,6 +450,7 @@ bool cache_config_ok(const jd_cache_config_t* g) {
   return true;
 }
 
+bool on_tensor_cores(const jd_cache_config_t& g) { return g.dtype == JD_DTYPE_BF16 && (g.head_dim == 64 || g.head_dim == 128); }
 int rows_of(const jd_cache_config_t& g) { return g.max_nodes * (g.q_heads / g.kv_heads); }
 
 size_t carve_cache(const jd_cache_config_t& g, char* base, jd_cache_s* c) {
@@ -467,9 +468,9 @@ size_t carve_cache(const jd_cache_config_t& g, char* base, jd_cache_s* c) {
   int* md = (int*)take((size_t)g.num_pages * 4);
   int* mc = (int*)take(256);
   int4* sp = (int4*)take((size_t)2 * kMaxCtas * sizeof(int4));
-  // two partial results for each CTA of an attention call: up to 256 rows each on the tensor cores (one CTA per SM),
-  // kSimtRows on CUDA cores (two per SM)
-  const size_t rows = std::max<size_t>(std::min(rows_of(g), 256), 2 * kSimtRows);
+  // two partial results for each CTA of an attention call: up to 256 rows each on the tensor cores (one CTA per SM), where
+  // they take the cache, kSimtRows on CUDA cores (two per SM)
+  const size_t rows = std::max<size_t>(on_tensor_cores(g) ? std::min(rows_of(g), 256) : 0, 2 * kSimtRows);
   float* part = (float*)take((size_t)kMaxCtas * 2 * rows * (g.head_dim + kPartPad) * 4);
   if (c) {
     c->status = status; c->commit_cnt = cnt; c->reserve_cnt = rc;
@@ -579,7 +580,7 @@ jd_status_t jd_cache_create(jd_cache_t* out, const jd_cache_config_t* cfg, const
   c->last_stream = nullptr;
   carve_cache(*cfg, (char*)b->workspace, c);
   c->tm_ok = false;
-  if (cfg->dtype == JD_DTYPE_BF16 && (cfg->head_dim == 64 || cfg->head_dim == 128)) {
+  if (on_tensor_cores(*cfg)) {
     const uint64_t rows = (uint64_t)cfg->num_layers * cfg->num_pages * cfg->kv_heads * cfg->page_size;
     const uint32_t box = (uint32_t)std::min(cfg->page_size, 1 << kTensorTileShift);
     c->tm_ok = encode_rows(&c->tm_k, b->k_pages, rows, (uint64_t)cfg->head_dim, box) &&

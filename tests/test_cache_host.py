@@ -398,3 +398,19 @@ def test_a_reserve_that_32_bits_do_not_hold_is_refused():
     for n in ((1 << 32) + 1, 1 << 31, -(1 << 32) + 5):
         with pytest.raises(ValueError):
             c.reserve(n)
+
+
+def test_workspace_holds_the_parts_that_the_cache_can_have():
+    """Parts of up to 256 rows are the tensor-core kernel's alone; others are of 16 rows, two to each of at most 512 CTAs."""
+    need = jd.load().jd_cache_workspace_bytes
+    books = 1 << 17                                      # counters, and three numbers a page
+    for D in (8, 80, 256):
+        for dtype in (jd.JD_DTYPE_F32, jd.JD_DTYPE_BF16):
+            got = need(C.byref(config(head_dim=D, dtype=dtype)))
+            parts = 512 * 2 * 16 * (D + 4) * 4
+            assert parts <= got <= parts + books, (D, dtype)
+    for D in (64, 128):
+        assert need(C.byref(config(head_dim=D, dtype=jd.JD_DTYPE_F32))) <= 512 * 2 * 16 * (D + 4) * 4 + books
+        for nodes, rows in ((1, 32), (8, 32), (9, 36), (26, 104), (128, 256)):     # 4 query heads of a kv head
+            got = need(C.byref(config(head_dim=D, max_nodes=nodes)))
+            assert 256 * 2 * rows * (D + 4) * 4 <= got <= 256 * 2 * rows * (D + 4) * 4 + books, (D, nodes)
