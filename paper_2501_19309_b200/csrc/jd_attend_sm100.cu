@@ -253,15 +253,17 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     sh.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  pdl_wait();      // so far nothing was touched that another kernel knows of
+  // Tensor memory is taken behind the wait and held before the next kernel may start: a block that holds it while it waits for a kernel in
+  // front, whose blocks on the same SM have yet to take theirs, would wait for good, and so would this one for a block behind it.
   if (warp == 9) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem_base)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
-  pdl_wait();      // so far nothing was touched that another kernel knows of
-  pdl_trigger();
   if (rb == 0 && tid == 0) split_none(p, g);
   unit_prefix(p, sh.prefix, sh.warp_sums, sh.extents);   // ends with a barrier
+  pdl_trigger();
   tc_fence_after();
   const int64_t units = (int64_t)sh.prefix[p.B] * p.c.kv_heads;
   const int64_t run0 = run_start(units, p.groups, g), run1 = run_start(units, p.groups, g + 1);

@@ -414,3 +414,12 @@ def test_workspace_holds_the_parts_that_the_cache_can_have():
         for nodes, rows in ((1, 32), (8, 32), (9, 36), (26, 104), (128, 256)):     # 4 query heads of a kv head
             got = need(C.byref(config(head_dim=D, max_nodes=nodes)))
             assert 256 * 2 * rows * (D + 4) * 4 <= got <= 256 * 2 * rows * (D + 4) * 4 + books, (D, nodes)
+
+
+def test_tensor_memory_is_taken_between_the_wait_and_the_trigger():
+    """A kernel that holds tensor memory while it waits for the one in front, or lets the next one start before it holds it, can wait for good on an
+    SM that two of them share: shown by the order in the source, which no run may try."""
+    src = open(os.path.join(ROOT, "paper_2501_19309_b200", "csrc", "jd_attend_sm100.cu")).read()
+    body = src[src.index("attend_sm100_kernel("):]
+    at = [body.index(x) for x in ("pdl_wait();", "tcgen05.alloc", "unit_prefix(", "pdl_trigger();", "tcgen05.dealloc")]
+    assert at == sorted(at) and all(body.count(x) == 1 for x in ("pdl_wait();", "tcgen05.alloc", "pdl_trigger();"))
