@@ -328,7 +328,7 @@ typedef struct {
 } jd_rope_t;
 
 typedef struct {
-  int64_t tokens;          /* >= 0; 0 launches nothing */
+  int64_t tokens;          /* 0..2^31 - 1; 0 launches nothing */
   int32_t heads, head_dim; /* >= 1; head_dim 1..256 */
   int32_t dtype;           /* JD_DTYPE_F32 or JD_DTYPE_BF16 */
   int32_t inverse;         /* 1: turn by the negative angle. The map is linear and this is its transpose:

@@ -238,7 +238,6 @@ cudaError_t launch_rope(const jd_rope_args_t& a, int64_t xs, int64_t os, cudaStr
   // about kRopeUnitsPerThread pieces per thread, so that a block's angles pay for themselves
   const int per_block = std::max(1, std::min(kTokensPerBlock, kRopeThreads * kRopeUnitsPerThread / std::max(1, units)));
   const int64_t blocks = (a.tokens + per_block - 1) / per_block;
-  if (blocks > 0x7FFFFFFF) return cudaErrorInvalidValue;
   return launch_chained(vec ? rope_kernel<T, true> : rope_kernel<T, false>, dim3((unsigned)blocks), dim3(kRopeThreads), 0, st, (const T*)a.x,
                         (T*)a.out, a.tokens, a.heads, a.head_dim, xs, os, a.positions, a.rope.inv_freq, half, a.rope.layout, a.rope.amplitude,
                         a.inverse, per_block);
@@ -315,7 +314,7 @@ jd_status_t jd_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, d
 }
 
 jd_status_t jd_rope(const jd_rope_args_t* a, void* cuda_stream) {
-  if (!a || a->tokens < 0 || a->heads < 1 || a->head_dim < 1 || a->head_dim > 256) return JD_ERR_INVALID_ARG;
+  if (!a || a->tokens < 0 || a->tokens > 0x7FFFFFFF || a->heads < 1 || a->head_dim < 1 || a->head_dim > 256) return JD_ERR_INVALID_ARG;
   if (a->dtype != JD_DTYPE_F32 && a->dtype != JD_DTYPE_BF16) return JD_ERR_INVALID_ARG;
   if (!rope_ok(a->rope, a->head_dim) || a->x_stride < 0 || a->out_stride < 0) return JD_ERR_INVALID_ARG;
   const int64_t dense = (int64_t)a->heads * a->head_dim;
@@ -330,7 +329,8 @@ jd_status_t jd_rope(const jd_rope_args_t* a, void* cuda_stream) {
   if (a->x == a->out && xs != os) return JD_ERR_INVALID_ARG;
   const cudaError_t err = a->dtype == JD_DTYPE_F32 ? launch_rope<float>(*a, xs, os, (cudaStream_t)cuda_stream)
                                                    : launch_rope<__nv_bfloat16>(*a, xs, os, (cudaStream_t)cuda_stream);
-  return err == cudaSuccess ? JD_OK : JD_ERR_CUDA;
+  if (err != cudaSuccess) { cudaGetLastError(); return JD_ERR_CUDA; }
+  return JD_OK;
 }
 
 }  // extern "C"

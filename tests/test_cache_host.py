@@ -423,3 +423,8 @@ def test_tensor_memory_is_taken_between_the_wait_and_the_trigger():
     body = src[src.index("attend_sm100_kernel("):]
     at = [body.index(x) for x in ("pdl_wait();", "tcgen05.alloc", "unit_prefix(", "pdl_trigger();", "tcgen05.dealloc")]
     assert at == sorted(at) and all(body.count(x) == 1 for x in ("pdl_wait();", "tcgen05.alloc", "pdl_trigger();"))
+
+
+def test_more_tokens_than_a_rotation_takes_are_a_bad_argument():
+    for n in (1 << 31, 1 << 40, (1 << 63) - 1):
+        assert jd.load().jd_rope(C.byref(rope_args(tokens=n)), None) == jd.JD_ERR_INVALID_ARG
