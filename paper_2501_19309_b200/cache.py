@@ -90,6 +90,7 @@ class Rotary:
     def __init__(self, inv_freq: torch.Tensor, layout: str = "half", amplitude: float = 1.0):
         _require(inv_freq.dtype == torch.float32 and inv_freq.is_contiguous() and inv_freq.dim() == 1,
                  "inv_freq: a contiguous float32 vector")
+        _require(not inv_freq.requires_grad, "inv_freq: no autograd here; detach it")
         self.inv_freq, self.layout, self.amplitude = inv_freq, layout, float(amplitude)
         self.rot_dim = 2 * inv_freq.numel()
         self._layout = LAYOUTS[layout]
@@ -210,6 +211,7 @@ class PagedCache:
     def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, seq_len: torch.Tensor, held: torch.Tensor,
                  refs: torch.Tensor, free_bits: torch.Tensor, q_heads: int, max_nodes: int = 64):
         self.h = None
+        _require(not (k.requires_grad or v.requires_grad), "k, v: no autograd here; detach them")
         _require(k.dim() == 5 and k.is_cuda and k.is_contiguous() and k.dtype in _DTYPES, "k: contiguous [layers, pages, kv_heads, page_size, head_dim]")
         _require(v.shape == k.shape and v.dtype == k.dtype and v.device == k.device and v.is_contiguous(), "v: like k")
         self.device, self.index, self.dtype = k.device, k.get_device(), k.dtype

@@ -428,3 +428,14 @@ def test_tensor_memory_is_taken_between_the_wait_and_the_trigger():
 def test_more_tokens_than_a_rotation_takes_are_a_bad_argument():
     for n in (1 << 31, 1 << 40, (1 << 63) - 1):
         assert jd.load().jd_rope(C.byref(rope_args(tokens=n)), None) == jd.JD_ERR_INVALID_ARG
+
+
+def test_frequencies_and_pages_that_require_gradients_are_refused():
+    from paper_2501_19309_b200.cache import PagedCache
+    with pytest.raises(ValueError, match="autograd"):
+        jd.Rotary(torch.ones(4, requires_grad=True))
+    ints = torch.zeros(1, dtype=torch.int32)
+    for i in range(2):
+        k, v = (torch.zeros(1, 1, 1, 8, 8, requires_grad=i == j) for j in range(2))
+        with pytest.raises(ValueError, match="autograd"):
+            PagedCache(k, v, ints.view(1, 1), ints, ints, ints, ints, 1)
