@@ -1144,3 +1144,18 @@ def test_a_prompt_in_blocks(variant, dtype, D):
         w = 2 * (D + 4) * 2.0 ** -24 * A + 2.0 ** -20 + x * 2.0 ** -24
         extra, step = (2.0 ** -8, 2.0 ** -8) if dtype == "bf16" else (0.0, 2.0 ** -24)
         assert bool(((out[b, :x].double().transpose(0, 1) - want).abs() <= spread * (w + extra) + want.abs() * step + 1e-30).all())
+
+
+@pytest.mark.parametrize("variant,dtype,D", VARIANTS)
+@pytest.mark.parametrize("T,group", [(128, 160), (127, 400)])
+def test_attend_more_row_blocks_than_multiprocessors(variant, dtype, D, T, group):
+    """So many query heads of a kv head that one block a row block is all that the grid has."""
+    lens = [70, 0, 300]
+    c = L.filled_cache(lens, T, q_heads=group, kv_heads=1, D=D, dtype=dtype, max_nodes=T, seed=5)
+    q = rand((3, T, group, D), 4, dtype)
+    parents = [L.random_tree(T, np.random.default_rng(s)) for s in range(3)]
+    see = torch.from_numpy(np.stack([O.visible(p)[0] for p in parents])).cuda()
+    got = c.attend(0, q, L.device_tree(parents), variant=variant)
+    assert c.status() == jd.JD_OK
+    out, lse, tol, ltol = attend64(c, q, see, D ** -0.5)
+    assert bool(((got["out"].double() - out).abs() <= tol).all()) and bool(((got["lse"].double() - lse).abs() <= ltol).all())
