@@ -300,6 +300,10 @@ jd_status_t jd_verify_static(int32_t d, int32_t V, const void* W, const void* w_
  * the host, and a whole step can be captured in a CUDA graph. A block is what Sec. 3.1 forwards in
  * parallel: node 0 is the last context token, nodes 1..T-1 are draft tokens, in a chain or in a
  * tree (a node's number is larger than its parent's).
+ *
+ * A prompt goes in the same way, without jd_verify, in chains of up to max_nodes tokens that are kept whole: reserve, append and
+ * attend with T tokens, commit with accept_len = T - 1 and no paths (prompts of different lengths: num_nodes, and slot -1 where
+ * one has ended).
  * ========================================================================================= */
 
 /* Which elements of a head turn together. HALF: i with i + rot_dim / 2; INTERLEAVED: 2 i with 2 i + 1. */
@@ -398,7 +402,8 @@ jd_status_t jd_cache_destroy(jd_cache_t c);   /* frees host memory only; NULL is
  * sequences' order; and where the page that holds token seq_len has rows in use and other owners, a copy of those
  * rows in a page of the sequence's own (all layers). A sequence named later in the call counts as owner until its turn,
  * so that the last one keeps the page. All or nothing: if pages are short, or a table is, nothing changes and
- * JD_ERR_PAGES is reported. Reserve before append, and fork only between commit and append. */
+ * JD_ERR_PAGES is reported. Reserve before append, and fork only between commit and reserve: behind a fork the page that a
+ * block begins in has two owners, and append writes nothing there. */
 jd_status_t jd_cache_reserve(jd_cache_t c, int32_t B, const int32_t* slots, int32_t n, void* cuda_stream);
 
 /* The block of drafted tokens of a step. */
@@ -489,7 +494,7 @@ jd_status_t jd_cache_truncate(jd_cache_t c, int32_t B, const int32_t* slots, con
 jd_status_t jd_cache_compact(jd_cache_t c, int32_t* used, void* cuda_stream);
 
 /* Synchronises the stream of the cache's last call and returns and clears the device status: *out = JD_OK, JD_ERR_PAGES,
- * JD_ERR_BAD_INDEX or JD_ERR_TIMEOUT, the first since the last query. Not during a capture. */
+ * JD_ERR_BAD_INDEX or JD_ERR_TIMEOUT, the first since the last query. That stream has to exist still. Not during a capture. */
 jd_status_t jd_cache_last_status(jd_cache_t c, int* out);
 
 #ifdef __cplusplus

@@ -10,6 +10,8 @@
 // 128, one token each: 260 us, 4.0 TB/s; 8 blocks of 26 nodes, 16 heads on 4 of 128 over 2,000 tokens: 200 us, 17 TFLOP/s, of which
 // 58 % of the issue slots, 50 % of the shared-memory accesses and 36 % of the FMA pipe: what stays is shared memory's latency (the
 // largest stall) and the barriers between a tile's four phases, with 16 warps on an SM.
+// bf16 head widths that the tensor-core kernel does not take come here too, far from its rates: 16 sequences of 8,000 tokens, 8 heads, one
+// token each, 32 query heads: 352 us for heads of 80, 397 of 96, 1,530 of 256 (one block on an SM), against 91 of 128 there.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>

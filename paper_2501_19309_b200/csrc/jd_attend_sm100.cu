@@ -20,11 +20,14 @@
 // TMA, a box per page and 64 columns, through a ring; one or two more issue the MMAs.
 //
 // What bounds it (B200, 148 SMs):
-//   up to 128 rows   HBM: 16 sequences of 40,000 tokens, 8 kv heads of 128, one token each: 386 us, 6.8 TB/s; heads of 64: 204 us, 6.4 TB/s
+//   up to 128 rows   long contexts: HBM. 16 sequences of 40,000 tokens, 8 kv heads of 128, one token each: 391 us, 6.7 TB/s; heads of 64: 204 us,
+//                    6.4 TB/s. Ragged batches: beginning and ending segments (16 chains of 9 on 90 to 6,000 tokens, heads of 64: 36 us, 44 %
+//                    of the HBM rate)
 //   129 rows and up  the chains' own latency: a pair of row tiles takes about 3,450 cycles a tile, of which its products are 2,200 (S: 75
 //                    cycles a step of 16 columns, as Q comes from shared memory again every time; P V: 64), its exponentials
-//                    2,050 on each SM partition and the rest the hand-overs between them; 416 rows over 131,046 tokens: 252 us,
-//                    885 TFLOP/s, at clocks that the power limit holds near 1.5 GHz
+//                    2,050 on each SM partition and the rest the hand-overs between them; 416 rows over 131,046 tokens: 252 us, 885 TFLOP/s,
+//                    in short bursts; back to back the power limit holds the clock near 1.5 GHz: 298 us, 750 TFLOP/s. 4 sequences of
+//                    208 rows on 9,000 to 40,000 tokens: heads of 128 114 us, of 64 102 us
 //   short contexts   about 8,000 cycles to begin and end a segment
 // Tried and slower: a second pair of softmax warpgroups, half the columns each (275 against 260 us on that case); a quarter of the
 // exponentials as polynomials on the FMA pipe (274); S in halves of 64 tokens with a buffer each, so that the next is ready when
