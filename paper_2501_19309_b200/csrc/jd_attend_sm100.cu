@@ -226,9 +226,48 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
+// Sums of the values of cached tokens begin .. end - 1 that are not finite, in four columns from c; begin is a multiple of 8. A call of its own,
+// since it is hardly ever made, with 32 loads under way at once, since other roles' waits have a limit (some 1.8 s; 65 ns a token and call,
+// up to eight calls a thread and piece: some 3 million tokens of a piece, with infinities in all columns and no NaN).
+template <int D>
+__device__ __noinline__ float4 spoilt_by_context(const AttendParams& p, int slot, int head, int begin, int end, int c) {
+  constexpr int kGroups = 4, kGroup = 8;               // no page is smaller than a group
+  float sum[4] = {};
+  for (int kv0 = begin; kv0 < end; kv0 += kGroups * kGroup) {
+    uint2 y[kGroups * kGroup];
+    int page[kGroups];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const int kv = kv0 + g * kGroup;
+      page[g] = kv < end ? __ldcg(p.c.table + (int64_t)slot * p.c.max_pages + (kv >> p.c.page_shift)) : -1;
+    }
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const int kv = kv0 + g * kGroup;
+      const bool there = page[g] >= 0 && page[g] < p.c.pages;
+      const uint2* v = reinterpret_cast<const uint2*>(reinterpret_cast<const __nv_bfloat16*>(p.c.v) +
+                                                      page_row(p.c, p.layer, there ? page[g] : 0, head, kv & (p.c.page_size - 1)) * D + c);
+#pragma unroll
+      for (int k = 0; k < kGroup; ++k) {
+        const uint2 x = __ldcg(v + k * (D / 4));       // rows of the page behind the last token are there, whatever they hold
+        y[g * kGroup + k] = there && kv + k < end ? x : make_uint2(0u, 0u);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kGroups * kGroup; ++k) {
+      const float e[4] = {__uint_as_float(y[k].x << 16), __uint_as_float(y[k].x & 0xFFFF0000u), __uint_as_float(y[k].y << 16), __uint_as_float(y[k].y & 0xFFFF0000u)};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (!isfinite(e[i])) sum[i] += e[i];
+    }
+    if (isnan(sum[0]) && isnan(sum[1]) && isnan(sum[2]) && isnan(sum[3])) break;
+  }
+  return make_float4(sum[0], sum[1], sum[2], sum[3]);
+}
+
 template <int D, int kMode>
 __global__ void __launch_bounds__(kThreads, 1)
-attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const AttendParams p) {
+attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ AttendParams p) {
   using Sh = Shape<D, kMode>;
   constexpr bool kPair = Sh::kPair;
   constexpr int kCopies = Sh::kCopies, kCopyRows = Sh::kCopyRows, kCols = Sh::kCols;
@@ -699,29 +738,34 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           lost &= sum_ok;
         }
         if (odd || lost) {
-          // The values that are not finite, of this piece's nodes (taken out of V) or of all its tokens, to the rows that see them. What is finite does
-          // not count beside them.
+          // What is finite does not count beside what is not.
           float sum[kN] = {};
-          const int end = min((x.tile0 + x.tiles) * kTile, ex.kv_end);
-          for (int kv = max(x.tile0 * kTile, lost ? 0 : ex.ctx); kv < end; ++kv) {
-            const int j = kv - ex.ctx;
-            if (j >= 0 && !((mine.node_mask[t][j >> 5] >> (j & 31)) & 1u)) continue;
-            const int page = p.c.table[(int64_t)ex.slot * p.c.max_pages + (kv >> p.c.page_shift)];
-            if (page < 0 || page >= p.c.pages) continue;
-            const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(p.c.v) + page_row(p.c, p.layer, page, x.head, kv & (p.c.page_size - 1)) * D + c;
+          if (odd) {                                 // values of this piece's nodes that are not finite, to the rows that see them
+            for (int j = 0; j < ex.nodes; ++j) {
+              const int kv = ex.ctx + j;
+              if (kv < x.tile0 * kTile || kv >= (x.tile0 + x.tiles) * kTile || kv >= ex.kv_end || !((mine.node_mask[t][j >> 5] >> (j & 31)) & 1u)) continue;
+              const int page = p.c.table[(int64_t)ex.slot * p.c.max_pages + (kv >> p.c.page_shift)];
+              if (page < 0 || page >= p.c.pages) continue;
+              const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(p.c.v) + page_row(p.c, p.layer, page, x.head, kv & (p.c.page_size - 1)) * D + c;
 #pragma unroll
-            for (int i = 0; i < kN; ++i) {
-              const float y = __bfloat162float(v[i]);
-              if (!isfinite(y)) sum[i] += y;
+              for (int i = 0; i < kN; ++i) {
+                const float y = __bfloat162float(v[i]);
+                if (!isfinite(y)) sum[i] += y;
+              }
             }
-            bool settled = !odd;                     // nothing changes a NaN
+          }
+          if constexpr (kCopies > 1) {
+            if (lost) {
+              const float4 y = spoilt_by_context<D>(p, ex.slot, x.head, x.tile0 * kTile, min((x.tile0 + x.tiles) * kTile, ex.ctx), c);
+              const float of[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-            for (int i = 0; i < kN; ++i) settled &= isnan(sum[i]) || !isnan(o[i]);
-            if (settled) break;
+              for (int i = 0; i < kN; ++i)
+                if (isnan(o[i]) && of[i] != 0.f) o[i] = of[i];
+            }
           }
 #pragma unroll
           for (int i = 0; i < kN; ++i)
-            if (sum[i] != 0.f) o[i] = lost && isnan(o[i]) ? sum[i] : o[i] + sum[i];
+            if (sum[i] != 0.f) o[i] += sum[i];
         }
         if (whole) {
           uint2* out = reinterpret_cast<uint2*>(p.out + ((int64_t)x.b * p.T + t) * p.out_stride + ((int64_t)h * D + c) * 2);

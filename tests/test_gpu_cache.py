@@ -1159,3 +1159,33 @@ def test_attend_more_row_blocks_than_multiprocessors(variant, dtype, D, T, group
     assert c.status() == jd.JD_OK
     out, lse, tol, ltol = attend64(c, q, see, D ** -0.5)
     assert bool(((got["out"].double() - out).abs() <= tol).all()) and bool(((got["lse"].double() - lse).abs() <= ltol).all())
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("T,group", [(1, 4), (20, 2)])
+def test_infinite_values_in_every_column_of_long_pieces(D, T, group):
+    """150 segments of 100,000 tokens, about one to a CTA: finding the infinities takes no time that a wait inside the kernel
+    would run out in, and a NaN behind them is found as well."""
+    n, B, page = 100000, 75, 64
+    per = -(-(n + T) // page)
+    c = L.empty_cache(1, per, page, 2 * group, 2, D, B, per, T, fill=3)
+    c.page_table.copy_(torch.arange(per, dtype=torch.int32, device="cuda").expand(B, per))       # all sequences read the same pages
+    c.refs.fill_(B)
+    c.free_bits.zero_()
+    c.seq_len.fill_(n)
+    c.held.fill_(per)
+    c.v[0, 5 // page, :, 5] = float("inf")
+    c.v[0, 6 // page, :, 6, 3] = float("-inf")
+    c.v[0, (n - 1) // page, :, (n - 1) % page, 7] = float("nan")
+    q = rand((B, T, 2 * group, D), 4)
+    got = c.attend(0, q, variant="tensor")
+    assert c.status() == jd.JD_OK
+    want = torch.full_like(q, float("inf"))
+    want[..., [3, 7]] = float("nan")
+    assert bool(((got["out"] == want) | (got["out"].isnan() & want.isnan())).all()) and bool(got["lse"].isfinite().all())
+    start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    start.record()
+    c.attend(0, q, variant="tensor")
+    end.record()
+    assert c.status() == jd.JD_OK
+    assert start.elapsed_time(end) < 100                # ms; 2 without infinities. The waits' limit is some 1,800
