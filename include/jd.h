@@ -456,7 +456,8 @@ typedef struct {
  * bf16 in front of their product with v. A row that sees nothing gets out = 0 and lse = -inf. Whatever stands
  * in rows that a node may not see (infinities and NaN too) stays without effect on it. A value of a seen row that is not finite
  * makes that element of the output what the sum has it be, the infinity or NaN, as long as the row's weight is one that
- * float32 holds; below that NaN may stand for the infinity. Pointers 16-byte aligned, strides multiples of 16 bytes. */
+ * float32 holds; below that NaN may stand for the infinity. Numerators are divided at the end, so a value times the
+ * number of tokens has to stay below 2^119. Pointers 16-byte aligned, strides multiples of 16 bytes. */
 jd_status_t jd_cache_attend(jd_cache_t c, const jd_attend_args_t* args, void* cuda_stream);
 
 typedef struct {
