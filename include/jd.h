@@ -286,6 +286,46 @@ jd_status_t jd_check_workspace_guards(jd_handle_t h, int32_t* damaged);
 jd_status_t jd_verify_static(int32_t d, int32_t V, const void* W, const void* w_judge, float b_judge,
                              const jd_verify_args_t* args, uint32_t* device_status, void* cuda_stream);
 
+/* ---------------------------------------------------------------- verification from probabilities */
+
+/* How the children of a node were drawn from the draft's distribution there: each by itself, or each from what the ones before it left. */
+typedef enum { JD_SIBLINGS_INDEPENDENT = 0, JD_SIBLINGS_DISTINCT = 1 } jd_siblings_t;
+
+typedef struct {
+  int32_t B;                    /* sequences, 0..65535; 0 launches nothing */
+  int32_t nodes;                /* T, 1..128: node 0 is the last context token, nodes 1..T-1 are drafted tokens */
+  int32_t V;                    /* 1..2^28 */
+  int32_t dtype;                /* of the probabilities: JD_DTYPE_F32 or JD_DTYPE_BF16 */
+  const void* target;           /* [B][T][V] target's probabilities behind each node, target_stride elements between rows (0: V) */
+  const void* draft;            /* [B][T-1][V] distribution that a node's children were drawn from, draft_stride (0: V). Rows of nodes
+                                   without children are not read; NULL if T is 1 */
+  int64_t target_stride, draft_stride;
+  const int32_t* tokens;        /* [B][T-1] token of node i at i - 1 */
+  const int32_t* parents;       /* [T] or [B][T]: a node's parent has a smaller number (entry 0 is not read). NULL: chains */
+  int32_t per_seq;              /* 0: one tree for all sequences, 1: one for each */
+  const int32_t* num_nodes;     /* [B] nodes of each sequence, 0..T (clamped), or NULL: T. 0: nothing of the sequence is read or written */
+  const float* accept_u;        /* [B][T-1] uniform numbers of [0, 1), one for each drafted token */
+  const float* sample_u;        /* [B] for the next token */
+  const float* judge_scores;    /* [B][T-1] as jd_verify writes them; read unless mode is JD_MODE_STANDARD */
+  float tau;                    /* 0..1 */
+  int32_t mode, resample;       /* jd_mode_t, jd_resample_t */
+  int32_t siblings;             /* jd_siblings_t */
+  int32_t* accept_len;          /* [B] accepted tokens along the path */
+  int32_t* next_token;          /* [B] */
+  int32_t* path;                /* [B][T-1] nodes of the path, -1 behind its end (jd_cache_commit takes it with num_paths 1), or NULL */
+  uint32_t* device_status;      /* DEVICE word that becomes the first problem if it holds JD_OK: JD_ERR_BAD_TOKEN (a token outside 0..V-1 is
+                                   never accepted), JD_ERR_BAD_INDEX (a node whose parent does not come before it is no child), or NULL */
+} jd_verify_probs_args_t;
+
+/* Speculative sampling from probabilities that are there already, of chains and trees, by random numbers that are given. From node 0 on, with
+ * w = the target's weights, W = 1, q = the draft's and Q = 1, a node's children are tried in the order of their numbers: token x is accepted
+ * where u W q(x) < w(x) Q (or its judge score exceeds tau, by mode), and the walk goes on at that child; else w becomes max(0, w Q - W q) and W its
+ * sum, and of distinct siblings q(x) becomes 0 and Q less by it. Where no child is left the next token is the first whose running sum of w
+ * exceeds u W; with JD_RESAMPLE_TARGET_P, and where w is zero, of the target's own weights. A row without mass gives V - 1. Probabilities are taken
+ * as they are (finite, not negative; sums need not be 1), all arithmetic is float64. Asynchronous on the stream; uses the current device; no
+ * workspace. */
+jd_status_t jd_verify_probs(const jd_verify_probs_args_t* args, void* cuda_stream);
+
 /* =========================================================================================
  * Around the verification call: rotary positions, a paged key / value cache and the attention
  * of a drafted block over it. One decoding step of a target layer stack is
@@ -349,6 +389,66 @@ typedef struct {
  * for every token and head. The angle is formed and reduced in float64, so that far positions lose nothing;
  * the products are float32, rounded once. Asynchronous on the stream; uses the current device. */
 jd_status_t jd_rope(const jd_rope_args_t* args, void* cuda_stream);
+
+/* Several position axes (time, row and column of an image, say): every frequency takes one of a token's positions. */
+typedef struct {
+  int32_t num_axes;           /* 1..4 positions of a token */
+  const uint8_t* axis_of;     /* HOST [rot_dim / 2], each < num_axes: the axis of every frequency; NULL: all 0. Read during the call */
+} jd_rope_axes_t;
+
+/* RMS norms of the heads of queries and of keys: x w / sqrt(mean(x^2) + eps) over head_dim, in front of the rotation. */
+typedef struct {
+  const float* q_weight;      /* DEVICE [head_dim], 4-byte aligned; NULL: ones */
+  const float* k_weight;
+  float eps;                  /* >= 0 and finite */
+} jd_head_norm_t;
+
+typedef struct {
+  int64_t tokens;             /* 0..2^31 - 1; 0 launches nothing */
+  int32_t q_heads, k_heads;   /* 0..65536 each, one at least */
+  int32_t head_dim;           /* 1..256 */
+  int32_t dtype;              /* JD_DTYPE_F32 or JD_DTYPE_BF16 */
+  int32_t inverse;            /* 1: turn by the negative angle; without norm only (norms have jd_head_rope_grad) */
+  const void* q;              /* [tokens][q_heads][head_dim], q_stride elements between tokens (0: dense); not read if q_heads is 0 */
+  const void* k;              /* [tokens][k_heads][head_dim], k_stride */
+  void* q_out;                /* like q; out == in with the same stride is allowed, any other overlap is undefined */
+  void* k_out;
+  int64_t q_stride, k_stride, q_out_stride, k_out_stride;
+  const int32_t* positions;   /* [tokens][num_axes], any int32 */
+  jd_rope_t rope;
+  const jd_head_norm_t* norm; /* HOST struct; NULL: the rotation alone */
+  const jd_rope_axes_t* axes; /* HOST struct; NULL: one axis */
+} jd_head_rope_args_t;
+
+/* Norms of query and key heads and their rotation in one pass; statistics and products are float32, rounded once at the end. The sum
+ * of a head's squares has to stay below float32's largest number. Asynchronous on the stream; uses the current device. */
+jd_status_t jd_head_rope(const jd_head_rope_args_t* args, void* cuda_stream);
+
+typedef struct {
+  int64_t tokens;
+  int32_t q_heads, k_heads, head_dim, dtype;
+  const void* q;              /* the inputs of the forward call */
+  const void* k;
+  const void* q_out_grad;     /* gradients of its outputs, same shapes and type */
+  const void* k_out_grad;
+  void* q_grad;               /* gradients of its inputs; may be q_out_grad or q itself (k's likewise) with the same stride */
+  void* k_grad;
+  int64_t q_stride, k_stride, q_out_grad_stride, k_out_grad_stride, q_grad_stride, k_grad_stride;
+  const int32_t* positions;
+  jd_rope_t rope;
+  const jd_head_norm_t* norm; /* required */
+  const jd_rope_axes_t* axes;
+  float* q_weight_grad;       /* [head_dim] summed over tokens and heads in a fixed order, or NULL. No heads or no tokens: zeroes */
+  float* k_weight_grad;
+  void* workspace;            /* jd_head_rope_grad_workspace_bytes(), 4-byte aligned; NULL without weight gradients. Calls that may
+                                 run at the same time take one each */
+  size_t workspace_bytes;
+} jd_head_rope_grad_args_t;
+
+size_t jd_head_rope_grad_workspace_bytes(int32_t head_dim);   /* 0: invalid */
+
+/* Backward pass of jd_head_rope with a norm: nothing but its inputs is kept from the forward call. Results repeat bit for bit. */
+jd_status_t jd_head_rope_grad(const jd_head_rope_grad_args_t* args, void* cuda_stream);
 
 /* ---------------------------------------------------------------- paged cache */
 
@@ -434,6 +534,15 @@ typedef struct {
  * seq_len + j, and the turned queries to q_out. seq_len stays. Rows whose page is missing or has other owners are
  * skipped and reported (jd_cache_reserve has to come first). Pointers 16-byte aligned, strides multiples of 16 bytes. */
 jd_status_t jd_cache_append(jd_cache_t c, const jd_append_args_t* args, void* cuda_stream);
+
+typedef struct {
+  const jd_head_norm_t* norm;  /* HOST struct: queries and keys are normalised in front of the rotation; NULL: not */
+  const jd_rope_axes_t* axes;  /* HOST struct: axes of args->rope; NULL: one */
+  const int32_t* positions;    /* [B][T][num_axes] in place of seq_len + depth; NULL: those, on every axis */
+} jd_append_heads_t;
+
+/* jd_cache_append with norms of the heads, several position axes or positions of the caller's, in the same pass. */
+jd_status_t jd_cache_append_heads(jd_cache_t c, const jd_append_args_t* args, const jd_append_heads_t* heads, void* cuda_stream);
 
 /* Kernel family of jd_cache_attend. TENSOR: tcgen05 kernel, bf16 with head_dim 64 or 128. SIMT: any cache. */
 typedef enum { JD_ATTEND_AUTO = 0, JD_ATTEND_SIMT = 1, JD_ATTEND_TENSOR = 2 } jd_attend_variant_t;

@@ -51,6 +51,9 @@ def _require(ok: bool, what: str) -> None:
 _raw_stream = torch._C._cuda_getCurrentRawStream
 _TREE = "iiPPP"
 _ROPE_ARGS = struct.Struct("@qiiiiPPqqPPiif")
+_HEAD_ROPE_ARGS = struct.Struct("@qiiiiiPPPPqqqqPPiifPP")
+_HEAD_ROPE_GRAD_ARGS = struct.Struct("@qiiiiPPPPPPqqqqqqPPiifPPPPPN")
+_APPEND_HEADS_ARGS = struct.Struct("@PPP")
 _APPEND_ARGS = struct.Struct("@iiP" + _TREE + "PPPPqqqqP")
 _ATTEND_ARGS = struct.Struct("@iiP" + _TREE + "PPqqPfi")
 _COMMIT_ARGS = struct.Struct("@iPPiiPP")
@@ -84,10 +87,33 @@ def rope_frequencies(rot_dim: int, base: float = 500000.0, scaling: Optional[str
     return out, amplitude.value
 
 
-class Rotary:
-    """Rotary positions: frequencies [rot_dim / 2] (float32, on the device), layout and amplitude."""
+class HeadNorm:
+    """RMS norms of query and key heads, x w / sqrt(mean(x ** 2) + eps): weights [head_dim] (float32, on the device; None: ones)."""
 
-    def __init__(self, inv_freq: torch.Tensor, layout: str = "half", amplitude: float = 1.0):
+    def __init__(self, q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6):
+        given = [w for w in (q_weight, k_weight) if w is not None]
+        for w in given:
+            _require(w.dtype == torch.float32 and w.is_contiguous() and w.dim() == 1 and w.is_cuda, "weights: contiguous float32 vectors on the device")
+            _require(not w.requires_grad, "weights: no autograd here; detach them")
+            _require(w.shape == given[0].shape and w.device == given[0].device, "weights: of one head_dim, on one device")
+        _require(eps >= 0 and math.isfinite(eps), "eps: not negative, finite")
+        self.q_weight, self.k_weight, self.eps = q_weight, k_weight, float(eps)
+        self.head_dim = given[0].shape[0] if given else None
+        self.index = given[0].get_device() if given else None
+        self.c = jd.jd_head_norm_t(*(0 if w is None else w.data_ptr() for w in (q_weight, k_weight)), self.eps)
+        self.ref = C.addressof(self.c)
+
+    def _of(self, head_dim: int, index: int) -> int:
+        if self.head_dim is not None and (self.head_dim != head_dim or self.index != index):
+            raise ValueError("norm: weights [head_dim] on the call's device")
+        return self.ref
+
+
+class Rotary:
+    """Rotary positions: frequencies [rot_dim / 2] (float32, on the device), layout and amplitude. axes: the position axis of every
+    frequency (host numbers from 0, at most four axes; a token then has a position on each), None: one axis."""
+
+    def __init__(self, inv_freq: torch.Tensor, layout: str = "half", amplitude: float = 1.0, axes=None):
         _require(inv_freq.dtype == torch.float32 and inv_freq.is_contiguous() and inv_freq.dim() == 1,
                  "inv_freq: a contiguous float32 vector")
         _require(not inv_freq.requires_grad, "inv_freq: no autograd here; detach it")
@@ -97,12 +123,20 @@ class Rotary:
         self.c = jd.jd_rope_t(inv_freq.data_ptr(), self.rot_dim, self._layout, self.amplitude)
         self.ref = C.addressof(self.c)
         self.index = inv_freq.get_device()
+        self.num_axes, self.axes_ref = 1, 0
+        if axes is not None:
+            axes = [int(a) for a in axes]
+            _require(len(axes) == inv_freq.numel() and len(axes) > 0 and min(axes) >= 0 and max(axes) < 4, "axes: one of 0..3 for each frequency")
+            self.num_axes = max(axes) + 1
+            self._axis_of = (C.c_uint8 * len(axes))(*axes)
+            self._axes = jd.jd_rope_axes_t(self.num_axes, C.addressof(self._axis_of))
+            self.axes_ref = C.addressof(self._axes)
         self._lib = jd.load()
 
     def rotate(self, x: torch.Tensor, positions: torch.Tensor, out: Optional[torch.Tensor] = None, inverse: bool = False,
                stream=None) -> torch.Tensor:
-        """Turns x [tokens, heads, head_dim] (tokens may be strided) to its positions [tokens] (int32). ``inverse`` turns back: with
-        the gradient of the output as x, the result is the gradient of the input. ``out`` may be x."""
+        """Turns x [tokens, heads, head_dim] (tokens may be strided) to its positions [tokens] (int32; with axes [tokens, axes]). ``inverse``
+        turns back: with the gradient of the output as x, the result is the gradient of the input. ``out`` may be x."""
         if x.dim() != 3 or x.dtype not in _DTYPES or not x.is_cuda:
             raise ValueError("x: [tokens, heads, head_dim], float32 or bfloat16, on the device")
         n, heads, dim = x.shape
@@ -112,28 +146,125 @@ class Rotary:
         elif out.shape != x.shape or out.dtype is not x.dtype or out.get_device() != index:
             raise ValueError("out: like x")
         x_step, out_step = self._step(x, "x", n, heads, dim), self._step(out, "out", n, heads, dim)
-        at = _ints(positions, "positions", index, (n,))
-        if self.index != index:
-            raise ValueError("inv_freq and x on one device")
+        at = self._positions(positions, index, n)
         if n == 0:
+            return out
+        if self.axes_ref:
+            a = jd.jd_head_rope_args_t()
+            _HEAD_ROPE_ARGS.pack_into(a, 0, n, heads, 0, dim, _DTYPES[x.dtype], 1 if inverse else 0, x.data_ptr(), 0, out.data_ptr(), 0, x_step, 0,
+                                      out_step, 0, at, self.inv_freq.data_ptr(), self.rot_dim, self._layout, self.amplitude, 0, self.axes_ref)
+            self._call("jd_head_rope", a, index, stream)
             return out
         a = jd.jd_rope_args_t()
         _ROPE_ARGS.pack_into(a, 0, n, heads, dim, _DTYPES[x.dtype], 1 if inverse else 0, x.data_ptr(), out.data_ptr(), x_step, out_step, at,
                              self.inv_freq.data_ptr(), self.rot_dim, self._layout, self.amplitude)
-        if torch._C._cuda_getDevice() == index:
-            st = self._lib.jd_rope(a, _stream(stream, index))
-        else:
-            with torch.cuda.device(index):
-                st = self._lib.jd_rope(a, _stream(stream, index))
-        if st != jd.JD_OK:
-            raise jd.JdError(st, "jd_rope")
+        self._call("jd_rope", a, index, stream)
         return out
 
+    def rotate_qk(self, q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, norm: Optional[HeadNorm] = None,
+                  q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, stream=None):
+        """Queries and keys [tokens, heads, head_dim] (tokens may be strided) in one pass: normalised (``norm``), then turned to their positions
+        [tokens] or, with axes, [tokens, axes]. Returns (q_out, k_out), which may be q and k; k may be None."""
+        n, dim, index, heads = self._pair(q, k)
+        outs = []
+        for x, out, name in ((q, q_out, "q_out"), (k, k_out, "k_out")):
+            if x is None:
+                out = None
+            elif out is None:
+                out = x.new_empty(tuple(x.shape))
+            elif out.shape != x.shape or out.dtype is not x.dtype or out.get_device() != index:
+                raise ValueError("%s: like its input" % name)
+            outs.append(out)
+        steps = [0 if x is None else self._step(x, name, n, h, dim, "the gradient is rotate_qk_grad()")
+                 for x, name, h in ((q, "q", heads[0]), (k, "k", heads[1]), (outs[0], "q_out", heads[0]), (outs[1], "k_out", heads[1]))]
+        at = self._positions(positions, index, n)
+        norm_ref = 0 if norm is None else norm._of(dim, index)
+        if n > 0:
+            a = jd.jd_head_rope_args_t()
+            _HEAD_ROPE_ARGS.pack_into(a, 0, n, *heads, dim, _DTYPES[q.dtype], 0, *(0 if x is None else x.data_ptr() for x in (q, k, *outs)), *steps, at,
+                                      self.inv_freq.data_ptr(), self.rot_dim, self._layout, self.amplitude, norm_ref, self.axes_ref)
+            self._call("jd_head_rope", a, index, stream)
+        return outs[0], outs[1]
+
+    def rotate_qk_grad(self, q_out_grad: torch.Tensor, k_out_grad: Optional[torch.Tensor], q: torch.Tensor, k: Optional[torch.Tensor],
+                       positions: torch.Tensor, norm: HeadNorm, out: Optional[dict] = None, weights: bool = True,
+                       workspace: Optional[torch.Tensor] = None, stream=None) -> dict:
+        """Backward pass of :meth:`rotate_qk` with a norm: the gradients of its outputs and its inputs give a dict with "q", "k" (the inputs'
+        gradients) and, unless ``weights`` is False, "q_weight", "k_weight" (float32 [head_dim], set, not added to). ``out``: such a dict with
+        tensors to use. ``workspace``: uint8, ``jd_head_rope_grad_workspace_bytes`` of them; calls that may run at the same time take one each."""
+        n, dim, index, heads = self._pair(q, k)
+        got = dict(out or {})
+        if (k is None) != (k_out_grad is None):
+            raise ValueError("k, k_out_grad: both or neither")
+        for name, x, g in (("q", q, q_out_grad), ("k", k, k_out_grad)):
+            if x is None:
+                got[name] = None
+                continue
+            if got.get(name) is None:
+                got[name] = x.new_empty(tuple(x.shape))
+            for y, what in ((g, name + "_out_grad"), (got[name], "out: " + name)):
+                if y.shape != x.shape or y.dtype is not x.dtype or y.get_device() != index:
+                    raise ValueError("%s: like its input" % what)
+        wptr = [0, 0]
+        for i, name in enumerate(("q_weight", "k_weight")):
+            if not weights:
+                got.pop(name, None)
+                continue
+            if got.get(name) is None:
+                got[name] = q.new_empty((dim,), dtype=torch.float32)
+            w = got[name]
+            if w.shape != (dim,) or w.dtype is not torch.float32 or not w.is_contiguous() or w.get_device() != index or w.requires_grad:
+                raise ValueError("%s: a contiguous float32 vector [head_dim] on the device" % name)
+            wptr[i] = w.data_ptr()
+        need = 0
+        if weights:
+            need = self._lib.jd_head_rope_grad_workspace_bytes(dim)
+            if workspace is None:
+                workspace = q.new_empty((max(need, 4),), dtype=torch.uint8)
+            elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.numel() < need or workspace.get_device() != index:
+                raise ValueError("workspace: %d contiguous bytes (uint8) on the device" % need)
+        steps = [0 if x is None else self._step(x, name, n, h, dim, "this is the gradient")
+                 for x, name, h in ((q, "q", heads[0]), (k, "k", heads[1]), (q_out_grad, "q_out_grad", heads[0]), (k_out_grad, "k_out_grad", heads[1]),
+                                    (got["q"], "out: q", heads[0]), (got["k"], "out: k", heads[1]))]
+        at = self._positions(positions, index, n)
+        a = jd.jd_head_rope_grad_args_t()
+        _HEAD_ROPE_GRAD_ARGS.pack_into(a, 0, n, *heads, dim, _DTYPES[q.dtype], *(0 if x is None else x.data_ptr() for x in (
+                                           q, k, q_out_grad, k_out_grad, got["q"], got["k"])), *steps, at, self.inv_freq.data_ptr(), self.rot_dim,
+                                       self._layout, self.amplitude, norm._of(dim, index), self.axes_ref, *wptr,
+                                       workspace.data_ptr() if weights else 0, need)
+        self._call("jd_head_rope_grad", a, index, stream)
+        return got
+
+    def _pair(self, q, k):
+        """(tokens, head_dim, device, (heads of q, heads of k)) of a call on queries and keys."""
+        if q.dim() != 3 or q.dtype not in _DTYPES or not q.is_cuda:
+            raise ValueError("q: [tokens, heads, head_dim], float32 or bfloat16, on the device")
+        n, heads, dim = q.shape
+        if k is not None and (k.dim() != 3 or k.shape[0] != n or k.shape[2] != dim or k.dtype is not q.dtype or k.get_device() != q.get_device()):
+            raise ValueError("k: [tokens, heads, head_dim] like q")
+        return n, dim, q.get_device(), (heads, 0 if k is None else k.shape[1])
+
+    def _positions(self, positions: torch.Tensor, index: int, n: int) -> int:
+        at = _ints(positions, "positions", index, (n,) if not self.axes_ref else (n, self.num_axes))
+        if self.index != index:
+            raise ValueError("inv_freq and x on one device")
+        return at
+
+    def _call(self, name: str, args, index: int, stream) -> None:
+        call = getattr(self._lib, name)
+        if torch._C._cuda_getDevice() == index:
+            st = call(args, _stream(stream, index))
+        else:
+            with torch.cuda.device(index):
+                st = call(args, _stream(stream, index))
+        if st != jd.JD_OK:
+            raise jd.JdError(st, name)
+
     @staticmethod
-    def _step(t: torch.Tensor, name: str, n: int, heads: int, dim: int) -> int:
+    def _step(t: torch.Tensor, name: str, n: int, heads: int, dim: int, gradient: str = "the gradient is rotate(grad, positions, inverse=True)") -> int:
         """Elements between tokens, 0: dense."""
         if t.requires_grad and torch.is_grad_enabled() or _fw._current_level >= 0 and _has_tangent(t):
-            raise ValueError("%s: no autograd here; detach it, the gradient is rotate(grad, positions, inverse=True)" % name)
+            raise ValueError("%s: no autograd here; detach it, %s" % (name, gradient))
         if t.is_contiguous():
             return 0
         step, by_head, by_element = t.stride()
@@ -307,9 +438,11 @@ class PagedCache:
             raise jd.JdError(st, "jd_cache_reserve")
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, tree: Optional[Tree] = None, rotary: Optional[Rotary] = None,
-               q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None, stream=None):
+               q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None, stream=None,
+               norm: Optional[HeadNorm] = None, positions: Optional[torch.Tensor] = None):
         """Writes a block's keys and values [B, T, kv_heads, head_dim] behind the sequences' tokens, turned to their positions,
-        and returns the turned queries (q_out; a new tensor if None), or None without q."""
+        and returns the turned queries (q_out; a new tensor if None), or None without q. norm: queries and keys are normalised in front of
+        the rotation. positions: [B, T] (int32; [B, T, axes] where the rotary has axes) in place of seq_len + depth, which count on every axis."""
         if k.dim() != 4:
             raise ValueError("k, v: [B, T, kv_heads, head_dim]")
         B, T, _, D = k.shape
@@ -334,7 +467,18 @@ class PagedCache:
             rope = rotary.ref
         a = jd.jd_append_args_t()
         _APPEND_ARGS.pack_into(a, 0, B, layer, at, t0, t1, t2, t3, t4, k.data_ptr(), v.data_ptr(), q_ptr, o_ptr, k_step, v_step, q_step, o_step, rope)
-        st = self._lib.jd_cache_append(self.h, a, _stream(stream, self.index))
+        if norm is None and positions is None and (rotary is None or rotary.axes_ref == 0):
+            st = self._lib.jd_cache_append(self.h, a, _stream(stream, self.index))
+        else:
+            axes = 0 if rotary is None else rotary.axes_ref
+            where = 0
+            if positions is not None:
+                if rotary is None:
+                    raise ValueError("positions: of a rotary")
+                where = _ints(positions, "positions", self.index, (B, T) if axes == 0 else (B, T, rotary.num_axes))
+            x = jd.jd_append_heads_t()
+            _APPEND_HEADS_ARGS.pack_into(x, 0, 0 if norm is None else norm._of(D, self.index), axes, where)
+            st = self._lib.jd_cache_append_heads(self.h, a, x, _stream(stream, self.index))
         if st != jd.JD_OK:
             raise jd.JdError(st, "jd_cache_append")
         return q_out

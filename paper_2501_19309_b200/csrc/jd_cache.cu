@@ -523,6 +523,20 @@ bool tree_ok(jd_cache_t c, const jd_tree_t& t) {
   return t.nodes >= 1 && t.nodes <= c->cfg.max_nodes && (t.per_seq == 0 || t.per_seq == 1) && on4(t.mask) && on4(t.depth) && on4(t.num_nodes);
 }
 
+bool append_ok(jd_cache_t c, const jd_append_args_t* a) {
+  if (!c || !a || !batch_ok(c, a->B, a->slots) || !tree_ok(c, a->tree)) return false;
+  const jd_cache_config_t& g = c->cfg;
+  const int e = g.dtype == JD_DTYPE_F32 ? 4 : 2;
+  if (a->layer < 0 || a->layer >= g.num_layers || !a->k || !a->v || !on16(a->k) || !on16(a->v)) return false;
+  const int64_t kd = (int64_t)g.kv_heads * g.head_dim, qd = (int64_t)g.q_heads * g.head_dim;
+  if (!stride_ok(a->k_stride, kd, e) || !stride_ok(a->v_stride, kd, e)) return false;
+  if (a->q) {
+    if (!a->q_out || !on16(a->q) || !on16(a->q_out) || !stride_ok(a->q_stride, qd, e) || !stride_ok(a->q_out_stride, qd, e)) return false;
+    if (a->q == a->q_out && (a->q_stride ? a->q_stride : qd) != (a->q_out_stride ? a->q_out_stride : qd)) return false;
+  }
+  return !a->rope || rope_valid(*a->rope, g.head_dim);
+}
+
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                   const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -609,20 +623,17 @@ jd_status_t jd_cache_reserve(jd_cache_t c, int32_t B, const int32_t* slots, int3
 }
 
 jd_status_t jd_cache_append(jd_cache_t c, const jd_append_args_t* a, void* cuda_stream) {
-  if (!c || !a || !batch_ok(c, a->B, a->slots) || !tree_ok(c, a->tree)) return JD_ERR_INVALID_ARG;
-  const jd_cache_config_t& g = c->cfg;
-  const int e = g.dtype == JD_DTYPE_F32 ? 4 : 2;
-  if (a->layer < 0 || a->layer >= g.num_layers || !a->k || !a->v || !on16(a->k) || !on16(a->v)) return JD_ERR_INVALID_ARG;
-  const int64_t kd = (int64_t)g.kv_heads * g.head_dim, qd = (int64_t)g.q_heads * g.head_dim;
-  if (!stride_ok(a->k_stride, kd, e) || !stride_ok(a->v_stride, kd, e)) return JD_ERR_INVALID_ARG;
-  if (a->q) {
-    if (!a->q_out || !on16(a->q) || !on16(a->q_out) || !stride_ok(a->q_stride, qd, e) || !stride_ok(a->q_out_stride, qd, e)) return JD_ERR_INVALID_ARG;
-    if (a->q == a->q_out && (a->q_stride ? a->q_stride : qd) != (a->q_out_stride ? a->q_out_stride : qd)) return JD_ERR_INVALID_ARG;
-  }
-  if (a->rope && !rope_valid(*a->rope, g.head_dim)) return JD_ERR_INVALID_ARG;
-  OnDevice dev(g.device);
+  if (!append_ok(c, a)) return JD_ERR_INVALID_ARG;
+  OnDevice dev(c->cfg.device);
   if (!dev.ok()) return JD_ERR_CUDA;
-  return finish(c, run_append(view_of(c), *a, g.q_heads, g.dtype, (cudaStream_t)cuda_stream), (cudaStream_t)cuda_stream);
+  return finish(c, run_append(view_of(c), *a, c->cfg.q_heads, c->cfg.dtype, (cudaStream_t)cuda_stream), (cudaStream_t)cuda_stream);
+}
+
+jd_status_t jd_cache_append_heads(jd_cache_t c, const jd_append_args_t* a, const jd_append_heads_t* x, void* cuda_stream) {
+  if (!append_ok(c, a) || !x || !append_heads_valid(x->norm, x->axes, a->rope) || !on4(x->positions)) return JD_ERR_INVALID_ARG;
+  OnDevice dev(c->cfg.device);
+  if (!dev.ok()) return JD_ERR_CUDA;
+  return finish(c, run_append_heads(view_of(c), *a, *x, c->cfg.q_heads, c->cfg.dtype, (cudaStream_t)cuda_stream), (cudaStream_t)cuda_stream);
 }
 
 jd_status_t jd_cache_attend(jd_cache_t c, const jd_attend_args_t* a, void* cuda_stream) {

@@ -250,5 +250,7 @@ constexpr int tensor_seg_cost(int head_dim, int rows) { return head_dim == 64 ? 
 
 bool rope_valid(const jd_rope_t& r, int head_dim);
 cudaError_t run_append(const CacheView& c, const jd_append_args_t& a, int q_heads, int dtype, cudaStream_t st);
+bool append_heads_valid(const jd_head_norm_t* n, const jd_rope_axes_t* a, const jd_rope_t* r);
+cudaError_t run_append_heads(const CacheView& c, const jd_append_args_t& a, const jd_append_heads_t& x, int q_heads, int dtype, cudaStream_t st);
 
 }  // namespace jd

@@ -10,50 +10,14 @@
 #include <algorithm>
 #include <cmath>
 
-#include "jd_cache.h"
+#include "jd_rope.cuh"
 
 namespace jd {
 namespace {
 
 constexpr int kRopeThreads = 256;
 constexpr int kRopeUnitsPerThread = 4;
-constexpr int kMaxHalf = 128;   // rot_dim / 2
 constexpr int kTokensPerBlock = 8;
-
-__device__ __forceinline__ float2 turn_of(int pos, float freq, float amplitude, bool inverse) {
-  const double turns = (double)pos * ((double)freq * 0.15915494309189533577);   // 1 / (2 pi)
-  const float half_turns = (float)(2.0 * (turns - rint(turns)));
-  float s, c;
-  sincospif(half_turns, &s, &c);
-  return make_float2(c * amplitude, (inverse ? -s : s) * amplitude);
-}
-
-// 8 elements of a head as float32, one or two 16-byte accesses
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float* v) {
-  const uint4 u = *reinterpret_cast<const uint4*>(p);
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
-}
-__device__ __forceinline__ void load8(const float* p, float* v) {
-  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-}
-__device__ __forceinline__ void store8(__nv_bfloat16* p, const float* v) {
-  uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-    w[i] = *reinterpret_cast<const uint32_t*>(&h);
-  }
-  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-}
-__device__ __forceinline__ void store8(float* p, const float* v) {
-  reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-  reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-}
-__device__ __forceinline__ float from_float(float v, float) { return v; }
-__device__ __forceinline__ __nv_bfloat16 from_float(float v, __nv_bfloat16) { return __float2bfloat16_rn(v); }
 
 // One unit of a head: the unit-th piece that turns, or behind those a piece that passes through.
 // kVec: pieces of 8 elements, rot_dim % 16 == 0, head_dim % 8 == 0 and 16-byte rows; else single pairs / elements.
@@ -225,9 +189,6 @@ bool rope_ok(const jd_rope_t& r, int head_dim) {
          r.rot_dim <= head_dim && r.rot_dim <= 2 * kMaxHalf && (r.layout == JD_ROPE_HALF || r.layout == JD_ROPE_INTERLEAVED) &&
          std::isfinite(r.amplitude);
 }
-
-// pieces of 8 elements: whole pieces turn together and rows start on 16 bytes
-bool vec_ok(int rot_dim, int head_dim) { return rot_dim % 16 == 0 && head_dim % 8 == 0; }
 
 template <typename T>
 cudaError_t launch_rope(const jd_rope_args_t& a, int64_t xs, int64_t os, cudaStream_t st) {

@@ -29,6 +29,7 @@ JD_RULE_SAMPLING, JD_RULE_TOPK = 0, 1
 JD_NORM_NONE, JD_NORM_RMS = 0, 1
 JD_ROPE_HALF, JD_ROPE_INTERLEAVED = 0, 1
 JD_ROPE_SCALE_NONE, JD_ROPE_SCALE_LINEAR, JD_ROPE_SCALE_BANDS, JD_ROPE_SCALE_YARN = 0, 1, 2, 3
+JD_SIBLINGS_INDEPENDENT, JD_SIBLINGS_DISTINCT = 0, 1
 JD_ATTEND_AUTO, JD_ATTEND_SIMT, JD_ATTEND_TENSOR = 0, 1, 2
 
 MODES = {"standard": JD_MODE_STANDARD, "judge": JD_MODE_JUDGE, "judge_or_standard": JD_MODE_JUDGE_OR_STANDARD}
@@ -42,7 +43,9 @@ EXPORTS = ["jd_version", "jd_status_string", "jd_workspace_bytes", "jd_create", 
            "jd_quantize_rows_e4m3", "jd_check_workspace_guards", "jd_selftest_stale_timeout",
            "jd_debug_phase_stamps", "jd_rope_frequencies", "jd_rope", "jd_cache_workspace_bytes", "jd_cache_create",
            "jd_cache_destroy", "jd_cache_reserve", "jd_cache_append", "jd_cache_attend", "jd_cache_commit",
-           "jd_cache_fork", "jd_cache_truncate", "jd_cache_compact", "jd_cache_last_status"]
+           "jd_cache_fork", "jd_cache_truncate", "jd_cache_compact", "jd_cache_last_status", "jd_head_rope",
+           "jd_head_rope_grad", "jd_head_rope_grad_workspace_bytes", "jd_cache_append_heads",
+           "jd_verify_probs"]
 
 
 class jd_config_t(C.Structure):
@@ -67,6 +70,42 @@ class jd_rope_args_t(C.Structure):
     _fields_ = [("tokens", C.c_int64), ("heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
                 ("inverse", C.c_int32), ("x", C.c_void_p), ("out", C.c_void_p), ("x_stride", C.c_int64),
                 ("out_stride", C.c_int64), ("positions", C.c_void_p), ("rope", jd_rope_t)]
+
+
+class jd_rope_axes_t(C.Structure):
+    _fields_ = [("num_axes", C.c_int32), ("axis_of", C.c_void_p)]
+
+
+class jd_head_norm_t(C.Structure):
+    _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("eps", C.c_float)]
+
+
+class jd_head_rope_args_t(C.Structure):
+    _fields_ = [("tokens", C.c_int64)] + [(n, C.c_int32) for n in ("q_heads", "k_heads", "head_dim", "dtype", "inverse")] + \
+               [(n, C.c_void_p) for n in ("q", "k", "q_out", "k_out")] + \
+               [(n, C.c_int64) for n in ("q_stride", "k_stride", "q_out_stride", "k_out_stride")] + \
+               [("positions", C.c_void_p), ("rope", jd_rope_t), ("norm", C.c_void_p), ("axes", C.c_void_p)]
+
+
+class jd_head_rope_grad_args_t(C.Structure):
+    _fields_ = [("tokens", C.c_int64)] + [(n, C.c_int32) for n in ("q_heads", "k_heads", "head_dim", "dtype")] + \
+               [(n, C.c_void_p) for n in ("q", "k", "q_out_grad", "k_out_grad", "q_grad", "k_grad")] + \
+               [(n, C.c_int64) for n in ("q_stride", "k_stride", "q_out_grad_stride", "k_out_grad_stride", "q_grad_stride", "k_grad_stride")] + \
+               [("positions", C.c_void_p), ("rope", jd_rope_t)] + \
+               [(n, C.c_void_p) for n in ("norm", "axes", "q_weight_grad", "k_weight_grad", "workspace")] + [("workspace_bytes", C.c_size_t)]
+
+
+class jd_append_heads_t(C.Structure):
+    _fields_ = [("norm", C.c_void_p), ("axes", C.c_void_p), ("positions", C.c_void_p)]
+
+
+class jd_verify_probs_args_t(C.Structure):
+    _fields_ = [("B", C.c_int32), ("nodes", C.c_int32), ("V", C.c_int32), ("dtype", C.c_int32), ("target", C.c_void_p),
+                ("draft", C.c_void_p), ("target_stride", C.c_int64), ("draft_stride", C.c_int64), ("tokens", C.c_void_p),
+                ("parents", C.c_void_p), ("per_seq", C.c_int32), ("num_nodes", C.c_void_p), ("accept_u", C.c_void_p),
+                ("sample_u", C.c_void_p), ("judge_scores", C.c_void_p), ("tau", C.c_float), ("mode", C.c_int32),
+                ("resample", C.c_int32), ("siblings", C.c_int32), ("accept_len", C.c_void_p), ("next_token", C.c_void_p),
+                ("path", C.c_void_p), ("device_status", C.c_void_p)]
 
 
 class jd_cache_config_t(C.Structure):
@@ -147,6 +186,11 @@ def load():
     lib.jd_rope_frequencies.argtypes = [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_double, C.c_double, C.c_double,
                                         C.c_void_p, C.c_void_p]
     lib.jd_rope.argtypes = [C.POINTER(jd_rope_args_t), C.c_void_p]
+    lib.jd_verify_probs.argtypes = [C.POINTER(jd_verify_probs_args_t), C.c_void_p]
+    lib.jd_head_rope.argtypes = [C.POINTER(jd_head_rope_args_t), C.c_void_p]
+    lib.jd_head_rope_grad.argtypes = [C.POINTER(jd_head_rope_grad_args_t), C.c_void_p]
+    lib.jd_head_rope_grad_workspace_bytes.argtypes = [C.c_int32]
+    lib.jd_cache_append_heads.argtypes = [C.c_void_p, C.POINTER(jd_append_args_t), C.POINTER(jd_append_heads_t), C.c_void_p]
     lib.jd_cache_workspace_bytes.restype = C.c_size_t
     lib.jd_cache_workspace_bytes.argtypes = [C.POINTER(jd_cache_config_t)]
     lib.jd_cache_create.argtypes = [C.POINTER(C.c_void_p), C.POINTER(jd_cache_config_t), C.POINTER(jd_cache_buffers_t)]
@@ -160,7 +204,9 @@ def load():
     lib.jd_cache_compact.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p]
     lib.jd_cache_last_status.argtypes = [C.c_void_p, C.POINTER(C.c_int)]
     for name in EXPORTS:
-        if name not in ("jd_version", "jd_status_string", "jd_workspace_bytes", "jd_cache_workspace_bytes"):
+        if name.endswith("workspace_bytes"):
+            getattr(lib, name).restype = C.c_size_t
+        elif name not in ("jd_version", "jd_status_string"):
             getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib
@@ -400,7 +446,10 @@ class Verifier:
 
 # ------------------------------------------------------------------ around the verification call (cache.py)
 def __getattr__(name: str):
-    if name in ("PagedCache", "Rotary", "Tree", "rope_frequencies", "mask_words"):     # torch is imported on first use only
+    if name in ("PagedCache", "Rotary", "HeadNorm", "Tree", "rope_frequencies", "mask_words"):     # torch is imported on first use only
         from . import cache
         return getattr(cache, name)
+    if name == "verify_probs":
+        from . import probs
+        return probs.verify_probs
     raise AttributeError("module %r has no attribute %r" % (__name__, name))
