@@ -569,6 +569,28 @@ typedef struct {
  * number of tokens has to stay below 2^119. Pointers 16-byte aligned, strides multiples of 16 bytes. */
 jd_status_t jd_cache_attend(jd_cache_t c, const jd_attend_args_t* args, void* cuda_stream);
 
+/* Sequences whose leading pages are the same (forks, samples of one prompt, requests behind one system prompt): a plan lets their attention
+ * read those pages once for all of them. HOST struct. The buffer is the caller's, on the cache's device: 256-byte aligned,
+ * jd_cache_shared_bytes() of it, zero-filled before its first use; calls that may run at the same time take a plan each. */
+typedef struct {
+  int32_t B;          /* sequences of the calls, 1..1024 */
+  int32_t nodes;      /* most nodes of a call, 1..max_nodes */
+  void* buffer;
+  size_t bytes;
+} jd_shared_t;
+
+size_t jd_cache_shared_bytes(jd_cache_t c, int32_t B, int32_t nodes);   /* 0: invalid */
+
+/* Finds on the device which of the B sequences hold the same pages in front, as the tables stand. groups: device [B], entries with the same
+ * number (not below 0) are compared; NULL: those with the same first page. A group's prefix is what all its members have in common with its first
+ * entry, in whole 128 tokens of full pages; groups that would save too little stay apart. Once for all layers of a step, behind
+ * jd_cache_reserve or in front of it. */
+jd_status_t jd_cache_share(jd_cache_t c, const jd_shared_t* plan, const int32_t* slots, const int32_t* groups, void* cuda_stream);
+
+/* jd_cache_attend for the plan's B and slots, the shared prefixes read once. The results are the same up to float32 rounding, whatever the plan: a
+ * sequence whose slot or tables the plan does not fit any more is attended to by itself. */
+jd_status_t jd_cache_attend_shared(jd_cache_t c, const jd_attend_args_t* args, const jd_shared_t* plan, void* cuda_stream);
+
 typedef struct {
   int32_t B;
   const int32_t* slots;

@@ -335,6 +335,20 @@ def mask_words(see: torch.Tensor) -> torch.Tensor:
     return torch.where(w >= 1 << 31, w - (1 << 32), w).to(torch.int32)
 
 
+class SharedPrefix:
+    """A plan of :meth:`PagedCache.share`: which of B sequences hold the same pages in front, and room for the results of up to ``nodes`` nodes of
+    each. Calls that may run at the same time take a plan each."""
+
+    def __init__(self, cache: "PagedCache", B: int, nodes: int):
+        need = cache._lib.jd_cache_shared_bytes(cache.h, B, nodes)
+        if need == 0:
+            raise ValueError("share: up to 1024 sequences, 1..max_nodes nodes")
+        self.B, self.nodes, self.cache = B, nodes, cache
+        self.buffer = torch.zeros(need, dtype=torch.uint8, device=cache.device)
+        self.c = jd.jd_shared_t(B, nodes, self.buffer.data_ptr(), need)
+        torch.cuda.current_stream(cache.index).synchronize()     # the zeroes are there, whatever stream the first call is on
+
+
 class PagedCache:
     """Keys and values of many sequences in pages, and the tables that say whose they are (``jd_cache_buffers_t``). Adopts the
     tensors it is given, which the caller may read between calls; :meth:`allocate` makes an empty cache."""
@@ -484,10 +498,10 @@ class PagedCache:
         return q_out
 
     def attend(self, layer: int, q: torch.Tensor, tree: Optional[Tree] = None, scale: Optional[float] = None, out: Optional[dict] = None,
-               slots: Optional[torch.Tensor] = None, variant="auto", stream=None) -> dict:
+               slots: Optional[torch.Tensor] = None, variant="auto", stream=None, shared: Optional[SharedPrefix] = None) -> dict:
         """Attention of q [B, T, q_heads, head_dim] over the sequences' tokens and the block's visible nodes; scale: on q . k,
         default head_dim ** -0.5. Returns (and takes) a dict with "out" like q and "lse" [B, T, q_heads] (may be absent in a
-        dict that is given)."""
+        dict that is given). shared: a plan of :meth:`share` for the same sequences; pages that they have in common are read once."""
         if q.dim() != 4:
             raise ValueError("q: [B, T, q_heads, head_dim]")
         B, T, H, D = q.shape
@@ -507,10 +521,32 @@ class PagedCache:
         a = jd.jd_attend_args_t()
         _ATTEND_ARGS.pack_into(a, 0, B, layer, at, t0, t1, t2, t3, t4, q.data_ptr(), o.data_ptr(), q_step, o_step, l_ptr,
                                self._scale if scale is None else scale, ATTEND_VARIANTS[variant] if isinstance(variant, str) else int(variant))
-        st = self._lib.jd_cache_attend(self.h, a, _stream(stream, self.index))
+        if shared is None:
+            st = self._lib.jd_cache_attend(self.h, a, _stream(stream, self.index))
+        else:
+            if shared.cache is not self or shared.B != B or shared.nodes < T:
+                raise ValueError("shared: a plan of this cache for %d sequences of %d nodes" % (B, T))
+            st = self._lib.jd_cache_attend_shared(self.h, a, shared.c, _stream(stream, self.index))
         if st != jd.JD_OK:
             raise jd.JdError(st, "jd_cache_attend")
         return out
+
+    def share(self, nodes: int, slots: Optional[torch.Tensor] = None, groups: Optional[torch.Tensor] = None, plan: Optional[SharedPrefix] = None,
+              stream=None) -> SharedPrefix:
+        """Finds which of the sequences hold the same pages in front, as the tables stand (``jd_cache_share``): forks, samples of one prompt,
+        requests behind one system prompt. groups [B]: entries with the same number are compared, None: those with the same first page. Made once for
+        all layers of a step, for calls of up to ``nodes`` nodes; ``plan``: one to use again (else a new one is allocated, which waits for
+        the current stream). A plan that the tables have left behind costs time, not results."""
+        B = self._batch(slots)
+        if plan is None:
+            plan = SharedPrefix(self, B, nodes)
+        elif plan.cache is not self or plan.B != B or plan.nodes < nodes:
+            raise ValueError("plan: of this cache for %d sequences of %d nodes" % (B, nodes))
+        st = self._lib.jd_cache_share(self.h, plan.c, _ints(slots, "slots", self.index), _ints(groups, "groups", self.index, (B,)),
+                                      _stream(stream, self.index))
+        if st != jd.JD_OK:
+            raise jd.JdError(st, "jd_cache_share")
+        return plan
 
     def commit(self, accept_len: torch.Tensor, paths: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None,
                chosen: Optional[torch.Tensor] = None, path_len: Optional[int] = None, stream=None) -> torch.Tensor:

@@ -54,9 +54,14 @@ size_t simt_smem(int head_dim, int rows) {
   return sizeof(float) * ((size_t)2 * kTile * pitch_of(head_dim) + rows * pitch_of(head_dim) + (rows == 4 ? 1 : 2) * kTile * score_pad(rows));
 }
 
+template <typename E> __device__ __forceinline__ int member0_of(const E& ex) {
+  if constexpr (std::is_same_v<E, SharedExtent>) return ex.more;
+  else return 0;
+}
+
 // kCols: groups of 128 columns that a lane's accumulators cover (head_dim <= 128 kCols)
 // kRows: query rows of the block, 4 or 16
-template <typename T, int kCols, int kRows>
+template <typename T, int kCols, int kRows, int kShare>
 __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_simt_kernel(AttendParams p) {
   constexpr int kScorePad = score_pad(kRows);
   extern __shared__ __align__(16) float smem[];
@@ -72,11 +77,12 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
   float* sS1 = sS + kTile * kScorePad;   // 16 rows: the other half of the columns' share
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int g = blockIdx.x / p.row_blocks, rb = blockIdx.x - g * p.row_blocks;
-  const int r0 = rb * kRows, nrows = min(kRows, p.rows - r0);
+  int r0 = rb * kRows, nrows = min(kRows, p.rows - r0);   // of a group's rows: move with the piece
   pdl_wait();
   pdl_trigger();
-  if (rb == 0 && tid == 0) split_none(p, g);
-  unit_prefix(p, prefix, warp_sums);
+  if (kShare == kAlone && rb == 0 && tid == 0) split_none(p, g);
+  unit_prefix(ShareOf<kShare>(), p, prefix, warp_sums);
+  if (kShare == kPrefix && tid == 0) check_shared(p, blockIdx.x, gridDim.x);
   const int64_t units = (int64_t)prefix[p.B] * p.c.kv_heads;
   if (units == 0) return;
   const int64_t run0 = run_start(units, p.groups, g), run1 = run_start(units, p.groups, g + 1);
@@ -85,24 +91,37 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
 
   const int step = kCols == 1 && D <= 64 ? 2 : 1, col_lane = step == 2 ? lane & 15 : lane, my_token = step == 2 ? lane >> 4 : 0;
   for (int64_t u = run0; u < run1;) {
-    const Piece x = piece_at(p, prefix, u, run1);
+    const Piece x = piece_at<kShare>(p, prefix, u, run1);
     u = x.next;
     if (x.tiles == 0) continue;
-    const int b = x.b, head = x.head, tiles = x.all, tile0 = x.tile0, ntiles = x.tiles;
-    const SeqExtent ex = seq_extent(p, b);
+    const int b = x.b, head = x.head, tiles = x.all, tile0 = x.first + x.tile0, ntiles = x.tiles;
+    const Extent<kShare> ex = extent_at<kShare>(p, b);
+    if constexpr (kShare == kPrefix) {
+      r0 = x.row0;
+      nrows = min(kRows, ex.nodes - r0);
+    }
 
     __syncthreads();   // the previous segment's buffers are free
     for (int i = tid; i < kRows * (D / 4); i += kThreads) {
       const int r = i / (D / 4), d = (i - r * (D / 4)) * 4;
       float v[4] = {0.f, 0.f, 0.f, 0.f};
-      const int t = (r0 + r) / p.group, gq = (r0 + r) - t * p.group;
-      if (r < nrows && t < ex.nodes)
-        load4<T>(reinterpret_cast<const T*>(p.q + ((int64_t)b * p.T + t) * p.q_stride) + (int64_t)(head * p.group + gq) * D + d, v);
+      int from = b, row = r0 + r;
+      bool there = r < nrows;
+      if (kShare == kPrefix && there) {              // whose row it is
+        const int m = row / p.rows;
+        from = __ldcg(p.sh.member + member0_of(ex) + m);
+        row -= m * p.rows;
+      }
+      const int t = row / p.group, gq = row - t * p.group;
+      if (kShare == kPrefix) there = there && (!p.num_nodes || t < __ldcg(p.num_nodes + from));
+      else there = there && t < ex.nodes;
+      if (there)
+        load4<T>(reinterpret_cast<const T*>(p.q + ((int64_t)from * p.T + t) * p.q_stride) + (int64_t)(head * p.group + gq) * D + d, v);
 #pragma unroll
       for (int k = 0; k < 4; ++k) sQ[r * pitch + d + k] = v[k];
     }
     if (tid < kRows) { s_m[tid] = -INFINITY; s_l[tid] = 0.f; }
-    for (int i = tid; i < kRows * p.W; i += kThreads) {
+    for (int i = tid; kShare != kPrefix && i < kRows * p.W; i += kThreads) {
       const int r = i / p.W, w = i - r * p.W, t = (r0 + r) / p.group;
       s_mask[r][w] = r < nrows && t < ex.nodes ? node_word(p, b, t, w, ex.nodes) : 0u;
     }
@@ -292,8 +311,9 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
         if (d < D && my_token == 0) store4(sK + (warp * kRows + r) * D + d, &acc[r][4 * j]);
       }
     __syncthreads();
-    const bool whole = ntiles == tiles;
-    if (!whole && tile0 == 0 && rb == 0 && tid == 0) split_set(p, g, units, x);
+    const bool whole = ntiles == tiles, begins = x.tile0 == 0;
+    const bool direct = whole && (kShare == kAlone || (kShare == kSuffix && x.first == 0));   // nothing to add
+    if (kShare == kAlone && !whole && tile0 == 0 && rb == 0 && tid == 0) split_set(p, g, units, x);
     for (int i = tid; i < nrows * (D / 4); i += kThreads) {
       const int r = i / (D / 4), d = (i - r * (D / 4)) * 4;
       float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -302,7 +322,7 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
         const float4 y = *reinterpret_cast<const float4*>(sK + (w * kRows + r) * D + d);
         x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
       }
-      if (whole) {
+      if (direct) {
         const int t = (r0 + r) / p.group, gq = (r0 + r) - t * p.group;
         if (t >= ex.nodes) continue;
         const float l = s_l[r], inv = l == 0.f ? 0.f : 1.f / l;
@@ -311,7 +331,10 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
         store4(reinterpret_cast<T*>(p.out + ((int64_t)b * p.T + t) * p.out_stride) + (int64_t)h * D + d, o);
         if (d == 0 && p.lse) p.lse[((int64_t)b * p.T + t) * p.q_heads + h] = l == 0.f ? -INFINITY : (s_m[r] + log2f(l)) * 0.69314718055994531f;
       } else {
-        float* part = p.part + (((int64_t)blockIdx.x * 2 + (tile0 == 0 ? 1 : 0)) * p.part_rows + r) * (D + kPartPad);
+        float* part = p.part + (((int64_t)blockIdx.x * 2 + (begins ? 1 : 0)) * p.part_rows + r) * (D + kPartPad);
+        if (kShare != kAlone && whole)
+          part = (kShare == kPrefix ? p.sh.rec_a : p.sh.rec_b) +
+                 (((int64_t)(kShare == kPrefix ? member0_of(ex) : b) * p.rows + r0 + r) * p.c.kv_heads + head) * (D + kPartPad);
         *reinterpret_cast<float4*>(part + d) = x;
         if (d == 0) { part[D] = s_m[r]; part[D + 1] = s_l[r]; }
       }
@@ -381,6 +404,25 @@ __device__ __forceinline__ RowSum<kCols> sum_parts(int first, int last, int step
   return s;
 }
 
+// What a block's warps have summed up, columns 128 j + 4 lane ..
+template <int kCols>
+__device__ __forceinline__ void add_warps(const float4 (*s_o)[kCols][32], const float2* s_ml, int j, int lane, float* y, float& m, float& l) {
+  m = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < kJoinWarps; ++w) m = fmaxf(m, s_ml[w].x);
+  const float base = m == -INFINITY ? 0.f : m;
+  l = 0.f;
+  y[0] = y[1] = y[2] = y[3] = 0.f;
+#pragma unroll
+  for (int w = 0; w < kJoinWarps; ++w) {
+    const float f = exp2f(s_ml[w].x - base);
+    const float4 x = s_o[w][j][lane];
+    l += f * s_ml[w].y;
+    if (s_ml[w].x == -INFINITY) continue;
+    y[0] = fmaf(f, x.x, y[0]); y[1] = fmaf(f, x.y, y[1]); y[2] = fmaf(f, x.z, y[2]); y[3] = fmaf(f, x.w, y[3]);
+  }
+}
+
 template <typename T, int kCols>
 __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendParams p) {
   __shared__ float4 s_o[kJoinWarps][kCols][32];
@@ -447,29 +489,90 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendPara
     if (lane == 0) s_ml[warp] = make_float2(s.m, s.l);
     __syncthreads();
     if (warp < kCols) {   // columns 128 warp ..
-      float top = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, s_ml[w].x);
-      const float base = top == -INFINITY ? 0.f : top;
-      float sum = 0.f, y[4] = {};
-#pragma unroll
-      for (int w = 0; w < kJoinWarps; ++w) {
-        const float f = exp2f(s_ml[w].x - base);
-        const float4 x = s_o[w][warp][lane];
-        sum += f * s_ml[w].y;
-        if (s_ml[w].x == -INFINITY) continue;
-        y[0] = fmaf(f, x.x, y[0]); y[1] = fmaf(f, x.y, y[1]); y[2] = fmaf(f, x.z, y[2]); y[3] = fmaf(f, x.w, y[3]);
-      }
+      float y[4], top, sum;
+      add_warps<kCols>(s_o, s_ml, warp, lane, y, top, sum);
       write(row, 128 * warp + lane * 4, y, top, sum);
     }
   }
 }
 
-template <typename T>
+// Adds up the prefix call's and the suffix call's results of every row, parts and records alike. A warp for a row, or, with few rows, whose
+// parts from many SMs are what takes the time, a block of four. Rows that the suffix call has written already (no prefix, one run) are left alone.
+constexpr int kSharedFewRows = 4096;
+
+template <typename T, int kCols>
+__global__ void __launch_bounds__(32 * kJoinWarps) attend_shared_join_kernel(const __grid_constant__ AttendParams a, const __grid_constant__ AttendParams p, bool few) {
+  __shared__ float4 s_o[kJoinWarps][kCols][32];
+  __shared__ float2 s_ml[kJoinWarps];
+  pdl_wait();
+  pdl_trigger();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int D = p.c.head_dim, pitch = D + kPartPad;
+  const int64_t id = few ? blockIdx.x : (int64_t)blockIdx.x * kJoinWarps + warp;
+  if (id >= (int64_t)p.B * p.T * p.q_heads) return;
+  const int64_t token = id / p.q_heads;
+  const int h = (int)(id - token * p.q_heads), b = (int)(token / p.T), t = (int)(token - (int64_t)b * p.T);
+  const int head = h / p.group, row = t * p.group + h - head * p.group;
+  const int nodes = p.num_nodes ? min(max(__ldcg(p.num_nodes + b), 0), p.T) : p.T;
+  const int ub0 = __ldcg(p.sh.units_b + b), n = __ldcg(p.sh.units_b + b + 1) - ub0, first = __ldcg(p.sh.first + b);
+  const int64_t all_b = (int64_t)__ldcg(p.sh.units_b + p.B) * p.c.kv_heads;
+  if (t >= nodes || n == 0) return;                    // n == 0: a padding sequence
+  const int64_t seg_b = (int64_t)ub0 * p.c.kv_heads + (int64_t)head * n;
+  const int b0 = run_of(all_b, p.groups, seg_b + p.seg_cost), b1 = run_of(all_b, p.groups, seg_b + n - 1);
+  if (first == 0 && b0 == b1) return;
+  int a0 = 0, count_a = 0, row_a = 0, block_row = 0;
+  int64_t record_a = 0;
+  if (first > 0) {
+    const int g = __ldcg(p.sh.entry_group + b), start = __ldcg(p.sh.group_start + g), members = __ldcg(p.sh.group_start + g + 1) - start;
+    row_a = __ldcg(p.sh.entry_place + b) * p.rows + row;
+    record_a = ((int64_t)start * p.rows + row_a) * p.c.kv_heads + head;
+    const int blocks = row_blocks_of(a, members * p.rows), block = row_a / a.rows_per_block, na = a.seg_cost + (first >> a.tile_shift);
+    block_row = row_a - block * a.rows_per_block;
+    const int64_t all_a = (int64_t)__ldcg(p.sh.units_a + p.B) * p.c.kv_heads;
+    const int64_t seg_a = (int64_t)__ldcg(p.sh.units_a + g) * p.c.kv_heads + ((int64_t)head * blocks + block) * na;
+    a0 = run_of(all_a, a.groups, seg_a + a.seg_cost);
+    count_a = run_of(all_a, a.groups, seg_a + na - 1) - a0 + 1;
+  }
+  const int rb = row / p.rows_per_block;
+  auto at = [&](int i) -> const float* {               // part i: the prefix's first
+    if (i < count_a) {
+      if (count_a == 1) return p.sh.rec_a + record_a * pitch;
+      return a.part + (((int64_t)(a0 + i) * 2 + (i == 0 ? 1 : 0)) * a.part_rows + block_row) * pitch;
+    }
+    i -= count_a;
+    if (b0 == b1) return p.sh.rec_b + (((int64_t)b * p.rows + row) * p.c.kv_heads + head) * pitch;
+    return p.part + ((((int64_t)(b0 + i) * p.row_blocks + rb) * 2 + (i == 0 ? 1 : 0)) * p.part_rows + row - rb * p.rows_per_block) * pitch;
+  };
+  const int last = count_a + b1 - b0;
+  auto write = [&](int d, const float* o, float m, float l) {   // columns d .. d + 3
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+    if (d < D) store4(reinterpret_cast<T*>(p.out + token * p.out_stride) + (int64_t)h * D + d, y);
+    if (d == 0 && p.lse) p.lse[id] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+  };
+  if (!few) {
+    const RowSum<kCols> s = sum_parts<kCols>(0, last, 1, D, lane, at);
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) write(128 * j + lane * 4, s.o[j], s.m, s.l);
+    return;
+  }
+  const RowSum<kCols> s = sum_parts<kCols>(warp, last, kJoinWarps, D, lane, at);
+#pragma unroll
+  for (int j = 0; j < kCols; ++j) s_o[warp][j][lane] = make_float4(s.o[j][0], s.o[j][1], s.o[j][2], s.o[j][3]);
+  if (lane == 0) s_ml[warp] = make_float2(s.m, s.l);
+  __syncthreads();
+  if (warp < kCols) {
+    float y[4], m, l;
+    add_warps<kCols>(s_o, s_ml, warp, lane, y, m, l);
+    write(128 * warp + lane * 4, y, m, l);
+  }
+}
+
+template <typename T, int kShare>
 cudaError_t launch_simt(const AttendParams& p, cudaStream_t st) {
   const bool few = p.rows_per_block == 4;
-  auto kernel = p.c.head_dim <= 128 ? (few ? attend_simt_kernel<T, 1, 4> : attend_simt_kernel<T, 1, 16>)
-                                    : (few ? attend_simt_kernel<T, 2, 4> : attend_simt_kernel<T, 2, 16>);
+  auto kernel = p.c.head_dim <= 128 ? (few ? attend_simt_kernel<T, 1, 4, kShare> : attend_simt_kernel<T, 1, 16, kShare>)
+                                    : (few ? attend_simt_kernel<T, 2, 4, kShare> : attend_simt_kernel<T, 2, 16, kShare>);
   return launch_chained(kernel, dim3((unsigned)(p.groups * p.row_blocks)), dim3(kThreads), simt_smem(p.c.head_dim, p.rows_per_block), st, p);
 }
 
@@ -481,7 +584,14 @@ bool raise_limit(K kernel, size_t bytes) {
 }  // namespace
 
 cudaError_t run_attend_simt(const AttendParams& p, int dtype, cudaStream_t st) {
-  return dtype == JD_DTYPE_F32 ? launch_simt<float>(p, st) : launch_simt<__nv_bfloat16>(p, st);
+  return dtype == JD_DTYPE_F32 ? launch_simt<float, kAlone>(p, st) : launch_simt<__nv_bfloat16, kAlone>(p, st);
+}
+
+cudaError_t run_attend_shared_simt(const AttendParams& prefix, const AttendParams& suffix, int dtype, cudaStream_t st) {
+  const bool f32 = dtype == JD_DTYPE_F32;
+  const cudaError_t err = f32 ? launch_simt<float, kPrefix>(prefix, st) : launch_simt<__nv_bfloat16, kPrefix>(prefix, st);
+  if (err != cudaSuccess) return err;
+  return f32 ? launch_simt<float, kSuffix>(suffix, st) : launch_simt<__nv_bfloat16, kSuffix>(suffix, st);
 }
 
 cudaError_t run_attend_join(const AttendParams& p, int dtype, cudaStream_t st) {
@@ -493,11 +603,21 @@ cudaError_t run_attend_join(const AttendParams& p, int dtype, cudaStream_t st) {
   return launch_chained(kernel, grid, dim3(32 * kJoinWarps), 0, st, p);
 }
 
-template <typename T>
-bool raise_limits() {
-  return raise_limit(attend_simt_kernel<T, 1, 4>, simt_smem(128, 4)) && raise_limit(attend_simt_kernel<T, 1, 16>, simt_smem(128, 16)) &&
-         raise_limit(attend_simt_kernel<T, 2, 4>, simt_smem(256, 4)) && raise_limit(attend_simt_kernel<T, 2, 16>, simt_smem(256, 16));
+cudaError_t run_attend_shared_join(const AttendParams& prefix, const AttendParams& suffix, int dtype, cudaStream_t st) {
+  const int64_t rows = (int64_t)suffix.B * suffix.T * suffix.q_heads;
+  const bool few = rows <= kSharedFewRows;
+  const dim3 grid((unsigned)(few ? rows : (rows + kJoinWarps - 1) / kJoinWarps));
+  auto kernel = dtype == JD_DTYPE_F32 ? (suffix.c.head_dim <= 128 ? attend_shared_join_kernel<float, 1> : attend_shared_join_kernel<float, 2>)
+                                      : (suffix.c.head_dim <= 128 ? attend_shared_join_kernel<__nv_bfloat16, 1> : attend_shared_join_kernel<__nv_bfloat16, 2>);
+  return launch_chained(kernel, grid, dim3(32 * kJoinWarps), 0, st, prefix, suffix, few);
 }
-bool simt_attend_configure() { return raise_limits<float>() && raise_limits<__nv_bfloat16>(); }
+
+template <typename T, int kShare>
+bool raise_limits() {
+  return raise_limit(attend_simt_kernel<T, 1, 4, kShare>, simt_smem(128, 4)) && raise_limit(attend_simt_kernel<T, 1, 16, kShare>, simt_smem(128, 16)) &&
+         raise_limit(attend_simt_kernel<T, 2, 4, kShare>, simt_smem(256, 4)) && raise_limit(attend_simt_kernel<T, 2, 16, kShare>, simt_smem(256, 16));
+}
+template <int kShare> bool raise_both() { return raise_limits<float, kShare>() && raise_limits<__nv_bfloat16, kShare>(); }
+bool simt_attend_configure() { return raise_both<kAlone>() && raise_both<kPrefix>() && raise_both<kSuffix>(); }
 
 }  // namespace jd

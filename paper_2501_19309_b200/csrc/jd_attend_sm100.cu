@@ -77,7 +77,7 @@ template <int D, int kMode> struct Shape {
   static constexpr int kPieces = kPair && kFetchAhead ? 3 : 2;
 };
 
-template <int kPieces> struct Shared {
+template <int kPieces, int kShare> struct Shared {
   uint64_t full[8], empty[8];
   uint64_t s_full[2], p_ready[2][2], o_done[2], q_ready[2];   // p_ready: first and second 64 columns of P
   uint32_t tmem_base;
@@ -90,13 +90,13 @@ template <int kPieces> struct Shared {
     int odd_values;                      // nodes hold values that are not finite
   } piece[kPieces];
   int prefix[kMaxCacheBatch + 1];
-  SeqExtent extents[kMaxCacheBatch];
+  Extent<kShare> extents[kMaxCacheBatch];
 };
 
-template <int D, int kMode>
+template <int D, int kMode, int kShare>
 constexpr size_t attend_smem() {
   using S = Shape<D, kMode>;
-  return 1024 + (sizeof(Shared<S::kPieces>) + 1023) / 1024 * 1024 + (size_t)(S::kStages + S::kQTiles) * S::kTileBytes + S::kStageBytes;
+  return 1024 + (sizeof(Shared<S::kPieces, kShare>) + 1023) / 1024 * 1024 + (size_t)(S::kStages + S::kQTiles) * S::kTileBytes + S::kStageBytes;
 }
 
 // Bounded wait that gives up as soon as another role has.
@@ -265,7 +265,13 @@ __device__ __noinline__ float4 spoilt_by_context(const AttendParams& p, int slot
   return make_float4(sum[0], sum[1], sum[2], sum[3]);
 }
 
-template <int D, int kMode>
+// Row 0 of a group among the rows of all members of all groups.
+template <typename E> __device__ __forceinline__ int64_t ex_first_row(const AttendParams& p, const E& ex) {
+  if constexpr (std::is_same_v<E, SharedExtent>) return (int64_t)ex.more * p.rows;
+  else return 0;
+}
+
+template <int D, int kMode, int kShare>
 __global__ void __launch_bounds__(kThreads, 1)
 attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ AttendParams p) {
   using Sh = Shape<D, kMode>;
@@ -274,7 +280,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   constexpr int kStages = Sh::kStages, kChunks = Sh::kChunks, kChunkBytes = Sh::kChunkBytes, kTileBytes = Sh::kTileBytes;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  using Shm = Shared<Sh::kPieces>;
+  using Shm = Shared<Sh::kPieces, kShare>;
   Shm& sh = *reinterpret_cast<Shm*>(smem);
   uint8_t* q_smem = smem + (sizeof(Shm) + 1023) / 1024 * 1024;
   uint8_t* ring = q_smem + Sh::kQTiles * kTileBytes;
@@ -303,8 +309,8 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
-  if (rb == 0 && tid == 0) split_none(p, g);
-  unit_prefix(p, sh.prefix, sh.warp_sums, sh.extents);   // ends with a barrier
+  if (kShare == kAlone && rb == 0 && tid == 0) split_none(p, g);
+  unit_prefix(ShareOf<kShare>(), p, sh.prefix, sh.warp_sums, sh.extents);   // ends with a barrier
   pdl_trigger();
   tc_fence_after();
   const int64_t units = (int64_t)sh.prefix[p.B] * p.c.kv_heads;
@@ -314,6 +320,8 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (kShare == kPrefix && warp == 11 && lane == 0) check_shared(p, blockIdx.x, gridDim.x);
+    __syncwarp();
     if (warp == 8 || warp == 10) {
       // ------------------------------------------------------------------ producers: warp 8 fetches K tiles, warp 10 V tiles
       // Ring items are K and V of the run's tiles in turn. A box costs the issuing warp about 100 cycles, whatever its size, which with
@@ -327,12 +335,12 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       uint32_t phase = 0;
       bool ok = true;
       for (int64_t u = run0; u < run1 && ok;) {
-        const Piece x = piece_at(p, sh.prefix, u, run1);
+        const Piece x = piece_at<kShare>(p, sh.prefix, u, run1, sh.extents);
         u = x.next;
         if (x.tiles == 0) continue;
-        const SeqExtent ex = sh.extents[x.b];
+        const Extent<kShare> ex = sh.extents[x.b];
         const int32_t* table = p.c.table + (int64_t)ex.slot * p.c.max_pages;
-        auto token_of = [&](int t) { return (x.tile0 + t) * kTile + (lane << box_shift); };   // this lane's box of tile t
+        auto token_of = [&](int t) { return (x.first + x.tile0 + t) * kTile + (lane << box_shift); };   // this lane's box of tile t
         auto fetch = [&](int t) {
           const int at = token_of(t);
           return t < x.tiles && lane < boxes_per_tile && at < ex.kv_end ? __ldcg(table + (at >> shift)) : 0;
@@ -419,7 +427,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       };
       int base = 0;                                    // ring items of the pieces in front
       for (int64_t u = uniform64(run0); u < uniform64(run1);) {
-        const Piece x = piece_at(p, sh.prefix, u, run1);
+        const Piece x = piece_at<kShare>(p, sh.prefix, u, run1, sh.extents);
         const int n = __shfl_sync(0xffffffffu, x.tiles, 0);
         u = uniform64(x.next);
         if (n == 0) continue;
@@ -466,11 +474,12 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     const int w = warp >> 2, r = tid & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t t_s = tmem + lanes + w * 128, t_o = tmem + lanes + 256 + w * 128;
-    const int r0 = rb * p.rows_per_block;
+    int r0 = rb * p.rows_per_block;                                 // of a group's rows: moves with the piece
     const int copy = r / kCopyRows, col0 = copy * kCols;            // the copy that this warp belongs to, and its columns
-    const int my_row = r0 + r % kCopyRows + (kPair ? w * 128 : 0);
-    const bool warp_live = my_row - lane < p.rows;
-    const int t_node = my_row / p.group, gq = my_row - t_node * p.group;
+    const int my_place = r % kCopyRows + (kPair ? w * 128 : 0);
+    int my_row = r0 + my_place;
+    bool warp_live = my_row - lane < p.rows;
+    const int t_node = my_row / p.group, gq = my_row - t_node * p.group;   // where rows are a sequence's
     const float c2 = p.scale_log2;
     const float c2_far = __uint_as_float((__float_as_uint(c2) + 0x7FFFFFu) & 0xFF800000u);
     uint32_t s_phase = 0, o_phase = 0;
@@ -489,7 +498,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       Piece y;
       y.tiles = 0;
       while (u < run1) {
-        y = piece_at(p, sh.prefix, u, run1);
+        y = piece_at<kShare>(p, sh.prefix, u, run1, sh.extents);
         u = y.next;
         if (y.tiles > 0) break;
       }
@@ -497,6 +506,24 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     };
     auto fetch = [&](const Piece& y) {
       if (y.tiles == 0) return;
+      if constexpr (kShare == kPrefix) {             // rows of all members one behind another: whose each is comes first
+        const Extent<kShare> ex = sh.extents[y.b];
+        int64_t from[kQLoads];
+#pragma unroll
+        for (int i = 0; i < kQLoads; ++i) {
+          const int row = y.row0 + (kPair ? w * 128 : 0) + q_r + i * kQRows, m = (int)((uint32_t)row / (uint32_t)p.rows), at = row - m * p.rows;
+          const int t = (int)((uint32_t)at / (uint32_t)p.group);
+          from[i] = -1;
+          if (row < ex.nodes) {
+            const int b = __ldcg(p.sh.member + ex.more + m);
+            if (!p.num_nodes || t < __ldcg(p.num_nodes + b))
+              from[i] = ((int64_t)b * p.T + t) * p.q_stride + ((int64_t)y.head * p.group + at - t * p.group) * (D * 2) + q_c * 16;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < kQLoads; ++i) q_regs[i] = from[i] >= 0 ? __ldcg(reinterpret_cast<const uint4*>(p.q + from[i])) : make_uint4(0u, 0u, 0u, 0u);
+        return;
+      }
       const int nodes = sh.extents[y.b].nodes;
       const char* q_seq = p.q + (int64_t)y.b * p.T * p.q_stride + (int64_t)y.head * p.group * (D * 2) + q_c * 16;
       // every load is made, rows that are not there from the first one's place: no branch stands between a load and the next
@@ -522,10 +549,12 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     auto behind = [&]() { return now + 1 == Sh::kPieces ? 0 : now + 1; };
     // the fetched piece's masks and Q to shared memory, and the word to the chains that have tiles in it: no other waits for it
     auto hand_over = [&](const Piece& y, typename Shm::PerPiece& to) {
+      if constexpr (kShare != kPrefix) {
 #pragma unroll
-      for (int i = 0; i < kMaskLoads; ++i) {
-        const int at = tid + i * 256, t = at / p.W;
-        if (t < p.T) to.node_mask[t][at - t * p.W] = mask_regs[i];
+        for (int i = 0; i < kMaskLoads; ++i) {
+          const int at = tid + i * 256, t = at / p.W;
+          if (t < p.T) to.node_mask[t][at - t * p.W] = mask_regs[i];
+        }
       }
       if (tid == 0) to.odd_values = 0;
       uint8_t* q_dst = q_smem + (kPair ? w * kTileBytes : 0) + (q_c >> 3) * kChunkBytes;
@@ -550,13 +579,18 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       hand_over(x, sh.piece[0]);
     }
     while (x.tiles > 0) {
-      const SeqExtent ex = sh.extents[x.b];
+      const Extent<kShare> ex = sh.extents[x.b];
       typename Shm::PerPiece& mine = sh.piece[now];
+      if constexpr (kShare == kPrefix) {
+        r0 = x.row0;
+        my_row = r0 + my_place;
+        warp_live = my_row - lane < ex.nodes;
+      }
       float m = -INFINITY, l = 0.f;
       int done = 0;                                  // tiles of this piece that this warpgroup has taken
       for (int t = kPair ? 0 : w; t < x.tiles; t += kPair ? 1 : 2, ++done) {
-        const int kv0 = (x.tile0 + t) * kTile;
-        const bool tail = kv0 + kTile > ex.ctx;      // holds nodes, or ends behind the sequence
+        const int kv0 = (x.first + x.tile0 + t) * kTile;
+        const bool tail = kShare != kPrefix && kv0 + kTile > ex.ctx;   // holds nodes, or ends behind the sequence
         wait(smem_u32(&sh.s_full[w]), s_phase, abort_flag);
         s_phase ^= 1u;
         // V rows that are no tokens may hold anything: 0 x NaN would reach every row. They become zeroes; and so do values of nodes
@@ -689,8 +723,9 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       if (done > 0) wait(smem_u32(&sh.o_done[w]), o_phase ^ 1u, abort_flag);
       tc_fence_after();
       const bool whole = x.tiles == x.all;
-      if (!whole && x.tile0 == 0 && rb == 0 && tid == 0) split_set(p, g, units, x);
-      const bool live = my_row < p.rows && t_node < ex.nodes;
+      if (kShare == kAlone && !whole && x.tile0 == 0 && rb == 0 && tid == 0) split_set(p, g, units, x);
+      const bool live = kShare == kPrefix ? my_row < ex.nodes : my_row < p.rows && t_node < ex.nodes;
+      const bool direct = whole && (kShare == kAlone || (kShare == kSuffix && x.first == 0));   // nothing to add
       float f0 = 1.f, f1 = 0.f;                      // factors on this lane's O_0 and O_1 (pair mode: on its own O)
       if constexpr (!kPair) {
         mine.ml[w][r][0] = m;
@@ -722,15 +757,22 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         if (kCopies > 1 && copy == 0) mine.inv[w][r] = l == 0.f ? 0.f : 1.f / l;   // each warpgroup its own
       }
       const bool two = !kPair && x.tiles > 1;
-      const float inv = !whole ? 1.f : (l == 0.f ? 0.f : 1.f / l);
+      const float inv = !direct ? 1.f : (l == 0.f ? 0.f : 1.f / l);
       const bool odd = *reinterpret_cast<volatile int*>(&mine.odd_values) != 0;
+      // where row 0 of the numerators would stand, and how far rows are apart: a slot of this CTA, or the rows' records
       float* part0 = p.part + (((int64_t)blockIdx.x * 2 + (x.tile0 == 0 ? 1 : 0)) * p.part_rows - r0) * (D + kPartPad);
+      int64_t part_step = D + kPartPad;
+      if (kShare != kAlone && whole) {
+        part_step = (int64_t)p.c.kv_heads * (D + kPartPad);
+        part0 = kShare == kPrefix ? p.sh.rec_a + (int64_t)ex_first_row(p, ex) * part_step : p.sh.rec_b + (int64_t)x.b * p.rows * part_step;
+        part0 += x.head * (D + kPartPad);
+      }
       // kN elements of a query row from column c: back to a part, or out. With copies, an element that is no number while the row's
       // sum is one has met an infinity of V: one copy's weight makes it that infinity, the others' zeroes make it NaN.
       auto write = [&](auto count, int row, int c, float* o, float factor, bool sum_ok) {
         constexpr int kN = decltype(count)::value;
         const int t = row / p.group, h = x.head * p.group + row - t * p.group;
-        if (row >= p.rows || t >= ex.nodes) return;
+        if (kShare == kPrefix ? row >= ex.nodes : row >= p.rows || t >= ex.nodes) return;
         bool lost = false;
         if constexpr (kCopies > 1) {
 #pragma unroll
@@ -740,10 +782,10 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         if (odd || lost) {
           // What is finite does not count beside what is not.
           float sum[kN] = {};
-          if (odd) {                                 // values of this piece's nodes that are not finite, to the rows that see them
+          if (kShare != kPrefix && odd) {            // values of this piece's nodes that are not finite, to the rows that see them
             for (int j = 0; j < ex.nodes; ++j) {
               const int kv = ex.ctx + j;
-              if (kv < x.tile0 * kTile || kv >= (x.tile0 + x.tiles) * kTile || kv >= ex.kv_end || !((mine.node_mask[t][j >> 5] >> (j & 31)) & 1u)) continue;
+              if (kv < (x.first + x.tile0) * kTile || kv >= (x.first + x.tile0 + x.tiles) * kTile || kv >= ex.kv_end || !((mine.node_mask[t][j >> 5] >> (j & 31)) & 1u)) continue;
               const int page = p.c.table[(int64_t)ex.slot * p.c.max_pages + (kv >> p.c.page_shift)];
               if (page < 0 || page >= p.c.pages) continue;
               const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(p.c.v) + page_row(p.c, p.layer, page, x.head, kv & (p.c.page_size - 1)) * D + c;
@@ -756,7 +798,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           }
           if constexpr (kCopies > 1) {
             if (lost) {
-              const float4 y = spoilt_by_context<D>(p, ex.slot, x.head, x.tile0 * kTile, min((x.tile0 + x.tiles) * kTile, ex.ctx), c);
+              const float4 y = spoilt_by_context<D>(p, ex.slot, x.head, (x.first + x.tile0) * kTile, min((x.first + x.tile0 + x.tiles) * kTile, ex.ctx), c);
               const float of[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
               for (int i = 0; i < kN; ++i)
@@ -767,12 +809,12 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           for (int i = 0; i < kN; ++i)
             if (sum[i] != 0.f) o[i] += sum[i];
         }
-        if (whole) {
+        if (direct) {
           uint2* out = reinterpret_cast<uint2*>(p.out + ((int64_t)x.b * p.T + t) * p.out_stride + ((int64_t)h * D + c) * 2);
 #pragma unroll
           for (int i = 0; i < kN; i += 4) out[i / 4] = make_uint2(pack_bf16(o[i] * factor, o[i + 1] * factor), pack_bf16(o[i + 2] * factor, o[i + 3] * factor));
         } else {
-          float4* part = reinterpret_cast<float4*>(part0 + (int64_t)row * (D + kPartPad) + c);
+          float4* part = reinterpret_cast<float4*>(part0 + row * part_step + c);
 #pragma unroll
           for (int i = 0; i < kN; i += 4) part[i / 4] = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
         }
@@ -822,7 +864,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           asm volatile("bar.sync %0, 128;" ::"r"(2 + w) : "memory");
           for (int i = r; i < kCopyRows * kPlaces; i += 128) {
             const int row = i / kPlaces, q = i % kPlaces;
-            if (r0 + row >= p.rows) continue;
+            if (r0 + row >= (kShare == kPrefix ? ex.nodes : p.rows)) continue;
             float y[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < kCopies; ++k) {
@@ -830,17 +872,17 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
               y[0] += v.x; y[1] += v.y; y[2] += v.z; y[3] += v.w;
             }
             const float by = mine.inv[w][row];
-            write(std::integral_constant<int, 4>(), r0 + row, c + q * 4, y, whole ? by : 1.f, !isnan(by));
+            write(std::integral_constant<int, 4>(), r0 + row, c + q * 4, y, direct ? by : 1.f, !isnan(by));
           }
           asm volatile("bar.sync %0, 128;" ::"r"(2 + w) : "memory");
         }
       }
       if (live && copy == 0 && (kPair || w == 0)) {
         const float m2 = m * c2;
-        if (whole) {
+        if (direct) {
           if (p.lse) p.lse[((int64_t)x.b * p.T + t_node) * p.q_heads + x.head * p.group + gq] = l == 0.f ? -INFINITY : (m2 + log2f(l)) * 0.69314718055994531f;
         } else {
-          *reinterpret_cast<float2*>(part0 + (int64_t)my_row * (D + kPartPad) + D) = make_float2(m == -INFINITY ? -INFINITY : m2, l);
+          *reinterpret_cast<float2*>(part0 + my_row * part_step + D) = make_float2(m == -INFINITY ? -INFINITY : m2, l);
         }
       }
       tc_fence_before();
@@ -866,30 +908,40 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   }
 }
 
-template <int D, int kMode>
+template <int D, int kMode, int kShare>
 cudaError_t launch(const AttendParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st) {
-  return launch_chained(attend_sm100_kernel<D, kMode>, dim3((unsigned)(p.groups * p.row_blocks)), dim3(kThreads), attend_smem<D, kMode>(), st, tm_k, tm_v, p);
+  return launch_chained(attend_sm100_kernel<D, kMode, kShare>, dim3((unsigned)(p.groups * p.row_blocks)), dim3(kThreads), attend_smem<D, kMode, kShare>(), st, tm_k, tm_v, p);
 }
-template <int D>
-cudaError_t launch_mode(const AttendParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st) {
-  if (p.rows_per_block > 128) return launch<D, kPairMode>(p, tm_k, tm_v, st);
-  if (p.rows > 64) return launch<D, 1>(p, tm_k, tm_v, st);
-  return p.rows > 32 ? launch<D, 2>(p, tm_k, tm_v, st) : launch<D, 4>(p, tm_k, tm_v, st);
+// most: rows that a segment may have
+template <int D, int kShare>
+cudaError_t launch_mode(const AttendParams& p, int most, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st) {
+  if (p.rows_per_block > 128) return launch<D, kPairMode, kShare>(p, tm_k, tm_v, st);
+  if (most > 64) return launch<D, 1, kShare>(p, tm_k, tm_v, st);
+  return most > 32 ? launch<D, 2, kShare>(p, tm_k, tm_v, st) : launch<D, 4, kShare>(p, tm_k, tm_v, st);
 }
-template <int D, int kMode>
+template <int D, int kMode, int kShare>
 bool configure() {
-  static_assert(attend_smem<D, kMode>() <= 227 * 1024, "shared memory of an SM");
-  return cudaFuncSetAttribute(attend_sm100_kernel<D, kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)attend_smem<D, kMode>()) == cudaSuccess;
+  static_assert(attend_smem<D, kMode, kShare>() <= 227 * 1024, "shared memory of an SM");
+  return cudaFuncSetAttribute(attend_sm100_kernel<D, kMode, kShare>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)attend_smem<D, kMode, kShare>()) == cudaSuccess;
 }
-template <int D>
-bool configure_modes() { return configure<D, kPairMode>() && configure<D, 1>() && configure<D, 2>() && configure<D, 4>(); }
+template <int D, int kShare>
+bool configure_modes() { return configure<D, kPairMode, kShare>() && configure<D, 1, kShare>() && configure<D, 2, kShare>() && configure<D, 4, kShare>(); }
 
 }  // namespace
 
 cudaError_t run_attend_tensor(const AttendParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st) {
-  return p.c.head_dim == 64 ? launch_mode<64>(p, tm_k, tm_v, st) : launch_mode<128>(p, tm_k, tm_v, st);
+  return p.c.head_dim == 64 ? launch_mode<64, kAlone>(p, p.rows, tm_k, tm_v, st) : launch_mode<128, kAlone>(p, p.rows, tm_k, tm_v, st);
 }
 
-bool attend_configure() { return simt_attend_configure() && configure_modes<64>() && configure_modes<128>(); }
+cudaError_t run_attend_shared_tensor(const AttendParams& prefix, int most, const AttendParams& suffix, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
+                                     cudaStream_t st) {
+  const bool narrow = prefix.c.head_dim == 64;
+  const cudaError_t err = narrow ? launch_mode<64, kPrefix>(prefix, most, tm_k, tm_v, st) : launch_mode<128, kPrefix>(prefix, most, tm_k, tm_v, st);
+  if (err != cudaSuccess) return err;
+  return narrow ? launch_mode<64, kSuffix>(suffix, suffix.rows, tm_k, tm_v, st) : launch_mode<128, kSuffix>(suffix, suffix.rows, tm_k, tm_v, st);
+}
+
+template <int kShare> bool configure_widths() { return configure_modes<64, kShare>() && configure_modes<128, kShare>(); }
+bool attend_configure() { return simt_attend_configure() && configure_widths<kAlone>() && configure_widths<kPrefix>() && configure_widths<kSuffix>(); }
 
 }  // namespace jd

@@ -537,6 +537,81 @@ bool append_ok(jd_cache_t c, const jd_append_args_t* a) {
   return !a->rope || rope_valid(*a->rope, g.head_dim);
 }
 
+bool attend_ok(jd_cache_t c, const jd_attend_args_t* a) {
+  if (!c || !a || !batch_ok(c, a->B, a->slots) || !tree_ok(c, a->tree)) return false;
+  const jd_cache_config_t& g = c->cfg;
+  const int e = g.dtype == JD_DTYPE_F32 ? 4 : 2;
+  if (a->layer < 0 || a->layer >= g.num_layers || !a->q || !a->out || a->q == a->out || !on16(a->q) || !on16(a->out) || !on4(a->lse)) return false;
+  const int64_t qd = (int64_t)g.q_heads * g.head_dim;
+  if (!stride_ok(a->q_stride, qd, e) || !stride_ok(a->out_stride, qd, e) || !(a->scale > 0.f && std::isfinite(a->scale))) return false;
+  return a->variant >= JD_ATTEND_AUTO && a->variant <= JD_ATTEND_TENSOR;
+}
+
+AttendParams attend_params(jd_cache_t c, const jd_attend_args_t& a, bool tensor) {
+  const jd_cache_config_t& g = c->cfg;
+  const int e = g.dtype == JD_DTYPE_F32 ? 4 : 2;
+  const int64_t qd = (int64_t)g.q_heads * g.head_dim;
+  AttendParams p = {};
+  p.c = view_of(c);
+  p.B = a.B; p.layer = a.layer; p.T = a.tree.nodes; p.W = (a.tree.nodes + 31) / 32;
+  p.q_heads = g.q_heads; p.group = g.q_heads / g.kv_heads;
+  p.rows = p.T * p.group;
+  p.slots = a.slots;
+  p.mask = a.tree.mask;
+  p.mask_stride = a.tree.per_seq ? (int64_t)p.T * p.W : 0;
+  p.num_nodes = a.tree.num_nodes;
+  p.q = (const char*)a.q; p.out = (char*)a.out;
+  p.q_stride = (a.q_stride ? a.q_stride : qd) * e; p.out_stride = (a.out_stride ? a.out_stride : qd) * e;
+  p.lse = a.lse;
+  p.scale_log2 = a.scale * 1.4426950408889634f;
+  p.part = c->part;
+  p.split = c->split;
+  if (tensor) {
+    p.tile_shift = kTensorTileShift;
+    p.seg_cost = tensor_seg_cost(g.head_dim, p.rows);
+    p.rows_per_block = p.rows > 128 ? 256 : 128;
+  } else {
+    p.tile_shift = kSimtTileShift;
+    p.seg_cost = kSimtSegCost;
+    p.rows_per_block = p.rows <= 4 ? 4 : kSimtRows;   // one token's few rows leave the others' registers and products out
+  }
+  p.part_rows = std::min(p.rows, p.rows_per_block);
+  p.row_blocks = (p.rows + p.rows_per_block - 1) / p.rows_per_block;
+  p.groups = std::max(1, (tensor ? c->num_sms : 2 * c->num_sms) / p.row_blocks);
+  return p;
+}
+
+// The parts of a plan's buffer; its size.
+size_t carve_shared(jd_cache_t c, int B, int nodes, char* base, SharedView* s) {
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    char* p = base ? base + off : nullptr;
+    off += (bytes + 255) / 256 * 256;
+    return p;
+  };
+  const jd_cache_config_t& g = c->cfg;
+  SharedView v;
+  v.count = (int32_t*)take(256);
+  v.groups = base ? v.count + 1 : nullptr;
+  for (int32_t** x : {&v.leader, &v.same, &v.group_start, &v.group_tokens, &v.group_leader, &v.member, &v.entry_group, &v.entry_place, &v.entry_slot,
+                      &v.first, &v.units_a, &v.units_b})
+    *x = (int32_t*)take((size_t)(B + 1) * 4);
+  const size_t row = (size_t)(g.head_dim + kPartPad) * 4, rows = (size_t)B * nodes * (g.q_heads / g.kv_heads);
+  v.rec_a = (float*)take(rows * g.kv_heads * row);
+  v.rec_b = (float*)take(rows * g.kv_heads * row);
+  // two parts for each CTA of the prefix call, as in carve_cache
+  const size_t most = std::max<size_t>(c->tm_ok ? std::min<size_t>(rows, 256) : 0, 2 * std::min<size_t>(rows, kSimtRows));
+  v.part = (float*)take((size_t)c->num_sms * 2 * most * row);
+  if (s) *s = v;
+  return off;
+}
+bool shared_ok(jd_cache_t c, const jd_shared_t* plan, SharedView* s) {
+  if (!c || !plan || plan->B < 1 || plan->B > kMaxCacheBatch || plan->nodes < 1 || plan->nodes > c->cfg.max_nodes) return false;
+  if (!plan->buffer || (reinterpret_cast<uintptr_t>(plan->buffer) & 255u) || plan->bytes < carve_shared(c, plan->B, plan->nodes, nullptr, nullptr)) return false;
+  carve_shared(c, plan->B, plan->nodes, (char*)plan->buffer, s);
+  return true;
+}
+
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                   const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -637,49 +712,53 @@ jd_status_t jd_cache_append_heads(jd_cache_t c, const jd_append_args_t* a, const
 }
 
 jd_status_t jd_cache_attend(jd_cache_t c, const jd_attend_args_t* a, void* cuda_stream) {
-  if (!c || !a || !batch_ok(c, a->B, a->slots) || !tree_ok(c, a->tree)) return JD_ERR_INVALID_ARG;
-  const jd_cache_config_t& g = c->cfg;
-  const int e = g.dtype == JD_DTYPE_F32 ? 4 : 2;
-  if (a->layer < 0 || a->layer >= g.num_layers || !a->q || !a->out || a->q == a->out || !on16(a->q) || !on16(a->out) || !on4(a->lse))
-    return JD_ERR_INVALID_ARG;
-  const int64_t qd = (int64_t)g.q_heads * g.head_dim;
-  if (!stride_ok(a->q_stride, qd, e) || !stride_ok(a->out_stride, qd, e) || !(a->scale > 0.f && std::isfinite(a->scale))) return JD_ERR_INVALID_ARG;
-  if (a->variant < JD_ATTEND_AUTO || a->variant > JD_ATTEND_TENSOR) return JD_ERR_INVALID_ARG;
+  if (!attend_ok(c, a)) return JD_ERR_INVALID_ARG;
   if (a->variant == JD_ATTEND_TENSOR && !c->tm_ok) return JD_ERR_UNSUPPORTED;
   const bool tensor = a->variant != JD_ATTEND_SIMT && c->tm_ok;
-  OnDevice dev(g.device);
+  OnDevice dev(c->cfg.device);
   if (!dev.ok()) return JD_ERR_CUDA;
-  AttendParams p;
-  p.c = view_of(c);
-  p.B = a->B; p.layer = a->layer; p.T = a->tree.nodes; p.W = (a->tree.nodes + 31) / 32;
-  p.q_heads = g.q_heads; p.group = g.q_heads / g.kv_heads;
-  p.rows = p.T * p.group;
-  p.slots = a->slots;
-  p.mask = a->tree.mask;
-  p.mask_stride = a->tree.per_seq ? (int64_t)p.T * p.W : 0;
-  p.num_nodes = a->tree.num_nodes;
-  p.q = (const char*)a->q; p.out = (char*)a->out;
-  p.q_stride = (a->q_stride ? a->q_stride : qd) * e; p.out_stride = (a->out_stride ? a->out_stride : qd) * e;
-  p.lse = a->lse;
-  p.scale_log2 = a->scale * 1.4426950408889634f;
-  p.part = c->part;
-  p.split = c->split;
-  if (tensor) {
-    p.tile_shift = kTensorTileShift;
-    p.seg_cost = tensor_seg_cost(g.head_dim, p.rows);
-    p.rows_per_block = p.rows > 128 ? 256 : 128;
-  } else {
-    p.tile_shift = kSimtTileShift;
-    p.seg_cost = kSimtSegCost;
-    p.rows_per_block = p.rows <= 4 ? 4 : kSimtRows;   // one token's few rows leave the others' registers and products out
-  }
-  p.part_rows = std::min(p.rows, p.rows_per_block);
-  p.row_blocks = (p.rows + p.rows_per_block - 1) / p.rows_per_block;
-  p.groups = std::max(1, (tensor ? c->num_sms : 2 * c->num_sms) / p.row_blocks);
+  const AttendParams p = attend_params(c, *a, tensor);
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  cudaError_t err = tensor ? run_attend_tensor(p, c->tm_k, c->tm_v, st) : run_attend_simt(p, g.dtype, st);
+  cudaError_t err = tensor ? run_attend_tensor(p, c->tm_k, c->tm_v, st) : run_attend_simt(p, c->cfg.dtype, st);
   // one group alone splits nothing
-  if (err == cudaSuccess && p.groups > 1) err = run_attend_join(p, g.dtype, st);
+  if (err == cudaSuccess && p.groups > 1) err = run_attend_join(p, c->cfg.dtype, st);
+  return finish(c, err, st);
+}
+
+size_t jd_cache_shared_bytes(jd_cache_t c, int32_t B, int32_t nodes) {
+  return c && B >= 1 && B <= kMaxCacheBatch && nodes >= 1 && nodes <= c->cfg.max_nodes ? carve_shared(c, B, nodes, nullptr, nullptr) : 0;
+}
+
+jd_status_t jd_cache_share(jd_cache_t c, const jd_shared_t* plan, const int32_t* slots, const int32_t* groups, void* cuda_stream) {
+  SharedView s;
+  if (!shared_ok(c, plan, &s) || !batch_ok(c, plan->B, slots) || !on4(groups)) return JD_ERR_INVALID_ARG;
+  OnDevice dev(c->cfg.device);
+  if (!dev.ok()) return JD_ERR_CUDA;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  return finish(c, run_share(view_of(c), s, plan->B, plan->nodes * (c->cfg.q_heads / c->cfg.kv_heads), slots, groups, st), st);
+}
+
+jd_status_t jd_cache_attend_shared(jd_cache_t c, const jd_attend_args_t* a, const jd_shared_t* plan, void* cuda_stream) {
+  SharedView s;
+  if (!attend_ok(c, a) || !shared_ok(c, plan, &s) || plan->B != a->B || a->tree.nodes > plan->nodes) return JD_ERR_INVALID_ARG;
+  if (a->B == 1) return jd_cache_attend(c, a, cuda_stream);   // nobody to share with
+  if (a->variant == JD_ATTEND_TENSOR && !c->tm_ok) return JD_ERR_UNSUPPORTED;
+  const bool tensor = a->variant != JD_ATTEND_SIMT && c->tm_ok;
+  OnDevice dev(c->cfg.device);
+  if (!dev.ok()) return JD_ERR_CUDA;
+  AttendParams suffix = attend_params(c, *a, tensor);
+  suffix.sh = s;
+  AttendParams prefix = suffix;
+  const int most = a->B * suffix.rows;                        // rows of a group: up to 2^27
+  prefix.rows_per_block = tensor ? (most > 128 ? 256 : 128) : (most <= 4 ? 4 : kSimtRows);
+  prefix.part_rows = std::min(most, prefix.rows_per_block);
+  prefix.row_blocks = 1;
+  prefix.groups = tensor ? c->num_sms : 2 * c->num_sms;
+  if (tensor) prefix.seg_cost = tensor_seg_cost(c->cfg.head_dim, most);
+  prefix.part = s.part;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  cudaError_t err = tensor ? run_attend_shared_tensor(prefix, most, suffix, c->tm_k, c->tm_v, st) : run_attend_shared_simt(prefix, suffix, c->cfg.dtype, st);
+  if (err == cudaSuccess) err = run_attend_shared_join(prefix, suffix, c->cfg.dtype, st);
   return finish(c, err, st);
 }
 

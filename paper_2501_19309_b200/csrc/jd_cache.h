@@ -4,6 +4,8 @@
 
 #include <cuda.h>
 
+#include <type_traits>
+
 #include "jd_common.cuh"
 
 struct jd_cache_s {
@@ -77,6 +79,37 @@ __device__ __forceinline__ void slot_state(const CacheView& c, int slot, int& le
 // of its group if the part begins the segment, else in slot 0, so two slots are enough.
 // The cut depends on nothing but the lengths and the SM count: results repeat bit for bit.
 // ---------------------------------------------------------------------------------------
+// Sequences that share a prefix (jd_cache_share). A call is then two: the prefix tiles of every group once, for the rows of all its members
+// one behind another (kPrefix: a "sequence" is a group, its rows in blocks of rows_per_block), and the tiles behind them for every sequence by itself
+// (kSuffix); a join adds the two up. Every piece leaves numerators, maximum and sum: of a whole segment in a record of the row's own, of a part in its
+// group's slot.
+enum Share { kAlone = 0, kPrefix = 1, kSuffix = 2 };
+template <int kShare> using ShareOf = std::integral_constant<int, kShare>;
+
+constexpr int kPrefixTokens = 128;   // prefixes are cut to whole tiles of the tensor-core kernel, which are whole tiles of the other
+// tiles of kPrefixTokens that a group has to save: what its segment costs to begin, end and join is four to six tiles
+constexpr int kPrefixWorth = 8;
+
+struct SharedView {                  // arrays of a plan of B sequences, all on the device
+  int32_t* count;                    // [1] blocks of jd_cache_share that are done (self-resetting)
+  int32_t* groups;                   // [1]
+  int32_t* leader;                   // [B] the first entry with the same beginning, and the tokens that both have in the same pages: scratch
+  int32_t* same;
+  int32_t* group_start;              // [B + 1] first of the group's members
+  int32_t* group_tokens;             // [B]
+  int32_t* group_leader;             // [B] entry
+  int32_t* member;                   // [B] entries by group
+  int32_t* entry_group;              // [B] -1: none
+  int32_t* entry_place;              // [B] number within the group
+  int32_t* entry_slot;               // [B]
+  int32_t* first;                    // [B] tokens that the prefix call takes off the sequence, as the tables stand at the call
+  int32_t* units_a;                  // [B + 1] units of the two calls (unit_prefix)
+  int32_t* units_b;
+  float* rec_a;                      // [B x T x group][kv_heads][head_dim + kPartPad] rows by group member; by entry
+  float* rec_b;
+  float* part;                       // parts of the prefix call
+};
+
 struct AttendParams {
   CacheView c;
   int B, layer, T, W;              // W: mask words of a row
@@ -96,6 +129,7 @@ struct AttendParams {
   int64_t q_stride, out_stride;    // bytes between tokens
   float* lse;
   float scale_log2;                // scale x log2(e)
+  SharedView sh;                   // kPrefix, kSuffix
   int4* split;                     // [groups] sequence, kv head and last group of the segment that the group leaves unfinished; x < 0: none
   float* part;                     // [groups * row_blocks][2][part_rows][head_dim + kPartPad]
 };
@@ -105,6 +139,14 @@ constexpr int kPartPad = 4;        // a part's row is head_dim numerators, m, l 
 struct SeqExtent {
   int slot, ctx, nodes, kv_end;
 };
+// With a shared prefix: of a sequence its first tile behind it; of a group its first member, and its rows in place of nodes.
+struct SharedExtent : SeqExtent {
+  int more;
+};
+template <int kShare> struct ExtentOf { using type = SharedExtent; };
+template <> struct ExtentOf<kAlone> { using type = SeqExtent; };
+template <int kShare> using Extent = typename ExtentOf<kShare>::type;
+
 __device__ __forceinline__ SeqExtent seq_extent(const AttendParams& p, int b) {
   SeqExtent e;
   e.slot = slot_of(p.c, p.slots, b);
@@ -121,18 +163,80 @@ __device__ __forceinline__ int extent_units(const AttendParams& p, const SeqExte
   return p.seg_cost + max(1, (e.kv_end + (1 << p.tile_shift) - 1) >> p.tile_shift);
 }
 
-// prefix[b] = units of one kv head in the sequences before b, prefix[B] = all; extents (optional): what seq_extent says of each
+// Whether slot has the first `tokens` tokens in the same pages as slot `lead`, which had them so when the plan was made. Tables change
+// from their ends alone or as a whole, so the last page of the prefix tells.
+__device__ __forceinline__ bool still_shared(const CacheView& c, int slot, int lead, int tokens) {
+  int len, held, lead_len, lead_held;
+  slot_state(c, slot, len, held);
+  slot_state(c, lead, lead_len, lead_held);
+  if (tokens < 1 || tokens > len || tokens > lead_len) return false;
+  const int at = (tokens - 1) >> c.page_shift;
+  return __ldcg(c.table + (int64_t)slot * c.max_pages + at) == __ldcg(c.table + (int64_t)lead * c.max_pages + at);
+}
+// By the prefix call, for the suffix call and the join: what is taken off each sequence. A plan that the tables have left behind takes nothing off.
+__device__ __forceinline__ void check_shared(const AttendParams& p, int i0, int step) {
+  const int groups = min(max(__ldcg(p.sh.groups), 0), p.B);
+  for (int b = i0; b < p.B; b += step) {
+    const int slot = p.slots ? __ldcg(p.slots + b) : b, g = __ldcg(p.sh.entry_group + b);
+    int first = 0;
+    if (slot >= 0 && slot < p.c.max_seqs && g >= 0 && g < groups && slot == __ldcg(p.sh.entry_slot + b)) {
+      const int tokens = __ldcg(p.sh.group_tokens + g), lead = __ldcg(p.sh.entry_slot + __ldcg(p.sh.group_leader + g));
+      if (still_shared(p.c, slot, lead, tokens)) first = tokens;
+    }
+    p.sh.first[b] = first;
+  }
+}
+
+// What sequence or group i of the call is.
+template <int kShare> __device__ __forceinline__ Extent<kShare> extent_at(const AttendParams& p, int i) {
+  if constexpr (kShare == kAlone) {
+    return seq_extent(p, i);
+  } else if constexpr (kShare == kSuffix) {
+    SharedExtent e;
+    static_cast<SeqExtent&>(e) = seq_extent(p, i);
+    e.more = e.slot < 0 ? 0 : __ldcg(p.sh.first + i) >> p.tile_shift;
+    return e;
+  } else {
+    SharedExtent e;
+    e.slot = -1;
+    e.ctx = e.nodes = e.kv_end = e.more = 0;
+    if (i >= __ldcg(p.sh.groups)) return e;
+    const int start = __ldcg(p.sh.group_start + i), tokens = __ldcg(p.sh.group_tokens + i), lead = __ldcg(p.sh.entry_slot + __ldcg(p.sh.group_leader + i));
+    int len, held;
+    slot_state(p.c, lead, len, held);
+    if (tokens > len) return e;
+    e.slot = lead;
+    e.ctx = e.kv_end = tokens;
+    e.more = start;
+    e.nodes = (__ldcg(p.sh.group_start + i + 1) - start) * p.rows;
+    return e;
+  }
+}
+__device__ __forceinline__ int row_blocks_of(const AttendParams& p, int rows) { return (int)((uint32_t)(rows + p.rows_per_block - 1) / (uint32_t)p.rows_per_block); }
+template <int kShare> __device__ __forceinline__ int units_at(const AttendParams& p, const Extent<kShare>& e) {
+  if constexpr (kShare == kAlone) {
+    return extent_units(p, e);
+  } else if constexpr (kShare == kSuffix) {
+    const int n = extent_units(p, e);
+    return n == 0 ? 0 : max(n - e.more, p.seg_cost + 1);
+  } else {
+    return e.nodes == 0 ? 0 : row_blocks_of(p, e.nodes) * (p.seg_cost + (e.ctx >> p.tile_shift));
+  }
+}
+
+// prefix[b] = units of one kv head in the sequences before b, prefix[B] = all; extents (optional): what extent_at says of each
 // sequence. By the whole block.
-__device__ __forceinline__ void unit_prefix(const AttendParams& p, int* prefix, int* warp_sums, SeqExtent* extents = nullptr) {
+template <int kShare>
+__device__ __forceinline__ void unit_prefix(ShareOf<kShare>, const AttendParams& p, int* prefix, int* warp_sums, Extent<kShare>* extents = nullptr) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nthreads = blockDim.x, nwarps = nthreads >> 5;
   int carry = 0;
   for (int b0 = 0; b0 < p.B; b0 += nthreads) {
     const int b = b0 + tid;
     int n = 0;
     if (b < p.B) {
-      const SeqExtent e = seq_extent(p, b);
+      const Extent<kShare> e = extent_at<kShare>(p, b);
       if (extents) extents[b] = e;
-      n = extent_units(p, e);
+      n = units_at<kShare>(p, e);
     }
     int x = n;
 #pragma unroll
@@ -153,6 +257,11 @@ __device__ __forceinline__ void unit_prefix(const AttendParams& p, int* prefix, 
   }
   if (tid == 0) prefix[p.B] = carry;
   __syncthreads();
+  if constexpr (kShare != kAlone) {
+    int32_t* to = kShare == kPrefix ? p.sh.units_a : p.sh.units_b;
+    if (blockIdx.x == 0)
+      for (int i = tid; i <= p.B; i += nthreads) to[i] = prefix[i];
+  }
 }
 
 // First unit of run g, and the run that holds unit u; 32-bit divisions where they are enough (64-bit ones take ten times as long).
@@ -173,21 +282,36 @@ __device__ __forceinline__ int run_of(int64_t units, int groups, int64_t u) {
 struct Piece {
   int b, head, tile0, tiles, all;   // all: tiles of the whole segment
   int64_t next;                     // first unit behind it
+  int first;                        // the segment's first tile in the sequence; 0 unless a prefix is taken off
+  int row0;                         // the segment's first row; 0 unless rows are a group's
 };
-__device__ __forceinline__ Piece piece_at(const AttendParams& p, const int* prefix, int64_t u, int64_t run1) {
+template <int kShare = kAlone>
+__device__ __forceinline__ Piece piece_at(const AttendParams& p, const int* prefix, int64_t u, int64_t run1, const Extent<kShare>* extents = nullptr) {
   Piece x;
+  x.first = x.row0 = 0;
   int lo = 0, hi = p.B - 1;         // the last sequence with units whose first is at or before u
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if ((int64_t)prefix[mid] * p.c.kv_heads <= u) lo = mid; else hi = mid - 1;
   }
   x.b = lo;
-  const int n = prefix[lo + 1] - prefix[lo];
   const int64_t first = (int64_t)prefix[lo] * p.c.kv_heads;
-  const int in_seq = (int)(u - first);
-  x.head = (int)((uint32_t)in_seq / (uint32_t)n);
-  const int at = in_seq - x.head * n;
-  const int64_t seg_end = first + (int64_t)(x.head + 1) * n;
+  int n = prefix[lo + 1] - prefix[lo], segment;
+  if constexpr (kShare == kPrefix) {   // a group's segments: heads, and blocks of its rows within
+    const Extent<kShare> e = extents ? extents[lo] : extent_at<kShare>(p, lo);
+    const int blocks = row_blocks_of(p, e.nodes);
+    n = p.seg_cost + (e.ctx >> p.tile_shift);
+    const int64_t in_seq = u - first;
+    segment = in_seq < 0x7FFFFFFF ? (int)((uint32_t)in_seq / (uint32_t)n) : (int)(in_seq / n);
+    x.head = (int)((uint32_t)segment / (uint32_t)blocks);
+    x.row0 = (segment - x.head * blocks) * p.rows_per_block;
+  } else {
+    const int in_seq = (int)(u - first);
+    x.head = segment = (int)((uint32_t)in_seq / (uint32_t)n);
+    if constexpr (kShare == kSuffix) x.first = extents ? extents[lo].more : extent_at<kShare>(p, lo).more;
+  }
+  const int at = (int)(u - first - (int64_t)segment * n);
+  const int64_t seg_end = first + (int64_t)(segment + 1) * n;
   x.next = min(seg_end, run1);
   x.all = n - p.seg_cost;
   x.tile0 = max(0, at - p.seg_cost);
@@ -238,6 +362,11 @@ inline cudaError_t launch_chained(void (*kernel)(Params...), dim3 grid, dim3 blo
 cudaError_t run_attend_simt(const AttendParams& p, int dtype, cudaStream_t st);
 cudaError_t run_attend_tensor(const AttendParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st);
 cudaError_t run_attend_join(const AttendParams& p, int dtype, cudaStream_t st);
+// The two calls of an attention with a plan, and what adds them up. most: rows that a group may have
+cudaError_t run_attend_shared_simt(const AttendParams& prefix, const AttendParams& suffix, int dtype, cudaStream_t st);
+cudaError_t run_attend_shared_tensor(const AttendParams& prefix, int most, const AttendParams& suffix, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
+                                     cudaStream_t st);
+cudaError_t run_attend_shared_join(const AttendParams& prefix, const AttendParams& suffix, int dtype, cudaStream_t st);
 bool simt_attend_configure();
 bool attend_configure();   // dynamic shared-memory limits on the current device, once per device
 constexpr int kSimtRows = 16, kSimtTileShift = 6, kSimtSegCost = 1;
@@ -248,6 +377,7 @@ constexpr int kTensorTileShift = 7;
 // 4,000 tokens: 101 us at 1, 70 at 4, 66 at 5, 68 at 6).
 constexpr int tensor_seg_cost(int head_dim, int rows) { return head_dim == 64 ? 6 : (rows > 128 ? 5 : 4); }
 
+cudaError_t run_share(const CacheView& c, const SharedView& s, int B, int rows, const int32_t* slots, const int32_t* groups, cudaStream_t st);
 bool rope_valid(const jd_rope_t& r, int head_dim);
 cudaError_t run_append(const CacheView& c, const jd_append_args_t& a, int q_heads, int dtype, cudaStream_t st);
 bool append_heads_valid(const jd_head_norm_t* n, const jd_rope_axes_t* a, const jd_rope_t* r);

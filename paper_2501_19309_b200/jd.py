@@ -45,7 +45,7 @@ EXPORTS = ["jd_version", "jd_status_string", "jd_workspace_bytes", "jd_create", 
            "jd_cache_destroy", "jd_cache_reserve", "jd_cache_append", "jd_cache_attend", "jd_cache_commit",
            "jd_cache_fork", "jd_cache_truncate", "jd_cache_compact", "jd_cache_last_status", "jd_head_rope",
            "jd_head_rope_grad", "jd_head_rope_grad_workspace_bytes", "jd_cache_append_heads",
-           "jd_verify_probs"]
+           "jd_verify_probs", "jd_cache_shared_bytes", "jd_cache_share", "jd_cache_attend_shared"]
 
 
 class jd_config_t(C.Structure):
@@ -136,6 +136,10 @@ class jd_attend_args_t(C.Structure):
                 ("scale", C.c_float), ("variant", C.c_int32)]
 
 
+class jd_shared_t(C.Structure):
+    _fields_ = [("B", C.c_int32), ("nodes", C.c_int32), ("buffer", C.c_void_p), ("bytes", C.c_size_t)]
+
+
 class jd_commit_args_t(C.Structure):
     _fields_ = [("B", C.c_int32), ("slots", C.c_void_p), ("accept_len", C.c_void_p), ("num_paths", C.c_int32),
                 ("path_len", C.c_int32), ("paths", C.c_void_p), ("chosen", C.c_void_p)]
@@ -198,13 +202,16 @@ def load():
     lib.jd_cache_reserve.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p]
     lib.jd_cache_append.argtypes = [C.c_void_p, C.POINTER(jd_append_args_t), C.c_void_p]
     lib.jd_cache_attend.argtypes = [C.c_void_p, C.POINTER(jd_attend_args_t), C.c_void_p]
+    lib.jd_cache_shared_bytes.argtypes = [C.c_void_p, C.c_int32, C.c_int32]
+    lib.jd_cache_share.argtypes = [C.c_void_p, C.POINTER(jd_shared_t), C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.jd_cache_attend_shared.argtypes = [C.c_void_p, C.POINTER(jd_attend_args_t), C.POINTER(jd_shared_t), C.c_void_p]
     lib.jd_cache_commit.argtypes = [C.c_void_p, C.POINTER(jd_commit_args_t), C.c_void_p]
     lib.jd_cache_fork.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
     lib.jd_cache_truncate.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
     lib.jd_cache_compact.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p]
     lib.jd_cache_last_status.argtypes = [C.c_void_p, C.POINTER(C.c_int)]
     for name in EXPORTS:
-        if name.endswith("workspace_bytes"):
+        if name.endswith("_bytes"):
             getattr(lib, name).restype = C.c_size_t
         elif name not in ("jd_version", "jd_status_string"):
             getattr(lib, name).restype = C.c_int
@@ -446,7 +453,7 @@ class Verifier:
 
 # ------------------------------------------------------------------ around the verification call (cache.py)
 def __getattr__(name: str):
-    if name in ("PagedCache", "Rotary", "HeadNorm", "Tree", "rope_frequencies", "mask_words"):     # torch is imported on first use only
+    if name in ("PagedCache", "Rotary", "HeadNorm", "SharedPrefix", "Tree", "rope_frequencies", "mask_words"):     # torch is imported on first use only
         from . import cache
         return getattr(cache, name)
     if name == "verify_probs":
