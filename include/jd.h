@@ -573,7 +573,7 @@ jd_status_t jd_cache_attend(jd_cache_t c, const jd_attend_args_t* args, void* cu
  * read those pages once for all of them. HOST struct. The buffer is the caller's, on the cache's device: 256-byte aligned,
  * jd_cache_shared_bytes() of it, zero-filled before its first use; calls that may run at the same time take a plan each. */
 typedef struct {
-  int32_t B;          /* sequences of the calls, 1..1024 */
+  int32_t B;          /* sequences of the calls, 1..512 */
   int32_t nodes;      /* most nodes of a call, 1..max_nodes */
   void* buffer;
   size_t bytes;

@@ -342,7 +342,7 @@ class SharedPrefix:
     def __init__(self, cache: "PagedCache", B: int, nodes: int):
         need = cache._lib.jd_cache_shared_bytes(cache.h, B, nodes)
         if need == 0:
-            raise ValueError("share: up to 1024 sequences, 1..max_nodes nodes")
+            raise ValueError("share: up to 512 sequences, 1..max_nodes nodes")
         self.B, self.nodes, self.cache = B, nodes, cache
         self.buffer = torch.zeros(need, dtype=torch.uint8, device=cache.device)
         self.c = jd.jd_shared_t(B, nodes, self.buffer.data_ptr(), need)

@@ -54,11 +54,6 @@ size_t simt_smem(int head_dim, int rows) {
   return sizeof(float) * ((size_t)2 * kTile * pitch_of(head_dim) + rows * pitch_of(head_dim) + (rows == 4 ? 1 : 2) * kTile * score_pad(rows));
 }
 
-template <typename E> __device__ __forceinline__ int member0_of(const E& ex) {
-  if constexpr (std::is_same_v<E, SharedExtent>) return ex.more;
-  else return 0;
-}
-
 // kCols: groups of 128 columns that a lane's accumulators cover (head_dim <= 128 kCols)
 // kRows: query rows of the block, 4 or 16
 template <typename T, int kCols, int kRows, int kShare>
@@ -77,13 +72,12 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
   float* sS1 = sS + kTile * kScorePad;   // 16 rows: the other half of the columns' share
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int g = blockIdx.x / p.row_blocks, rb = blockIdx.x - g * p.row_blocks;
-  int r0 = rb * kRows, nrows = min(kRows, p.rows - r0);   // of a group's rows: move with the piece
+  int r0 = rb * kRows, nrows = min(kRows, p.rows - r0);   // with shared prefixes they move with the piece
   pdl_wait();
   pdl_trigger();
   if (kShare == kAlone && rb == 0 && tid == 0) split_none(p, g);
   unit_prefix(ShareOf<kShare>(), p, prefix, warp_sums);
-  if (kShare == kPrefix && tid == 0) check_shared(p, blockIdx.x, gridDim.x);
-  const int64_t units = (int64_t)prefix[p.B] * p.c.kv_heads;
+  const int64_t units = (int64_t)prefix[items_of<kShare>(p)] * p.c.kv_heads;
   if (units == 0) return;
   const int64_t run0 = run_start(units, p.groups, g), run1 = run_start(units, p.groups, g + 1);
   const T* kbase = reinterpret_cast<const T*>(p.c.k);
@@ -94,11 +88,12 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
     const Piece x = piece_at<kShare>(p, prefix, u, run1);
     u = x.next;
     if (x.tiles == 0) continue;
-    const int b = x.b, head = x.head, tiles = x.all, tile0 = x.first + x.tile0, ntiles = x.tiles;
-    const Extent<kShare> ex = extent_at<kShare>(p, b);
-    if constexpr (kShare == kPrefix) {
+    const bool shared_rows = kShare == kShared && x.b < p.max_groups;
+    const int b = x.b - (kShare == kShared ? p.max_groups : 0), head = x.head, tiles = x.all, tile0 = x.first + x.tile0, ntiles = x.tiles;
+    const Extent<kShare> ex = extent_at<kShare>(p, x.b);
+    if constexpr (kShare == kShared) {
       r0 = x.row0;
-      nrows = min(kRows, ex.nodes - r0);
+      nrows = min(kRows, (shared_rows ? ex.nodes : p.rows) - r0);
     }
 
     __syncthreads();   // the previous segment's buffers are free
@@ -107,13 +102,13 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
       float v[4] = {0.f, 0.f, 0.f, 0.f};
       int from = b, row = r0 + r;
       bool there = r < nrows;
-      if (kShare == kPrefix && there) {              // whose row it is
+      if (shared_rows && there) {                    // whose row it is
         const int m = row / p.rows;
         from = __ldcg(p.sh.member + member0_of(ex) + m);
         row -= m * p.rows;
       }
       const int t = row / p.group, gq = row - t * p.group;
-      if (kShare == kPrefix) there = there && (!p.num_nodes || t < __ldcg(p.num_nodes + from));
+      if (shared_rows) there = there && (!p.num_nodes || t < __ldcg(p.num_nodes + from));
       else there = there && t < ex.nodes;
       if (there)
         load4<T>(reinterpret_cast<const T*>(p.q + ((int64_t)from * p.T + t) * p.q_stride) + (int64_t)(head * p.group + gq) * D + d, v);
@@ -121,7 +116,7 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
       for (int k = 0; k < 4; ++k) sQ[r * pitch + d + k] = v[k];
     }
     if (tid < kRows) { s_m[tid] = -INFINITY; s_l[tid] = 0.f; }
-    for (int i = tid; kShare != kPrefix && i < kRows * p.W; i += kThreads) {
+    for (int i = tid; !shared_rows && i < kRows * p.W; i += kThreads) {
       const int r = i / p.W, w = i - r * p.W, t = (r0 + r) / p.group;
       s_mask[r][w] = r < nrows && t < ex.nodes ? node_word(p, b, t, w, ex.nodes) : 0u;
     }
@@ -312,7 +307,7 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
       }
     __syncthreads();
     const bool whole = ntiles == tiles, begins = x.tile0 == 0;
-    const bool direct = whole && (kShare == kAlone || (kShare == kSuffix && x.first == 0));   // nothing to add
+    const bool direct = whole && (kShare == kAlone || (!shared_rows && x.first == 0));   // nothing to add
     if (kShare == kAlone && !whole && tile0 == 0 && rb == 0 && tid == 0) split_set(p, g, units, x);
     for (int i = tid; i < nrows * (D / 4); i += kThreads) {
       const int r = i / (D / 4), d = (i - r * (D / 4)) * 4;
@@ -333,8 +328,8 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
       } else {
         float* part = p.part + (((int64_t)blockIdx.x * 2 + (begins ? 1 : 0)) * p.part_rows + r) * (D + kPartPad);
         if (kShare != kAlone && whole)
-          part = (kShare == kPrefix ? p.sh.rec_a : p.sh.rec_b) +
-                 (((int64_t)(kShare == kPrefix ? member0_of(ex) : b) * p.rows + r0 + r) * p.c.kv_heads + head) * (D + kPartPad);
+          part = (shared_rows ? p.sh.rec_group : p.sh.rec_own) +
+                 (((shared_rows ? member0_of(ex) : b) * p.rows + r0 + r) * p.c.kv_heads + head) * (D + kPartPad);
         *reinterpret_cast<float4*>(part + d) = x;
         if (d == 0) { part[D] = s_m[r]; part[D + 1] = s_l[r]; }
       }
@@ -496,12 +491,22 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendPara
   }
 }
 
-// Adds up the prefix call's and the suffix call's results of every row, parts and records alike. A warp for a row, or, with few rows, whose
-// parts from many SMs are what takes the time, a block of four. Rows that the suffix call has written already (no prefix, one run) are left alone.
+// Adds up what a row's group and the row's sequence have left, parts and records alike. A warp for a row, or, with few rows, whose
+// parts from many SMs are what takes the time, a block of four. Rows that are written already (no prefix, one run) are left alone.
 constexpr int kSharedFewRows = 4096;
 
+struct Parts {                       // of a row in one segment
+  int run, count;                    // the first run with tiles of the segment, and their number; 1: a record
+};
+__device__ __forceinline__ Parts parts_of(const AttendParams& p, int64_t all, int64_t first_unit, int n) {
+  Parts x;
+  x.run = run_of(all, p.groups, first_unit + p.seg_cost);
+  x.count = run_of(all, p.groups, first_unit + n - 1) - x.run + 1;
+  return x;
+}
+
 template <typename T, int kCols>
-__global__ void __launch_bounds__(32 * kJoinWarps) attend_shared_join_kernel(const __grid_constant__ AttendParams a, const __grid_constant__ AttendParams p, bool few) {
+__global__ void __launch_bounds__(32 * kJoinWarps) attend_shared_join_kernel(AttendParams p, bool few) {
   __shared__ float4 s_o[kJoinWarps][kCols][32];
   __shared__ float2 s_ml[kJoinWarps];
   pdl_wait();
@@ -514,36 +519,32 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_shared_join_kernel(con
   const int h = (int)(id - token * p.q_heads), b = (int)(token / p.T), t = (int)(token - (int64_t)b * p.T);
   const int head = h / p.group, row = t * p.group + h - head * p.group;
   const int nodes = p.num_nodes ? min(max(__ldcg(p.num_nodes + b), 0), p.T) : p.T;
-  const int ub0 = __ldcg(p.sh.units_b + b), n = __ldcg(p.sh.units_b + b + 1) - ub0, first = __ldcg(p.sh.first + b);
-  const int64_t all_b = (int64_t)__ldcg(p.sh.units_b + p.B) * p.c.kv_heads;
-  if (t >= nodes || n == 0) return;                    // n == 0: a padding sequence
-  const int64_t seg_b = (int64_t)ub0 * p.c.kv_heads + (int64_t)head * n;
-  const int b0 = run_of(all_b, p.groups, seg_b + p.seg_cost), b1 = run_of(all_b, p.groups, seg_b + n - 1);
-  if (first == 0 && b0 == b1) return;
-  int a0 = 0, count_a = 0, row_a = 0, block_row = 0;
-  int64_t record_a = 0;
+  const int32_t* units = p.sh.units + p.max_groups + b;
+  const int u0 = __ldcg(units), own_units = __ldcg(units + 1) - u0, first = __ldcg(p.sh.first + b), g = __ldcg(p.sh.entry_group + b);
+  const int64_t all = (int64_t)__ldcg(p.sh.units + p.max_groups + p.B) * p.c.kv_heads;
+  if (t >= nodes || own_units == 0) return;            // own_units == 0: a padding sequence
+  const int blocks = row_blocks_of(p, p.rows), block = row / p.rows_per_block, n = own_units / blocks;
+  const Parts own = parts_of(p, all, (int64_t)u0 * p.c.kv_heads + ((int64_t)head * blocks + block) * n, n);
+  if (first == 0 && own.count == 1) return;
+  Parts group = {0, 0};
+  int64_t group_row = 0;             // among the rows of all groups; in its block
+  int group_place = 0;
   if (first > 0) {
-    const int g = __ldcg(p.sh.entry_group + b), start = __ldcg(p.sh.group_start + g), members = __ldcg(p.sh.group_start + g + 1) - start;
-    row_a = __ldcg(p.sh.entry_place + b) * p.rows + row;
-    record_a = ((int64_t)start * p.rows + row_a) * p.c.kv_heads + head;
-    const int blocks = row_blocks_of(a, members * p.rows), block = row_a / a.rows_per_block, na = a.seg_cost + (first >> a.tile_shift);
-    block_row = row_a - block * a.rows_per_block;
-    const int64_t all_a = (int64_t)__ldcg(p.sh.units_a + p.B) * p.c.kv_heads;
-    const int64_t seg_a = (int64_t)__ldcg(p.sh.units_a + g) * p.c.kv_heads + ((int64_t)head * blocks + block) * na;
-    a0 = run_of(all_a, a.groups, seg_a + a.seg_cost);
-    count_a = run_of(all_a, a.groups, seg_a + na - 1) - a0 + 1;
+    const int start = __ldcg(p.sh.group_start + g), v0 = __ldcg(p.sh.units + g), group_units = __ldcg(p.sh.units + g + 1) - v0;
+    const int at = __ldcg(p.sh.entry_place + b) * p.rows + row, gn = p.seg_cost + (first >> p.tile_shift), gblocks = group_units / gn;
+    const int gblock = at / p.rows_per_block;
+    group_row = (int64_t)start * p.rows + at;
+    group_place = at - gblock * p.rows_per_block;
+    group = parts_of(p, all, (int64_t)v0 * p.c.kv_heads + ((int64_t)head * gblocks + gblock) * gn, gn);
   }
-  const int rb = row / p.rows_per_block;
-  auto at = [&](int i) -> const float* {               // part i: the prefix's first
-    if (i < count_a) {
-      if (count_a == 1) return p.sh.rec_a + record_a * pitch;
-      return a.part + (((int64_t)(a0 + i) * 2 + (i == 0 ? 1 : 0)) * a.part_rows + block_row) * pitch;
-    }
-    i -= count_a;
-    if (b0 == b1) return p.sh.rec_b + (((int64_t)b * p.rows + row) * p.c.kv_heads + head) * pitch;
-    return p.part + ((((int64_t)(b0 + i) * p.row_blocks + rb) * 2 + (i == 0 ? 1 : 0)) * p.part_rows + row - rb * p.rows_per_block) * pitch;
+  auto at = [&](int i) -> const float* {               // part i: the group's first
+    const bool of_group = i < group.count;
+    if (!of_group) i -= group.count;
+    const Parts x = of_group ? group : own;
+    if (x.count == 1) return (of_group ? p.sh.rec_group + (group_row * p.c.kv_heads + head) * pitch : p.sh.rec_own + (((int64_t)b * p.rows + row) * p.c.kv_heads + head) * pitch);
+    return p.part + (((int64_t)(x.run + i) * 2 + (i == 0 ? 1 : 0)) * p.part_rows + (of_group ? group_place : row - block * p.rows_per_block)) * pitch;
   };
-  const int last = count_a + b1 - b0;
+  const int last = group.count + own.count - 1;
   auto write = [&](int d, const float* o, float m, float l) {   // columns d .. d + 3
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const float y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
@@ -587,11 +588,8 @@ cudaError_t run_attend_simt(const AttendParams& p, int dtype, cudaStream_t st) {
   return dtype == JD_DTYPE_F32 ? launch_simt<float, kAlone>(p, st) : launch_simt<__nv_bfloat16, kAlone>(p, st);
 }
 
-cudaError_t run_attend_shared_simt(const AttendParams& prefix, const AttendParams& suffix, int dtype, cudaStream_t st) {
-  const bool f32 = dtype == JD_DTYPE_F32;
-  const cudaError_t err = f32 ? launch_simt<float, kPrefix>(prefix, st) : launch_simt<__nv_bfloat16, kPrefix>(prefix, st);
-  if (err != cudaSuccess) return err;
-  return f32 ? launch_simt<float, kSuffix>(suffix, st) : launch_simt<__nv_bfloat16, kSuffix>(suffix, st);
+cudaError_t run_attend_shared_simt(const AttendParams& p, int dtype, cudaStream_t st) {
+  return dtype == JD_DTYPE_F32 ? launch_simt<float, kShared>(p, st) : launch_simt<__nv_bfloat16, kShared>(p, st);
 }
 
 cudaError_t run_attend_join(const AttendParams& p, int dtype, cudaStream_t st) {
@@ -603,13 +601,13 @@ cudaError_t run_attend_join(const AttendParams& p, int dtype, cudaStream_t st) {
   return launch_chained(kernel, grid, dim3(32 * kJoinWarps), 0, st, p);
 }
 
-cudaError_t run_attend_shared_join(const AttendParams& prefix, const AttendParams& suffix, int dtype, cudaStream_t st) {
-  const int64_t rows = (int64_t)suffix.B * suffix.T * suffix.q_heads;
+cudaError_t run_attend_shared_join(const AttendParams& p, int dtype, cudaStream_t st) {
+  const int64_t rows = (int64_t)p.B * p.T * p.q_heads;
   const bool few = rows <= kSharedFewRows;
   const dim3 grid((unsigned)(few ? rows : (rows + kJoinWarps - 1) / kJoinWarps));
-  auto kernel = dtype == JD_DTYPE_F32 ? (suffix.c.head_dim <= 128 ? attend_shared_join_kernel<float, 1> : attend_shared_join_kernel<float, 2>)
-                                      : (suffix.c.head_dim <= 128 ? attend_shared_join_kernel<__nv_bfloat16, 1> : attend_shared_join_kernel<__nv_bfloat16, 2>);
-  return launch_chained(kernel, grid, dim3(32 * kJoinWarps), 0, st, prefix, suffix, few);
+  auto kernel = dtype == JD_DTYPE_F32 ? (p.c.head_dim <= 128 ? attend_shared_join_kernel<float, 1> : attend_shared_join_kernel<float, 2>)
+                                      : (p.c.head_dim <= 128 ? attend_shared_join_kernel<__nv_bfloat16, 1> : attend_shared_join_kernel<__nv_bfloat16, 2>);
+  return launch_chained(kernel, grid, dim3(32 * kJoinWarps), 0, st, p, few);
 }
 
 template <typename T, int kShare>
@@ -618,6 +616,6 @@ bool raise_limits() {
          raise_limit(attend_simt_kernel<T, 2, 4, kShare>, simt_smem(256, 4)) && raise_limit(attend_simt_kernel<T, 2, 16, kShare>, simt_smem(256, 16));
 }
 template <int kShare> bool raise_both() { return raise_limits<float, kShare>() && raise_limits<__nv_bfloat16, kShare>(); }
-bool simt_attend_configure() { return raise_both<kAlone>() && raise_both<kPrefix>() && raise_both<kSuffix>(); }
+bool simt_attend_configure() { return raise_both<kAlone>() && raise_both<kShared>(); }
 
 }  // namespace jd

@@ -265,12 +265,6 @@ __device__ __noinline__ float4 spoilt_by_context(const AttendParams& p, int slot
   return make_float4(sum[0], sum[1], sum[2], sum[3]);
 }
 
-// Row 0 of a group among the rows of all members of all groups.
-template <typename E> __device__ __forceinline__ int64_t ex_first_row(const AttendParams& p, const E& ex) {
-  if constexpr (std::is_same_v<E, SharedExtent>) return (int64_t)ex.more * p.rows;
-  else return 0;
-}
-
 template <int D, int kMode, int kShare>
 __global__ void __launch_bounds__(kThreads, 1)
 attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ AttendParams p) {
@@ -313,15 +307,13 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   unit_prefix(ShareOf<kShare>(), p, sh.prefix, sh.warp_sums, sh.extents);   // ends with a barrier
   pdl_trigger();
   tc_fence_after();
-  const int64_t units = (int64_t)sh.prefix[p.B] * p.c.kv_heads;
+  const int64_t units = (int64_t)sh.prefix[items_of<kShare>(p)] * p.c.kv_heads;
   const int64_t run0 = run_start(units, p.groups, g), run1 = run_start(units, p.groups, g + 1);
   const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem_base, 0);
   const uint32_t ring_addr = smem_u32(ring), q_addr = smem_u32(q_smem);
 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-    if (kShare == kPrefix && warp == 11 && lane == 0) check_shared(p, blockIdx.x, gridDim.x);
-    __syncwarp();
     if (warp == 8 || warp == 10) {
       // ------------------------------------------------------------------ producers: warp 8 fetches K tiles, warp 10 V tiles
       // Ring items are K and V of the run's tiles in turn. A box costs the issuing warp about 100 cycles, whatever its size, which with
@@ -474,12 +466,12 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     const int w = warp >> 2, r = tid & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t t_s = tmem + lanes + w * 128, t_o = tmem + lanes + 256 + w * 128;
-    int r0 = rb * p.rows_per_block;                                 // of a group's rows: moves with the piece
+    int r0 = rb * p.rows_per_block;                                 // with shared prefixes it moves with the piece
     const int copy = r / kCopyRows, col0 = copy * kCols;            // the copy that this warp belongs to, and its columns
     const int my_place = r % kCopyRows + (kPair ? w * 128 : 0);
     int my_row = r0 + my_place;
     bool warp_live = my_row - lane < p.rows;
-    const int t_node = my_row / p.group, gq = my_row - t_node * p.group;   // where rows are a sequence's
+    int t_node = my_row / p.group, gq = my_row - t_node * p.group;  // where rows are a sequence's
     const float c2 = p.scale_log2;
     const float c2_far = __uint_as_float((__float_as_uint(c2) + 0x7FFFFFu) & 0xFF800000u);
     uint32_t s_phase = 0, o_phase = 0;
@@ -506,22 +498,28 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     };
     auto fetch = [&](const Piece& y) {
       if (y.tiles == 0) return;
-      if constexpr (kShare == kPrefix) {             // rows of all members one behind another: whose each is comes first
+      if constexpr (kShare == kShared) {             // whose row each is comes first: a group's are those of all members one behind another
         const Extent<kShare> ex = sh.extents[y.b];
+        const bool group = y.b < p.max_groups;
         int64_t from[kQLoads];
 #pragma unroll
         for (int i = 0; i < kQLoads; ++i) {
-          const int row = y.row0 + (kPair ? w * 128 : 0) + q_r + i * kQRows, m = (int)((uint32_t)row / (uint32_t)p.rows), at = row - m * p.rows;
+          const int row = y.row0 + (kPair ? w * 128 : 0) + q_r + i * kQRows, m = group ? (int)((uint32_t)row / (uint32_t)p.rows) : 0, at = row - m * p.rows;
           const int t = (int)((uint32_t)at / (uint32_t)p.group);
           from[i] = -1;
-          if (row < ex.nodes) {
-            const int b = __ldcg(p.sh.member + ex.more + m);
-            if (!p.num_nodes || t < __ldcg(p.num_nodes + b))
+          if (row < (group ? ex.nodes : p.rows)) {
+            const int b = group ? __ldcg(p.sh.member + ex.more + m) : y.b - p.max_groups;
+            if (group ? !p.num_nodes || t < __ldcg(p.num_nodes + b) : t < ex.nodes)
               from[i] = ((int64_t)b * p.T + t) * p.q_stride + ((int64_t)y.head * p.group + at - t * p.group) * (D * 2) + q_c * 16;
           }
         }
 #pragma unroll
         for (int i = 0; i < kQLoads; ++i) q_regs[i] = from[i] >= 0 ? __ldcg(reinterpret_cast<const uint4*>(p.q + from[i])) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int i = 0; i < kMaskLoads; ++i) {
+          const int at = tid + i * 256, t = at / p.W, k = at - t * p.W;
+          mask_regs[i] = !group && t < ex.nodes ? node_word(p, y.b - p.max_groups, t, k, ex.nodes) : 0u;
+        }
         return;
       }
       const int nodes = sh.extents[y.b].nodes;
@@ -549,12 +547,10 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     auto behind = [&]() { return now + 1 == Sh::kPieces ? 0 : now + 1; };
     // the fetched piece's masks and Q to shared memory, and the word to the chains that have tiles in it: no other waits for it
     auto hand_over = [&](const Piece& y, typename Shm::PerPiece& to) {
-      if constexpr (kShare != kPrefix) {
 #pragma unroll
-        for (int i = 0; i < kMaskLoads; ++i) {
-          const int at = tid + i * 256, t = at / p.W;
-          if (t < p.T) to.node_mask[t][at - t * p.W] = mask_regs[i];
-        }
+      for (int i = 0; i < kMaskLoads; ++i) {
+        const int at = tid + i * 256, t = at / p.W;
+        if (t < p.T) to.node_mask[t][at - t * p.W] = mask_regs[i];
       }
       if (tid == 0) to.odd_values = 0;
       uint8_t* q_dst = q_smem + (kPair ? w * kTileBytes : 0) + (q_c >> 3) * kChunkBytes;
@@ -581,16 +577,21 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     while (x.tiles > 0) {
       const Extent<kShare> ex = sh.extents[x.b];
       typename Shm::PerPiece& mine = sh.piece[now];
-      if constexpr (kShare == kPrefix) {
+      const bool group = kShare == kShared && x.b < p.max_groups;
+      const int own = x.b - (kShare == kShared ? p.max_groups : 0);     // the sequence
+      const int rows = group ? ex.nodes : p.rows;
+      if constexpr (kShare == kShared) {
         r0 = x.row0;
         my_row = r0 + my_place;
-        warp_live = my_row - lane < ex.nodes;
+        warp_live = my_row - lane < rows;
+        t_node = my_row / p.group;
+        gq = my_row - t_node * p.group;
       }
       float m = -INFINITY, l = 0.f;
       int done = 0;                                  // tiles of this piece that this warpgroup has taken
       for (int t = kPair ? 0 : w; t < x.tiles; t += kPair ? 1 : 2, ++done) {
         const int kv0 = (x.first + x.tile0 + t) * kTile;
-        const bool tail = kShare != kPrefix && kv0 + kTile > ex.ctx;   // holds nodes, or ends behind the sequence
+        const bool tail = kv0 + kTile > ex.ctx;      // holds nodes, or ends behind the sequence; a group's never
         wait(smem_u32(&sh.s_full[w]), s_phase, abort_flag);
         s_phase ^= 1u;
         // V rows that are no tokens may hold anything: 0 x NaN would reach every row. They become zeroes; and so do values of nodes
@@ -724,8 +725,8 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       tc_fence_after();
       const bool whole = x.tiles == x.all;
       if (kShare == kAlone && !whole && x.tile0 == 0 && rb == 0 && tid == 0) split_set(p, g, units, x);
-      const bool live = kShare == kPrefix ? my_row < ex.nodes : my_row < p.rows && t_node < ex.nodes;
-      const bool direct = whole && (kShare == kAlone || (kShare == kSuffix && x.first == 0));   // nothing to add
+      const bool live = my_row < rows && (group || t_node < ex.nodes);
+      const bool direct = whole && (kShare == kAlone || (!group && x.first == 0));   // nothing to add
       float f0 = 1.f, f1 = 0.f;                      // factors on this lane's O_0 and O_1 (pair mode: on its own O)
       if constexpr (!kPair) {
         mine.ml[w][r][0] = m;
@@ -764,7 +765,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       int64_t part_step = D + kPartPad;
       if (kShare != kAlone && whole) {
         part_step = (int64_t)p.c.kv_heads * (D + kPartPad);
-        part0 = kShare == kPrefix ? p.sh.rec_a + (int64_t)ex_first_row(p, ex) * part_step : p.sh.rec_b + (int64_t)x.b * p.rows * part_step;
+        part0 = (group ? p.sh.rec_group + member0_of(ex) * p.rows * part_step : p.sh.rec_own + (int64_t)own * p.rows * part_step);
         part0 += x.head * (D + kPartPad);
       }
       // kN elements of a query row from column c: back to a part, or out. With copies, an element that is no number while the row's
@@ -772,7 +773,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       auto write = [&](auto count, int row, int c, float* o, float factor, bool sum_ok) {
         constexpr int kN = decltype(count)::value;
         const int t = row / p.group, h = x.head * p.group + row - t * p.group;
-        if (kShare == kPrefix ? row >= ex.nodes : row >= p.rows || t >= ex.nodes) return;
+        if (row >= rows || (!group && t >= ex.nodes)) return;
         bool lost = false;
         if constexpr (kCopies > 1) {
 #pragma unroll
@@ -782,7 +783,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         if (odd || lost) {
           // What is finite does not count beside what is not.
           float sum[kN] = {};
-          if (kShare != kPrefix && odd) {            // values of this piece's nodes that are not finite, to the rows that see them
+          if (odd) {                                 // values of this piece's nodes that are not finite, to the rows that see them
             for (int j = 0; j < ex.nodes; ++j) {
               const int kv = ex.ctx + j;
               if (kv < (x.first + x.tile0) * kTile || kv >= (x.first + x.tile0 + x.tiles) * kTile || kv >= ex.kv_end || !((mine.node_mask[t][j >> 5] >> (j & 31)) & 1u)) continue;
@@ -810,7 +811,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             if (sum[i] != 0.f) o[i] += sum[i];
         }
         if (direct) {
-          uint2* out = reinterpret_cast<uint2*>(p.out + ((int64_t)x.b * p.T + t) * p.out_stride + ((int64_t)h * D + c) * 2);
+          uint2* out = reinterpret_cast<uint2*>(p.out + ((int64_t)own * p.T + t) * p.out_stride + ((int64_t)h * D + c) * 2);
 #pragma unroll
           for (int i = 0; i < kN; i += 4) out[i / 4] = make_uint2(pack_bf16(o[i] * factor, o[i + 1] * factor), pack_bf16(o[i + 2] * factor, o[i + 3] * factor));
         } else {
@@ -864,7 +865,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           asm volatile("bar.sync %0, 128;" ::"r"(2 + w) : "memory");
           for (int i = r; i < kCopyRows * kPlaces; i += 128) {
             const int row = i / kPlaces, q = i % kPlaces;
-            if (r0 + row >= (kShare == kPrefix ? ex.nodes : p.rows)) continue;
+            if (r0 + row >= rows) continue;
             float y[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < kCopies; ++k) {
@@ -880,7 +881,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       if (live && copy == 0 && (kPair || w == 0)) {
         const float m2 = m * c2;
         if (direct) {
-          if (p.lse) p.lse[((int64_t)x.b * p.T + t_node) * p.q_heads + x.head * p.group + gq] = l == 0.f ? -INFINITY : (m2 + log2f(l)) * 0.69314718055994531f;
+          if (p.lse) p.lse[((int64_t)own * p.T + t_node) * p.q_heads + x.head * p.group + gq] = l == 0.f ? -INFINITY : (m2 + log2f(l)) * 0.69314718055994531f;
         } else {
           *reinterpret_cast<float2*>(part0 + my_row * part_step + D) = make_float2(m == -INFINITY ? -INFINITY : m2, l);
         }
@@ -933,15 +934,11 @@ cudaError_t run_attend_tensor(const AttendParams& p, const CUtensorMap& tm_k, co
   return p.c.head_dim == 64 ? launch_mode<64, kAlone>(p, p.rows, tm_k, tm_v, st) : launch_mode<128, kAlone>(p, p.rows, tm_k, tm_v, st);
 }
 
-cudaError_t run_attend_shared_tensor(const AttendParams& prefix, int most, const AttendParams& suffix, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
-                                     cudaStream_t st) {
-  const bool narrow = prefix.c.head_dim == 64;
-  const cudaError_t err = narrow ? launch_mode<64, kPrefix>(prefix, most, tm_k, tm_v, st) : launch_mode<128, kPrefix>(prefix, most, tm_k, tm_v, st);
-  if (err != cudaSuccess) return err;
-  return narrow ? launch_mode<64, kSuffix>(suffix, suffix.rows, tm_k, tm_v, st) : launch_mode<128, kSuffix>(suffix, suffix.rows, tm_k, tm_v, st);
+cudaError_t run_attend_shared_tensor(const AttendParams& p, int most, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st) {
+  return p.c.head_dim == 64 ? launch_mode<64, kShared>(p, most, tm_k, tm_v, st) : launch_mode<128, kShared>(p, most, tm_k, tm_v, st);
 }
 
 template <int kShare> bool configure_widths() { return configure_modes<64, kShare>() && configure_modes<128, kShare>(); }
-bool attend_configure() { return simt_attend_configure() && configure_widths<kAlone>() && configure_widths<kPrefix>() && configure_widths<kSuffix>(); }
+bool attend_configure() { return simt_attend_configure() && configure_widths<kAlone>() && configure_widths<kShared>(); }
 
 }  // namespace jd

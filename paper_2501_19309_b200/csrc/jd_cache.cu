@@ -592,21 +592,21 @@ size_t carve_shared(jd_cache_t c, int B, int nodes, char* base, SharedView* s) {
   const jd_cache_config_t& g = c->cfg;
   SharedView v;
   v.count = (int32_t*)take(256);
-  v.groups = base ? v.count + 1 : nullptr;
-  for (int32_t** x : {&v.leader, &v.same, &v.group_start, &v.group_tokens, &v.group_leader, &v.member, &v.entry_group, &v.entry_place, &v.entry_slot,
-                      &v.first, &v.units_a, &v.units_b})
+  for (int32_t** x : {&v.leader, &v.same, &v.group_start, &v.group_tokens, &v.group_slot, &v.member, &v.entry_group, &v.entry_place, &v.entry_slot,
+                      &v.entry_lead, &v.entry_tokens, &v.first})
     *x = (int32_t*)take((size_t)(B + 1) * 4);
+  v.units = (int32_t*)take((size_t)(B / 2 + B + 1) * 4);
   const size_t row = (size_t)(g.head_dim + kPartPad) * 4, rows = (size_t)B * nodes * (g.q_heads / g.kv_heads);
-  v.rec_a = (float*)take(rows * g.kv_heads * row);
-  v.rec_b = (float*)take(rows * g.kv_heads * row);
-  // two parts for each CTA of the prefix call, as in carve_cache
+  v.rec_group = (float*)take(rows * g.kv_heads * row);
+  v.rec_own = (float*)take(rows * g.kv_heads * row);
+  // two parts for each CTA, as in carve_cache
   const size_t most = std::max<size_t>(c->tm_ok ? std::min<size_t>(rows, 256) : 0, 2 * std::min<size_t>(rows, kSimtRows));
   v.part = (float*)take((size_t)c->num_sms * 2 * most * row);
   if (s) *s = v;
   return off;
 }
 bool shared_ok(jd_cache_t c, const jd_shared_t* plan, SharedView* s) {
-  if (!c || !plan || plan->B < 1 || plan->B > kMaxCacheBatch || plan->nodes < 1 || plan->nodes > c->cfg.max_nodes) return false;
+  if (!c || !plan || plan->B < 1 || plan->B > kMaxSharedBatch || plan->nodes < 1 || plan->nodes > c->cfg.max_nodes) return false;
   if (!plan->buffer || (reinterpret_cast<uintptr_t>(plan->buffer) & 255u) || plan->bytes < carve_shared(c, plan->B, plan->nodes, nullptr, nullptr)) return false;
   carve_shared(c, plan->B, plan->nodes, (char*)plan->buffer, s);
   return true;
@@ -726,7 +726,7 @@ jd_status_t jd_cache_attend(jd_cache_t c, const jd_attend_args_t* a, void* cuda_
 }
 
 size_t jd_cache_shared_bytes(jd_cache_t c, int32_t B, int32_t nodes) {
-  return c && B >= 1 && B <= kMaxCacheBatch && nodes >= 1 && nodes <= c->cfg.max_nodes ? carve_shared(c, B, nodes, nullptr, nullptr) : 0;
+  return c && B >= 1 && B <= kMaxSharedBatch && nodes >= 1 && nodes <= c->cfg.max_nodes ? carve_shared(c, B, nodes, nullptr, nullptr) : 0;
 }
 
 jd_status_t jd_cache_share(jd_cache_t c, const jd_shared_t* plan, const int32_t* slots, const int32_t* groups, void* cuda_stream) {
@@ -746,19 +746,19 @@ jd_status_t jd_cache_attend_shared(jd_cache_t c, const jd_attend_args_t* a, cons
   const bool tensor = a->variant != JD_ATTEND_SIMT && c->tm_ok;
   OnDevice dev(c->cfg.device);
   if (!dev.ok()) return JD_ERR_CUDA;
-  AttendParams suffix = attend_params(c, *a, tensor);
-  suffix.sh = s;
-  AttendParams prefix = suffix;
-  const int most = a->B * suffix.rows;                        // rows of a group: up to 2^27
-  prefix.rows_per_block = tensor ? (most > 128 ? 256 : 128) : (most <= 4 ? 4 : kSimtRows);
-  prefix.part_rows = std::min(most, prefix.rows_per_block);
-  prefix.row_blocks = 1;
-  prefix.groups = tensor ? c->num_sms : 2 * c->num_sms;
-  if (tensor) prefix.seg_cost = tensor_seg_cost(c->cfg.head_dim, most);
-  prefix.part = s.part;
+  AttendParams p = attend_params(c, *a, tensor);
+  const int most = a->B * p.rows;                             // rows of a group: up to 2^26
+  p.sh = s;
+  p.max_groups = a->B / 2;
+  p.rows_per_block = tensor ? (most > 128 ? 256 : 128) : (most <= 4 ? 4 : kSimtRows);
+  p.part_rows = std::min(most, p.rows_per_block);
+  p.row_blocks = 1;
+  p.groups = tensor ? c->num_sms : 2 * c->num_sms;
+  if (tensor) p.seg_cost = tensor_seg_cost(c->cfg.head_dim, most);
+  p.part = s.part;
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  cudaError_t err = tensor ? run_attend_shared_tensor(prefix, most, suffix, c->tm_k, c->tm_v, st) : run_attend_shared_simt(prefix, suffix, c->cfg.dtype, st);
-  if (err == cudaSuccess) err = run_attend_shared_join(prefix, suffix, c->cfg.dtype, st);
+  cudaError_t err = tensor ? run_attend_shared_tensor(p, most, c->tm_k, c->tm_v, st) : run_attend_shared_simt(p, c->cfg.dtype, st);
+  if (err == cudaSuccess) err = run_attend_shared_join(p, c->cfg.dtype, st);
   return finish(c, err, st);
 }
 

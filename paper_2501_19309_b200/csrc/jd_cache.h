@@ -79,35 +79,37 @@ __device__ __forceinline__ void slot_state(const CacheView& c, int slot, int& le
 // of its group if the part begins the segment, else in slot 0, so two slots are enough.
 // The cut depends on nothing but the lengths and the SM count: results repeat bit for bit.
 // ---------------------------------------------------------------------------------------
-// Sequences that share a prefix (jd_cache_share). A call is then two: the prefix tiles of every group once, for the rows of all its members
-// one behind another (kPrefix: a "sequence" is a group, its rows in blocks of rows_per_block), and the tiles behind them for every sequence by itself
-// (kSuffix); a join adds the two up. Every piece leaves numerators, maximum and sum: of a whole segment in a record of the row's own, of a part in its
-// group's slot.
-enum Share { kAlone = 0, kPrefix = 1, kSuffix = 2 };
+// Sequences that share a prefix (jd_cache_share). The call's items are then the groups, each with the tiles of its prefix and the rows of all its
+// members one behind another, and the sequences with the tiles behind their prefix; an item's rows are cut into blocks of rows_per_block, and its
+// segments are the kv heads and the blocks within. All lie in one division: the groups' long segments and the sequences' short ones fill the SMs
+// together. A piece of a group, or of a sequence with a prefix, leaves numerators, maximum and sum: of a whole segment in a record of the row's
+// own, of a part in its run's slot; a join adds them up.
+enum Share { kAlone = 0, kShared = 1 };
 template <int kShare> using ShareOf = std::integral_constant<int, kShare>;
 
+constexpr int kMaxSharedBatch = 512; // sequences of a plan: groups and sequences are at most 1.5 times as many items
 constexpr int kPrefixTokens = 128;   // prefixes are cut to whole tiles of the tensor-core kernel, which are whole tiles of the other
 // tiles of kPrefixTokens that a group has to save: what its segment costs to begin, end and join is four to six tiles
 constexpr int kPrefixWorth = 8;
 
 struct SharedView {                  // arrays of a plan of B sequences, all on the device
   int32_t* count;                    // [1] blocks of jd_cache_share that are done (self-resetting)
-  int32_t* groups;                   // [1]
   int32_t* leader;                   // [B] the first entry with the same beginning, and the tokens that both have in the same pages: scratch
   int32_t* same;
-  int32_t* group_start;              // [B + 1] first of the group's members
-  int32_t* group_tokens;             // [B]
-  int32_t* group_leader;             // [B] entry
+  int32_t* group_start;              // [B / 2 + 1] first of the group's members
+  int32_t* group_tokens;             // [B / 2] 0: no group
+  int32_t* group_slot;               // [B / 2] slot whose pages are read
   int32_t* member;                   // [B] entries by group
   int32_t* entry_group;              // [B] -1: none
   int32_t* entry_place;              // [B] number within the group
-  int32_t* entry_slot;               // [B]
-  int32_t* first;                    // [B] tokens that the prefix call takes off the sequence, as the tables stand at the call
-  int32_t* units_a;                  // [B + 1] units of the two calls (unit_prefix)
-  int32_t* units_b;
-  float* rec_a;                      // [B x T x group][kv_heads][head_dim + kPartPad] rows by group member; by entry
-  float* rec_b;
-  float* part;                       // parts of the prefix call
+  int32_t* entry_slot;               // [B] slot when the plan was made
+  int32_t* entry_lead;               // [B] the group's slot
+  int32_t* entry_tokens;             // [B] its prefix, 0: none
+  int32_t* first;                    // [B] tokens that the call takes off the sequence, as the tables stand: written by it for its join
+  int32_t* units;                    // [B / 2 + B + 1] the call's division (unit_prefix), likewise
+  float* rec_group;                  // [B x T x group][kv_heads][head_dim + kPartPad] rows by group member; by entry
+  float* rec_own;
+  float* part;                       // parts of the call
 };
 
 struct AttendParams {
@@ -129,7 +131,8 @@ struct AttendParams {
   int64_t q_stride, out_stride;    // bytes between tokens
   float* lse;
   float scale_log2;                // scale x log2(e)
-  SharedView sh;                   // kPrefix, kSuffix
+  SharedView sh;                   // kShared
+  int max_groups;                  // items in front of the sequences; 0 for kAlone
   int4* split;                     // [groups] sequence, kv head and last group of the segment that the group leaves unfinished; x < 0: none
   float* part;                     // [groups * row_blocks][2][part_rows][head_dim + kPartPad]
 };
@@ -139,13 +142,17 @@ constexpr int kPartPad = 4;        // a part's row is head_dim numerators, m, l 
 struct SeqExtent {
   int slot, ctx, nodes, kv_end;
 };
-// With a shared prefix: of a sequence its first tile behind it; of a group its first member, and its rows in place of nodes.
+// With shared prefixes: of a sequence its first tile behind the prefix; of a group its first member, and its rows in place of nodes.
 struct SharedExtent : SeqExtent {
   int more;
 };
 template <int kShare> struct ExtentOf { using type = SharedExtent; };
 template <> struct ExtentOf<kAlone> { using type = SeqExtent; };
 template <int kShare> using Extent = typename ExtentOf<kShare>::type;
+
+// a group's first member
+__device__ __forceinline__ int64_t member0_of(const SeqExtent&) { return 0; }
+__device__ __forceinline__ int64_t member0_of(const SharedExtent& e) { return e.more; }
 
 __device__ __forceinline__ SeqExtent seq_extent(const AttendParams& p, int b) {
   SeqExtent e;
@@ -163,80 +170,72 @@ __device__ __forceinline__ int extent_units(const AttendParams& p, const SeqExte
   return p.seg_cost + max(1, (e.kv_end + (1 << p.tile_shift) - 1) >> p.tile_shift);
 }
 
-// Whether slot has the first `tokens` tokens in the same pages as slot `lead`, which had them so when the plan was made. Tables change
-// from their ends alone or as a whole, so the last page of the prefix tells.
-__device__ __forceinline__ bool still_shared(const CacheView& c, int slot, int lead, int tokens) {
-  int len, held, lead_len, lead_held;
-  slot_state(c, slot, len, held);
-  slot_state(c, lead, lead_len, lead_held);
-  if (tokens < 1 || tokens > len || tokens > lead_len) return false;
-  const int at = (tokens - 1) >> c.page_shift;
-  return __ldcg(c.table + (int64_t)slot * c.max_pages + at) == __ldcg(c.table + (int64_t)lead * c.max_pages + at);
-}
-// By the prefix call, for the suffix call and the join: what is taken off each sequence. A plan that the tables have left behind takes nothing off.
-__device__ __forceinline__ void check_shared(const AttendParams& p, int i0, int step) {
-  const int groups = min(max(__ldcg(p.sh.groups), 0), p.B);
-  for (int b = i0; b < p.B; b += step) {
-    const int slot = p.slots ? __ldcg(p.slots + b) : b, g = __ldcg(p.sh.entry_group + b);
-    int first = 0;
-    if (slot >= 0 && slot < p.c.max_seqs && g >= 0 && g < groups && slot == __ldcg(p.sh.entry_slot + b)) {
-      const int tokens = __ldcg(p.sh.group_tokens + g), lead = __ldcg(p.sh.entry_slot + __ldcg(p.sh.group_leader + g));
-      if (still_shared(p.c, slot, lead, tokens)) first = tokens;
-    }
-    p.sh.first[b] = first;
-  }
+// Tokens that sequence b leaves to its group: those of the plan if slot still has them in the group's pages, else none, so that a plan which the tables
+// have left behind costs time alone. Tables change from their ends or as a whole, so lengths and the prefix's last page tell; so that the
+// loads are under way together, none waits for another's outcome.
+__device__ __forceinline__ int prefix_of(const AttendParams& p, int b, int slot, int ctx) {
+  const int tokens = __ldcg(p.sh.entry_tokens + b), was = __ldcg(p.sh.entry_slot + b), lead = __ldcg(p.sh.entry_lead + b);
+  if (tokens < 1 || slot < 0 || slot != was || lead < 0 || lead >= p.c.max_seqs || (tokens - 1) >> p.c.page_shift >= p.c.max_pages) return 0;
+  const int at = (tokens - 1) >> p.c.page_shift;
+  const int mine = __ldcg(p.c.table + (int64_t)slot * p.c.max_pages + at), its = __ldcg(p.c.table + (int64_t)lead * p.c.max_pages + at);
+  int len, held;
+  slot_state(p.c, lead, len, held);
+  return mine == its && tokens <= ctx && tokens <= len ? tokens : 0;
 }
 
-// What sequence or group i of the call is.
+// Item i of the call: a group if i < p.max_groups, else a sequence.
 template <int kShare> __device__ __forceinline__ Extent<kShare> extent_at(const AttendParams& p, int i) {
   if constexpr (kShare == kAlone) {
     return seq_extent(p, i);
-  } else if constexpr (kShare == kSuffix) {
-    SharedExtent e;
-    static_cast<SeqExtent&>(e) = seq_extent(p, i);
-    e.more = e.slot < 0 ? 0 : __ldcg(p.sh.first + i) >> p.tile_shift;
-    return e;
   } else {
     SharedExtent e;
+    if (i >= p.max_groups) {
+      const int b = i - p.max_groups;
+      static_cast<SeqExtent&>(e) = seq_extent(p, b);
+      e.more = prefix_of(p, b, e.slot, e.ctx) >> p.tile_shift;
+      return e;
+    }
     e.slot = -1;
     e.ctx = e.nodes = e.kv_end = e.more = 0;
-    if (i >= __ldcg(p.sh.groups)) return e;
-    const int start = __ldcg(p.sh.group_start + i), tokens = __ldcg(p.sh.group_tokens + i), lead = __ldcg(p.sh.entry_slot + __ldcg(p.sh.group_leader + i));
+    const int start = __ldcg(p.sh.group_start + i), end = __ldcg(p.sh.group_start + i + 1), tokens = __ldcg(p.sh.group_tokens + i);
+    const int lead = __ldcg(p.sh.group_slot + i);
+    if (tokens < 1 || lead < 0 || lead >= p.c.max_seqs) return e;
     int len, held;
     slot_state(p.c, lead, len, held);
     if (tokens > len) return e;
     e.slot = lead;
     e.ctx = e.kv_end = tokens;
     e.more = start;
-    e.nodes = (__ldcg(p.sh.group_start + i + 1) - start) * p.rows;
+    e.nodes = (end - start) * p.rows;
     return e;
   }
 }
 __device__ __forceinline__ int row_blocks_of(const AttendParams& p, int rows) { return (int)((uint32_t)(rows + p.rows_per_block - 1) / (uint32_t)p.rows_per_block); }
-template <int kShare> __device__ __forceinline__ int units_at(const AttendParams& p, const Extent<kShare>& e) {
-  if constexpr (kShare == kAlone) {
-    return extent_units(p, e);
-  } else if constexpr (kShare == kSuffix) {
-    const int n = extent_units(p, e);
-    return n == 0 ? 0 : max(n - e.more, p.seg_cost + 1);
-  } else {
-    return e.nodes == 0 ? 0 : row_blocks_of(p, e.nodes) * (p.seg_cost + (e.ctx >> p.tile_shift));
-  }
+template <int kShare> __device__ __forceinline__ int item_blocks(const AttendParams& p, int i, const Extent<kShare>& e) {
+  return kShare == kAlone ? 1 : row_blocks_of(p, i < p.max_groups ? e.nodes : p.rows);
 }
+template <int kShare> __device__ __forceinline__ int units_at(const AttendParams& p, int i, const Extent<kShare>& e) {
+  const int n = extent_units(p, e);
+  if constexpr (kShare == kAlone) return n;
+  else return n == 0 ? 0 : item_blocks<kShare>(p, i, e) * (i < p.max_groups ? n : max(n - e.more, p.seg_cost + 1));
+}
+template <int kShare> __device__ __forceinline__ int items_of(const AttendParams& p) { return kShare == kAlone ? p.B : p.max_groups + p.B; }
 
-// prefix[b] = units of one kv head in the sequences before b, prefix[B] = all; extents (optional): what extent_at says of each
-// sequence. By the whole block.
+// prefix[b] = units of one kv head in the items before b, prefix[items] = all; extents (optional): what extent_at says of each
+// item. By the whole block.
 template <int kShare>
 __device__ __forceinline__ void unit_prefix(ShareOf<kShare>, const AttendParams& p, int* prefix, int* warp_sums, Extent<kShare>* extents = nullptr) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nthreads = blockDim.x, nwarps = nthreads >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nthreads = blockDim.x, nwarps = nthreads >> 5, items = items_of<kShare>(p);
   int carry = 0;
-  for (int b0 = 0; b0 < p.B; b0 += nthreads) {
+  for (int b0 = 0; b0 < items; b0 += nthreads) {
     const int b = b0 + tid;
     int n = 0;
-    if (b < p.B) {
+    if (b < items) {
       const Extent<kShare> e = extent_at<kShare>(p, b);
       if (extents) extents[b] = e;
-      n = units_at<kShare>(p, e);
+      n = units_at<kShare>(p, b, e);
+      if constexpr (kShare == kShared)
+        if (blockIdx.x == 0 && b >= p.max_groups) p.sh.first[b - p.max_groups] = e.more << p.tile_shift;
     }
     int x = n;
 #pragma unroll
@@ -251,16 +250,15 @@ __device__ __forceinline__ void unit_prefix(ShareOf<kShare>, const AttendParams&
       if (w < warp) before += warp_sums[w];
       all += warp_sums[w];
     }
-    if (b < p.B) prefix[b] = before + x - n;
+    if (b < items) prefix[b] = before + x - n;
     carry += all;
     __syncthreads();
   }
-  if (tid == 0) prefix[p.B] = carry;
+  if (tid == 0) prefix[items] = carry;
   __syncthreads();
-  if constexpr (kShare != kAlone) {
-    int32_t* to = kShare == kPrefix ? p.sh.units_a : p.sh.units_b;
+  if constexpr (kShare == kShared) {
     if (blockIdx.x == 0)
-      for (int i = tid; i <= p.B; i += nthreads) to[i] = prefix[i];
+      for (int i = tid; i <= items; i += nthreads) p.sh.units[i] = prefix[i];
   }
 }
 
@@ -280,16 +278,16 @@ __device__ __forceinline__ int run_of(int64_t units, int groups, int64_t u) {
 
 // One stretch of a run inside a segment. tiles may be 0: the run holds only units that stand for the segment's fixed cost.
 struct Piece {
-  int b, head, tile0, tiles, all;   // all: tiles of the whole segment
+  int b, head, tile0, tiles, all;   // b: item; all: tiles of the whole segment
   int64_t next;                     // first unit behind it
   int first;                        // the segment's first tile in the sequence; 0 unless a prefix is taken off
-  int row0;                         // the segment's first row; 0 unless rows are a group's
+  int row0;                         // the segment's first row; 0 where CTAs share a sequence's rows
 };
 template <int kShare = kAlone>
 __device__ __forceinline__ Piece piece_at(const AttendParams& p, const int* prefix, int64_t u, int64_t run1, const Extent<kShare>* extents = nullptr) {
   Piece x;
   x.first = x.row0 = 0;
-  int lo = 0, hi = p.B - 1;         // the last sequence with units whose first is at or before u
+  int lo = 0, hi = items_of<kShare>(p) - 1;   // the last item with units whose first is at or before u
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if ((int64_t)prefix[mid] * p.c.kv_heads <= u) lo = mid; else hi = mid - 1;
@@ -297,18 +295,18 @@ __device__ __forceinline__ Piece piece_at(const AttendParams& p, const int* pref
   x.b = lo;
   const int64_t first = (int64_t)prefix[lo] * p.c.kv_heads;
   int n = prefix[lo + 1] - prefix[lo], segment;
-  if constexpr (kShare == kPrefix) {   // a group's segments: heads, and blocks of its rows within
+  if constexpr (kShare == kShared) {
     const Extent<kShare> e = extents ? extents[lo] : extent_at<kShare>(p, lo);
-    const int blocks = row_blocks_of(p, e.nodes);
-    n = p.seg_cost + (e.ctx >> p.tile_shift);
-    const int64_t in_seq = u - first;
-    segment = in_seq < 0x7FFFFFFF ? (int)((uint32_t)in_seq / (uint32_t)n) : (int)(in_seq / n);
+    const int blocks = item_blocks<kShare>(p, lo, e);
+    if (lo >= p.max_groups) x.first = e.more;
+    n = (int)((uint32_t)n / (uint32_t)blocks);
+    const int64_t in_item = u - first;
+    segment = in_item < 0x7FFFFFFF ? (int)((uint32_t)in_item / (uint32_t)n) : (int)(in_item / n);
     x.head = (int)((uint32_t)segment / (uint32_t)blocks);
     x.row0 = (segment - x.head * blocks) * p.rows_per_block;
   } else {
     const int in_seq = (int)(u - first);
     x.head = segment = (int)((uint32_t)in_seq / (uint32_t)n);
-    if constexpr (kShare == kSuffix) x.first = extents ? extents[lo].more : extent_at<kShare>(p, lo).more;
   }
   const int at = (int)(u - first - (int64_t)segment * n);
   const int64_t seg_end = first + (int64_t)(segment + 1) * n;
@@ -362,11 +360,10 @@ inline cudaError_t launch_chained(void (*kernel)(Params...), dim3 grid, dim3 blo
 cudaError_t run_attend_simt(const AttendParams& p, int dtype, cudaStream_t st);
 cudaError_t run_attend_tensor(const AttendParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st);
 cudaError_t run_attend_join(const AttendParams& p, int dtype, cudaStream_t st);
-// The two calls of an attention with a plan, and what adds them up. most: rows that a group may have
-cudaError_t run_attend_shared_simt(const AttendParams& prefix, const AttendParams& suffix, int dtype, cudaStream_t st);
-cudaError_t run_attend_shared_tensor(const AttendParams& prefix, int most, const AttendParams& suffix, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
-                                     cudaStream_t st);
-cudaError_t run_attend_shared_join(const AttendParams& prefix, const AttendParams& suffix, int dtype, cudaStream_t st);
+// Attention with a plan, and what adds its results up. most: rows that a segment may have
+cudaError_t run_attend_shared_simt(const AttendParams& p, int dtype, cudaStream_t st);
+cudaError_t run_attend_shared_tensor(const AttendParams& p, int most, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st);
+cudaError_t run_attend_shared_join(const AttendParams& p, int dtype, cudaStream_t st);
 bool simt_attend_configure();
 bool attend_configure();   // dynamic shared-memory limits on the current device, once per device
 constexpr int kSimtRows = 16, kSimtTileShift = 6, kSimtSegCost = 1;

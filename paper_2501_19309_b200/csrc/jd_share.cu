@@ -9,7 +9,7 @@
 namespace jd {
 namespace {
 
-constexpr int kThreads = kMaxCacheBatch;          // the last block: one for each entry
+constexpr int kThreads = kMaxSharedBatch;         // the last block: one for each entry
 constexpr int64_t kMostUnits = (int64_t)1 << 30;  // of all groups' prefix segments, whatever kernel takes them: their sums are 32 bits
 
 // Inclusive sums over the block's threads.
@@ -105,13 +105,14 @@ __global__ void __launch_bounds__(kThreads) share_kernel(CacheView c, SharedView
     s.group_start[g] = start[t];
     s.group_start[g + 1] = start[t] + n;          // the next group's, if there is one, writes the same
     s.group_tokens[g] = tokens;
-    s.group_leader[g] = t;
+    s.group_slot[g] = __ldcg(s.entry_slot + t);
   }
   if (t == kThreads - 1) {
-    *s.groups = (int)(upto >> 32);
     *s.count = 0;
+    s_last = (int)(upto >> 32);                   // groups
   }
   __syncthreads();
+  if (t >= s_last && t < B / 2) s.group_tokens[t] = 0;
   if (t < B) {
     const int g = mine >= 0 ? number[mine] : -1;
     int place = 0;
@@ -121,6 +122,8 @@ __global__ void __launch_bounds__(kThreads) share_kernel(CacheView c, SharedView
     }
     s.entry_group[t] = g;
     s.entry_place[t] = place;
+    s.entry_lead[t] = g >= 0 ? __ldcg(s.entry_slot + mine) : -1;
+    s.entry_tokens[t] = g >= 0 ? least[mine] & ~(kPrefixTokens - 1) : 0;
   }
 }
 
