@@ -87,6 +87,18 @@ def rope_frequencies(rot_dim: int, base: float = 500000.0, scaling: Optional[str
     return out, amplitude.value
 
 
+_NORMED, _IS_GRAD = "the gradient is rotate_qk_grad()", "this is the gradient"
+_NOTHING = {}
+_grad_workspaces = {}
+
+
+def _grad_workspace(head_dim: int) -> int:
+    need = _grad_workspaces.get(head_dim)
+    if need is None:
+        need = _grad_workspaces[head_dim] = jd.load().jd_head_rope_grad_workspace_bytes(head_dim)
+    return need
+
+
 class HeadNorm:
     """RMS norms of query and key heads, x w / sqrt(mean(x ** 2) + eps): weights [head_dim] (float32, on the device; None: ones)."""
 
@@ -122,6 +134,7 @@ class Rotary:
         self._layout = LAYOUTS[layout]
         self.c = jd.jd_rope_t(inv_freq.data_ptr(), self.rot_dim, self._layout, self.amplitude)
         self.ref = C.addressof(self.c)
+        self._freq = inv_freq.data_ptr()
         self.index = inv_freq.get_device()
         self.num_axes, self.axes_ref = 1, 0
         if axes is not None:
@@ -152,39 +165,36 @@ class Rotary:
         if self.axes_ref:
             a = jd.jd_head_rope_args_t()
             _HEAD_ROPE_ARGS.pack_into(a, 0, n, heads, 0, dim, _DTYPES[x.dtype], 1 if inverse else 0, x.data_ptr(), 0, out.data_ptr(), 0, x_step, 0,
-                                      out_step, 0, at, self.inv_freq.data_ptr(), self.rot_dim, self._layout, self.amplitude, 0, self.axes_ref)
-            self._call("jd_head_rope", a, index, stream)
+                                      out_step, 0, at, self._freq, self.rot_dim, self._layout, self.amplitude, 0, self.axes_ref)
+            self._call(self._lib.jd_head_rope, a, index, stream)
             return out
         a = jd.jd_rope_args_t()
         _ROPE_ARGS.pack_into(a, 0, n, heads, dim, _DTYPES[x.dtype], 1 if inverse else 0, x.data_ptr(), out.data_ptr(), x_step, out_step, at,
-                             self.inv_freq.data_ptr(), self.rot_dim, self._layout, self.amplitude)
-        self._call("jd_rope", a, index, stream)
+                             self._freq, self.rot_dim, self._layout, self.amplitude)
+        self._call(self._lib.jd_rope, a, index, stream)
         return out
 
     def rotate_qk(self, q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, norm: Optional[HeadNorm] = None,
                   q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, stream=None):
         """Queries and keys [tokens, heads, head_dim] (tokens may be strided) in one pass: normalised (``norm``), then turned to their positions
         [tokens] or, with axes, [tokens, axes]. Returns (q_out, k_out), which may be q and k; k may be None."""
-        n, dim, index, heads = self._pair(q, k)
-        outs = []
-        for x, out, name in ((q, q_out, "q_out"), (k, k_out, "k_out")):
-            if x is None:
-                out = None
-            elif out is None:
-                out = x.new_empty(tuple(x.shape))
-            elif out.shape != x.shape or out.dtype is not x.dtype or out.get_device() != index:
-                raise ValueError("%s: like its input" % name)
-            outs.append(out)
-        steps = [0 if x is None else self._step(x, name, n, h, dim, "the gradient is rotate_qk_grad()")
-                 for x, name, h in ((q, "q", heads[0]), (k, "k", heads[1]), (outs[0], "q_out", heads[0]), (outs[1], "k_out", heads[1]))]
+        n, dim, index, q_heads, k_heads = self._pair(q, k)
+        q_step, k_ptr, k_step, ko_ptr, ko_step = self._step(q, "q", n, q_heads, dim, _NORMED), 0, 0, 0, 0
+        q_out, qo_step = self._like(q, q_out, "q_out", n, q_heads, dim, index)
+        if k is not None:
+            k_ptr, k_step = k.data_ptr(), self._step(k, "k", n, k_heads, dim, _NORMED)
+            k_out, ko_step = self._like(k, k_out, "k_out", n, k_heads, dim, index)
+            ko_ptr = k_out.data_ptr()
+        else:
+            k_out = None
         at = self._positions(positions, index, n)
         norm_ref = 0 if norm is None else norm._of(dim, index)
         if n > 0:
             a = jd.jd_head_rope_args_t()
-            _HEAD_ROPE_ARGS.pack_into(a, 0, n, *heads, dim, _DTYPES[q.dtype], 0, *(0 if x is None else x.data_ptr() for x in (q, k, *outs)), *steps, at,
-                                      self.inv_freq.data_ptr(), self.rot_dim, self._layout, self.amplitude, norm_ref, self.axes_ref)
-            self._call("jd_head_rope", a, index, stream)
-        return outs[0], outs[1]
+            _HEAD_ROPE_ARGS.pack_into(a, 0, n, q_heads, k_heads, dim, _DTYPES[q.dtype], 0, q.data_ptr(), k_ptr, q_out.data_ptr(), ko_ptr, q_step, k_step,
+                                      qo_step, ko_step, at, self._freq, self.rot_dim, self._layout, self.amplitude, norm_ref, self.axes_ref)
+            self._call(self._lib.jd_head_rope, a, index, stream)
+        return q_out, k_out
 
     def rotate_qk_grad(self, q_out_grad: torch.Tensor, k_out_grad: Optional[torch.Tensor], q: torch.Tensor, k: Optional[torch.Tensor],
                        positions: torch.Tensor, norm: HeadNorm, out: Optional[dict] = None, weights: bool = True,
@@ -192,73 +202,83 @@ class Rotary:
         """Backward pass of :meth:`rotate_qk` with a norm: the gradients of its outputs and its inputs give a dict with "q", "k" (the inputs'
         gradients) and, unless ``weights`` is False, "q_weight", "k_weight" (float32 [head_dim], set, not added to). ``out``: such a dict with
         tensors to use. ``workspace``: uint8, ``jd_head_rope_grad_workspace_bytes`` of them; calls that may run at the same time take one each."""
-        n, dim, index, heads = self._pair(q, k)
-        got = dict(out or {})
+        n, dim, index, q_heads, k_heads = self._pair(q, k)
         if (k is None) != (k_out_grad is None):
             raise ValueError("k, k_out_grad: both or neither")
-        for name, x, g in (("q", q, q_out_grad), ("k", k, k_out_grad)):
-            if x is None:
-                got[name] = None
-                continue
-            if got.get(name) is None:
-                got[name] = x.new_empty(tuple(x.shape))
-            for y, what in ((g, name + "_out_grad"), (got[name], "out: " + name)):
-                if y.shape != x.shape or y.dtype is not x.dtype or y.get_device() != index:
-                    raise ValueError("%s: like its input" % what)
-        wptr = [0, 0]
-        for i, name in enumerate(("q_weight", "k_weight")):
-            if not weights:
-                got.pop(name, None)
-                continue
-            if got.get(name) is None:
-                got[name] = q.new_empty((dim,), dtype=torch.float32)
-            w = got[name]
-            if w.shape != (dim,) or w.dtype is not torch.float32 or not w.is_contiguous() or w.get_device() != index or w.requires_grad:
-                raise ValueError("%s: a contiguous float32 vector [head_dim] on the device" % name)
-            wptr[i] = w.data_ptr()
-        need = 0
+        out = out or _NOTHING
+        q_step, (_, gq_step) = self._step(q, "q", n, q_heads, dim, _IS_GRAD), self._like(q, q_out_grad, "q_out_grad", n, q_heads, dim, index)
+        q_grad, dq_step = self._like(q, out.get("q"), "out: q", n, q_heads, dim, index)
+        k_grad, k_ptr, gk_ptr, dk_ptr, k_step, gk_step, dk_step = None, 0, 0, 0, 0, 0, 0
+        if k is not None:
+            k_step, (_, gk_step) = self._step(k, "k", n, k_heads, dim, _IS_GRAD), self._like(k, k_out_grad, "k_out_grad", n, k_heads, dim, index)
+            k_grad, dk_step = self._like(k, out.get("k"), "out: k", n, k_heads, dim, index)
+            k_ptr, gk_ptr, dk_ptr = k.data_ptr(), k_out_grad.data_ptr(), k_grad.data_ptr()
+        got = dict(q=q_grad, k=k_grad)
+        wq_ptr = wk_ptr = work_ptr = need = 0
         if weights:
-            need = self._lib.jd_head_rope_grad_workspace_bytes(dim)
-            if workspace is None:
-                workspace = q.new_empty((max(need, 4),), dtype=torch.uint8)
-            elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.numel() < need or workspace.get_device() != index:
-                raise ValueError("workspace: %d contiguous bytes (uint8) on the device" % need)
-        steps = [0 if x is None else self._step(x, name, n, h, dim, "this is the gradient")
-                 for x, name, h in ((q, "q", heads[0]), (k, "k", heads[1]), (q_out_grad, "q_out_grad", heads[0]), (k_out_grad, "k_out_grad", heads[1]),
-                                    (got["q"], "out: q", heads[0]), (got["k"], "out: k", heads[1]))]
+            need = _grad_workspace(dim)
+            wq, wk = out.get("q_weight"), out.get("k_weight")
+            if wq is None and wk is None and workspace is None:      # one allocation: both weights' gradients, then the workspace
+                both = q.new_empty((2 * dim + need // 4,), dtype=torch.float32)
+                wq, wk = both[:dim], both[dim:2 * dim]
+                wq_ptr = both.data_ptr()
+                wk_ptr, work_ptr = wq_ptr + 4 * dim, wq_ptr + 8 * dim
+            else:
+                wq, wk = (q.new_empty((dim,), dtype=torch.float32) if w is None else w for w in (wq, wk))
+                for w in (wq, wk):
+                    if w.shape != (dim,) or w.dtype is not torch.float32 or not w.is_contiguous() or w.get_device() != index or w.requires_grad:
+                        raise ValueError("q_weight, k_weight: contiguous float32 vectors [head_dim] on the device")
+                if workspace is None:
+                    workspace = q.new_empty((need,), dtype=torch.uint8)
+                elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.numel() < need or workspace.get_device() != index:
+                    raise ValueError("workspace: %d contiguous bytes (uint8) on the device" % need)
+                wq_ptr, wk_ptr, work_ptr = wq.data_ptr(), wk.data_ptr(), workspace.data_ptr()
+            got["q_weight"], got["k_weight"] = wq, wk
         at = self._positions(positions, index, n)
         a = jd.jd_head_rope_grad_args_t()
-        _HEAD_ROPE_GRAD_ARGS.pack_into(a, 0, n, *heads, dim, _DTYPES[q.dtype], *(0 if x is None else x.data_ptr() for x in (
-                                           q, k, q_out_grad, k_out_grad, got["q"], got["k"])), *steps, at, self.inv_freq.data_ptr(), self.rot_dim,
-                                       self._layout, self.amplitude, norm._of(dim, index), self.axes_ref, *wptr,
-                                       workspace.data_ptr() if weights else 0, need)
-        self._call("jd_head_rope_grad", a, index, stream)
+        _HEAD_ROPE_GRAD_ARGS.pack_into(a, 0, n, q_heads, k_heads, dim, _DTYPES[q.dtype], q.data_ptr(), k_ptr, q_out_grad.data_ptr(), gk_ptr,
+                                       q_grad.data_ptr(), dk_ptr, q_step, k_step, gq_step, gk_step, dq_step, dk_step, at, self._freq, self.rot_dim,
+                                       self._layout, self.amplitude, norm._of(dim, index), self.axes_ref, wq_ptr, wk_ptr, work_ptr, need)
+        self._call(self._lib.jd_head_rope_grad, a, index, stream)
         return got
 
+    def _like(self, x: torch.Tensor, y: Optional[torch.Tensor], name: str, n: int, heads: int, dim: int, index: int):
+        """(y, its elements between tokens): a new tensor like x if None."""
+        if y is None:
+            return x.new_empty((n, heads, dim)), 0
+        if y.shape != x.shape or y.dtype is not x.dtype or y.get_device() != index:
+            raise ValueError("%s: like its input" % name)
+        return y, self._step(y, name, n, heads, dim, _IS_GRAD)
+
     def _pair(self, q, k):
-        """(tokens, head_dim, device, (heads of q, heads of k)) of a call on queries and keys."""
+        """(tokens, head_dim, device, heads of q, heads of k) of a call on queries and keys."""
         if q.dim() != 3 or q.dtype not in _DTYPES or not q.is_cuda:
             raise ValueError("q: [tokens, heads, head_dim], float32 or bfloat16, on the device")
         n, heads, dim = q.shape
-        if k is not None and (k.dim() != 3 or k.shape[0] != n or k.shape[2] != dim or k.dtype is not q.dtype or k.get_device() != q.get_device()):
+        index = q.get_device()
+        if k is None:
+            return n, dim, index, heads, 0
+        if k.dim() != 3 or k.dtype is not q.dtype or k.get_device() != index:
             raise ValueError("k: [tokens, heads, head_dim] like q")
-        return n, dim, q.get_device(), (heads, 0 if k is None else k.shape[1])
+        kn, k_heads, k_dim = k.shape
+        if kn != n or k_dim != dim:
+            raise ValueError("k: [tokens, heads, head_dim] like q")
+        return n, dim, index, heads, k_heads
 
     def _positions(self, positions: torch.Tensor, index: int, n: int) -> int:
-        at = _ints(positions, "positions", index, (n,) if not self.axes_ref else (n, self.num_axes))
+        at = _ints(positions, "positions", index, (n, self.num_axes) if self.axes_ref else (n,))
         if self.index != index:
             raise ValueError("inv_freq and x on one device")
         return at
 
-    def _call(self, name: str, args, index: int, stream) -> None:
-        call = getattr(self._lib, name)
+    def _call(self, call, args, index: int, stream) -> None:
         if torch._C._cuda_getDevice() == index:
             st = call(args, _stream(stream, index))
         else:
             with torch.cuda.device(index):
                 st = call(args, _stream(stream, index))
         if st != jd.JD_OK:
-            raise jd.JdError(st, name)
+            raise jd.JdError(st, call.__name__)
 
     @staticmethod
     def _step(t: torch.Tensor, name: str, n: int, heads: int, dim: int, gradient: str = "the gradient is rotate(grad, positions, inverse=True)") -> int:

@@ -64,22 +64,28 @@ def verify_probs(target: torch.Tensor, draft: Optional[torch.Tensor], tokens: to
                                 parents.shape not in ((T,), (B, T))):
         raise ValueError("parents: contiguous int32 [T] or [B, T] on the target's device")
     if out is None:
-        out = dict(accept_len=tokens.new_empty((B,)), next_token=tokens.new_empty((B,)), path=tokens.new_empty((B, M)))
-    path = out.get("path")
+        # rows of one allocation: lengths, tokens, paths
+        flat = tokens.new_empty((B * (M + 2),))
+        out = dict(accept_len=flat[:B], next_token=flat[B:2 * B], path=flat[2 * B:].view(B, M))
+        len_ptr = flat.data_ptr()
+        next_ptr, path_ptr = len_ptr + 4 * B, len_ptr + 8 * B
+    else:
+        path = out.get("path")
+        len_ptr, next_ptr = _plain(out["accept_len"], "accept_len", (B,), i32, index), _plain(out["next_token"], "next_token", (B,), i32, index)
+        path_ptr = 0 if path is None else _plain(path, "path", (B, M), i32, index)
     mode = jd.MODES[mode] if isinstance(mode, str) else int(mode)
     if mode != jd.JD_MODE_STANDARD and judge_scores is None:
         raise ValueError("judge_scores: [B, T - 1] for a mode that judges")
     a = jd.jd_verify_probs_args_t()
+    bm = (B, M)
     _ARGS.pack_into(a, 0, B, T, V, _DTYPES[dt], target.data_ptr(), 0 if M <= 0 else draft.data_ptr(), t_step, d_step,
-                    _plain(tokens, "tokens", (B, M), i32, index), 0 if parents is None else parents.data_ptr(),
+                    _plain(tokens, "tokens", bm, i32, index), 0 if parents is None else parents.data_ptr(),
                     1 if parents is not None and parents.dim() == 2 else 0,
                     0 if num_nodes is None else _plain(num_nodes, "num_nodes", (B,), i32, index),
-                    _plain(accept_u, "accept_u", (B, M), f32, index), _plain(sample_u, "sample_u", (B,), f32, index),
-                    0 if judge_scores is None else _plain(judge_scores, "judge_scores", (B, M), f32, index), tau, mode,
+                    _plain(accept_u, "accept_u", bm, f32, index), _plain(sample_u, "sample_u", (B,), f32, index),
+                    0 if judge_scores is None else _plain(judge_scores, "judge_scores", bm, f32, index), tau, mode,
                     jd.RESAMPLE[resample] if isinstance(resample, str) else int(resample),
-                    SIBLINGS[siblings] if isinstance(siblings, str) else int(siblings),
-                    _plain(out["accept_len"], "accept_len", (B,), i32, index), _plain(out["next_token"], "next_token", (B,), i32, index),
-                    0 if path is None else _plain(path, "path", (B, M), i32, index),
+                    SIBLINGS[siblings] if isinstance(siblings, str) else int(siblings), len_ptr, next_ptr, path_ptr,
                     0 if status is None else _plain(status, "status", (1,), i32, index))
     lib = jd.load()
     if torch._C._cuda_getDevice() == index:
