@@ -577,13 +577,15 @@ typedef struct {
   int32_t nodes;      /* most nodes of a call, 1..max_nodes */
   void* buffer;
   size_t bytes;
+  int32_t rows;       /* 0: jd_cache_share weighs what sharing costs against what it saves and picks the form; 32, 64, 128 or 256 (a cache on the tensor
+                         cores), 4 or 16 (else): whatever can be shared is, in the form with so many query rows to a block */
 } jd_shared_t;
 
 size_t jd_cache_shared_bytes(jd_cache_t c, int32_t B, int32_t nodes);   /* 0: invalid */
 
 /* Finds on the device which of the B sequences hold the same pages in front, as the tables stand. groups: device [B], entries with the same
  * number (not below 0) are compared; NULL: those with the same first page. A group's prefix is what all its members have in common with its first
- * entry, in whole 128 tokens of full pages; groups that would save too little stay apart. Once for all layers of a step, behind
+ * entry, in whole 128 tokens of full pages. Unless plan->rows says otherwise the calls share by cost, all groups or none. Once for all layers of a step, behind
  * jd_cache_reserve or in front of it. */
 jd_status_t jd_cache_share(jd_cache_t c, const jd_shared_t* plan, const int32_t* slots, const int32_t* groups, void* cuda_stream);
 

@@ -552,16 +552,19 @@ class PagedCache:
         return out
 
     def share(self, nodes: int, slots: Optional[torch.Tensor] = None, groups: Optional[torch.Tensor] = None, plan: Optional[SharedPrefix] = None,
-              stream=None) -> SharedPrefix:
+              stream=None, rows: int = 0) -> SharedPrefix:
         """Finds which of the sequences hold the same pages in front, as the tables stand (``jd_cache_share``): forks, samples of one prompt,
         requests behind one system prompt. groups [B]: entries with the same number are compared, None: those with the same first page. Made once for
         all layers of a step, for calls of up to ``nodes`` nodes; ``plan``: one to use again (else a new one is allocated, which waits for
-        the current stream). A plan that the tables have left behind costs time, not results."""
+        the current stream). Whether the calls share, and in which form, goes by what it costs; ``rows`` has them share whatever they can with that many
+        query rows to a block: 32, 64, 128, 256 on the tensor cores, 4, 16 else. A plan that the tables have left behind costs time, not results."""
         B = self._batch(slots)
         if plan is None:
             plan = SharedPrefix(self, B, nodes)
         elif plan.cache is not self or plan.B != B or plan.nodes < nodes:
             raise ValueError("plan: of this cache for %d sequences of %d nodes" % (B, nodes))
+        _require(rows in (0, 4, 16, 32, 64, 128, 256), "rows: 0, 4, 16, 32, 64, 128 or 256")
+        plan.c.rows = rows
         st = self._lib.jd_cache_share(self.h, plan.c, _ints(slots, "slots", self.index), _ints(groups, "groups", self.index, (B,)),
                                       _stream(stream, self.index))
         if st != jd.JD_OK:

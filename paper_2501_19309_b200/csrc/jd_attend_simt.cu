@@ -57,7 +57,7 @@ size_t simt_smem(int head_dim, int rows) {
 // kCols: groups of 128 columns that a lane's accumulators cover (head_dim <= 128 kCols)
 // kRows: query rows of the block, 4 or 16
 template <typename T, int kCols, int kRows, int kShare>
-__global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_simt_kernel(AttendParams p) {
+__device__ __forceinline__ void attend_simt(const AttendParams& p, const Division cut) {
   constexpr int kScorePad = score_pad(kRows);
   extern __shared__ __align__(16) float smem[];
   __shared__ int prefix[kMaxCacheBatch + 1], warp_sums[kThreads / 32];
@@ -76,7 +76,7 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
   pdl_wait();
   pdl_trigger();
   if (kShare == kAlone && rb == 0 && tid == 0) split_none(p, g);
-  unit_prefix(ShareOf<kShare>(), p, prefix, warp_sums);
+  unit_prefix(ShareOf<kShare>(), p, cut, prefix, warp_sums);
   const int64_t units = (int64_t)prefix[items_of<kShare>(p)] * p.c.kv_heads;
   if (units == 0) return;
   const int64_t run0 = run_start(units, p.groups, g), run1 = run_start(units, p.groups, g + 1);
@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
 
   const int step = kCols == 1 && D <= 64 ? 2 : 1, col_lane = step == 2 ? lane & 15 : lane, my_token = step == 2 ? lane >> 4 : 0;
   for (int64_t u = run0; u < run1;) {
-    const Piece x = piece_at<kShare>(p, prefix, u, run1);
+    const Piece x = piece_at<kShare>(p, cut, prefix, u, run1);
     u = x.next;
     if (x.tiles == 0) continue;
     const bool shared_rows = kShare == kShared && x.b < p.max_groups;
@@ -326,7 +326,7 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
         store4(reinterpret_cast<T*>(p.out + ((int64_t)b * p.T + t) * p.out_stride) + (int64_t)h * D + d, o);
         if (d == 0 && p.lse) p.lse[((int64_t)b * p.T + t) * p.q_heads + h] = l == 0.f ? -INFINITY : (s_m[r] + log2f(l)) * 0.69314718055994531f;
       } else {
-        float* part = p.part + (((int64_t)blockIdx.x * 2 + (begins ? 1 : 0)) * p.part_rows + r) * (D + kPartPad);
+        float* part = p.part + (((int64_t)blockIdx.x * 2 + (begins ? 1 : 0)) * cut.part_rows + r) * (D + kPartPad);
         if (kShare != kAlone && whole)
           part = (shared_rows ? p.sh.rec_group : p.sh.rec_own) +
                  (((shared_rows ? member0_of(ex) : b) * p.rows + r0 + r) * p.c.kv_heads + head) * (D + kPartPad);
@@ -335,6 +335,19 @@ __global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_
       }
     }
   }
+}
+
+template <typename T, int kCols, int kRows>
+__global__ void __launch_bounds__(kThreads, kCols * kRows <= 16 ? 2 : 1) attend_simt_kernel(AttendParams p) {
+  attend_simt<T, kCols, kRows, kAlone>(p, own_division(p));
+}
+// With a plan that names one of two forms.
+template <typename T, int kCols, int kFirst, int kSecond>
+__global__ void __launch_bounds__(kThreads, kCols * kSecond <= 16 ? 2 : 1) attend_simt_shared_kernel(const __grid_constant__ AttendParams p) {
+  const Division d = plan_division<false>(p);
+  if constexpr (kFirst == kSecond) attend_simt<T, kCols, kFirst, kShared>(p, d);
+  else if (d.rows_per_block == kSecond) attend_simt<T, kCols, kSecond, kShared>(p, d);
+  else attend_simt<T, kCols, kFirst, kShared>(p, d);
 }
 
 // Joins the partial results of split segments; rows of whole segments are written already.
@@ -492,25 +505,25 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(AttendPara
 }
 
 // Adds up what a row's group and the row's sequence have left, parts and records alike. A warp for a row, or, with few rows, whose
-// parts from many SMs are what takes the time, a block of four. Rows that are written already (no prefix, one run) are left alone.
-constexpr int kSharedFewRows = 4096;
+// parts from many SMs are what takes the time, a block of four (64 sequences of one token
+// and 32 heads: a layer 53 us, 58 with blocks for 2048 rows; 16 sequences 27.7, 28.2 with a warp for each). Rows that are written already (no prefix, one run) are left alone.
+constexpr int kSharedFewRows = 512;
 
 struct Parts {                       // of a row in one segment
   int run, count;                    // the first run with tiles of the segment, and their number; 1: a record
 };
-__device__ __forceinline__ Parts parts_of(const AttendParams& p, int64_t all, int64_t first_unit, int n) {
+__device__ __forceinline__ Parts parts_of(const AttendParams& p, const Division& d, int64_t all, int64_t first_unit, int n) {
   Parts x;
-  x.run = run_of(all, p.groups, first_unit + p.seg_cost);
+  x.run = run_of(all, p.groups, first_unit + d.seg_cost);
   x.count = run_of(all, p.groups, first_unit + n - 1) - x.run + 1;
   return x;
 }
 
-template <typename T, int kCols>
-__global__ void __launch_bounds__(32 * kJoinWarps) attend_shared_join_kernel(AttendParams p, bool few) {
+template <typename T, int kCols, bool kTensor>
+__global__ void __launch_bounds__(32 * kJoinWarps)
+attend_shared_join_kernel(AttendParams p, bool few) {
   __shared__ float4 s_o[kJoinWarps][kCols][32];
   __shared__ float2 s_ml[kJoinWarps];
-  pdl_wait();
-  pdl_trigger();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int D = p.c.head_dim, pitch = D + kPartPad;
   const int64_t id = few ? blockIdx.x : (int64_t)blockIdx.x * kJoinWarps + warp;
@@ -518,31 +531,37 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_shared_join_kernel(Att
   const int64_t token = id / p.q_heads;
   const int h = (int)(id - token * p.q_heads), b = (int)(token / p.T), t = (int)(token - (int64_t)b * p.T);
   const int head = h / p.group, row = t * p.group + h - head * p.group;
+  pdl_wait();
+  pdl_trigger();
+  // the loads go out together, whether the row needs them or not
+  const Division cut = plan_division<kTensor>(p);
   const int nodes = p.num_nodes ? min(max(__ldcg(p.num_nodes + b), 0), p.T) : p.T;
   const int32_t* units = p.sh.units + p.max_groups + b;
   const int u0 = __ldcg(units), own_units = __ldcg(units + 1) - u0, first = __ldcg(p.sh.first + b), g = __ldcg(p.sh.entry_group + b);
+  const int member = __ldcg(p.sh.entry_place + b);
   const int64_t all = (int64_t)__ldcg(p.sh.units + p.max_groups + p.B) * p.c.kv_heads;
+  const bool grouped = g >= 0 && g < p.max_groups;
+  const int start = grouped ? __ldcg(p.sh.group_start + g) : 0, v0 = grouped ? __ldcg(p.sh.units + g) : 0, group_units = grouped ? __ldcg(p.sh.units + g + 1) - v0 : 0;
   if (t >= nodes || own_units == 0) return;            // own_units == 0: a padding sequence
-  const int blocks = row_blocks_of(p, p.rows), block = row / p.rows_per_block, n = own_units / blocks;
-  const Parts own = parts_of(p, all, (int64_t)u0 * p.c.kv_heads + ((int64_t)head * blocks + block) * n, n);
+  const int blocks = row_blocks_of(cut, p.rows), block = row / cut.rows_per_block, n = own_units / blocks;
+  const Parts own = parts_of(p, cut, all, (int64_t)u0 * p.c.kv_heads + ((int64_t)head * blocks + block) * n, n);
   if (first == 0 && own.count == 1) return;
   Parts group = {0, 0};
   int64_t group_row = 0;             // among the rows of all groups; in its block
   int group_place = 0;
-  if (first > 0) {
-    const int start = __ldcg(p.sh.group_start + g), v0 = __ldcg(p.sh.units + g), group_units = __ldcg(p.sh.units + g + 1) - v0;
-    const int at = __ldcg(p.sh.entry_place + b) * p.rows + row, gn = p.seg_cost + (first >> p.tile_shift), gblocks = group_units / gn;
-    const int gblock = at / p.rows_per_block;
+  if (first > 0 && grouped) {
+    const int at = member * p.rows + row, gn = cut.seg_cost + (first >> p.tile_shift), gblocks = group_units / gn;
+    const int gblock = at / cut.rows_per_block;
     group_row = (int64_t)start * p.rows + at;
-    group_place = at - gblock * p.rows_per_block;
-    group = parts_of(p, all, (int64_t)v0 * p.c.kv_heads + ((int64_t)head * gblocks + gblock) * gn, gn);
+    group_place = at - gblock * cut.rows_per_block;
+    group = parts_of(p, cut, all, (int64_t)v0 * p.c.kv_heads + ((int64_t)head * gblocks + gblock) * gn, gn);
   }
   auto at = [&](int i) -> const float* {               // part i: the group's first
     const bool of_group = i < group.count;
     if (!of_group) i -= group.count;
     const Parts x = of_group ? group : own;
     if (x.count == 1) return (of_group ? p.sh.rec_group + (group_row * p.c.kv_heads + head) * pitch : p.sh.rec_own + (((int64_t)b * p.rows + row) * p.c.kv_heads + head) * pitch);
-    return p.part + (((int64_t)(x.run + i) * 2 + (i == 0 ? 1 : 0)) * p.part_rows + (of_group ? group_place : row - block * p.rows_per_block)) * pitch;
+    return p.part + (((int64_t)(x.run + i) * 2 + (i == 0 ? 1 : 0)) * cut.part_rows + (of_group ? group_place : row - block * cut.rows_per_block)) * pitch;
   };
   const int last = group.count + own.count - 1;
   auto write = [&](int d, const float* o, float m, float l) {   // columns d .. d + 3
@@ -569,12 +588,20 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_shared_join_kernel(Att
   }
 }
 
-template <typename T, int kShare>
+template <typename T>
 cudaError_t launch_simt(const AttendParams& p, cudaStream_t st) {
   const bool few = p.rows_per_block == 4;
-  auto kernel = p.c.head_dim <= 128 ? (few ? attend_simt_kernel<T, 1, 4, kShare> : attend_simt_kernel<T, 1, 16, kShare>)
-                                    : (few ? attend_simt_kernel<T, 2, 4, kShare> : attend_simt_kernel<T, 2, 16, kShare>);
+  auto kernel = p.c.head_dim <= 128 ? (few ? attend_simt_kernel<T, 1, 4> : attend_simt_kernel<T, 1, 16>)
+                                    : (few ? attend_simt_kernel<T, 2, 4> : attend_simt_kernel<T, 2, 16>);
   return launch_chained(kernel, dim3((unsigned)(p.groups * p.row_blocks)), dim3(kThreads), simt_smem(p.c.head_dim, p.rows_per_block), st, p);
+}
+// the pairs of shared_forms()
+template <typename T>
+cudaError_t launch_simt_shared(const AttendParams& p, cudaStream_t st) {
+  const bool few = p.rows_per_block == 4, two = p.second_rows != p.rows_per_block;
+  auto kernel = p.c.head_dim <= 128 ? (two ? attend_simt_shared_kernel<T, 1, 4, 16> : few ? attend_simt_shared_kernel<T, 1, 4, 4> : attend_simt_shared_kernel<T, 1, 16, 16>)
+                                    : (few ? attend_simt_shared_kernel<T, 2, 4, 4> : attend_simt_shared_kernel<T, 2, 16, 16>);
+  return launch_chained(kernel, dim3((unsigned)p.groups), dim3(kThreads), simt_smem(p.c.head_dim, std::max(p.rows_per_block, p.second_rows)), st, p);
 }
 
 template <typename K>
@@ -585,11 +612,11 @@ bool raise_limit(K kernel, size_t bytes) {
 }  // namespace
 
 cudaError_t run_attend_simt(const AttendParams& p, int dtype, cudaStream_t st) {
-  return dtype == JD_DTYPE_F32 ? launch_simt<float, kAlone>(p, st) : launch_simt<__nv_bfloat16, kAlone>(p, st);
+  return dtype == JD_DTYPE_F32 ? launch_simt<float>(p, st) : launch_simt<__nv_bfloat16>(p, st);
 }
 
 cudaError_t run_attend_shared_simt(const AttendParams& p, int dtype, cudaStream_t st) {
-  return dtype == JD_DTYPE_F32 ? launch_simt<float, kShared>(p, st) : launch_simt<__nv_bfloat16, kShared>(p, st);
+  return dtype == JD_DTYPE_F32 ? launch_simt_shared<float>(p, st) : launch_simt_shared<__nv_bfloat16>(p, st);
 }
 
 cudaError_t run_attend_join(const AttendParams& p, int dtype, cudaStream_t st) {
@@ -603,19 +630,22 @@ cudaError_t run_attend_join(const AttendParams& p, int dtype, cudaStream_t st) {
 
 cudaError_t run_attend_shared_join(const AttendParams& p, int dtype, cudaStream_t st) {
   const int64_t rows = (int64_t)p.B * p.T * p.q_heads;
-  const bool few = rows <= kSharedFewRows;
+  const bool few = rows <= kSharedFewRows, tensor = p.tile_shift == kTensorTileShift;
   const dim3 grid((unsigned)(few ? rows : (rows + kJoinWarps - 1) / kJoinWarps));
-  auto kernel = dtype == JD_DTYPE_F32 ? (p.c.head_dim <= 128 ? attend_shared_join_kernel<float, 1> : attend_shared_join_kernel<float, 2>)
-                                      : (p.c.head_dim <= 128 ? attend_shared_join_kernel<__nv_bfloat16, 1> : attend_shared_join_kernel<__nv_bfloat16, 2>);
+  auto kernel = dtype == JD_DTYPE_F32 ? (p.c.head_dim <= 128 ? attend_shared_join_kernel<float, 1, false> : attend_shared_join_kernel<float, 2, false>)
+                : tensor              ? attend_shared_join_kernel<__nv_bfloat16, 1, true>
+                                      : (p.c.head_dim <= 128 ? attend_shared_join_kernel<__nv_bfloat16, 1, false> : attend_shared_join_kernel<__nv_bfloat16, 2, false>);
   return launch_chained(kernel, grid, dim3(32 * kJoinWarps), 0, st, p, few);
 }
 
-template <typename T, int kShare>
+template <typename T>
 bool raise_limits() {
-  return raise_limit(attend_simt_kernel<T, 1, 4, kShare>, simt_smem(128, 4)) && raise_limit(attend_simt_kernel<T, 1, 16, kShare>, simt_smem(128, 16)) &&
-         raise_limit(attend_simt_kernel<T, 2, 4, kShare>, simt_smem(256, 4)) && raise_limit(attend_simt_kernel<T, 2, 16, kShare>, simt_smem(256, 16));
+  return raise_limit(attend_simt_kernel<T, 1, 4>, simt_smem(128, 4)) && raise_limit(attend_simt_kernel<T, 1, 16>, simt_smem(128, 16)) &&
+         raise_limit(attend_simt_kernel<T, 2, 4>, simt_smem(256, 4)) && raise_limit(attend_simt_kernel<T, 2, 16>, simt_smem(256, 16)) &&
+         raise_limit(attend_simt_shared_kernel<T, 1, 4, 4>, simt_smem(128, 4)) && raise_limit(attend_simt_shared_kernel<T, 1, 4, 16>, simt_smem(128, 16)) &&
+         raise_limit(attend_simt_shared_kernel<T, 1, 16, 16>, simt_smem(128, 16)) && raise_limit(attend_simt_shared_kernel<T, 2, 4, 4>, simt_smem(256, 4)) &&
+         raise_limit(attend_simt_shared_kernel<T, 2, 16, 16>, simt_smem(256, 16));
 }
-template <int kShare> bool raise_both() { return raise_limits<float, kShare>() && raise_limits<__nv_bfloat16, kShare>(); }
-bool simt_attend_configure() { return raise_both<kAlone>() && raise_both<kShared>(); }
+bool simt_attend_configure() { return raise_limits<float>() && raise_limits<__nv_bfloat16>(); }
 
 }  // namespace jd

@@ -265,9 +265,9 @@ __device__ __noinline__ float4 spoilt_by_context(const AttendParams& p, int slot
   return make_float4(sum[0], sum[1], sum[2], sum[3]);
 }
 
+// The kernels' body: the kernels themselves, one for a call's form or all of them for a plan to choose from, stand behind it.
 template <int D, int kMode, int kShare>
-__global__ void __launch_bounds__(kThreads, 1)
-attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ AttendParams p) {
+__device__ __forceinline__ void attend_sm100_kernel(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const AttendParams& p, const Division d) {
   using Sh = Shape<D, kMode>;
   constexpr bool kPair = Sh::kPair;
   constexpr int kCopies = Sh::kCopies, kCopyRows = Sh::kCopyRows, kCols = Sh::kCols;
@@ -304,7 +304,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   }
   tc_fence_before();
   if (kShare == kAlone && rb == 0 && tid == 0) split_none(p, g);
-  unit_prefix(ShareOf<kShare>(), p, sh.prefix, sh.warp_sums, sh.extents);   // ends with a barrier
+  unit_prefix(ShareOf<kShare>(), p, d, sh.prefix, sh.warp_sums, sh.extents);   // ends with a barrier
   pdl_trigger();
   tc_fence_after();
   const int64_t units = (int64_t)sh.prefix[items_of<kShare>(p)] * p.c.kv_heads;
@@ -327,7 +327,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       uint32_t phase = 0;
       bool ok = true;
       for (int64_t u = run0; u < run1 && ok;) {
-        const Piece x = piece_at<kShare>(p, sh.prefix, u, run1, sh.extents);
+        const Piece x = piece_at<kShare>(p, d, sh.prefix, u, run1, sh.extents);
         u = x.next;
         if (x.tiles == 0) continue;
         const Extent<kShare> ex = sh.extents[x.b];
@@ -419,7 +419,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       };
       int base = 0;                                    // ring items of the pieces in front
       for (int64_t u = uniform64(run0); u < uniform64(run1);) {
-        const Piece x = piece_at<kShare>(p, sh.prefix, u, run1, sh.extents);
+        const Piece x = piece_at<kShare>(p, d, sh.prefix, u, run1, sh.extents);
         const int n = __shfl_sync(0xffffffffu, x.tiles, 0);
         u = uniform64(x.next);
         if (n == 0) continue;
@@ -466,7 +466,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     const int w = warp >> 2, r = tid & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t t_s = tmem + lanes + w * 128, t_o = tmem + lanes + 256 + w * 128;
-    int r0 = rb * p.rows_per_block;                                 // with shared prefixes it moves with the piece
+    int r0 = rb * d.rows_per_block;                                 // with shared prefixes it moves with the piece
     const int copy = r / kCopyRows, col0 = copy * kCols;            // the copy that this warp belongs to, and its columns
     const int my_place = r % kCopyRows + (kPair ? w * 128 : 0);
     int my_row = r0 + my_place;
@@ -490,7 +490,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       Piece y;
       y.tiles = 0;
       while (u < run1) {
-        y = piece_at<kShare>(p, sh.prefix, u, run1, sh.extents);
+        y = piece_at<kShare>(p, d, sh.prefix, u, run1, sh.extents);
         u = y.next;
         if (y.tiles > 0) break;
       }
@@ -761,7 +761,7 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       const float inv = !direct ? 1.f : (l == 0.f ? 0.f : 1.f / l);
       const bool odd = *reinterpret_cast<volatile int*>(&mine.odd_values) != 0;
       // where row 0 of the numerators would stand, and how far rows are apart: a slot of this CTA, or the rows' records
-      float* part0 = p.part + (((int64_t)blockIdx.x * 2 + (x.tile0 == 0 ? 1 : 0)) * p.part_rows - r0) * (D + kPartPad);
+      float* part0 = p.part + (((int64_t)blockIdx.x * 2 + (x.tile0 == 0 ? 1 : 0)) * d.part_rows - r0) * (D + kPartPad);
       int64_t part_step = D + kPartPad;
       if (kShare != kAlone && whole) {
         part_step = (int64_t)p.c.kv_heads * (D + kPartPad);
@@ -909,36 +909,72 @@ attend_sm100_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   }
 }
 
-template <int D, int kMode, int kShare>
+template <int D, int kMode>
+__global__ void __launch_bounds__(kThreads, 1)
+attend_alone(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ AttendParams p) {
+  attend_sm100_kernel<D, kMode, kAlone>(tm_k, tm_v, p, own_division(p));
+}
+// With a plan that names one of two forms.
+template <int D, int kFirst, int kSecond>
+__global__ void __launch_bounds__(kThreads, 1)
+attend_shared(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ AttendParams p) {
+  const Division d = plan_division<true>(p);
+  if constexpr (kFirst == kSecond) attend_sm100_kernel<D, kFirst, kShared>(tm_k, tm_v, p, d);
+  else if (d.rows_per_block == p.second_rows) attend_sm100_kernel<D, kSecond, kShared>(tm_k, tm_v, p, d);
+  else attend_sm100_kernel<D, kFirst, kShared>(tm_k, tm_v, p, d);
+}
+template <int D, int kFirst, int kSecond>
+constexpr size_t shared_smem() { return std::max(attend_smem<D, kFirst, kShared>(), attend_smem<D, kSecond, kShared>()); }
+
+template <int D, int kMode>
 cudaError_t launch(const AttendParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st) {
-  return launch_chained(attend_sm100_kernel<D, kMode, kShare>, dim3((unsigned)(p.groups * p.row_blocks)), dim3(kThreads), attend_smem<D, kMode, kShare>(), st, tm_k, tm_v, p);
+  return launch_chained(attend_alone<D, kMode>, dim3((unsigned)(p.groups * p.row_blocks)), dim3(kThreads), attend_smem<D, kMode, kAlone>(), st, tm_k, tm_v, p);
 }
-// most: rows that a segment may have
-template <int D, int kShare>
-cudaError_t launch_mode(const AttendParams& p, int most, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st) {
-  if (p.rows_per_block > 128) return launch<D, kPairMode, kShare>(p, tm_k, tm_v, st);
-  if (most > 64) return launch<D, 1, kShare>(p, tm_k, tm_v, st);
-  return most > 32 ? launch<D, 2, kShare>(p, tm_k, tm_v, st) : launch<D, 4, kShare>(p, tm_k, tm_v, st);
+template <int D>
+cudaError_t launch_mode(const AttendParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st) {
+  if (p.rows_per_block > 128) return launch<D, kPairMode>(p, tm_k, tm_v, st);
+  if (p.rows > 64) return launch<D, 1>(p, tm_k, tm_v, st);
+  return p.rows > 32 ? launch<D, 2>(p, tm_k, tm_v, st) : launch<D, 4>(p, tm_k, tm_v, st);
 }
-template <int D, int kMode, int kShare>
-bool configure() {
-  static_assert(attend_smem<D, kMode, kShare>() <= 227 * 1024, "shared memory of an SM");
-  return cudaFuncSetAttribute(attend_sm100_kernel<D, kMode, kShare>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)attend_smem<D, kMode, kShare>()) == cudaSuccess;
+template <typename K>
+bool configure(K kernel, size_t bytes) {
+  return bytes <= 227 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
 }
-template <int D, int kShare>
-bool configure_modes() { return configure<D, kPairMode, kShare>() && configure<D, 1, kShare>() && configure<D, 2, kShare>() && configure<D, 4, kShare>(); }
+template <int D, int kFirst, int kSecond>
+cudaError_t launch_shared(const AttendParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st) {
+  return launch_chained(attend_shared<D, kFirst, kSecond>, dim3((unsigned)p.groups), dim3(kThreads), shared_smem<D, kFirst, kSecond>(), st, tm_k, tm_v, p);
+}
+// the pairs of shared_forms()
+template <int D>
+cudaError_t launch_forms(const AttendParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st) {
+  const bool one = p.second_rows == p.rows_per_block;
+  switch (p.rows_per_block) {
+    case 32: return one ? launch_shared<D, 4, 4>(p, tm_k, tm_v, st) : launch_shared<D, 4, 2>(p, tm_k, tm_v, st);
+    case 64: return one ? launch_shared<D, 2, 2>(p, tm_k, tm_v, st) : launch_shared<D, 2, 1>(p, tm_k, tm_v, st);
+    case 128: return one ? launch_shared<D, 1, 1>(p, tm_k, tm_v, st) : launch_shared<D, 1, kPairMode>(p, tm_k, tm_v, st);
+    default: return launch_shared<D, kPairMode, kPairMode>(p, tm_k, tm_v, st);
+  }
+}
+template <int D, int kMode> bool configure_mode() {
+  return configure(attend_alone<D, kMode>, attend_smem<D, kMode, kAlone>()) && configure(attend_shared<D, kMode, kMode>, shared_smem<D, kMode, kMode>());
+}
+template <int D, int kFirst, int kSecond> bool configure_forms() { return configure(attend_shared<D, kFirst, kSecond>, shared_smem<D, kFirst, kSecond>()); }
+template <int D>
+bool configure_modes() {
+  return configure_mode<D, kPairMode>() && configure_mode<D, 1>() && configure_mode<D, 2>() && configure_mode<D, 4>() && configure_forms<D, 4, 2>() &&
+         configure_forms<D, 2, 1>() && configure_forms<D, 1, kPairMode>();
+}
 
 }  // namespace
 
 cudaError_t run_attend_tensor(const AttendParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st) {
-  return p.c.head_dim == 64 ? launch_mode<64, kAlone>(p, p.rows, tm_k, tm_v, st) : launch_mode<128, kAlone>(p, p.rows, tm_k, tm_v, st);
+  return p.c.head_dim == 64 ? launch_mode<64>(p, tm_k, tm_v, st) : launch_mode<128>(p, tm_k, tm_v, st);
 }
 
-cudaError_t run_attend_shared_tensor(const AttendParams& p, int most, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st) {
-  return p.c.head_dim == 64 ? launch_mode<64, kShared>(p, most, tm_k, tm_v, st) : launch_mode<128, kShared>(p, most, tm_k, tm_v, st);
+cudaError_t run_attend_shared_tensor(const AttendParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st) {
+  return p.c.head_dim == 64 ? launch_forms<64>(p, tm_k, tm_v, st) : launch_forms<128>(p, tm_k, tm_v, st);
 }
 
-template <int kShare> bool configure_widths() { return configure_modes<64, kShare>() && configure_modes<128, kShare>(); }
-bool attend_configure() { return simt_attend_configure() && configure_widths<kAlone>() && configure_widths<kShared>(); }
+bool attend_configure() { return simt_attend_configure() && configure_modes<64>() && configure_modes<128>(); }
 
 }  // namespace jd

@@ -596,6 +596,7 @@ size_t carve_shared(jd_cache_t c, int B, int nodes, char* base, SharedView* s) {
                       &v.entry_lead, &v.entry_tokens, &v.first})
     *x = (int32_t*)take((size_t)(B + 1) * 4);
   v.units = (int32_t*)take((size_t)(B / 2 + B + 1) * 4);
+  v.form = (int32_t*)take(8);
   const size_t row = (size_t)(g.head_dim + kPartPad) * 4, rows = (size_t)B * nodes * (g.q_heads / g.kv_heads);
   v.rec_group = (float*)take(rows * g.kv_heads * row);
   v.rec_own = (float*)take(rows * g.kv_heads * row);
@@ -605,9 +606,15 @@ size_t carve_shared(jd_cache_t c, int B, int nodes, char* base, SharedView* s) {
   if (s) *s = v;
   return off;
 }
+bool form_ok(int rows) {
+  for (int m = 0; m < kSharedForms; ++m)
+    if (rows == form_rows(m)) return true;
+  return false;
+}
 bool shared_ok(jd_cache_t c, const jd_shared_t* plan, SharedView* s) {
   if (!c || !plan || plan->B < 1 || plan->B > kMaxSharedBatch || plan->nodes < 1 || plan->nodes > c->cfg.max_nodes) return false;
   if (!plan->buffer || (reinterpret_cast<uintptr_t>(plan->buffer) & 255u) || plan->bytes < carve_shared(c, plan->B, plan->nodes, nullptr, nullptr)) return false;
+  if (plan->rows != 0 && !form_ok(plan->rows)) return false;
   carve_shared(c, plan->B, plan->nodes, (char*)plan->buffer, s);
   return true;
 }
@@ -732,10 +739,11 @@ size_t jd_cache_shared_bytes(jd_cache_t c, int32_t B, int32_t nodes) {
 jd_status_t jd_cache_share(jd_cache_t c, const jd_shared_t* plan, const int32_t* slots, const int32_t* groups, void* cuda_stream) {
   SharedView s;
   if (!shared_ok(c, plan, &s) || !batch_ok(c, plan->B, slots) || !on4(groups)) return JD_ERR_INVALID_ARG;
+  if (plan->rows >= form_rows(0) && !c->tm_ok) return JD_ERR_UNSUPPORTED;
   OnDevice dev(c->cfg.device);
   if (!dev.ok()) return JD_ERR_CUDA;
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  return finish(c, run_share(view_of(c), s, plan->B, plan->nodes * (c->cfg.q_heads / c->cfg.kv_heads), slots, groups, st), st);
+  return finish(c, run_share(view_of(c), s, *plan, c->cfg.q_heads, c->tm_ok, c->num_sms, slots, groups, st), st);
 }
 
 jd_status_t jd_cache_attend_shared(jd_cache_t c, const jd_attend_args_t* a, const jd_shared_t* plan, void* cuda_stream) {
@@ -747,17 +755,18 @@ jd_status_t jd_cache_attend_shared(jd_cache_t c, const jd_attend_args_t* a, cons
   OnDevice dev(c->cfg.device);
   if (!dev.ok()) return JD_ERR_CUDA;
   AttendParams p = attend_params(c, *a, tensor);
-  const int most = a->B * p.rows;                             // rows of a group: up to 2^26
+  const Forms forms = shared_forms(tensor, c->cfg.head_dim, plan->rows, plan->B, plan->nodes * p.group);
   p.sh = s;
   p.max_groups = a->B / 2;
-  p.rows_per_block = tensor ? (most > 128 ? 256 : 128) : (most <= 4 ? 4 : kSimtRows);
-  p.part_rows = std::min(most, p.rows_per_block);
+  p.rows_per_block = forms.first;
+  p.second_rows = forms.second;
+  p.part_rows = std::min(a->B * p.rows, p.rows_per_block);
+  if (tensor) p.seg_cost = tensor_seg_cost(c->cfg.head_dim, p.rows_per_block);
   p.row_blocks = 1;
   p.groups = tensor ? c->num_sms : 2 * c->num_sms;
-  if (tensor) p.seg_cost = tensor_seg_cost(c->cfg.head_dim, most);
   p.part = s.part;
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  cudaError_t err = tensor ? run_attend_shared_tensor(p, most, c->tm_k, c->tm_v, st) : run_attend_shared_simt(p, c->cfg.dtype, st);
+  cudaError_t err = tensor ? run_attend_shared_tensor(p, c->tm_k, c->tm_v, st) : run_attend_shared_simt(p, c->cfg.dtype, st);
   if (err == cudaSuccess) err = run_attend_shared_join(p, c->cfg.dtype, st);
   return finish(c, err, st);
 }

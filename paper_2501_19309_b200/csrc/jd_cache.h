@@ -89,8 +89,39 @@ template <int kShare> using ShareOf = std::integral_constant<int, kShare>;
 
 constexpr int kMaxSharedBatch = 512; // sequences of a plan: groups and sequences are at most 1.5 times as many items
 constexpr int kPrefixTokens = 128;   // prefixes are cut to whole tiles of the tensor-core kernel, which are whole tiles of the other
-// tiles of kPrefixTokens that a group has to save: what its segment costs to begin, end and join is four to six tiles
-constexpr int kPrefixWorth = 8;
+// tiles of kPrefixTokens that a group has to save to be one; whether the call shares anything at all goes by its cost (form_cost)
+constexpr int kPrefixWorth = 2;
+
+constexpr int kSimtRows = 16, kSimtTileShift = 6, kSimtSegCost = 1;
+constexpr int kTensorTileShift = 7;
+// what beginning and ending a segment costs, in tiles: some 8,000 cycles, against 1,400 (64 columns) or 2,800 (128) for a tile at
+// HBM rate. A batch of 16 chains up to 6,000 tokens long: 40 us at 3, 36 at 6, 38 at 10 (64 columns). More than 128 rows: a pair of row
+// tiles takes longer a tile, and its parts are large, so that cutting a segment less often pays too (16 trees of 208 rows on 200 to
+// 4,000 tokens: 101 us at 1, 70 at 4, 66 at 5, 68 at 6).
+__host__ __device__ constexpr int tensor_seg_cost(int head_dim, int rows) { return head_dim == 64 ? 6 : (rows > 128 ? 5 : 4); }
+
+// Rows of a block that a shared call may have: those of the tensor-core kernel's forms, or of the other's.
+constexpr int kTensorForms = 4, kSharedForms = 6;
+__host__ __device__ constexpr int form_rows(int form) { return form < kTensorForms ? 32 << form : (form == kTensorForms ? 4 : 16); }
+// The forms that a plan chooses from. A block of few rows costs a sequence's own few tokens least, one of many saves a group passes over its prefix: the
+// smallest form that takes a sequence's rows, and, where the batch has the rows for long work, twice that in the same kernel, of which the plan picks by cost.
+// A second form costs every call some 4 us (the code no longer stays in the instruction cache: 15.1 us alone, 19.2 with another beside it), a
+// wrong one up to twice the time. Of random calls with 33 to 64 rows of 128 columns the sum of times falls by 8 % with the rule, with 65 to 128 rows by 10 %. On
+// CUDA cores, whose code is short, up to 4 rows of a sequence go in blocks of 4 or of 16; with more than 128 columns the latter would take the former's
+// second block off the SM.
+constexpr int kSecondForm = 1024;
+struct Forms { int first, second; };
+__host__ __device__ inline Forms shared_forms(bool tensor, int head_dim, int want, int B, int rows) {
+  if (want && tensor == (want >= form_rows(0))) return Forms{want, want};
+  if (!tensor) return rows > 4 ? Forms{kSimtRows, kSimtRows} : Forms{4, head_dim > 128 ? 4 : kSimtRows};
+  const int first = rows <= 32 ? 32 : (rows <= 64 ? 64 : (rows <= 128 ? 128 : 256));
+  return Forms{first, first < 256 && B * rows >= kSecondForm ? 2 * first : first};
+}
+
+// How a call's rows are cut: for sequences by themselves by the host, with a plan by its form.
+struct Division {
+  int rows_per_block, part_rows, seg_cost;
+};
 
 struct SharedView {                  // arrays of a plan of B sequences, all on the device
   int32_t* count;                    // [1] blocks of jd_cache_share that are done (self-resetting)
@@ -107,6 +138,7 @@ struct SharedView {                  // arrays of a plan of B sequences, all on 
   int32_t* entry_tokens;             // [B] its prefix, 0: none
   int32_t* first;                    // [B] tokens that the call takes off the sequence, as the tables stand: written by it for its join
   int32_t* units;                    // [B / 2 + B + 1] the call's division (unit_prefix), likewise
+  int32_t* form;                     // [2] rows of a block of the calls on the tensor cores and of the others
   float* rec_group;                  // [B x T x group][kv_heads][head_dim + kPartPad] rows by group member; by entry
   float* rec_own;
   float* part;                       // parts of the call
@@ -133,6 +165,7 @@ struct AttendParams {
   float scale_log2;                // scale x log2(e)
   SharedView sh;                   // kShared
   int max_groups;                  // items in front of the sequences; 0 for kAlone
+  int second_rows;                 // the other rows_per_block that the plan may name
   int4* split;                     // [groups] sequence, kv head and last group of the segment that the group leaves unfinished; x < 0: none
   float* part;                     // [groups * row_blocks][2][part_rows][head_dim + kPartPad]
 };
@@ -165,9 +198,9 @@ __device__ __forceinline__ SeqExtent seq_extent(const AttendParams& p, int b) {
   e.kv_end = min(e.ctx + e.nodes, held << p.c.page_shift);
   return e;
 }
-__device__ __forceinline__ int extent_units(const AttendParams& p, const SeqExtent& e) {
+__device__ __forceinline__ int extent_units(const AttendParams& p, const Division& d, const SeqExtent& e) {
   if (e.slot < 0 || e.nodes == 0) return 0;
-  return p.seg_cost + max(1, (e.kv_end + (1 << p.tile_shift) - 1) >> p.tile_shift);
+  return d.seg_cost + max(1, (e.kv_end + (1 << p.tile_shift) - 1) >> p.tile_shift);
 }
 
 // Tokens that sequence b leaves to its group: those of the plan if slot still has them in the group's pages, else none, so that a plan which the tables
@@ -210,21 +243,22 @@ template <int kShare> __device__ __forceinline__ Extent<kShare> extent_at(const 
     return e;
   }
 }
-__device__ __forceinline__ int row_blocks_of(const AttendParams& p, int rows) { return (int)((uint32_t)(rows + p.rows_per_block - 1) / (uint32_t)p.rows_per_block); }
-template <int kShare> __device__ __forceinline__ int item_blocks(const AttendParams& p, int i, const Extent<kShare>& e) {
-  return kShare == kAlone ? 1 : row_blocks_of(p, i < p.max_groups ? e.nodes : p.rows);
+__device__ __forceinline__ int row_blocks_of(const Division& d, int rows) { return (int)((uint32_t)(rows + d.rows_per_block - 1) / (uint32_t)d.rows_per_block); }
+__device__ __forceinline__ Division own_division(const AttendParams& p) { return Division{p.rows_per_block, p.part_rows, p.seg_cost}; }
+template <int kShare> __device__ __forceinline__ int item_blocks(const AttendParams& p, const Division& d, int i, const Extent<kShare>& e) {
+  return kShare == kAlone ? 1 : row_blocks_of(d, i < p.max_groups ? e.nodes : p.rows);
 }
-template <int kShare> __device__ __forceinline__ int units_at(const AttendParams& p, int i, const Extent<kShare>& e) {
-  const int n = extent_units(p, e);
+template <int kShare> __device__ __forceinline__ int units_at(const AttendParams& p, const Division& d, int i, const Extent<kShare>& e) {
+  const int n = extent_units(p, d, e);
   if constexpr (kShare == kAlone) return n;
-  else return n == 0 ? 0 : item_blocks<kShare>(p, i, e) * (i < p.max_groups ? n : max(n - e.more, p.seg_cost + 1));
+  else return n == 0 ? 0 : item_blocks<kShare>(p, d, i, e) * (i < p.max_groups ? n : max(n - e.more, d.seg_cost + 1));
 }
 template <int kShare> __device__ __forceinline__ int items_of(const AttendParams& p) { return kShare == kAlone ? p.B : p.max_groups + p.B; }
 
 // prefix[b] = units of one kv head in the items before b, prefix[items] = all; extents (optional): what extent_at says of each
 // item. By the whole block.
 template <int kShare>
-__device__ __forceinline__ void unit_prefix(ShareOf<kShare>, const AttendParams& p, int* prefix, int* warp_sums, Extent<kShare>* extents = nullptr) {
+__device__ __forceinline__ void unit_prefix(ShareOf<kShare>, const AttendParams& p, const Division& d, int* prefix, int* warp_sums, Extent<kShare>* extents = nullptr) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nthreads = blockDim.x, nwarps = nthreads >> 5, items = items_of<kShare>(p);
   int carry = 0;
   for (int b0 = 0; b0 < items; b0 += nthreads) {
@@ -233,7 +267,7 @@ __device__ __forceinline__ void unit_prefix(ShareOf<kShare>, const AttendParams&
     if (b < items) {
       const Extent<kShare> e = extent_at<kShare>(p, b);
       if (extents) extents[b] = e;
-      n = units_at<kShare>(p, b, e);
+      n = units_at<kShare>(p, d, b, e);
       if constexpr (kShare == kShared)
         if (blockIdx.x == 0 && b >= p.max_groups) p.sh.first[b - p.max_groups] = e.more << p.tile_shift;
     }
@@ -284,7 +318,7 @@ struct Piece {
   int row0;                         // the segment's first row; 0 where CTAs share a sequence's rows
 };
 template <int kShare = kAlone>
-__device__ __forceinline__ Piece piece_at(const AttendParams& p, const int* prefix, int64_t u, int64_t run1, const Extent<kShare>* extents = nullptr) {
+__device__ __forceinline__ Piece piece_at(const AttendParams& p, const Division& d, const int* prefix, int64_t u, int64_t run1, const Extent<kShare>* extents = nullptr) {
   Piece x;
   x.first = x.row0 = 0;
   int lo = 0, hi = items_of<kShare>(p) - 1;   // the last item with units whose first is at or before u
@@ -297,13 +331,13 @@ __device__ __forceinline__ Piece piece_at(const AttendParams& p, const int* pref
   int n = prefix[lo + 1] - prefix[lo], segment;
   if constexpr (kShare == kShared) {
     const Extent<kShare> e = extents ? extents[lo] : extent_at<kShare>(p, lo);
-    const int blocks = item_blocks<kShare>(p, lo, e);
+    const int blocks = item_blocks<kShare>(p, d, lo, e);
     if (lo >= p.max_groups) x.first = e.more;
     n = (int)((uint32_t)n / (uint32_t)blocks);
     const int64_t in_item = u - first;
     segment = in_item < 0x7FFFFFFF ? (int)((uint32_t)in_item / (uint32_t)n) : (int)(in_item / n);
     x.head = (int)((uint32_t)segment / (uint32_t)blocks);
-    x.row0 = (segment - x.head * blocks) * p.rows_per_block;
+    x.row0 = (segment - x.head * blocks) * d.rows_per_block;
   } else {
     const int in_seq = (int)(u - first);
     x.head = segment = (int)((uint32_t)in_seq / (uint32_t)n);
@@ -311,9 +345,9 @@ __device__ __forceinline__ Piece piece_at(const AttendParams& p, const int* pref
   const int at = (int)(u - first - (int64_t)segment * n);
   const int64_t seg_end = first + (int64_t)(segment + 1) * n;
   x.next = min(seg_end, run1);
-  x.all = n - p.seg_cost;
-  x.tile0 = max(0, at - p.seg_cost);
-  x.tiles = max(0, at + (int)(x.next - u) - p.seg_cost) - x.tile0;
+  x.all = n - d.seg_cost;
+  x.tile0 = max(0, at - d.seg_cost);
+  x.tiles = max(0, at + (int)(x.next - u) - d.seg_cost) - x.tile0;
   return x;
 }
 
@@ -336,6 +370,19 @@ __device__ __forceinline__ void split_set(const AttendParams& p, int g, int64_t 
 
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// How a call with a plan cuts its rows, once the kernel that may have made the plan is done.
+template <bool kTensor> __device__ __forceinline__ Division plan_division(const AttendParams& p) {
+  Division d = own_division(p);
+  if (p.second_rows == p.rows_per_block) return d;
+  pdl_wait();
+  if (__ldcg(p.sh.form + (kTensor ? 0 : 1)) == p.second_rows) {
+    d.rows_per_block = p.second_rows;
+    d.part_rows = min(p.B * p.rows, p.second_rows);
+    if (kTensor) d.seg_cost = tensor_seg_cost(p.c.head_dim, p.second_rows);
+  }
+  return d;
+}
 
 // A kernel that starts early runs while the one in front of it still writes, so nothing it reads is read-only for its whole life: the
 // kernels here use no non-coherent loads (__ldg, const __restrict__), and take what other kernels write from L2 (__ldcg) or by plain
@@ -360,21 +407,14 @@ inline cudaError_t launch_chained(void (*kernel)(Params...), dim3 grid, dim3 blo
 cudaError_t run_attend_simt(const AttendParams& p, int dtype, cudaStream_t st);
 cudaError_t run_attend_tensor(const AttendParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st);
 cudaError_t run_attend_join(const AttendParams& p, int dtype, cudaStream_t st);
-// Attention with a plan, and what adds its results up. most: rows that a segment may have
+// Attention with a plan, and what adds its results up.
 cudaError_t run_attend_shared_simt(const AttendParams& p, int dtype, cudaStream_t st);
-cudaError_t run_attend_shared_tensor(const AttendParams& p, int most, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st);
+cudaError_t run_attend_shared_tensor(const AttendParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st);
 cudaError_t run_attend_shared_join(const AttendParams& p, int dtype, cudaStream_t st);
 bool simt_attend_configure();
 bool attend_configure();   // dynamic shared-memory limits on the current device, once per device
-constexpr int kSimtRows = 16, kSimtTileShift = 6, kSimtSegCost = 1;
-constexpr int kTensorTileShift = 7;
-// what beginning and ending a segment costs, in tiles: some 8,000 cycles, against 1,400 (64 columns) or 2,800 (128) for a tile at
-// HBM rate. A batch of 16 chains up to 6,000 tokens long: 40 us at 3, 36 at 6, 38 at 10 (64 columns). More than 128 rows: a pair of row
-// tiles takes longer a tile, and its parts are large, so that cutting a segment less often pays too (16 trees of 208 rows on 200 to
-// 4,000 tokens: 101 us at 1, 70 at 4, 66 at 5, 68 at 6).
-constexpr int tensor_seg_cost(int head_dim, int rows) { return head_dim == 64 ? 6 : (rows > 128 ? 5 : 4); }
 
-cudaError_t run_share(const CacheView& c, const SharedView& s, int B, int rows, const int32_t* slots, const int32_t* groups, cudaStream_t st);
+cudaError_t run_share(const CacheView& c, const SharedView& s, const jd_shared_t& plan, int q_heads, bool tensor, int num_sms, const int32_t* slots, const int32_t* groups, cudaStream_t st);
 bool rope_valid(const jd_rope_t& r, int head_dim);
 cudaError_t run_append(const CacheView& c, const jd_append_args_t& a, int q_heads, int dtype, cudaStream_t st);
 bool append_heads_valid(const jd_head_norm_t* n, const jd_rope_axes_t* a, const jd_rope_t* r);

@@ -137,7 +137,7 @@ class jd_attend_args_t(C.Structure):
 
 
 class jd_shared_t(C.Structure):
-    _fields_ = [("B", C.c_int32), ("nodes", C.c_int32), ("buffer", C.c_void_p), ("bytes", C.c_size_t)]
+    _fields_ = [("B", C.c_int32), ("nodes", C.c_int32), ("buffer", C.c_void_p), ("bytes", C.c_size_t), ("rows", C.c_int32)]
 
 
 class jd_commit_args_t(C.Structure):

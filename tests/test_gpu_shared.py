@@ -36,6 +36,22 @@ def forked(prefixes, members, own, T, *, page=16, q_heads=4, kv_heads=2, D=64, d
     return c, slots[torch.as_tensor(np.asarray(perm), device="cuda")].contiguous()
 
 
+def forms(c):
+    """By cost, and every form in which the cache's calls can share."""
+    return (0, 32, 64, 128, 256) if c.dtype == torch.bfloat16 and c.head_dim in (64, 128) else (0, 4, 16)
+
+
+def arrays(plan):
+    """The plan's arrays behind its counter, each from a multiple of 256 bytes: first members, tokens of the groups, members, groups of the entries."""
+    torch.cuda.synchronize()
+    ints, step = plan.buffer[256:].view(torch.int32), ((plan.B + 1) * 4 + 255) // 256 * 64
+    return [ints[k * step:k * step + n].tolist() for k, n in ((2, plan.B // 2), (3, plan.B // 2), (5, plan.B), (6, plan.B))]
+
+
+def shares(plan):
+    return any(n > 0 for n in arrays(plan)[1])
+
+
 def tree_of(T, seed, style="tree"):
     parents = L.random_tree(T, np.random.default_rng(seed), style)
     return L.device_tree(parents), O.visible(parents)[0]
@@ -74,12 +90,14 @@ def test_shared_attention(prefixes, members, own, T, page, q_heads, kv_heads, D,
     c, slots = forked(prefixes, members, own, T, page=page, q_heads=q_heads, kv_heads=kv_heads, D=D, dtype=dtype)
     tree, see = tree_of(T, 3)
     q = rand((len(own), T, q_heads, D), 9, dtype)
-    plan = c.share(T, slots=slots)
-    for variant in ("auto", "simt"):
-        got = c.attend(0, q, tree, slots=slots, shared=plan, variant=variant)
-        check(c, q, see, got, slots)
-        again = c.attend(0, q, tree, slots=slots, shared=plan, variant=variant)
-        assert torch.equal(got["out"], again["out"]) and torch.equal(got["lse"], again["lse"])     # bit for bit
+    plan = None
+    for rows in forms(c) + (4, 16):
+        plan = c.share(T, slots=slots, plan=plan, rows=rows)
+        for variant in ("auto", "simt"):
+            got = c.attend(0, q, tree, slots=slots, shared=plan, variant=variant)
+            check(c, q, see, got, slots)
+            again = c.attend(0, q, tree, slots=slots, shared=plan, variant=variant)
+            assert torch.equal(got["out"], again["out"]) and torch.equal(got["lse"], again["lse"])     # bit for bit
     assert c.status() == jd.JD_OK
 
 
@@ -101,23 +119,24 @@ def test_random_batches(seed):
     parents = L.random_tree(T, rng)
     tree, see = L.device_tree(parents, num_nodes=nodes), O.visible(parents)[0]
     q = rand((len(names), T, kv * group, D), seed)
-    out = dict(out=torch.full_like(q, 7.0), lse=torch.full(q.shape[:3], 7.0, device="cuda"))
-    plan = c.share(T, slots=slots)
-    c.attend(0, q, tree, slots=slots, shared=plan, out=out)
-    check(c, q, see, out, slots, nodes)
-    for b, n in enumerate(nodes.tolist()):
-        n = 0 if names[b] < 0 else n
-        assert (out["out"][b, n:] == 7).all() and (out["lse"][b, n:] == 7).all()      # rows behind the nodes are left as they were
+    for rows in forms(c):
+        out = dict(out=torch.full_like(q, 7.0), lse=torch.full(q.shape[:3], 7.0, device="cuda"))
+        plan = c.share(T, slots=slots, rows=rows)
+        c.attend(0, q, tree, slots=slots, shared=plan, out=out)
+        check(c, q, see, out, slots, nodes)
+        for b, n in enumerate(nodes.tolist()):
+            n = 0 if names[b] < 0 else n
+            assert (out["out"][b, n:] == 7).all() and (out["lse"][b, n:] == 7).all()      # rows behind the nodes are left as they were
 
 
-@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("f32", 64)])
-def test_plans_that_the_tables_have_left_behind(dtype, D):
+@pytest.mark.parametrize("dtype,D,rows", [("bf16", 128, 32), ("bf16", 128, 256), ("f32", 64, 4), ("f32", 64, 16), ("bf16", 64, 0)])
+def test_plans_that_the_tables_have_left_behind(dtype, D, rows):
     """A plan is made, then a member is cut back into the prefix and grows again, the leader is, a slot is emptied and becomes something else, pages move: results stay
     right with the old plan, and with one of other slots."""
     c, slots = forked([800, 700], [4, 3], [20] * 7, 4, q_heads=4, kv_heads=2, D=D, dtype=dtype, order=np.arange(7))
     tree, see = tree_of(4, 1)
     q = rand((7, 4, 4, D), 5, dtype)
-    plan = c.share(4, slots=slots)
+    plan = c.share(4, slots=slots, rows=rows)
 
     def right(now):
         c.reserve(4, slots=slots)
@@ -140,7 +159,7 @@ def test_plans_that_the_tables_have_left_behind(dtype, D):
     right(slots.flip(0).contiguous())                                   # other slots than the plan's
     c.compact()
     right(slots)
-    plan = c.share(4, slots=slots, plan=plan)                           # and made anew
+    plan = c.share(4, slots=slots, plan=plan, rows=rows)                # and made anew
     right(slots)
 
 
@@ -155,7 +174,7 @@ def test_numbers_of_the_callers():
     tree, see = tree_of(3, 1)
     q = rand((6, 3, 4, 64), 2)
     for numbers in (None, [0, 0, 0, 1, 1, 1], [5, 5, -1, 5, -7, 5], [0, 1, 2, 3, 4, 5], [0, 1, 0, 1, 0, 1]):
-        plan = c.share(3, slots=slots, groups=None if numbers is None else L.ints(numbers))
+        plan = c.share(3, slots=slots, groups=None if numbers is None else L.ints(numbers), rows=32)
         check(c, q, see, c.attend(0, q, tree, slots=slots, shared=plan), slots)
     assert c.status() == jd.JD_OK
 
@@ -163,29 +182,38 @@ def test_numbers_of_the_callers():
 def test_prefixes_are_found():
     """The plan's own arrays: what is shared, in whole tiles, by whom."""
     c, slots = forked([1000, 640], [3, 2], [30, 0, 500, 9, 9], 1, order=[3, 0, 4, 1, 2])
+    plan = c.share(1, slots=slots, rows=64)
+    start, tokens, member, entry = arrays(plan)
+    # entries 1, 3 and 4 share 1000 tokens, 992 in full pages, seven tiles of 128; 0 and 2 share 640, five
+    assert (start, tokens, member, entry) == ([0, 2], [640, 896], [0, 2, 1, 3, 4], [0, 1, 0, 1, 1])
+    plan = c.share(1, slots=slots, plan=plan)                           # some microseconds for a dozen tiles: not by cost
+    assert arrays(plan)[1] == [0, 0] and arrays(plan)[3] == [-1] * 5 and not shares(plan)
+
+
+def test_what_pays_is_shared():
+    """By cost: 40 sequences behind 4000 tokens are, and as lengths have it; pairs of short ones are not."""
+    c, slots = forked([4000], [40], [5] * 40, 1, page=16, q_heads=16, kv_heads=4, D=128)
     plan = c.share(1, slots=slots)
-    torch.cuda.synchronize()
-    ints = plan.buffer[256:].view(torch.int32)
-    step = 64                                                           # arrays of 6 numbers, 256 bytes apart
-    start, tokens = ints[2 * step:2 * step + 2].tolist(), ints[3 * step:3 * step + 2].tolist()
-    member, entry = ints[5 * step:5 * step + 3].tolist(), ints[6 * step:6 * step + 5].tolist()
-    # three share 1000 tokens, 992 in full pages, seven tiles of 128; 640 tokens for two would save five tiles: too few
-    assert (start, tokens, member, entry) == ([0, 3], [896, 0], [1, 3, 4], [-1, 0, -1, 0, 0])
+    assert arrays(plan)[1][:2] == [3968, 0] and arrays(plan)[3] == [0] * 40
+    c.truncate(L.ints([130] * 40), slots=slots)
+    assert not shares(c.share(1, slots=slots, plan=plan))
+    c, slots = forked([4000], [40], [5] * 40, 1, page=16, q_heads=16, kv_heads=4, D=128, dtype="f32")
+    assert arrays(c.share(1, slots=slots))[1][:2] == [3968, 0]
 
 
-@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 64)])
-def test_a_captured_step_replays(dtype, D):
+@pytest.mark.parametrize("dtype,D,rows", [("bf16", 128, 64), ("bf16", 64, 256), ("bf16", 64, 0), ("f32", 64, 4), ("f32", 64, 16)])
+def test_a_captured_step_replays(dtype, D, rows):
     """Plan and attention in a graph; lengths and what is shared change between replays."""
     c, slots = forked([900], [5], [20] * 5, 4, q_heads=8, kv_heads=2, D=D, dtype=dtype, layers=2)
     tree, see = tree_of(4, 2)
     q = rand((5, 4, 8, D), 5, dtype)
-    plan = c.share(4, slots=slots)
+    plan = c.share(4, rows=rows, slots=slots)
     outs = [c.attend(i, q, tree, slots=slots, shared=plan) for i in range(2)]
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         c.reserve(4, slots=slots)
-        c.share(4, slots=slots, plan=plan)
+        c.share(4, rows=rows, slots=slots, plan=plan)
         outs = [c.attend(i, q, tree, slots=slots, shared=plan) for i in range(2)]
     for i in range(3):
         if i == 1:
@@ -204,14 +232,14 @@ def test_two_handles_two_plans_two_streams():
     d = jd.PagedCache(c.k, c.v, c.page_table, c.seq_len, c.held, c.refs, c.free_bits, c.q_heads, c.max_nodes)
     tree, _ = tree_of(3, 2)
     q = rand((6, 3, 8, 128), 5)
-    plans = [x.share(3, slots=slots) for x in (c, d)]
+    plans = [x.share(3, rows=128, slots=slots) for x in (c, d)]
     want = c.attend(0, q, tree, slots=slots, shared=plans[0])
     torch.cuda.synchronize()
     streams, got = [torch.cuda.Stream() for _ in range(2)], []
     for _ in range(20):
         for x, plan, s in zip((c, d), plans, streams):
             with torch.cuda.stream(s):
-                x.share(3, slots=slots, plan=plan)
+                x.share(3, rows=128, slots=slots, plan=plan)
                 got.append(x.attend(0, q, tree, slots=slots, shared=plan))
     torch.cuda.synchronize()
     assert all(torch.equal(x["out"], want["out"]) and torch.equal(x["lse"], want["lse"]) for x in got)
@@ -234,7 +262,11 @@ def test_values_that_are_not_finite(dtype, D, T, q_heads):
     if T > 1:
         c.v[0, int(table[int(slots[1]), (lens[1] + 1) // 16]), 0, (lens[1] + 1) % 16, 11] = float("-inf")   # node 1 of sequence 1: its own alone
     q = rand((4, T, q_heads, D), 5, dtype)
-    got = c.attend(0, q, tree, slots=slots, shared=c.share(T, slots=slots))
+    for rows in forms(c):
+        values_hold(c, q, tree, slots, T, c.attend(0, q, tree, slots=slots, shared=c.share(T, slots=slots, rows=rows)))
+
+
+def values_hold(c, q, tree, slots, T, got):
     o = got["out"].float()
     assert (o[..., 7] == float("inf")).all() and torch.isnan(o[2, ..., 9]).all()
     hit = torch.zeros_like(o, dtype=torch.bool)
@@ -250,8 +282,8 @@ def test_values_that_are_not_finite(dtype, D, T, q_heads):
 def test_a_long_prefix_and_many_sequences():
     c, slots = forked([20000], [60], [1] * 60, 1, page=128, q_heads=4, kv_heads=1, D=64)
     q = rand((60, 1, 4, 64), 5)
-    got = c.attend(0, q, slots=slots, shared=c.share(1, slots=slots))
-    check(c, q, np.ones((1, 1), dtype=bool), got, slots)
+    for rows in forms(c):
+        check(c, q, np.ones((1, 1), dtype=bool), c.attend(0, q, slots=slots, shared=c.share(1, slots=slots, rows=rows)), slots)
 
 
 def test_more_sequences_than_threads():
@@ -259,11 +291,12 @@ def test_more_sequences_than_threads():
     n = 256
     c, slots = forked([1200] * 2, [n, n], [0] * (2 * n), 1, page=64, q_heads=1, kv_heads=1, D=64, order=np.arange(2 * n).reshape(2, n).T.reshape(-1))
     q = rand((2 * n, 1, 1, 64), 5)
-    got = c.attend(0, q, slots=slots, shared=c.share(1, slots=slots))
     plain = c.attend(0, q, slots=slots)
-    # weights rounded to bf16 in either call, and both outputs: 4 steps
-    assert (got["out"].float() - plain["out"].float()).abs().max() <= 4 * 2.0 ** -8 * c.v.float().abs().max()
-    assert (got["lse"] - plain["lse"]).abs().max() <= 1e-5
+    for rows in forms(c):
+        got = c.attend(0, q, slots=slots, shared=c.share(1, slots=slots, rows=rows))
+        # weights rounded to bf16 in either call, and both outputs: 4 steps
+        assert (got["out"].float() - plain["out"].float()).abs().max() <= 4 * 2.0 ** -8 * c.v.float().abs().max()
+        assert (got["lse"] - plain["lse"]).abs().max() <= 1e-5
     with pytest.raises(ValueError, match="512"):
         L.empty_cache(1, 1, 8, 1, 1, 8, 513, 1, 1).share(1)
 
@@ -282,7 +315,7 @@ def test_a_step_with_everything():
         outs = []
         for step in range(3):
             c.reserve(T, slots=slots)
-            plan = c.share(T, slots=slots) if shared else None
+            plan = c.share(T, slots=slots, rows=32) if shared else None
             for layer in range(2):
                 q, k, v = (rand((B, T, h, 64), 10 * step + 3 * layer + i) for i, h in enumerate((4, 2, 2)))
                 q = c.append(layer, k, v, tree, rotary=r, q=q, slots=slots, norm=norm)
@@ -309,7 +342,8 @@ def test_refusals():
     for bad in (lambda: c.attend(0, q, slots=slots, shared=plan), lambda: d.attend(0, q[:, :2], slots=slots, shared=plan), lambda: c.share(9, slots=slots),
                 lambda: c.share(0, slots=slots), lambda: c.share(4, slots=slots, plan=plan), lambda: c.share(2, slots=slots[:2].contiguous(), plan=plan),
                 lambda: d.share(2, slots=slots, plan=plan), lambda: c.attend(0, q[:2, :2].contiguous(), slots=slots[:2].contiguous(), shared=plan),
-                lambda: c.share(2, slots=slots, groups=torch.zeros(3, device="cuda")), lambda: c.share(2, slots=slots, groups=L.ints([0, 1]))):
+                lambda: c.share(2, slots=slots, groups=torch.zeros(3, device="cuda")), lambda: c.share(2, slots=slots, groups=L.ints([0, 1])),
+                lambda: c.share(2, slots=slots, rows=8)):
         with pytest.raises(ValueError):
             bad()
     lib, a = c._lib, jd.jd_attend_args_t()
@@ -318,6 +352,12 @@ def test_refusals():
     for x in (small, off, jd.jd_shared_t(3, 2, 0, plan.c.bytes), jd.jd_shared_t(0, 2, plan.c.buffer, plan.c.bytes), jd.jd_shared_t(513, 2, plan.c.buffer, plan.c.bytes)):
         assert lib.jd_cache_share(c.h, x, slots.data_ptr(), None, None) == jd.JD_ERR_INVALID_ARG
         assert lib.jd_cache_attend_shared(c.h, a, x, None) == jd.JD_ERR_INVALID_ARG
+    for rows, want in ((8, jd.JD_ERR_INVALID_ARG), (-4, jd.JD_ERR_INVALID_ARG), (512, jd.JD_ERR_INVALID_ARG)):
+        x = jd.jd_shared_t(3, 2, plan.c.buffer, plan.c.bytes, rows)
+        assert lib.jd_cache_share(c.h, x, slots.data_ptr(), None, None) == want
+    e, _ = forked([300], [3], [1, 2, 3], 4, D=64, dtype="f32")
+    with pytest.raises(jd.JdError):
+        e.share(2, slots=slots, rows=64)                                # no tensor cores for it
     bad = L.ints([3, 99, 4])
     c.attend(0, q[:, :2].contiguous(), slots=bad, shared=c.share(2, slots=bad, plan=plan))
     assert c.status() == jd.JD_ERR_BAD_INDEX
