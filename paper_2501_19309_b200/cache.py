@@ -10,6 +10,9 @@ One decoding step of a stack of target layers::
     out = verifier.verify(H, draft_tokens, draft_logits, ...)    # accept_len stays on the device
     cache.commit(out["accept_len"])                              # keep the accepted nodes, drop the rest (of a tree: with paths)
 
+Heads that are normalised take ``append(norm=HeadNorm(..))``, tokens with several positions ``Rotary(axes=..)``, and sequences that share leading
+pages a plan: ``plan = cache.share(T)`` once a step, then ``attend(.., shared=plan)``.
+
 Argument marshalling only; every step runs inside the library's kernels.  All calls are enqueued on ``stream`` (default:
 torch's current stream of the cache's device) and none waits for the device, except :meth:`PagedCache.status`.  Outputs that a
 call makes itself are allocated on the current stream: with another ``stream``, pass them in.  Nothing here records a graph for
