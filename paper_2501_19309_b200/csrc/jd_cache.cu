@@ -756,6 +756,9 @@ jd_status_t jd_cache_attend_shared(jd_cache_t c, const jd_attend_args_t* a, cons
   if (!dev.ok()) return JD_ERR_CUDA;
   AttendParams p = attend_params(c, *a, tensor);
   const Forms forms = shared_forms(tensor, c->cfg.head_dim, plan->rows, plan->B, plan->nodes * p.group);
+  // the division's sums are 32 bits: the plan bounds the groups' part, and a batch whose own could pass the rest goes by itself
+  const int64_t tiles = ((int64_t)c->cfg.max_pages * c->cfg.page_size >> p.tile_shift) + 8;
+  if (a->B * ((p.rows + forms.first - 1) / forms.first) * tiles > kMostUnits) return jd_cache_attend(c, a, cuda_stream);
   p.sh = s;
   p.max_groups = a->B / 2;
   p.rows_per_block = forms.first;

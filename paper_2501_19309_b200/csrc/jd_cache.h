@@ -89,6 +89,8 @@ template <int kShare> using ShareOf = std::integral_constant<int, kShare>;
 
 constexpr int kMaxSharedBatch = 512; // sequences of a plan: groups and sequences are at most 1.5 times as many items
 constexpr int kPrefixTokens = 128;   // prefixes are cut to whole tiles of the tensor-core kernel, which are whole tiles of the other
+// units of all groups' prefix segments, whatever kernel takes them, and of all sequences' own ones: the sums of both are 32 bits
+constexpr int64_t kMostUnits = (int64_t)1 << 30;
 // tiles of kPrefixTokens that a group has to save to be one; whether the call shares anything at all goes by its cost (form_cost)
 constexpr int kPrefixWorth = 2;
 

@@ -11,7 +11,6 @@ namespace jd {
 namespace {
 
 constexpr int kThreads = kMaxSharedBatch;         // the last block: one for each entry
-constexpr int64_t kMostUnits = (int64_t)1 << 30;  // of all groups' prefix segments, whatever kernel takes them: their sums are 32 bits
 
 // Inclusive sums over the block's threads; buf [kThreads / 32].
 __device__ __forceinline__ unsigned long long scan(unsigned long long v, unsigned long long* buf) {

@@ -361,3 +361,19 @@ def test_refusals():
     bad = L.ints([3, 99, 4])
     c.attend(0, q[:, :2].contiguous(), slots=bad, shared=c.share(2, slots=bad, plan=plan))
     assert c.status() == jd.JD_ERR_BAD_INDEX
+
+
+def test_more_work_than_the_division_counts():
+    """Caches whose sequences could have more tiles and rows than 32 bits hold: the call is the one without a plan."""
+    B, T, heads = 8, 128, 64
+    c = L.empty_cache(1, 40, 1024, heads, 1, 8, B + 1, 1 << 14, T, "f32", fill=1)
+    c.reserve(2100, slots=L.ints([B]))
+    c.seq_len[B:] = L.ints([2100])
+    slots = torch.arange(B, dtype=torch.int32, device="cuda")
+    c.fork(L.ints([B] * B), slots)
+    c.reserve(T, slots=slots)
+    q = rand((B, T, heads, 8), 3, "f32")
+    plan = c.share(T, slots=slots, rows=16)
+    assert shares(plan) and c.status() == jd.JD_OK
+    got, want = c.attend(0, q, slots=slots, shared=plan), c.attend(0, q, slots=slots)
+    assert torch.equal(got["out"], want["out"]) and torch.equal(got["lse"], want["lse"]) and torch.isfinite(want["out"]).all()
