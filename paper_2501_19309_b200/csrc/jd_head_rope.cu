@@ -24,9 +24,10 @@ constexpr int kMaxAxes = 4;
 constexpr int kGradBlocks = 1024;         // most blocks of the backward pass, each with a partial sum of dw
 // Blocks on an SM, and the tokens whose angles a block forms at most, that many heads a group of lanes at a time: 16,384 tokens of 32 + 8 heads of 128 take
 // 62 us with 8 tokens, 64 with 4 or 16, 75 with 2; backwards (8,192 tokens) 65 us with 16, 70 with 8, 76 with 32; with three blocks an SM, whose registers do not
-// hold the sums, 89.
+// hold the sums, 89. Pairs side by side need half the registers: 72 us with three blocks, 84 with two, 73 with four.
 constexpr int kForwardBlocks = 4, kForwardTokens = 8, kForwardTurns = 20;
-constexpr int kBackwardBlocks = 2, kBackwardTokens = 16, kBackwardTurns = 40;
+constexpr int kBackwardTokens = 16, kBackwardTurns = 40;
+constexpr int backward_blocks(bool half) { return half ? 2 : 3; }
 
 enum Form { kScalar = 0, kHalfVec = 1, kPairVec = 2 };   // single elements; 8 + 8 of them half a rotation apart; 8 that hold 4 pairs
 
@@ -509,7 +510,7 @@ __global__ void __launch_bounds__(kThreads, kForwardBlocks) head_rope_kernel(con
 
 // Blocks [0, q_blocks) walk over the tokens' queries, the others over the keys, so that a lane's sums of g n, whose elements stay the same, are registers.
 template <typename T, bool kHalf>
-__global__ void __launch_bounds__(kThreads, kBackwardBlocks) head_rope_grad_kernel(const __grid_constant__ HeadParams p, const __grid_constant__ AxisMap m) {
+__global__ void __launch_bounds__(kThreads, backward_blocks(kHalf)) head_rope_grad_kernel(const __grid_constant__ HeadParams p, const __grid_constant__ AxisMap m) {
   using P = Piece8<T, kHalf>;
   constexpr int kTwos = P::kTwos;
   extern __shared__ Two turns[];                       // [tokens][twos][pieces] cosines and sines, then the weights; in the end the warps' sums
@@ -926,7 +927,7 @@ template <typename T, int kForm> struct Forward {
 template <typename T, int kForm> struct Backward {
   static cudaError_t go(HeadParams& p, int* blocks, const AxisMap& m, cudaStream_t st) {
     const int groups = kThreads / p.lanes, heads = p.q_heads + p.k_heads;
-    const int64_t most = std::min(kGradBlocks - 1, num_sms() * kBackwardBlocks);
+    const int64_t most = std::min(kGradBlocks - 1, num_sms() * backward_blocks(kForm != kPairVec));
     // an even share of the tokens for every block, but three heads a group of lanes at least
     const int64_t more = std::max(p.q_heads, p.k_heads), least = (3 * groups + more - 1) / more;
     p.per_block = kForm == kScalar ? kTokensPerBlock
