@@ -8,7 +8,7 @@
 // has pieces of 16 bytes (or, half a rotation apart, pairs of them) hold it in registers: a sum over the head is a few shuffles, and nothing is
 // read twice. A block takes a few tokens: it forms the cosines and sines of their angles once, times the weights, and shares them among the heads through
 // shared memory, while the first heads' loads are under way. Shapes that are no multiple of 16 bytes take single elements, a warp for a head.
-// 16,384 tokens of 32 + 8 heads of 128, bf16: 58 us, 5.8 TB/s (issue slots 75 %); backwards, 8,192 tokens: 65 us, 3.9 TB/s (16 warps an SM, issue slots 56 %).
+// 16,384 tokens of 32 + 8 heads of 128, bf16: 58 us, 5.8 TB/s (issue slots 75 %); backwards, 8,192 tokens: 63.5 us, 4.0 TB/s (16 warps an SM, issue slots 56 %).
 #include <algorithm>
 #include <cmath>
 
@@ -24,7 +24,7 @@ constexpr int kMaxAxes = 4;
 constexpr int kGradBlocks = 1024;         // most blocks of the backward pass, each with a partial sum of dw
 // Blocks on an SM, and the tokens whose angles a block forms at most, that many heads a group of lanes at a time: 16,384 tokens of 32 + 8 heads of 128 take
 // 62 us with 8 tokens, 64 with 4 or 16, 75 with 2; backwards (8,192 tokens) 65 us with 16, 70 with 8, 76 with 32; with three blocks an SM, whose registers do not
-// hold the sums, 89. Pairs side by side need half the registers: 72 us with three blocks, 84 with two, 73 with four.
+// hold the sums, 89. Pairs side by side need half the registers: 72 us with three blocks (70 since), 84 with two, 73 with four.
 constexpr int kForwardBlocks = 4, kForwardTokens = 8, kForwardTurns = 20;
 constexpr int kBackwardTokens = 16, kBackwardTurns = 40;
 constexpr int backward_blocks(bool half) { return half ? 2 : 3; }
@@ -61,6 +61,17 @@ __device__ __forceinline__ int scalar_units(const HeadShape& s) { return s.head_
 __device__ __forceinline__ float sum_over(float v, int lanes) {
   for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
+}
+
+// two sums at once, their shuffles' latencies beside one another: 8,192 tokens of 32 + 8 heads of 128 backwards 63.5 us, 64.8 one behind the other
+__device__ __forceinline__ void sums_over(float& v, float& w, int lanes) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    if (o >= lanes) continue;
+    const float x = __shfl_xor_sync(0xffffffffu, v, o), y = __shfl_xor_sync(0xffffffffu, w, o);
+    v += x;
+    w += y;
+  }
 }
 
 // One head by a warp: y = R(n w).
@@ -206,7 +217,8 @@ __global__ void __launch_bounds__(kThreads) head_rope_grad_scalar_kernel(const _
         squares = fmaf(xa[k], xa[k], fmaf(xb[k], xb[k], squares));
         dot = fmaf(ga[k] * wa[k], xa[k], fmaf(gb[k] * wb[k], xb[k], dot));
       }
-      const float r = rsqrtf(sum_over(squares, 32) * per_dim + s.eps), mean = sum_over(dot, 32) * r * per_dim;   // mean of g w n
+      sums_over(squares, dot, 32);
+      const float r = rsqrtf(squares * per_dim + s.eps), mean = dot * r * per_dim;   // mean of g w n
       __syncwarp();                                    // d may be x or g
 #pragma unroll
       for (int k = 0; k < kScalarUnits; ++k) {
@@ -583,7 +595,10 @@ __global__ void __launch_bounds__(kThreads, backward_blocks(kHalf)) head_rope_gr
       float s0, s1, d0, d1;
       unpack2(squares, s0, s1);
       unpack2(dot, d0, d1);
-      const float r = rsqrtf(sum_over(s0 + s1, x.lanes) * per_dim + s.eps), mean = sum_over(d0 + d1, x.lanes) * r * per_dim;   // mean of g w n
+      s0 += s1;
+      d0 += d1;
+      sums_over(s0, d0, x.lanes);
+      const float r = rsqrtf(s0 * per_dim + s.eps), mean = d0 * r * per_dim;   // mean of g w n
       const uint64_t r2 = pack2(r, r), mean2 = pack2(-mean, -mean);
 #pragma unroll
       for (int j = 0; j < kTwos; ++j) {
