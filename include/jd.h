@@ -400,7 +400,7 @@ typedef struct {
 typedef struct {
   const float* q_weight;      /* DEVICE [head_dim], 4-byte aligned; NULL: ones */
   const float* k_weight;
-  float eps;                  /* >= 0 and finite */
+  float eps;                  /* >= 0 and finite; with 0 a head of zeroes is NaN, and so is a sum of gradients that it is part of */
 } jd_head_norm_t;
 
 typedef struct {

@@ -598,7 +598,8 @@ __global__ void __launch_bounds__(kThreads, backward_blocks(kHalf)) head_rope_gr
       s0 += s1;
       d0 += d1;
       sums_over(s0, d0, x.lanes);
-      const float r = rsqrtf(s0 * per_dim + s.eps), mean = d0 * r * per_dim;   // mean of g w n
+      // 0 for a group of lanes whose item is behind the last: its zeroes add nothing to the weights' sums, where 1 / sqrt(0) times them would be NaN
+      const float r = t < n ? rsqrtf(s0 * per_dim + s.eps) : 0.f, mean = d0 * r * per_dim;   // mean of g w n
       const uint64_t r2 = pack2(r, r), mean2 = pack2(-mean, -mean);
 #pragma unroll
       for (int j = 0; j < kTwos; ++j) {

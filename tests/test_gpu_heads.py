@@ -282,3 +282,20 @@ def test_append_with_norms_refusals_and_bad_pages():
     assert (c.k != before).any(-1).sum() <= 4 * 2                          # sequence 0's rows alone
     c.append(0, k, k, norm=norm, slots=L.ints([0, 0]))
     assert c.status() == jd.JD_ERR_BAD_INDEX                               # a slot named twice
+
+
+@pytest.mark.parametrize("n,heads,D,rot,layout,dtype", [
+    (3, (1, 1), 128, 128, "half", "bf16"), (3, (1, 3), 128, 64, "interleaved", "f32"), (5, (3, 1), 64, 64, "half", "f32"), (1, (2, 1), 64, 64, "interleaved", "bf16"),
+    (1, (1, 1), 16, 16, "half", "bf16"), (33, (5, 3), 80, 48, "interleaved", "bf16"), (7, (1, 2), 20, 6, "half", "f32")])
+def test_gradients_without_eps(n, heads, D, rot, layout, dtype):
+    """eps = 0 and no head of zeroes: groups of lanes that have no head in a block's last step stay out of the weights' sums."""
+    q, k, pos, r, angle, amp = setup(n, heads, D, rot, layout, None, dtype, seed=5)
+    gq, gk = rand(q.shape, 11, dtype), rand(k.shape, 12, dtype)
+    w = [1 + 0.3 * rand((D,), 7), 1 + 0.3 * rand((D,), 8)]
+    got = r.rotate_qk_grad(gq, gk, q, k, pos.cuda(), jd.HeadNorm(*w, eps=0.0))
+    for name, g, x, wt in (("q", gq, q, w[0]), ("k", gk, k, w[1])):
+        g, x, wt = L.f64(g), L.f64(x), L.f64(wt)
+        dx, dw = S.heads_grad(g, x, wt, 0.0, angle, layout, amp)
+        bx, bw = grad_bounds(g, x, wt, 0.0, amp, dtype, dx)
+        assert (np.abs(L.f64(got[name]) - dx) <= bx).all()
+        assert (np.abs(L.f64(got[name + "_weight"]) - dw) <= bw).all()
