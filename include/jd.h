@@ -320,7 +320,8 @@ typedef struct {
 /* Speculative sampling from probabilities that are there already, of chains and trees, by random numbers that are given. From node 0 on, with
  * w = the target's weights, W = 1, q = the draft's and Q = 1, a node's children are tried in the order of their numbers: token x is accepted
  * where u W q(x) < w(x) Q (or its judge score exceeds tau, by mode), and the walk goes on at that child; else w becomes max(0, w Q - W q) and W its
- * sum, and of distinct siblings q(x) becomes 0 and Q less by it. Where no child is left the next token is the first whose running sum of w
+ * sum, and of distinct siblings q(x) becomes 0 and Q what is left of q: less by q(x) while that is half or more, from then on the sum of q. Once W or Q
+ * is 0 a sibling leaves w as it is. Where no child is left the next token is the first whose running sum of w
  * exceeds u W; with JD_RESAMPLE_TARGET_P, and where w is zero, of the target's own weights. A row without mass gives V - 1. Probabilities are taken
  * as they are (finite, not negative; sums need not be 1), all arithmetic is float64. Asynchronous on the stream; uses the current device; no
  * workspace. */

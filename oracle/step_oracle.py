@@ -67,7 +67,7 @@ def verify(p, q, tokens, accept_u, sample_u, parents=None, judged=None, mode="st
             status = status or BAD_INDEX
     at, path = 0, []
     while True:
-        w, W, Q = p[at].copy(), 1.0, 1.0
+        w, W, Q, summed = p[at].copy(), 1.0, 1.0, False
         d = q[at].copy() if children[at] else None
         for i in children[at]:
             x = int(tokens[i - 1])
@@ -78,11 +78,15 @@ def verify(p, q, tokens, accept_u, sample_u, parents=None, judged=None, mode="st
                 path.append(i)
                 at = i
                 break
+            if not (W > 0 and Q > 0):          # nothing to take, or to take from
+                continue
             w = np.maximum(0.0, w * Q - W * d)
             W = w.sum()
             if distinct and inside:
                 Q -= d[x]
                 d[x] = 0.0
+                summed = summed or Q < 0.5     # a row's own rounding is no longer small beside what is left
+                Q = d.sum() if summed else Q
         else:
             break
     if resample == "target_p" or w.sum() == 0:

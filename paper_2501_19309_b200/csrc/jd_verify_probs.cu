@@ -2,8 +2,10 @@
 //
 // The walk stands at a node, first the last context token. With w = the target's weights there, W = 1, q = the draft's and Q = 1, its children
 // are tried in order: x is accepted where u W q(x) < w(x) Q, and the walk goes on at that child; else
-//     w <- max(0, w Q - W q),   W <- sum w,   distinct siblings: q(x) <- 0, Q <- Q - q(x).
-// (W and Q are what w and q would be divided by.) Where no child is left the next token is the first whose running sum of w exceeds u W. Only a
+//     w <- max(0, w Q - W q),   W <- sum w,   distinct siblings: q(x) <- 0, Q <- what is left of q.
+// (W and Q are what w and q would be divided by.) What is left is 1 - the rejected tokens' q as long as that is half of the row: a row of stored weights adds up to 1 within half
+// a step of their type, so Q is off by a step at most. A confident draft leaves less than that rounding: there Q is summed, by the pass that sums w. Where nothing
+// is left of either, a sibling leaves w as it is. Where no child is left the next token is the first whose running sum of w exceeds u W. Only a
 // node where something was rejected, and the last one, cost a pass over their rows; all other tests are single entries.
 //
 // Latency bounds the small calls and the rows' bytes the large ones. A thread-block cluster takes a sequence: the threads of each block fetch the
@@ -70,10 +72,11 @@ struct Rejections {                        // of the node that the walk stands a
   int x[kMaxNodes];                        // distinct siblings: the token; -1: none
 };
 __device__ __forceinline__ double positive(double x) { return x > 0.0 ? x : 0.0; }
-// What is left of the lane's entries v .. after n rejections.
+// w Q - W q, both products rounded alike: of the last token that is left of either nothing stays.
+__device__ __forceinline__ double less(double w, double Q, double W, double q) { return positive(__dsub_rn(__dmul_rn(w, Q), __dmul_rn(W, q))); }
+// What is left of the lane's entries v .. after n rejections; d: of the draft's, the last rejected token among them still.
 template <typename T, int kW>
-__device__ __forceinline__ void weights_of(const Rejections& r, bool distinct, int n, const uint4& x, const uint4& y, int v, double* w) {
-  double d[kW];
+__device__ __forceinline__ void weights_of(const Rejections& r, bool distinct, int n, const uint4& x, const uint4& y, int v, double* w, double* d) {
 #pragma unroll
   for (int e = 0; e < kW; ++e) {
     d[e] = entry<T>(y, e);
@@ -86,7 +89,7 @@ __device__ __forceinline__ void weights_of(const Rejections& r, bool distinct, i
 #pragma unroll
     for (int e = 0; e < kW; ++e) {
       if (gone == e) d[e] = 0.0;
-      w[e] = positive(w[e] * Q - W * d[e]);
+      w[e] = less(w[e], Q, W, d[e]);
     }
   }
 }
@@ -140,6 +143,7 @@ __device__ __forceinline__ bool wait_cluster(uint32_t barrier, uint32_t parity) 
 struct WalkState {
   int cur, last, len, rejected;
   bool ended, drawing, lost;               // no child left; the weights of the draw have been summed; a block's sum did not come
+  bool sum_left;                           // Q is summed
   double W, Q, total;
 };
 
@@ -176,8 +180,8 @@ __global__ void __launch_bounds__(kThreads, 2) verify_probs_kernel(const __grid_
   __shared__ uint8_t s_judge[kMaxNodes], s_first[kMaxNodes];      // by the judge; as a first child
   __shared__ Rejections s_rej;
   __shared__ WalkState s_walk;
-  __shared__ double s_warp[kWarps], s_part[kWarps][kParts], s_step[kWarps], s_goal;
-  __shared__ __align__(8) double s_block[2][kMaxCluster];
+  __shared__ double s_warp[kWarps], s_left[kWarps], s_part[kWarps][kParts], s_step[kWarps], s_goal;
+  __shared__ __align__(8) double s_block[2][kMaxCluster], s_block_left[2][kMaxCluster];
   __shared__ __align__(8) uint64_t s_arrived[2];
   __shared__ int s_pass, s_at, s_begin;    // s_pass: weights after that many rejections are to be summed; < 0: the draw; < -1: given up
   int rank, blocks;
@@ -223,7 +227,7 @@ __global__ void __launch_bounds__(kThreads, 2) verify_probs_kernel(const __grid_
     s_token[tid] = x;
     s_parent[tid] = parent;
   }
-  if (tid == 0) s_walk = WalkState{0, 0, 0, 0, false, false, false, 1.0, 1.0, 0.0};
+  if (tid == 0) s_walk = WalkState{0, 0, 0, 0, false, false, false, false, 1.0, 1.0, 0.0};
   __syncthreads();
 
   const int v0 = (rank * kWarps + warp) * p.range, v1 = min(v0 + p.range, p.V);   // this warp's stretch
@@ -268,7 +272,7 @@ __global__ void __launch_bounds__(kThreads, 2) verify_probs_kernel(const __grid_
             double w = s_p[next];
 #pragma unroll 1
             for (int j = 0; j < x.rejected; ++j) {
-              w = positive(w * s_rej.Q[j] - s_rej.W[j] * d);
+              w = less(w, s_rej.Q[j], s_rej.W[j], d);
               if (p.distinct && token == s_rej.x[j]) d = 0.0;
             }
             ok = token >= 0 && ((p.mode != JD_MODE_JUDGE && (double)s_u[next] * x.W * d < w * x.Q) || s_judge[next]);
@@ -279,19 +283,24 @@ __global__ void __launch_bounds__(kThreads, 2) verify_probs_kernel(const __grid_
             x.cur = next;
             x.W = x.Q = 1.0;
             x.rejected = 0;
+            x.sum_left = false;
             continue;
           }
+          if (!(x.W > 0.0 && x.Q > 0.0)) continue;     // nothing to take, or to take from
           __syncwarp();
           if (lane == 0) { s_rej.W[x.rejected] = x.W; s_rej.Q[x.rejected] = x.Q; s_rej.x[x.rejected] = token; }
           want = ++x.rejected;
-          if (p.distinct) x.Q -= d;
+          if (p.distinct) {
+            x.Q -= d;
+            x.sum_left |= x.Q < 0.5;
+          }
           x.ended = false;
           break;
         }
         if (x.ended) {                     // what the draw goes by: the rest after the last rejection, summed already, or the target's own weights
           const bool rest = x.rejected > 0 && x.W > 0.0 && p.resample == JD_RESAMPLE_RESIDUAL;
           if (rest) x.drawing = true;
-          else { x.rejected = 0; want = 0; }
+          else { x.rejected = 0; want = 0; x.sum_left = false; }
         }
       } else {
         x.drawing = true;
@@ -310,12 +319,13 @@ __global__ void __launch_bounds__(kThreads, 2) verify_probs_kernel(const __grid_
     const int node = s_walk.cur;
     const T* prow = target + node * p.target_stride;
     const T* qrow = draft + node * p.draft_stride;
-    double sum = 0.0;                      // of the warp
+    const bool sum_left = s_walk.sum_left;
+    double sum = 0.0, left = 0.0;          // of the warp; of the lane
 #pragma unroll 1
     for (int w0 = v0, i = 0; w0 < v1; w0 += p.part, ++i) {
       const int w1 = min(w0 + p.part, v1);
       double part = 0.0;
-      if (n <= 1) {                        // of no rejection: q = 0
+      if (n <= 1 && !sum_left) {           // of no rejection: q = 0
         uint4 x[2], y[2];
         auto fetch = [&](int v) {
 #pragma unroll
@@ -345,32 +355,47 @@ __global__ void __launch_bounds__(kThreads, 2) verify_probs_kernel(const __grid_
           const uint4 a = x, d = y;
           x = load_entries<T, kVec>(prow, v + kStep, w1);
           y = load_entries<T, kVec>(qrow, v + kStep, w1);
-          double w[kW];
-          weights_of<T, kW>(s_rej, p.distinct, n, a, d, v, w);
+          double w[kW], of_q[kW];
+          weights_of<T, kW>(s_rej, p.distinct, n, a, d, v, w, of_q);
+          const int gone = s_rej.x[n - 1] - v;
 #pragma unroll
-          for (int e = 0; e < kW; ++e) part += w[e];
+          for (int e = 0; e < kW; ++e) {
+            part += w[e];
+            if (gone != e) left += of_q[e];
+          }
         }
       }
       part = warp_sum_double(part);
       if (lane == 0) s_part[warp][i] = part;
       sum += part;
     }
-    if (lane == 0) s_warp[warp] = sum;
+    if (sum_left) left = warp_sum_double(left);
+    if (lane == 0) { s_warp[warp] = sum; s_left[warp] = left; }
     if (pass == 0) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");   // every block has begun, its barriers are there
     __syncthreads();
     if (warp == 0) {
       // Buffers and barriers in turn: a block sends its sum of the next pass when it has every sum of this one.
       const uint32_t barrier = smem_u32(&s_arrived[pass & 1]);
-      if (lane == 0) mbar_expect_tx(barrier, 8 * blocks);
+      if (lane == 0) mbar_expect_tx(barrier, (sum_left ? 16 : 8) * blocks);
       const double s = warp_sum_double(lane < kWarps ? s_warp[lane] : 0.0);
       __syncwarp();
       if (lane < blocks) send(in_block(smem_u32(&s_block[pass & 1][rank]), lane), s, in_block(barrier, lane));
+      if (sum_left) {
+        const double q = warp_sum_double(lane < kWarps ? s_left[lane] : 0.0);
+        if (lane < blocks) send(in_block(smem_u32(&s_block_left[pass & 1][rank]), lane), q, in_block(barrier, lane));
+      }
       unsigned it = 0;
       bool lost = false;
       while (!wait_cluster(barrier, (pass >> 1) & 1) && !lost) lost = ++it >= kSpinLimit;
       double all = lane < blocks ? s_block[pass & 1][lane] : 0.0;
 #pragma unroll
       for (int o = kMaxCluster / 2; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+      if (sum_left) {
+        double rest = lane < blocks ? s_block_left[pass & 1][lane] : 0.0;
+#pragma unroll
+        for (int o = kMaxCluster / 2; o > 0; o >>= 1) rest += __shfl_xor_sync(0xffffffffu, rest, o);
+        if (lane == 0) s_walk.Q = rest;
+      }
       if (lane == 0) {
         s_walk.W = all;
         s_walk.lost = lost;
@@ -414,12 +439,12 @@ __global__ void __launch_bounds__(kThreads, 2) verify_probs_kernel(const __grid_
   const int begin = s_begin, end = min((int)min((int64_t)begin + p.part, (int64_t)(begin / p.range + 1) * p.range), p.V);
   double goal = s_goal, last_goal = goal;
   int found = -1, last_found = begin;
-  double w[kW], of_lane = 0.0;
+  double w[kW], of_q[kW], of_lane = 0.0;
   int held = -1;                           // the step that this warp has in hand
   auto take_step = [&](int v) {
     const int at = v + lane * kW;
     const uint4 x = load_entries<T, kVec>(prow, at, end), y = n > 0 ? load_entries<T, kVec>(qrow, at, end) : make_uint4(0u, 0u, 0u, 0u);
-    weights_of<T, kW>(s_rej, p.distinct, n, x, y, at, w);
+    weights_of<T, kW>(s_rej, p.distinct, n, x, y, at, w, of_q);
     of_lane = 0.0;
 #pragma unroll
     for (int e = 0; e < kW; ++e) of_lane += w[e];

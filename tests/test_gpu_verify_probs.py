@@ -220,3 +220,52 @@ def test_refusals():
     big, q, tok, u = torch.ones(1, 130, 4, device="cuda"), torch.ones(1, 129, 4, device="cuda"), torch.zeros(1, 129, dtype=torch.int32, device="cuda"), torch.zeros(1, 129, device="cuda")
     with pytest.raises(jd.JdError):
         jd.verify_probs(big, q, tok, u, torch.zeros(1, device="cuda"))
+
+
+# ------------------------------------------------------------------------------------------- confident drafts
+def confident(which, dtype):
+    """(target, draft) rows of four tokens."""
+    logits = torch.tensor([20., 0, 0.5, -1] if which == 1 else [20., 19, 0.5, -1])
+    draft = torch.softmax(logits, 0) if which in (1, 2) else torch.tensor({.9: [.9, .04, .03, .03], .99: [.99, .004, .003, .003], .999: [.999, .0004, .0003, .0003]}[which])
+    return torch.tensor([.5, .2, .2, .1]).to(L.DT[dtype]), draft.to(L.DT[dtype])
+
+
+def siblings_of(p, q, B, n, seed):
+    """B stars of n siblings drawn from q without replacement."""
+    gen = torch.Generator().manual_seed(seed)
+    keys = q.double().log() - torch.empty(B, len(q), dtype=torch.float64).exponential_(generator=gen).log()
+    s = dict(target=p.expand(B, n + 1, len(p)), draft=q.expand(B, n, len(q)), tokens=keys.topk(n, 1).indices.to(torch.int32), accept_u=torch.rand(B, n, generator=gen),
+             sample_u=torch.rand(B, generator=gen), judge_scores=torch.rand(B, n, generator=gen))
+    return {k: v.contiguous().cuda() for k, v in s.items()}, np.array([[-1] + [0] * n] * B)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [2, 3, 4])
+@pytest.mark.parametrize("which", [1, 2, .9, .99, .999])
+def test_distinct_siblings_of_a_confident_draft(which, n, dtype):
+    p, q = confident(which, dtype)
+    s, parents = siblings_of(p, q, 1500, n, seed=n)
+    for mode in MODES:
+        check(s, parents, call(s, parents, siblings="distinct", mode=mode, tau=0.7), siblings="distinct", mode=mode, tau=0.7)
+
+
+@pytest.mark.parametrize("n", [2, 3, 4])
+@pytest.mark.parametrize("which", [1, 2, .9, .99, .999])
+def test_the_targets_law_behind_a_confident_draft(which, n):
+    """60,000 sequences, float32 rows whose sums are 1 within 2^-23: chi^2 of 3 degrees of freedom is above 41 once in 10^8 runs."""
+    p, q = confident(which, "f32")
+    s, parents = siblings_of(p, q, 60000, n, seed=10 + n)
+    got = jd.verify_probs(s["target"], s["draft"], s["tokens"], s["accept_u"], s["sample_u"], parents=L.ints(parents[0]), siblings="distinct")
+    first = got["path"][:, 0].long()
+    emitted = torch.where(first > 0, s["tokens"].gather(1, (first - 1).clamp(min=0)[:, None])[:, 0], got["next_token"])
+    count, want = torch.bincount(emitted.long(), minlength=4).double().cpu(), p.double() / p.double().sum() * 60000
+    assert float(((count - want) ** 2 / want).sum()) < 41
+
+
+@pytest.mark.parametrize("V,dtype", [(5000, "f32"), (33001, "f32"), (5000, "bf16")])
+def test_confident_rows_of_a_vocabulary(V, dtype):
+    """Rows that put 0.9 to 1 on a token: chains, and trees whose nodes have several children."""
+    for seed, style in enumerate(("tree", "star", "chain")):
+        s, parents = inputs(40, 9, V, dtype, seed, style, sharp=8.0)
+        for siblings in ("independent", "distinct"):
+            check(s, parents, call(s, parents, chain=style == "chain", siblings=siblings), siblings=siblings)

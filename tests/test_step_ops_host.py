@@ -242,3 +242,83 @@ def test_model_reports_and_falls_back():
     assert S.verify(p, q, [0], [0.0], 0.99) == ([1], 0, S.OK)
     assert S.verify(p, q, [0], [0.0], 0.99, mode="judge", judged=[False]) == ([], 1, S.OK)
     assert S.verify(np.zeros((1, 3)), np.zeros((0, 3)), [], [], 0.5) == ([], 2, S.OK)
+
+
+# ------------------------------------------------------------------------------------------- rows as they are stored
+def _stored(x, dtype):
+    """Float64 values of what float32 or bfloat16 holds of x."""
+    return torch.as_tensor(np.asarray(x), dtype=torch.float64).to({"f32": torch.float32, "bf16": torch.bfloat16}[dtype]).double().numpy()
+
+
+def _stored_softmax(z, dtype):
+    return _stored(torch.softmax(torch.as_tensor(np.asarray(z), dtype=torch.float32), 0).numpy(), dtype)
+
+
+def _edge(holds):
+    """The number of [0, 1] up to which holds(u) is true, by halving."""
+    lo, hi = 0.0, 1.0
+    if not holds(lo):
+        return 0.0
+    for _ in range(40):
+        mid = (lo + hi) / 2
+        lo, hi = (mid, hi) if holds(mid) else (lo, mid)
+    return hi
+
+
+def _law_of_the_model(p, q, children, distinct):
+    """The law of the first emitted token by the model's own decisions: siblings drawn from the row as a sampler draws them, from what is left over its sum, and
+    the borders of every number's interval found by halving."""
+    V, T, law = len(p), children + 1, np.zeros(len(p))
+    P, D, below = np.tile(p, (T, 1)), np.tile(q, (T - 1, 1)), 1 - 2.0 ** -24
+
+    def emitted(prob, tokens):
+        u = [below] * children
+        for i in range(children):
+            def taken(x):
+                return S.verify(P, D, tokens, u[:i] + [x] + u[i + 1:], 0.5, parents=[-1] + [0] * children, distinct=distinct)[0] == [i + 1]
+            accept = _edge(taken)
+            law[tokens[i]] += prob * accept
+            prob *= 1 - accept
+            if accept > below:
+                return
+        edges = [0.0] + [_edge(lambda x: S.verify(P, D, tokens, u, x, parents=[-1] + [0] * children, distinct=distinct)[1] <= v) for v in range(V)]
+        law[:] += prob * np.diff(edges)
+
+    def drawn(prob, tokens, d):
+        if len(tokens) == children:
+            return emitted(prob, tokens)
+        for x in range(V):
+            if d[x] > 0:
+                left = d.copy()
+                if distinct:
+                    left[x] = 0
+                drawn(prob * d[x] / d.sum(), tokens + [x], left)
+
+    drawn(1.0, [], q.copy())
+    return law
+
+
+CONFIDENT = [  # the draft's row and its type: one token holds what the type rounds to 1, or nearly all; two hold all; none does
+    (_stored_softmax([20, 0, 0.5, -1], "f32"), "float32, 1 as stored"), (_stored([.9, .04, .03, .03], "f32"), "float32, .9"),
+    (_stored([.99, .004, .003, .003], "f32"), "float32, .99"), (_stored_softmax([20, 19, 0.5, -1], "f32"), "float32, two tokens"),
+    (_stored([.9, .04, .03, .03], "bf16"), "bf16, .9"), (_stored([.99, .004, .003, .003], "bf16"), "bf16, .99"), (_stored([.999, .0004, .0003, .0003], "bf16"), "bf16, .999"),
+    (_stored([.55, .44, .006, .004], "bf16"), "bf16, two tokens"), (_stored([.4, .3, .2, .1], "bf16"), "bf16, flat")]
+
+
+@pytest.mark.parametrize("distinct", [False, True])
+@pytest.mark.parametrize("children", [2, 3, 4])
+@pytest.mark.parametrize("row", [r for r, _ in CONFIDENT], ids=[n for _, n in CONFIDENT])
+def test_the_targets_law_behind_confident_drafts(row, children, distinct):
+    """With e = how far the rows' sums are from 1: acceptances and what is left after the first rejection are off by 2 e in all; a later sibling's by the error of what is taken
+    for the rest of the draft's row, at most 2 e of it (subtracted from 1, half of the row is left at least; else it is the sum). Halving and numbers that end below 1: 10^-6."""
+    p = _stored([.5, .2, .2, .1], "f32")
+    e = abs(row.sum() - 1) + abs(p.sum() - 1)
+    law = _law_of_the_model(p, row, children, distinct)
+    assert np.abs(law - p).max() <= (2 + 4 * (children - 1)) * e + 1e-6
+
+
+def test_siblings_of_a_draft_that_has_nothing_left():
+    """One token holds the whole row: the rest of the row is nothing, and what it was sampled from cannot reject the target's weights a second time."""
+    p, q = np.array([[.5, .3, .2]] * 4), np.array([[1., 0., 0.]] * 3)
+    for u, want in ((0.1, 1), (0.59, 1), (0.61, 2), (0.9, 2)):                    # p without token 0: (0, .6, .4)
+        assert S.verify(p, q, [0, 1, 2], [0.6, 0.999, 0.999], u, parents=[-1, 0, 0, 0], distinct=True) == ([], want, S.OK)
