@@ -81,6 +81,8 @@ def verify(p, q, tokens, accept_u, sample_u, parents=None, judged=None, mode="st
             if not (W > 0 and Q > 0):          # nothing to take, or to take from
                 continue
             w = np.maximum(0.0, w * Q - W * d)
+            e = np.frexp(w.sum())[1]           # kept near 1: the products would leave float64
+            w = np.ldexp(w, -e)
             W = w.sum()
             if distinct and inside:
                 Q -= d[x]

@@ -5,7 +5,8 @@
 //     w <- max(0, w Q - W q),   W <- sum w,   distinct siblings: q(x) <- 0, Q <- what is left of q.
 // (W and Q are what w and q would be divided by.) What is left is 1 - the rejected tokens' q as long as that is half of the row: a row of stored weights adds up to 1 within half
 // a step of their type, so Q is off by a step at most. A confident draft leaves less than that rounding: there Q is summed, by the pass that sums w. Where nothing
-// is left of either, a sibling leaves w as it is. Where no child is left the next token is the first whose running sum of w exceeds u W. Only a
+// is left of either, a sibling leaves w as it is. The products of W and Q on the way would leave float64 behind some 80 siblings of a confident draft: each pair is taken times the
+// power of two that brings both near 1, which rounds nothing, so that a step's sum is what the step itself leaves. Where no child is left the next token is the first whose running sum of w exceeds u W. Only a
 // node where something was rejected, and the last one, cost a pass over their rows; all other tests are single entries.
 //
 // Latency bounds the small calls and the rows' bytes the large ones. A thread-block cluster takes a sequence: the threads of each block fetch the
@@ -68,9 +69,11 @@ template <typename T> __device__ __forceinline__ float entry(const uint4& r, int
 }
 
 struct Rejections {                        // of the node that the walk stands at
-  double W[kMaxNodes], Q[kMaxNodes];       // in front of each
+  double W[kMaxNodes], Q[kMaxNodes];       // in front of each, times a power of two
   int x[kMaxNodes];                        // distinct siblings: the token; -1: none
 };
+// 2^-e of x = m 2^e, m from 1 to 2
+__device__ __forceinline__ double to_one(double x) { return __hiloint2double(0x7FE00000 - (__double2hiint(x) & 0x7FF00000), 0); }
 __device__ __forceinline__ double positive(double x) { return x > 0.0 ? x : 0.0; }
 // w Q - W q, both products rounded alike: of the last token that is left of either nothing stays.
 __device__ __forceinline__ double less(double w, double Q, double W, double q) { return positive(__dsub_rn(__dmul_rn(w, Q), __dmul_rn(W, q))); }
@@ -288,7 +291,12 @@ __global__ void __launch_bounds__(kThreads, 2) verify_probs_kernel(const __grid_
           }
           if (!(x.W > 0.0 && x.Q > 0.0)) continue;     // nothing to take, or to take from
           __syncwarp();
-          if (lane == 0) { s_rej.W[x.rejected] = x.W; s_rej.Q[x.rejected] = x.Q; s_rej.x[x.rejected] = token; }
+          if (lane == 0) {
+            const double f = to_one(x.W) * to_one(x.Q);
+            s_rej.W[x.rejected] = x.W * f;
+            s_rej.Q[x.rejected] = x.Q * f;
+            s_rej.x[x.rejected] = token;
+          }
           want = ++x.rejected;
           if (p.distinct) {
             x.Q -= d;

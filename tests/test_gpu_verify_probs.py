@@ -269,3 +269,26 @@ def test_confident_rows_of_a_vocabulary(V, dtype):
         s, parents = inputs(40, 9, V, dtype, seed, style, sharp=8.0)
         for siblings in ("independent", "distinct"):
             check(s, parents, call(s, parents, chain=style == "chain", siblings=siblings), siblings=siblings)
+
+
+@pytest.mark.parametrize("siblings", ["independent", "distinct"])
+def test_many_rejections_leave_the_rest_of_the_target(siblings):
+    """127 siblings of confident rows, all rejected: the products of what is left on the way are far below float64's smallest number."""
+    rng = np.random.default_rng(5)
+    V, n, B = 2000, 127, 24
+    p, q = (torch.softmax(torch.as_tensor(12 * rng.normal(size=V)), 0).numpy() for _ in range(2))
+    tokens = np.argsort(-(np.log(q) + rng.gumbel(size=V)))[:n]
+    left = q.copy()
+    for x in tokens:
+        p[x] = left[x] / left.sum() / 250
+        left[x] = 0
+    other = np.setdiff1d(np.arange(V), tokens)
+    p[other] *= (1 - p[tokens].sum()) / p[other].sum()
+    put = lambda x, *shape: torch.as_tensor(x, dtype=torch.float32, device="cuda").expand(*shape).contiguous()   # noqa: E731
+    s = dict(target=put(p, B, n + 1, V), draft=put(q, B, n, V), tokens=L.ints(np.tile(tokens, (B, 1))), accept_u=put(0.999, B, n), sample_u=put(np.linspace(0.001, 0.999, B), B),
+             judge_scores=put(0.0, B, n))
+    parents = np.array([[-1] + [0] * n] * B)
+    got = call(s, parents, siblings=siblings)
+    check(s, parents, got, siblings=siblings)
+    if siblings == "distinct":
+        assert not np.isin(got["next_token"].cpu().numpy(), tokens).any()      # the target's own row would give some of them

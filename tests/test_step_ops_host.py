@@ -322,3 +322,37 @@ def test_siblings_of_a_draft_that_has_nothing_left():
     p, q = np.array([[.5, .3, .2]] * 4), np.array([[1., 0., 0.]] * 3)
     for u, want in ((0.1, 1), (0.59, 1), (0.61, 2), (0.9, 2)):                    # p without token 0: (0, .6, .4)
         assert S.verify(p, q, [0, 1, 2], [0.6, 0.999, 0.999], u, parents=[-1, 0, 0, 0], distinct=True) == ([], want, S.OK)
+
+
+def _shares(p, q, tokens, distinct):
+    """What is left of p after rejections of all tokens, each step divided by its sums."""
+    w, d = p.copy(), q.copy()
+    for x in tokens:
+        if d.sum() > 0 and w.sum() > 0:
+            w = np.maximum(0.0, w / w.sum() - d / d.sum())
+        if distinct:
+            d[x] = 0
+    return w / w.sum()
+
+
+@pytest.mark.parametrize("distinct", [False, True])
+def test_many_rejections_leave_the_rest_of_the_target(distinct):
+    """127 siblings of confident rows, all rejected: what is left keeps its size, however small the products of what was left on the way."""
+    rng = np.random.default_rng(5)
+    V, n = 2000, 127
+    p, q = (_stored_softmax(12 * rng.normal(size=V), "f32") for _ in range(2))
+    tokens = np.argsort(-(np.log(np.maximum(q, 1e-300)) + rng.gumbel(size=V)))[:n] if distinct else rng.choice(V, size=n, p=q / q.sum())
+    left = q.copy()
+    for x in tokens:                                                              # rejected: the target's weight is 1/250 of the draft's there
+        p[x] = left[x] / left.sum() / 250
+        if distinct:
+            left[x] = 0
+    other = np.setdiff1d(np.arange(V), tokens)
+    p[other] *= (1 - p[tokens].sum()) / p[other].sum()
+    run = np.cumsum(_shares(p, q, tokens, distinct))
+    us = np.linspace(0.001, 0.999, 41)
+    got = [S.verify(np.tile(p, (n + 1, 1)), np.tile(q, (n, 1)), tokens, [0.999] * n, u, parents=[-1] + [0] * n, distinct=distinct) for u in us]
+    assert all(path == [] for path, _, _ in got)
+    # sums in another order and rows whose sum is off 1 by 2^-23 move a border between tokens by some 10^-6
+    for u, (_, token, _) in zip(us, got):
+        assert token in {int(np.searchsorted(run, x, side="right")) for x in (u - 1e-5, u, u + 1e-5)}
