@@ -323,7 +323,8 @@ typedef struct {
  * sum, and of distinct siblings q(x) becomes 0 and Q what is left of q: less by q(x) while that is half or more, from then on the sum of q. Once W or Q
  * is 0 a sibling leaves w as it is. Where no child is left the next token is the first whose running sum of w
  * exceeds u W; with JD_RESAMPLE_TARGET_P, and where w is zero, of the target's own weights. A row without mass gives V - 1. Probabilities are taken
- * as they are (finite, not negative; sums need not be 1), all arithmetic is float64. Asynchronous on the stream; uses the current device; no
+ * as they are (finite, not negative; sums need not be 1). Arithmetic is float64; the sums of a row behind up to one rejection are pairs of float32, off
+ * by some 2^-48, unless float32 does not hold them. Asynchronous on the stream; uses the current device; no
  * workspace. */
 jd_status_t jd_verify_probs(const jd_verify_probs_args_t* args, void* cuda_stream);
 

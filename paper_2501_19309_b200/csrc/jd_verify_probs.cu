@@ -6,7 +6,7 @@
 // (W and Q are what w and q would be divided by.) What is left is 1 - the rejected tokens' q as long as that is half of the row: a row of stored weights adds up to 1 within half
 // a step of their type, so Q is off by a step at most. A confident draft leaves less than that rounding: there Q is summed, by the pass that sums w. Where nothing
 // is left of either, a sibling leaves w as it is. The products of W and Q on the way would leave float64 behind some 80 siblings of a confident draft: each pair is taken times the
-// power of two that brings both near 1, which rounds nothing, so that a step's sum is what the step itself leaves. Where no child is left the next token is the first whose running sum of w exceeds u W. Only a
+// power of two that brings their product near 1, which rounds nothing, so that a step's sum is what the step itself leaves. Where no child is left the next token is the first whose running sum of w exceeds u W. Only a
 // node where something was rejected, and the last one, cost a pass over their rows; all other tests are single entries.
 //
 // Latency bounds the small calls and the rows' bytes the large ones. A thread-block cluster takes a sequence: the threads of each block fetch the
@@ -16,7 +16,8 @@
 // and lane. Loops are kept small: code that a block runs once or twice is fetched line by line, and unrolled eight times over it took longer than its work
 // (16 trees of 25 drafted tokens, vocabulary 128,256: 40 us, 23 so). 64 chains of 16: 20 to 22 us, where the rows' bytes take 10; one chain of 8: 11 us, of which the
 // fetches and the first tests take 2, the pass 3, the sums' way through the cluster and the draw 3.
-// Sums are float64: a token of 10^-6 is to be told from its neighbour behind 10^5 others, and so every launch shape finds the same one.
+// A token of 10^-6 is to be told from its neighbour behind 10^5 others, and every launch shape is to find the same one: sums are float64, or, behind up to one rejection,
+// pairs of float32 that are off by some 2^-48 (LongSum); a pass whose sum float32 does not hold is taken again in float64.
 #include <algorithm>
 #include <cmath>
 
@@ -146,7 +147,7 @@ __device__ __forceinline__ bool wait_cluster(uint32_t barrier, uint32_t parity) 
 struct WalkState {
   int cur, last, len, rejected;
   bool ended, drawing, lost;               // no child left; the weights of the draw have been summed; a block's sum did not come
-  bool sum_left;                           // Q is summed
+  bool sum_left, wide;                     // Q is summed; float32 has not held a sum
   double W, Q, total;
 };
 
@@ -230,7 +231,7 @@ __global__ void __launch_bounds__(kThreads, 2) verify_probs_kernel(const __grid_
     s_token[tid] = x;
     s_parent[tid] = parent;
   }
-  if (tid == 0) s_walk = WalkState{0, 0, 0, 0, false, false, false, false, 1.0, 1.0, 0.0};
+  if (tid == 0) s_walk = WalkState{0, 0, 0, 0, false, false, false, false, false, 1.0, 1.0, 0.0};
   __syncthreads();
 
   const int v0 = (rank * kWarps + warp) * p.range, v1 = min(v0 + p.range, p.V);   // this warp's stretch
@@ -238,7 +239,10 @@ __global__ void __launch_bounds__(kThreads, 2) verify_probs_kernel(const __grid_
     if (warp == 0) {                       // the walk goes on, alike in all lanes; every block's takes the same steps
       WalkState x = s_walk;
       int want = -1;
-      if (!x.ended && !p.parents && pass == 0) {   // a chain: up to its first rejection at once
+      if (!x.wide && !(x.W < INFINITY)) {  // the same pass again, in float64
+        x.wide = true;
+        want = x.rejected;
+      } else if (!x.ended && !p.parents && pass == 0) {   // a chain: up to its first rejection at once
         int stop = nodes;
 #pragma unroll 1
         for (int k = (nodes - 1) >> 5; k >= 0; --k) {
@@ -327,13 +331,13 @@ __global__ void __launch_bounds__(kThreads, 2) verify_probs_kernel(const __grid_
     const int node = s_walk.cur;
     const T* prow = target + node * p.target_stride;
     const T* qrow = draft + node * p.draft_stride;
-    const bool sum_left = s_walk.sum_left;
+    const bool sum_left = s_walk.sum_left, in_double = n > 1 || sum_left || s_walk.wide;
     double sum = 0.0, left = 0.0;          // of the warp; of the lane
 #pragma unroll 1
     for (int w0 = v0, i = 0; w0 < v1; w0 += p.part, ++i) {
       const int w1 = min(w0 + p.part, v1);
       double part = 0.0;
-      if (n <= 1 && !sum_left) {           // of no rejection: q = 0
+      if (!in_double) {                    // of no rejection: q = 0
         uint4 x[2], y[2];
         auto fetch = [&](int v) {
 #pragma unroll
@@ -365,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, 2) verify_probs_kernel(const __grid_
           y = load_entries<T, kVec>(qrow, v + kStep, w1);
           double w[kW], of_q[kW];
           weights_of<T, kW>(s_rej, p.distinct, n, a, d, v, w, of_q);
-          const int gone = s_rej.x[n - 1] - v;
+          const int gone = n > 0 ? s_rej.x[n - 1] - v : -1;
 #pragma unroll
           for (int e = 0; e < kW; ++e) {
             part += w[e];

@@ -292,3 +292,14 @@ def test_many_rejections_leave_the_rest_of_the_target(siblings):
     check(s, parents, got, siblings=siblings)
     if siblings == "distinct":
         assert not np.isin(got["next_token"].cpu().numpy(), tokens).any()      # the target's own row would give some of them
+
+
+@pytest.mark.parametrize("siblings", ["independent", "distinct"])
+@pytest.mark.parametrize("V,dtype", [(3, "f32"), (1000, "f32"), (70001, "f32"), (5000, "bf16")])
+def test_weights_whose_sum_float32_does_not_hold(V, dtype, siblings):
+    """Finite, not negative, their sums whatever they are."""
+    for seed, style in enumerate(("chain", "star", "tree")):
+        s, parents = inputs(6, 6, V, "f32", seed, style)
+        s["target"], s["draft"] = ((torch.rand(x.shape, generator=torch.Generator().manual_seed(seed + i)) * 3.3e38).to(L.DT[dtype]).cuda() for i, x in enumerate((s["target"], s["draft"])))
+        s["accept_u"] = s["accept_u"] * 0.3 + 0.7
+        check(s, parents, call(s, parents, chain=style == "chain", siblings=siblings), siblings=siblings)
