@@ -221,21 +221,22 @@ class Rotary:
         if weights:
             need = _grad_workspace(dim)
             wq, wk = out.get("q_weight"), out.get("k_weight")
-            if wq is None and wk is None and workspace is None:      # one allocation: both weights' gradients, then the workspace
-                both = q.new_empty((2 * dim + need // 4,), dtype=torch.float32)
-                wq, wk, _ = both.unsafe_split_with_sizes((dim, dim, need // 4))
+            if wq is None and wk is None:      # one allocation for both; the workspace is one of its own, that goes when the call is done
+                both = q.new_empty((2 * dim,), dtype=torch.float32)
+                wq, wk = both.unsafe_split_with_sizes((dim, dim))
                 wq_ptr = both.data_ptr()
-                wk_ptr, work_ptr = wq_ptr + 4 * dim, wq_ptr + 8 * dim
+                wk_ptr = wq_ptr + 4 * dim
             else:
                 wq, wk = (q.new_empty((dim,), dtype=torch.float32) if w is None else w for w in (wq, wk))
                 for w in (wq, wk):
                     if w.shape != (dim,) or w.dtype is not torch.float32 or not w.is_contiguous() or w.get_device() != index or w.requires_grad:
                         raise ValueError("q_weight, k_weight: contiguous float32 vectors [head_dim] on the device")
-                if workspace is None:
-                    workspace = q.new_empty((need,), dtype=torch.uint8)
-                elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.numel() < need or workspace.get_device() != index:
-                    raise ValueError("workspace: %d contiguous bytes (uint8) on the device" % need)
-                wq_ptr, wk_ptr, work_ptr = wq.data_ptr(), wk.data_ptr(), workspace.data_ptr()
+                wq_ptr, wk_ptr = wq.data_ptr(), wk.data_ptr()
+            if workspace is None:
+                workspace = q.new_empty((need,), dtype=torch.uint8)
+            elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.numel() < need or workspace.get_device() != index:
+                raise ValueError("workspace: %d contiguous bytes (uint8) on the device" % need)
+            work_ptr = workspace.data_ptr()
             got["q_weight"], got["k_weight"] = wq, wk
         at = self._positions(positions, index, n)
         a = jd.jd_head_rope_grad_args_t()

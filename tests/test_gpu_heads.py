@@ -299,3 +299,10 @@ def test_gradients_without_eps(n, heads, D, rot, layout, dtype):
         bx, bw = grad_bounds(g, x, wt, 0.0, amp, dtype, dx)
         assert (np.abs(L.f64(got[name]) - dx) <= bx).all()
         assert (np.abs(L.f64(got[name + "_weight"]) - dw) <= bw).all()
+
+
+def test_weight_gradients_hold_no_workspace():
+    """What a program keeps of a call is its gradients, not the room for their partial sums."""
+    q, k, pos, r, _, _ = setup(9, (2, 1), 128, 128, "half", None, "f32")
+    got = r.rotate_qk_grad(q, k, q, k, pos.cuda(), jd.HeadNorm())
+    assert all(got[name].untyped_storage().nbytes() <= 2 * 128 * 4 for name in ("q_weight", "k_weight"))
