@@ -102,6 +102,15 @@ def _grad_workspace(head_dim: int) -> int:
     return need
 
 
+def _scratch(like: torch.Tensor, need: int, index: int, stream) -> torch.Tensor:
+    """Workspace of a call that makes it itself: of the memory of the stream that the call runs on, since the tensor is gone when the call returns and what
+    had its memory before, or has it next, must not run beside the call's kernels."""
+    if stream is None or stream.cuda_stream == _raw_stream(index):
+        return like.new_empty((need,), dtype=torch.uint8)
+    with torch.cuda.stream(stream):
+        return like.new_empty((need,), dtype=torch.uint8)
+
+
 class HeadNorm:
     """RMS norms of query and key heads, x w / sqrt(mean(x ** 2) + eps): weights [head_dim] (float32, on the device; None: ones)."""
 
@@ -233,7 +242,7 @@ class Rotary:
                         raise ValueError("q_weight, k_weight: contiguous float32 vectors [head_dim] on the device")
                 wq_ptr, wk_ptr = wq.data_ptr(), wk.data_ptr()
             if workspace is None:
-                workspace = q.new_empty((need,), dtype=torch.uint8)
+                workspace = _scratch(q, need, index, stream)
             elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.numel() < need or workspace.get_device() != index:
                 raise ValueError("workspace: %d contiguous bytes (uint8) on the device" % need)
             work_ptr = workspace.data_ptr()

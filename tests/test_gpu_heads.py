@@ -306,3 +306,21 @@ def test_weight_gradients_hold_no_workspace():
     q, k, pos, r, _, _ = setup(9, (2, 1), 128, 128, "half", None, "f32")
     got = r.rotate_qk_grad(q, k, q, k, pos.cuda(), jd.HeadNorm())
     assert all(got[name].untyped_storage().nbytes() <= 2 * 128 * 4 for name in ("q_weight", "k_weight"))
+
+
+def test_a_workspace_of_the_call_on_another_stream():
+    """Outputs are given, the workspace is not: what is allocated behind the call must not be memory that its kernels have yet to use."""
+    n, D = 512, 128
+    q, k, pos, r, _, _ = setup(n, (8, 2), D, D, "half", None, "bf16", seed=9)
+    gq, gk, norm, pos = rand(q.shape, 11, "bf16"), rand(k.shape, 12, "bf16"), jd.HeadNorm(1 + 0.3 * rand((D,), 7), 1 + 0.3 * rand((D,), 8)), pos.cuda()
+    want = r.rotate_qk_grad(gq, gk, q, k, pos, norm)
+    out = {name: torch.empty_like(x) for name, x in want.items()}
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(50_000_000)                                      # some 30 ms: the call's kernels run behind what follows
+    assert r.rotate_qk_grad(gq, gk, q, k, pos, norm, out=out, stream=side) == out
+    later = [torch.full((jd.load().jd_head_rope_grad_workspace_bytes(D),), 77, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    torch.cuda.synchronize()
+    assert all(bool((x == 77).all()) for x in later)
+    assert all(torch.equal(out[name], want[name]) for name in want)
