@@ -379,7 +379,16 @@ class SharedPrefix:
         self.B, self.nodes, self.cache = B, nodes, cache
         self.buffer = torch.zeros(need, dtype=torch.uint8, device=cache.device)
         self.c = jd.jd_shared_t(B, nodes, self.buffer.data_ptr(), need)
+        self._streams = set()
         torch.cuda.current_stream(cache.index).synchronize()     # the zeroes are there, whatever stream the first call is on
+
+    def _on(self, stream) -> int:
+        """The stream of a call; the buffer's memory is not handed out before that stream is done with it, should the plan be dropped while it runs."""
+        raw = _stream(stream, self.cache.index)
+        if raw not in self._streams:
+            self.buffer.record_stream(torch.cuda.current_stream(self.cache.index) if stream is None else stream)
+            self._streams.add(raw)
+        return raw
 
 
 class PagedCache:
@@ -559,7 +568,7 @@ class PagedCache:
         else:
             if shared.cache is not self or shared.B != B or shared.nodes < T:
                 raise ValueError("shared: a plan of this cache for %d sequences of %d nodes" % (B, T))
-            st = self._lib.jd_cache_attend_shared(self.h, a, shared.c, _stream(stream, self.index))
+            st = self._lib.jd_cache_attend_shared(self.h, a, shared.c, shared._on(stream))
         if st != jd.JD_OK:
             raise jd.JdError(st, "jd_cache_attend")
         return out
@@ -578,8 +587,7 @@ class PagedCache:
             raise ValueError("plan: of this cache for %d sequences of %d nodes" % (B, nodes))
         _require(rows in (0, 4, 16, 32, 64, 128, 256), "rows: 0, 4, 16, 32, 64, 128 or 256")
         plan.c.rows = rows
-        st = self._lib.jd_cache_share(self.h, plan.c, _ints(slots, "slots", self.index), _ints(groups, "groups", self.index, (B,)),
-                                      _stream(stream, self.index))
+        st = self._lib.jd_cache_share(self.h, plan.c, _ints(slots, "slots", self.index), _ints(groups, "groups", self.index, (B,)), plan._on(stream))
         if st != jd.JD_OK:
             raise jd.JdError(st, "jd_cache_share")
         return plan

@@ -377,3 +377,30 @@ def test_more_work_than_the_division_counts():
     assert shares(plan) and c.status() == jd.JD_OK
     got, want = c.attend(0, q, slots=slots, shared=plan), c.attend(0, q, slots=slots)
     assert torch.equal(got["out"], want["out"]) and torch.equal(got["lse"], want["lse"]) and torch.isfinite(want["out"]).all()
+
+
+def test_a_plan_that_is_dropped_while_its_calls_run():
+    """What is allocated behind the calls must not be the plan's memory as long as another stream's kernels have yet to use it."""
+    c, slots = forked([1200], [6], [30] * 6, 3, q_heads=8, kv_heads=2, D=128)
+    tree, _ = tree_of(3, 2)
+    q, side = rand((6, 3, 8, 128), 5), torch.cuda.Stream()
+    want = c.attend(0, q, tree, slots=slots)
+    for given in (True, False):                    # as an argument, and as the current stream of the calls
+        out = {name: torch.empty_like(x) for name, x in want.items()}
+        plan = c.share(3, rows=128, slots=slots)
+        need = plan.buffer.numel()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(50_000_000)          # some 30 ms
+            if not given:
+                c.attend(0, q, tree, slots=slots, shared=plan, out=out)
+        if given:
+            c.share(3, rows=128, slots=slots, plan=plan, stream=side)
+            c.attend(0, q, tree, slots=slots, shared=plan, out=out, stream=side)
+        del plan
+        later = [torch.full((need,), 77, dtype=torch.uint8, device="cuda") for _ in range(4)]
+        torch.cuda.synchronize()
+        assert all(bool((x == 77).all()) for x in later)
+        # weights are rounded to bf16 against another maximum, outputs once
+        assert float((out["out"].float() - want["out"].float()).abs().max()) <= 4 * 2.0 ** -8 * float(c.v.abs().max())
+        del later
