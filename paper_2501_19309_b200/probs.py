@@ -47,7 +47,7 @@ def verify_probs(target: torch.Tensor, draft: Optional[torch.Tensor], tokens: to
     (row i: of node i); tokens [B, T - 1] (int32); accept_u [B, T - 1] and sample_u [B]: uniform float32 numbers of [0, 1). parents [T] or [B, T]
     (int32, a parent before its children): trees, None: chains; ``siblings``: whether children of a node were drawn "independent" of one another or
     "distinct" (without replacement). judge_scores [B, T - 1] and tau as in ``Verifier.verify``, read by the modes that judge. num_nodes [B]: nodes of
-    each sequence of a padded batch (0: its outputs stay as they were). Returns (and takes as ``out``) a dict with "accept_len" [B],
+    each sequence of a padded batch (0: its outputs stay as they were, -1 in those that the call makes; ``commit`` leaves the sequence out by slot -1). Returns (and takes as ``out``) a dict with "accept_len" [B],
     "next_token" [B] and "path" [B, T - 1], the nodes of the accepted tokens, -1 behind them: ``cache.commit(out["accept_len"][:, None],
     out["path"][:, None])``. status: int32 [1] that becomes the first problem (a token or parent out of range) if it holds 0.
     All tensors on one device; enqueued on ``stream`` (default: the current one), where tensors that the call makes are allocated."""
@@ -66,6 +66,12 @@ def verify_probs(target: torch.Tensor, draft: Optional[torch.Tensor], tokens: to
     if out is None:
         # parts of one allocation, cut in one call: 2 us where slices take 1.4 each
         flat = tokens.new_empty((B * (M + 2),))
+        if num_nodes is not None:      # where there are no nodes nothing is written: -1, on the call's stream
+            if stream is None:
+                flat.fill_(-1)
+            else:
+                with torch.cuda.stream(stream):
+                    flat.fill_(-1)
         length, token, path = flat.unsafe_split_with_sizes((B, B, B * M))
         out = dict(accept_len=length, next_token=token, path=path.view(B, M))
         len_ptr = flat.data_ptr()

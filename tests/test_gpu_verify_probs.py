@@ -303,3 +303,19 @@ def test_weights_whose_sum_float32_does_not_hold(V, dtype, siblings):
         s["target"], s["draft"] = ((torch.rand(x.shape, generator=torch.Generator().manual_seed(seed + i)) * 3.3e38).to(L.DT[dtype]).cuda() for i, x in enumerate((s["target"], s["draft"])))
         s["accept_u"] = s["accept_u"] * 0.3 + 0.7
         check(s, parents, call(s, parents, chain=style == "chain", siblings=siblings), siblings=siblings)
+
+
+def test_outputs_of_sequences_without_nodes():
+    """Outputs that the call makes itself hold -1 there, whatever the memory held before, on whatever stream."""
+    s, parents = inputs(9, 8, 100, "f32", 4, shared=True)
+    num, want = L.ints([8, 0, 3, 8, 1, 5, 0, 8, 2]), None
+    for stream in (None, torch.cuda.Stream()):
+        for _ in range(3):
+            junk = torch.full((9 * 9,), 12345, dtype=torch.int32, device="cuda")
+            torch.cuda.synchronize()
+            del junk
+            got = call(s, parents, shared=True, num_nodes=num, stream=stream)
+            torch.cuda.synchronize()
+            check(s, parents, got, num_nodes=num)
+            for b in (1, 6):
+                assert got["accept_len"][b] == got["next_token"][b] == -1 and (got["path"][b] == -1).all()
