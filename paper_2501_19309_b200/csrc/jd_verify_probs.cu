@@ -39,7 +39,7 @@ struct ProbsParams {
   int64_t parents_stride;                  // 0: shared
   const float *accept_u, *sample_u, *judge;
   float tau;
-  int mode, resample, distinct;
+  int mode, resample, distinct;            // distinct: never of chains, whose nodes have one child
   int32_t *accept_len, *next_token, *path;
   unsigned* status;
 };
@@ -176,7 +176,8 @@ __device__ __forceinline__ Found find(double m, double goal, int lane) {
   return f;
 }
 
-template <typename T, bool kVec>
+// kDistinct apart: what is left of the draft's row costs calls that have no use for it 0.3 (chains) to 3 us (16 trees of 25), by its code and registers alone.
+template <typename T, bool kVec, bool kDistinct>
 __global__ void __launch_bounds__(kThreads, 2) verify_probs_kernel(const __grid_constant__ ProbsParams p) {
   constexpr int kW = kWide<T>, kStep = 32 * kW;        // entries of a lane and of a warp at a time
   __shared__ int s_token[kMaxNodes], s_path[kMaxNodes], s_parent[kMaxNodes];
@@ -280,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, 2) verify_probs_kernel(const __grid_
 #pragma unroll 1
             for (int j = 0; j < x.rejected; ++j) {
               w = less(w, s_rej.Q[j], s_rej.W[j], d);
-              if (p.distinct && token == s_rej.x[j]) d = 0.0;
+              if (kDistinct && token == s_rej.x[j]) d = 0.0;
             }
             ok = token >= 0 && ((p.mode != JD_MODE_JUDGE && (double)s_u[next] * x.W * d < w * x.Q) || s_judge[next]);
           }
@@ -302,7 +303,7 @@ __global__ void __launch_bounds__(kThreads, 2) verify_probs_kernel(const __grid_
             s_rej.x[x.rejected] = token;
           }
           want = ++x.rejected;
-          if (p.distinct) {
+          if (kDistinct) {
             x.Q -= d;
             x.sum_left |= x.Q < 0.5;
           }
@@ -331,7 +332,7 @@ __global__ void __launch_bounds__(kThreads, 2) verify_probs_kernel(const __grid_
     const int node = s_walk.cur;
     const T* prow = target + node * p.target_stride;
     const T* qrow = draft + node * p.draft_stride;
-    const bool sum_left = s_walk.sum_left, in_double = n > 1 || sum_left || s_walk.wide;
+    const bool sum_left = kDistinct && s_walk.sum_left, in_double = n > 1 || sum_left || s_walk.wide;
     double sum = 0.0, left = 0.0;          // of the warp; of the lane
 #pragma unroll 1
     for (int w0 = v0, i = 0; w0 < v1; w0 += p.part, ++i) {
@@ -368,12 +369,13 @@ __global__ void __launch_bounds__(kThreads, 2) verify_probs_kernel(const __grid_
           x = load_entries<T, kVec>(prow, v + kStep, w1);
           y = load_entries<T, kVec>(qrow, v + kStep, w1);
           double w[kW], of_q[kW];
-          weights_of<T, kW>(s_rej, p.distinct, n, a, d, v, w, of_q);
-          const int gone = n > 0 ? s_rej.x[n - 1] - v : -1;
+          weights_of<T, kW>(s_rej, kDistinct, n, a, d, v, w, of_q);
 #pragma unroll
-          for (int e = 0; e < kW; ++e) {
-            part += w[e];
-            if (gone != e) left += of_q[e];
+          for (int e = 0; e < kW; ++e) part += w[e];
+          if (sum_left) {
+            const int gone = s_rej.x[n - 1] - v;
+#pragma unroll
+            for (int e = 0; e < kW; ++e) left += gone == e ? 0.0 : of_q[e];
           }
         }
       }
@@ -456,7 +458,7 @@ __global__ void __launch_bounds__(kThreads, 2) verify_probs_kernel(const __grid_
   auto take_step = [&](int v) {
     const int at = v + lane * kW;
     const uint4 x = load_entries<T, kVec>(prow, at, end), y = n > 0 ? load_entries<T, kVec>(qrow, at, end) : make_uint4(0u, 0u, 0u, 0u);
-    weights_of<T, kW>(s_rej, p.distinct, n, x, y, at, w, of_q);
+    weights_of<T, kW>(s_rej, kDistinct, n, x, y, at, w, of_q);
     of_lane = 0.0;
 #pragma unroll
     for (int e = 0; e < kW; ++e) of_lane += w[e];
@@ -511,7 +513,7 @@ cudaError_t launch_probs(const ProbsParams& p, int blocks, cudaStream_t st) {
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, verify_probs_kernel<T, kVec>, p);
+  return cudaLaunchKernelEx(&cfg, p.distinct ? verify_probs_kernel<T, kVec, true> : verify_probs_kernel<T, kVec, false>, p);
 }
 
 bool on(const void* p, uintptr_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
@@ -549,7 +551,7 @@ extern "C" jd_status_t jd_verify_probs(const jd_verify_probs_args_t* a, void* cu
   p.tokens = a->tokens; p.parents = a->parents; p.num_nodes = a->num_nodes;
   p.parents_stride = a->per_seq ? a->nodes : 0;
   p.accept_u = a->accept_u; p.sample_u = a->sample_u; p.judge = a->judge_scores;
-  p.tau = a->tau; p.mode = a->mode; p.resample = a->resample; p.distinct = a->siblings == JD_SIBLINGS_DISTINCT;
+  p.tau = a->tau; p.mode = a->mode; p.resample = a->resample; p.distinct = a->siblings == JD_SIBLINGS_DISTINCT && a->parents;
   p.accept_len = a->accept_len; p.next_token = a->next_token; p.path = a->path;
   p.status = a->device_status;
   // As many blocks for a sequence as keep all sequences on the device at once
