@@ -422,8 +422,8 @@ typedef struct {
   const jd_rope_axes_t* axes; /* HOST struct; NULL: one axis */
 } jd_head_rope_args_t;
 
-/* Norms of query and key heads and their rotation in one pass; statistics and products are float32, rounded once at the end. The sum
- * of a head's squares has to stay below float32's largest number. Asynchronous on the stream; uses the current device. */
+/* Norms of query and key heads and their rotation in one pass; statistics and products are float32, rounded once at the end; angles are
+ * reduced in 64 bits and good to 2^-32 of a turn, far positions among them. The sum of a head's squares has to stay below float32's largest number. Asynchronous on the stream; uses the current device. */
 jd_status_t jd_head_rope(const jd_head_rope_args_t* args, void* cuda_stream);
 
 typedef struct {
@@ -591,8 +591,9 @@ size_t jd_cache_shared_bytes(jd_cache_t c, int32_t B, int32_t nodes);   /* 0: in
  * jd_cache_reserve or in front of it. */
 jd_status_t jd_cache_share(jd_cache_t c, const jd_shared_t* plan, const int32_t* slots, const int32_t* groups, void* cuda_stream);
 
-/* jd_cache_attend for the plan's B and slots, the shared prefixes read once. The results are the same up to float32 rounding, whatever the plan: a
- * sequence whose slot or tables the plan does not fit any more is attended to by itself. */
+/* jd_cache_attend for the plan's B and slots, the shared prefixes read once. The results are the same up to the roundings stated there, whatever the
+ * plan: a sequence whose slot or tables the plan does not fit any more, after whatever calls on the cache, is attended to by itself. (Its slot, its and its group's lengths
+ * and the prefix's last page are compared, by which every change that calls make shows; a table that was written by other hands wants a new plan.) */
 jd_status_t jd_cache_attend_shared(jd_cache_t c, const jd_attend_args_t* args, const jd_shared_t* plan, void* cuda_stream);
 
 typedef struct {

@@ -579,7 +579,8 @@ class PagedCache:
         requests behind one system prompt. groups [B]: entries with the same number are compared, None: those with the same first page. Made once for
         all layers of a step, for calls of up to ``nodes`` nodes; ``plan``: one to use again (else a new one is allocated, which waits for
         the current stream). Whether the calls share, and in which form, goes by what it costs; ``rows`` has them share whatever they can with that many
-        query rows to a block: 32, 64, 128, 256 on the tensor cores, 4, 16 else. A plan that the tables have left behind costs time, not results."""
+        query rows to a block: 32, 64, 128, 256 on the tensor cores, 4, 16 else. A plan that the tables have left behind by calls on the cache costs time, not
+        results; tables that were written otherwise want a new one."""
         B = self._batch(slots)
         if plan is None:
             plan = SharedPrefix(self, B, nodes)

@@ -107,7 +107,8 @@ constexpr int kTensorForms = 4, kSharedForms = 6;
 __host__ __device__ constexpr int form_rows(int form) { return form < kTensorForms ? 32 << form : (form == kTensorForms ? 4 : 16); }
 // The forms that a plan chooses from. A block of few rows costs a sequence's own few tokens least, one of many saves a group passes over its prefix: the
 // smallest form that takes a sequence's rows, and, where the batch has the rows for long work, twice that in the same kernel, of which the plan picks by cost.
-// A second form costs every call some 4 us (the code no longer stays in the instruction cache: 15.1 us alone, 19.2 with another beside it), a
+// A second form costs every call some 4 us (the code no longer stays in the instruction cache, and registers are spilled: 436 bytes of blocks of 128 and 256 rows of
+// 128 columns, 68 of the latter alone; 15.1 us alone, 19.2 with another beside it), a
 // wrong one up to twice the time. Of random calls with 33 to 64 rows of 128 columns the sum of times falls by 8 % with the rule, with 65 to 128 rows by 10 %. On
 // CUDA cores, whose code is short, up to 4 rows of a sequence go in blocks of 4 or of 16; with more than 128 columns the latter would take the former's
 // second block off the SM.
@@ -206,7 +207,8 @@ __device__ __forceinline__ int extent_units(const AttendParams& p, const Divisio
 }
 
 // Tokens that sequence b leaves to its group: those of the plan if slot still has them in the group's pages, else none, so that a plan which the tables
-// have left behind costs time alone. Tables change from their ends or as a whole, so lengths and the prefix's last page tell; so that the
+// have left behind costs time alone. Calls change tables from their ends or as a whole, and a page has the same place in all tables that hold it, so lengths and the
+// prefix's last page tell; so that the
 // loads are under way together, none waits for another's outcome.
 __device__ __forceinline__ int prefix_of(const AttendParams& p, int b, int slot, int ctx) {
   const int tokens = __ldcg(p.sh.entry_tokens + b), was = __ldcg(p.sh.entry_slot + b), lead = __ldcg(p.sh.entry_lead + b);

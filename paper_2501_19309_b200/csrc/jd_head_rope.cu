@@ -359,7 +359,8 @@ template <bool kHalf> __device__ __forceinline__ Place place_of(const HeadShape&
 // of a head read neighbouring words. Forward, with the weights in: y_a = r (x_a ca + x_b sb), y_b = r (x_b cb + x_a sa).
 struct __align__(16) Two { uint64_t x, y; };
 
-// An angle as a 64-bit fraction of a turn: position times frequency wraps by itself.
+// An angle as a 64-bit fraction of a turn: position times frequency wraps by itself. The frequency's turns are a float64 product, rounded to 2^-63, and its error counts
+// once for every position, as in turn_of; of the product the upper 32 bits are taken, 2^-32 of a turn. One integer product a token in place of turn_of's float64 operations.
 __device__ __forceinline__ uint64_t turn_fraction(float freq) {
   const double turns = (double)freq * 0.15915494309189533577;   // 1 / (2 pi)
   return (uint64_t)(int64_t)__double2ll_rn((turns - rint(turns)) * 18446744073709551616.0 * 0.5) * 2u;

@@ -14,8 +14,9 @@
 // another rejection at the node finds its rows in L1. The blocks' sums go into each other's shared memory by stores that count on a barrier there (a
 // cluster barrier and its fences take twice as long). The draw narrows down block, warp and part of its stretch by the sums that the pass has left, then step
 // and lane. Loops are kept small: code that a block runs once or twice is fetched line by line, and unrolled eight times over it took longer than its work
-// (16 trees of 25 drafted tokens, vocabulary 128,256: 40 us, 23 so). 64 chains of 16: 20 to 22 us, where the rows' bytes take 10; one chain of 8: 11 us, of which the
-// fetches and the first tests take 2, the pass 3, the sums' way through the cluster and the draw 3.
+// (16 trees of 25 drafted tokens, vocabulary 128,256: 40 us, 25 so; 27 with independent siblings, which are rejected more often). 64 chains of 16: 22 us, where the rows' bytes
+// take 10; one chain of 8: 11 us, of which the fetches and the first tests take 2, the pass 3, the sums' way through the cluster and the draw 3. 64 registers for two blocks
+// spill 16 (float32) to 104 bytes (bfloat16) with distinct siblings, 0 to 76 else.
 // A token of 10^-6 is to be told from its neighbour behind 10^5 others, and every launch shape is to find the same one: sums are float64, or, behind up to one rejection,
 // pairs of float32 that are off by some 2^-48 (LongSum); a pass whose sum float32 does not hold is taken again in float64.
 #include <algorithm>
